@@ -195,6 +195,116 @@ int pcr_decode_tensor(pcr_record* rec, int k, const pcr_crop* crops, int size, c
 size_t pcr_msssim_scratch_bytes(pcr_record* rec);
 int pcr_msssim(pcr_record* rec, const void* rgb_a, const void* rgb_b, void* scratch, float* dev_scores, void* stream);
 
+/* ---- From decoded pixels to a sequence model -------------------------------------------------
+ * The paper trains on batches of one size (pcr_decode_tensor).  Models that take images as sequences
+ * take every image at a size of its own instead: as a run of patches, told apart by positions on
+ * several axes (time, row, column), which turn the queries and keys of their tokens.  The calls below
+ * make the tokens out of a decode's output, the positions out of the sequences' segments, and turn
+ * queries and keys.  They hold no state: everything is the caller's DEVICE memory on the current
+ * device, work is enqueued on `stream`, and nothing is allocated, so all of them may be captured. */
+
+/* One image of a token batch: a row of a DEVICE table. */
+typedef struct {
+    int64_t offset;         /* first byte of the image's pixels in `rgb` (pcr_image_info.out_offset)  */
+    int64_t width, height;  /* of the image, 1 .. 2^20: packed RGB, 3 * width bytes per row           */
+    int64_t x0, y0, w, h;   /* the rectangle that becomes tokens                                      */
+    int64_t rows, cols;     /* patches down and across: it is resampled to cols*patch x rows*patch    */
+    int64_t flip;           /* 1: mirror the columns                                                  */
+} pcr_patch_image;
+
+/* Patch tokens of a decode's output.  Token i stands for patch l of image m, (m, l) = index[i]: the
+ * image's rectangle is resampled to cols*patch x rows*patch pixels as pcr_decode_tensor does
+ * (bilinear, half-pixel centres, the rectangle's edge pixels repeated, no low-pass filter; where a
+ * sample falls between pixels is worked out in whole numbers), normalised, (v / 255 - mean[c]) / std[c]
+ * in single precision, and cut into patches; the token is the patch's 3 * patch * patch values, channel
+ * after channel, row after row, rounded once to dtype.  Patches are numbered in blocks of merge x merge,
+ * blocks row by row and patches row by row in a block (merge = 1: row by row).
+ *   rgb       : DEVICE, 4-byte aligned, rgb_bytes bytes.
+ *   images    : DEVICE, n_images rows.   index : DEVICE, n_tokens pairs of int32, 8-byte aligned.
+ *   patch     : 1..32.   merge : 1..64.   mean, std : HOST, three floats each, std > 0.
+ *   tokens    : DEVICE, n_tokens x (3 * patch * patch) elements of dtype.
+ * A token whose entry names no image, no patch of it, or an image that does not lie inside `rgb` (or a
+ * rectangle not inside its image, or rows or cols that are no multiples of merge, or a resampled side
+ * over 2^20) is all zeros: tables are on the device and are not read by the host.
+ * Errors: PCR_E_ARG, PCR_E_CUDA. */
+int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* images, int n_images, const int32_t* index,
+                     int64_t n_tokens, int patch, int merge, const float* mean, const float* std, int dtype, void* tokens,
+                     void* stream);
+
+/* Positions of packed sequences of text and of image or clip grids, on three axes (time, height,
+ * width).  segments: DEVICE, n_segments rows of four int32 (t, h, w, sequence), 16-byte aligned:
+ * t tokens of text where h or w is 0, else a grid of t x h x w tokens (frame after frame, row after row;
+ * with merge > 1 in blocks of merge x merge like the patches, where h and w are multiples of it).  The
+ * rows of a sequence stand together.  A sequence's positions begin at 0; a text token takes the next
+ * position on all axes; token (f, y, x) of a grid takes base + (f * time_step, y, x), where base is the
+ * position that comes next; what follows a grid goes on behind the largest position in it.
+ *   n_tokens   : columns of `positions`; tokens of further segments are left out, and columns behind the
+ *                last token are left as they are (PCR_POSITIONS_ZERO_TAIL: set to 0).
+ *   flags      : PCR_POSITIONS_RESTART begins at 0 with every segment (an image encoder's positions).
+ *   positions  : DEVICE int32, three rows, axis_stride >= n_tokens elements apart.
+ *   next       : DEVICE int32, n_sequences: the position with which a sequence goes on (for the tokens
+ *                that a model adds one by one); 0 for a sequence without segments.
+ *   scratch    : DEVICE, pcr_token_positions_scratch_bytes(n_segments) bytes, 8-byte aligned.
+ * Counts below zero are taken as 0; positions are kept modulo 2^32.   time_step : 0 .. 2^20.
+ * Errors: PCR_E_ARG, PCR_E_CUDA. */
+#define PCR_POSITIONS_RESTART 1
+#define PCR_POSITIONS_ZERO_TAIL 2
+size_t pcr_token_positions_scratch_bytes(int n_segments);
+int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_tokens, int n_sequences, int merge, int time_step,
+                        int flags, int32_t* positions, int64_t axis_stride, int32_t* next, void* scratch, void* stream);
+
+/* Queries and keys.  Element (b, t, h, j) of an operand lies at b * stride[0] + t * stride[1] +
+ * h * stride[2] + j; a head's elements stand side by side. */
+#define PCR_F64 3
+typedef struct {
+    const void* x;                 /* input                                                            */
+    void* y;                       /* output; backward: the gradient of x.  x itself (or dy itself) with the
+                                      same strides, or memory that shares no element with any operand  */
+    const void* dy;                /* backward: the gradient of the forward's output                   */
+    const void* weight;            /* norm: head_dim weights; NULL = ones                              */
+    void* dweight;                 /* backward: gradient of weight, same type; NULL = not wanted       */
+    int64_t x_stride[3], y_stride[3], dy_stride[3];  /* in elements: batch, token, head                */
+    int32_t heads;                 /* 0: this operand is left out                                      */
+    int32_t rsvd;
+} pcr_heads;
+typedef struct {
+    pcr_heads q, k;
+    const int32_t* positions;      /* DEVICE; axis a of token (b, t) at a, b, t times these strides    */
+    int64_t position_stride[3];
+    const void* inv_freq;          /* DEVICE, rot_dim / 2 frequencies, float or double (freq_dtype)    */
+    const int32_t* axes;           /* DEVICE, rot_dim / 2: the axis that turns pair i; an axis outside
+                                      0 .. n_axes - 1 leaves the pair as it is                         */
+    int64_t batch, tokens;         /* tokens of each sequence; batch * tokens < 2^31                   */
+    int32_t n_axes;                /* 1..4 */
+    int32_t head_dim, rot_dim;     /* head_dim 1..512; the first rot_dim elements are turned (even, may be 0) */
+    int32_t interleaved;           /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2 i, 2 i + 1)           */
+    int32_t inverse;               /* pcr_rotate: 1 = by the negative angle, which is also its gradient */
+    int32_t dtype;                 /* of x, y, dy: PCR_F16, PCR_F32, PCR_BF16                          */
+    int32_t freq_dtype;            /* PCR_F32 or PCR_F64                                               */
+    int32_t weight_dtype;          /* dtype or PCR_F32                                                 */
+    float eps;                     /* >= 0 */
+    int32_t rsvd;
+} pcr_turn_args;
+
+/* Rotation of queries and keys, one launch: pair (a, b) becomes (a cos - b sin, a sin + b cos) with the
+ * angle positions[axes[i]] * inv_freq[i], whose whole turns are taken off in double precision (far
+ * positions lose nothing); single precision from there, one rounding to dtype.  Any strides and
+ * alignments of whole elements; in place is allowed.
+ * Errors: PCR_E_ARG (also for an output that overlaps itself), PCR_E_CUDA. */
+int pcr_rotate(const pcr_turn_args* args, void* stream);
+
+/* The same behind a root-mean-square norm of every head, in one pass: x * weight / sqrt(mean(x^2) + eps),
+ * then the rotation; sums and products in single precision, one rounding.  inverse has to be 0. */
+int pcr_norm_rotate(const pcr_turn_args* args, void* stream);
+
+/* Its backward pass from x and dy (nothing is kept from the forward pass): y = gradient of x, dweight =
+ * gradient of the weights, summed over all rows in single precision and always in the same order.
+ *   scratch : DEVICE, pcr_norm_rotate_scratch_bytes(args) bytes (for the same args on the same device;
+ *             0 for args that the call would refuse), 4-byte aligned; not needed without a dweight.
+ * y may be x or dy. */
+size_t pcr_norm_rotate_scratch_bytes(const pcr_turn_args* args);
+int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* stream);
+
 /* Chroma upsampling of the decodes that follow (pcr_decode, pcr_decode_more).  The paper hands
  * its reassembled files to stock decoders (Section 5) and does not name the filter.
  *   PCR_UPSAMPLE_REPLICATE (default): pixel (x, y) takes chroma sample (x >> 1, y >> 1).

@@ -4,3 +4,5 @@ from .binding import (ImageInfo, PcrError, pcr_close, pcr_coeffs, pcr_decode, pc
                       pcr_out_bytes, pcr_prefix_bytes, pcr_status, strerror, pcr_get_scan, pcr_set_profiling,
                       pcr_get_profile, pcr_pixels_noalloc, pcr_decode_more, pcr_release_cached_memory, pcr_decode_tensor, pcr_msssim, pcr_msssim_scratch_bytes, pcr_set_upsampling)
 from .record import Decoder  # noqa: F401
+from .tokens import (PatchPlan, norm_rotate, norm_rotate_backward, patch_plan, patch_tokens, rotary_axes, rotate,  # noqa: F401
+                     token_positions)

@@ -18,7 +18,9 @@ EXPORTS = ("pcr_open", "pcr_num_images", "pcr_num_groups", "pcr_get_image", "pcr
            "pcr_decode", "pcr_evict", "pcr_status", "pcr_coeffs", "pcr_image_blocks", "pcr_launch_count",
            "pcr_strerror", "pcr_close", "pcr_get_scan", "pcr_set_profiling", "pcr_get_profile",
            "pcr_pixels_noalloc", "pcr_decode_more", "pcr_release_cached_memory", "pcr_decode_tensor", "pcr_msssim", "pcr_msssim_scratch_bytes", "pcr_set_upsampling",
-           "pcr_selftest_bounded_wait", "pcr_get_sampling", "pcr_set_record_cache", "pcr_get_images")
+           "pcr_selftest_bounded_wait", "pcr_get_sampling", "pcr_set_record_cache", "pcr_get_images",
+           "pcr_patch_tokens", "pcr_token_positions", "pcr_token_positions_scratch_bytes", "pcr_rotate", "pcr_norm_rotate",
+           "pcr_norm_rotate_backward", "pcr_norm_rotate_scratch_bytes")
 
 
 class ImageInfo(C.Structure):
@@ -79,6 +81,15 @@ def lib():
         L.pcr_selftest_bounded_wait.argtypes = [C.POINTER(C.c_int)]
         L.pcr_set_record_cache.argtypes = [C.c_size_t]
         L.pcr_get_sampling.argtypes = [vp, C.POINTER(C.c_int), C.POINTER(C.c_int), C.POINTER(C.c_int)]
+        L.pcr_patch_tokens.argtypes = [vp, C.c_size_t, vp, C.c_int, vp, C.c_int64, C.c_int, C.c_int, C.c_char_p, C.c_char_p, C.c_int, vp, vp]
+        L.pcr_token_positions_scratch_bytes.restype = C.c_size_t
+        L.pcr_token_positions_scratch_bytes.argtypes = [C.c_int]
+        L.pcr_token_positions.argtypes = [vp, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, vp, C.c_int64, vp, vp, vp]
+        L.pcr_rotate.argtypes = [C.c_char_p, vp]                  # (a pcr_turn_args, packed by the caller)
+        L.pcr_norm_rotate.argtypes = [C.c_char_p, vp]
+        L.pcr_norm_rotate_scratch_bytes.restype = C.c_size_t
+        L.pcr_norm_rotate_scratch_bytes.argtypes = [C.c_char_p]
+        L.pcr_norm_rotate_backward.argtypes = [C.c_char_p, vp, vp]
         L.pcr_launch_count.restype = C.c_uint64
         L.pcr_launch_count.argtypes = []
         L.pcr_strerror.restype = C.c_char_p
@@ -147,7 +158,8 @@ def pcr_decode_more(handle: int, k: int, out_dev_ptr: int, stream: int = 0) -> N
     _chk(lib().pcr_decode_more(handle, k, out_dev_ptr, stream), "pcr_decode_more")
 
 
-PCR_F16, PCR_F32, PCR_BF16 = 0, 1, 2
+PCR_F16, PCR_F32, PCR_BF16, PCR_F64 = 0, 1, 2, 3
+PCR_POSITIONS_RESTART, PCR_POSITIONS_ZERO_TAIL = 1, 2
 
 
 def pcr_decode_tensor(handle: int, k: int, crops_host_ptr: int, size: int, mean_host_ptr: int, std_host_ptr: int,

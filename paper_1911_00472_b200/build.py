@@ -8,8 +8,9 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpcr_b200.so")
-SOURCES = ["pcr_lib.cu"]
-HEADERS = ["pcr_types.h", "pcr_entropy.cuh", "pcr_long.cuh", "pcr_pixels.cuh", "pcr_refine.cuh", "pcr_sequential.cuh", "pcr_msssim.cuh"]
+SOURCES = ["pcr_lib.cu", "pcr_tokens.cu"]
+HEADERS = ["pcr_types.h", "pcr_entropy.cuh", "pcr_long.cuh", "pcr_pixels.cuh", "pcr_refine.cuh", "pcr_sequential.cuh", "pcr_msssim.cuh",
+           "pcr_heads.cuh", "pcr_launches.h", "pcr_patches.cuh"]
 
 
 def _nvcc() -> str:
@@ -32,7 +33,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-t", "0",
            "-shared", "-Xcompiler", "-fPIC", "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]

@@ -24,6 +24,7 @@
 
 #include "../../include/pcr.h"
 #include "pcr_entropy.cuh"
+#include "pcr_launches.h"
 #include "pcr_long.cuh"
 #include "pcr_msssim.cuh"
 #include "pcr_pixels.cuh"
@@ -33,7 +34,7 @@
 
 using namespace pcr;
 
-static std::atomic<uint64_t> g_launches{0};
+namespace pcr { std::atomic<uint64_t> g_launches{0}; }
 
 // Device buffers of closed records are kept for the next pcr_open instead of going back to the
 // driver: cudaMalloc and cudaFree cost milliseconds and cudaFree waits for the whole device, which

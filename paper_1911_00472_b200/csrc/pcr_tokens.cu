@@ -1,0 +1,257 @@
+// Host side of the operators between decoded pixels and a sequence model (see include/pcr.h): patch tokens, token
+// positions, queries and keys turned by positions.  Every call checks its arguments, enqueues kernels on the caller's
+// stream and returns; nothing is allocated and nothing is kept between calls.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdlib.h>
+
+#include <algorithm>
+
+#include "../../include/pcr.h"
+#include "pcr_heads.cuh"
+#include "pcr_launches.h"
+#include "pcr_patches.cuh"
+
+using namespace pcr;
+
+namespace {
+
+int sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return 148;
+    }
+    return n;
+}
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+size_t size_of(int dtype) { return dtype == PCR_F32 ? 4 : 2; }
+
+int finish() { return cudaGetLastError() == cudaSuccess ? PCR_OK : PCR_E_CUDA; }
+
+// Whether two elements of a strided output can be one and the same: sizes and strides sorted, each stride has to step
+// over all that the smaller ones reach.
+bool overlaps_itself(const int64_t (&stride)[3], int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
+    const int64_t size[3] = {batch, tokens, heads};
+    auto far = [&](int i) { const __int128 s = stride[i]; return s < 0 ? -s : s; };
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return far(a) < far(b); });
+    __int128 reach = dim - 1;
+    for (int i : order) {
+        if (size[i] <= 1) continue;
+        if (far(i) <= reach) return true;
+        reach += (size[i] - 1) * far(i);
+    }
+    return false;
+}
+
+int check_heads(const pcr_turn_args& a, bool norm, bool back) {
+    if (a.dtype != PCR_F16 && a.dtype != PCR_F32 && a.dtype != PCR_BF16) return PCR_E_ARG;
+    if (a.batch < 0 || a.tokens < 0 || a.batch > INT32_MAX || a.tokens > INT32_MAX || a.batch * a.tokens > INT32_MAX) return PCR_E_ARG;
+    if (a.head_dim < 1 || a.head_dim > kMaxHeadDim || a.rot_dim < 0 || a.rot_dim > a.head_dim || a.rot_dim % 2) return PCR_E_ARG;
+    if (a.n_axes < 1 || a.n_axes > kMaxAxes || (a.interleaved & ~1) || (a.inverse & ~1)) return PCR_E_ARG;
+    if (a.freq_dtype != PCR_F32 && a.freq_dtype != PCR_F64) return PCR_E_ARG;
+    if (norm && (!(a.eps >= 0.f) || isinf(a.eps) || a.inverse || (a.weight_dtype != PCR_F32 && a.weight_dtype != a.dtype))) return PCR_E_ARG;
+    if (a.q.heads < 0 || a.k.heads < 0 || a.q.heads > 65535 || a.k.heads > 65535 || a.q.heads + a.k.heads > 65535) return PCR_E_ARG;
+    const size_t es = size_of(a.dtype), ws = size_of(a.weight_dtype);
+    const bool any = a.batch * a.tokens > 0;
+    if (any && (!a.positions || !aligned(a.positions, 4))) return PCR_E_ARG;
+    if (any && a.rot_dim > 0 && (!a.inv_freq || !a.axes || !aligned(a.inv_freq, a.freq_dtype == PCR_F64 ? 8 : 4) || !aligned(a.axes, 4))) return PCR_E_ARG;
+    for (const pcr_heads* h : {&a.q, &a.k}) {
+        if (norm && (!aligned(h->weight, ws) || (back && (!aligned(h->dweight, ws) || (h->dweight && !h->weight))))) return PCR_E_ARG;
+        if (!any || h->heads == 0) continue;
+        if (!h->x || !h->y || !aligned(h->x, es) || !aligned(h->y, es) || (back && (!h->dy || !aligned(h->dy, es)))) return PCR_E_ARG;
+        if (overlaps_itself(h->y_stride, a.batch, a.tokens, h->heads, a.head_dim)) return PCR_E_ARG;
+    }
+    return PCR_OK;
+}
+
+// Vectors of `v` elements: whether every row starts on one and the pairs fall into whole ones.
+bool fits(const pcr_turn_args& a, bool back, int v) {
+    if (a.head_dim % (2 * v) || a.rot_dim % (2 * v) || a.head_dim / (2 * v) > 32) return false;
+    const size_t bytes = v * size_of(a.dtype);
+    for (const pcr_heads* h : {&a.q, &a.k}) {
+        if (h->heads == 0) continue;
+        if (!aligned(h->x, bytes) || !aligned(h->y, bytes) || (back && !aligned(h->dy, bytes))) return false;
+        const int64_t size[3] = {a.batch, a.tokens, h->heads};
+        for (int i = 0; i < 3; ++i) {
+            if (size[i] <= 1) continue;
+            if (h->x_stride[i] % v || h->y_stride[i] % v || (back && h->dy_stride[i] % v)) return false;
+        }
+    }
+    return true;
+}
+
+// How a call is cut: vectors of `v` pairs (0: value by value), `per` heads of a token to a thread, CTAs.
+struct Cut { int v, per, slots[2]; unsigned groups; };
+
+Cut cut_of(const pcr_turn_args& a, bool back) {
+    Cut c = {0, 1, {0, 0}, 1};
+    for (int v : {8, 4, 2})
+        if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
+    const int64_t n = a.batch * a.tokens, heads = a.q.heads + a.k.heads;
+    const int rows = c.v ? 32 / (a.head_dim / (2 * c.v)) : 1;       // tokens of a warp
+    const int64_t warps = std::max<int64_t>((n + rows - 1) / rows, 1);
+    const int64_t want = (int64_t)sm_count() * 32;                  // warps that fill the GPU
+    const int64_t slots = std::min<int64_t>((want + warps - 1) / warps, std::max<int64_t>(heads, 1));
+    c.per = (int)std::max<int64_t>((heads + slots - 1) / slots, 1);
+    c.slots[0] = (a.q.heads + c.per - 1) / c.per;
+    c.slots[1] = (a.k.heads + c.per - 1) / c.per;
+    constexpr int kWarps = kHeadThreads / 32;
+    int64_t groups = (warps + kWarps - 1) / kWarps;
+    if (back) groups = std::min<int64_t>(groups, std::max<int64_t>((int64_t)sm_count() * 8 / std::max(c.slots[0] + c.slots[1], 1), 1));
+    c.groups = (unsigned)groups;
+    return c;
+}
+
+void fill(HeadArgs& A, const pcr_turn_args& a, const Cut& c) {
+    const pcr_heads* from[2] = {&a.q, &a.k};
+    for (int i = 0; i < 2; ++i) {
+        HeadBlock& H = A.part[i];
+        const pcr_heads& h = *from[i];
+        H.x = h.x; H.y = h.y; H.g = h.dy; H.weight = h.weight; H.partial = nullptr;
+        for (int j = 0; j < 3; ++j) { H.xs[j] = h.x_stride[j]; H.ys[j] = h.y_stride[j]; H.gs[j] = h.dy_stride[j]; A.ps[j] = a.position_stride[j]; }
+        H.heads = h.heads; H.slots = c.slots[i];
+    }
+    A.positions = a.positions; A.inv_freq = a.inv_freq; A.axes = a.axes;
+    A.tokens = (uint32_t)(a.batch * a.tokens); A.seq = (uint32_t)std::max<int64_t>(a.tokens, 1);
+    A.n_axes = a.n_axes; A.freq64 = a.freq_dtype == PCR_F64; A.weight32 = a.weight_dtype == PCR_F32; A.inverse = a.inverse;
+    A.dim = a.head_dim; A.rot = a.rot_dim; A.chunks = c.v ? a.head_dim / (2 * c.v) : 32; A.per = c.per;
+    A.eps = a.eps; A.inv_dim = 1.f / (float)a.head_dim;
+}
+
+template <typename T, int kMode, bool kNext>
+void launch(const HeadArgs& A, const Cut& c, cudaStream_t st) {
+    const dim3 grid(c.groups, (unsigned)(c.slots[0] + c.slots[1]));
+    if (sizeof(T) == 2 && c.v == 8) heads_kernel<T, sizeof(T) == 2 ? 8 : 4, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    else if (c.v == 4) heads_kernel<T, 4, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    else if (c.v == 2) heads_kernel<T, 2, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    else heads_any_kernel<T, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    ++g_launches;
+}
+
+template <int kMode>
+void launch_mode(const HeadArgs& A, const Cut& c, int dtype, bool next, cudaStream_t st) {
+    if (dtype == PCR_F16) { if (next) launch<__half, kMode, true>(A, c, st); else launch<__half, kMode, false>(A, c, st); }
+    else if (dtype == PCR_BF16) { if (next) launch<__nv_bfloat16, kMode, true>(A, c, st); else launch<__nv_bfloat16, kMode, false>(A, c, st); }
+    else { if (next) launch<float, kMode, true>(A, c, st); else launch<float, kMode, false>(A, c, st); }
+}
+
+bool nothing(const pcr_turn_args& a) { return a.batch * a.tokens == 0 || a.q.heads + a.k.heads == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int pcr_rotate(const pcr_turn_args* args, void* stream) {
+    if (!args) return PCR_E_ARG;
+    if (int rc = check_heads(*args, false, false)) return rc;
+    if (nothing(*args)) return PCR_OK;
+    const Cut c = cut_of(*args, false);
+    HeadArgs A;
+    fill(A, *args, c);
+    launch_mode<kTurn>(A, c, args->dtype, args->interleaved != 0, static_cast<cudaStream_t>(stream));
+    return finish();
+}
+
+int pcr_norm_rotate(const pcr_turn_args* args, void* stream) {
+    if (!args) return PCR_E_ARG;
+    if (int rc = check_heads(*args, true, false)) return rc;
+    if (nothing(*args)) return PCR_OK;
+    const Cut c = cut_of(*args, false);
+    HeadArgs A;
+    fill(A, *args, c);
+    launch_mode<kNormTurn>(A, c, args->dtype, args->interleaved != 0, static_cast<cudaStream_t>(stream));
+    return finish();
+}
+
+size_t pcr_norm_rotate_scratch_bytes(const pcr_turn_args* args) {
+    if (!args || check_heads(*args, true, true) != PCR_OK || nothing(*args)) return 0;
+    const Cut c = cut_of(*args, true);
+    return (size_t)(c.slots[0] + c.slots[1]) * c.groups * args->head_dim * sizeof(float);
+}
+
+int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* stream) {
+    if (!args) return PCR_E_ARG;
+    if (int rc = check_heads(*args, true, true)) return rc;
+    const bool sums = args->q.dweight || args->k.dweight;
+    if (sums && !nothing(*args) && (!scratch || !aligned(scratch, 4))) return PCR_E_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    WeightSums S = {{nullptr, nullptr}, {args->q.dweight, args->k.dweight}, {0, 0}, args->head_dim, args->weight_dtype == PCR_F32};
+    if (!nothing(*args)) {
+        const Cut c = cut_of(*args, true);
+        HeadArgs A;
+        fill(A, *args, c);
+        float* at = static_cast<float*>(scratch);
+        for (int i = 0; i < 2; ++i) {
+            if (S.dw[i]) { A.part[i].partial = at; S.partial[i] = at; S.rows[i] = (int32_t)(c.slots[i] * c.groups); }
+            if (at) at += (size_t)c.slots[i] * c.groups * args->head_dim;
+        }
+        launch_mode<kNormTurnBack>(A, c, args->dtype, args->interleaved != 0, st);
+    }
+    if (sums) {
+        const dim3 grid((unsigned)((args->head_dim + kSumCols - 1) / kSumCols), 2);
+        if (args->dtype == PCR_F16) weight_sums_kernel<__half><<<grid, kSumThreads, 0, st>>>(S);
+        else if (args->dtype == PCR_BF16) weight_sums_kernel<__nv_bfloat16><<<grid, kSumThreads, 0, st>>>(S);
+        else weight_sums_kernel<float><<<grid, kSumThreads, 0, st>>>(S);
+        ++g_launches;
+    }
+    return finish();
+}
+
+int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* images, int n_images, const int32_t* index,
+                     int64_t n_tokens, int patch, int merge, const float* mean, const float* std_, int dtype, void* tokens, void* stream) {
+    static_assert(sizeof(pcr_patch_image) == sizeof(PatchImage), "pcr_patch_image and PatchImage have the same layout");
+    if (n_images < 0 || n_tokens < 0 || n_tokens > INT32_MAX || patch < 1 || patch > kMaxPatch || merge < 1 || merge > 64) return PCR_E_ARG;
+    if (!mean || !std_ || (dtype != PCR_F16 && dtype != PCR_F32 && dtype != PCR_BF16)) return PCR_E_ARG;
+    for (int c = 0; c < 3; ++c)
+        if (!(std_[c] > 0.f) || !(fabsf(mean[c]) <= 3.0e38f) || isinf(std_[c])) return PCR_E_ARG;
+    if (n_tokens == 0) return PCR_OK;
+    if ((n_images > 0 && (!rgb || !images)) || !index || !tokens) return PCR_E_ARG;
+    if (!aligned(rgb, 4) || !aligned(images, 8) || !aligned(index, 8) || !aligned(tokens, size_of(dtype))) return PCR_E_ARG;
+    PatchArgs A;
+    A.rgb = static_cast<const uint8_t*>(rgb); A.images = reinterpret_cast<const PatchImage*>(images);
+    A.index = reinterpret_cast<const int2*>(index); A.out = tokens; A.rgb_bytes = rgb_bytes;
+    A.n_tokens = (uint32_t)n_tokens; A.n_images = n_images; A.patch = patch; A.merge = merge;
+    for (int c = 0; c < 3; ++c) { A.scale[c] = 1.f / (255.f * std_[c]); A.shift[c] = -mean[c] / std_[c]; }
+    const int each = 32 / patch;
+    const size_t own = ((size_t)each * 3 * patch * patch * size_of(dtype) + 15) / 16 * 16;
+    const int64_t warps = (n_tokens + each - 1) / each;
+    const unsigned grid = (unsigned)((warps + kPatchWarps - 1) / kPatchWarps);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == PCR_F16) patch_tokens_kernel<__half><<<grid, 32 * kPatchWarps, own * kPatchWarps, st>>>(A);
+    else if (dtype == PCR_BF16) patch_tokens_kernel<__nv_bfloat16><<<grid, 32 * kPatchWarps, own * kPatchWarps, st>>>(A);
+    else patch_tokens_kernel<float><<<grid, 32 * kPatchWarps, own * kPatchWarps, st>>>(A);
+    ++g_launches;
+    return finish();
+}
+
+size_t pcr_token_positions_scratch_bytes(int n_segments) { return n_segments < 0 ? 0 : ((size_t)n_segments + 1) * 12 + 16; }
+
+int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_tokens, int n_sequences, int merge, int time_step,
+                        int flags, int32_t* positions, int64_t axis_stride, int32_t* next, void* scratch, void* stream) {
+    if (n_segments < 0 || n_sequences < 0 || n_tokens < 0 || n_tokens > INT32_MAX || merge < 1 || merge > 64) return PCR_E_ARG;
+    if (time_step < 0 || time_step > (1 << 20) || (flags & ~(PCR_POSITIONS_RESTART | PCR_POSITIONS_ZERO_TAIL))) return PCR_E_ARG;
+    if ((n_segments > 0 && !segments) || (n_tokens > 0 && !positions) || (n_sequences > 0 && !next) || !scratch) return PCR_E_ARG;
+    if (!aligned(segments, 16) || !aligned(positions, 4) || !aligned(next, 4) || !aligned(scratch, 8)) return PCR_E_ARG;
+    if (n_tokens > 0 && axis_stride < n_tokens) return PCR_E_ARG;
+    PositionArgs A;
+    A.segments = reinterpret_cast<const int4*>(segments);
+    A.starts = static_cast<int64_t*>(scratch);
+    A.bases = reinterpret_cast<int32_t*>(A.starts + n_segments + 1);
+    A.positions = positions; A.next = next; A.stride = axis_stride; A.n_tokens = (uint32_t)n_tokens;
+    A.n_segments = n_segments; A.n_sequences = n_sequences; A.merge = merge; A.time_step = time_step;
+    A.restart = (flags & PCR_POSITIONS_RESTART) != 0; A.zero_tail = (flags & PCR_POSITIONS_ZERO_TAIL) != 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    position_scan_kernel<<<1, kScanThreads, 0, st>>>(A);
+    ++g_launches;
+    if (n_tokens > 0) {
+        position_fill_kernel<<<(unsigned)((n_tokens + kFillThreads - 1) / kFillThreads), kFillThreads, 0, st>>>(A);
+        ++g_launches;
+    }
+    return finish();
+}
+
+}  // extern "C"

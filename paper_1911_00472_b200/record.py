@@ -9,6 +9,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from . import tokens as T
 
 
 class Decoder:
@@ -91,6 +92,18 @@ class Decoder:
                                 codes[dtype], rgb.data_ptr(), tensor.data_ptr(),
                                 s.cuda_stream)
         return tensor
+
+    def patch_plan(self, patch: int, merge: int = 1, crops=None, grids=None) -> T.PatchPlan:
+        """What this record's images become as patch tokens, each at its own size (see tokens.patch_plan)."""
+        return T.patch_plan(self.info, patch, merge=merge, crops=crops, grids=grids, device=self.device)
+
+    def decode_patches(self, k: int, plan: T.PatchPlan, mean, std, dtype: torch.dtype = torch.bfloat16,
+                       rgb: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                       stream: torch.cuda.Stream | None = None) -> torch.Tensor:
+        """Decode at fidelity k to the patch tokens of `plan`, (tokens, 3 * patch * patch): pcr_decode, then
+        pcr_patch_tokens on the same stream."""
+        rgb = self.decode(k, rgb, stream)
+        return T.patch_tokens(rgb, plan.images, plan.index, plan.patch, mean, std, merge=plan.merge, dtype=dtype, out=out, stream=stream)
 
     def msssim(self, rgb_a: torch.Tensor, rgb_b: torch.Tensor, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
         """Multi-scale SSIM of every image between two decodes of this record: (N,) float32 on the

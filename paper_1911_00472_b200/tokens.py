@@ -1,0 +1,343 @@
+"""From decoded pixels to a sequence model: patch tokens, positions on several axes, and the queries and keys they turn.
+
+torch is used for memory and streams only; all arithmetic happens behind the C ABI (include/pcr.h: pcr_patch_tokens,
+pcr_token_positions, pcr_rotate, pcr_norm_rotate, pcr_norm_rotate_backward).  Nothing is kept between calls and nothing
+waits, so every call may be captured into a graph.  Gradients are calls of their own (rotate with inverse=True,
+norm_rotate_backward): operands that autograd follows are refused, not silently cut off.
+
+Work goes to `stream` (default: torch's current stream of the operands' device); what a call allocates belongs to it.
+"""
+from __future__ import annotations
+
+import contextlib
+import struct
+from typing import NamedTuple
+
+import numpy as np
+import torch
+
+from . import binding as B
+
+_CODES = {torch.float16: B.PCR_F16, torch.float32: B.PCR_F32, torch.bfloat16: B.PCR_BF16}
+_FREQ_CODES = {torch.float32: B.PCR_F32, torch.float64: B.PCR_F64}
+_TURN_ARGS = struct.Struct("<5Q9q2i5Q9q2iQ3qQQqq8ifi")         # pcr_turn_args
+_NO_HEADS = (0,) * 16
+
+
+@contextlib.contextmanager
+def _switched(device, stream):
+    with torch.cuda.device(device):
+        if stream is None:
+            yield
+        else:
+            with torch.cuda.stream(stream):
+                yield
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on(device: torch.device, stream):
+    """The context in which a call allocates and launches: the operands' device, and `stream` where one is given."""
+    if device.type != "cuda":
+        raise ValueError("operands have to be on a CUDA device")
+    if stream is None and torch.cuda.current_device() == device.index:
+        return _HERE
+    if stream is not None and stream.device != device:
+        raise ValueError("the stream belongs to another device than the operands")
+    return _switched(device, stream)
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all operands have to be on one device")
+
+
+def _no_autograd(*tensors):
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
+
+
+# ---- queries and keys ---------------------------------------------------------------------------------------------------
+
+
+def _strides(t):
+    return t.stride()[:-1] if t.dim() == 4 else (0,) + t.stride()[:-1]
+
+
+def _operand(t, like, name):
+    """Checks one query- or key-shaped tensor against the queries."""
+    if t.dim() != like.dim() or t.shape[:-2] != like.shape[:-2] or t.shape[-1] != like.shape[-1] or t.dtype != like.dtype:
+        raise ValueError(f"{name} must have the tokens, head size and dtype of the queries")
+
+
+def _rows(t):
+    """The tensor itself, or a copy where the elements of a head do not stand side by side."""
+    return t if t is None or t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+def _heads(x, y, dy, weight, dweight):
+    return (x.data_ptr(), y.data_ptr(), 0 if dy is None else dy.data_ptr(), 0 if weight is None else weight.data_ptr(),
+            0 if dweight is None else dweight.data_ptr(), *_strides(x), *_strides(y), *((0, 0, 0) if dy is None else _strides(dy)),
+            x.shape[-2], 0)
+
+
+def _turn_args(q, k, heads_q, heads_k, positions, inv_freq, axes, interleaved, inverse, weights, eps):
+    lead, rot = q.shape[:-2], 2 * inv_freq.numel()
+    if positions.dtype != torch.int32 or positions.shape[1:] != lead:
+        raise ValueError("positions must be int32 with shape (axes, *tokens)")
+    if inv_freq.dtype not in _FREQ_CODES or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous float32 or float64 vector")
+    if axes.dtype != torch.int32 or axes.shape != inv_freq.shape or not axes.is_contiguous():
+        raise ValueError("axes must be a contiguous int32 vector as long as inv_freq")
+    weight_type = None
+    for w in weights:
+        if w is None:
+            continue
+        if w.shape != q.shape[-1:] or not w.is_contiguous() or w.dtype not in (q.dtype, torch.float32) or weight_type not in (None, w.dtype):
+            raise ValueError("weights must be contiguous vectors of the head size, of the operands' type or float32, both alike")
+        weight_type = w.dtype
+    _same_device(q.device, k, positions, inv_freq, axes, *weights)
+    ps = positions.stride()
+    batch, ps = (lead[0], ps) if q.dim() == 4 else (1, (ps[0], 0, ps[1]))
+    return _TURN_ARGS.pack(*heads_q, *heads_k, positions.data_ptr(), *ps, inv_freq.data_ptr(), axes.data_ptr(), batch, lead[-1],
+                           positions.shape[0], q.shape[-1], rot, bool(interleaved), bool(inverse), _CODES[q.dtype],
+                           _FREQ_CODES[inv_freq.dtype], _CODES[weight_type or q.dtype], eps, 0)
+
+
+def _check_queries(q, k):
+    if q.dim() not in (3, 4) or q.dtype not in _CODES:
+        raise ValueError("queries must be (tokens, heads, size) or (batch, tokens, heads, size) of float16, bfloat16 or float32")
+    if k is not None:
+        _operand(k, q, "k")
+
+
+def _outputs(q, k, out):
+    if out is None:
+        return torch.empty_like(q, memory_format=torch.contiguous_format), None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
+    for o, x in zip(out, (q, k), strict=True):
+        if (o is None) != (x is None):
+            raise ValueError("out must have an output for each operand")
+        if x is not None:
+            if o.shape != x.shape:
+                raise ValueError("out must have the shapes of the operands")
+            _operand(o, q, "out")
+            if o.shape[-1] > 1 and o.stride(-1) != 1:
+                raise ValueError("the elements of a head of out must stand side by side")
+            _same_device(q.device, o)
+    return out
+
+
+def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False, out=None, stream=None):
+    """Queries and keys turned by the positions of their tokens.
+
+    q, k      (tokens, heads, size) or (batch, tokens, heads, size) of any strides (slices of one projection's output);
+              only where a head's elements do not stand side by side are they copied first; k may be None or have
+              another number of heads
+    positions (n_axes, *tokens) int32, any strides (expanded batches too)
+    inv_freq, axes   frequency and axis of every pair of elements (rotary_axes makes them); the first 2 * len(inv_freq)
+              elements of a head are turned, the others copied
+    interleaved      pairs (2 i, 2 i + 1) in place of (i, i + size / 2)
+    inverse   by the negative angle: the gradient of the forward call
+    out       (q, k) to write to, the operands themselves allowed
+    """
+    _check_queries(q, k)
+    _no_autograd(q, k)
+    with _on(q.device, stream):
+        q, k = _rows(q), _rows(k)
+        y, z = _outputs(q, k, out)
+        args = _turn_args(q, k, _heads(q, y, None, None, None), _NO_HEADS if k is None else _heads(k, z, None, None, None),
+                          positions, inv_freq, axes, interleaved, inverse, (), 0.0)
+        B._chk(B.lib().pcr_rotate(args, torch.cuda.current_stream(q.device).cuda_stream), "pcr_rotate")
+    return y, z
+
+
+def norm_rotate(q, k, q_weight, k_weight, positions, inv_freq, axes, *, eps=1e-6, interleaved=False, out=None, stream=None):
+    """Queries and keys behind a root-mean-square norm of every head, then turned (see rotate), in one pass.
+
+    q_weight, k_weight   (size,) of the operands' type or float32; None: ones
+    """
+    _check_queries(q, k)
+    _no_autograd(q, k, q_weight, k_weight)
+    with _on(q.device, stream):
+        q, k = _rows(q), _rows(k)
+        y, z = _outputs(q, k, out)
+        args = _turn_args(q, k, _heads(q, y, None, q_weight, None), _NO_HEADS if k is None else _heads(k, z, None, k_weight, None),
+                          positions, inv_freq, axes, interleaved, False, (q_weight, k_weight), eps)
+        B._chk(B.lib().pcr_norm_rotate(args, torch.cuda.current_stream(q.device).cuda_stream), "pcr_norm_rotate")
+    return y, z
+
+
+def norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, inv_freq, axes, *, eps=1e-6, interleaved=False,
+                         out=None, stream=None):
+    """Gradients of norm_rotate from those of its outputs and from its inputs: (q, k, q_weight, k_weight).
+
+    out   where the gradients of q and k go; (grad_q, grad_k) or (q, k) themselves allowed
+    """
+    _check_queries(q, k)
+    if (k is None) != (grad_k is None) or grad_q.shape != q.shape or (k is not None and grad_k.shape != k.shape):
+        raise ValueError("gradients must have the shapes of their operands")
+    _operand(grad_q, q, "grad_q")
+    if k is not None:
+        _operand(grad_k, q, "grad_k")
+    elif k_weight is not None:
+        raise ValueError("k_weight without keys")
+    _no_autograd(q, k, q_weight, k_weight, grad_q, grad_k)
+    _same_device(q.device, grad_q, grad_k)
+    with _on(q.device, stream):
+        q, k, grad_q, grad_k = _rows(q), _rows(k), _rows(grad_q), _rows(grad_k)
+        y, z = _outputs(q, k, out)
+        dwq, dwk = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
+        args = _turn_args(q, k, _heads(q, y, grad_q, q_weight, dwq), _NO_HEADS if k is None else _heads(k, z, grad_k, k_weight, dwk),
+                          positions, inv_freq, axes, interleaved, False, (q_weight, k_weight), eps)
+        L = B.lib()
+        scratch = torch.empty(L.pcr_norm_rotate_scratch_bytes(args) // 4, dtype=torch.float32, device=q.device)
+        B._chk(L.pcr_norm_rotate_backward(args, scratch.data_ptr(), torch.cuda.current_stream(q.device).cuda_stream), "pcr_norm_rotate_backward")
+    return y, z, dwq, dwk
+
+
+def rotary_axes(rot, base=10000.0, sections=None, *, interleaved_axes=False, per_axis=False, device="cuda:0"):
+    """(inv_freq, axes) of `rot` turned elements, rot / 2 pairs.
+
+    sections          pairs of each axis (their sum is rot / 2); None: one axis
+    interleaved_axes  pair i belongs to axis i mod len(sections) while that axis has pairs left, otherwise the sections
+                      are runs
+    per_axis          every axis has the whole range of frequencies over its own pairs (image encoders), otherwise
+                      frequency i is base ** (-2 i / rot) whatever the axis
+    """
+    half = rot // 2
+    sections = [half] if sections is None else list(sections)
+    if rot % 2 or rot < 0 or sum(sections) != half or min(sections) < 0 or len(sections) > 4:
+        raise ValueError("sections must be up to four counts of pairs that add up to rot / 2")
+    if interleaved_axes:
+        left, axes = list(sections), []
+        while len(axes) < half:
+            for a in range(len(left)):
+                if left[a]:
+                    left[a] -= 1
+                    axes.append(a)
+    else:
+        axes = [a for a, n in enumerate(sections) for _ in range(n)]
+    seen, freq = [0] * len(sections), []
+    for i, a in enumerate(axes):
+        freq.append(base ** (-seen[a] / sections[a]) if per_axis else base ** (-i / half))
+        seen[a] += 1
+    return torch.tensor(freq, dtype=torch.float64, device=device), torch.tensor(axes, dtype=torch.int32, device=device)
+
+
+# ---- positions ------------------------------------------------------------------------------------------------------------
+
+
+def token_positions(segments, n_tokens, n_sequences, *, merge=1, time_step=1, restart=False, out=None, stream=None):
+    """Positions (3, n_tokens) of packed sequences and the position (n_sequences,) with which each goes on, both int32.
+
+    segments    (n, 4) int32 on the device: time (or tokens), height, width, sequence; text has no height or width, the
+                rows of a sequence stand together
+    merge       grids are numbered in blocks of merge x merge, as patches are
+    time_step   positions between two frames of a grid
+    restart     every segment begins at 0 (an image encoder's positions)
+    out         (3, at least n_tokens) int32 to write to: columns behind the last token stay as they are; without it they are 0
+    """
+    if segments.dtype != torch.int32 or segments.dim() != 2 or segments.shape[1] != 4 or not segments.is_contiguous():
+        raise ValueError("segments must be a contiguous (n, 4) int32 tensor")
+    if out is not None and (out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < n_tokens or out.stride(1) != 1):
+        raise ValueError("out must be int32 of shape (3, n_tokens) with a row's elements side by side")
+    _same_device(segments.device, out)
+    with _on(segments.device, stream):
+        flags = B.PCR_POSITIONS_RESTART if restart else 0
+        if out is None:
+            flags |= B.PCR_POSITIONS_ZERO_TAIL
+            out = torch.empty((3, n_tokens), dtype=torch.int32, device=segments.device)
+        after = torch.empty(n_sequences, dtype=torch.int32, device=segments.device)
+        L = B.lib()
+        scratch = torch.empty(L.pcr_token_positions_scratch_bytes(segments.shape[0]), dtype=torch.uint8, device=segments.device)
+        B._chk(L.pcr_token_positions(segments.data_ptr(), segments.shape[0], n_tokens, n_sequences, merge, time_step, flags, out.data_ptr(),
+                                     out.stride(0), after.data_ptr(), scratch.data_ptr(),
+                                     torch.cuda.current_stream(segments.device).cuda_stream), "pcr_token_positions")
+    return out, after
+
+
+# ---- patches --------------------------------------------------------------------------------------------------------------
+
+
+def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.bfloat16, out=None, stream=None):
+    """Patch tokens (n_tokens, 3 * patch * patch) of the images of a decode's output.
+
+    rgb      uint8 output of a decode
+    images   (n, 10) int64 on the device, a row per image: first byte, width, height, rectangle x0, y0, w, h, patches down
+             and across, flip
+    index    (n_tokens, 2) int32 on the device: image and patch of every token; an entry that does not fit gives zeros
+    merge    patches are numbered in blocks of merge x merge
+    """
+    if rgb.dtype != torch.uint8 or rgb.dim() != 1 or not rgb.is_contiguous():
+        raise ValueError("rgb must be a contiguous uint8 vector")
+    if images.dtype != torch.int64 or images.dim() != 2 or images.shape[1] != 10 or not images.is_contiguous():
+        raise ValueError("images must be a contiguous (n, 10) int64 tensor")
+    if index.dtype != torch.int32 or index.dim() != 2 or index.shape[1] != 2 or not index.is_contiguous():
+        raise ValueError("index must be a contiguous (n, 2) int32 tensor")
+    if dtype not in _CODES:
+        raise ValueError("dtype must be torch.float16, torch.bfloat16 or torch.float32")
+    shape = (index.shape[0], 3 * patch * patch)
+    if out is not None and (out.shape != shape or out.dtype != dtype or not out.is_contiguous()):
+        raise ValueError("out must be contiguous, (n_tokens, 3 * patch * patch) of dtype")
+    _same_device(rgb.device, images, index, out)
+    with _on(rgb.device, stream):
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=rgb.device)
+        B._chk(B.lib().pcr_patch_tokens(rgb.data_ptr(), rgb.numel(), images.data_ptr(), images.shape[0], index.data_ptr(), shape[0], patch,
+                                        merge, struct.pack("3f", *mean), struct.pack("3f", *std), _CODES[dtype], out.data_ptr(),
+                                        torch.cuda.current_stream(rgb.device).cuda_stream), "pcr_patch_tokens")
+    return out
+
+
+class PatchPlan(NamedTuple):
+    """What the images of a record become: tables on the device (see patch_tokens), and patches down and across on the host."""
+    images: torch.Tensor
+    index: torch.Tensor
+    grids: np.ndarray
+    patch: int
+    merge: int
+
+    def segments(self, merged: bool = False) -> torch.Tensor:
+        """Segments of token_positions, an image a sequence: its patches, or (merged) its blocks of merge x merge."""
+        m = self.merge if merged else 1
+        n = len(self.grids)
+        rows = np.stack([np.ones(n), self.grids[:, 0] // m, self.grids[:, 1] // m, np.arange(n)], 1).astype(np.int32)
+        return torch.from_numpy(rows).to(self.index.device)
+
+
+def patch_plan(info, patch, *, merge=1, crops=None, grids=None, device="cuda:0") -> PatchPlan:
+    """Plan of the images of `info` (Decoder.info: out_offset, width, height).
+
+    crops   (n, 5) x0, y0, w, h, flip as for Decoder.decode_tensor; None: the whole images
+    grids   (n, 2) patches down and across; None: the rectangle's sides rounded to whole blocks, at least one
+    """
+    n = len(info)
+    size = np.array([(i.out_offset, i.width, i.height) for i in info], dtype=np.int64).reshape(n, 3)
+    if crops is None:
+        crops = np.concatenate([np.zeros((n, 2), np.int64), size[:, 1:], np.zeros((n, 1), np.int64)], 1)
+    crops = np.ascontiguousarray(crops, dtype=np.int64)
+    if crops.shape != (n, 5):
+        raise ValueError("crops must have shape (n_images, 5)")
+    x0, y0, w, h, flip = crops.T
+    if (crops[:, :2] < 0).any() or (crops[:, 2:4] < 1).any() or (x0 + w > size[:, 1]).any() or (y0 + h > size[:, 2]).any() or ((flip != 0) & (flip != 1)).any():
+        raise ValueError("every rectangle must lie inside its image, flip 0 or 1")
+    if not 1 <= patch <= 32 or not 1 <= merge <= 64:
+        raise ValueError("patch must be 1..32, merge 1..64")
+    unit = patch * merge
+    if grids is None:
+        grids = merge * np.maximum(1, (2 * crops[:, [3, 2]] + unit) // (2 * unit))
+    grids = np.ascontiguousarray(grids, dtype=np.int64)
+    if grids.shape != (n, 2) or (grids < 1).any() or (grids % merge).any() or (grids * patch > 1 << 20).any():
+        raise ValueError("grids must have shape (n_images, 2), whole blocks of merge x merge patches, sides of 2^20 pixels at most")
+    count = grids[:, 0] * grids[:, 1]
+    if count.sum() >= 1 << 31:
+        raise ValueError("too many tokens for one batch")
+    image = np.repeat(np.arange(n), count)
+    local = np.arange(len(image)) - np.repeat(np.cumsum(count) - count, count)
+    table = np.concatenate([size, crops[:, :4], grids, crops[:, 4:]], 1)
+    index = np.stack([image, local], 1).astype(np.int32)
+    return PatchPlan(torch.from_numpy(table).to(device), torch.from_numpy(index).to(device), grids, patch, merge)
