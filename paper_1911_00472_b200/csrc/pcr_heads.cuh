@@ -30,7 +30,7 @@ struct HeadBlock {
     const void* weight;
     float* partial;               // backward: sums of dw, one row of head_dim per CTA
     int64_t xs[3], ys[3], gs[3];
-    int32_t heads, slots;         // slots: shares of the heads, `per` heads each but for the last
+    int32_t heads, slots;         // value by value: shares of `per` heads; backward by vectors: CTAs that take this operand
 };
 
 struct HeadArgs {
@@ -85,158 +85,383 @@ __device__ __forceinline__ void positions_of(const HeadArgs& A, uint32_t b, uint
 
 enum { kTurn = 0, kNormTurn = 1, kNormTurnBack = 2 };
 
-// Sum of v over the `n` lanes of a row that begins at lane `first`; every lane of the row gets it.
-__device__ __forceinline__ float row_sum(float v, int first, int at, int n) {
+// Sums over the `n` lanes of a row that begins at lane `first`, this lane being number `at` of it; every lane of the row
+// gets them.  n is the same for all lanes: the steps that it has no use for are skipped together.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int first, int at, int n) {
     if ((n & (n - 1)) == 0) {
-        for (int o = n >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            if (n > o) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+            }
+        return;
     }
-    for (int o = n > 16 ? 16 : n > 8 ? 8 : n > 4 ? 4 : 2; o > 0; o >>= 1) {
-        const float w = __shfl_down_sync(0xffffffffu, v, o);
-        if (at + o < n) v += w;
-    }
-    return __shfl_sync(0xffffffffu, v, first);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (n > o) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float w = __shfl_down_sync(0xffffffffu, v[k], o);
+                v[k] += at + o < n ? w : 0.f;
+            }
+        }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, v[k], first);
 }
 
-// grid (token groups, slots of queries then keys).  A warp takes 32 / chunks tokens at a time; tokens go round the grid.
-template <typename T, int V, int kMode, bool kNext>
-__global__ void __launch_bounds__(kHeadThreads) heads_kernel(const __grid_constant__ HeadArgs A) {
-    using VT = Vec<T, V>;
-    const int which = (int)blockIdx.y >= A.part[0].slots ? 1 : 0;
-    const HeadBlock& H = A.part[which];
-    const int slot = (int)blockIdx.y - (which ? A.part[0].slots : 0);
-    const int h0 = slot * A.per, h1 = min(h0 + A.per, H.heads);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int nc = A.chunks, rows = 32 / nc;
-    const int sub = lane / nc, chunk = lane - sub * nc, first = sub * nc;
-    const bool in_row = sub < rows;
-    // where this thread's two vectors lie in a head
-    const int turning = A.rot / (2 * V);
-    const bool turns = chunk < turning;
-    const int pair0 = chunk * V;
-    int o1, o2;
-    if (kNext) { o1 = 2 * V * chunk; o2 = o1 + V; }
-    else if (turns) { o1 = pair0; o2 = pair0 + A.rot / 2; }
-    else { o1 = A.rot + 2 * V * (chunk - turning); o2 = o1 + V; }
-    float w1[V], w2[V], dw1[V], dw2[V];
-    if (kMode != kTurn) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const bool there = H.weight != nullptr && in_row;
-            w1[i] = there ? weight_of<T>(A, H.weight, o1 + i) : 1.f;
-            w2[i] = there ? weight_of<T>(A, H.weight, o2 + i) : 1.f;
-            dw1[i] = dw2[i] = 0.f;
-        }
+// What a CTA of the vector kernels keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its
+// axis, and the weights of both norms.
+struct HeadTables {
+    uint2 turn[kMaxHeadDim / 2];
+    int32_t axis[kMaxHeadDim / 2];
+    float w[2][kMaxHeadDim];
+};
+
+template <typename T, bool kNorm>
+__device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables& S) {
+    for (int j = threadIdx.x; j < A.rot / 2; j += kHeadThreads) {
+        double t = freq_at(A, j) * 0.15915494309189533577;                   // 1 / (2 pi)
+        t -= floor(t);
+        const unsigned long long f = __double2ull_rn(t * 18446744073709551616.0);      // (2^64 itself, a whole turn, saturates to just below)
+        S.turn[j] = make_uint2((uint32_t)f, (uint32_t)(f >> 32));
+        S.axis[j] = A.axes[j];
     }
-    constexpr int kWarps = kHeadThreads / 32;
-    const uint32_t step = gridDim.x * (uint32_t)(kWarps * rows);
-    const uint32_t base0 = (blockIdx.x * kWarps + warp) * (uint32_t)rows;
-    for (uint32_t base = base0; base < A.tokens; base += step) {           // (the bound holds for the whole warp: shuffles inside)
-        const uint32_t n = base + (uint32_t)sub;
-        const bool live = in_row && n < A.tokens;
-        const uint32_t b = live ? n / A.seq : 0, t = live ? n - b * A.seq : 0;
-        float c[V], s[V];
-        {
-            int32_t p[kMaxAxes] = {0, 0, 0, 0};
-            if (live && turns) positions_of(A, b, t, p);
+    if (kNorm)
+        for (int j = threadIdx.x; j < 2 * A.dim; j += kHeadThreads) {
+            const int which = j >= A.dim, i = j - (which ? A.dim : 0);
+            const void* w = which ? A.part[1].weight : A.part[0].weight;
+            S.w[which][i] = w != nullptr ? weight_of<T>(A, w, i) : 1.f;
+        }
+}
+
+// cosine and sine of a position's turn.  The product of the position and the 64-bit fraction is taken modulo 2^64, that is
+// modulo whole turns: exact but for the fraction's own rounding (2^-65 turns a position), however far the position.  The
+// upper 32 bits are kept (2^-32 turns: 1.5e-9 of an angle).  16-bit results take the hardware's sine and cosine, off by
+// 2^-21.4 at most, where the result is rounded to 2^-9 or 2^-12: 5 instructions in the place of about 40.
+template <typename T>
+__device__ __forceinline__ void turn_by(int32_t position, uint2 turn, bool inverse, float& c, float& s) {
+    const uint32_t p = (uint32_t)position;
+    uint32_t hi = __umulhi(p, turn.x) + p * turn.y;
+    if (position < 0) hi -= turn.x;                                          // p is position + 2^32 there
+    const float half_turns = (float)(int32_t)hi * 4.656612873077393e-10f;    // 2^-31
+    if (sizeof(T) == 2) __sincosf(half_turns * 3.14159265358979f, &s, &c);
+    else sincospif(half_turns, &s, &c);
+    if (inverse) s = -s;
+}
+
+// Where the lanes of a warp stand: `chunk` of a row, which of the warp's rows, the two vectors of the chunk inside a head.
+template <int V, bool kNext> struct Place {
+    int nc, rows, sub, chunk, first, pair, o1, o2;
+    bool in_row, turns;
+    __device__ __forceinline__ explicit Place(const HeadArgs& A) {
+        const int lane = threadIdx.x & 31, turning = A.rot / (2 * V);
+        nc = A.chunks; rows = 32 / nc; sub = lane / nc; chunk = lane - sub * nc; first = sub * nc;
+        in_row = sub < rows; turns = chunk < turning; pair = chunk * V;
+        if (kNext) { o1 = 2 * V * chunk; o2 = o1 + V; }
+        else if (turns) { o1 = pair; o2 = pair + A.rot / 2; }
+        else { o1 = A.rot + 2 * V * (chunk - turning); o2 = o1 + V; }
+    }
+};
+
+// The elements that make pair i: of the first and of the second vector, or 2 i and 2 i + 1 of both together.
+template <int V, bool kNext> __device__ __forceinline__ float& one(float (&p)[V], float (&q)[V], int i) {
+    return kNext ? (2 * i < V ? p[(2 * i) % V] : q[(2 * i) % V]) : p[i];
+}
+template <int V, bool kNext> __device__ __forceinline__ float& two(float (&p)[V], float (&q)[V], int i) {
+    return kNext ? (2 * i < V ? p[(2 * i + 1) % V] : q[(2 * i + 1) % V]) : q[i];
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void turns_of(const HeadArgs& A, const HeadTables& S, const int32_t (&p)[kMaxAxes], bool turns, int pair, float (&c)[V], float (&s)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        c[i] = 1.f; s[i] = 0.f;
+        if (turns) turn_by<T>(on_axis(p, S.axis[pair + i]), S.turn[pair + i], A.inverse, c[i], s[i]);
+    }
+}
+
+template <typename T, int V> struct Row { Vec<T, V> a, b; };
+template <typename T, int V>
+__device__ __forceinline__ Row<T, V> load_row(const T* x, int gap) {
+    return {*reinterpret_cast<const Vec<T, V>*>(x), *reinterpret_cast<const Vec<T, V>*>(x + gap)};
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_row(T* y, int gap, const float (&r1)[V], const float (&r2)[V]) {
+    Vec<T, V> y1, y2;
+#pragma unroll
+    for (int i = 0; i < V; ++i) { y1.v[i] = from_f<T>(r1[i]); y2.v[i] = from_f<T>(r2[i]); }
+    *reinterpret_cast<Vec<T, V>*>(y) = y1;
+    *reinterpret_cast<Vec<T, V>*>(y + gap) = y2;
+}
+__device__ __forceinline__ void soon(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+
+// Forward: grid (token groups, shares of `per` heads of queries and keys in a row).  A warp takes 32 / chunks tokens, a
+// thread `per` heads of its token, kAhead of them at a time.  Lanes without a token go along with the last one's data and
+// store nothing: no shuffle and no load stands in a branch.
+template <typename T, int V, bool kNorm, bool kNext>
+__global__ void __launch_bounds__(kHeadThreads, kNorm ? 5 : 6) heads_kernel(const __grid_constant__ HeadArgs A) {
+    constexpr int kWarps = kHeadThreads / 32, kAhead = (V * sizeof(T) >= 16 ? 1 : 2) * 4;
+    __shared__ HeadTables S;
+    const Place<V, kNext> at(A);
+    const uint32_t n0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * (uint32_t)at.rows + (uint32_t)at.sub;
+    const bool live = at.in_row && n0 < A.tokens;
+    const uint32_t n = min(n0, A.tokens - 1), b = n / A.seq, t = n - b * A.seq;
+    const int gap = at.o2 - at.o1, from = (int)blockIdx.y * A.per, to = from + A.per;
+    int which = from < A.part[0].heads ? 0 : 1;
+    {   // the first row is on its way while the tables are filled
+        const HeadBlock& H = A.part[which];
+        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + (int64_t)(from - (which ? A.part[0].heads : 0)) * H.xs[2] + at.o1;
+        soon(x); soon(x + gap);
+    }
+    int32_t p[kMaxAxes];
+    positions_of(A, b, t, p);
+    fill_tables<T, kNorm>(A, S);
+    __syncthreads();
+    float c[V], s[V];
+    turns_of<T, V>(A, S, p, at.turns, at.pair, c, s);
+#pragma unroll 1
+    for (; which < 2; ++which) {
+        const HeadBlock& H = A.part[which];
+        const int base = which ? A.part[0].heads : 0;
+        const int h0 = max(from - base, 0), h1 = min(to - base, H.heads);
+        if (h0 >= h1) continue;
+        // a' = a wa c - b wb s, b' = a wa s + b wb c: four factors a pair, the same for all heads
+        float ac[V], as[V], bc[V], bs[V];
+        if (kNorm) {
+            float w1[V], w2[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) { w1[i] = S.w[which][at.o1 + i]; w2[i] = S.w[which][at.o2 + i]; }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                c[i] = 1.f; s[i] = 0.f;
-                if (live && turns) turn_of(on_axis(p, __ldg(A.axes + pair0 + i)), freq_at(A, pair0 + i), A.inverse, c[i], s[i]);
+                const float wa = one<V, kNext>(w1, w2, i), wb = two<V, kNext>(w1, w2, i);
+                ac[i] = wa * c[i]; as[i] = wa * s[i]; bc[i] = wb * c[i]; bs[i] = wb * s[i];
             }
         }
-        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1];
-        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1];
-        const T* g = kMode == kNormTurnBack ? static_cast<const T*>(H.g) + (int64_t)b * H.gs[0] + (int64_t)t * H.gs[1] : nullptr;
-        for (int h = h0; h < h1; ++h) {
-            VT x1, x2, g1, g2;
+        const int64_t xs = H.xs[2], ys = H.ys[2];
+        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + h0 * xs + at.o1;
+        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + h0 * ys + at.o1;
+        auto work = [&](const Row<T, V>& row) {
+            float a1[V], a2[V], r[1] = {1.f};
 #pragma unroll
-            for (int i = 0; i < V; ++i) { x1.v[i] = x2.v[i] = from_f<T>(0.f); g1.v[i] = g2.v[i] = from_f<T>(0.f); }
-            if (live) {
-                const T* xr = x + (int64_t)h * H.xs[2];
-                x1 = *reinterpret_cast<const VT*>(xr + o1); x2 = *reinterpret_cast<const VT*>(xr + o2);
-                if (kMode == kNormTurnBack) {
-                    const T* gr = g + (int64_t)h * H.gs[2];
-                    g1 = *reinterpret_cast<const VT*>(gr + o1); g2 = *reinterpret_cast<const VT*>(gr + o2);
-                }
+            for (int i = 0; i < V; ++i) { a1[i] = to_f(row.a.v[i]); a2[i] = to_f(row.b.v[i]); }
+            if (kNorm) {
+                r[0] = 0.f;
+#pragma unroll
+                for (int i = 0; i < V; ++i) r[0] += a1[i] * a1[i] + a2[i] * a2[i];
+                row_sums<1>(r, at.first, at.chunk, at.nc);
+                r[0] = rsqrtf(r[0] * A.inv_dim + A.eps);
             }
-            float a1[V], a2[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) { a1[i] = to_f(x1.v[i]); a2[i] = to_f(x2.v[i]); }
-            // element i of the first and of the second vector are a pair, or 2 i and 2 i + 1 of both together
-            auto pairwise = [&](float (&p)[V], float (&q)[V], float sign) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float& a = kNext ? (2 * i < V ? p[(2 * i) % V] : q[(2 * i) % V]) : p[i];
-                    float& e = kNext ? (2 * i < V ? p[(2 * i + 1) % V] : q[(2 * i + 1) % V]) : q[i];
-                    const float si = sign * s[i], u = a * c[i] - e * si, v = a * si + e * c[i];
-                    a = u; e = v;
-                }
-            };
             float r1[V], r2[V];
-            if (kMode == kTurn) {
-                pairwise(a1, a2, 1.f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) { r1[i] = a1[i]; r2[i] = a2[i]; }
-            } else {
-                float sq = 0.f;
+            for (int i = 0; i < V; ++i) {
+                const float a = one<V, kNext>(a1, a2, i) * r[0], e = two<V, kNext>(a1, a2, i) * r[0];
+                one<V, kNext>(r1, r2, i) = kNorm ? a * ac[i] - e * bs[i] : a * c[i] - e * s[i];
+                two<V, kNext>(r1, r2, i) = kNorm ? a * as[i] + e * bc[i] : a * s[i] + e * c[i];
+            }
+            if (live) store_row<T, V>(y, gap, r1, r2);
+            y += ys;
+        };
+        int h = h0;
+#pragma unroll 1
+        for (; h + kAhead <= h1; h += kAhead) {
+            Row<T, V> rows[kAhead];
 #pragma unroll
-                for (int i = 0; i < V; ++i) sq += a1[i] * a1[i] + a2[i] * a2[i];
-                if (kMode == kNormTurn) {
-                    sq = row_sum(sq, first, chunk, nc);
-                    const float r = 1.f / sqrtf(sq * A.inv_dim + A.eps);
+            for (int k = 0; k < kAhead; ++k, x += xs) rows[k] = load_row<T, V>(x, gap);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) { r1[i] = a1[i] * r * w1[i]; r2[i] = a2[i] * r * w2[i]; }
-                    pairwise(r1, r2, 1.f);
-                } else {
-                    float d1[V], d2[V], dot = 0.f;
+            for (int k = 0; k < kAhead; ++k) work(rows[k]);
+        }
+#pragma unroll 1
+        for (; h < h1; ++h, x += xs) work(load_row<T, V>(x, gap));
+    }
+}
+
+// Two single-precision numbers in one register pair; the operations below take both in one instruction.
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 pack2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(F2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// A row's pairs, two by two: first elements in a, second ones in b.
+template <int V> struct Pairs { F2 a[V / 2], b[V / 2]; };
+template <typename T, int V, bool kNext>
+__device__ __forceinline__ Pairs<V> pairs_of(const Row<T, V>& row) {
+    float f[V], g[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) { d1[i] = to_f(g1.v[i]); d2[i] = to_f(g2.v[i]); }
-                    pairwise(d1, d2, -1.f);
+    for (int i = 0; i < V; ++i) { f[i] = to_f(row.a.v[i]); g[i] = to_f(row.b.v[i]); }
+    Pairs<V> r;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) dot += d1[i] * w1[i] * a1[i] + d2[i] * w2[i] * a2[i];
-                    sq = row_sum(sq, first, chunk, nc);
-                    dot = row_sum(dot, first, chunk, nc);
-                    const float r = live ? 1.f / sqrtf(sq * A.inv_dim + A.eps) : 0.f;
-                    const float m = dot * r * A.inv_dim;
+    for (int i = 0; i < V; i += 2) {
+        r.a[i / 2] = pack2(one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
+        r.b[i / 2] = pack2(two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
+    }
+    return r;
+}
+template <int V, bool kNext>
+__device__ __forceinline__ void elements_of(const Pairs<V>& p, float (&f)[V], float (&g)[V]) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float u1 = a1[i] * r, u2 = a2[i] * r;
-                        r1[i] = r * (d1[i] * w1[i] - u1 * m); r2[i] = r * (d2[i] * w2[i] - u2 * m);
-                        dw1[i] += d1[i] * u1; dw2[i] += d2[i] * u2;
-                    }
+    for (int i = 0; i < V; i += 2) {
+        unpack2(p.a[i / 2], one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
+        unpack2(p.b[i / 2], two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
+    }
+}
+
+// Copies of N bytes to shared memory that the thread does not wait for, and the wait for all but the newest `kLeft` groups.
+template <int N> __device__ __forceinline__ void copy_soon(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(N) : "memory");
+}
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+// Backward: the first part[0].slots CTAs take the queries, the others the keys; a warp goes round the tokens and over all
+// heads of each, so that the sums for the weights stay in registers to the end.
+//   q = d a, dot = sum of q w, dw += q r, dx = r (d w - a r^2 dot / dim)
+// Two operands, their factors and the sums leave no registers for rows on their way, and a row's work is a long chain of
+// dependent steps.  So every lane has a ring of kStages groups of rows in shared memory that it alone fills and reads: no
+// barrier, and kStages - 1 groups are always on their way.
+template <typename T, int V, bool kNext>
+__global__ void __launch_bounds__(kHeadThreads, 4) heads_back_kernel(const __grid_constant__ HeadArgs A) {
+    constexpr int kWarps = kHeadThreads / 32, kStages = 4, N = V / 2, kBytes = V * (int)sizeof(T), kGroup = kBytes >= 16 ? 1 : 2;
+    using VT = Vec<T, V>;
+    struct Ring { VT rows[kStages][kGroup][4][32]; int32_t positions[kStages][kMaxAxes][32]; };
+    __shared__ HeadTables S;
+    __shared__ union { Ring ring[kWarps]; float sums[kWarps][kMaxHeadDim]; } U;
+    const int which = (int)blockIdx.x >= A.part[0].slots ? 1 : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const HeadBlock& H = A.part[which];
+    const uint32_t mine = blockIdx.x - (which ? (uint32_t)A.part[0].slots : 0u);
+    const Place<V, kNext> at(A);
+    const int gap = at.o2 - at.o1, heads = H.heads;
+    const int64_t xs = H.xs[2], gs = H.gs[2], ys = H.ys[2];
+    const uint64_t step = (uint64_t)H.slots * kWarps * at.rows, begin = (uint64_t)(mine * kWarps + warp) * at.rows;
+    Ring& R = U.ring[warp];
+    auto token_of = [&](uint64_t base, uint32_t& b, uint32_t& t) {        // lanes without one go along with the last
+        const uint32_t n = (uint32_t)min(base + at.sub, (uint64_t)A.tokens - 1);
+        b = n / A.seq; t = n - b * A.seq;
+    };
+
+    // the side that fills
+    uint64_t fbase = begin;
+    int fhead = 0, fstage = 0;
+    const T *fx = nullptr, *fg = nullptr;
+    auto fill = [&]() {
+        if (fbase < A.tokens) {
+            if (fhead == 0) {
+                uint32_t b, t;
+                token_of(fbase, b, t);
+                fx = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + at.o1;
+                fg = static_cast<const T*>(H.g) + (int64_t)b * H.gs[0] + (int64_t)t * H.gs[1] + at.o1;
+                const int32_t* p = A.positions + (int64_t)b * A.ps[1] + (int64_t)t * A.ps[2];
+#pragma unroll
+                for (int a = 0; a < kMaxAxes; ++a)
+                    if (a < A.n_axes) copy_soon<4>(&R.positions[fstage][a][lane], p + (int64_t)a * A.ps[0]);
+            }
+#pragma unroll
+            for (int k = 0; k < kGroup; ++k, fx += xs, fg += gs)
+                if (fhead + k < heads) {
+                    copy_soon<kBytes>(&R.rows[fstage][k][0][lane], fx); copy_soon<kBytes>(&R.rows[fstage][k][1][lane], fx + gap);
+                    copy_soon<kBytes>(&R.rows[fstage][k][2][lane], fg); copy_soon<kBytes>(&R.rows[fstage][k][3][lane], fg + gap);
+                }
+            fhead += kGroup;
+            if (fhead >= heads) { fhead = 0; fbase += step; }
+        }
+        fstage = (fstage + 1) % kStages;
+        copies_close();
+    };
+#pragma unroll
+    for (int k = 0; k < kStages - 1; ++k) fill();
+    fill_tables<T, true>(A, S);
+    __syncthreads();
+    Pairs<V> w, dw;
+    {
+        Row<float, V> r;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { r.a.v[i] = S.w[which][at.o1 + i]; r.b.v[i] = S.w[which][at.o2 + i]; }
+        w = pairs_of<float, V, kNext>(r);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) dw.a[i] = dw.b[i] = 0;
+    int stage = 0;
+#pragma unroll 1
+    for (uint64_t base = begin; base < A.tokens; base += step) {
+        const bool live = at.in_row && base + at.sub < A.tokens;
+        uint32_t b, t;
+        token_of(base, b, t);
+        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + at.o1;
+        F2 c[N], s[N], ns[N];
+#pragma unroll 1
+        for (int h = 0; h < heads; h += kGroup) {
+            copies_wait<kStages - 2>();
+            if (h == 0) {
+                int32_t p[kMaxAxes];
+#pragma unroll
+                for (int a = 0; a < kMaxAxes; ++a) p[a] = a < A.n_axes ? R.positions[stage][a][lane] : 0;
+                float fc[V], fs[V];
+                turns_of<T, V>(A, S, p, at.turns, at.pair, fc, fs);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    c[i] = pack2(fc[2 * i], fc[2 * i + 1]); s[i] = pack2(fs[2 * i], fs[2 * i + 1]); ns[i] = pack2(-fs[2 * i], -fs[2 * i + 1]);
                 }
             }
-            if (live) {
-                VT y1, y2;
+            auto work = [&](int k) {
+                const VT* from = &R.rows[stage][k][0][lane];
+                const Row<T, V> row = {from[0], from[32]}, grow = {from[64], from[96]};
+                const Pairs<V> x2 = pairs_of<T, V, kNext>(row);
+                Pairs<V> d = pairs_of<T, V, kNext>(grow), q;
+                F2 sq = 0, dot = 0;
 #pragma unroll
-                for (int i = 0; i < V; ++i) { y1.v[i] = from_f<T>(r1[i]); y2.v[i] = from_f<T>(r2[i]); }
-                T* yr = y + (int64_t)h * H.ys[2];
-                *reinterpret_cast<VT*>(yr + o1) = y1; *reinterpret_cast<VT*>(yr + o2) = y2;
-            }
+                for (int i = 0; i < N; ++i) {
+                    const F2 u = fma2(d.b[i], s[i], mul2(d.a[i], c[i])), v = fma2(d.a[i], ns[i], mul2(d.b[i], c[i]));
+                    q.a[i] = mul2(u, x2.a[i]); q.b[i] = mul2(v, x2.b[i]);
+                    sq = fma2(x2.a[i], x2.a[i], sq); sq = fma2(x2.b[i], x2.b[i], sq);
+                    dot = fma2(q.a[i], w.a[i], dot); dot = fma2(q.b[i], w.b[i], dot);
+                    d.a[i] = mul2(u, w.a[i]); d.b[i] = mul2(v, w.b[i]);
+                }
+                float sum[2], other[2];
+                unpack2(sq, sum[0], other[0]); unpack2(dot, sum[1], other[1]);
+                sum[0] += other[0]; sum[1] += other[1];
+                row_sums<2>(sum, at.first, at.chunk, at.nc);
+                const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m = -(sum[1] * r * A.inv_dim * r), rl = live ? r : 0.f;
+                const F2 r2 = pack2(r, r), m2 = pack2(m, m), rl2 = pack2(rl, rl);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    d.a[i] = mul2(fma2(x2.a[i], m2, d.a[i]), r2); d.b[i] = mul2(fma2(x2.b[i], m2, d.b[i]), r2);
+                    dw.a[i] = fma2(q.a[i], rl2, dw.a[i]); dw.b[i] = fma2(q.b[i], rl2, dw.b[i]);
+                }
+                float y1[V], y2[V];
+                elements_of<V, kNext>(d, y1, y2);
+                if (live) store_row<T, V>(y, gap, y1, y2);
+                y += ys;
+            };
+            if (kGroup == 2 && h + 2 <= heads) { work(0); work(1); }
+            else work(0);
+            stage = (stage + 1) % kStages;
+            fill();
         }
     }
-    if (kMode == kNormTurnBack) {
-        if (H.partial == nullptr) return;                       // (the same for the whole CTA)
-        __shared__ float sums[kWarps][kMaxHeadDim];
-        // the rows of a warp, in the order of their lanes
+    copies_wait<0>();
+    if (H.partial == nullptr) return;                           // (the same for the whole CTA)
+    __syncthreads();                                            // the rings make room for the sums
+    // the rows of a warp in the order of their lanes, then the warps in theirs
+    float dw1[V], dw2[V];
+    elements_of<V, kNext>(dw, dw1, dw2);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float p = dw1[i], q = dw2[i];
-            for (int k = 1; k < rows; ++k) {
-                const float pk = __shfl_sync(0xffffffffu, dw1[i], chunk + k * nc), qk = __shfl_sync(0xffffffffu, dw2[i], chunk + k * nc);
-                p += pk; q += qk;
-            }
-            if (sub == 0) { sums[warp][o1 + i] = p; sums[warp][o2 + i] = q; }
+    for (int i = 0; i < V; ++i) {
+        float p = dw1[i], q = dw2[i];
+        for (int k = 1; k < at.rows; ++k) {
+            const float pk = __shfl_sync(0xffffffffu, dw1[i], at.chunk + k * at.nc), qk = __shfl_sync(0xffffffffu, dw2[i], at.chunk + k * at.nc);
+            p += pk; q += qk;
         }
-        __syncthreads();
-        float* out = H.partial + ((size_t)slot * gridDim.x + blockIdx.x) * A.dim;
-        for (int j = threadIdx.x; j < A.dim; j += kHeadThreads) {
-            float v = 0.f;
+        if (at.sub == 0) { U.sums[warp][at.o1 + i] = p; U.sums[warp][at.o2 + i] = q; }
+    }
+    __syncthreads();
+    float* out = H.partial + (size_t)mine * A.dim;
+    for (int j = threadIdx.x; j < A.dim; j += kHeadThreads) {
+        float v = 0.f;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) v += sums[k][j];
-            out[j] = v;
-        }
+        for (int k = 0; k < kWarps; ++k) v += U.sums[k][j];
+        out[j] = v;
     }
 }
 
@@ -278,10 +503,10 @@ __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_co
                     }
                     for (int j = A.rot + lane; j < A.dim; j += 32) dot += to_f(g[j]) * weight(j) * to_f(x[j]);
                 }
-                sq = row_sum(sq, 0, lane, 32);
-                if (kMode == kNormTurnBack) dot = row_sum(dot, 0, lane, 32);
-                r = 1.f / sqrtf(sq * A.inv_dim + A.eps);
-                m = dot * r * A.inv_dim;
+                float sum[2] = {sq, dot};
+                row_sums<2>(sum, 0, lane, 32);
+                r = rsqrtf(sum[0] * A.inv_dim + A.eps);
+                m = sum[1] * r * A.inv_dim;
             }
             for (int i = lane; i < half; i += 32) {
                 const int ja = kNext ? 2 * i : i, jb = kNext ? 2 * i + 1 : i + half;

@@ -84,25 +84,35 @@ bool fits(const pcr_turn_args& a, bool back, int v) {
     return true;
 }
 
-// How a call is cut: vectors of `v` pairs (0: value by value), `per` heads of a token to a thread, CTAs.
-struct Cut { int v, per, slots[2]; unsigned groups; };
+// How a call is cut: vectors of `v` pairs (0: value by value), `per` heads of a token to a thread, the grid, and how many
+// rows of partial sums each operand's weights get.
+struct Cut { int v, per, slots[2], rows[2]; unsigned x, y; };
 
 Cut cut_of(const pcr_turn_args& a, bool back) {
-    Cut c = {0, 1, {0, 0}, 1};
+    Cut c = {};
     for (int v : {8, 4, 2})
         if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
-    const int64_t n = a.batch * a.tokens, heads = a.q.heads + a.k.heads;
-    const int rows = c.v ? 32 / (a.head_dim / (2 * c.v)) : 1;       // tokens of a warp
-    const int64_t warps = std::max<int64_t>((n + rows - 1) / rows, 1);
-    const int64_t want = (int64_t)sm_count() * 32;                  // warps that fill the GPU
-    const int64_t slots = std::min<int64_t>((want + warps - 1) / warps, std::max<int64_t>(heads, 1));
-    c.per = (int)std::max<int64_t>((heads + slots - 1) / slots, 1);
-    c.slots[0] = (a.q.heads + c.per - 1) / c.per;
-    c.slots[1] = (a.k.heads + c.per - 1) / c.per;
     constexpr int kWarps = kHeadThreads / 32;
-    int64_t groups = (warps + kWarps - 1) / kWarps;
-    if (back) groups = std::min<int64_t>(groups, std::max<int64_t>((int64_t)sm_count() * 8 / std::max(c.slots[0] + c.slots[1], 1), 1));
-    c.groups = (unsigned)groups;
+    const int64_t n = a.batch * a.tokens, heads = a.q.heads + a.k.heads, sms = sm_count();
+    const int rows = c.v ? 32 / (a.head_dim / (2 * c.v)) : 1;       // tokens of a warp
+    const int64_t warps = (n + rows - 1) / rows, groups = (warps + kWarps - 1) / kWarps;
+    // heads are shared out while that gives the SMs warps that they lack
+    const int64_t shares = std::min<int64_t>((sms * 32 + warps - 1) / warps, heads);
+    c.per = (int)((heads + shares - 1) / shares);
+    if (back && c.v) {
+        // CTAs by the operands' heads: those of both end at about the same time
+        const int64_t all = std::min<int64_t>(sms * 4, groups * ((a.q.heads > 0) + (a.k.heads > 0)));
+        c.slots[0] = a.q.heads == 0 ? 0 : (int)std::min(groups, std::max<int64_t>(1, (all * a.q.heads + heads / 2) / heads));
+        c.slots[1] = a.k.heads == 0 ? 0 : (int)std::min(groups, std::max<int64_t>(1, all - c.slots[0]));
+        c.x = c.slots[0] + c.slots[1]; c.y = 1;
+        c.rows[0] = c.slots[0]; c.rows[1] = c.slots[1];
+    } else {
+        c.slots[0] = (a.q.heads + c.per - 1) / c.per;
+        c.slots[1] = (a.k.heads + c.per - 1) / c.per;
+        c.y = c.v ? (unsigned)((heads + c.per - 1) / c.per) : (unsigned)(c.slots[0] + c.slots[1]);
+        c.x = (unsigned)(back ? std::min<int64_t>(groups, std::max<int64_t>(sms * 8 / c.y, 1)) : groups);
+        c.rows[0] = c.slots[0] * c.x; c.rows[1] = c.slots[1] * c.x;
+    }
     return c;
 }
 
@@ -122,12 +132,18 @@ void fill(HeadArgs& A, const pcr_turn_args& a, const Cut& c) {
     A.eps = a.eps; A.inv_dim = 1.f / (float)a.head_dim;
 }
 
+template <typename T, int V, int kMode, bool kNext>
+void launch_vectors(const HeadArgs& A, dim3 grid, cudaStream_t st) {
+    if constexpr (kMode == kNormTurnBack) heads_back_kernel<T, V, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    else heads_kernel<T, V, kMode == kNormTurn, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+}
+
 template <typename T, int kMode, bool kNext>
 void launch(const HeadArgs& A, const Cut& c, cudaStream_t st) {
-    const dim3 grid(c.groups, (unsigned)(c.slots[0] + c.slots[1]));
-    if (sizeof(T) == 2 && c.v == 8) heads_kernel<T, sizeof(T) == 2 ? 8 : 4, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
-    else if (c.v == 4) heads_kernel<T, 4, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
-    else if (c.v == 2) heads_kernel<T, 2, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    const dim3 grid(c.x, c.y);
+    if (sizeof(T) == 2 && c.v == 8) launch_vectors<T, sizeof(T) == 2 ? 8 : 4, kMode, kNext>(A, grid, st);
+    else if (c.v == 4) launch_vectors<T, 4, kMode, kNext>(A, grid, st);
+    else if (c.v == 2) launch_vectors<T, 2, kMode, kNext>(A, grid, st);
     else heads_any_kernel<T, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
     ++g_launches;
 }
@@ -170,7 +186,7 @@ int pcr_norm_rotate(const pcr_turn_args* args, void* stream) {
 size_t pcr_norm_rotate_scratch_bytes(const pcr_turn_args* args) {
     if (!args || check_heads(*args, true, true) != PCR_OK || nothing(*args)) return 0;
     const Cut c = cut_of(*args, true);
-    return (size_t)(c.slots[0] + c.slots[1]) * c.groups * args->head_dim * sizeof(float);
+    return ((size_t)c.rows[0] + c.rows[1]) * args->head_dim * sizeof(float);
 }
 
 int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* stream) {
@@ -186,8 +202,8 @@ int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* str
         fill(A, *args, c);
         float* at = static_cast<float*>(scratch);
         for (int i = 0; i < 2; ++i) {
-            if (S.dw[i]) { A.part[i].partial = at; S.partial[i] = at; S.rows[i] = (int32_t)(c.slots[i] * c.groups); }
-            if (at) at += (size_t)c.slots[i] * c.groups * args->head_dim;
+            if (S.dw[i]) { A.part[i].partial = at; S.partial[i] = at; S.rows[i] = c.rows[i]; }
+            if (at) at += (size_t)c.rows[i] * args->head_dim;
         }
         launch_mode<kNormTurnBack>(A, c, args->dtype, args->interleaved != 0, st);
     }
