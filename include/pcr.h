@@ -244,7 +244,8 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
  *   positions  : DEVICE int32, three rows, axis_stride >= n_tokens elements apart.
  *   next       : DEVICE int32, n_sequences: the position with which a sequence goes on (for the tokens
  *                that a model adds one by one); 0 for a sequence without segments.
- *   scratch    : DEVICE, pcr_token_positions_scratch_bytes(n_segments) bytes, 8-byte aligned.
+ *   scratch    : DEVICE, pcr_token_positions_scratch_bytes(n_segments) bytes (0 up to 16384 segments),
+ *                8-byte aligned.
  * Counts below zero are taken as 0; positions are kept modulo 2^32.   time_step : 0 .. 2^20.
  * Errors: PCR_E_ARG, PCR_E_CUDA. */
 #define PCR_POSITIONS_RESTART 1

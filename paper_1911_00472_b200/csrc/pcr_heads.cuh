@@ -41,7 +41,7 @@ struct HeadArgs {
     const int32_t* axes;
     uint32_t tokens, seq;         // batch * tokens of a sequence, tokens of a sequence
     int32_t n_axes, freq64, weight32, inverse;
-    int32_t dim, rot, chunks, per;
+    int32_t dim, rot, lanes, per;   // lanes: of a row
     float eps, inv_dim;
 };
 
@@ -85,42 +85,50 @@ __device__ __forceinline__ void positions_of(const HeadArgs& A, uint32_t b, uint
 
 enum { kTurn = 0, kNormTurn = 1, kNormTurnBack = 2 };
 
-// Sums over the `n` lanes of a row that begins at lane `first`, this lane being number `at` of it; every lane of the row
-// gets them.  n is the same for all lanes: the steps that it has no use for are skipped together.
+// Sums over the `n` lanes of a row, this lane being number `at` of it, the row's first lane `first`; every lane gets them.
+// Where n is no power of two, sums of 1, 2, 4, ... lanes going round the row are made, and those that n's bits name added
+// up: as few shuffles as for the next larger power of two and no condition on the lane.  n is the same for all lanes.
 template <int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], int first, int at, int n) {
     if ((n & (n - 1)) == 0) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            if (n > o) {
+        for (int o = 1; o < 32; o <<= 1) {
+            if (o >= n) return;
 #pragma unroll
-                for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-            }
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
         return;
     }
+    auto round = [&](int o) { const int l = at + o; return first + (l < n ? l : l - n); };
+    float all[N];
+    int have = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (n > o) {
+    for (int o = 1; o < 32; o <<= 1) {
+        if (n & o) {
+            const int from = round(have);
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float w = __shfl_down_sync(0xffffffffu, v[k], o);
-                v[k] += at + o < n ? w : 0.f;
-            }
+            for (int k = 0; k < N; ++k) all[k] = have == 0 ? v[k] : all[k] + __shfl_sync(0xffffffffu, v[k], from);
+            have += o;
         }
+        if (2 * o > n) break;
+        const int from = round(o);
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, v[k], first);
+        for (int k = 0; k < N; ++k) v[k] += __shfl_sync(0xffffffffu, v[k], from);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = all[k];
 }
 
 // What a CTA of the vector kernels keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its
 // axis, and the weights of both norms.
-struct HeadTables {
+template <int kParts> struct HeadTables {          // 0 parts: no weights, 1: of one operand, 2: of both
     uint2 turn[kMaxHeadDim / 2];
     int32_t axis[kMaxHeadDim / 2];
-    float w[2][kMaxHeadDim];
+    float w[kParts > 0 ? kParts : 1][kParts > 0 ? kMaxHeadDim : 1];
 };
 
-template <typename T, bool kNorm>
-__device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables& S) {
+template <typename T, int kParts>
+__device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables<kParts>& S, int first) {
     for (int j = threadIdx.x; j < A.rot / 2; j += kHeadThreads) {
         double t = freq_at(A, j) * 0.15915494309189533577;                   // 1 / (2 pi)
         t -= floor(t);
@@ -128,12 +136,11 @@ __device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables& S) {
         S.turn[j] = make_uint2((uint32_t)f, (uint32_t)(f >> 32));
         S.axis[j] = A.axes[j];
     }
-    if (kNorm)
-        for (int j = threadIdx.x; j < 2 * A.dim; j += kHeadThreads) {
-            const int which = j >= A.dim, i = j - (which ? A.dim : 0);
-            const void* w = which ? A.part[1].weight : A.part[0].weight;
-            S.w[which][i] = w != nullptr ? weight_of<T>(A, w, i) : 1.f;
-        }
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        const void* w = A.part[first + k].weight;
+        for (int j = threadIdx.x; j < A.dim; j += kHeadThreads) S.w[k][j] = w != nullptr ? weight_of<T>(A, w, j) : 1.f;
+    }
 }
 
 // cosine and sine of a position's turn.  The product of the position and the 64-bit fraction is taken modulo 2^64, that is
@@ -151,17 +158,24 @@ __device__ __forceinline__ void turn_by(int32_t position, uint2 turn, bool inver
     if (inverse) s = -s;
 }
 
-// Where the lanes of a warp stand: `chunk` of a row, which of the warp's rows, the two vectors of the chunk inside a head.
-template <int V, bool kNext> struct Place {
-    int nc, rows, sub, chunk, first, pair, o1, o2;
-    bool in_row, turns;
+// Where the lanes of a warp stand: number `at` of a row, which of the warp's rows, and the K chunks of the row that this
+// lane has: every `lanes`-th, two vectors each.
+template <int V, int K, bool kNext> struct Place {
+    int lanes, rows, sub, at, first;
+    int o1[K], o2[K], pair[K];
+    bool in_row, turns[K];
     __device__ __forceinline__ explicit Place(const HeadArgs& A) {
         const int lane = threadIdx.x & 31, turning = A.rot / (2 * V);
-        nc = A.chunks; rows = 32 / nc; sub = lane / nc; chunk = lane - sub * nc; first = sub * nc;
-        in_row = sub < rows; turns = chunk < turning; pair = chunk * V;
-        if (kNext) { o1 = 2 * V * chunk; o2 = o1 + V; }
-        else if (turns) { o1 = pair; o2 = pair + A.rot / 2; }
-        else { o1 = A.rot + 2 * V * (chunk - turning); o2 = o1 + V; }
+        lanes = A.lanes; rows = 32 / lanes; sub = lane / lanes; at = lane - sub * lanes; first = sub * lanes;
+        in_row = sub < rows;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int chunk = at + k * lanes;
+            turns[k] = chunk < turning; pair[k] = chunk * V;
+            if (kNext) { o1[k] = 2 * V * chunk; o2[k] = o1[k] + V; }
+            else if (turns[k]) { o1[k] = pair[k]; o2[k] = pair[k] + A.rot / 2; }
+            else { o1[k] = A.rot + 2 * V * (chunk - turning); o2[k] = o1[k] + V; }
+        }
     }
 };
 
@@ -173,110 +187,6 @@ template <int V, bool kNext> __device__ __forceinline__ float& two(float (&p)[V]
     return kNext ? (2 * i < V ? p[(2 * i + 1) % V] : q[(2 * i + 1) % V]) : q[i];
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void turns_of(const HeadArgs& A, const HeadTables& S, const int32_t (&p)[kMaxAxes], bool turns, int pair, float (&c)[V], float (&s)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        c[i] = 1.f; s[i] = 0.f;
-        if (turns) turn_by<T>(on_axis(p, S.axis[pair + i]), S.turn[pair + i], A.inverse, c[i], s[i]);
-    }
-}
-
-template <typename T, int V> struct Row { Vec<T, V> a, b; };
-template <typename T, int V>
-__device__ __forceinline__ Row<T, V> load_row(const T* x, int gap) {
-    return {*reinterpret_cast<const Vec<T, V>*>(x), *reinterpret_cast<const Vec<T, V>*>(x + gap)};
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_row(T* y, int gap, const float (&r1)[V], const float (&r2)[V]) {
-    Vec<T, V> y1, y2;
-#pragma unroll
-    for (int i = 0; i < V; ++i) { y1.v[i] = from_f<T>(r1[i]); y2.v[i] = from_f<T>(r2[i]); }
-    *reinterpret_cast<Vec<T, V>*>(y) = y1;
-    *reinterpret_cast<Vec<T, V>*>(y + gap) = y2;
-}
-__device__ __forceinline__ void soon(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
-
-// Forward: grid (token groups, shares of `per` heads of queries and keys in a row).  A warp takes 32 / chunks tokens, a
-// thread `per` heads of its token, kAhead of them at a time.  Lanes without a token go along with the last one's data and
-// store nothing: no shuffle and no load stands in a branch.
-template <typename T, int V, bool kNorm, bool kNext>
-__global__ void __launch_bounds__(kHeadThreads, kNorm ? 5 : 6) heads_kernel(const __grid_constant__ HeadArgs A) {
-    constexpr int kWarps = kHeadThreads / 32, kAhead = (V * sizeof(T) >= 16 ? 1 : 2) * 4;
-    __shared__ HeadTables S;
-    const Place<V, kNext> at(A);
-    const uint32_t n0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * (uint32_t)at.rows + (uint32_t)at.sub;
-    const bool live = at.in_row && n0 < A.tokens;
-    const uint32_t n = min(n0, A.tokens - 1), b = n / A.seq, t = n - b * A.seq;
-    const int gap = at.o2 - at.o1, from = (int)blockIdx.y * A.per, to = from + A.per;
-    int which = from < A.part[0].heads ? 0 : 1;
-    {   // the first row is on its way while the tables are filled
-        const HeadBlock& H = A.part[which];
-        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + (int64_t)(from - (which ? A.part[0].heads : 0)) * H.xs[2] + at.o1;
-        soon(x); soon(x + gap);
-    }
-    int32_t p[kMaxAxes];
-    positions_of(A, b, t, p);
-    fill_tables<T, kNorm>(A, S);
-    __syncthreads();
-    float c[V], s[V];
-    turns_of<T, V>(A, S, p, at.turns, at.pair, c, s);
-#pragma unroll 1
-    for (; which < 2; ++which) {
-        const HeadBlock& H = A.part[which];
-        const int base = which ? A.part[0].heads : 0;
-        const int h0 = max(from - base, 0), h1 = min(to - base, H.heads);
-        if (h0 >= h1) continue;
-        // a' = a wa c - b wb s, b' = a wa s + b wb c: four factors a pair, the same for all heads
-        float ac[V], as[V], bc[V], bs[V];
-        if (kNorm) {
-            float w1[V], w2[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) { w1[i] = S.w[which][at.o1 + i]; w2[i] = S.w[which][at.o2 + i]; }
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float wa = one<V, kNext>(w1, w2, i), wb = two<V, kNext>(w1, w2, i);
-                ac[i] = wa * c[i]; as[i] = wa * s[i]; bc[i] = wb * c[i]; bs[i] = wb * s[i];
-            }
-        }
-        const int64_t xs = H.xs[2], ys = H.ys[2];
-        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + h0 * xs + at.o1;
-        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + h0 * ys + at.o1;
-        auto work = [&](const Row<T, V>& row) {
-            float a1[V], a2[V], r[1] = {1.f};
-#pragma unroll
-            for (int i = 0; i < V; ++i) { a1[i] = to_f(row.a.v[i]); a2[i] = to_f(row.b.v[i]); }
-            if (kNorm) {
-                r[0] = 0.f;
-#pragma unroll
-                for (int i = 0; i < V; ++i) r[0] += a1[i] * a1[i] + a2[i] * a2[i];
-                row_sums<1>(r, at.first, at.chunk, at.nc);
-                r[0] = rsqrtf(r[0] * A.inv_dim + A.eps);
-            }
-            float r1[V], r2[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float a = one<V, kNext>(a1, a2, i) * r[0], e = two<V, kNext>(a1, a2, i) * r[0];
-                one<V, kNext>(r1, r2, i) = kNorm ? a * ac[i] - e * bs[i] : a * c[i] - e * s[i];
-                two<V, kNext>(r1, r2, i) = kNorm ? a * as[i] + e * bc[i] : a * s[i] + e * c[i];
-            }
-            if (live) store_row<T, V>(y, gap, r1, r2);
-            y += ys;
-        };
-        int h = h0;
-#pragma unroll 1
-        for (; h + kAhead <= h1; h += kAhead) {
-            Row<T, V> rows[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k, x += xs) rows[k] = load_row<T, V>(x, gap);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) work(rows[k]);
-        }
-#pragma unroll 1
-        for (; h < h1; ++h, x += xs) work(load_row<T, V>(x, gap));
-    }
-}
-
 // Two single-precision numbers in one register pair; the operations below take both in one instruction.
 using F2 = unsigned long long;
 __device__ __forceinline__ F2 pack2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
@@ -284,27 +194,166 @@ __device__ __forceinline__ void unpack2(F2 v, float& a, float& b) { asm("mov.b64
 __device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 
-// A row's pairs, two by two: first elements in a, second ones in b.
-template <int V> struct Pairs { F2 a[V / 2], b[V / 2]; };
-template <typename T, int V, bool kNext>
-__device__ __forceinline__ Pairs<V> pairs_of(const Row<T, V>& row) {
-    float f[V], g[V];
+// The chunks of a row that a lane has: as they lie in memory, and as pairs two by two, first elements in a, second in b.
+template <typename T, int V, int K> struct Row { Vec<T, V> a[K], b[K]; };
+template <int V, int K> struct Pairs { F2 a[K][V / 2], b[K][V / 2]; };
+
+template <typename T, int V, int K, bool kNext>
+__device__ __forceinline__ Row<T, V, K> load_row(const T* x, const Place<V, K, kNext>& at) {
+    Row<T, V, K> r;
 #pragma unroll
-    for (int i = 0; i < V; ++i) { f[i] = to_f(row.a.v[i]); g[i] = to_f(row.b.v[i]); }
-    Pairs<V> r;
+    for (int k = 0; k < K; ++k) { r.a[k] = *reinterpret_cast<const Vec<T, V>*>(x + at.o1[k]); r.b[k] = *reinterpret_cast<const Vec<T, V>*>(x + at.o2[k]); }
+    return r;
+}
+template <typename T, int V, int K, bool kNext>
+__device__ __forceinline__ Pairs<V, K> pairs_of(const Row<T, V, K>& row) {
+    Pairs<V, K> r;
 #pragma unroll
-    for (int i = 0; i < V; i += 2) {
-        r.a[i / 2] = pack2(one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
-        r.b[i / 2] = pack2(two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
+    for (int k = 0; k < K; ++k) {
+        float f[V], g[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) { f[i] = to_f(row.a[k].v[i]); g[i] = to_f(row.b[k].v[i]); }
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            r.a[k][i / 2] = pack2(one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
+            r.b[k][i / 2] = pack2(two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
+        }
     }
     return r;
 }
-template <int V, bool kNext>
-__device__ __forceinline__ void elements_of(const Pairs<V>& p, float (&f)[V], float (&g)[V]) {
+template <typename T, int V, int K, bool kNext>
+__device__ __forceinline__ Row<T, V, K> row_of(const Pairs<V, K>& p) {
+    Row<T, V, K> r;
 #pragma unroll
-    for (int i = 0; i < V; i += 2) {
-        unpack2(p.a[i / 2], one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
-        unpack2(p.b[i / 2], two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
+    for (int k = 0; k < K; ++k) {
+        float f[V], g[V];
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unpack2(p.a[k][i / 2], one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
+            unpack2(p.b[k][i / 2], two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) { r.a[k].v[i] = from_f<T>(f[i]); r.b[k].v[i] = from_f<T>(g[i]); }
+    }
+    return r;
+}
+template <typename T, int V, int K, bool kNext>
+__device__ __forceinline__ void store_row(T* y, const Place<V, K, kNext>& at, const Row<T, V, K>& r) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) { *reinterpret_cast<Vec<T, V>*>(y + at.o1[k]) = r.a[k]; *reinterpret_cast<Vec<T, V>*>(y + at.o2[k]) = r.b[k]; }
+}
+template <int V, int K, bool kNext>
+__device__ __forceinline__ Pairs<V, K> weights_of(const float* w, const Place<V, K, kNext>& at) {
+    return pairs_of<float, V, K, kNext>(load_row<float, V, K, kNext>(w, at));
+}
+// cosine and sine of the lane's pairs at a token's positions
+template <typename T, int V, int K, bool kNext, int kParts>
+__device__ __forceinline__ void turns_of(const HeadArgs& A, const HeadTables<kParts>& S, const int32_t (&p)[kMaxAxes], const Place<V, K, kNext>& at, F2 (&c)[K][V / 2], F2 (&s)[K][V / 2]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            float fc[2] = {1.f, 1.f}, fs[2] = {0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int pair = at.pair[k] + i + j;
+                if (at.turns[k]) turn_by<T>(on_axis(p, S.axis[pair]), S.turn[pair], A.inverse, fc[j], fs[j]);
+            }
+            c[k][i / 2] = pack2(fc[0], fc[1]); s[k][i / 2] = pack2(fs[0], fs[1]);
+        }
+}
+__device__ __forceinline__ F2 negative(F2 v) { return v ^ 0x8000000080000000ull; }
+__device__ __forceinline__ void soon(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+
+// Forward: grid (token groups, shares of `per` heads of queries and keys in a row).  A warp takes 32 / lanes tokens, a
+// thread `per` heads of its token, kAhead of them at a time.  Lanes without a token go along with the last one's data and
+// store nothing: no shuffle and no load stands in a branch.
+template <typename T, int V, int K, bool kNorm, bool kNext>
+__global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? (kNorm ? 3 : 4) : kNorm ? 5 : 6) heads_kernel(const __grid_constant__ HeadArgs A) {
+    constexpr int kWarps = kHeadThreads / 32, kBytes = V * K * (int)sizeof(T), kAhead = kBytes > 16 ? 2 : kBytes > 8 ? 4 : 8;
+    __shared__ HeadTables<kNorm ? 2 : 0> S;
+    const Place<V, K, kNext> at(A);
+    const uint32_t n0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * (uint32_t)at.rows + (uint32_t)at.sub;
+    const bool live = at.in_row && n0 < A.tokens;
+    const uint32_t n = min(n0, A.tokens - 1), b = n / A.seq, t = n - b * A.seq;
+    const int from = (int)blockIdx.y * A.per, to = from + A.per;
+    int which = from < A.part[0].heads ? 0 : 1;
+    {   // the first row is on its way while the tables are filled
+        const HeadBlock& H = A.part[which];
+        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + (int64_t)(from - (which ? A.part[0].heads : 0)) * H.xs[2];
+#pragma unroll
+        for (int k = 0; k < K; ++k) { soon(x + at.o1[k]); soon(x + at.o2[k]); }
+    }
+    int32_t p[kMaxAxes];
+    positions_of(A, b, t, p);
+    fill_tables<T>(A, S, 0);
+    __syncthreads();
+    F2 c[K][V / 2], s[K][V / 2];
+    turns_of<T, V, K, kNext>(A, S, p, at, c, s);
+#pragma unroll 1
+    for (; which < 2; ++which) {
+        const HeadBlock& H = A.part[which];
+        const int base = which ? A.part[0].heads : 0;
+        const int h0 = max(from - base, 0), h1 = min(to - base, H.heads);
+        if (h0 >= h1) continue;
+        // a' = a wa c + b (-wb s), b' = a wa s + b wb c: four factors a pair, the same for all heads
+        F2 ac[K][V / 2], as[K][V / 2], bc[K][V / 2], bs[K][V / 2];
+        {
+            Pairs<V, K> w;
+            if (kNorm) w = weights_of<V, K, kNext>(S.w[kNorm ? which : 0], at);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) {
+                    ac[k][i] = kNorm ? mul2(w.a[k][i], c[k][i]) : c[k][i];
+                    as[k][i] = kNorm ? mul2(w.a[k][i], s[k][i]) : s[k][i];
+                    bc[k][i] = kNorm ? mul2(w.b[k][i], c[k][i]) : c[k][i];
+                    bs[k][i] = negative(kNorm ? mul2(w.b[k][i], s[k][i]) : s[k][i]);
+                }
+        }
+        const int64_t xs = H.xs[2], ys = H.ys[2];
+        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + h0 * xs;
+        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + h0 * ys;
+        auto work = [&](const Row<T, V, K>& row) {
+            Pairs<V, K> v = pairs_of<T, V, K, kNext>(row);
+            if (kNorm) {
+                F2 sq = 0;
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < V / 2; ++i) { sq = fma2(v.a[k][i], v.a[k][i], sq); sq = fma2(v.b[k][i], v.b[k][i], sq); }
+                float sum[1], other;
+                unpack2(sq, sum[0], other);
+                sum[0] += other;
+                row_sums<1>(sum, at.first, at.at, at.lanes);
+                const float r = rsqrtf(sum[0] * A.inv_dim + A.eps);
+                const F2 r2 = pack2(r, r);
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < V / 2; ++i) { v.a[k][i] = mul2(v.a[k][i], r2); v.b[k][i] = mul2(v.b[k][i], r2); }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) {
+                    const F2 u = fma2(v.b[k][i], bs[k][i], mul2(v.a[k][i], ac[k][i])), e = fma2(v.b[k][i], bc[k][i], mul2(v.a[k][i], as[k][i]));
+                    v.a[k][i] = u; v.b[k][i] = e;
+                }
+            if (live) store_row<T, V, K, kNext>(y, at, row_of<T, V, K, kNext>(v));
+            y += ys;
+        };
+        int h = h0;
+#pragma unroll 1
+        for (; h + kAhead <= h1; h += kAhead) {
+            Row<T, V, K> rows[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k, x += xs) rows[k] = load_row<T, V, K, kNext>(x, at);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) work(rows[k]);
+        }
+#pragma unroll 1
+        for (; h < h1; ++h, x += xs) work(load_row<T, V, K, kNext>(x, at));
     }
 }
 
@@ -318,21 +367,20 @@ template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatil
 // Backward: the first part[0].slots CTAs take the queries, the others the keys; a warp goes round the tokens and over all
 // heads of each, so that the sums for the weights stay in registers to the end.
 //   q = d a, dot = sum of q w, dw += q r, dx = r (d w - a r^2 dot / dim)
-// Two operands, their factors and the sums leave no registers for rows on their way, and a row's work is a long chain of
-// dependent steps.  So every lane has a ring of kStages groups of rows in shared memory that it alone fills and reads: no
-// barrier, and kStages - 1 groups are always on their way.
-template <typename T, int V, bool kNext>
-__global__ void __launch_bounds__(kHeadThreads, 4) heads_back_kernel(const __grid_constant__ HeadArgs A) {
-    constexpr int kWarps = kHeadThreads / 32, kStages = 4, N = V / 2, kBytes = V * (int)sizeof(T), kGroup = kBytes >= 16 ? 1 : 2;
+// Two operands, their factors and the sums leave no registers for rows on their way.  So every lane has a ring of kStages
+// groups of rows in shared memory that it alone fills and reads: no barrier, and kStages - 1 groups are always on their way.
+template <typename T, int V, int K, bool kNext>
+__global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? 3 : 4) heads_back_kernel(const __grid_constant__ HeadArgs A) {
+    constexpr int kWarps = kHeadThreads / 32, kBytes = V * (int)sizeof(T), kGroup = kBytes * K >= 16 ? 1 : 2, kStages = kBytes * K * kGroup > 24 ? 2 : kBytes * K * kGroup > 16 ? 3 : 4, N = V / 2;
     using VT = Vec<T, V>;
-    struct Ring { VT rows[kStages][kGroup][4][32]; int32_t positions[kStages][kMaxAxes][32]; };
-    __shared__ HeadTables S;
+    struct Ring { VT rows[kStages][kGroup][K][4][32]; int32_t positions[kStages][kMaxAxes][32]; };
+    __shared__ HeadTables<1> S;
     __shared__ union { Ring ring[kWarps]; float sums[kWarps][kMaxHeadDim]; } U;
     const int which = (int)blockIdx.x >= A.part[0].slots ? 1 : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const HeadBlock& H = A.part[which];
     const uint32_t mine = blockIdx.x - (which ? (uint32_t)A.part[0].slots : 0u);
-    const Place<V, kNext> at(A);
-    const int gap = at.o2 - at.o1, heads = H.heads;
+    const Place<V, K, kNext> at(A);
+    const int heads = H.heads;
     const int64_t xs = H.xs[2], gs = H.gs[2], ys = H.ys[2];
     const uint64_t step = (uint64_t)H.slots * kWarps * at.rows, begin = (uint64_t)(mine * kWarps + warp) * at.rows;
     Ring& R = U.ring[warp];
@@ -350,46 +398,47 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_back_kernel(const __gri
             if (fhead == 0) {
                 uint32_t b, t;
                 token_of(fbase, b, t);
-                fx = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + at.o1;
-                fg = static_cast<const T*>(H.g) + (int64_t)b * H.gs[0] + (int64_t)t * H.gs[1] + at.o1;
+                fx = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1];
+                fg = static_cast<const T*>(H.g) + (int64_t)b * H.gs[0] + (int64_t)t * H.gs[1];
                 const int32_t* p = A.positions + (int64_t)b * A.ps[1] + (int64_t)t * A.ps[2];
 #pragma unroll
                 for (int a = 0; a < kMaxAxes; ++a)
                     if (a < A.n_axes) copy_soon<4>(&R.positions[fstage][a][lane], p + (int64_t)a * A.ps[0]);
             }
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k, fx += xs, fg += gs)
-                if (fhead + k < heads) {
-                    copy_soon<kBytes>(&R.rows[fstage][k][0][lane], fx); copy_soon<kBytes>(&R.rows[fstage][k][1][lane], fx + gap);
-                    copy_soon<kBytes>(&R.rows[fstage][k][2][lane], fg); copy_soon<kBytes>(&R.rows[fstage][k][3][lane], fg + gap);
+            for (int m = 0; m < kGroup; ++m, fx += xs, fg += gs)
+                if (fhead + m < heads) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        VT(*to)[32] = R.rows[fstage][m][k];
+                        copy_soon<kBytes>(&to[0][lane], fx + at.o1[k]); copy_soon<kBytes>(&to[1][lane], fx + at.o2[k]);
+                        copy_soon<kBytes>(&to[2][lane], fg + at.o1[k]); copy_soon<kBytes>(&to[3][lane], fg + at.o2[k]);
+                    }
                 }
             fhead += kGroup;
             if (fhead >= heads) { fhead = 0; fbase += step; }
         }
-        fstage = (fstage + 1) % kStages;
+        fstage = fstage + 1 == kStages ? 0 : fstage + 1;
         copies_close();
     };
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < kStages - 1; ++k) fill();
-    fill_tables<T, true>(A, S);
+    fill_tables<T>(A, S, which);
     __syncthreads();
-    Pairs<V> w, dw;
-    {
-        Row<float, V> r;
+    const Pairs<V, K> w = weights_of<V, K, kNext>(S.w[0], at);
+    Pairs<V, K> dw;
 #pragma unroll
-        for (int i = 0; i < V; ++i) { r.a.v[i] = S.w[which][at.o1 + i]; r.b.v[i] = S.w[which][at.o2 + i]; }
-        w = pairs_of<float, V, kNext>(r);
-    }
+    for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int i = 0; i < N; ++i) dw.a[i] = dw.b[i] = 0;
+        for (int i = 0; i < N; ++i) dw.a[k][i] = dw.b[k][i] = 0;
     int stage = 0;
 #pragma unroll 1
     for (uint64_t base = begin; base < A.tokens; base += step) {
         const bool live = at.in_row && base + at.sub < A.tokens;
         uint32_t b, t;
         token_of(base, b, t);
-        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + at.o1;
-        F2 c[N], s[N], ns[N];
+        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1];
+        F2 c[K][N], s[K][N];
 #pragma unroll 1
         for (int h = 0; h < heads; h += kGroup) {
             copies_wait<kStages - 2>();
@@ -397,46 +446,47 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_back_kernel(const __gri
                 int32_t p[kMaxAxes];
 #pragma unroll
                 for (int a = 0; a < kMaxAxes; ++a) p[a] = a < A.n_axes ? R.positions[stage][a][lane] : 0;
-                float fc[V], fs[V];
-                turns_of<T, V>(A, S, p, at.turns, at.pair, fc, fs);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    c[i] = pack2(fc[2 * i], fc[2 * i + 1]); s[i] = pack2(fs[2 * i], fs[2 * i + 1]); ns[i] = pack2(-fs[2 * i], -fs[2 * i + 1]);
-                }
+                turns_of<T, V, K, kNext>(A, S, p, at, c, s);
             }
-            auto work = [&](int k) {
-                const VT* from = &R.rows[stage][k][0][lane];
-                const Row<T, V> row = {from[0], from[32]}, grow = {from[64], from[96]};
-                const Pairs<V> x2 = pairs_of<T, V, kNext>(row);
-                Pairs<V> d = pairs_of<T, V, kNext>(grow), q;
+            auto work = [&](int m) {
+                Row<T, V, K> row, grow;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    VT(*from)[32] = R.rows[stage][m][k];
+                    row.a[k] = from[0][lane]; row.b[k] = from[1][lane]; grow.a[k] = from[2][lane]; grow.b[k] = from[3][lane];
+                }
+                const Pairs<V, K> x2 = pairs_of<T, V, K, kNext>(row);
+                Pairs<V, K> d = pairs_of<T, V, K, kNext>(grow), q;
                 F2 sq = 0, dot = 0;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const F2 u = fma2(d.b[i], s[i], mul2(d.a[i], c[i])), v = fma2(d.a[i], ns[i], mul2(d.b[i], c[i]));
-                    q.a[i] = mul2(u, x2.a[i]); q.b[i] = mul2(v, x2.b[i]);
-                    sq = fma2(x2.a[i], x2.a[i], sq); sq = fma2(x2.b[i], x2.b[i], sq);
-                    dot = fma2(q.a[i], w.a[i], dot); dot = fma2(q.b[i], w.b[i], dot);
-                    d.a[i] = mul2(u, w.a[i]); d.b[i] = mul2(v, w.b[i]);
-                }
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const F2 u = fma2(d.b[k][i], s[k][i], mul2(d.a[k][i], c[k][i])), v = fma2(d.a[k][i], negative(s[k][i]), mul2(d.b[k][i], c[k][i]));
+                        q.a[k][i] = mul2(u, x2.a[k][i]); q.b[k][i] = mul2(v, x2.b[k][i]);
+                        sq = fma2(x2.a[k][i], x2.a[k][i], sq); sq = fma2(x2.b[k][i], x2.b[k][i], sq);
+                        dot = fma2(q.a[k][i], w.a[k][i], dot); dot = fma2(q.b[k][i], w.b[k][i], dot);
+                        d.a[k][i] = mul2(u, w.a[k][i]); d.b[k][i] = mul2(v, w.b[k][i]);
+                    }
                 float sum[2], other[2];
                 unpack2(sq, sum[0], other[0]); unpack2(dot, sum[1], other[1]);
                 sum[0] += other[0]; sum[1] += other[1];
-                row_sums<2>(sum, at.first, at.chunk, at.nc);
-                const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m = -(sum[1] * r * A.inv_dim * r), rl = live ? r : 0.f;
-                const F2 r2 = pack2(r, r), m2 = pack2(m, m), rl2 = pack2(rl, rl);
+                row_sums<2>(sum, at.first, at.at, at.lanes);
+                const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m1 = -(sum[1] * r * A.inv_dim * r), rl = live ? r : 0.f;
+                const F2 r2 = pack2(r, r), m2 = pack2(m1, m1), rl2 = pack2(rl, rl);
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    d.a[i] = mul2(fma2(x2.a[i], m2, d.a[i]), r2); d.b[i] = mul2(fma2(x2.b[i], m2, d.b[i]), r2);
-                    dw.a[i] = fma2(q.a[i], rl2, dw.a[i]); dw.b[i] = fma2(q.b[i], rl2, dw.b[i]);
-                }
-                float y1[V], y2[V];
-                elements_of<V, kNext>(d, y1, y2);
-                if (live) store_row<T, V>(y, gap, y1, y2);
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        d.a[k][i] = mul2(fma2(x2.a[k][i], m2, d.a[k][i]), r2); d.b[k][i] = mul2(fma2(x2.b[k][i], m2, d.b[k][i]), r2);
+                        dw.a[k][i] = fma2(q.a[k][i], rl2, dw.a[k][i]); dw.b[k][i] = fma2(q.b[k][i], rl2, dw.b[k][i]);
+                    }
+                if (live) store_row<T, V, K, kNext>(y, at, row_of<T, V, K, kNext>(d));
                 y += ys;
             };
-            if (kGroup == 2 && h + 2 <= heads) { work(0); work(1); }
+            if (kGroup == 2 && h + 2 <= heads) { work(0); work(kGroup - 1); }
             else work(0);
-            stage = (stage + 1) % kStages;
+            stage = stage + 1 == kStages ? 0 : stage + 1;
             fill();
         }
     }
@@ -444,17 +494,18 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_back_kernel(const __gri
     if (H.partial == nullptr) return;                           // (the same for the whole CTA)
     __syncthreads();                                            // the rings make room for the sums
     // the rows of a warp in the order of their lanes, then the warps in theirs
-    float dw1[V], dw2[V];
-    elements_of<V, kNext>(dw, dw1, dw2);
+    const Row<float, V, K> mine_dw = row_of<float, V, K, kNext>(dw);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        float p = dw1[i], q = dw2[i];
-        for (int k = 1; k < at.rows; ++k) {
-            const float pk = __shfl_sync(0xffffffffu, dw1[i], at.chunk + k * at.nc), qk = __shfl_sync(0xffffffffu, dw2[i], at.chunk + k * at.nc);
-            p += pk; q += qk;
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float p = mine_dw.a[k].v[i], q = mine_dw.b[k].v[i];
+            for (int m = 1; m < at.rows; ++m) {
+                const int from = at.at + m * at.lanes;
+                p += __shfl_sync(0xffffffffu, mine_dw.a[k].v[i], from); q += __shfl_sync(0xffffffffu, mine_dw.b[k].v[i], from);
+            }
+            if (at.sub == 0) { U.sums[warp][at.o1[k] + i] = p; U.sums[warp][at.o2[k] + i] = q; }
         }
-        if (at.sub == 0) { U.sums[warp][at.o1 + i] = p; U.sums[warp][at.o2 + i] = q; }
-    }
     __syncthreads();
     float* out = H.partial + (size_t)mine * A.dim;
     for (int j = threadIdx.x; j < A.dim; j += kHeadThreads) {

@@ -35,69 +35,74 @@ __device__ __forceinline__ Tap tap_of(int32_t o, int32_t out, int32_t side) {
         const int32_t den = 2 * out;
         const int32_t num = min(max((2 * o + 1) * side - out, 0), (side - 1) * den);
         t.lo = (int32_t)((uint32_t)num / (uint32_t)den);
-        t.f = (float)(num - t.lo * den) / (float)den;
+        t.f = __fdividef((float)(num - t.lo * den), (float)den);         // (off by 2 units in the last place at most)
     } else {
         const int64_t den = 2 * (int64_t)out;
         const int64_t num = min(max((2 * (int64_t)o + 1) * side - out, (int64_t)0), (side - 1) * den);
         t.lo = (int32_t)(num / den);
-        t.f = (float)(num - t.lo * den) / (float)den;
+        t.f = __fdividef((float)(num - t.lo * den), (float)den);
     }
     return t;
 }
 
 // Whether a token's entry stands for a patch of pixels that are there.
 __device__ __forceinline__ bool patch_ok(const PatchArgs& A, const PatchImage& m, int32_t local) {
-    const int64_t p = A.patch;
-    return m.width >= 1 && m.width <= kMaxSide && m.height >= 1 && m.height <= kMaxSide && m.offset >= 0 &&
-           (uint64_t)m.offset <= A.rgb_bytes && (uint64_t)(3 * m.width * m.height) <= A.rgb_bytes - (uint64_t)m.offset &&
+    const int64_t most = kMaxSide / A.patch;
+    if (m.width < 1 || m.width > kMaxSide || m.height < 1 || m.height > kMaxSide || m.offset < 0 || m.rows < 1 || m.cols < 1 || m.rows > most || m.cols > most) return false;
+    const int32_t rows = (int32_t)m.rows, cols = (int32_t)m.cols;
+    return (uint64_t)m.offset <= A.rgb_bytes && (uint64_t)(3 * m.width * m.height) <= A.rgb_bytes - (uint64_t)m.offset &&
            m.x0 >= 0 && m.y0 >= 0 && m.w >= 1 && m.h >= 1 && m.w <= m.width && m.h <= m.height && m.x0 <= m.width - m.w &&
-           m.y0 <= m.height - m.h && m.rows >= 1 && m.cols >= 1 && m.rows <= kMaxSide / p && m.cols <= kMaxSide / p &&
-           m.rows % A.merge == 0 && m.cols % A.merge == 0 && (m.flip == 0 || m.flip == 1) && local >= 0 && local < m.rows * m.cols;
+           m.y0 <= m.height - m.h && rows % A.merge == 0 && cols % A.merge == 0 && (m.flip == 0 || m.flip == 1) && local >= 0 &&
+           local < m.rows * m.cols;
 }
 
-__device__ __forceinline__ float byte_f(uint32_t word, int i) {          // byte i of a word: exact through 2^23 + byte
-    return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440u | (uint32_t)i)) - 8388608.f;
-}
+// Bytes become floats as 2^23 + byte, exactly; differences need no more, what is added to has the 2^23 taken off.
+__device__ __forceinline__ float byte_up(uint32_t word, int i) { return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440u | (uint32_t)i)); }
+constexpr float kUp = 8388608.f;
 
-// The two pixels from byte `at` of the buffer on, mixed: aligned words where they lie inside the buffer.
-__device__ __forceinline__ void mix_pixels(const PatchArgs& A, uint64_t at, float f, float (&v)[3]) {
-    uint32_t lo, hi;
-    const uint64_t word = at & ~3ull;
-    if (word + 12 <= A.rgb_bytes) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(A.rgb + word);
-        const uint32_t sh = (uint32_t)(at & 3) * 8, w0 = __ldg(p), w1 = __ldg(p + 1), w2 = sh == 24 ? __ldg(p + 2) : 0;
-        lo = __funnelshift_r(w0, w1, sh);
-        hi = __funnelshift_r(w1, w2, sh);
-    } else {                                                             // (a tap of weight 0 may lie behind the last pixel)
-        lo = A.rgb[at] | (uint32_t)A.rgb[at + 1] << 8 | (uint32_t)A.rgb[at + 2] << 16;
-        hi = 0;
-        if (f != 0.f) {
-            lo |= (uint32_t)A.rgb[at + 3] << 24;
-            hi = A.rgb[at + 4] | (uint32_t)A.rgb[at + 5] << 8;
-        }
-    }
-    const float r0 = byte_f(lo, 0), g0 = byte_f(lo, 1), b0 = byte_f(lo, 2), r1 = byte_f(lo, 3), g1 = byte_f(hi, 0), b1 = byte_f(hi, 1);
-    v[0] = r0 + f * (r1 - r0); v[1] = g0 + f * (g1 - g0); v[2] = b0 + f * (b1 - b0);
+struct Rgb { F2 rg; float b; };
+
+// The pixel whose bytes are the lowest three of `lo` mixed with the next one (fourth byte of `lo`, two of `hi`).
+__device__ __forceinline__ Rgb mix_bytes(uint32_t lo, uint32_t hi, float f) {
+    const F2 a = pack2(byte_up(lo, 0), byte_up(lo, 1)), e = pack2(byte_up(lo, 3), byte_up(hi, 0));
+    const float ab = byte_up(lo, 2), eb = byte_up(hi, 1);
+    return {fma2(pack2(f, f), fma2(a, pack2(-1.f, -1.f), e), fma2(a, pack2(1.f, 1.f), pack2(-kUp, -kUp))), fmaf(f, eb - ab, ab - kUp)};
+}
+// ... read as aligned words, which have to lie inside the buffer
+__device__ __forceinline__ Rgb mix_words(const uint8_t* at, float f) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
+    const uint32_t sh = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 3) * 8, w0 = __ldg(p), w1 = __ldg(p + 1);
+    uint32_t w2 = 0;
+    if (sh == 24) w2 = __ldg(p + 2);
+    return mix_bytes(__funnelshift_r(w0, w1, sh), __funnelshift_r(w1, w2, sh), f);
+}
+// ... byte by byte, the next pixel only where it counts: it may lie behind the last one
+__device__ __forceinline__ Rgb mix_single(const uint8_t* at, float f) {
+    uint32_t lo = at[0] | (uint32_t)at[1] << 8 | (uint32_t)at[2] << 16, hi = 0;
+    if (f != 0.f) { lo |= (uint32_t)at[3] << 24; hi = at[4] | (uint32_t)at[5] << 8; }
+    return mix_bytes(lo, hi, f);
 }
 
 // A lane a column of a patch, walking down its rows: a source row that serves two output rows is read and mixed once.
-// A warp takes 32 / patch tokens; their values meet in shared memory and leave as whole vectors.
+// A warp takes 32 / patch tokens; their values meet in shared memory and leave as whole vectors.  Every lane asks for one
+// of the source rows before the walk begins, so that the rows arrive together and not one after the other.
 template <typename T>
 __global__ void __launch_bounds__(32 * kPatchWarps) patch_tokens_kernel(const __grid_constant__ PatchArgs A) {
     extern __shared__ __align__(16) unsigned char s_raw[];
+    __shared__ float2 s_rows[kPatchWarps][32];                    // (first byte of the upper source row as bits, weight of the lower)
     const int p = A.patch, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int each = 32 / p, area = p * p, values = 3 * area;
     const int sub = lane / p, px = lane - sub * p;
-    const size_t own = ((size_t)each * values * sizeof(T) + 15) / 16 * 16;
+    const uint32_t own = ((uint32_t)(each * values) * (uint32_t)sizeof(T) + 15) / 16 * 16;
     T* const buf = reinterpret_cast<T*>(s_raw + warp * own);
-    const uint64_t first = ((uint64_t)blockIdx.x * kPatchWarps + warp) * (uint64_t)each;
+    const uint64_t first = ((uint64_t)blockIdx.x * (blockDim.x >> 5) + warp) * (uint64_t)each;
     if (first >= A.n_tokens) return;
     const int count = (int)min((uint64_t)each, A.n_tokens - first);
     const bool here = sub < count;
-    bool ok = false;
-    int64_t corner = 0, pitch = 0;        // first byte of the rectangle, bytes of a row
-    Tap tx = {0, 0.f}, ty = {0, 0.f};     // this lane's column; the row that has this lane's number
-    int32_t h = 1;
+    bool ok = false, words = false;
+    const uint8_t* base = nullptr;        // the rectangle's first row at this lane's column
+    int64_t pitch = 0;
+    float fx = 0.f;
     if (here) {
         const int2 at = A.index[first + sub];
         if (at.x >= 0 && at.x < A.n_images) {
@@ -105,41 +110,66 @@ __global__ void __launch_bounds__(32 * kPatchWarps) patch_tokens_kernel(const __
             ok = patch_ok(A, m, at.y);
             if (ok) {
                 const int32_t cols = (int32_t)m.cols, mg = A.merge, band = mg * cols;
-                const int32_t block = at.y / band, rest = at.y - block * band;
-                const int32_t in = rest % (mg * mg);
-                const int32_t row = block * mg + in / mg, col = rest / (mg * mg) * mg + in % mg;
+                const int32_t block = at.y / band, rest = at.y - block * band, square = mg * mg;
+                const int32_t side = rest / square, in = rest - side * square;
+                const int32_t row = block * mg + in / mg, col = side * mg + in % mg;
                 int32_t ox = col * p + px;
                 if (m.flip) ox = cols * p - 1 - ox;
-                tx = tap_of(ox, cols * p, (int32_t)m.w);
-                ty = tap_of(row * p + px, (int32_t)m.rows * p, (int32_t)m.h);
+                const Tap tx = tap_of(ox, cols * p, (int32_t)m.w), ty = tap_of(row * p + px, (int32_t)m.rows * p, (int32_t)m.h);
                 pitch = 3 * m.width;
-                corner = m.offset + m.y0 * pitch + 3 * m.x0;
-                h = (int32_t)m.h;
+                fx = tx.f;
+                const int64_t corner = m.offset + m.y0 * pitch + 3 * m.x0;
+                base = A.rgb + corner + 3 * (int64_t)tx.lo;
+                // rows are counted in bytes from the first, 32 bits; words are read where none can end behind the buffer
+                words = m.h * pitch < (int64_t)1 << 31 && (uint64_t)(corner + (m.h - 1) * pitch + 3 * m.w + 12) <= A.rgb_bytes;
+                const uint32_t off = words ? (uint32_t)ty.lo * (uint32_t)pitch : (uint32_t)ty.lo;
+                s_rows[warp][lane] = make_float2(__uint_as_float(off), ty.f);
+                if (words) {
+                    const uint8_t* row0 = base - 3 * (int64_t)px + off;       // about where the patch's part of this row begins: no more than a hint
+                    if (row0 >= A.rgb && row0 + 3 * p < A.rgb + A.rgb_bytes) { soon(row0); soon(row0 + 3 * p); }
+                }
             }
         }
     }
-    const int64_t left = corner + 3 * (int64_t)tx.lo;
-    T* o = buf + (here ? sub * values + px : 0);
-    float top[3] = {0.f, 0.f, 0.f}, low[3] = {0.f, 0.f, 0.f};
-    int32_t top_row = -1, low_row = -1;
-    for (int dy = 0; dy < p; ++dy, o += p) {
-        const int from = min(sub * p + dy, 31);
-        const int32_t ya = __shfl_sync(0xffffffffu, ty.lo, from);
-        const float fy = __shfl_sync(0xffffffffu, ty.f, from);
-        if (!here) continue;
-        float v[3] = {0.f, 0.f, 0.f};
-        if (ok) {
-            const int32_t yb = min(ya + 1, h - 1);
-            if (ya != top_row) {
-                if (ya == low_row) { top[0] = low[0]; top[1] = low[1]; top[2] = low[2]; }
-                else mix_pixels(A, (uint64_t)(left + ya * pitch), tx.f, top);
-                top_row = ya;
+    __syncwarp();
+    if (here) {
+        T* o = buf + sub * values + px;
+        const F2 scale = pack2(A.scale[0], A.scale[1]), shift = pack2(A.shift[0], A.shift[1]), minus = pack2(-1.f, -1.f);
+        auto put = [&](const Rgb& top, const Rgb& low, float fy) {
+            const F2 rg = fma2(fma2(pack2(fy, fy), fma2(top.rg, minus, low.rg), top.rg), scale, shift);
+            float r, g;
+            unpack2(rg, r, g);
+            o[0] = from_f<T>(r); o[area] = from_f<T>(g); o[2 * area] = from_f<T>(fmaf(fmaf(fy, low.b - top.b, top.b), A.scale[2], A.shift[2]));
+            o += p;
+        };
+        const float2* rows = &s_rows[warp][sub * p];
+        if (words) {
+            Rgb top = {0, 0.f}, low = {0, 0.f};
+            uint32_t top_at = ~0u, low_at = ~0u;
+            const uint32_t down = (uint32_t)pitch;
+            for (int dy = 0; dy < p; ++dy) {
+                const float2 r = rows[dy];
+                const uint32_t a = __float_as_uint(r.x), e = r.y != 0.f ? a + down : a;     // (weight 0: the row below may not be there)
+                if (a != top_at) {
+                    if (a == low_at) top = low; else top = mix_words(base + a, fx);
+                    top_at = a;
+                }
+                if (e != low_at) {
+                    if (e == top_at) low = top; else low = mix_words(base + e, fx);
+                    low_at = e;
+                }
+                put(top, low, r.y);
             }
-            if (yb != low_row) { mix_pixels(A, (uint64_t)(left + yb * pitch), tx.f, low); low_row = yb; }
-#pragma unroll
-            for (int c = 0; c < 3; ++c) v[c] = (top[c] + fy * (low[c] - top[c])) * A.scale[c] + A.shift[c];
+        } else if (ok) {
+            for (int dy = 0; dy < p; ++dy) {
+                const float2 r = rows[dy];
+                const uint8_t* a = base + (int64_t)__float_as_uint(r.x) * pitch;
+                const Rgb top = mix_single(a, fx), low = r.y != 0.f ? mix_single(a + pitch, fx) : top;
+                put(top, low, r.y);
+            }
+        } else {
+            for (int dy = 0; dy < p; ++dy, o += p) o[0] = o[area] = o[2 * area] = from_f<T>(0.f);
         }
-        o[0] = from_f<T>(v[0]); o[area] = from_f<T>(v[1]); o[2 * area] = from_f<T>(v[2]);
     }
     __syncwarp();
     const uint32_t bytes = (uint32_t)(count * values * (int)sizeof(T));
@@ -166,29 +196,79 @@ struct PositionArgs {
     int32_t* positions;
     int32_t* next;
     int64_t stride;                // of the axes of `positions`
-    uint32_t n_tokens;
+    uint32_t n_tokens, run;        // run: tokens of a CTA
     int32_t n_segments, n_sequences, merge, time_step, restart, zero_tail;
 };
 
 __device__ __forceinline__ void segment_sizes(const PositionArgs& A, const int4& s, int64_t& count, int64_t& extent) {
-    if (s.y <= 0 || s.z <= 0) { count = extent = max(s.x, 0); return; }
-    const int64_t t = max(s.x, 0);
-    const unsigned __int128 all = (unsigned __int128)t * (uint64_t)s.y * (uint64_t)s.z;
-    count = all > ((uint64_t)1 << 32) ? (int64_t)1 << 32 : (int64_t)all;       // (more than any output holds)
-    extent = t == 0 ? 0 : max((t - 1) * A.time_step, (int64_t)max(s.y, s.z) - 1) + 1;
+    const int32_t t = max(s.x, 0);
+    if (s.y <= 0 || s.z <= 0) { count = extent = t; return; }
+    const uint64_t plane = (uint64_t)(uint32_t)s.y * (uint32_t)s.z, most = (uint64_t)1 << 32;
+    count = t == 0 ? 0 : (int64_t)min(min(plane, most) * (uint32_t)t, most);       // (more than any output holds)
+    extent = t == 0 ? 0 : max((int64_t)(t - 1) * A.time_step, (int64_t)max(s.y, s.z) - 1) + 1;
 }
 
-// One CTA: every thread sums a run of segments, the runs' sums meet in shared memory, every thread goes over its run again.
+// Positions of token number l of a segment that begins at position `base`.
+__device__ __forceinline__ void position_in(const PositionArgs& A, const int4& s, int32_t base, uint32_t l, int32_t& pt, int32_t& ph, int32_t& pw) {
+    if (s.y <= 0 || s.z <= 0) { pt = ph = pw = base + (int32_t)l; return; }
+    const uint64_t plane = (uint64_t)(uint32_t)s.y * (uint32_t)s.z;
+    uint32_t f = 0, rest = l, row, col;
+    if ((plane >> 32) == 0) { f = l / (uint32_t)plane; rest = l - f * (uint32_t)plane; }
+    const uint32_t m = (uint32_t)A.merge;
+    if (m > 1 && s.y % A.merge == 0 && s.z % A.merge == 0) {
+        const uint64_t band = (uint64_t)m * (uint32_t)s.z;
+        const uint32_t block = band >> 32 ? 0 : rest / (uint32_t)band, in = rest - block * (uint32_t)band, q = in % (m * m);
+        row = block * m + q / m; col = in / (m * m) * m + q % m;
+    } else {
+        row = rest / (uint32_t)s.z; col = rest - row * (uint32_t)s.z;
+    }
+    pt = base + (int32_t)f * A.time_step; ph = base + (int32_t)row; pw = base + (int32_t)col;
+}
+
+// Sums over the threads before this one, of kScanThreads threads: tokens, and positions since the last begin of a sequence
+// (`first`: whether one lies in this thread's share).  In: the thread's own; out: those before it.  `total`: all tokens.
 constexpr int kScanThreads = 1024;
-__global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __grid_constant__ PositionArgs A) {
-    __shared__ int64_t s_tokens[kScanThreads], s_extent[kScanThreads];
-    __shared__ int32_t s_first[kScanThreads];       // whether a sequence begins inside the run
+__device__ __forceinline__ void sums_before(int64_t& tokens, int64_t& extent, bool first, int64_t& total) {
+    __shared__ int64_t s_tokens[32], s_extent[32];
+    __shared__ int32_t s_first[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto scan = [&](int64_t& t, int64_t& e, int32_t& f) {                // inclusive, over a warp
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t t2 = __shfl_up_sync(0xffffffffu, t, o), e2 = __shfl_up_sync(0xffffffffu, e, o);
+            const int32_t f2 = __shfl_up_sync(0xffffffffu, f, o);
+            if (lane >= o) { t += t2; if (!f) e += e2; f |= f2; }
+        }
+    };
+    int64_t t = tokens, e = extent;
+    int32_t f = first;
+    scan(t, e, f);
+    if (lane == 31) { s_tokens[warp] = t; s_extent[warp] = e; s_first[warp] = f; }
+    __syncthreads();
+    int64_t wt = s_tokens[lane], we = s_extent[lane];
+    int32_t wf = s_first[lane];
+    scan(wt, we, wf);
+    total = __shfl_sync(0xffffffffu, wt, 31);
+    // the warps before, then the lanes before
+    const int64_t bt = __shfl_sync(0xffffffffu, wt, max(warp - 1, 0)), be = __shfl_sync(0xffffffffu, we, max(warp - 1, 0));
+    const int64_t lt = __shfl_up_sync(0xffffffffu, t, 1), le = __shfl_up_sync(0xffffffffu, e, 1);
+    const int32_t lf = __shfl_up_sync(0xffffffffu, f, 1);
+    tokens = (warp ? bt : 0) + (lane ? lt : 0);
+    extent = (lane ? le : 0) + (warp && !(lane && lf) ? be : 0);
+    __syncthreads();                                                      // the arrays may be used again
+}
+
+// Goes over this thread's share of the segments; put(i, first token, first position) is called for each.  A sequence's end
+// is written to A.next where `ends` is set.
+template <typename Put>
+__device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool ends, Put put) {
     const int tid = threadIdx.x, n = A.n_segments, each = (int)(((int64_t)n + kScanThreads - 1) / kScanThreads);
     const int a = (int)min((int64_t)tid * each, (int64_t)n), b = (int)min((int64_t)a + each, (int64_t)n);
-    for (int i = tid; i < A.n_sequences; i += kScanThreads) A.next[i] = 0;
-    int64_t tokens = 0, extent = 0;
-    bool first = false;
     const int32_t before = a > 0 && a < n ? A.segments[a - 1].w : -1;
+    if (ends)
+        for (int i = tid; i < A.n_sequences; i += kScanThreads) A.next[i] = 0;
+    int64_t tokens = 0, extent = 0, total;
+    bool first = false;
     for (int i = a, seq = before; i < b; ++i) {
         const int4 s = A.segments[i];
         int64_t c, e;
@@ -197,31 +277,51 @@ __global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __gri
         seq = s.w;
         tokens += c; extent += e;
     }
-    s_tokens[tid] = tokens; s_extent[tid] = extent; s_first[tid] = first;
-    __syncthreads();
-    for (int o = 1; o < kScanThreads; o <<= 1) {      // inclusive sums; positions stop at a sequence's begin
-        int64_t t = 0, e = 0;
-        int32_t f = 0;
-        if (tid >= o) { t = s_tokens[tid - o]; e = s_extent[tid - o]; f = s_first[tid - o]; }
-        __syncthreads();
-        s_tokens[tid] += t;
-        if (!s_first[tid]) { s_extent[tid] += e; s_first[tid] = f; }
-        __syncthreads();
-    }
-    tokens = tid ? s_tokens[tid - 1] : 0;
-    extent = tid ? s_extent[tid - 1] : 0;
+    sums_before(tokens, extent, first, total);
     for (int i = a, seq = before; i < b; ++i) {
         const int4 s = A.segments[i];
         int64_t c, e;
         segment_sizes(A, s, c, e);
         if (s.w != seq || A.restart) extent = 0;
         seq = s.w;
-        A.starts[i] = tokens; A.bases[i] = (int32_t)extent;
+        put(i, tokens, (int32_t)extent);
         tokens += c; extent += e;
-        const bool last = i + 1 == n || A.segments[i + 1].w != s.w;
-        if (last && s.w >= 0 && s.w < A.n_sequences) A.next[s.w] = (int32_t)extent;
+        if (ends && (i + 1 == n || A.segments[i + 1].w != s.w) && s.w >= 0 && s.w < A.n_sequences) A.next[s.w] = (int32_t)extent;
     }
-    if (tid == kScanThreads - 1) A.starts[n] = s_tokens[tid];
+    return total;
+}
+
+// Up to kFewSegments segments: every CTA works out where all of them begin, keeps that in shared memory and writes its own
+// run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out of L2.
+constexpr int kFewSegments = 16384, kRunTokens = 1024;
+__global__ void __launch_bounds__(kScanThreads) positions_kernel(const __grid_constant__ PositionArgs A) {
+    extern __shared__ uint2 s_begin[];                                    // (first token, first position)
+    const int64_t total = walk_segments(A, blockIdx.x == 0, [&](int i, int64_t token, int32_t position) {
+        s_begin[i] = make_uint2((uint32_t)min(token, (int64_t)0xffffffff), (uint32_t)position);
+    });
+    __syncthreads();
+    const uint32_t t0 = (uint32_t)min((uint64_t)blockIdx.x * A.run, (uint64_t)A.n_tokens), t1 = (uint32_t)min((uint64_t)t0 + A.run, (uint64_t)A.n_tokens);
+    for (uint64_t tok = (uint64_t)t0 + threadIdx.x; tok < t1; tok += kScanThreads) {
+        const uint32_t token = (uint32_t)tok;
+        int32_t pt = 0, ph = 0, pw = 0;
+        if ((int64_t)token < total) {
+            int lo = 0, hi = A.n_segments;                                // the last segment that begins at or before the token
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_begin[mid].x <= token) lo = mid; else hi = mid;
+            }
+            position_in(A, A.segments[lo], (int32_t)s_begin[lo].y, token - s_begin[lo].x, pt, ph, pw);
+        } else if (!A.zero_tail) {
+            break;
+        }
+        A.positions[token] = pt; A.positions[A.stride + token] = ph; A.positions[2 * A.stride + token] = pw;
+    }
+}
+
+// More segments: one CTA writes where each begins to device memory, then a thread a token looks its segment up there.
+__global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __grid_constant__ PositionArgs A) {
+    const int64_t total = walk_segments(A, true, [&](int i, int64_t token, int32_t position) { A.starts[i] = token; A.bases[i] = position; });
+    if (threadIdx.x == 0) A.starts[A.n_segments] = total;
 }
 
 constexpr int kFillThreads = 256;
@@ -231,30 +331,12 @@ __global__ void __launch_bounds__(kFillThreads) position_fill_kernel(const __gri
     const uint32_t token = (uint32_t)tok;
     int32_t pt = 0, ph = 0, pw = 0;
     if ((int64_t)token < A.starts[A.n_segments]) {
-        int lo = 0, hi = A.n_segments;                // the last segment that begins at or before the token
+        int lo = 0, hi = A.n_segments;
         while (hi - lo > 1) {
             const int mid = lo + ((hi - lo) >> 1);
             if (A.starts[mid] <= (int64_t)token) lo = mid; else hi = mid;
         }
-        const int4 s = A.segments[lo];
-        const int32_t base = A.bases[lo];
-        const uint32_t l = (uint32_t)((int64_t)token - A.starts[lo]);
-        if (s.y <= 0 || s.z <= 0) { pt = ph = pw = base + (int32_t)l; }
-        else {
-            const uint64_t plane = (uint64_t)s.y * (uint64_t)s.z;
-            uint32_t f, rest;
-            if (plane >> 32) { f = 0; rest = l; } else { f = l / (uint32_t)plane; rest = l - f * (uint32_t)plane; }
-            uint32_t row, col;
-            const uint32_t m = (uint32_t)A.merge;
-            if (m > 1 && s.y % A.merge == 0 && s.z % A.merge == 0) {
-                const uint64_t band = (uint64_t)m * (uint32_t)s.z;
-                const uint32_t block = (uint32_t)(rest / band), in = (uint32_t)(rest - block * band), q = in % (m * m);
-                row = block * m + q / m; col = in / (m * m) * m + q % m;
-            } else {
-                row = rest / (uint32_t)s.z; col = rest - row * (uint32_t)s.z;
-            }
-            pt = base + (int32_t)f * A.time_step; ph = base + (int32_t)row; pw = base + (int32_t)col;
-        }
+        position_in(A, A.segments[lo], A.bases[lo], (uint32_t)((int64_t)token - A.starts[lo]), pt, ph, pw);
     } else if (!A.zero_tail) {
         return;
     }

@@ -84,17 +84,21 @@ bool fits(const pcr_turn_args& a, bool back, int v) {
     return true;
 }
 
-// How a call is cut: vectors of `v` pairs (0: value by value), `per` heads of a token to a thread, the grid, and how many
+// How a call is cut: vectors of `v` pairs (0: value by value), `k` chunks of two vectors to a lane, `per` heads of a token to a thread, the grid, and how many
 // rows of partial sums each operand's weights get.
-struct Cut { int v, per, slots[2], rows[2]; unsigned x, y; };
+struct Cut { int v, k, lanes, per, slots[2], rows[2]; unsigned x, y; };
 
 Cut cut_of(const pcr_turn_args& a, bool back) {
     Cut c = {};
     for (int v : {8, 4, 2})
         if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
+    // lanes have up to 24 elements of a row: what a row costs whatever its size is then shared by fewer lanes
+    const int chunks = c.v ? a.head_dim / (2 * c.v) : 32;
+    c.k = c.v == 8 || c.v == 0 ? 1 : chunks % 3 == 0 && chunks % 2 != 0 && c.v * size_of(a.dtype) * 3 <= 32 ? 3 : chunks % 2 == 0 ? 2 : 1;
+    c.lanes = chunks / c.k;
     constexpr int kWarps = kHeadThreads / 32;
     const int64_t n = a.batch * a.tokens, heads = a.q.heads + a.k.heads, sms = sm_count();
-    const int rows = c.v ? 32 / (a.head_dim / (2 * c.v)) : 1;       // tokens of a warp
+    const int rows = 32 / c.lanes;       // tokens of a warp
     const int64_t warps = (n + rows - 1) / rows, groups = (warps + kWarps - 1) / kWarps;
     // heads are shared out while that gives the SMs warps that they lack
     const int64_t shares = std::min<int64_t>((sms * 32 + warps - 1) / warps, heads);
@@ -128,22 +132,29 @@ void fill(HeadArgs& A, const pcr_turn_args& a, const Cut& c) {
     A.positions = a.positions; A.inv_freq = a.inv_freq; A.axes = a.axes;
     A.tokens = (uint32_t)(a.batch * a.tokens); A.seq = (uint32_t)std::max<int64_t>(a.tokens, 1);
     A.n_axes = a.n_axes; A.freq64 = a.freq_dtype == PCR_F64; A.weight32 = a.weight_dtype == PCR_F32; A.inverse = a.inverse;
-    A.dim = a.head_dim; A.rot = a.rot_dim; A.chunks = c.v ? a.head_dim / (2 * c.v) : 32; A.per = c.per;
+    A.dim = a.head_dim; A.rot = a.rot_dim; A.lanes = c.lanes; A.per = c.per;
     A.eps = a.eps; A.inv_dim = 1.f / (float)a.head_dim;
 }
 
-template <typename T, int V, int kMode, bool kNext>
+template <typename T, int V, int K, int kMode, bool kNext>
 void launch_vectors(const HeadArgs& A, dim3 grid, cudaStream_t st) {
-    if constexpr (kMode == kNormTurnBack) heads_back_kernel<T, V, kNext><<<grid, kHeadThreads, 0, st>>>(A);
-    else heads_kernel<T, V, kMode == kNormTurn, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    if constexpr (kMode == kNormTurnBack) heads_back_kernel<T, V, K, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    else heads_kernel<T, V, K, kMode == kNormTurn, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+}
+
+template <typename T, int V, int kMode, bool kNext>
+void launch_chunks(const HeadArgs& A, int k, dim3 grid, cudaStream_t st) {
+    if (k == 3) launch_vectors<T, V, V * sizeof(T) * 3 <= 32 ? 3 : 1, kMode, kNext>(A, grid, st);
+    else if (k == 2) launch_vectors<T, V, 2, kMode, kNext>(A, grid, st);
+    else launch_vectors<T, V, 1, kMode, kNext>(A, grid, st);
 }
 
 template <typename T, int kMode, bool kNext>
 void launch(const HeadArgs& A, const Cut& c, cudaStream_t st) {
     const dim3 grid(c.x, c.y);
-    if (sizeof(T) == 2 && c.v == 8) launch_vectors<T, sizeof(T) == 2 ? 8 : 4, kMode, kNext>(A, grid, st);
-    else if (c.v == 4) launch_vectors<T, 4, kMode, kNext>(A, grid, st);
-    else if (c.v == 2) launch_vectors<T, 2, kMode, kNext>(A, grid, st);
+    if (sizeof(T) == 2 && c.v == 8) launch_vectors<T, sizeof(T) == 2 ? 8 : 4, 1, kMode, kNext>(A, grid, st);
+    else if (c.v == 4) launch_chunks<T, 4, kMode, kNext>(A, c.k, grid, st);
+    else if (c.v == 2) launch_chunks<T, 2, kMode, kNext>(A, c.k, grid, st);
     else heads_any_kernel<T, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
     ++g_launches;
 }
@@ -235,32 +246,45 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
     const int each = 32 / patch;
     const size_t own = ((size_t)each * 3 * patch * patch * size_of(dtype) + 15) / 16 * 16;
     const int64_t warps = (n_tokens + each - 1) / each;
-    const unsigned grid = (unsigned)((warps + kPatchWarps - 1) / kPatchWarps);
+    const int in_cta = own * kPatchWarps > 40 * 1024 ? kPatchWarps / 2 : kPatchWarps;      // (32 x 32 patches in single precision)
+    const unsigned grid = (unsigned)((warps + in_cta - 1) / in_cta);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == PCR_F16) patch_tokens_kernel<__half><<<grid, 32 * kPatchWarps, own * kPatchWarps, st>>>(A);
-    else if (dtype == PCR_BF16) patch_tokens_kernel<__nv_bfloat16><<<grid, 32 * kPatchWarps, own * kPatchWarps, st>>>(A);
-    else patch_tokens_kernel<float><<<grid, 32 * kPatchWarps, own * kPatchWarps, st>>>(A);
+    if (dtype == PCR_F16) patch_tokens_kernel<__half><<<grid, 32 * in_cta, own * in_cta, st>>>(A);
+    else if (dtype == PCR_BF16) patch_tokens_kernel<__nv_bfloat16><<<grid, 32 * in_cta, own * in_cta, st>>>(A);
+    else patch_tokens_kernel<float><<<grid, 32 * in_cta, own * in_cta, st>>>(A);
     ++g_launches;
     return finish();
 }
 
-size_t pcr_token_positions_scratch_bytes(int n_segments) { return n_segments < 0 ? 0 : ((size_t)n_segments + 1) * 12 + 16; }
+size_t pcr_token_positions_scratch_bytes(int n_segments) { return n_segments <= kFewSegments ? 0 : ((size_t)n_segments + 1) * 12 + 16; }
 
 int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_tokens, int n_sequences, int merge, int time_step,
                         int flags, int32_t* positions, int64_t axis_stride, int32_t* next, void* scratch, void* stream) {
     if (n_segments < 0 || n_sequences < 0 || n_tokens < 0 || n_tokens > INT32_MAX || merge < 1 || merge > 64) return PCR_E_ARG;
     if (time_step < 0 || time_step > (1 << 20) || (flags & ~(PCR_POSITIONS_RESTART | PCR_POSITIONS_ZERO_TAIL))) return PCR_E_ARG;
-    if ((n_segments > 0 && !segments) || (n_tokens > 0 && !positions) || (n_sequences > 0 && !next) || !scratch) return PCR_E_ARG;
+    if ((n_segments > 0 && !segments) || (n_tokens > 0 && !positions) || (n_sequences > 0 && !next) || (n_segments > kFewSegments && !scratch)) return PCR_E_ARG;
     if (!aligned(segments, 16) || !aligned(positions, 4) || !aligned(next, 4) || !aligned(scratch, 8)) return PCR_E_ARG;
     if (n_tokens > 0 && axis_stride < n_tokens) return PCR_E_ARG;
     PositionArgs A;
     A.segments = reinterpret_cast<const int4*>(segments);
     A.starts = static_cast<int64_t*>(scratch);
     A.bases = reinterpret_cast<int32_t*>(A.starts + n_segments + 1);
-    A.positions = positions; A.next = next; A.stride = axis_stride; A.n_tokens = (uint32_t)n_tokens;
+    A.positions = positions; A.next = next; A.stride = axis_stride; A.n_tokens = (uint32_t)n_tokens; A.run = 0;
     A.n_segments = n_segments; A.n_sequences = n_sequences; A.merge = merge; A.time_step = time_step;
     A.restart = (flags & PCR_POSITIONS_RESTART) != 0; A.zero_tail = (flags & PCR_POSITIONS_ZERO_TAIL) != 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (n_segments <= kFewSegments) {
+        const int64_t runs = std::min<int64_t>(std::max<int64_t>((n_tokens + kRunTokens - 1) / kRunTokens, 1), sm_count());
+        A.run = (uint32_t)(((n_tokens + runs - 1) / runs + 31) / 32 * 32);
+        const size_t shared = (size_t)n_segments * sizeof(uint2);
+        if (shared > 40 * 1024 && cudaFuncSetAttribute(positions_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) {
+            cudaGetLastError();
+            return PCR_E_CUDA;
+        }
+        positions_kernel<<<(unsigned)runs, kScanThreads, shared, st>>>(A);
+        ++g_launches;
+        return finish();
+    }
     position_scan_kernel<<<1, kScanThreads, 0, st>>>(A);
     ++g_launches;
     if (n_tokens > 0) {

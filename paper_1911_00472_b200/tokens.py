@@ -21,7 +21,7 @@ from . import binding as B
 _CODES = {torch.float16: B.PCR_F16, torch.float32: B.PCR_F32, torch.bfloat16: B.PCR_BF16}
 _FREQ_CODES = {torch.float32: B.PCR_F32, torch.float64: B.PCR_F64}
 _TURN_ARGS = struct.Struct("<5Q9q2i5Q9q2iQ3qQQqq8ifi")         # pcr_turn_args
-_NO_HEADS = (0,) * 16
+_NO_HEADS, _NO_STRIDES = (0,) * 16, (0,) * 4
 
 
 @contextlib.contextmanager
@@ -35,6 +35,8 @@ def _switched(device, stream):
 
 
 _HERE = contextlib.nullcontext()
+# the handle of a device's current stream, without the object around it: a third of what a small call costs
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _on(device: torch.device, stream):
@@ -54,24 +56,7 @@ def _same_device(device, *tensors):
             raise ValueError("all operands have to be on one device")
 
 
-def _no_autograd(*tensors):
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
-
-
 # ---- queries and keys ---------------------------------------------------------------------------------------------------
-
-
-def _strides(t):
-    return t.stride()[:-1] if t.dim() == 4 else (0,) + t.stride()[:-1]
-
-
-def _operand(t, like, name):
-    """Checks one query- or key-shaped tensor against the queries."""
-    if t.dim() != like.dim() or t.shape[:-2] != like.shape[:-2] or t.shape[-1] != like.shape[-1] or t.dtype != like.dtype:
-        raise ValueError(f"{name} must have the tokens, head size and dtype of the queries")
 
 
 def _rows(t):
@@ -79,56 +64,88 @@ def _rows(t):
     return t if t is None or t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
 
 
-def _heads(x, y, dy, weight, dweight):
-    return (x.data_ptr(), y.data_ptr(), 0 if dy is None else dy.data_ptr(), 0 if weight is None else weight.data_ptr(),
-            0 if dweight is None else dweight.data_ptr(), *_strides(x), *_strides(y), *((0, 0, 0) if dy is None else _strides(dy)),
-            x.shape[-2], 0)
-
-
-def _turn_args(q, k, heads_q, heads_k, positions, inv_freq, axes, interleaved, inverse, weights, eps):
-    lead, rot = q.shape[:-2], 2 * inv_freq.numel()
-    if positions.dtype != torch.int32 or positions.shape[1:] != lead:
-        raise ValueError("positions must be int32 with shape (axes, *tokens)")
-    if inv_freq.dtype not in _FREQ_CODES or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
-        raise ValueError("inv_freq must be a contiguous float32 or float64 vector")
-    if axes.dtype != torch.int32 or axes.shape != inv_freq.shape or not axes.is_contiguous():
-        raise ValueError("axes must be a contiguous int32 vector as long as inv_freq")
-    weight_type = None
-    for w in weights:
-        if w is None:
-            continue
-        if w.shape != q.shape[-1:] or not w.is_contiguous() or w.dtype not in (q.dtype, torch.float32) or weight_type not in (None, w.dtype):
-            raise ValueError("weights must be contiguous vectors of the head size, of the operands' type or float32, both alike")
-        weight_type = w.dtype
-    _same_device(q.device, k, positions, inv_freq, axes, *weights)
-    ps = positions.stride()
-    batch, ps = (lead[0], ps) if q.dim() == 4 else (1, (ps[0], 0, ps[1]))
-    return _TURN_ARGS.pack(*heads_q, *heads_k, positions.data_ptr(), *ps, inv_freq.data_ptr(), axes.data_ptr(), batch, lead[-1],
-                           positions.shape[0], q.shape[-1], rot, bool(interleaved), bool(inverse), _CODES[q.dtype],
-                           _FREQ_CODES[inv_freq.dtype], _CODES[weight_type or q.dtype], eps, 0)
-
-
-def _check_queries(q, k):
-    if q.dim() not in (3, 4) or q.dtype not in _CODES:
+def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
+    """What the calls ask of their operands; returns (batch, tokens, size, type of the weights).  One look at each property:
+    small calls take as long as the host does."""
+    shape, dtype, device = q.shape, q.dtype, q.get_device()
+    if len(shape) == 4:
+        batch, tokens, _, size = shape
+    elif len(shape) == 3:
+        batch, (tokens, _, size) = 1, shape
+    else:
+        batch = tokens = size = None
+    if size is None or dtype not in _CODES:
         raise ValueError("queries must be (tokens, heads, size) or (batch, tokens, heads, size) of float16, bfloat16 or float32")
     if k is not None:
-        _operand(k, q, "k")
+        other = k.shape
+        if len(other) != len(shape) or other[-3] != tokens or other[-1] != size or other[0] != shape[0] or k.dtype != dtype:
+            raise ValueError("k must have the tokens, head size and dtype of the queries")
+    other = positions.shape
+    if len(other) != len(shape) - 1 or other[-1] != tokens or other[1] != shape[0] or positions.dtype != torch.int32:
+        raise ValueError("positions must be int32 with shape (axes, *tokens)")
+    other = inv_freq.shape
+    if len(other) != 1 or inv_freq.dtype not in _FREQ_CODES or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous float32 or float64 vector")
+    if axes.shape != other or axes.dtype != torch.int32 or not axes.is_contiguous():
+        raise ValueError("axes must be a contiguous int32 vector as long as inv_freq")
+    near = device == positions.get_device() == inv_freq.get_device() == axes.get_device() and (k is None or k.get_device() == device)
+    followed = q.requires_grad or (k is not None and k.requires_grad)
+    weight = dtype
+    if q_weight is not None or k_weight is not None:
+        weight = (k_weight if q_weight is None else q_weight).dtype
+        for w in (q_weight, k_weight):
+            if w is not None:
+                if w.shape != (size,) or w.dtype != weight or (weight != dtype and weight != torch.float32) or not w.is_contiguous():
+                    raise ValueError("weights must be contiguous vectors of the head size, of the operands' type or float32, both alike")
+                near = near and w.get_device() == device
+                followed = followed or w.requires_grad
+        if k is None and k_weight is not None:
+            raise ValueError("k_weight without keys")
+    for g, x in zip(grads, (q, k)):
+        if (g is None) != (x is None) or (x is not None and (g.shape != x.shape or g.dtype != dtype)):
+            raise ValueError("gradients must have the shapes and the dtype of their operands")
+        if g is not None:
+            near = near and g.get_device() == device
+            followed = followed or g.requires_grad
+    if not near:
+        raise ValueError("all operands have to be on one device")
+    if followed and torch.is_grad_enabled():
+        raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
+    return batch, tokens, size, weight
 
 
 def _outputs(q, k, out):
     if out is None:
-        return torch.empty_like(q, memory_format=torch.contiguous_format), None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
+        return torch.empty_like(q), None if k is None else torch.empty_like(k)
     for o, x in zip(out, (q, k), strict=True):
         if (o is None) != (x is None):
             raise ValueError("out must have an output for each operand")
         if x is not None:
-            if o.shape != x.shape:
-                raise ValueError("out must have the shapes of the operands")
-            _operand(o, q, "out")
+            if o.shape != x.shape or o.dtype != x.dtype:
+                raise ValueError("out must have the shapes and the dtype of the operands")
             if o.shape[-1] > 1 and o.stride(-1) != 1:
                 raise ValueError("the elements of a head of out must stand side by side")
             _same_device(q.device, o)
     return out
+
+
+def _heads(x, y, dy, weight, dweight):
+    """A pcr_heads: addresses, then strides of batch, token and head (the elements' own, the last, are 1)."""
+    if x is None:
+        return _NO_HEADS
+    xs, ys, gs = x.stride(), y.stride(), _NO_STRIDES if dy is None else dy.stride()
+    if len(xs) == 3:
+        xs, ys, gs = (0, *xs), (0, *ys), (0, *gs) if dy is not None else gs
+    return (x.data_ptr(), y.data_ptr(), 0 if dy is None else dy.data_ptr(), 0 if weight is None else weight.data_ptr(),
+            0 if dweight is None else dweight.data_ptr(), *xs[:3], *ys[:3], *gs[:3], x.shape[-2], 0)
+
+
+def _pack(heads_q, heads_k, positions, inv_freq, axes, q, dims, interleaved, inverse, eps):
+    batch, tokens, size, weight = dims
+    ps = positions.stride()
+    return _TURN_ARGS.pack(*heads_q, *heads_k, positions.data_ptr(), *(ps if len(ps) == 3 else (ps[0], 0, ps[1])), inv_freq.data_ptr(),
+                           axes.data_ptr(), batch, tokens, positions.shape[0], size, 2 * inv_freq.shape[0], bool(interleaved), bool(inverse),
+                           _CODES[q.dtype], _FREQ_CODES[inv_freq.dtype], _CODES[weight], eps, 0)
 
 
 def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False, out=None, stream=None):
@@ -144,14 +161,12 @@ def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False,
     inverse   by the negative angle: the gradient of the forward call
     out       (q, k) to write to, the operands themselves allowed
     """
-    _check_queries(q, k)
-    _no_autograd(q, k)
+    dims = _check(q, k, positions, inv_freq, axes, None, None, ())
     with _on(q.device, stream):
         q, k = _rows(q), _rows(k)
         y, z = _outputs(q, k, out)
-        args = _turn_args(q, k, _heads(q, y, None, None, None), _NO_HEADS if k is None else _heads(k, z, None, None, None),
-                          positions, inv_freq, axes, interleaved, inverse, (), 0.0)
-        B._chk(B.lib().pcr_rotate(args, torch.cuda.current_stream(q.device).cuda_stream), "pcr_rotate")
+        args = _pack(_heads(q, y, None, None, None), _heads(k, z, None, None, None), positions, inv_freq, axes, q, dims, interleaved, inverse, 0.0)
+        B._chk(B.lib().pcr_rotate(args, _raw_stream(q.device.index)), "pcr_rotate")
     return y, z
 
 
@@ -160,14 +175,12 @@ def norm_rotate(q, k, q_weight, k_weight, positions, inv_freq, axes, *, eps=1e-6
 
     q_weight, k_weight   (size,) of the operands' type or float32; None: ones
     """
-    _check_queries(q, k)
-    _no_autograd(q, k, q_weight, k_weight)
+    dims = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, ())
     with _on(q.device, stream):
         q, k = _rows(q), _rows(k)
         y, z = _outputs(q, k, out)
-        args = _turn_args(q, k, _heads(q, y, None, q_weight, None), _NO_HEADS if k is None else _heads(k, z, None, k_weight, None),
-                          positions, inv_freq, axes, interleaved, False, (q_weight, k_weight), eps)
-        B._chk(B.lib().pcr_norm_rotate(args, torch.cuda.current_stream(q.device).cuda_stream), "pcr_norm_rotate")
+        args = _pack(_heads(q, y, None, q_weight, None), _heads(k, z, None, k_weight, None), positions, inv_freq, axes, q, dims, interleaved, False, eps)
+        B._chk(B.lib().pcr_norm_rotate(args, _raw_stream(q.device.index)), "pcr_norm_rotate")
     return y, z
 
 
@@ -177,25 +190,15 @@ def norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, in
 
     out   where the gradients of q and k go; (grad_q, grad_k) or (q, k) themselves allowed
     """
-    _check_queries(q, k)
-    if (k is None) != (grad_k is None) or grad_q.shape != q.shape or (k is not None and grad_k.shape != k.shape):
-        raise ValueError("gradients must have the shapes of their operands")
-    _operand(grad_q, q, "grad_q")
-    if k is not None:
-        _operand(grad_k, q, "grad_k")
-    elif k_weight is not None:
-        raise ValueError("k_weight without keys")
-    _no_autograd(q, k, q_weight, k_weight, grad_q, grad_k)
-    _same_device(q.device, grad_q, grad_k)
+    dims = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, (grad_q, grad_k))
     with _on(q.device, stream):
         q, k, grad_q, grad_k = _rows(q), _rows(k), _rows(grad_q), _rows(grad_k)
         y, z = _outputs(q, k, out)
         dwq, dwk = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
-        args = _turn_args(q, k, _heads(q, y, grad_q, q_weight, dwq), _NO_HEADS if k is None else _heads(k, z, grad_k, k_weight, dwk),
-                          positions, inv_freq, axes, interleaved, False, (q_weight, k_weight), eps)
+        args = _pack(_heads(q, y, grad_q, q_weight, dwq), _heads(k, z, grad_k, k_weight, dwk), positions, inv_freq, axes, q, dims, interleaved, False, eps)
         L = B.lib()
-        scratch = torch.empty(L.pcr_norm_rotate_scratch_bytes(args) // 4, dtype=torch.float32, device=q.device)
-        B._chk(L.pcr_norm_rotate_backward(args, scratch.data_ptr(), torch.cuda.current_stream(q.device).cuda_stream), "pcr_norm_rotate_backward")
+        scratch = inv_freq.new_empty(-(-L.pcr_norm_rotate_scratch_bytes(args) // inv_freq.element_size()))
+        B._chk(L.pcr_norm_rotate_backward(args, scratch.data_ptr(), _raw_stream(q.device.index)), "pcr_norm_rotate_backward")
     return y, z, dwq, dwk
 
 
@@ -250,13 +253,14 @@ def token_positions(segments, n_tokens, n_sequences, *, merge=1, time_step=1, re
         flags = B.PCR_POSITIONS_RESTART if restart else 0
         if out is None:
             flags |= B.PCR_POSITIONS_ZERO_TAIL
-            out = torch.empty((3, n_tokens), dtype=torch.int32, device=segments.device)
-        after = torch.empty(n_sequences, dtype=torch.int32, device=segments.device)
+            out = segments.new_empty((3, n_tokens))
+        after = segments.new_empty(n_sequences)
         L = B.lib()
-        scratch = torch.empty(L.pcr_token_positions_scratch_bytes(segments.shape[0]), dtype=torch.uint8, device=segments.device)
+        need = L.pcr_token_positions_scratch_bytes(segments.shape[0])
+        scratch = segments.new_empty(-(-need // 4)) if need else after
         B._chk(L.pcr_token_positions(segments.data_ptr(), segments.shape[0], n_tokens, n_sequences, merge, time_step, flags, out.data_ptr(),
-                                     out.stride(0), after.data_ptr(), scratch.data_ptr(),
-                                     torch.cuda.current_stream(segments.device).cuda_stream), "pcr_token_positions")
+                                     out.stride(0), after.data_ptr(), scratch.data_ptr(), _raw_stream(segments.device.index)),
+               "pcr_token_positions")
     return out, after
 
 
@@ -286,10 +290,10 @@ def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.b
     _same_device(rgb.device, images, index, out)
     with _on(rgb.device, stream):
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=rgb.device)
+            out = rgb.new_empty(shape, dtype=dtype)
         B._chk(B.lib().pcr_patch_tokens(rgb.data_ptr(), rgb.numel(), images.data_ptr(), images.shape[0], index.data_ptr(), shape[0], patch,
                                         merge, struct.pack("3f", *mean), struct.pack("3f", *std), _CODES[dtype], out.data_ptr(),
-                                        torch.cuda.current_stream(rgb.device).cuda_stream), "pcr_patch_tokens")
+                                        _raw_stream(rgb.device.index)), "pcr_patch_tokens")
     return out
 
 

@@ -136,11 +136,15 @@ def test_token_positions_refuses():
     ok = [4096, 3, 100, 2, 1, 1, 0, 4096, 100, 4096, 4096, None]
     call = B.lib().pcr_token_positions
     for at, bad in [(0, None), (0, 4104), (1, -1), (2, -1), (2, 1 << 31), (3, -1), (4, 0), (4, 65), (5, -1), (5, (1 << 20) + 1), (6, 4), (7, None), (7, 4098), (8, 99),
-                    (9, None), (9, 4097), (10, None), (10, 4100)]:
+                    (9, None), (9, 4097), (10, 4100)]:
         args = list(ok)
         args[at] = bad
         assert call(*args) == E, (at, bad)
-    assert B.lib().pcr_token_positions_scratch_bytes(-1) == 0
+    need = B.lib().pcr_token_positions_scratch_bytes
+    assert need(-1) == 0 and need(3) == 0 and need(20000) >= 12 * 20001
+    args = list(ok)
+    args[1], args[10] = 20000, None               # so many segments need scratch memory
+    assert call(*args) == E
 
 
 def test_operands_on_the_host_are_refused():
