@@ -220,7 +220,7 @@ typedef struct {
  * after channel, row after row, rounded once to dtype.  Patches are numbered in blocks of merge x merge,
  * blocks row by row and patches row by row in a block (merge = 1: row by row).
  *   rgb       : DEVICE, 4-byte aligned, rgb_bytes bytes.
- *   images    : DEVICE, n_images rows.   index : DEVICE, n_tokens pairs of int32, 8-byte aligned.
+ *   images    : DEVICE, n_images rows, 16-byte aligned.   index : DEVICE, n_tokens pairs of int32, 8-byte aligned.
  *   patch     : 1..32.   merge : 1..64.   mean, std : HOST, three floats each, std > 0.
  *   tokens    : DEVICE, n_tokens x (3 * patch * patch) elements of dtype.
  * A token whose entry names no image, no patch of it, or an image that does not lie inside `rgb` (or a

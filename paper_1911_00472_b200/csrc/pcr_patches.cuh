@@ -22,58 +22,99 @@ struct PatchArgs {
     void* out;
     uint64_t rgb_bytes;
     uint32_t n_tokens;
-    int32_t n_images, patch, merge;
+    int32_t n_images, patch, merge, each;        // each: tokens of a warp
+    uint32_t by_lanes, by_merge;   // lane / lanes of a patch = lane * by_lanes >> 16, i / merge = i * by_merge >> 20 (i < merge^2)
     float scale[3], shift[3];      // (v / 255 - mean) / std = v * scale + shift
 };
 
 // Bilinear taps with half-pixel centres: the source coordinate (o + 1/2) side / out - 1/2 as a whole number over 2 out,
 // so that where it falls between pixels is exact whatever the sizes.
 struct Tap { int32_t lo; float f; };
-__device__ __forceinline__ Tap tap_of(int32_t o, int32_t out, int32_t side) {
+struct Axis { int32_t out, side; float inv; bool small; };               // resampled and source pixels, 1 / (2 out)
+__device__ __forceinline__ Axis axis_of(int32_t out, int32_t side) {
+    return {out, side, __fdividef(1.f, 2.f * (float)out), (int64_t)out * side < (1 << 29)};
+}
+__device__ __forceinline__ Tap tap_of(int32_t o, const Axis& x) {
     Tap t;
-    if ((int64_t)out * side < (1 << 29)) {
-        const int32_t den = 2 * out;
-        const int32_t num = min(max((2 * o + 1) * side - out, 0), (side - 1) * den);
-        t.lo = (int32_t)((uint32_t)num / (uint32_t)den);
-        t.f = __fdividef((float)(num - t.lo * den), (float)den);         // (off by 2 units in the last place at most)
+    if (x.small) {
+        // below 2^30, and the quotient below 2^20: with the approximate reciprocal it is off by one at most
+        const int32_t den = 2 * x.out;
+        const int32_t num = min(max((2 * o + 1) * x.side - x.out, 0), (x.side - 1) * den);
+        t.lo = (int32_t)((float)num * x.inv);
+        int32_t rest = num - t.lo * den;
+        if (rest < 0) { --t.lo; rest += den; }
+        if (rest >= den) { ++t.lo; rest -= den; }
+        t.f = (float)rest * x.inv;                                       // (off by 3 roundings)
     } else {
-        const int64_t den = 2 * (int64_t)out;
-        const int64_t num = min(max((2 * (int64_t)o + 1) * side - out, (int64_t)0), (side - 1) * den);
+        const int64_t den = 2 * (int64_t)x.out;
+        const int64_t num = min(max((2 * (int64_t)o + 1) * x.side - x.out, (int64_t)0), (x.side - 1) * den);
         t.lo = (int32_t)(num / den);
-        t.f = __fdividef((float)(num - t.lo * den), (float)den);
+        t.f = (float)(num - t.lo * den) / (float)den;
     }
     return t;
 }
 
-// Whether a token's entry stands for a patch of pixels that are there.
-__device__ __forceinline__ bool patch_ok(const PatchArgs& A, const PatchImage& m, int32_t local) {
-    const int64_t most = kMaxSide / A.patch;
-    if (m.width < 1 || m.width > kMaxSide || m.height < 1 || m.height > kMaxSide || m.offset < 0 || m.rows < 1 || m.cols < 1 || m.rows > most || m.cols > most) return false;
-    const int32_t rows = (int32_t)m.rows, cols = (int32_t)m.cols;
-    return (uint64_t)m.offset <= A.rgb_bytes && (uint64_t)(3 * m.width * m.height) <= A.rgb_bytes - (uint64_t)m.offset &&
-           m.x0 >= 0 && m.y0 >= 0 && m.w >= 1 && m.h >= 1 && m.w <= m.width && m.h <= m.height && m.x0 <= m.width - m.w &&
-           m.y0 <= m.height - m.h && rows % A.merge == 0 && cols % A.merge == 0 && (m.flip == 0 || m.flip == 1) && local >= 0 &&
-           local < m.rows * m.cols;
+// a / b where a < 2^22: one unit off at most before it is put right
+__device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) {
+    if ((a | b) >= 1u << 22) return a / b;
+    uint32_t q = (uint32_t)__fdividef((float)a, (float)b);
+    const int32_t rest = (int32_t)(a - q * b);
+    return rest < 0 ? q - 1 : rest >= (int32_t)b ? q + 1 : q;
+}
+
+// A token's patch: whether there is one, and where.
+struct Patch {
+    bool ok, words, flip;          // words: rows may be counted in 32 bits, and aligned words read without leaving the buffer
+    int32_t row, col;
+    int64_t pitch;
+    const uint8_t* corner;         // the rectangle's first byte
+    Axis x, y;
+};
+__device__ __forceinline__ void look_up(const PatchArgs& A, int2 token, Patch& r) {
+    r.ok = r.words = false;
+    const int32_t image = token.x;
+    if (image < 0 || image >= A.n_images) return;
+    const longlong2* from = reinterpret_cast<const longlong2*>(A.images + image);
+    const longlong2 m0 = __ldg(from), m1 = __ldg(from + 1), m2 = __ldg(from + 2), m3 = __ldg(from + 3), m4 = __ldg(from + 4);
+    const PatchImage m = {m0.x, m0.y, m1.x, m1.y, m2.x, m2.y, m3.x, m3.y, m4.x, m4.y};
+    // (a negative number has its upper bits set)
+    if (((uint64_t)(m.width | m.height | m.x0 | m.y0 | m.w | m.h | m.rows | m.cols | m.flip) >> 21) != 0 || m.offset < 0) return;
+    const int32_t width = (int32_t)m.width, height = (int32_t)m.height, w = (int32_t)m.w, h = (int32_t)m.h, rows = (int32_t)m.rows, cols = (int32_t)m.cols;
+    const uint32_t odd = (uint32_t)(A.merge - 1);
+    const bool whole = (A.merge & odd) == 0 ? ((rows | cols) & odd) == 0 : rows % A.merge == 0 && cols % A.merge == 0;
+    const uint64_t room = A.rgb_bytes - (uint64_t)m.offset;
+    r.ok = width >= 1 && width <= kMaxSide && height >= 1 && height <= kMaxSide && (uint64_t)m.offset <= A.rgb_bytes &&
+           3 * (uint64_t)width * (uint64_t)height <= room && w >= 1 && h >= 1 && (int32_t)m.x0 + w <= width && (int32_t)m.y0 + h <= height &&
+           rows >= 1 && cols >= 1 && rows * A.patch <= kMaxSide && cols * A.patch <= kMaxSide && whole && m.flip <= 1;
+    if (!r.ok || token.y < 0 || token.y >= (int64_t)rows * cols) { r.ok = false; return; }
+    const uint32_t mg = (uint32_t)A.merge, band = mg * (uint32_t)cols, block = quotient((uint32_t)token.y, band), rest = (uint32_t)token.y - block * band;
+    const uint32_t side = mg == 1 ? rest : quotient(rest, mg * mg), in = rest - side * (mg * mg), down = in * A.by_merge >> 20;
+    r.row = (int32_t)(block * mg + down); r.col = (int32_t)(side * mg + in - down * mg);
+    r.flip = m.flip != 0;
+    r.pitch = 3 * (int64_t)width;
+    const int64_t corner = m.y0 * r.pitch + 3 * m.x0, behind = corner + (h - 1) * r.pitch + 3 * w + 16;
+    r.words = h * r.pitch < (int64_t)1 << 31 && (uint64_t)behind <= room;
+    r.corner = A.rgb + m.offset + corner;
+    r.x = axis_of(cols * A.patch, w);
+    r.y = axis_of(rows * A.patch, h);
 }
 
 // Bytes become floats as 2^23 + byte, exactly; differences need no more, what is added to has the 2^23 taken off.
 __device__ __forceinline__ float byte_up(uint32_t word, int i) { return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440u | (uint32_t)i)); }
 constexpr float kUp = 8388608.f;
 
-struct Rgb { F2 rg; float b; };
-
 // The pixel whose bytes are the lowest three of `lo` mixed with the next one (fourth byte of `lo`, two of `hi`).
+struct Rgb { float r, g, b; };
 __device__ __forceinline__ Rgb mix_bytes(uint32_t lo, uint32_t hi, float f) {
-    const F2 a = pack2(byte_up(lo, 0), byte_up(lo, 1)), e = pack2(byte_up(lo, 3), byte_up(hi, 0));
-    const float ab = byte_up(lo, 2), eb = byte_up(hi, 1);
-    return {fma2(pack2(f, f), fma2(a, pack2(-1.f, -1.f), e), fma2(a, pack2(1.f, 1.f), pack2(-kUp, -kUp))), fmaf(f, eb - ab, ab - kUp)};
+    const float r = byte_up(lo, 0), g = byte_up(lo, 1), b = byte_up(lo, 2);
+    return {fmaf(f, byte_up(lo, 3) - r, r - kUp), fmaf(f, byte_up(hi, 0) - g, g - kUp), fmaf(f, byte_up(hi, 1) - b, b - kUp)};
 }
 // ... read as aligned words, which have to lie inside the buffer
 __device__ __forceinline__ Rgb mix_words(const uint8_t* at, float f) {
     const uint32_t* p = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
-    const uint32_t sh = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 3) * 8, w0 = __ldg(p), w1 = __ldg(p + 1);
+    const uint32_t sh = (uint32_t)reinterpret_cast<uintptr_t>(at) << 3, w0 = __ldg(p), w1 = __ldg(p + 1);        // (shifts count modulo 32)
     uint32_t w2 = 0;
-    if (sh == 24) w2 = __ldg(p + 2);
+    if ((sh & 31) == 24) w2 = __ldg(p + 2);
     return mix_bytes(__funnelshift_r(w0, w1, sh), __funnelshift_r(w1, w2, sh), f);
 }
 // ... byte by byte, the next pixel only where it counts: it may lie behind the last one
@@ -83,94 +124,156 @@ __device__ __forceinline__ Rgb mix_single(const uint8_t* at, float f) {
     return mix_bytes(lo, hi, f);
 }
 
-// A lane a column of a patch, walking down its rows: a source row that serves two output rows is read and mixed once.
-// A warp takes 32 / patch tokens; their values meet in shared memory and leave as whole vectors.  Every lane asks for one
-// of the source rows before the walk begins, so that the rows arrive together and not one after the other.
-template <typename T>
-__global__ void __launch_bounds__(32 * kPatchWarps) patch_tokens_kernel(const __grid_constant__ PatchArgs A) {
+// One or two columns of a source row, mixed; two at a time in every instruction.
+template <int kCols> struct Mixed { F2 c[3]; };
+template <> struct Mixed<1> { float c[3]; };
+
+// The words that two neighbouring columns lie in: the left one's six bytes begin at `sh` bits into the first, the right
+// one's 0, 3 or 6 bytes further on.
+struct Words { uint32_t w0, w1, w2, w3, sh; };
+__device__ __forceinline__ Words words_at(const uint8_t* at, bool wide) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
+    Words r = {__ldg(p), __ldg(p + 1), __ldg(p + 2), 0, (uint32_t)reinterpret_cast<uintptr_t>(at) << 3};
+    if (wide) r.w3 = __ldg(p + 3);
+    return r;
+}
+__device__ __forceinline__ Mixed<2> mix_words(const Words& w, bool wide, uint32_t shift, F2 f) {
+    const uint32_t x0 = __funnelshift_r(w.w0, w.w1, w.sh), x1 = __funnelshift_r(w.w1, w.w2, w.sh), x2 = __funnelshift_r(w.w2, w.w3, w.sh);
+    const uint32_t a = wide ? x1 : x0, b = wide ? x2 : x1, y0 = __funnelshift_r(a, b, shift), y1 = __funnelshift_r(b, x2, shift);
+    const F2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f), down = pack2(-kUp, -kUp);
+    Mixed<2> r;
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+        const F2 left = pack2(byte_up(x0, c), byte_up(y0, c)), right = c == 0 ? pack2(byte_up(x0, 3), byte_up(y0, 3)) : pack2(byte_up(x1, c - 1), byte_up(y1, c - 1));
+        r.c[c] = fma2(f, fma2(left, minus, right), fma2(left, one, down));
+    }
+    return r;
+}
+
+// Values of one or two columns side by side.
+__device__ __forceinline__ void put_two(float* to, float a, float b, bool swap) { *reinterpret_cast<float2*>(to) = swap ? make_float2(b, a) : make_float2(a, b); }
+__device__ __forceinline__ void put_two(__half* to, float a, float b, bool swap) {
+    __half2 v = __floats2half2_rn(a, b);
+    if (swap) v = __lowhigh2highlow(v);
+    *reinterpret_cast<__half2*>(to) = v;
+}
+__device__ __forceinline__ void put_two(__nv_bfloat16* to, float a, float b, bool swap) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    if (swap) v = __lowhigh2highlow(v);
+    *reinterpret_cast<__nv_bfloat162*>(to) = v;
+}
+
+// A lane kCols neighbouring columns of a patch, walking down its rows: a source row that serves two output rows is read and
+// mixed once, and its words are asked for one row ahead.  A warp takes 32 / lanes-of-a-patch tokens, whose values meet in
+// shared memory and leave as whole vectors, or (kDirect) are written as they come.  Instructions bound it (bytes to numbers, two mixes, a scale), not HBM: two
+// columns to a lane share the walk's addresses, words and conditions and go two to an instruction; patches of odd size go
+// one column to a lane.
+template <typename T, int kCols, bool kDirect>
+__global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const __grid_constant__ PatchArgs A) {
     extern __shared__ __align__(16) unsigned char s_raw[];
-    __shared__ float2 s_rows[kPatchWarps][32];                    // (first byte of the upper source row as bits, weight of the lower)
-    const int p = A.patch, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int each = 32 / p, area = p * p, values = 3 * area;
-    const int sub = lane / p, px = lane - sub * p;
+    __shared__ uint4 s_rows[kPatchWarps][kMaxPatch * kCols];      // first bytes of the upper and the lower source row, weight of the lower
+    const int p = A.patch, across = p / kCols, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int each = A.each, area = p * p, values = 3 * area;
+    const int sub = (int)(lane * A.by_lanes >> 16), px = (lane - sub * across) * kCols;
     const uint32_t own = ((uint32_t)(each * values) * (uint32_t)sizeof(T) + 15) / 16 * 16;
     T* const buf = reinterpret_cast<T*>(s_raw + warp * own);
     const uint64_t first = ((uint64_t)blockIdx.x * (blockDim.x >> 5) + warp) * (uint64_t)each;
     if (first >= A.n_tokens) return;
     const int count = (int)min((uint64_t)each, A.n_tokens - first);
     const bool here = sub < count;
-    bool ok = false, words = false;
-    const uint8_t* base = nullptr;        // the rectangle's first row at this lane's column
-    int64_t pitch = 0;
-    float fx = 0.f;
+    Patch m;
+    m.ok = m.words = false;
+    const uint8_t *base = nullptr, *other = nullptr;        // the rectangle's first row at the left column, at the right one
+    float fl = 0.f, fr = 0.f;
+    uint4* const rows0 = &s_rows[warp][here ? sub * p : 0];
     if (here) {
-        const int2 at = A.index[first + sub];
-        if (at.x >= 0 && at.x < A.n_images) {
-            const PatchImage m = A.images[at.x];
-            ok = patch_ok(A, m, at.y);
-            if (ok) {
-                const int32_t cols = (int32_t)m.cols, mg = A.merge, band = mg * cols;
-                const int32_t block = at.y / band, rest = at.y - block * band, square = mg * mg;
-                const int32_t side = rest / square, in = rest - side * square;
-                const int32_t row = block * mg + in / mg, col = side * mg + in % mg;
-                int32_t ox = col * p + px;
-                if (m.flip) ox = cols * p - 1 - ox;
-                const Tap tx = tap_of(ox, cols * p, (int32_t)m.w), ty = tap_of(row * p + px, (int32_t)m.rows * p, (int32_t)m.h);
-                pitch = 3 * m.width;
-                fx = tx.f;
-                const int64_t corner = m.offset + m.y0 * pitch + 3 * m.x0;
-                base = A.rgb + corner + 3 * (int64_t)tx.lo;
-                // rows are counted in bytes from the first, 32 bits; words are read where none can end behind the buffer
-                words = m.h * pitch < (int64_t)1 << 31 && (uint64_t)(corner + (m.h - 1) * pitch + 3 * m.w + 12) <= A.rgb_bytes;
-                const uint32_t off = words ? (uint32_t)ty.lo * (uint32_t)pitch : (uint32_t)ty.lo;
-                s_rows[warp][lane] = make_float2(__uint_as_float(off), ty.f);
-                if (words) {
-                    const uint8_t* row0 = base - 3 * (int64_t)px + off;       // about where the patch's part of this row begins: no more than a hint
-                    if (row0 >= A.rgb && row0 + 3 * p < A.rgb + A.rgb_bytes) { soon(row0); soon(row0 + 3 * p); }
-                }
+        look_up(A, A.index[first + sub], m);
+        if (m.ok) {
+            // the columns of a mirrored patch run to the left: its second is the left one
+            const int32_t ox = m.flip ? m.x.out - kCols - (m.col * p + px) : m.col * p + px;
+            const Tap tl = tap_of(ox, m.x), tr = kCols == 2 ? tap_of(ox + 1, m.x) : tl;
+            fl = tl.f; fr = tr.f;
+            base = m.corner + 3 * tl.lo; other = m.corner + 3 * tr.lo;
+            const uint32_t pitch = m.words ? (uint32_t)m.pitch : 1u;
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) {
+                const Tap ty = tap_of(m.row * p + px + k, m.y);
+                const uint32_t off = (uint32_t)ty.lo * pitch;
+                rows0[px + k] = make_uint4(off, ty.f != 0.f ? off + pitch : off, __float_as_uint(ty.f), 0);       // (weight 0: the row below may not be there)
+                if (m.words) soon(base + off);               // the patch's diagonal: its rows arrive together
             }
         }
     }
     __syncwarp();
     if (here) {
-        T* o = buf + sub * values + px;
-        const F2 scale = pack2(A.scale[0], A.scale[1]), shift = pack2(A.shift[0], A.shift[1]), minus = pack2(-1.f, -1.f);
-        auto put = [&](const Rgb& top, const Rgb& low, float fy) {
-            const F2 rg = fma2(fma2(pack2(fy, fy), fma2(top.rg, minus, low.rg), top.rg), scale, shift);
-            float r, g;
-            unpack2(rg, r, g);
-            o[0] = from_f<T>(r); o[area] = from_f<T>(g); o[2 * area] = from_f<T>(fmaf(fmaf(fy, low.b - top.b, top.b), A.scale[2], A.shift[2]));
-            o += p;
-        };
-        const float2* rows = &s_rows[warp][sub * p];
-        if (words) {
-            Rgb top = {0, 0.f}, low = {0, 0.f};
+        T* o = (kDirect ? static_cast<T*>(A.out) + (first + sub) * (uint64_t)values : buf + sub * values) + px;
+        const uint4* rows = rows0;
+        const bool swap = m.flip && m.ok;
+        auto value = [&](int c, float top, float low, float fy) { return fmaf(fmaf(fy, low - top, top), A.scale[c], A.shift[c]); };
+        if (kCols == 2 && m.words && other - base <= 6) {
+            const bool wide = other - base == 6;             // the right column two pixels on
+            const uint32_t shift = wide ? 16 : other != base ? 24 : 0;
+            const F2 f = pack2(fl, fr), minus = pack2(-1.f, -1.f);
             uint32_t top_at = ~0u, low_at = ~0u;
-            const uint32_t down = (uint32_t)pitch;
-            for (int dy = 0; dy < p; ++dy) {
-                const float2 r = rows[dy];
-                const uint32_t a = __float_as_uint(r.x), e = r.y != 0.f ? a + down : a;     // (weight 0: the row below may not be there)
-                if (a != top_at) {
-                    if (a == low_at) top = low; else top = mix_words(base + a, fx);
-                    top_at = a;
+            // On entry `top` holds the mixed row at low_at and `low` the one at top_at (the last output row's, roles swapped): as
+            // a rule an output row's upper source row is the last one's lower, and one row is mixed.
+            auto step = [&](Mixed<2>& top, Mixed<2>& low, const Words& now, Words& next, T* to, const uint4& r, const uint4& after) {
+                next = words_at(base + after.y, wide);
+                if (r.x != low_at) top = r.x == top_at ? low : mix_words(words_at(base + r.x, wide), wide, shift, f);
+                low = mix_words(now, wide, shift, f);
+                top_at = r.x; low_at = r.y;
+                const float fy = __uint_as_float(r.z);
+                const F2 fy2 = pack2(fy, fy);
+#pragma unroll
+                for (int c = 0; c < 3; ++c) {
+                    const F2 v = fma2(fma2(fy2, fma2(top.c[c], minus, low.c[c]), top.c[c]), pack2(A.scale[c], A.scale[c]), pack2(A.shift[c], A.shift[c]));
+                    float a, b;
+                    unpack2(v, a, b);
+                    put_two(to + c * area, a, b, swap);
                 }
-                if (e != low_at) {
-                    if (e == top_at) low = top; else low = mix_words(base + e, fx);
-                    low_at = e;
-                }
-                put(top, low, r.y);
+            };
+            Mixed<2> u = {}, v = {};
+            Words even = words_at(base + rows[0].y, wide), odd;
+#pragma unroll 1
+            for (int dy = 0; dy < p; dy += 2, o += 2 * p, rows += 2) {
+                const uint4 r0 = rows[0], r1 = rows[1], r2 = rows[dy + 2 < p ? 2 : 1];
+                step(u, v, even, odd, o, r0, r1);
+                step(v, u, odd, even, o + p, r1, r2);
             }
-        } else if (ok) {
-            for (int dy = 0; dy < p; ++dy) {
-                const float2 r = rows[dy];
-                const uint8_t* a = base + (int64_t)__float_as_uint(r.x) * pitch;
-                const Rgb top = mix_single(a, fx), low = r.y != 0.f ? mix_single(a + pitch, fx) : top;
-                put(top, low, r.y);
+        } else if (m.words) {
+            Rgb top[kCols], low[kCols];
+            const float f[2] = {fl, fr};
+            const uint8_t* const from[2] = {base, other};
+            uint32_t top_at = ~0u, low_at = ~0u;
+            for (int dy = 0; dy < p; ++dy, o += p) {
+                const uint4 r = rows[dy];
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) {
+                    if (r.x != top_at) { if (r.x == low_at) top[k] = low[k]; else top[k] = mix_words(from[k] + r.x, f[k]); }
+                    if (r.y != low_at) low[k] = mix_words(from[k] + r.y, f[k]);
+                    const float fy = __uint_as_float(r.z);
+                    T* to = o + (swap ? kCols - 1 - k : k);
+                    to[0] = from_f<T>(value(0, top[k].r, low[k].r, fy)); to[area] = from_f<T>(value(1, top[k].g, low[k].g, fy)); to[2 * area] = from_f<T>(value(2, top[k].b, low[k].b, fy));
+                }
+                top_at = r.x; low_at = r.y;
+            }
+        } else if (m.ok) {
+            for (int dy = 0; dy < p; ++dy, o += p) {
+                const uint4 r = rows[dy];
+                for (int k = 0; k < kCols; ++k) {
+                    const uint8_t* at = k ? other : base;
+                    const Rgb top = mix_single(at + r.x * m.pitch, k ? fr : fl), low = mix_single(at + r.y * m.pitch, k ? fr : fl);
+                    const float fy = __uint_as_float(r.z);
+                    T* to = o + (swap ? kCols - 1 - k : k);
+                    to[0] = from_f<T>(value(0, top.r, low.r, fy)); to[area] = from_f<T>(value(1, top.g, low.g, fy)); to[2 * area] = from_f<T>(value(2, top.b, low.b, fy));
+                }
             }
         } else {
-            for (int dy = 0; dy < p; ++dy, o += p) o[0] = o[area] = o[2 * area] = from_f<T>(0.f);
+            for (int dy = 0; dy < p; ++dy, o += p)
+                for (int k = 0; k < kCols; ++k) o[k] = o[k + area] = o[k + 2 * area] = from_f<T>(0.f);
         }
     }
+    if (kDirect) return;
     __syncwarp();
     const uint32_t bytes = (uint32_t)(count * values * (int)sizeof(T));
     unsigned char* out = static_cast<unsigned char*>(A.out) + first * (uint64_t)values * sizeof(T);

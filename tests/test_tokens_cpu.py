@@ -121,7 +121,7 @@ def test_patch_tokens_refuses():
     m, s = struct.pack("3f", 0.5, 0.5, 0.5), struct.pack("3f", 0.2, 0.2, 0.2)
     ok = [4096, 1000, 4096, 2, 4096, 10, 14, 2, m, s, B.PCR_BF16, 4096, None]
     call = B.lib().pcr_patch_tokens
-    for at, bad in [(0, None), (0, 4097), (2, None), (2, 4100), (3, -1), (4, None), (4, 4100), (5, -1), (5, 1 << 31), (6, 0), (6, 33), (7, 0), (7, 65), (8, None),
+    for at, bad in [(0, None), (0, 4097), (2, None), (2, 4104), (3, -1), (4, None), (4, 4100), (5, -1), (5, 1 << 31), (6, 0), (6, 33), (7, 0), (7, 65), (8, None),
                     (9, None), (9, struct.pack("3f", 0.2, 0.0, 0.2)), (9, struct.pack("3f", 0.2, math.nan, 0.2)), (8, struct.pack("3f", math.inf, 0, 0)),
                     (10, 3), (11, None), (11, 4097)]:
         args = list(ok)
