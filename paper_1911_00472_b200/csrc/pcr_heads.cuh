@@ -14,6 +14,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 namespace pcr {
@@ -45,7 +46,8 @@ struct HeadArgs {
     float eps, inv_dim;
 };
 
-template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
+// N elements as 32-bit words: two 16-bit elements are taken apart and put together in one or two instructions.
+template <typename T, int N> struct alignas(sizeof(T) * N) Vec { uint32_t w[N * sizeof(T) / 4]; };
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
@@ -54,6 +56,34 @@ template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ void two_of(uint32_t w, float& a, float& b, __nv_bfloat16) { a = __uint_as_float(w << 16); b = __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ void two_of(uint32_t w, float& a, float& b, __half) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x; b = f.y;
+}
+__device__ __forceinline__ uint32_t word_of(float a, float b, __nv_bfloat16) { const __nv_bfloat162 v = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&v); }
+__device__ __forceinline__ uint32_t word_of(float a, float b, __half) { const __half2 v = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&v); }
+template <typename T, int N> __device__ __forceinline__ void floats_of(const Vec<T, N>& v, float (&f)[N]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = __uint_as_float(v.w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) two_of(v.w[i / 2], f[i], f[i + 1], T());
+    }
+}
+template <typename T, int N> __device__ __forceinline__ Vec<T, N> vec_of(const float (&f)[N]) {
+    Vec<T, N> v;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v.w[i] = __float_as_uint(f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) v.w[i / 2] = word_of(f[i], f[i + 1], T());
+    }
+    return v;
+}
 
 // cosine and sine of position * freq: the whole turns are taken off in 64 bits, what is left fits single precision
 __device__ __forceinline__ void turn_of(int32_t position, double freq, bool inverse, float& c, float& s) {
@@ -83,40 +113,64 @@ __device__ __forceinline__ void positions_of(const HeadArgs& A, uint32_t b, uint
     for (int a = 0; a < kMaxAxes; ++a) p[a] = a < A.n_axes ? __ldg(at + (int64_t)a * A.ps[0]) : 0;
 }
 
+// The kernel that adds the weights' sums up is launched while this one runs and waits for its end.
+__device__ __forceinline__ void sums_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void sums_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 enum { kTurn = 0, kNormTurn = 1, kNormTurnBack = 2 };
 
-// Sums over the `n` lanes of a row, this lane being number `at` of it, the row's first lane `first`; every lane gets them.
-// Where n is no power of two, sums of 1, 2, 4, ... lanes going round the row are made, and those that n's bits name added
-// up: as few shuffles as for the next larger power of two and no condition on the lane.  n is the same for all lanes.
+// How the `n` lanes of a row add up.  Where n is no power of two, sums of 1, 2, 4, ... lanes going round the row are made,
+// and those that n's bits name added up: as few shuffles as for the next larger power of two, and no condition on the lane.
+// `twice` and `rest` hold the lanes to take from, six bits a step.  n is the same for all lanes.
+struct RowLanes {
+    int n;
+    bool power;
+    uint32_t twice, rest;
+    __device__ __forceinline__ RowLanes(int n_, int first, int at) : n(n_), power((n_ & (n_ - 1)) == 0), twice(0), rest(0) {
+        auto round = [&](int o) { const int l = at + o; return (uint32_t)(first + (l < n ? l : l - n)); };
+        int have = 0;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const int o = 1 << i;
+            if (o < n) twice |= round(o) << (6 * i);
+            if (n & o) { if (have < n) rest |= round(have) << (6 * i); have += o; }
+        }
+    }
+};
 template <int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], int first, int at, int n) {
-    if ((n & (n - 1)) == 0) {
+__device__ __forceinline__ void row_sums(float (&v)[N], const RowLanes& L) {
+    if (L.power) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            if (o >= n) return;
+            if (o >= L.n) return;
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
         }
         return;
     }
-    auto round = [&](int o) { const int l = at + o; return first + (l < n ? l : l - n); };
     float all[N];
-    int have = 0;
+    bool none = true;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        if (n & o) {
-            const int from = round(have);
+    for (int i = 0; i < 5; ++i) {
+        if (L.n >> i & 1) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) all[k] = have == 0 ? v[k] : all[k] + __shfl_sync(0xffffffffu, v[k], from);
-            have += o;
+            for (int k = 0; k < N; ++k) all[k] = none ? v[k] : all[k] + __shfl_sync(0xffffffffu, v[k], (int)(L.rest >> (6 * i)));
+            none = false;
         }
-        if (2 * o > n) break;
-        const int from = round(o);
+        if (L.n >> (i + 1) == 0) break;
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_sync(0xffffffffu, v[k], from);
+        for (int k = 0; k < N; ++k) v[k] += __shfl_sync(0xffffffffu, v[k], (int)(L.twice >> (6 * i)));
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = all[k];
+}
+
+// A frequency as the turns of one position, a fraction of 2^64 (a whole turn, 2^64 itself, saturates to just below).
+__device__ __forceinline__ uint2 fraction_of(double freq) {
+    double t = freq * 0.15915494309189533577;                   // 1 / (2 pi)
+    t -= floor(t);
+    const unsigned long long f = __double2ull_rn(t * 18446744073709551616.0);
+    return make_uint2((uint32_t)f, (uint32_t)(f >> 32));
 }
 
 // What a CTA of the vector kernels keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its
@@ -130,10 +184,7 @@ template <int kParts> struct HeadTables {          // 0 parts: no weights, 1: of
 template <typename T, int kParts>
 __device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables<kParts>& S, int first) {
     for (int j = threadIdx.x; j < A.rot / 2; j += kHeadThreads) {
-        double t = freq_at(A, j) * 0.15915494309189533577;                   // 1 / (2 pi)
-        t -= floor(t);
-        const unsigned long long f = __double2ull_rn(t * 18446744073709551616.0);      // (2^64 itself, a whole turn, saturates to just below)
-        S.turn[j] = make_uint2((uint32_t)f, (uint32_t)(f >> 32));
+        S.turn[j] = fraction_of(freq_at(A, j));
         S.axis[j] = A.axes[j];
     }
 #pragma unroll
@@ -158,25 +209,19 @@ __device__ __forceinline__ void turn_by(int32_t position, uint2 turn, bool inver
     if (inverse) s = -s;
 }
 
-// Where the lanes of a warp stand: number `at` of a row, which of the warp's rows, and the K chunks of the row that this
-// lane has: every `lanes`-th, two vectors each.
-template <int V, int K, bool kNext> struct Place {
-    int lanes, rows, sub, at, first;
-    int o1[K], o2[K], pair[K];
-    bool in_row, turns[K];
+// Where the lanes of a warp stand: number `at` of a row, which of the warp's rows, and where the lane's two vectors of V
+// elements begin in a head (`gap` elements apart).
+template <int V, bool kNext> struct Place {
+    int rows, sub, at, o1, gap, pair;
+    bool in_row, turns;
     __device__ __forceinline__ explicit Place(const HeadArgs& A) {
         const int lane = threadIdx.x & 31, turning = A.rot / (2 * V);
-        lanes = A.lanes; rows = 32 / lanes; sub = lane / lanes; at = lane - sub * lanes; first = sub * lanes;
-        in_row = sub < rows;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int chunk = at + k * lanes;
-            turns[k] = chunk < turning; pair[k] = chunk * V;
-            if (kNext) { o1[k] = 2 * V * chunk; o2[k] = o1[k] + V; }
-            else if (turns[k]) { o1[k] = pair[k]; o2[k] = pair[k] + A.rot / 2; }
-            else { o1[k] = A.rot + 2 * V * (chunk - turning); o2[k] = o1[k] + V; }
-        }
+        rows = 32 / A.lanes; sub = lane / A.lanes; at = lane - sub * A.lanes;
+        in_row = sub < rows; turns = at < turning; pair = at * V;
+        o1 = kNext ? 2 * V * at : turns ? pair : A.rot + 2 * V * (at - turning);
+        gap = kNext || !turns ? V : A.rot / 2;
     }
+    __device__ __forceinline__ RowLanes row_lanes(const HeadArgs& A) const { return RowLanes(A.lanes, sub * A.lanes, at); }
 };
 
 // The elements that make pair i: of the first and of the second vector, or 2 i and 2 i + 1 of both together.
@@ -194,85 +239,70 @@ __device__ __forceinline__ void unpack2(F2 v, float& a, float& b) { asm("mov.b64
 __device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 
-// The chunks of a row that a lane has: as they lie in memory, and as pairs two by two, first elements in a, second in b.
-template <typename T, int V, int K> struct Row { Vec<T, V> a[K], b[K]; };
-template <int V, int K> struct Pairs { F2 a[K][V / 2], b[K][V / 2]; };
+// A lane's part of a row: as it lies in memory, and as pairs two by two, first elements in a, second ones in b.
+template <typename T, int V> struct Row { Vec<T, V> a, b; };
+template <int V> struct Pairs { F2 a[V / 2], b[V / 2]; };
 
-template <typename T, int V, int K, bool kNext>
-__device__ __forceinline__ Row<T, V, K> load_row(const T* x, const Place<V, K, kNext>& at) {
-    Row<T, V, K> r;
-#pragma unroll
-    for (int k = 0; k < K; ++k) { r.a[k] = *reinterpret_cast<const Vec<T, V>*>(x + at.o1[k]); r.b[k] = *reinterpret_cast<const Vec<T, V>*>(x + at.o2[k]); }
-    return r;
+template <typename T, int V>
+__device__ __forceinline__ Row<T, V> load_row(const T* x, int gap) {
+    return {*reinterpret_cast<const Vec<T, V>*>(x), *reinterpret_cast<const Vec<T, V>*>(x + gap)};
 }
-template <typename T, int V, int K, bool kNext>
-__device__ __forceinline__ Pairs<V, K> pairs_of(const Row<T, V, K>& row) {
-    Pairs<V, K> r;
+template <typename T, int V>
+__device__ __forceinline__ void store_row(T* y, int gap, const Row<T, V>& r) {
+    *reinterpret_cast<Vec<T, V>*>(y) = r.a;
+    *reinterpret_cast<Vec<T, V>*>(y + gap) = r.b;
+}
+template <typename T, int V, bool kNext>
+__device__ __forceinline__ Pairs<V> pairs_of(const Row<T, V>& row) {
+    float f[V], g[V];
+    floats_of(row.a, f);
+    floats_of(row.b, g);
+    Pairs<V> r;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float f[V], g[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) { f[i] = to_f(row.a[k].v[i]); g[i] = to_f(row.b[k].v[i]); }
-#pragma unroll
-        for (int i = 0; i < V; i += 2) {
-            r.a[k][i / 2] = pack2(one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
-            r.b[k][i / 2] = pack2(two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
-        }
+    for (int i = 0; i < V; i += 2) {
+        r.a[i / 2] = pack2(one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
+        r.b[i / 2] = pack2(two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
     }
     return r;
 }
-template <typename T, int V, int K, bool kNext>
-__device__ __forceinline__ Row<T, V, K> row_of(const Pairs<V, K>& p) {
-    Row<T, V, K> r;
+template <typename T, int V, bool kNext>
+__device__ __forceinline__ Row<T, V> row_of(const Pairs<V>& p) {
+    float f[V], g[V];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float f[V], g[V];
-#pragma unroll
-        for (int i = 0; i < V; i += 2) {
-            unpack2(p.a[k][i / 2], one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
-            unpack2(p.b[k][i / 2], two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) { r.a[k].v[i] = from_f<T>(f[i]); r.b[k].v[i] = from_f<T>(g[i]); }
+    for (int i = 0; i < V; i += 2) {
+        unpack2(p.a[i / 2], one<V, kNext>(f, g, i), one<V, kNext>(f, g, i + 1));
+        unpack2(p.b[i / 2], two<V, kNext>(f, g, i), two<V, kNext>(f, g, i + 1));
     }
-    return r;
+    return {vec_of<T, V>(f), vec_of<T, V>(g)};
 }
-template <typename T, int V, int K, bool kNext>
-__device__ __forceinline__ void store_row(T* y, const Place<V, K, kNext>& at, const Row<T, V, K>& r) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) { *reinterpret_cast<Vec<T, V>*>(y + at.o1[k]) = r.a[k]; *reinterpret_cast<Vec<T, V>*>(y + at.o2[k]) = r.b[k]; }
-}
-template <int V, int K, bool kNext>
-__device__ __forceinline__ Pairs<V, K> weights_of(const float* w, const Place<V, K, kNext>& at) {
-    return pairs_of<float, V, K, kNext>(load_row<float, V, K, kNext>(w, at));
+template <int V, bool kNext>
+__device__ __forceinline__ Pairs<V> weights_of(const float* w, const Place<V, kNext>& at) {
+    return pairs_of<float, V, kNext>(load_row<float, V>(w + at.o1, at.gap));
 }
 // cosine and sine of the lane's pairs at a token's positions
-template <typename T, int V, int K, bool kNext, int kParts>
-__device__ __forceinline__ void turns_of(const HeadArgs& A, const HeadTables<kParts>& S, const int32_t (&p)[kMaxAxes], const Place<V, K, kNext>& at, F2 (&c)[K][V / 2], F2 (&s)[K][V / 2]) {
+template <typename T, int V, bool kNext, int kParts>
+__device__ __forceinline__ void turns_of(const HeadArgs& A, const HeadTables<kParts>& S, const int32_t (&p)[kMaxAxes], const Place<V, kNext>& at, F2 (&c)[V / 2], F2 (&s)[V / 2]) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int i = 0; i < V; i += 2) {
+        float fc[2] = {1.f, 1.f}, fs[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < V; i += 2) {
-            float fc[2] = {1.f, 1.f}, fs[2] = {0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int pair = at.pair[k] + i + j;
-                if (at.turns[k]) turn_by<T>(on_axis(p, S.axis[pair]), S.turn[pair], A.inverse, fc[j], fs[j]);
-            }
-            c[k][i / 2] = pack2(fc[0], fc[1]); s[k][i / 2] = pack2(fs[0], fs[1]);
-        }
+        for (int j = 0; j < 2; ++j)
+            if (at.turns) turn_by<T>(on_axis(p, S.axis[at.pair + i + j]), S.turn[at.pair + i + j], A.inverse, fc[j], fs[j]);
+        c[i / 2] = pack2(fc[0], fc[1]); s[i / 2] = pack2(fs[0], fs[1]);
+    }
 }
 __device__ __forceinline__ F2 negative(F2 v) { return v ^ 0x8000000080000000ull; }
 __device__ __forceinline__ void soon(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 
+constexpr int kRowsAhead = 4;
 // Forward: grid (token groups, shares of `per` heads of queries and keys in a row).  A warp takes 32 / lanes tokens, a
 // thread `per` heads of its token, kAhead of them at a time.  Lanes without a token go along with the last one's data and
 // store nothing: no shuffle and no load stands in a branch.
-template <typename T, int V, int K, bool kNorm, bool kNext>
-__global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? (kNorm ? 3 : 4) : kNorm ? 5 : 6) heads_kernel(const __grid_constant__ HeadArgs A) {
-    constexpr int kWarps = kHeadThreads / 32, kBytes = V * K * (int)sizeof(T), kAhead = kBytes > 16 ? 2 : kBytes > 8 ? 4 : 8;
+template <typename T, int V, bool kNorm, bool kNext>
+__global__ void __launch_bounds__(kHeadThreads, kNorm ? 5 : 6) heads_kernel(const __grid_constant__ HeadArgs A) {
+    constexpr int kWarps = kHeadThreads / 32, kAhead = kRowsAhead, N = V / 2;
     __shared__ HeadTables<kNorm ? 2 : 0> S;
-    const Place<V, K, kNext> at(A);
+    const Place<V, kNext> at(A);
     const uint32_t n0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * (uint32_t)at.rows + (uint32_t)at.sub;
     const bool live = at.in_row && n0 < A.tokens;
     const uint32_t n = min(n0, A.tokens - 1), b = n / A.seq, t = n - b * A.seq;
@@ -280,16 +310,16 @@ __global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? (kNorm ? 3 : 4) : kN
     int which = from < A.part[0].heads ? 0 : 1;
     {   // the first row is on its way while the tables are filled
         const HeadBlock& H = A.part[which];
-        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + (int64_t)(from - (which ? A.part[0].heads : 0)) * H.xs[2];
-#pragma unroll
-        for (int k = 0; k < K; ++k) { soon(x + at.o1[k]); soon(x + at.o2[k]); }
+        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + (int64_t)(from - (which ? A.part[0].heads : 0)) * H.xs[2] + at.o1;
+        soon(x); soon(x + at.gap);
     }
     int32_t p[kMaxAxes];
     positions_of(A, b, t, p);
     fill_tables<T>(A, S, 0);
     __syncthreads();
-    F2 c[K][V / 2], s[K][V / 2];
-    turns_of<T, V, K, kNext>(A, S, p, at, c, s);
+    const RowLanes lanes = at.row_lanes(A);
+    F2 c[N], s[N];
+    turns_of<T, V, kNext>(A, S, p, at, c, s);
 #pragma unroll 1
     for (; which < 2; ++which) {
         const HeadBlock& H = A.part[which];
@@ -297,191 +327,180 @@ __global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? (kNorm ? 3 : 4) : kN
         const int h0 = max(from - base, 0), h1 = min(to - base, H.heads);
         if (h0 >= h1) continue;
         // a' = a wa c + b (-wb s), b' = a wa s + b wb c: four factors a pair, the same for all heads
-        F2 ac[K][V / 2], as[K][V / 2], bc[K][V / 2], bs[K][V / 2];
+        F2 ac[N], as[N], bc[N], bs[N];
         {
-            Pairs<V, K> w;
-            if (kNorm) w = weights_of<V, K, kNext>(S.w[kNorm ? which : 0], at);
+            Pairs<V> w;
+            if (kNorm) w = weights_of<V, kNext>(S.w[kNorm ? which : 0], at);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V / 2; ++i) {
-                    ac[k][i] = kNorm ? mul2(w.a[k][i], c[k][i]) : c[k][i];
-                    as[k][i] = kNorm ? mul2(w.a[k][i], s[k][i]) : s[k][i];
-                    bc[k][i] = kNorm ? mul2(w.b[k][i], c[k][i]) : c[k][i];
-                    bs[k][i] = negative(kNorm ? mul2(w.b[k][i], s[k][i]) : s[k][i]);
-                }
+            for (int i = 0; i < N; ++i) {
+                ac[i] = kNorm ? mul2(w.a[i], c[i]) : c[i]; as[i] = kNorm ? mul2(w.a[i], s[i]) : s[i];
+                bc[i] = kNorm ? mul2(w.b[i], c[i]) : c[i]; bs[i] = negative(kNorm ? mul2(w.b[i], s[i]) : s[i]);
+            }
         }
         const int64_t xs = H.xs[2], ys = H.ys[2];
-        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + h0 * xs;
-        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + h0 * ys;
-        auto work = [&](const Row<T, V, K>& row) {
-            Pairs<V, K> v = pairs_of<T, V, K, kNext>(row);
+        const T* x = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + h0 * xs + at.o1;
+        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + h0 * ys + at.o1;
+        auto work = [&](const Row<T, V>& row) {
+            Pairs<V> v = pairs_of<T, V, kNext>(row);
             if (kNorm) {
                 F2 sq = 0;
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-#pragma unroll
-                    for (int i = 0; i < V / 2; ++i) { sq = fma2(v.a[k][i], v.a[k][i], sq); sq = fma2(v.b[k][i], v.b[k][i], sq); }
+                for (int i = 0; i < N; ++i) { sq = fma2(v.a[i], v.a[i], sq); sq = fma2(v.b[i], v.b[i], sq); }
                 float sum[1], other;
                 unpack2(sq, sum[0], other);
                 sum[0] += other;
-                row_sums<1>(sum, at.first, at.at, at.lanes);
+                row_sums<1>(sum, lanes);
                 const float r = rsqrtf(sum[0] * A.inv_dim + A.eps);
                 const F2 r2 = pack2(r, r);
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-#pragma unroll
-                    for (int i = 0; i < V / 2; ++i) { v.a[k][i] = mul2(v.a[k][i], r2); v.b[k][i] = mul2(v.b[k][i], r2); }
+                for (int i = 0; i < N; ++i) { v.a[i] = mul2(v.a[i], r2); v.b[i] = mul2(v.b[i], r2); }
             }
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V / 2; ++i) {
-                    const F2 u = fma2(v.b[k][i], bs[k][i], mul2(v.a[k][i], ac[k][i])), e = fma2(v.b[k][i], bc[k][i], mul2(v.a[k][i], as[k][i]));
-                    v.a[k][i] = u; v.b[k][i] = e;
-                }
-            if (live) store_row<T, V, K, kNext>(y, at, row_of<T, V, K, kNext>(v));
+            for (int i = 0; i < N; ++i) {
+                const F2 u = fma2(v.b[i], bs[i], mul2(v.a[i], ac[i])), e = fma2(v.b[i], bc[i], mul2(v.a[i], as[i]));
+                v.a[i] = u; v.b[i] = e;
+            }
+            if (live) store_row<T, V>(y, at.gap, row_of<T, V, kNext>(v));
             y += ys;
         };
         int h = h0;
 #pragma unroll 1
         for (; h + kAhead <= h1; h += kAhead) {
-            Row<T, V, K> rows[kAhead];
+            Row<T, V> rows[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k, x += xs) rows[k] = load_row<T, V, K, kNext>(x, at);
+            for (int k = 0; k < kAhead; ++k, x += xs) rows[k] = load_row<T, V>(x, at.gap);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) work(rows[k]);
         }
-#pragma unroll 1
-        for (; h < h1; ++h, x += xs) work(load_row<T, V, K, kNext>(x, at));
+        if (h < h1) {                              // (the bounds are the same for the whole CTA)
+            Row<T, V> rows[kAhead - 1];
+#pragma unroll
+            for (int k = 0; k < kAhead - 1; ++k, x += xs)
+                if (h + k < h1) rows[k] = load_row<T, V>(x, at.gap);
+#pragma unroll
+            for (int k = 0; k < kAhead - 1; ++k)
+                if (h + k < h1) work(rows[k]);
+        }
     }
 }
 
 // Copies of N bytes to shared memory that the thread does not wait for, and the wait for all but the newest `kLeft` groups.
-template <int N> __device__ __forceinline__ void copy_soon(void* to, const void* from) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(N) : "memory");
+template <int N> __device__ __forceinline__ void copy_soon(uint32_t to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(N) : "memory");
 }
 __device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// Backward: the first part[0].slots CTAs take the queries, the others the keys; a warp goes round the tokens and over all
-// heads of each, so that the sums for the weights stay in registers to the end.
+// Backward: the first part[0].slots CTAs take the queries, the others the keys, in turn each share of `per` heads; a warp
+// goes round the tokens and over its heads of each, so that the sums for the weights stay in registers to the end.
 //   q = d a, dot = sum of q w, dw += q r, dx = r (d w - a r^2 dot / dim)
 // Two operands, their factors and the sums leave no registers for rows on their way.  So every lane has a ring of kStages
 // groups of rows in shared memory that it alone fills and reads: no barrier, and kStages - 1 groups are always on their way.
-template <typename T, int V, int K, bool kNext>
-__global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? 3 : 4) heads_back_kernel(const __grid_constant__ HeadArgs A) {
-    constexpr int kWarps = kHeadThreads / 32, kBytes = V * (int)sizeof(T), kGroup = kBytes * K >= 16 ? 1 : 2, kStages = kBytes * K * kGroup > 24 ? 2 : kBytes * K * kGroup > 16 ? 3 : 4, N = V / 2;
+__host__ __device__ constexpr int kBackCtas(int vector_bytes) { return vector_bytes >= 16 ? 3 : 4; }      // of an SM: what the registers leave room for
+template <typename T, int V, bool kNext>
+__global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_back_kernel(const __grid_constant__ HeadArgs A) {
+    constexpr int kWarps = kHeadThreads / 32, kBytes = V * (int)sizeof(T), kGroup = kBytes >= 16 ? 1 : 2, kStages = 4, N = V / 2;
     using VT = Vec<T, V>;
-    struct Ring { VT rows[kStages][kGroup][K][4][32]; int32_t positions[kStages][kMaxAxes][32]; };
+    struct Stage { VT rows[kGroup][4][32]; int32_t positions[kMaxAxes][32]; };
     __shared__ HeadTables<1> S;
-    __shared__ union { Ring ring[kWarps]; float sums[kWarps][kMaxHeadDim]; } U;
+    __shared__ union { Stage ring[kWarps][kStages]; float sums[kWarps][kMaxHeadDim]; } U;
     const int which = (int)blockIdx.x >= A.part[0].slots ? 1 : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const HeadBlock& H = A.part[which];
     const uint32_t mine = blockIdx.x - (which ? (uint32_t)A.part[0].slots : 0u);
-    const Place<V, K, kNext> at(A);
-    const int heads = H.heads;
+    const Place<V, kNext> at(A);
+    const uint32_t shares = (uint32_t)(H.heads + A.per - 1) / (uint32_t)A.per, group = mine / shares;
+    const int h0 = (int)(mine - group * shares) * A.per, heads = min(A.per, H.heads - h0);
     const int64_t xs = H.xs[2], gs = H.gs[2], ys = H.ys[2];
-    const uint64_t step = (uint64_t)H.slots * kWarps * at.rows, begin = (uint64_t)(mine * kWarps + warp) * at.rows;
-    Ring& R = U.ring[warp];
-    auto token_of = [&](uint64_t base, uint32_t& b, uint32_t& t) {        // lanes without one go along with the last
-        const uint32_t n = (uint32_t)min(base + at.sub, (uint64_t)A.tokens - 1);
+    const uint32_t step = (uint32_t)H.slots / shares * (uint32_t)(kWarps * at.rows), begin = (group * kWarps + warp) * (uint32_t)at.rows;     // (sums of tokens and steps fit)
+    auto token_of = [&](uint32_t base, uint32_t& b, uint32_t& t) {        // lanes without one go along with the last
+        const uint32_t n = min(base + at.sub, A.tokens - 1);
         b = n / A.seq; t = n - b * A.seq;
     };
 
     // the side that fills
-    uint64_t fbase = begin;
-    int fhead = 0, fstage = 0;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&U.ring[warp][0]) + lane * kBytes, ring_end = ring + kStages * (uint32_t)sizeof(Stage);
+    uint32_t fbase = begin, fat = ring;
+    int fhead = 0;
     const T *fx = nullptr, *fg = nullptr;
     auto fill = [&]() {
         if (fbase < A.tokens) {
             if (fhead == 0) {
                 uint32_t b, t;
                 token_of(fbase, b, t);
-                fx = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1];
-                fg = static_cast<const T*>(H.g) + (int64_t)b * H.gs[0] + (int64_t)t * H.gs[1];
+                fx = static_cast<const T*>(H.x) + (int64_t)b * H.xs[0] + (int64_t)t * H.xs[1] + h0 * xs + at.o1;
+                fg = static_cast<const T*>(H.g) + (int64_t)b * H.gs[0] + (int64_t)t * H.gs[1] + h0 * gs + at.o1;
                 const int32_t* p = A.positions + (int64_t)b * A.ps[1] + (int64_t)t * A.ps[2];
+                const uint32_t to = fat + (uint32_t)offsetof(Stage, positions) + lane * (4 - kBytes);
 #pragma unroll
                 for (int a = 0; a < kMaxAxes; ++a)
-                    if (a < A.n_axes) copy_soon<4>(&R.positions[fstage][a][lane], p + (int64_t)a * A.ps[0]);
+                    if (a < A.n_axes) copy_soon<4>(to + a * 128, p + (int64_t)a * A.ps[0]);
             }
 #pragma unroll
             for (int m = 0; m < kGroup; ++m, fx += xs, fg += gs)
-                if (fhead + m < heads) {
-#pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        VT(*to)[32] = R.rows[fstage][m][k];
-                        copy_soon<kBytes>(&to[0][lane], fx + at.o1[k]); copy_soon<kBytes>(&to[1][lane], fx + at.o2[k]);
-                        copy_soon<kBytes>(&to[2][lane], fg + at.o1[k]); copy_soon<kBytes>(&to[3][lane], fg + at.o2[k]);
-                    }
+                if (m == 0 || fhead + m < heads) {
+                    const uint32_t to = fat + m * 4 * 32 * kBytes;
+                    copy_soon<kBytes>(to, fx); copy_soon<kBytes>(to + 32 * kBytes, fx + at.gap);
+                    copy_soon<kBytes>(to + 64 * kBytes, fg); copy_soon<kBytes>(to + 96 * kBytes, fg + at.gap);
                 }
             fhead += kGroup;
             if (fhead >= heads) { fhead = 0; fbase += step; }
         }
-        fstage = fstage + 1 == kStages ? 0 : fstage + 1;
+        fat += (uint32_t)sizeof(Stage);
+        if (fat == ring_end) fat = ring;
         copies_close();
     };
 #pragma unroll 1
     for (int k = 0; k < kStages - 1; ++k) fill();
     fill_tables<T>(A, S, which);
     __syncthreads();
-    const Pairs<V, K> w = weights_of<V, K, kNext>(S.w[0], at);
-    Pairs<V, K> dw;
+    const RowLanes lanes = at.row_lanes(A);
+    const Pairs<V> w = weights_of<V, kNext>(S.w[0], at);
+    Pairs<V> dw;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < N; ++i) dw.a[k][i] = dw.b[k][i] = 0;
+    for (int i = 0; i < N; ++i) dw.a[i] = dw.b[i] = 0;
     int stage = 0;
 #pragma unroll 1
-    for (uint64_t base = begin; base < A.tokens; base += step) {
+    for (uint32_t base = begin; base < A.tokens; base += step) {
         const bool live = at.in_row && base + at.sub < A.tokens;
         uint32_t b, t;
         token_of(base, b, t);
-        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1];
-        F2 c[K][N], s[K][N];
+        T* y = static_cast<T*>(H.y) + (int64_t)b * H.ys[0] + (int64_t)t * H.ys[1] + h0 * ys + at.o1;
+        F2 c[N], s[N];
 #pragma unroll 1
         for (int h = 0; h < heads; h += kGroup) {
             copies_wait<kStages - 2>();
+            const Stage& from = U.ring[warp][stage];
             if (h == 0) {
                 int32_t p[kMaxAxes];
 #pragma unroll
-                for (int a = 0; a < kMaxAxes; ++a) p[a] = a < A.n_axes ? R.positions[stage][a][lane] : 0;
-                turns_of<T, V, K, kNext>(A, S, p, at, c, s);
+                for (int a = 0; a < kMaxAxes; ++a) p[a] = a < A.n_axes ? from.positions[a][lane] : 0;
+                turns_of<T, V, kNext>(A, S, p, at, c, s);
             }
             auto work = [&](int m) {
-                Row<T, V, K> row, grow;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    VT(*from)[32] = R.rows[stage][m][k];
-                    row.a[k] = from[0][lane]; row.b[k] = from[1][lane]; grow.a[k] = from[2][lane]; grow.b[k] = from[3][lane];
-                }
-                const Pairs<V, K> x2 = pairs_of<T, V, K, kNext>(row);
-                Pairs<V, K> d = pairs_of<T, V, K, kNext>(grow), q;
+                const Pairs<V> x2 = pairs_of<T, V, kNext>(Row<T, V>{from.rows[m][0][lane], from.rows[m][1][lane]});
+                Pairs<V> d = pairs_of<T, V, kNext>(Row<T, V>{from.rows[m][2][lane], from.rows[m][3][lane]}), q;
+                const F2 minus = pack2(-1.f, -1.f);
                 F2 sq = 0, dot = 0;
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        const F2 u = fma2(d.b[k][i], s[k][i], mul2(d.a[k][i], c[k][i])), v = fma2(d.a[k][i], negative(s[k][i]), mul2(d.b[k][i], c[k][i]));
-                        q.a[k][i] = mul2(u, x2.a[k][i]); q.b[k][i] = mul2(v, x2.b[k][i]);
-                        sq = fma2(x2.a[k][i], x2.a[k][i], sq); sq = fma2(x2.b[k][i], x2.b[k][i], sq);
-                        dot = fma2(q.a[k][i], w.a[k][i], dot); dot = fma2(q.b[k][i], w.b[k][i], dot);
-                        d.a[k][i] = mul2(u, w.a[k][i]); d.b[k][i] = mul2(v, w.b[k][i]);
-                    }
+                for (int i = 0; i < N; ++i) {
+                    const F2 u = fma2(d.b[i], s[i], mul2(d.a[i], c[i])), v = fma2(mul2(d.a[i], s[i]), minus, mul2(d.b[i], c[i]));
+                    q.a[i] = mul2(u, x2.a[i]); q.b[i] = mul2(v, x2.b[i]);
+                    sq = fma2(x2.a[i], x2.a[i], sq); sq = fma2(x2.b[i], x2.b[i], sq);
+                    dot = fma2(q.a[i], w.a[i], dot); dot = fma2(q.b[i], w.b[i], dot);
+                    d.a[i] = mul2(u, w.a[i]); d.b[i] = mul2(v, w.b[i]);
+                }
                 float sum[2], other[2];
                 unpack2(sq, sum[0], other[0]); unpack2(dot, sum[1], other[1]);
                 sum[0] += other[0]; sum[1] += other[1];
-                row_sums<2>(sum, at.first, at.at, at.lanes);
+                row_sums<2>(sum, lanes);
                 const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m1 = -(sum[1] * r * A.inv_dim * r), rl = live ? r : 0.f;
                 const F2 r2 = pack2(r, r), m2 = pack2(m1, m1), rl2 = pack2(rl, rl);
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        d.a[k][i] = mul2(fma2(x2.a[k][i], m2, d.a[k][i]), r2); d.b[k][i] = mul2(fma2(x2.b[k][i], m2, d.b[k][i]), r2);
-                        dw.a[k][i] = fma2(q.a[k][i], rl2, dw.a[k][i]); dw.b[k][i] = fma2(q.b[k][i], rl2, dw.b[k][i]);
-                    }
-                if (live) store_row<T, V, K, kNext>(y, at, row_of<T, V, K, kNext>(d));
+                for (int i = 0; i < N; ++i) {
+                    d.a[i] = mul2(fma2(x2.a[i], m2, d.a[i]), r2); d.b[i] = mul2(fma2(x2.b[i], m2, d.b[i]), r2);
+                    dw.a[i] = fma2(q.a[i], rl2, dw.a[i]); dw.b[i] = fma2(q.b[i], rl2, dw.b[i]);
+                }
+                if (live) store_row<T, V>(y, at.gap, row_of<T, V, kNext>(d));
                 y += ys;
             };
             if (kGroup == 2 && h + 2 <= heads) { work(0); work(kGroup - 1); }
@@ -491,21 +510,23 @@ __global__ void __launch_bounds__(kHeadThreads, V * K > 8 ? 3 : 4) heads_back_ke
         }
     }
     copies_wait<0>();
+    sums_may_start();
     if (H.partial == nullptr) return;                           // (the same for the whole CTA)
     __syncthreads();                                            // the rings make room for the sums
     // the rows of a warp in the order of their lanes, then the warps in theirs
-    const Row<float, V, K> mine_dw = row_of<float, V, K, kNext>(dw);
+    const Row<float, V> row_dw = row_of<float, V, kNext>(dw);
+    float dw1[V], dw2[V];
+    floats_of(row_dw.a, dw1);
+    floats_of(row_dw.b, dw2);
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float p = mine_dw.a[k].v[i], q = mine_dw.b[k].v[i];
-            for (int m = 1; m < at.rows; ++m) {
-                const int from = at.at + m * at.lanes;
-                p += __shfl_sync(0xffffffffu, mine_dw.a[k].v[i], from); q += __shfl_sync(0xffffffffu, mine_dw.b[k].v[i], from);
-            }
-            if (at.sub == 0) { U.sums[warp][at.o1[k] + i] = p; U.sums[warp][at.o2[k] + i] = q; }
+    for (int i = 0; i < V; ++i) {
+        float p = dw1[i], q = dw2[i];
+        for (int m = 1; m < at.rows; ++m) {
+            const int from = at.at + m * A.lanes;
+            p += __shfl_sync(0xffffffffu, dw1[i], from); q += __shfl_sync(0xffffffffu, dw2[i], from);
         }
+        if (at.sub == 0) { U.sums[warp][at.o1 + i] = p; U.sums[warp][at.o1 + at.gap + i] = q; }
+    }
     __syncthreads();
     float* out = H.partial + (size_t)mine * A.dim;
     for (int j = threadIdx.x; j < A.dim; j += kHeadThreads) {
@@ -555,7 +576,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_co
                     for (int j = A.rot + lane; j < A.dim; j += 32) dot += to_f(g[j]) * weight(j) * to_f(x[j]);
                 }
                 float sum[2] = {sq, dot};
-                row_sums<2>(sum, 0, lane, 32);
+                row_sums<2>(sum, RowLanes(32, 0, lane));
                 r = rsqrtf(sum[0] * A.inv_dim + A.eps);
                 m = sum[1] * r * A.inv_dim;
             }
@@ -617,11 +638,14 @@ __global__ void __launch_bounds__(kSumThreads) weight_sums_kernel(const WeightSu
     const float* partial = keys ? S.partial[1] : S.partial[0];
     const int rows = keys ? S.rows[1] : S.rows[0];
     void* const dw = keys ? S.dw[1] : S.dw[0];
+    sums_wait();
     if (dw == nullptr) return;
     const int col = threadIdx.x % kSumCols, row = threadIdx.x / kSumCols, j = blockIdx.x * kSumCols + col;
     float v = 0.f;
-    if (j < S.dim)
+    if (j < S.dim) {
+#pragma unroll 8
         for (int r = row; r < rows; r += kRows) v += partial[(size_t)r * S.dim + j];
+    }
     part[row][col] = v;
     __syncthreads();
     if (threadIdx.x < kSumCols && j < S.dim) {

@@ -84,30 +84,31 @@ bool fits(const pcr_turn_args& a, bool back, int v) {
     return true;
 }
 
-// How a call is cut: vectors of `v` pairs (0: value by value), `k` chunks of two vectors to a lane, `per` heads of a token to a thread, the grid, and how many
-// rows of partial sums each operand's weights get.
-struct Cut { int v, k, lanes, per, slots[2], rows[2]; unsigned x, y; };
+// How a call is cut: vectors of `v` pairs (0: value by value), lanes of a row, `per` heads of a token to a thread, the grid,
+// and how many rows of partial sums each operand's weights get.
+struct Cut { int v, lanes, per, slots[2], rows[2]; unsigned x, y; };
 
 Cut cut_of(const pcr_turn_args& a, bool back) {
     Cut c = {};
     for (int v : {8, 4, 2})
         if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
-    // lanes have up to 24 elements of a row: what a row costs whatever its size is then shared by fewer lanes
-    const int chunks = c.v ? a.head_dim / (2 * c.v) : 32;
-    c.k = c.v == 8 || c.v == 0 ? 1 : chunks % 3 == 0 && chunks % 2 != 0 && c.v * size_of(a.dtype) * 3 <= 32 ? 3 : chunks % 2 == 0 ? 2 : 1;
-    c.lanes = chunks / c.k;
+    c.lanes = c.v ? a.head_dim / (2 * c.v) : 32;
     constexpr int kWarps = kHeadThreads / 32;
     const int64_t n = a.batch * a.tokens, heads = a.q.heads + a.k.heads, sms = sm_count();
     const int rows = 32 / c.lanes;       // tokens of a warp
     const int64_t warps = (n + rows - 1) / rows, groups = (warps + kWarps - 1) / kWarps;
-    // heads are shared out while that gives the SMs warps that they lack
-    const int64_t shares = std::min<int64_t>((sms * 32 + warps - 1) / warps, heads);
+    // heads are shared out while that gives the SMs warps that they lack, as many to a share as are turned at a time
+    const int64_t want = sms * (back ? 4 : 32), shares = std::min<int64_t>((want + warps - 1) / warps, heads);
     c.per = (int)((heads + shares - 1) / shares);
+    if (!back && c.v && c.per > kRowsAhead) c.per = (c.per + kRowsAhead - 1) / kRowsAhead * kRowsAhead;
     if (back && c.v) {
         // CTAs by the operands' heads: those of both end at about the same time
-        const int64_t all = std::min<int64_t>(sms * 4, groups * ((a.q.heads > 0) + (a.k.heads > 0)));
-        c.slots[0] = a.q.heads == 0 ? 0 : (int)std::min(groups, std::max<int64_t>(1, (all * a.q.heads + heads / 2) / heads));
-        c.slots[1] = a.k.heads == 0 ? 0 : (int)std::min(groups, std::max<int64_t>(1, all - c.slots[0]));
+        const int ctas = kBackCtas(c.v * (int)size_of(a.dtype));
+        const int64_t of[2] = {a.q.heads, a.k.heads};
+        for (int i = 0; i < 2; ++i) {
+            const int64_t cuts = (of[i] + c.per - 1) / c.per;           // shares of this operand; whole rounds of them
+            c.slots[i] = cuts == 0 ? 0 : (int)(cuts * std::min(groups, std::max<int64_t>(1, (sms * ctas * of[i] + heads * cuts / 2) / (heads * cuts))));
+        }
         c.x = c.slots[0] + c.slots[1]; c.y = 1;
         c.rows[0] = c.slots[0]; c.rows[1] = c.slots[1];
     } else {
@@ -136,25 +137,18 @@ void fill(HeadArgs& A, const pcr_turn_args& a, const Cut& c) {
     A.eps = a.eps; A.inv_dim = 1.f / (float)a.head_dim;
 }
 
-template <typename T, int V, int K, int kMode, bool kNext>
-void launch_vectors(const HeadArgs& A, dim3 grid, cudaStream_t st) {
-    if constexpr (kMode == kNormTurnBack) heads_back_kernel<T, V, K, kNext><<<grid, kHeadThreads, 0, st>>>(A);
-    else heads_kernel<T, V, K, kMode == kNormTurn, kNext><<<grid, kHeadThreads, 0, st>>>(A);
-}
-
 template <typename T, int V, int kMode, bool kNext>
-void launch_chunks(const HeadArgs& A, int k, dim3 grid, cudaStream_t st) {
-    if (k == 3) launch_vectors<T, V, V * sizeof(T) * 3 <= 32 ? 3 : 1, kMode, kNext>(A, grid, st);
-    else if (k == 2) launch_vectors<T, V, 2, kMode, kNext>(A, grid, st);
-    else launch_vectors<T, V, 1, kMode, kNext>(A, grid, st);
+void launch_vectors(const HeadArgs& A, dim3 grid, cudaStream_t st) {
+    if constexpr (kMode == kNormTurnBack) heads_back_kernel<T, V, kNext><<<grid, kHeadThreads, 0, st>>>(A);
+    else heads_kernel<T, V, kMode == kNormTurn, kNext><<<grid, kHeadThreads, 0, st>>>(A);
 }
 
 template <typename T, int kMode, bool kNext>
 void launch(const HeadArgs& A, const Cut& c, cudaStream_t st) {
     const dim3 grid(c.x, c.y);
-    if (sizeof(T) == 2 && c.v == 8) launch_vectors<T, sizeof(T) == 2 ? 8 : 4, 1, kMode, kNext>(A, grid, st);
-    else if (c.v == 4) launch_chunks<T, 4, kMode, kNext>(A, c.k, grid, st);
-    else if (c.v == 2) launch_chunks<T, 2, kMode, kNext>(A, c.k, grid, st);
+    if (sizeof(T) == 2 && c.v == 8) launch_vectors<T, sizeof(T) == 2 ? 8 : 4, kMode, kNext>(A, grid, st);
+    else if (c.v == 4) launch_vectors<T, 4, kMode, kNext>(A, grid, st);
+    else if (c.v == 2) launch_vectors<T, 2, kMode, kNext>(A, grid, st);
     else heads_any_kernel<T, kMode, kNext><<<grid, kHeadThreads, 0, st>>>(A);
     ++g_launches;
 }
@@ -227,9 +221,15 @@ int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* str
     }
     if (sums) {
         const dim3 grid((unsigned)((args->head_dim + kSumCols - 1) / kSumCols), 2);
-        if (args->dtype == PCR_F16) weight_sums_kernel<__half><<<grid, kSumThreads, 0, st>>>(S);
-        else if (args->dtype == PCR_BF16) weight_sums_kernel<__nv_bfloat16><<<grid, kSumThreads, 0, st>>>(S);
-        else weight_sums_kernel<float><<<grid, kSumThreads, 0, st>>>(S);
+        cudaLaunchConfig_t config = {};
+        config.gridDim = grid; config.blockDim = dim3(kSumThreads); config.stream = st;
+        cudaLaunchAttribute early;
+        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        early.val.programmaticStreamSerializationAllowed = 1;
+        config.attrs = &early; config.numAttrs = nothing(*args) ? 0 : 1;
+        if (args->dtype == PCR_F16) cudaLaunchKernelEx(&config, weight_sums_kernel<__half>, S);
+        else if (args->dtype == PCR_BF16) cudaLaunchKernelEx(&config, weight_sums_kernel<__nv_bfloat16>, S);
+        else cudaLaunchKernelEx(&config, weight_sums_kernel<float>, S);
         ++g_launches;
     }
     return finish();
