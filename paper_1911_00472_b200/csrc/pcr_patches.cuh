@@ -306,6 +306,11 @@ struct PositionArgs {
 __device__ __forceinline__ void segment_sizes(const PositionArgs& A, const int4& s, int64_t& count, int64_t& extent) {
     const int32_t t = max(s.x, 0);
     if (s.y <= 0 || s.z <= 0) { count = extent = t; return; }
+    if ((t | s.y | s.z | A.time_step) < 1 << 10) {          // as a rule: in 32 bits
+        count = t * s.y * s.z;
+        extent = t == 0 ? 0 : max((t - 1) * A.time_step, max(s.y, s.z) - 1) + 1;
+        return;
+    }
     const uint64_t plane = (uint64_t)(uint32_t)s.y * (uint32_t)s.z, most = (uint64_t)1 << 32;
     count = t == 0 ? 0 : (int64_t)min(min(plane, most) * (uint32_t)t, most);       // (more than any output holds)
     extent = t == 0 ? 0 : max((int64_t)(t - 1) * A.time_step, (int64_t)max(s.y, s.z) - 1) + 1;
@@ -316,14 +321,15 @@ __device__ __forceinline__ void position_in(const PositionArgs& A, const int4& s
     if (s.y <= 0 || s.z <= 0) { pt = ph = pw = base + (int32_t)l; return; }
     const uint64_t plane = (uint64_t)(uint32_t)s.y * (uint32_t)s.z;
     uint32_t f = 0, rest = l, row, col;
-    if ((plane >> 32) == 0) { f = l / (uint32_t)plane; rest = l - f * (uint32_t)plane; }
+    if (s.x > 1 && (plane >> 32) == 0) { f = quotient(l, (uint32_t)plane); rest = l - f * (uint32_t)plane; }
     const uint32_t m = (uint32_t)A.merge;
     if (m > 1 && s.y % A.merge == 0 && s.z % A.merge == 0) {
         const uint64_t band = (uint64_t)m * (uint32_t)s.z;
-        const uint32_t block = band >> 32 ? 0 : rest / (uint32_t)band, in = rest - block * (uint32_t)band, q = in % (m * m);
-        row = block * m + q / m; col = in / (m * m) * m + q % m;
+        const uint32_t block = band >> 32 ? 0 : quotient(rest, (uint32_t)band), in = rest - block * (uint32_t)band, side = quotient(in, m * m), q = in - side * (m * m);
+        const uint32_t down = quotient(q, m);
+        row = block * m + down; col = side * m + q - down * m;
     } else {
-        row = rest / (uint32_t)s.z; col = rest - row * (uint32_t)s.z;
+        row = quotient(rest, (uint32_t)s.z); col = rest - row * (uint32_t)s.z;
     }
     pt = base + (int32_t)f * A.time_step; ph = base + (int32_t)row; pw = base + (int32_t)col;
 }
@@ -395,25 +401,76 @@ __device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool end
 }
 
 // Up to kFewSegments segments: every CTA works out where all of them begin, keeps that in shared memory and writes its own
-// run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out of L2.
+// run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out
+// of L2.  A thread finds its first token's segment by bisection and goes on from there.
 constexpr int kFewSegments = 16384, kRunTokens = 1024;
 __global__ void __launch_bounds__(kScanThreads) positions_kernel(const __grid_constant__ PositionArgs A) {
     extern __shared__ uint2 s_begin[];                                    // (first token, first position)
-    const int64_t total = walk_segments(A, blockIdx.x == 0, [&](int i, int64_t token, int32_t position) {
-        s_begin[i] = make_uint2((uint32_t)min(token, (int64_t)0xffffffff), (uint32_t)position);
-    });
+    const int n = A.n_segments, tid = threadIdx.x;
+    const bool ends = blockIdx.x + 1 == gridDim.x;                        // (the last CTA, behind all runs, writes the sequences' ends)
+    if (ends)
+        for (int i = tid; i < A.n_sequences; i += kScanThreads) A.next[i] = 0;
+#pragma unroll 4
+    for (int i = tid; i < n; i += kScanThreads) {                         // first: (tokens, and a mark where a sequence begins; positions)
+        const int4 s = A.segments[i];
+        int64_t c, e;
+        segment_sizes(A, s, c, e);
+        const bool first = A.restart || i == 0 || A.segments[i - 1].w != s.w;
+        s_begin[i] = make_uint2((uint32_t)min(c, (int64_t)0x7fffffff) | (first ? 0x80000000u : 0u), (uint32_t)e);      // (no output has more tokens)
+    }
     __syncthreads();
-    const uint32_t t0 = (uint32_t)min((uint64_t)blockIdx.x * A.run, (uint64_t)A.n_tokens), t1 = (uint32_t)min((uint64_t)t0 + A.run, (uint64_t)A.n_tokens);
-    for (uint64_t tok = (uint64_t)t0 + threadIdx.x; tok < t1; tok += kScanThreads) {
+    const int each = (n + kScanThreads - 1) / kScanThreads, a = min(tid * each, n), b = min(a + each, n);
+    int64_t tokens = 0, extent = 0, total;
+    bool first = false;
+    for (int i = a; i < b; ++i) {
+        const uint2 s = s_begin[i];
+        if (s.x >> 31) { first = true; extent = 0; }
+        tokens += s.x & 0x7fffffffu; extent += s.y;
+    }
+    sums_before(tokens, extent, first, total);
+    for (int i = a; i < b; ++i) {
+        const uint2 s = s_begin[i];
+        if (s.x >> 31) extent = 0;
+        s_begin[i] = make_uint2((uint32_t)min(tokens, (int64_t)0xffffffff), (uint32_t)extent);
+        tokens += s.x & 0x7fffffffu; extent += s.y;
+    }
+    __syncthreads();
+    if (ends) {
+#pragma unroll 4
+        for (int i = tid; i < n; i += kScanThreads) {
+            const int4 s = A.segments[i];
+            const int32_t after = i + 1 < n ? A.segments[i + 1].w : ~s.w;
+            int64_t c, e;
+            segment_sizes(A, s, c, e);
+            if (after != s.w && s.w >= 0 && s.w < A.n_sequences) A.next[s.w] = (int32_t)(s_begin[i].y + (uint32_t)e);
+        }
+    }
+    // a warp a stretch of the run: its tokens are in one segment after the other
+    const uint64_t stretch = A.run / (kScanThreads / 32), t0 = (uint64_t)blockIdx.x * A.run + (tid >> 5) * stretch, t1 = min(t0 + stretch, (uint64_t)A.n_tokens);
+    int at = 0;                                                           // the segment at hand
+    int4 s = make_int4(0, 0, 0, 0);
+    uint2 from = make_uint2(0, 0);
+    uint32_t behind = 0;                                                  // the first token behind it
+    bool any = false;
+    for (uint64_t tok = t0 + (tid & 31); tok < t1; tok += 32) {
         const uint32_t token = (uint32_t)tok;
         int32_t pt = 0, ph = 0, pw = 0;
         if ((int64_t)token < total) {
-            int lo = 0, hi = A.n_segments;                                // the last segment that begins at or before the token
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_begin[mid].x <= token) lo = mid; else hi = mid;
+            if (!any || token >= behind) {
+                int lo = at, hi = n;                                      // the last segment that begins at or before the token
+                for (int near = 0; any && near < 4 && lo + 1 < hi; ++near) {
+                    if (s_begin[lo + 1].x > token) { hi = lo + 1; break; }
+                    ++lo;
+                }
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (s_begin[mid].x <= token) lo = mid; else hi = mid;
+                }
+                at = lo; any = true;
+                s = A.segments[at]; from = s_begin[at];
+                behind = at + 1 < n ? s_begin[at + 1].x : 0xffffffffu;
             }
-            position_in(A, A.segments[lo], (int32_t)s_begin[lo].y, token - s_begin[lo].x, pt, ph, pw);
+            position_in(A, s, (int32_t)from.y, token - from.x, pt, ph, pw);
         } else if (!A.zero_tail) {
             break;
         }

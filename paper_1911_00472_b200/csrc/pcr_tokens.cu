@@ -287,14 +287,14 @@ int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_token
     A.restart = (flags & PCR_POSITIONS_RESTART) != 0; A.zero_tail = (flags & PCR_POSITIONS_ZERO_TAIL) != 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (n_segments <= kFewSegments) {
-        const int64_t runs = std::min<int64_t>(std::max<int64_t>((n_tokens + kRunTokens - 1) / kRunTokens, 1), sm_count());
-        A.run = (uint32_t)(((n_tokens + runs - 1) / runs + 31) / 32 * 32);
         const size_t shared = (size_t)n_segments * sizeof(uint2);
+        const int64_t runs = std::min<int64_t>(std::max<int64_t>((n_tokens + kRunTokens - 1) / kRunTokens, 1), sm_count() * (shared > 100 * 1024 ? 1 : 2) - 1);
+        A.run = (uint32_t)(((n_tokens + runs - 1) / runs + kScanThreads - 1) / kScanThreads * kScanThreads);      // whole rounds of every warp
         if (shared > 40 * 1024 && cudaFuncSetAttribute(positions_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) {
             cudaGetLastError();
             return PCR_E_CUDA;
         }
-        positions_kernel<<<(unsigned)runs, kScanThreads, shared, st>>>(A);
+        positions_kernel<<<(unsigned)runs + 1, kScanThreads, shared, st>>>(A);
         ++g_launches;
         return finish();
     }
