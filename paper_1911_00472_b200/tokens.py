@@ -59,11 +59,6 @@ def _same_device(device, *tensors):
 # ---- queries and keys ---------------------------------------------------------------------------------------------------
 
 
-def _rows(t):
-    """The tensor itself, or a copy where the elements of a head do not stand side by side."""
-    return t if t is None or t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
-
-
 def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
     """What the calls ask of their operands; returns (batch, tokens, size, type of the weights).  One look at each property:
     small calls take as long as the host does."""
@@ -114,9 +109,14 @@ def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
     return batch, tokens, size, weight
 
 
+def _like(t):
+    """An output of the operand's strides where its heads' elements stand side by side, a contiguous one otherwise."""
+    return torch.empty_like(t) if t.stride(-1) == 1 else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _outputs(q, k, out):
     if out is None:
-        return torch.empty_like(q), None if k is None else torch.empty_like(k)
+        return _like(q), None if k is None else _like(k)
     for o, x in zip(out, (q, k), strict=True):
         if (o is None) != (x is None):
             raise ValueError("out must have an output for each operand")
@@ -129,23 +129,54 @@ def _outputs(q, k, out):
     return out
 
 
-def _heads(x, y, dy, weight, dweight):
-    """A pcr_heads: addresses, then strides of batch, token and head (the elements' own, the last, are 1)."""
-    if x is None:
-        return _NO_HEADS
-    xs, ys, gs = x.stride(), y.stride(), _NO_STRIDES if dy is None else dy.stride()
-    if len(xs) == 3:
-        xs, ys, gs = (0, *xs), (0, *ys), (0, *gs) if dy is not None else gs
-    return (x.data_ptr(), y.data_ptr(), 0 if dy is None else dy.data_ptr(), 0 if weight is None else weight.data_ptr(),
-            0 if dweight is None else dweight.data_ptr(), *xs[:3], *ys[:3], *gs[:3], x.shape[-2], 0)
-
-
-def _pack(heads_q, heads_k, positions, inv_freq, axes, q, dims, interleaved, inverse, eps):
-    batch, tokens, size, weight = dims
+def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, interleaved, inverse, eps, out, stream):
+    """Checks, allocates, packs a pcr_turn_args and makes the call `name`; returns its outputs (and the weights' gradients)."""
+    batch, tokens, size, weight = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads)
+    device = q.get_device()
+    if device < 0:
+        raise ValueError("operands have to be on a CUDA device")
+    if stream is not None or torch.cuda.current_device() != device:
+        with _on(q.device, stream):
+            return _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, interleaved, inverse, eps, out, None)
+    y, z = _outputs(q, k, out)
+    dwq = dwk = None
+    if grads and q_weight is not None:
+        dwq = torch.empty_like(q_weight)
+    if grads and k_weight is not None:
+        dwk = torch.empty_like(k_weight)
+    parts, copies = [], []                               # (copies live until the call is made: others must not get their memory before)
+    for x, o, g, w, dw in ((q, y, grads[0] if grads else None, q_weight, dwq), (k, z, grads[1] if grads else None, k_weight, dwk)):
+        if x is None:
+            parts += _NO_HEADS
+            continue
+        xs = x.stride()
+        if xs[-1] != 1 and size > 1:                     # the elements of a head do not stand side by side
+            x = x.contiguous()
+            xs = x.stride()
+            copies.append(x)
+        gs, g_at = _NO_STRIDES, 0
+        if g is not None:
+            gs = g.stride()
+            if gs[-1] != 1 and size > 1:
+                g = g.contiguous()
+                gs = g.stride()
+                copies.append(g)
+            g_at = g.data_ptr()
+        ys = o.stride()
+        if len(xs) == 3:
+            xs, ys, gs = (0, *xs), (0, *ys), (0, *gs)
+        parts += (x.data_ptr(), o.data_ptr(), g_at, 0 if w is None else w.data_ptr(), 0 if dw is None else dw.data_ptr(), *xs[:3], *ys[:3], *gs[:3], x.shape[-2], 0)
     ps = positions.stride()
-    return _TURN_ARGS.pack(*heads_q, *heads_k, positions.data_ptr(), *(ps if len(ps) == 3 else (ps[0], 0, ps[1])), inv_freq.data_ptr(),
-                           axes.data_ptr(), batch, tokens, positions.shape[0], size, 2 * inv_freq.shape[0], bool(interleaved), bool(inverse),
-                           _CODES[q.dtype], _FREQ_CODES[inv_freq.dtype], _CODES[weight], eps, 0)
+    args = _TURN_ARGS.pack(*parts, positions.data_ptr(), *(ps if len(ps) == 3 else (ps[0], 0, ps[1])), inv_freq.data_ptr(), axes.data_ptr(), batch, tokens,
+                           positions.shape[0], size, 2 * inv_freq.shape[0], bool(interleaved), bool(inverse), _CODES[q.dtype], _FREQ_CODES[inv_freq.dtype],
+                           _CODES[weight], eps, 0)
+    L = B.lib()
+    if grads:
+        scratch = inv_freq.new_empty(-(-L.pcr_norm_rotate_scratch_bytes(args) // inv_freq.element_size()))
+        B._chk(L.pcr_norm_rotate_backward(args, scratch.data_ptr(), _raw_stream(device)), name)
+        return y, z, dwq, dwk
+    B._chk(getattr(L, name)(args, _raw_stream(device)), name)
+    return y, z
 
 
 def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False, out=None, stream=None):
@@ -161,13 +192,7 @@ def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False,
     inverse   by the negative angle: the gradient of the forward call
     out       (q, k) to write to, the operands themselves allowed
     """
-    dims = _check(q, k, positions, inv_freq, axes, None, None, ())
-    with _on(q.device, stream):
-        q, k = _rows(q), _rows(k)
-        y, z = _outputs(q, k, out)
-        args = _pack(_heads(q, y, None, None, None), _heads(k, z, None, None, None), positions, inv_freq, axes, q, dims, interleaved, inverse, 0.0)
-        B._chk(B.lib().pcr_rotate(args, _raw_stream(q.device.index)), "pcr_rotate")
-    return y, z
+    return _call("pcr_rotate", q, k, (), None, None, positions, inv_freq, axes, interleaved, inverse, 0.0, out, stream)
 
 
 def norm_rotate(q, k, q_weight, k_weight, positions, inv_freq, axes, *, eps=1e-6, interleaved=False, out=None, stream=None):
@@ -175,13 +200,7 @@ def norm_rotate(q, k, q_weight, k_weight, positions, inv_freq, axes, *, eps=1e-6
 
     q_weight, k_weight   (size,) of the operands' type or float32; None: ones
     """
-    dims = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, ())
-    with _on(q.device, stream):
-        q, k = _rows(q), _rows(k)
-        y, z = _outputs(q, k, out)
-        args = _pack(_heads(q, y, None, q_weight, None), _heads(k, z, None, k_weight, None), positions, inv_freq, axes, q, dims, interleaved, False, eps)
-        B._chk(B.lib().pcr_norm_rotate(args, _raw_stream(q.device.index)), "pcr_norm_rotate")
-    return y, z
+    return _call("pcr_norm_rotate", q, k, (), q_weight, k_weight, positions, inv_freq, axes, interleaved, False, eps, out, stream)
 
 
 def norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, inv_freq, axes, *, eps=1e-6, interleaved=False,
@@ -190,16 +209,7 @@ def norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, in
 
     out   where the gradients of q and k go; (grad_q, grad_k) or (q, k) themselves allowed
     """
-    dims = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, (grad_q, grad_k))
-    with _on(q.device, stream):
-        q, k, grad_q, grad_k = _rows(q), _rows(k), _rows(grad_q), _rows(grad_k)
-        y, z = _outputs(q, k, out)
-        dwq, dwk = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
-        args = _pack(_heads(q, y, grad_q, q_weight, dwq), _heads(k, z, grad_k, k_weight, dwk), positions, inv_freq, axes, q, dims, interleaved, False, eps)
-        L = B.lib()
-        scratch = inv_freq.new_empty(-(-L.pcr_norm_rotate_scratch_bytes(args) // inv_freq.element_size()))
-        B._chk(L.pcr_norm_rotate_backward(args, scratch.data_ptr(), _raw_stream(q.device.index)), "pcr_norm_rotate_backward")
-    return y, z, dwq, dwk
+    return _call("pcr_norm_rotate_backward", q, k, (grad_q, grad_k), q_weight, k_weight, positions, inv_freq, axes, interleaved, False, eps, out, stream)
 
 
 def rotary_axes(rot, base=10000.0, sections=None, *, interleaved_axes=False, per_axis=False, device="cuda:0"):
