@@ -205,19 +205,23 @@ def test_in_place_and_outputs_of_other_strides(interleaved):
         check_forward(before, q, angle, interleaved)
 
 
-def test_values_that_are_not_numbers_stay_in_their_rows():
-    q, k, positions, inv_freq, axes, wq, wk = make((1, 20, 4, 2, 128, 128), torch.bfloat16)
+@pytest.mark.parametrize("size", [128, 72, 80, 50])
+def test_values_that_are_not_numbers_stay_in_their_rows(size):
+    q, k, positions, inv_freq, axes, wq, wk = make((1, 20, 4, 2, size, size), torch.bfloat16)
     bad = q.clone()
     bad[0, 3, 1, 5] = math.nan
-    bad[0, 4, 2, 127] = math.inf
-    bad[0, 5, 3, 64] = torch.finfo(torch.bfloat16).min
+    bad[0, 4, 2, size - 1] = math.inf
+    bad[0, 5, 3, size // 2] = torch.finfo(torch.bfloat16).min
     plain, norm = P.rotate(q, k, positions, inv_freq, axes)[0], P.norm_rotate(q, k, wq, wk, positions, inv_freq, axes)[0]
     got, got_norm = P.rotate(bad, k, positions, inv_freq, axes)[0], P.norm_rotate(bad, k, wq, wk, positions, inv_freq, axes)[0]
     hit = torch.zeros(20, 4, dtype=torch.bool, device="cuda")
     hit[3, 1] = hit[4, 2] = hit[5, 3] = True
     assert torch.equal(got[0][~hit], plain[0][~hit]) and torch.equal(got_norm[0][~hit], norm[0][~hit])
-    assert bool(got[0, 3, 1, [5, 69]].isnan().all()) and int(got[0, 3, 1].isnan().sum()) == 2
+    assert bool(got[0, 3, 1, [5, 5 + size // 2]].isnan().all()) and int(got[0, 3, 1].isnan().sum()) == 2
     assert bool(got_norm[0, 3, 1].isnan().all())
+    g = torch.randn_like(q)
+    dx, dx_bad = (P.norm_rotate_backward(g, None, x, None, wq, None, positions, inv_freq, axes)[0] for x in (q, bad))
+    assert torch.equal(dx[0][~hit], dx_bad[0][~hit]) and bool(dx_bad[0, 3, 1].isnan().all())
     # a row of zeros: 1 / sqrt(eps) times nothing
     zero = P.norm_rotate(torch.zeros_like(q), k, wq, wk, positions, inv_freq, axes)[0]
     assert bool((zero == 0).all())
@@ -243,6 +247,36 @@ def test_offsets_past_32_bits():
     heads = torch.as_strided(buf, (1, 2, 2, 128), (0, 128, far, 1))
     check_forward(heads, P.rotate(heads, None, positions, inv_freq, axes)[0], angle, False)
     del buf
+
+
+def test_shared_heads_and_slices_of_one_buffer():
+    """Keys broadcast over heads, and queries and keys turned in place inside one projection's output."""
+    q, k, positions, inv_freq, axes, wq, wk = make((2, 19, 8, 1, 64, 64), torch.bfloat16)
+    shared = k.expand(-1, -1, 4, -1)
+    y = P.norm_rotate(q, shared, wq, wk, positions, inv_freq, axes)
+    one = P.norm_rotate(q, k, wq, wk, positions, inv_freq, axes)
+    assert y[1].shape == shared.shape and torch.equal(y[1], one[1].expand(-1, -1, 4, -1))
+    g = torch.randn_like(y[1])
+    dk = P.norm_rotate_backward(torch.randn_like(q), g, q, shared, wq, wk, positions, inv_freq, axes)
+    check_backward(shared, g, dk[1], dk[3], angle_of(positions, inv_freq, axes), False, wk, 1e-6)
+    qkv = torch.cat([q, k, torch.randn_like(k)], 2)
+    value = qkv[:, :, 9:].clone()
+    P.norm_rotate(qkv[:, :, :8], qkv[:, :, 8:9], wq, wk, positions, inv_freq, axes, out=(qkv[:, :, :8], qkv[:, :, 8:9]))
+    assert torch.equal(qkv[:, :, :8], one[0]) and torch.equal(qkv[:, :, 8:9], one[1]) and torch.equal(qkv[:, :, 9:], value)
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (300, 0), (129, 3)])
+def test_many_and_few_heads(heads):
+    q, k, positions, inv_freq, axes, wq, wk = make((1, 37, *heads, 64, 64), torch.float16, "packed")
+    angle = angle_of(positions, inv_freq, axes)
+    wk = wk if heads[1] else None
+    y = P.norm_rotate(q, k, wq, wk, positions, inv_freq, axes)
+    gq, gk = torch.randn_like(q), None if k is None else torch.randn_like(k)
+    b = P.norm_rotate_backward(gq, gk, q, k, wq, wk, positions, inv_freq, axes)
+    for i, (x, g, w) in enumerate([(q, gq, wq), (k, gk, wk)]):
+        if x is not None:
+            check_forward(x, y[i], angle, False, w, 1e-6)
+            check_backward(x, g, b[i], b[2 + i], angle, False, w, 1e-6)
 
 
 def test_nothing_to_do():

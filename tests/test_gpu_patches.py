@@ -113,6 +113,43 @@ def test_large_resampling_ratios():
     check(P.patch_tokens(rgb, plan.images, plan.index, 32, MEAN, STD, dtype=torch.float32), want)
 
 
+@pytest.mark.parametrize("patch", [14, 16, 9])
+@pytest.mark.parametrize("scale", [0.4, 0.99, 1.01, 1.7, 2.3, 5.0])
+def test_resampling_by_any_factor(patch, scale):
+    # neighbouring columns one source pixel apart, two or none, or further; source rows that repeat or are left out
+    pics, info, rgb = images([(211, 173), (96, 64)], 4)
+    crops = np.array([(3, 5, 200, 160, 0), (0, 0, 95, 63, 1)])
+    grids = np.maximum(1, np.round(crops[:, [3, 2]] / (patch * scale)).astype(int))
+    plan = P.patch_plan(info, patch, crops=crops, grids=grids)
+    want = np.concatenate([tokens_of(p, c, g, patch, 1) for p, c, g in zip(pics, crops, grids)])
+    for dtype in DTYPES:
+        check(P.patch_tokens(rgb, plan.images, plan.index, patch, MEAN, STD, dtype=dtype), want)
+
+
+def test_graphs_and_streams():
+    """Captured and replayed on other pixels, and on a stream of its own."""
+    pics, info, rgb = images(SIZES)
+    plan = P.patch_plan(info, 14, merge=2)
+    segments = plan.segments(merged=True)
+    T = len(plan.index) // 4
+    want = P.patch_tokens(rgb, plan.images, plan.index, 14, MEAN, STD, merge=2)
+    at, after = P.token_positions(segments, T, len(info))
+    work = torch.zeros_like(rgb)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = P.patch_tokens(work, plan.images, plan.index, 14, MEAN, STD, merge=2)
+        got_at, got_after = P.token_positions(segments, T, len(info))
+    work.copy_(rgb)
+    graph.replay()
+    assert torch.equal(got, want) and torch.equal(got_at, at) and torch.equal(got_after, after)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = P.patch_tokens(rgb, plan.images, plan.index, 14, MEAN, STD, merge=2, stream=side)
+    got_at, got_after = P.token_positions(segments, T, len(info), stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want) and torch.equal(got_at, at) and torch.equal(got_after, after)
+
+
 def test_entries_that_do_not_fit_give_zeros():
     pics, info, rgb = images(SIZES[:3])
     plan = P.patch_plan(info, 14, merge=2)
