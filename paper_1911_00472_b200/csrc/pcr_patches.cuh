@@ -404,22 +404,32 @@ __device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool end
 // run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out
 // of L2.  A thread finds its first token's segment by bisection and goes on from there.
 constexpr int kFewSegments = 16384, kRunTokens = 1024;
-__global__ void __launch_bounds__(kScanThreads) positions_kernel(const __grid_constant__ PositionArgs A) {
+__global__ void __launch_bounds__(kScanThreads, 2) positions_kernel(const __grid_constant__ PositionArgs A) {
     extern __shared__ uint2 s_begin[];                                    // (first token, first position)
     const int n = A.n_segments, tid = threadIdx.x;
     const bool ends = blockIdx.x + 1 == gridDim.x;                        // (the last CTA, behind all runs, writes the sequences' ends)
     if (ends)
         for (int i = tid; i < A.n_sequences; i += kScanThreads) A.next[i] = 0;
-#pragma unroll 4
-    for (int i = tid; i < n; i += kScanThreads) {                         // first: (tokens, and a mark where a sequence begins; positions)
-        const int4 s = A.segments[i];
-        int64_t c, e;
-        segment_sizes(A, s, c, e);
-        const bool first = A.restart || i == 0 || A.segments[i - 1].w != s.w;
-        s_begin[i] = make_uint2((uint32_t)min(c, (int64_t)0x7fffffff) | (first ? 0x80000000u : 0u), (uint32_t)e);      // (no output has more tokens)
+    for (int i0 = tid; i0 < n; i0 += 4 * kScanThreads) {                  // first: (tokens, and a mark where a sequence begins; positions)
+        int4 s[4];
+        int32_t before[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                                     // (four on their way at a time)
+            const int i = i0 + k * kScanThreads;
+            if (i < n) { s[k] = A.segments[i]; before[k] = i > 0 ? A.segments[i - 1].w : ~s[k].w; }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * kScanThreads;
+            if (i >= n) break;
+            int64_t c, e;
+            segment_sizes(A, s[k], c, e);
+            const bool first = A.restart || before[k] != s[k].w;
+            s_begin[i] = make_uint2((uint32_t)min(c, (int64_t)0x7fffffff) | (first ? 0x80000000u : 0u), (uint32_t)e);      // (no output has more tokens)
+        }
     }
     __syncthreads();
-    const int each = (n + kScanThreads - 1) / kScanThreads, a = min(tid * each, n), b = min(a + each, n);
+    const int each = (n + kScanThreads - 1) / kScanThreads | 1, a = min(tid * each, n), b = min(a + each, n);       // (odd: no two lanes in one bank)
     int64_t tokens = 0, extent = 0, total;
     bool first = false;
     for (int i = a; i < b; ++i) {
