@@ -124,6 +124,9 @@ __device__ __forceinline__ Rgb mix_single(const uint8_t* at, float f) {
     return mix_bytes(lo, hi, f);
 }
 
+struct True { static constexpr bool value = true; };
+struct False { static constexpr bool value = false; };
+
 // One or two columns of a source row, mixed; two at a time in every instruction.
 template <int kCols> struct Mixed { F2 c[3]; };
 template <> struct Mixed<1> { float c[3]; };
@@ -131,15 +134,18 @@ template <> struct Mixed<1> { float c[3]; };
 // The words that two neighbouring columns lie in: the left one's six bytes begin at `sh` bits into the first, the right
 // one's 0, 3 or 6 bytes further on.
 struct Words { uint32_t w0, w1, w2, w3, sh; };
+template <bool kPlain>                     // plain: `at` is a word already (its shift is the lane's own), and no column two pixels on
 __device__ __forceinline__ Words words_at(const uint8_t* at, bool wide) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(kPlain ? reinterpret_cast<uintptr_t>(at) : reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
     Words r = {__ldg(p), __ldg(p + 1), __ldg(p + 2), 0, (uint32_t)reinterpret_cast<uintptr_t>(at) << 3};
-    if (wide) r.w3 = __ldg(p + 3);
+    if (!kPlain && wide) r.w3 = __ldg(p + 3);
     return r;
 }
-__device__ __forceinline__ Mixed<2> mix_words(const Words& w, bool wide, uint32_t shift, F2 f) {
-    const uint32_t x0 = __funnelshift_r(w.w0, w.w1, w.sh), x1 = __funnelshift_r(w.w1, w.w2, w.sh), x2 = __funnelshift_r(w.w2, w.w3, w.sh);
-    const uint32_t a = wide ? x1 : x0, b = wide ? x2 : x1, y0 = __funnelshift_r(a, b, shift), y1 = __funnelshift_r(b, x2, shift);
+template <bool kPlain>
+__device__ __forceinline__ Mixed<2> mix_words(const Words& w, uint32_t own, bool wide, uint32_t shift, F2 f) {
+    const uint32_t sh = kPlain ? own : w.sh;
+    const uint32_t x0 = __funnelshift_r(w.w0, w.w1, sh), x1 = __funnelshift_r(w.w1, w.w2, sh), x2 = __funnelshift_r(w.w2, w.w3, sh);
+    const uint32_t a = !kPlain && wide ? x1 : x0, b = !kPlain && wide ? x2 : x1, y0 = __funnelshift_r(a, b, shift), y1 = __funnelshift_r(b, x2, shift);
     const F2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f), down = pack2(-kUp, -kUp);
     Mixed<2> r;
 #pragma unroll
@@ -204,6 +210,9 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
             }
         }
     }
+    // as a rule a warp's rows begin at whole words, are not mirrored, and its neighbouring columns at most a pixel apart:
+    // a third of the walk's shifts, selects and address arithmetic is then left out (they bound it)
+    const bool plain = kCols == 2 && __all_sync(0xffffffffu, !here || (m.words && !m.flip && (m.pitch & 3) == 0 && other - base <= 3));
     __syncwarp();
     if (here) {
         T* o = (kDirect ? static_cast<T*>(A.out) + (first + sub) * (uint64_t)values : buf + sub * values) + px;
@@ -211,35 +220,39 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
         const bool swap = m.flip && m.ok;
         auto value = [&](int c, float top, float low, float fy) { return fmaf(fmaf(fy, low - top, top), A.scale[c], A.shift[c]); };
         if (kCols == 2 && m.words && other - base <= 6) {
-            const bool wide = other - base == 6;             // the right column two pixels on
-            const uint32_t shift = wide ? 16 : other != base ? 24 : 0;
             const F2 f = pack2(fl, fr), minus = pack2(-1.f, -1.f);
-            uint32_t top_at = ~0u, low_at = ~0u;
             // On entry `top` holds the mixed row at low_at and `low` the one at top_at (the last output row's, roles swapped): as
             // a rule an output row's upper source row is the last one's lower, and one row is mixed.
-            auto step = [&](Mixed<2>& top, Mixed<2>& low, const Words& now, Words& next, T* to, const uint4& r, const uint4& after) {
-                next = words_at(base + after.y, wide);
-                if (r.x != low_at) top = r.x == top_at ? low : mix_words(words_at(base + r.x, wide), wide, shift, f);
-                low = mix_words(now, wide, shift, f);
-                top_at = r.x; low_at = r.y;
-                const float fy = __uint_as_float(r.z);
-                const F2 fy2 = pack2(fy, fy);
+            auto walk = [&](auto plain_, const uint8_t* from, uint32_t own_shift, bool wide, uint32_t shift, bool mirror) {
+                constexpr bool kPlain = decltype(plain_)::value;
+                uint32_t top_at = ~0u, low_at = ~0u;
+                auto step = [&](Mixed<2>& top, Mixed<2>& low, const Words& now, Words& next, T* to, const uint4& r, const uint4& after) {
+                    next = words_at<kPlain>(from + after.y, wide);
+                    if (r.x != low_at) top = r.x == top_at ? low : mix_words<kPlain>(words_at<kPlain>(from + r.x, wide), own_shift, wide, shift, f);
+                    low = mix_words<kPlain>(now, own_shift, wide, shift, f);
+                    top_at = r.x; low_at = r.y;
+                    const float fy = __uint_as_float(r.z);
+                    const F2 fy2 = pack2(fy, fy);
 #pragma unroll
-                for (int c = 0; c < 3; ++c) {
-                    const F2 v = fma2(fma2(fy2, fma2(top.c[c], minus, low.c[c]), top.c[c]), pack2(A.scale[c], A.scale[c]), pack2(A.shift[c], A.shift[c]));
-                    float a, b;
-                    unpack2(v, a, b);
-                    put_two(to + c * area, a, b, swap);
+                    for (int c = 0; c < 3; ++c) {
+                        const F2 v = fma2(fma2(fy2, fma2(top.c[c], minus, low.c[c]), top.c[c]), pack2(A.scale[c], A.scale[c]), pack2(A.shift[c], A.shift[c]));
+                        float a, b;
+                        unpack2(v, a, b);
+                        put_two(to + c * area, a, b, !kPlain && mirror);
+                    }
+                };
+                Mixed<2> u = {}, v = {};
+                Words even = words_at<kPlain>(from + rows[0].y, wide), odd;
+#pragma unroll 1
+                for (int dy = 0; dy < p; dy += 2, o += 2 * p, rows += 2) {
+                    const uint4 r0 = rows[0], r1 = rows[1], r2 = rows[dy + 2 < p ? 2 : 1];
+                    step(u, v, even, odd, o, r0, r1);
+                    step(v, u, odd, even, o + p, r1, r2);
                 }
             };
-            Mixed<2> u = {}, v = {};
-            Words even = words_at(base + rows[0].y, wide), odd;
-#pragma unroll 1
-            for (int dy = 0; dy < p; dy += 2, o += 2 * p, rows += 2) {
-                const uint4 r0 = rows[0], r1 = rows[1], r2 = rows[dy + 2 < p ? 2 : 1];
-                step(u, v, even, odd, o, r0, r1);
-                step(v, u, odd, even, o + p, r1, r2);
-            }
+            const uint32_t sh = (uint32_t)reinterpret_cast<uintptr_t>(base) << 3;
+            if (plain) walk(True(), base - (reinterpret_cast<uintptr_t>(base) & 3), sh, false, other != base ? 24 : 0, false);
+            else walk(False(), base, sh, other - base == 6, other - base == 6 ? 16 : other != base ? 24 : 0, swap);
         } else if (m.words) {
             Rgb top[kCols], low[kCols];
             const float f[2] = {fl, fr};

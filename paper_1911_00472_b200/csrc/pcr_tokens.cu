@@ -251,9 +251,11 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
     A.n_tokens = (uint32_t)n_tokens; A.n_images = n_images; A.patch = patch; A.merge = merge;
     for (int c = 0; c < 3; ++c) { A.scale[c] = 1.f / (255.f * std_[c]); A.shift[c] = -mean[c] / std_[c]; }
     const bool pairs = patch % 2 == 0;                         // two columns to a lane
-    // where a patch's rows are whole sectors of 32 bytes, lanes write them as they come (1024 images, patches of 16, 16 bits:
-    // 435 us in the place of 460); rows that share sectors with others go through shared memory
-    const bool direct = pairs && patch * size_of(dtype) % 32 == 0 && aligned(tokens, 32);
+    // Lanes write their values as they come, or through shared memory as whole vectors.  16 bits: as they come (1024 images,
+    // us, as they come / through shared memory: patches of 14 399 / 402, of 16 396 / 460; 300 images, of 28 104 / 130, of 8
+    // 162 / 164).  32 bits: as they come only where a patch's rows are whole sectors of 32 bytes (96 images, of 16 43 / 60;
+    // 300 images, of 14 211 / 164: the rows share sectors and the shared memory makes up for it).
+    const bool direct = pairs && (dtype == PCR_F32 ? patch % 8 == 0 && aligned(tokens, 32) : aligned(tokens, 4));
     const int lanes = pairs ? patch / 2 : patch;
     A.each = 32 / lanes; A.by_lanes = (65536u + lanes - 1) / lanes; A.by_merge = ((1u << 20) + merge - 1) / merge;
     const size_t own = ((size_t)A.each * 3 * patch * patch * size_of(dtype) + 15) / 16 * 16;
