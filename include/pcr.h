@@ -272,7 +272,7 @@ typedef struct {
     pcr_heads q, k;
     const int32_t* positions;      /* DEVICE; axis a of token (b, t) at a, b, t times these strides    */
     int64_t position_stride[3];
-    const void* inv_freq;          /* DEVICE, rot_dim / 2 frequencies, float or double (freq_dtype)    */
+    const void* inv_freq;          /* DEVICE, rot_dim / 2 finite frequencies, float or double (freq_dtype) */
     const int32_t* axes;           /* DEVICE, rot_dim / 2: the axis that turns pair i; an axis outside
                                       0 .. n_axes - 1 leaves the pair as it is                         */
     int64_t batch, tokens;         /* tokens of each sequence; batch * tokens < 2^31                   */
@@ -290,7 +290,8 @@ typedef struct {
 /* Rotation of queries and keys, one launch: pair (a, b) becomes (a cos - b sin, a sin + b cos) with the
  * angle positions[axes[i]] * inv_freq[i], whose whole turns are taken off in double precision (far
  * positions lose nothing); single precision from there, one rounding to dtype.  Any strides and
- * alignments of whole elements; in place is allowed.
+ * alignments of whole elements; in place is allowed.  Rows that stand on 16-byte boundaries in heads of
+ * a multiple of 16 (16 bits) or 8 (32 bits) elements are fastest, rows at odd elements slowest.
  * Errors: PCR_E_ARG (also for an output that overlaps itself), PCR_E_CUDA. */
 int pcr_rotate(const pcr_turn_args* args, void* stream);
 

@@ -171,9 +171,15 @@ __device__ __forceinline__ void put_two(__nv_bfloat16* to, float a, float b, boo
 
 // A lane kCols neighbouring columns of a patch, walking down its rows: a source row that serves two output rows is read and
 // mixed once, and its words are asked for one row ahead.  A warp takes 32 / lanes-of-a-patch tokens, whose values meet in
-// shared memory and leave as whole vectors, or (kDirect) are written as they come.  Instructions bound it (bytes to numbers, two mixes, a scale), not HBM: two
-// columns to a lane share the walk's addresses, words and conditions and go two to an instruction; patches of odd size go
-// one column to a lane.
+// shared memory and leave as whole vectors, or (kDirect) are written as they come.
+// What bounds it: instructions, not HBM (192 images to patches of 14, 16 bits: issued in 70 % of the cycles, four of ten
+// instructions on the integer pipe that takes bytes apart, L1 71 %, DRAM 28 %).  So two columns go to a lane (they share the walk's addresses, words
+// and conditions, and go two to an instruction: 568 -> 405 us for 1024 images; patches of odd size have one column a lane), and
+// what a token costs once (its entry, image and taps: a third of the instructions at patches of 14) is kept in 32 bits and
+// without divisions.  Looking up 32 tokens at once in shared memory (457 us) or keeping an image for several rounds of a warp
+// (560 to 620 in the place of 568) was slower: fewer warps fit.
+// Measured: 1024 images of 256 to 496 pixels a side to patches of 14, 16 bits: 405 us, 3.3 TB/s of what has to move; 96 crops of
+// images of 600 x 450 to patches of 16, 32 bits: 43 us, 4.6 TB/s; 768 patches of 4 small images: 6 us.
 template <typename T, int kCols, bool kDirect>
 __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const __grid_constant__ PatchArgs A) {
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -414,8 +420,10 @@ __device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool end
 }
 
 // Up to kFewSegments segments: every CTA works out where all of them begin, keeps that in shared memory and writes its own
-// run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out
-// of L2.  A thread finds its first token's segment by bisection and goes on from there.
+// run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out of L2.  A thread finds its first token's
+// segment by bisection and goes on from there.
+// Latency and the sums that every CTA repeats bound it: 8704 segments of 1.4 million tokens 19 us, 72 segments 6 us; 16384 segments
+// 18.5 us, one more, by the two launches below, 55.
 constexpr int kFewSegments = 16384, kRunTokens = 1024;
 __global__ void __launch_bounds__(kScanThreads, 2) positions_kernel(const __grid_constant__ PositionArgs A) {
     extern __shared__ uint2 s_begin[];                                    // (first token, first position)
@@ -501,7 +509,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) positions_kernel(const __grid
     }
 }
 
-// More segments: one CTA writes where each begins to device memory, then a thread a token looks its segment up there.
+// More segments: one CTA writes where each begins to device memory, then a thread a token looks its segment up there.  The one
+// CTA's walk over the segments bounds it (most of 55 us for 16385 segments); so many segments in one call are rare.
 __global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __grid_constant__ PositionArgs A) {
     const int64_t total = walk_segments(A, true, [&](int i, int64_t token, int32_t position) { A.starts[i] = token; A.bases[i] = position; });
     if (threadIdx.x == 0) A.starts[A.n_segments] = total;

@@ -90,6 +90,8 @@ struct Cut { int v, lanes, per, slots[2], rows[2]; unsigned x, y; };
 
 Cut cut_of(const pcr_turn_args& a, bool back) {
     Cut c = {};
+    // the longest vectors that fit: 8192 tokens, 40 heads of 128, bf16, by 16 / 8 / 4 bytes and value by value: rotation 31, 31, 34 and 103 us,
+    // norm 35, 41, 57 and 131, backward 55, 60, 89 and 397
     for (int v : {8, 4, 2})
         if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
     c.lanes = c.v ? a.head_dim / (2 * c.v) : 32;
@@ -97,7 +99,9 @@ Cut cut_of(const pcr_turn_args& a, bool back) {
     const int64_t n = a.batch * a.tokens, heads = a.q.heads + a.k.heads, sms = sm_count();
     const int rows = 32 / c.lanes;       // tokens of a warp
     const int64_t warps = (n + rows - 1) / rows, groups = (warps + kWarps - 1) / kWarps;
-    // heads are shared out while that gives the SMs warps that they lack, as many to a share as are turned at a time
+    // Heads are shared out while that gives the SMs warps that they lack (forward 32 an SM: 8191 tokens, 40 heads, rotation: 16
+    // an SM 36 us, 32 and 64 32 to 33; 16384 tokens of 5 heads, norm: 32 20.5 us, 64 22.6; backward 4: 514 tokens, 16 heads: 9.0 us,
+    // all heads in one share 12.4), forward whole batches of rows to a share (8192 tokens, 40 heads of 128, norm: 39.0 -> 35.6 us)
     const int64_t want = sms * (back ? 4 : 32), shares = std::min<int64_t>((want + warps - 1) / warps, heads);
     c.per = (int)((heads + shares - 1) / shares);
     if (!back && c.v && c.per > kRowsAhead) c.per = (c.per + kRowsAhead - 1) / kRowsAhead * kRowsAhead;
@@ -251,11 +255,12 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
     A.n_tokens = (uint32_t)n_tokens; A.n_images = n_images; A.patch = patch; A.merge = merge;
     for (int c = 0; c < 3; ++c) { A.scale[c] = 1.f / (255.f * std_[c]); A.shift[c] = -mean[c] / std_[c]; }
     const bool pairs = patch % 2 == 0;                         // two columns to a lane
-    // Lanes write their values as they come, or through shared memory as whole vectors.  16 bits: as they come (1024 images,
-    // us, as they come / through shared memory: patches of 14 399 / 402, of 16 396 / 460; 300 images, of 28 104 / 130, of 8
-    // 162 / 164).  32 bits: as they come only where a patch's rows are whole sectors of 32 bytes (96 images, of 16 43 / 60;
-    // 300 images, of 14 211 / 164: the rows share sectors and the shared memory makes up for it).
-    const bool direct = pairs && (dtype == PCR_F32 ? patch % 8 == 0 && aligned(tokens, 32) : aligned(tokens, 4));
+    // Lanes write their values as they come, or through shared memory as whole vectors.  As they come where a patch's rows are
+    // whole sectors of 32 bytes (400 images, patches of 16, 16 bits: 155 us, through shared memory 178; 96 images, of 16, 32
+    // bits: 43 and 60); 16 bits also beyond patches of 16, whose values would leave shared memory for few warps (300 images,
+    // of 28: 103 and 130).  Else rows share sectors, and shared memory makes up for it (1024 images, of 14, 16 bits: 431 and
+    // 405; 300 images, of 14, 32 bits: 211 and 164).
+    const bool direct = pairs && aligned(tokens, 32) && (patch * size_of(dtype) % 32 == 0 || (dtype != PCR_F32 && patch > 16));
     const int lanes = pairs ? patch / 2 : patch;
     A.each = 32 / lanes; A.by_lanes = (65536u + lanes - 1) / lanes; A.by_merge = ((1u << 20) + merge - 1) / merge;
     const size_t own = ((size_t)A.each * 3 * patch * patch * size_of(dtype) + 15) / 16 * 16;

@@ -2,9 +2,12 @@
 
 Tolerances, per element.  The kernels work in single precision, u = 2^-24, and round once to the output type, which is off
 by at most eps / 2 of the value.
-* cosine and sine: what is left of the angle after whole turns is rounded to single precision (at most pi u) and the
-  function is off by at most 2 units in the last place, so each is off by at most 8 u; a turned element is a sum of two
-  products, a cos - b sin, off by at most (|a| + |b|) (8 + 3) u: 16 u is taken.
+* cosine and sine, 32-bit operands: what is left of the angle after whole turns is rounded to single precision (at most pi u)
+  and the function is off by at most 2 units in the last place, so each is off by at most 8 u.  16-bit operands: the angle,
+  at most pi, carries two roundings and that of pi itself (2.5 u of it), the hardware's functions are off by at most
+  2^-21.41 = 6.0 u (sine) and 2^-21.19 = 7.0 u (cosine): the sine by 2.5 pi u + 6.0 u = 13.9 u at most, the cosine by 2.5 u times
+  the largest x sin x up to pi, 1.82, + 7.0 u = 11.6 u.  A turned element is a sum of two products, a cos - b sin, whose
+  roundings are 2 u more: (|a| + |b|) times 16 u is taken.
 * the norm: a sum of up to 512 squares in at most 16 additions a lane and 5 between lanes (or 32 and 5 where the lanes go
   over a head value by value), so 1 / sqrt is off by (37 + 6) / 2 u, and the products by 3 u more: 32 u in all.
 * backward: dx = r (d w - v m), m = mean(d w v) with v = x r; d w and v by the figures above, m by at most 37 + 16 + 32 + 8
