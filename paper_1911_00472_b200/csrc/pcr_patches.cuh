@@ -64,14 +64,14 @@ __device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) {
 
 // A token's patch: whether there is one, and where.
 struct Patch {
-    bool ok, words, flip;          // words: rows may be counted in 32 bits, and aligned words read without leaving the buffer
+    bool ok, near, words, flip;    // near: rows may be counted in 32 bits; words: and every row is followed by 16 bytes of the buffer
     int32_t row, col;
     int64_t pitch;
     const uint8_t* corner;         // the rectangle's first byte
     Axis x, y;
 };
 __device__ __forceinline__ void look_up(const PatchArgs& A, int2 token, Patch& r) {
-    r.ok = r.words = false;
+    r.ok = r.near = r.words = false;
     const int32_t image = token.x;
     if (image < 0 || image >= A.n_images) return;
     const longlong2* from = reinterpret_cast<const longlong2*>(A.images + image);
@@ -93,7 +93,8 @@ __device__ __forceinline__ void look_up(const PatchArgs& A, int2 token, Patch& r
     r.flip = m.flip != 0;
     r.pitch = 3 * (int64_t)width;
     const int64_t corner = m.y0 * r.pitch + 3 * m.x0, behind = corner + (h - 1) * r.pitch + 3 * w + 16;
-    r.words = h * r.pitch < (int64_t)1 << 31 && (uint64_t)behind <= room;
+    r.near = h * r.pitch < (int64_t)1 << 31;
+    r.words = r.near && (uint64_t)behind <= room;
     r.corner = A.rgb + m.offset + corner;
     r.x = axis_of(cols * A.patch, w);
     r.y = axis_of(rows * A.patch, h);
@@ -124,8 +125,10 @@ __device__ __forceinline__ Rgb mix_single(const uint8_t* at, float f) {
     return mix_bytes(lo, hi, f);
 }
 
-struct True { static constexpr bool value = true; };
-struct False { static constexpr bool value = false; };
+// How a walk reads its words.  kPlain: from addresses of whole words on (their shift is the lane's own), and no column two
+// pixels on; kFree: from any address; kEnd: and none beyond the end of the buffer.
+enum { kPlain, kFree, kEnd };
+template <int kHow> struct How { static constexpr int value = kHow; };
 
 // One or two columns of a source row, mixed; two at a time in every instruction.
 template <int kCols> struct Mixed { F2 c[3]; };
@@ -134,18 +137,31 @@ template <> struct Mixed<1> { float c[3]; };
 // The words that two neighbouring columns lie in: the left one's six bytes begin at `sh` bits into the first, the right
 // one's 0, 3 or 6 bytes further on.
 struct Words { uint32_t w0, w1, w2, w3, sh; };
-template <bool kPlain>                     // plain: `at` is a word already (its shift is the lane's own), and no column two pixels on
-__device__ __forceinline__ Words words_at(const uint8_t* at, bool wide) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(kPlain ? reinterpret_cast<uintptr_t>(at) : reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
-    Words r = {__ldg(p), __ldg(p + 1), __ldg(p + 2), 0, (uint32_t)reinterpret_cast<uintptr_t>(at) << 3};
-    if (!kPlain && wide) r.w3 = __ldg(p + 3);
+// The end of a buffer of at least four bytes: its last whole word, and the bytes behind that.
+struct End { const uint32_t* last; uint32_t rest; };
+__device__ __forceinline__ End end_of(const uint8_t* from, size_t bytes) {
+    const uint8_t* b = from + (bytes & ~(size_t)3);
+    const int n = (int)(bytes & 3);
+    return {reinterpret_cast<const uint32_t*>(b) - 1, (n > 0 ? b[0] : 0u) | (n > 1 ? (uint32_t)b[1] << 8 : 0u) | (n > 2 ? (uint32_t)b[2] << 16 : 0u)};
+}
+template <int kHow>
+__device__ __forceinline__ Words words_at(const uint8_t* at, bool wide, const End& end) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(kHow == kPlain ? reinterpret_cast<uintptr_t>(at) : reinterpret_cast<uintptr_t>(at) & ~(uintptr_t)3);
+    Words r = {0, 0, 0, 0, (uint32_t)reinterpret_cast<uintptr_t>(at) << 3};
+    if (kHow == kEnd) {                       // (what lies behind the last bytes has no weight: any number does)
+        auto word = [&](int i) { const uint32_t v = __ldg(p + i <= end.last ? p + i : end.last); return p + i <= end.last ? v : end.rest; };
+        r.w0 = word(0); r.w1 = word(1); r.w2 = word(2); r.w3 = word(3);
+        return r;
+    }
+    r.w0 = __ldg(p); r.w1 = __ldg(p + 1); r.w2 = __ldg(p + 2);
+    if (kHow != kPlain && wide) r.w3 = __ldg(p + 3);
     return r;
 }
-template <bool kPlain>
+template <int kHow>
 __device__ __forceinline__ Mixed<2> mix_words(const Words& w, uint32_t own, bool wide, uint32_t shift, F2 f) {
-    const uint32_t sh = kPlain ? own : w.sh;
+    const uint32_t sh = kHow == kPlain ? own : w.sh;
     const uint32_t x0 = __funnelshift_r(w.w0, w.w1, sh), x1 = __funnelshift_r(w.w1, w.w2, sh), x2 = __funnelshift_r(w.w2, w.w3, sh);
-    const uint32_t a = !kPlain && wide ? x1 : x0, b = !kPlain && wide ? x2 : x1, y0 = __funnelshift_r(a, b, shift), y1 = __funnelshift_r(b, x2, shift);
+    const uint32_t a = kHow != kPlain && wide ? x1 : x0, b = kHow != kPlain && wide ? x2 : x1, y0 = __funnelshift_r(a, b, shift), y1 = __funnelshift_r(b, x2, shift);
     const F2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f), down = pack2(-kUp, -kUp);
     Mixed<2> r;
 #pragma unroll
@@ -194,7 +210,7 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
     const int count = (int)min((uint64_t)each, A.n_tokens - first);
     const bool here = sub < count;
     Patch m;
-    m.ok = m.words = false;
+    m.ok = m.near = m.words = false;
     const uint8_t *base = nullptr, *other = nullptr;        // the rectangle's first row at the left column, at the right one
     float fl = 0.f, fr = 0.f;
     uint4* const rows0 = &s_rows[warp][here ? sub * p : 0];
@@ -206,36 +222,39 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
             const Tap tl = tap_of(ox, m.x), tr = kCols == 2 ? tap_of(ox + 1, m.x) : tl;
             fl = tl.f; fr = tr.f;
             base = m.corner + 3 * tl.lo; other = m.corner + 3 * tr.lo;
-            const uint32_t pitch = m.words ? (uint32_t)m.pitch : 1u;
+            const uint32_t pitch = m.near ? (uint32_t)m.pitch : 1u;
 #pragma unroll
             for (int k = 0; k < kCols; ++k) {
                 const Tap ty = tap_of(m.row * p + px + k, m.y);
                 const uint32_t off = (uint32_t)ty.lo * pitch;
                 rows0[px + k] = make_uint4(off, ty.f != 0.f ? off + pitch : off, __float_as_uint(ty.f), 0);       // (weight 0: the row below may not be there)
-                if (m.words) soon(base + off);               // the patch's diagonal: its rows arrive together
+                if (m.near) soon(base + off);                // the patch's diagonal: its rows arrive together
             }
         }
     }
-    // as a rule a warp's rows begin at whole words, are not mirrored, and its neighbouring columns at most a pixel apart:
-    // a third of the walk's shifts, selects and address arithmetic is then left out (they bound it)
+    // As a rule a warp's rows begin at whole words, are not mirrored, and its neighbouring columns at most a pixel apart:
+    // a third of the walk's shifts, selects and address arithmetic is then left out (they bound it).
     const bool plain = kCols == 2 && __all_sync(0xffffffffu, !here || (m.words && !m.flip && (m.pitch & 3) == 0 && other - base <= 3));
     __syncwarp();
+    // A patch whose last row (the lowest: its entry stands last) is the buffer's may have fewer than the four words that a lane
+    // reads: its warp looks at every word's place.
+    const bool at_end = !plain && __any_sync(0xffffffffu, here && m.near && !m.words && other + rows0[p - 1].y + 16 > A.rgb + A.rgb_bytes);
     if (here) {
         T* o = (kDirect ? static_cast<T*>(A.out) + (first + sub) * (uint64_t)values : buf + sub * values) + px;
         const uint4* rows = rows0;
         const bool swap = m.flip && m.ok;
         auto value = [&](int c, float top, float low, float fy) { return fmaf(fmaf(fy, low - top, top), A.scale[c], A.shift[c]); };
-        if (kCols == 2 && m.words && other - base <= 6) {
+        if (kCols == 2 && m.near && other - base <= 6 && A.rgb_bytes >= 4) {
             const F2 f = pack2(fl, fr), minus = pack2(-1.f, -1.f);
             // On entry `top` holds the mixed row at low_at and `low` the one at top_at (the last output row's, roles swapped): as
             // a rule an output row's upper source row is the last one's lower, and one row is mixed.
-            auto walk = [&](auto plain_, const uint8_t* from, uint32_t own_shift, bool wide, uint32_t shift, bool mirror) {
-                constexpr bool kPlain = decltype(plain_)::value;
+            auto walk = [&](auto how, const uint8_t* from, uint32_t own_shift, bool wide, uint32_t shift, bool mirror, const End& end) {
+                constexpr int kHow = decltype(how)::value;
                 uint32_t top_at = ~0u, low_at = ~0u;
                 auto step = [&](Mixed<2>& top, Mixed<2>& low, const Words& now, Words& next, T* to, const uint4& r, const uint4& after) {
-                    next = words_at<kPlain>(from + after.y, wide);
-                    if (r.x != low_at) top = r.x == top_at ? low : mix_words<kPlain>(words_at<kPlain>(from + r.x, wide), own_shift, wide, shift, f);
-                    low = mix_words<kPlain>(now, own_shift, wide, shift, f);
+                    next = words_at<kHow>(from + after.y, wide, end);
+                    if (r.x != low_at) top = r.x == top_at ? low : mix_words<kHow>(words_at<kHow>(from + r.x, wide, end), own_shift, wide, shift, f);
+                    low = mix_words<kHow>(now, own_shift, wide, shift, f);
                     top_at = r.x; low_at = r.y;
                     const float fy = __uint_as_float(r.z);
                     const F2 fy2 = pack2(fy, fy);
@@ -244,11 +263,11 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
                         const F2 v = fma2(fma2(fy2, fma2(top.c[c], minus, low.c[c]), top.c[c]), pack2(A.scale[c], A.scale[c]), pack2(A.shift[c], A.shift[c]));
                         float a, b;
                         unpack2(v, a, b);
-                        put_two(to + c * area, a, b, !kPlain && mirror);
+                        put_two(to + c * area, a, b, kHow != kPlain && mirror);
                     }
                 };
                 Mixed<2> u = {}, v = {};
-                Words even = words_at<kPlain>(from + rows[0].y, wide), odd;
+                Words even = words_at<kHow>(from + rows[0].y, wide, end), odd;
 #pragma unroll 1
                 for (int dy = 0; dy < p; dy += 2, o += 2 * p, rows += 2) {
                     const uint4 r0 = rows[0], r1 = rows[1], r2 = rows[dy + 2 < p ? 2 : 1];
@@ -257,9 +276,12 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
                 }
             };
             const uint32_t sh = (uint32_t)reinterpret_cast<uintptr_t>(base) << 3;
-            if (plain) walk(True(), base - (reinterpret_cast<uintptr_t>(base) & 3), sh, false, other != base ? 24 : 0, false);
-            else walk(False(), base, sh, other - base == 6, other - base == 6 ? 16 : other != base ? 24 : 0, swap);
-        } else if (m.words) {
+            const bool wide = other - base == 6;
+            const uint32_t shift = wide ? 16 : other != base ? 24 : 0;
+            if (plain) walk(How<kPlain>(), base - (reinterpret_cast<uintptr_t>(base) & 3), sh, false, shift, false, End());
+            else if (!at_end) walk(How<kFree>(), base, sh, wide, shift, swap, End());
+            else walk(How<kEnd>(), base, sh, wide, shift, swap, end_of(A.rgb, A.rgb_bytes));
+        } else if (m.near && !at_end) {
             Rgb top[kCols], low[kCols];
             const float f[2] = {fl, fr};
             const uint8_t* const from[2] = {base, other};
@@ -277,11 +299,12 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
                 top_at = r.x; low_at = r.y;
             }
         } else if (m.ok) {
+            const int64_t pitch = m.near ? 1 : m.pitch;        // (of what stands in s_rows)
             for (int dy = 0; dy < p; ++dy, o += p) {
                 const uint4 r = rows[dy];
                 for (int k = 0; k < kCols; ++k) {
                     const uint8_t* at = k ? other : base;
-                    const Rgb top = mix_single(at + r.x * m.pitch, k ? fr : fl), low = mix_single(at + r.y * m.pitch, k ? fr : fl);
+                    const Rgb top = mix_single(at + r.x * pitch, k ? fr : fl), low = mix_single(at + r.y * pitch, k ? fr : fl);
                     const float fy = __uint_as_float(r.z);
                     T* to = o + (swap ? kCols - 1 - k : k);
                     to[0] = from_f<T>(value(0, top.r, low.r, fy)); to[area] = from_f<T>(value(1, top.g, low.g, fy)); to[2 * area] = from_f<T>(value(2, top.b, low.b, fy));

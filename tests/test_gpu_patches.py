@@ -126,6 +126,26 @@ def test_resampling_by_any_factor(patch, scale):
         check(P.patch_tokens(rgb, plan.images, plan.index, patch, MEAN, STD, dtype=dtype), want)
 
 
+@pytest.mark.parametrize("patch", [14, 16, 9])
+@pytest.mark.parametrize("flip", [0, 1])
+def test_end_of_the_buffer(patch, flip):
+    """Images whose last pixel is the buffer's, of 0 to 3 bytes beyond a whole word: nothing behind it counts."""
+    for w, h in [(61, 43), (61, 44), (62, 45), (63, 47), (1, 1), (5, 1), (1, 3)]:
+        pics, info, _ = images([(8, 3), (w, h)], w)
+        pics, info = pics[1:], [Info(0, w, h)]
+        n = pics[0].size
+        for grid in [(max(1, h // patch), max(1, w // patch)), (5, 6), (1, 2)]:
+            crop = (0, 0, w, h, flip)
+            plan = P.patch_plan(info, patch, crops=np.array([crop]), grids=np.array([grid]))
+            got = []
+            for behind in (0, 255):
+                room = torch.full((n + 64,), behind, dtype=torch.uint8, device="cuda")
+                room[:n] = torch.from_numpy(pics[0].reshape(-1)).cuda()
+                got.append(P.patch_tokens(room[:n], plan.images, plan.index, patch, MEAN, STD, dtype=torch.float32))
+            assert torch.equal(got[0], got[1])
+            check(got[0], tokens_of(pics[0], crop, grid, patch, 1))
+
+
 def test_graphs_and_streams():
     """Captured and replayed on other pixels, and on a stream of its own."""
     pics, info, rgb = images(SIZES)
