@@ -507,14 +507,15 @@ __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_
                 unpack2(sq, sum[0], other[0]); unpack2(dot, sum[1], other[1]);
                 sum[0] += other[0]; sum[1] += other[1];
                 row_sums<2>(sum, lanes);
-                const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m1 = -(sum[1] * r * A.inv_dim * r), rl = live ? r : 0.f;
-                const F2 r2 = pack2(r, r), m2 = pack2(m1, m1), rl2 = pack2(rl, rl);
+                const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m1 = -(sum[1] * r * A.inv_dim * r);
+                const F2 r2 = pack2(r, r), m2 = pack2(m1, m1);
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    d.a[i] = mul2(fma2(x2.a[i], m2, d.a[i]), r2); d.b[i] = mul2(fma2(x2.b[i], m2, d.b[i]), r2);
-                    dw.a[i] = fma2(q.a[i], rl2, dw.a[i]); dw.b[i] = fma2(q.b[i], rl2, dw.b[i]);
+                for (int i = 0; i < N; ++i) { d.a[i] = mul2(fma2(x2.a[i], m2, d.a[i]), r2); d.b[i] = mul2(fma2(x2.b[i], m2, d.b[i]), r2); }
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) { dw.a[i] = fma2(q.a[i], r2, dw.a[i]); dw.b[i] = fma2(q.b[i], r2, dw.b[i]); }
+                    store_row<T, V>(y, at.gap, row_of<T, V, kNext>(d));
                 }
-                if (live) store_row<T, V>(y, at.gap, row_of<T, V, kNext>(d));
                 y += ys;
             };
             if (kGroup == 2 && h + 2 <= heads) { work(0); work(kGroup - 1); }

@@ -233,6 +233,21 @@ def test_values_that_are_not_numbers_stay_in_their_rows(size):
     check_backward(torch.zeros_like(q), g, dx[0], dx[2], angle_of(positions, inv_freq, axes), False, wq, 1e-6)
 
 
+@pytest.mark.parametrize("size", [128, 72])
+def test_an_infinite_gradient_in_the_last_token(size):
+    """Lanes without a token go along with the last one's data: they add nothing to the weights' gradient, no 0 * inf either."""
+    for tokens in (1, 5, 6, 7):
+        q, _, positions, inv_freq, axes, w, _ = make((1, tokens, 2, 0, size, size), torch.float32, seed=3)
+        g = torch.randn_like(q)
+        g[0, -1, 1, 3] = math.inf
+        _, _, dw, _ = P.norm_rotate_backward(g, None, q, None, w, None, positions, inv_freq, axes)
+        half = size // 2
+        assert bool(dw[[3, 3 + half]].isinf().all())
+        others = torch.ones(size, dtype=torch.bool, device="cuda")
+        others[[3, 3 + half]] = False
+        assert bool(dw[others].isfinite().all())
+
+
 def test_offsets_past_32_bits():
     # two tokens 2^31 + 256 elements apart, and heads as far
     far = (1 << 31) + 256
