@@ -297,7 +297,8 @@ int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_token
         const size_t shared = (size_t)n_segments * sizeof(uint2);
         const int64_t runs = std::min<int64_t>(std::max<int64_t>((n_tokens + kRunTokens - 1) / kRunTokens, 1), sm_count() * (shared > 100 * 1024 ? 1 : 2) - 1);
         A.run = (uint32_t)(((n_tokens + runs - 1) / runs + kScanThreads - 1) / kScanThreads * kScanThreads);      // whole rounds of every warp
-        if (shared > 40 * 1024 && cudaFuncSetAttribute(positions_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) {
+        // (always the same limit: calls from several host threads set it side by side)
+        if (shared > 40 * 1024 && cudaFuncSetAttribute(positions_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSegments * (int)sizeof(uint2)) != cudaSuccess) {
             cudaGetLastError();
             return PCR_E_CUDA;
         }

@@ -3,6 +3,8 @@
 Tolerance of a token's value (v / 255 - mean) / std: the weights of the taps and each of the two mixes are off by at most
 3 u of 255 (u = 2^-24; where a sample falls is worked out in whole numbers), scaling and shifting by 3 u of their
 terms: 16 u (1 / std + |mean / std|) is taken, and half a step of the output type.  Positions are whole numbers: equal."""
+from concurrent.futures import ThreadPoolExecutor
+
 import numpy as np
 import pytest
 import torch
@@ -268,6 +270,23 @@ def test_positions_many_segments(n):
     rows = [(int(rng.integers(0, 9)), 0, 0, int(s)) if rng.random() < 0.5 else (int(rng.integers(0, 3)), int(rng.integers(1, 6)), int(rng.integers(1, 6)), int(s)) for s in seq]
     check_positions(rows, int(seq[-1]) + 1)
     check_positions(rows, int(seq[-1]) + 1, restart=True, time_step=2)
+
+
+def test_positions_asked_for_by_several_threads():
+    """Calls of different sizes side by side: the kernel's limit of shared memory is the same for all."""
+    def work(n):
+        rng = np.random.default_rng(n)
+        rows = [(int(t), 0, 0, i // 7) for i, t in enumerate(rng.integers(0, 4, n))]
+        segments = torch.tensor(rows, dtype=torch.int32, device="cuda")
+        want, after = positions_of(rows, n // 7 + 1)
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        got = [P.token_positions(segments, want.shape[1], n // 7 + 1, stream=stream) for _ in range(50)]
+        stream.synchronize()
+        return all(np.array_equal(g.cpu().numpy(), want) and np.array_equal(e.cpu().numpy(), after) for g, e in got)
+
+    with ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(work, [16384, 5200, 9000, 700]))
 
 
 def test_positions_long_segments():
