@@ -445,10 +445,10 @@ __device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool end
 // Up to kFewSegments segments: every CTA works out where all of them begin, keeps that in shared memory and writes its own
 // run of tokens.  One launch; the segments are read by every CTA, 16 bytes each, out of L2.  A thread finds its first token's
 // segment by bisection and goes on from there.
-// Latency and the sums that every CTA repeats bound it: 8704 segments of 1.4 million tokens 19 us, 72 segments 6 us; 16384 segments
-// 18.5 us, one more, by the two launches below, 55.
+// Latency and the sums that every CTA repeats bound it: 8704 segments of 1.4 million tokens 16 us, 72 segments 6 us; 16384 segments
+// of 5 tokens 14 us, one more, by the two launches below, 39.
 constexpr int kFewSegments = 16384, kRunTokens = 1024;
-__global__ void __launch_bounds__(kScanThreads, 2) positions_kernel(const __grid_constant__ PositionArgs A) {
+__global__ void __launch_bounds__(kScanThreads) positions_kernel(const __grid_constant__ PositionArgs A) {
     extern __shared__ uint2 s_begin[];                                    // (first token, first position)
     const int n = A.n_segments, tid = threadIdx.x;
     const bool ends = blockIdx.x + 1 == gridDim.x;                        // (the last CTA, behind all runs, writes the sequences' ends)
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) positions_kernel(const __grid
 }
 
 // More segments: one CTA writes where each begins to device memory, then a thread a token looks its segment up there.  The one
-// CTA's walk over the segments bounds it (most of 55 us for 16385 segments); so many segments in one call are rare.
+// CTA's walk over the segments bounds it (most of 39 us for 16385 segments); so many segments in one call are rare.
 __global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __grid_constant__ PositionArgs A) {
     const int64_t total = walk_segments(A, true, [&](int i, int64_t token, int32_t position) { A.starts[i] = token; A.bases[i] = position; });
     if (threadIdx.x == 0) A.starts[A.n_segments] = total;
