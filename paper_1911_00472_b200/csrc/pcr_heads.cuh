@@ -170,6 +170,48 @@ __device__ __forceinline__ void row_sums(float (&v)[N], const RowLanes& L) {
     for (int k = 0; k < N; ++k) v[k] = all[k];
 }
 
+// The same with the number of steps known (the backward pass, which instructions bound: 16384 tokens, heads of 72, 9 lanes: 63.6 ->
+// 55.4 us; heads of 256, 16 lanes: 59.5 -> 51.4; of 128, 8 lanes: 54.7 -> 53.0; forward passes wait for memory and gain nothing).
+// kSteps > 0: rows of 2^kSteps lanes.  kSteps < 0: of any other number below 2^-kSteps; step i adds the sum that begins 2^i
+// lanes further on, which ends with the row, and the first lane's sum goes round.  32 is no multiple of such a number, so
+// that the warp's last lane is free to hold 0 for what lies behind a row.  0: any number (above).
+template <int kSteps> struct RowSums {
+    uint32_t from;                 // lanes to take from, five bits a step
+    int first;
+    bool spare;
+    __device__ __forceinline__ RowSums(int n, int first_, int at) : from(0), first(first_), spare((threadIdx.x & 31) == 31) {
+#pragma unroll
+        for (int i = 0; i < -kSteps; ++i) from |= (uint32_t)(!spare && at + (1 << i) < n ? (first + at + (1 << i)) & 31 : 31) << (5 * i);
+    }
+    template <int N> __device__ __forceinline__ void operator()(float (&v)[N]) const {
+        if constexpr (kSteps > 0) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], 1 << i);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = spare ? 0.f : v[k];
+#pragma unroll
+            for (int i = 0; i < -kSteps; ++i)
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] += __shfl_sync(0xffffffffu, v[k], (int)(from >> (5 * i)));
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, v[k], first);
+        }
+    }
+};
+template <> struct RowSums<0> {
+    RowLanes lanes;
+    __device__ __forceinline__ RowSums(int n, int first, int at) : lanes(n, first, at) {}
+    template <int N> __device__ __forceinline__ void operator()(float (&v)[N]) const { row_sums<N>(v, lanes); }
+};
+// Rows of 1, 2 and 4 lanes have few steps to save.
+inline int steps_of(int lanes) {
+    if ((lanes & (lanes - 1)) == 0) return lanes == 8 ? 3 : lanes == 16 ? 4 : lanes == 32 ? 5 : 0;
+    return lanes < 8 ? -3 : lanes < 16 ? -4 : -5;
+}
+
 // A frequency as the turns of one position, a fraction of 2^64 (a whole turn, 2^64 itself, saturates to just below).
 __device__ __forceinline__ uint2 fraction_of(double freq) {
     double t = freq * 0.15915494309189533577;                   // 1 / (2 pi)
@@ -226,7 +268,7 @@ template <int V, bool kNext> struct Place {
         o1 = kNext ? 2 * V * at : turns ? pair : A.rot + 2 * V * (at - turning);
         gap = kNext || !turns ? V : A.rot / 2;
     }
-    __device__ __forceinline__ RowLanes row_lanes(const HeadArgs& A) const { return RowLanes(A.lanes, sub * A.lanes, at); }
+    template <typename Sums> __device__ __forceinline__ Sums row_sums_of(const HeadArgs& A) const { return Sums(A.lanes, sub * A.lanes, at); }
 };
 
 // The elements that make pair i: of the first and of the second vector, or 2 i and 2 i + 1 of both together.
@@ -326,7 +368,7 @@ __global__ void __launch_bounds__(kHeadThreads, kNorm ? 5 : 6) heads_kernel(cons
     positions_of(A, b, t, p);
     fill_tables<T>(A, S, 0);
     __syncthreads();
-    const RowLanes lanes = at.row_lanes(A);
+    const auto lanes = at.template row_sums_of<RowLanes>(A);
     F2 c[N], s[N];
     turns_of<T, V, kNext>(A, S, p, at, c, s);
 #pragma unroll 1
@@ -411,7 +453,7 @@ template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatil
 // and the lines that rows of odd sizes touch in L1 (62 % busy), not HBM (39 %), for 16384 tokens, 32 heads of 72.  Lanes with three
 // chunks of a row each (105 us in the place of 64) and whole tokens copied to shared memory first (68 to 84) were slower.
 __host__ __device__ constexpr int kBackCtas(int vector_bytes) { return vector_bytes >= 16 ? 3 : 4; }      // of an SM: what the registers leave room for
-template <typename T, int V, bool kNext>
+template <typename T, int V, bool kNext, int kSteps>
 __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_back_kernel(const __grid_constant__ HeadArgs A) {
     constexpr int kWarps = kHeadThreads / 32, kBytes = V * (int)sizeof(T), kGroup = kBytes >= 16 ? 1 : 2, kStages = 4, N = V / 2;
     using VT = Vec<T, V>;
@@ -467,7 +509,7 @@ __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_
     for (int k = 0; k < kStages - 1; ++k) fill();
     fill_tables<T>(A, S, which);
     __syncthreads();
-    const RowLanes lanes = at.row_lanes(A);
+    const auto add_up = at.template row_sums_of<RowSums<kSteps>>(A);
     const Pairs<V> w = weights_of<V, kNext>(S.w[0], at);
     Pairs<V> dw;
 #pragma unroll
@@ -506,7 +548,7 @@ __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_
                 float sum[2], other[2];
                 unpack2(sq, sum[0], other[0]); unpack2(dot, sum[1], other[1]);
                 sum[0] += other[0]; sum[1] += other[1];
-                row_sums<2>(sum, lanes);
+                add_up(sum);
                 const float r = rsqrtf(sum[0] * A.inv_dim + A.eps), m1 = -(sum[1] * r * A.inv_dim * r);
                 const F2 r2 = pack2(r, r), m2 = pack2(m1, m1);
 #pragma unroll

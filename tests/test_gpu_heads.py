@@ -130,6 +130,21 @@ def test_shapes(shape, interleaved, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("vectors", list(range(1, 33)))
+def test_rows_of_any_number_of_vectors(vectors, dtype):
+    """Heads of 1 to 32 pairs of 16-byte vectors, a pair a lane: every way in which the lanes of a row add up, with heads of one
+    operand far larger than the other's and tokens that leave lanes without one."""
+    size = vectors * (16 if dtype.itemsize == 2 else 8)
+    q, k, positions, inv_freq, axes, wq, wk = make((2, 37, 3, 1, size, size), dtype, seed=vectors)
+    q[1] *= 100
+    angle = angle_of(positions, inv_freq, axes)
+    gq, gk = (torch.randn(t.shape, device="cuda").to(dtype) for t in (q, k))
+    b = P.norm_rotate_backward(gq, gk, q, k, wq, wk, positions, inv_freq, axes, eps=1e-6, interleaved=vectors % 2 == 1)
+    for i, (x, g, w) in enumerate([(q, gq, wq), (k, gk, wk)]):
+        check_backward(x, g, b[i], b[2 + i], angle, vectors % 2 == 1, w, 1e-6)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
 def test_many_rows_and_weights_of_single_precision(dtype):
     # more tokens than one round of the grid, so that the sums of the weights' gradients run over several
     q, k, positions, inv_freq, axes, wq, wk = make((2, 4099, 6, 2, 64, 64), dtype, "packed", weight_dtype=torch.float32)
