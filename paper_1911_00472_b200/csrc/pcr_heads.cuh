@@ -171,7 +171,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], const RowLanes& L) {
 }
 
 // The same with the number of steps known (the backward pass, which instructions bound: 16384 tokens, heads of 72, 9 lanes: 63.6 ->
-// 55.4 us; heads of 256, 16 lanes: 59.5 -> 51.4; of 128, 8 lanes: 54.7 -> 53.0; forward passes wait for memory and gain nothing).
+// 55.7 us; heads of 256, 16 lanes: 59.5 -> 51.4; of 128, 8 lanes: 54.7 -> 53.0; of 64, 4 lanes: 55.4 -> 53.5; 48 heads of 72 of which
+// 36 are turned, 18 lanes: 109 -> 84; forward passes wait for memory and gain nothing).
 // kSteps > 0: rows of 2^kSteps lanes.  kSteps < 0: of any other number below 2^-kSteps; step i adds the sum that begins 2^i
 // lanes further on, which ends with the row, and the first lane's sum goes round.  32 is no multiple of such a number, so
 // that the warp's last lane is free to hold 0 for what lies behind a row.  0: any number (above).
@@ -206,9 +207,9 @@ template <> struct RowSums<0> {
     __device__ __forceinline__ RowSums(int n, int first, int at) : lanes(n, first, at) {}
     template <int N> __device__ __forceinline__ void operator()(float (&v)[N]) const { row_sums<N>(v, lanes); }
 };
-// Rows of 1, 2 and 4 lanes have few steps to save.
+// (rows of 1 and 2 lanes, heads of 4 to 32 elements, have no steps to save)
 inline int steps_of(int lanes) {
-    if ((lanes & (lanes - 1)) == 0) return lanes == 8 ? 3 : lanes == 16 ? 4 : lanes == 32 ? 5 : 0;
+    if ((lanes & (lanes - 1)) == 0) return lanes == 4 ? 2 : lanes == 8 ? 3 : lanes == 16 ? 4 : lanes == 32 ? 5 : 0;
     return lanes < 8 ? -3 : lanes < 16 ? -4 : -5;
 }
 

@@ -144,16 +144,15 @@ void fill(HeadArgs& A, const pcr_turn_args& a, const Cut& c) {
 template <typename T, int V, int kMode, bool kNext>
 void launch_vectors(const HeadArgs& A, dim3 grid, cudaStream_t st) {
     if constexpr (kMode == kNormTurnBack) {
-        const int steps = V > 2 ? steps_of(A.lanes) : 0;              // (rows of the shortest vectors are rare)
+        const int steps = steps_of(A.lanes);
         auto with = [&](auto kernel) { kernel<<<grid, kHeadThreads, 0, st>>>(A); };
-        if constexpr (V > 2) {
-            if (steps == 3) return with(heads_back_kernel<T, V, kNext, 3>);
-            if (steps == 4) return with(heads_back_kernel<T, V, kNext, 4>);
-            if (steps == 5) return with(heads_back_kernel<T, V, kNext, 5>);
-            if (steps == -3) return with(heads_back_kernel<T, V, kNext, -3>);
-            if (steps == -4) return with(heads_back_kernel<T, V, kNext, -4>);
-            if (steps == -5) return with(heads_back_kernel<T, V, kNext, -5>);
-        }
+        if (steps == 2) return with(heads_back_kernel<T, V, kNext, 2>);
+        if (steps == 3) return with(heads_back_kernel<T, V, kNext, 3>);
+        if (steps == 4) return with(heads_back_kernel<T, V, kNext, 4>);
+        if (steps == 5) return with(heads_back_kernel<T, V, kNext, 5>);
+        if (steps == -3) return with(heads_back_kernel<T, V, kNext, -3>);
+        if (steps == -4) return with(heads_back_kernel<T, V, kNext, -4>);
+        if (steps == -5) return with(heads_back_kernel<T, V, kNext, -5>);
         with(heads_back_kernel<T, V, kNext, 0>);
     } else heads_kernel<T, V, kMode == kNormTurn, kNext><<<grid, kHeadThreads, 0, st>>>(A);
 }

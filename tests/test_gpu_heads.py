@@ -130,12 +130,13 @@ def test_shapes(shape, interleaved, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("short", [False, True])
 @pytest.mark.parametrize("vectors", list(range(1, 33)))
-def test_rows_of_any_number_of_vectors(vectors, dtype):
-    """Heads of 1 to 32 pairs of 16-byte vectors, a pair a lane: every way in which the lanes of a row add up, with heads of one
+def test_rows_of_any_number_of_vectors(vectors, short, dtype):
+    """Heads of 1 to 32 pairs of 16-byte vectors (short: of vectors of two elements, as four turned elements ask for), a pair a lane: every way in which the lanes of a row add up, with heads of one
     operand far larger than the other's and tokens that leave lanes without one."""
-    size = vectors * (16 if dtype.itemsize == 2 else 8)
-    q, k, positions, inv_freq, axes, wq, wk = make((2, 37, 3, 1, size, size), dtype, seed=vectors)
+    size = vectors * (4 if short else 16 if dtype.itemsize == 2 else 8)
+    q, k, positions, inv_freq, axes, wq, wk = make((2, 37, 3, 1, size, 4 if short else size), dtype, seed=vectors)
     q[1] *= 100
     angle = angle_of(positions, inv_freq, axes)
     gq, gk = (torch.randn(t.shape, device="cuda").to(dtype) for t in (q, k))
