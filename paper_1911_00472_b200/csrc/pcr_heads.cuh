@@ -14,7 +14,7 @@
 // Measured on a B200 (6461 GB/s copied): norm and rotation of 32768 tokens, 32 + 8 heads of 128, bf16: 117 us, 5.7 TB/s, 89 % of
 // the copy rate; rotation of 8191 tokens out of a packed projection, fp16: 34 us, 4.9 TB/s (1.7 rounds of CTAs, the rest is
 // their end); rotation of 12003 tokens, 32 heads of 80, fp32: 43 us, 5.7 TB/s.  Backward of 8192 tokens, 40 heads of 128, bf16:
-// 55 us, 4.6 TB/s; of 16384 tokens, 32 heads of 72, bf16: 63.6 us, 3.6 TB/s.
+// 53 us, 4.8 TB/s; of 16384 tokens, 32 heads of 72, bf16: 55.7 us, 4.1 TB/s.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -448,11 +448,12 @@ template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatil
 //   q = d a, dot = sum of q w, dw += q r, dx = r (d w - a r^2 dot / dim)
 // Two operands, their factors and the sums leave no registers for rows on their way.  So every lane has a ring of kStages
 // groups of rows in shared memory that it alone fills and reads: no barrier, and kStages - 1 groups are always on their way
-// (three stages in the place of four: 60 us in the place of 55 for 8192 tokens, 40 heads of 128).
-// With vectors of 16 bytes three CTAs an SM keep everything in registers (four spill: 73 us in the place of 55); with shorter
-// ones four.  What bounds it: instructions (61 % of the issue slots, 12 warps an SM whose rows are chains of dependent steps)
-// and the lines that rows of odd sizes touch in L1 (62 % busy), not HBM (39 %), for 16384 tokens, 32 heads of 72.  Lanes with three
-// chunks of a row each (105 us in the place of 64) and whole tokens copied to shared memory first (68 to 84) were slower.
+// (three stages in the place of four: 57.5 us in the place of 52 for 8192 tokens, 40 heads of 128).
+// With vectors of 16 bytes three CTAs an SM keep everything in registers (four: 59.5 us in the place of 52), with shorter ones
+// four (16384 tokens, 32 heads of 72: 55.5 us, three 59.5, five 66).  What bounds it there: the lines that rows of odd sizes touch
+// in L1 and the sums' shuffles (77 % busy) and instructions (56 % of the issue slots, 15 warps an SM whose rows are chains of
+// dependent steps), not HBM (43 %).  Lanes with three chunks of a row each (105 us in the place of 64 at the time) and whole
+// tokens copied to shared memory first (68 to 84) were slower.
 __host__ __device__ constexpr int kBackCtas(int vector_bytes) { return vector_bytes >= 16 ? 3 : 4; }      // of an SM: what the registers leave room for
 template <typename T, int V, bool kNext, int kSteps>
 __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_back_kernel(const __grid_constant__ HeadArgs A) {
@@ -597,7 +598,7 @@ __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_
 
 // Heads of any even or odd size, any alignment and any strides: a warp a token, lanes over pairs, then over what is not
 // turned, value by value.  Bound by its instructions and single loads: 8192 tokens, 40 heads of 128, bf16, off by one element, take
-// 103 us (rotation), 131 (norm), 397 (backward), where whole vectors take 31, 35 and 55.
+// 101 us (rotation), 131 (norm), 396 (backward), where whole vectors take 31, 35 and 53.
 template <typename T, int kMode, bool kNext>
 __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_constant__ HeadArgs A) {
     constexpr int kWarps = kHeadThreads / 32;

@@ -90,8 +90,8 @@ struct Cut { int v, lanes, per, slots[2], rows[2]; unsigned x, y; };
 
 Cut cut_of(const pcr_turn_args& a, bool back) {
     Cut c = {};
-    // the longest vectors that fit: 8192 tokens, 40 heads of 128, bf16, by 16 / 8 / 4 bytes and value by value: rotation 31, 31, 34 and 103 us,
-    // norm 35, 41, 57 and 131, backward 55, 60, 89 and 397
+    // the longest vectors that fit: 8192 tokens, 40 heads of 128, bf16, by 16 / 8 / 4 bytes and value by value: rotation 31, 31, 34 and 101 us,
+    // norm 35, 41, 57 and 131, backward 53, 56, 72 and 396
     for (int v : {8, 4, 2})
         if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
     c.lanes = c.v ? a.head_dim / (2 * c.v) : 32;
