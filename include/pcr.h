@@ -273,8 +273,8 @@ typedef struct {
     const int32_t* positions;      /* DEVICE; axis a of token (b, t) at a, b, t times these strides    */
     int64_t position_stride[3];
     const void* inv_freq;          /* DEVICE, rot_dim / 2 finite frequencies, float or double (freq_dtype) */
-    const int32_t* axes;           /* DEVICE, rot_dim / 2: the axis that turns pair i; an axis outside
-                                      0 .. n_axes - 1 leaves the pair as it is                         */
+    const int32_t* axes;           /* DEVICE, rot_dim / 2: the axis that turns pair i; on an axis outside
+                                      0 .. n_axes - 1 every position is 0                              */
     int64_t batch, tokens;         /* tokens of each sequence; batch * tokens < 2^31                   */
     int32_t n_axes;                /* 1..4 */
     int32_t head_dim, rot_dim;     /* head_dim 1..512; the first rot_dim elements are turned (even, may be 0) */
@@ -288,8 +288,8 @@ typedef struct {
 } pcr_turn_args;
 
 /* Rotation of queries and keys, one launch: pair (a, b) becomes (a cos - b sin, a sin + b cos) with the
- * angle positions[axes[i]] * inv_freq[i], whose whole turns are taken off in double precision (far
- * positions lose nothing); single precision from there, one rounding to dtype.  Any strides and
+ * angle positions[axes[i]] * inv_freq[i], whose whole turns are taken off in 64 bits (far positions
+ * lose nothing); single precision from there, one rounding to dtype.  Any strides and
  * alignments of whole elements; in place is allowed.  Rows that stand on 16-byte boundaries in heads of
  * a multiple of 16 (16 bits) or 8 (32 bits) elements are fastest, rows at odd elements slowest.
  * Errors: PCR_E_ARG (also for an output that overlaps itself), PCR_E_CUDA. */

@@ -294,6 +294,8 @@ def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.b
         raise ValueError("index must be a contiguous (n, 2) int32 tensor")
     if dtype not in _CODES:
         raise ValueError("dtype must be torch.float16, torch.bfloat16 or torch.float32")
+    if len(mean) != 3 or len(std) != 3:
+        raise ValueError("mean and std must have three values")
     shape = (index.shape[0], 3 * patch * patch)
     if out is not None and (out.shape != shape or out.dtype != dtype or not out.is_contiguous()):
         raise ValueError("out must be contiguous, (n_tokens, 3 * patch * patch) of dtype")

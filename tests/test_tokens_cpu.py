@@ -160,6 +160,12 @@ def test_operands_on_the_host_are_refused():
         P.rotate(q.requires_grad_(), None, torch.zeros(1, 4, dtype=torch.int32), f, a)
 
 
+@pytest.mark.parametrize("mean,std", [((0.5,) * 2, (1,) * 3), ((0.5,) * 3, (1,) * 4)])
+def test_means_of_other_than_three_channels_are_refused(mean, std):
+    with pytest.raises(ValueError, match="three"):
+        P.patch_tokens(torch.zeros(8, dtype=torch.uint8), torch.zeros(1, 10, dtype=torch.int64), torch.zeros(1, 2, dtype=torch.int32), 14, mean, std)
+
+
 def test_axes():
     f, a = P.rotary_axes(16, base=100.0, sections=(2, 3, 3), device="cpu")
     assert a.tolist() == [0, 0, 1, 1, 1, 2, 2, 2] and f.dtype == torch.float64 and a.dtype == torch.int32
