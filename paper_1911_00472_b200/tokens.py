@@ -15,6 +15,7 @@ from typing import NamedTuple
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -48,6 +49,11 @@ def _on(device: torch.device, stream):
     if stream is not None and stream.device != device:
         raise ValueError("the stream belongs to another device than the operands")
     return _switched(device, stream)
+
+
+def _has_tangent(tensors) -> bool:
+    """Whether forward-mode differentiation follows one of them.  The level says at once that none is followed, as a rule."""
+    return getattr(forward_ad, "_current_level", 0) >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 def _same_device(device, *tensors):
@@ -104,7 +110,7 @@ def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
             followed = followed or g.requires_grad
     if not near:
         raise ValueError("all operands have to be on one device")
-    if followed and torch.is_grad_enabled():
+    if (followed and torch.is_grad_enabled()) or _has_tangent((q, k, inv_freq, q_weight, k_weight, *grads)):
         raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
     return batch, tokens, size, weight
 
