@@ -90,7 +90,7 @@ def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
     if axes.shape != other or axes.dtype != torch.int32 or not axes.is_contiguous():
         raise ValueError("axes must be a contiguous int32 vector as long as inv_freq")
     near = device == positions.get_device() == inv_freq.get_device() == axes.get_device() and (k is None or k.get_device() == device)
-    followed = q.requires_grad or (k is not None and k.requires_grad)
+    followed = q.requires_grad or inv_freq.requires_grad or (k is not None and k.requires_grad)
     weight = dtype
     if q_weight is not None or k_weight is not None:
         weight = (k_weight if q_weight is None else q_weight).dtype

@@ -40,3 +40,13 @@ def test_operands_with_tangents_are_refused(name):
             T._check(**with_one(name, lambda t: forward_ad.make_dual(t, torch.ones_like(t))))
         with torch.no_grad(), pytest.raises(ValueError, match="autograd"):          # no_grad leaves tangents as they are
             T._check(**with_one(name, lambda t: forward_ad.make_dual(t, torch.ones_like(t))))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_operands_that_require_gradients_are_refused(name):
+    """Frequencies among them: a model that learns them would get no gradient."""
+    a = with_one(name, lambda t: t.clone().requires_grad_())
+    with pytest.raises(ValueError, match="autograd"):
+        T._check(**a)
+    with torch.no_grad():
+        assert T._check(**a)[:3] == (1, 4, 8)
