@@ -56,6 +56,12 @@ def _has_tangent(tensors) -> bool:
     return getattr(forward_ad, "_current_level", 0) >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
+def _not_followed(*outputs):
+    """Outputs are written without autograd's knowledge: none of them may stand in its graph."""
+    if (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in outputs)) or _has_tangent(outputs):
+        raise ValueError("autograd does not see this call: out must be detached")
+
+
 def _same_device(device, *tensors):
     for t in tensors:
         if t is not None and t.device != device:
@@ -132,6 +138,7 @@ def _outputs(q, k, out):
             if o.shape[-1] > 1 and o.stride(-1) != 1:
                 raise ValueError("the elements of a head of out must stand side by side")
             _same_device(q.device, o)
+    _not_followed(*out)
     return out
 
 
@@ -306,6 +313,7 @@ def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.b
     if out is not None and (out.shape != shape or out.dtype != dtype or not out.is_contiguous()):
         raise ValueError("out must be contiguous, (n_tokens, 3 * patch * patch) of dtype")
     _same_device(rgb.device, images, index, out)
+    _not_followed(out)
     with _on(rgb.device, stream):
         if out is None:
             out = rgb.new_empty(shape, dtype=dtype)

@@ -50,3 +50,23 @@ def test_operands_that_require_gradients_are_refused(name):
         T._check(**a)
     with torch.no_grad():
         assert T._check(**a)[:3] == (1, 4, 8)
+
+
+def test_outputs_that_autograd_follows_are_refused():
+    """Values written into a tensor that requires a gradient, or has a tangent, would keep a derivative that is not theirs."""
+    a = operands()
+    q, k = a["q"], a["k"]
+    leaf, plain = torch.empty_like(q, requires_grad=True), torch.empty_like(k)
+    for out in ((leaf, plain), (leaf * 1, plain), (leaf.detach().clone().requires_grad_().view_as(q), plain)):
+        with pytest.raises(ValueError, match="autograd"):
+            T._outputs(q, k, out)
+        with torch.no_grad():
+            assert T._outputs(q, k, out) is out
+    with forward_ad.dual_level(), pytest.raises(ValueError, match="autograd"):
+        T._outputs(q, k, (torch.empty_like(q), forward_ad.make_dual(plain, torch.ones_like(plain))))
+    rgb, images, index = torch.zeros(8, dtype=torch.uint8), torch.zeros(1, 10, dtype=torch.int64), torch.zeros(1, 2, dtype=torch.int32)
+    tokens = torch.empty(1, 48, requires_grad=True)
+    with pytest.raises(ValueError, match="autograd"):
+        P.patch_tokens(rgb, images, index, 4, (0,) * 3, (1,) * 3, dtype=torch.float32, out=tokens)
+    with pytest.raises(ValueError, match="CUDA"), torch.no_grad():
+        P.patch_tokens(rgb, images, index, 4, (0,) * 3, (1,) * 3, dtype=torch.float32, out=tokens)
