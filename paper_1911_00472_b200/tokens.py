@@ -62,6 +62,13 @@ def _not_followed(*outputs):
         raise ValueError("autograd does not see this call: out must be detached")
 
 
+def _written(outputs):
+    """Tells autograd that a caller's tensors hold other values now: a graph that kept one of them says so when it needs it."""
+    for t in outputs:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 def _same_device(device, *tensors):
     for t in tensors:
         if t is not None and t.device != device:
@@ -187,9 +194,11 @@ def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, inte
     if grads:
         scratch = inv_freq.new_empty(-(-L.pcr_norm_rotate_scratch_bytes(args) // inv_freq.element_size()))
         B._chk(L.pcr_norm_rotate_backward(args, scratch.data_ptr(), _raw_stream(device)), name)
-        return y, z, dwq, dwk
-    B._chk(getattr(L, name)(args, _raw_stream(device)), name)
-    return y, z
+    else:
+        B._chk(getattr(L, name)(args, _raw_stream(device)), name)
+    if out is not None:
+        _written(out)
+    return (y, z, dwq, dwk) if grads else (y, z)
 
 
 def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False, out=None, stream=None):
@@ -272,6 +281,7 @@ def token_positions(segments, n_tokens, n_sequences, *, merge=1, time_step=1, re
     if out is not None and (out.dtype != torch.int32 or out.dim() != 2 or out.shape[0] != 3 or out.shape[1] < n_tokens or out.stride(1) != 1):
         raise ValueError("out must be int32 of shape (3, n_tokens) with a row's elements side by side")
     _same_device(segments.device, out)
+    given = out
     with _on(segments.device, stream):
         flags = B.PCR_POSITIONS_RESTART if restart else 0
         if out is None:
@@ -284,6 +294,7 @@ def token_positions(segments, n_tokens, n_sequences, *, merge=1, time_step=1, re
         B._chk(L.pcr_token_positions(segments.data_ptr(), segments.shape[0], n_tokens, n_sequences, merge, time_step, flags, out.data_ptr(),
                                      out.stride(0), after.data_ptr(), scratch.data_ptr(), _raw_stream(segments.device.index)),
                "pcr_token_positions")
+    _written((given,))
     return out, after
 
 
@@ -314,12 +325,14 @@ def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.b
         raise ValueError("out must be contiguous, (n_tokens, 3 * patch * patch) of dtype")
     _same_device(rgb.device, images, index, out)
     _not_followed(out)
+    given = out
     with _on(rgb.device, stream):
         if out is None:
             out = rgb.new_empty(shape, dtype=dtype)
         B._chk(B.lib().pcr_patch_tokens(rgb.data_ptr(), rgb.numel(), images.data_ptr(), images.shape[0], index.data_ptr(), shape[0], patch,
                                         merge, struct.pack("3f", *mean), struct.pack("3f", *std), _CODES[dtype], out.data_ptr(),
                                         _raw_stream(rgb.device.index)), "pcr_patch_tokens")
+    _written((given,))
     return out
 
 

@@ -1,0 +1,49 @@
+"""Outputs of the token operators that the caller gives: what autograd and other operands may still need of that memory."""
+import pytest
+import torch
+
+import paper_1911_00472_b200 as P
+
+pytestmark = pytest.mark.gpu
+
+
+def heads(hq=2, hk=2):
+    q, k = torch.randn(5, hq, 16, device="cuda"), torch.randn(5, hk, 16, device="cuda")
+    inv_freq, axes = P.rotary_axes(16)
+    return q, k, torch.arange(5, device="cuda", dtype=torch.int32)[None], inv_freq, axes
+
+
+def test_autograd_notices_that_a_saved_tensor_was_written_to():
+    q, k, positions, inv_freq, axes = heads()
+    w = torch.randn(16, device="cuda", requires_grad=True)
+    ones = torch.ones(16, device="cuda")
+    gq, gk = torch.randn_like(q), torch.randn_like(k)
+    for call in (lambda: P.rotate(q, k, positions, inv_freq, axes, out=(q, k)),
+                 lambda: P.rotate(q, k, positions, inv_freq, axes, out=(q, k), stream=torch.cuda.Stream()),
+                 lambda: P.norm_rotate(q, None, ones, None, positions, inv_freq, axes, out=(q, None)),
+                 lambda: P.norm_rotate_backward(gq, gk, q, k, ones, ones, positions, inv_freq, axes, out=(q, k))):
+        loss = (q * w).sum()                       # keeps q for w's gradient
+        call()
+        torch.cuda.synchronize()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    rgb = torch.zeros(192, dtype=torch.uint8, device="cuda")
+    plan = P.patch_plan([type("Info", (), dict(out_offset=0, width=8, height=8))], 4)
+    tokens, scale = torch.zeros(4, 48, device="cuda"), torch.ones(48, device="cuda", requires_grad=True)
+    loss = (tokens * scale).sum()
+    P.patch_tokens(rgb, plan.images, plan.index, 4, (0.5,) * 3, (0.5,) * 3, dtype=torch.float32, out=tokens)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    at = torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    table = torch.randn(100, 2, device="cuda", requires_grad=True)
+    loss = table[at].sum()
+    P.token_positions(plan.segments(), 4, 1, out=at)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    # without an output given nothing that is there is written to
+    version = q._version
+    P.rotate(q, k, positions, inv_freq, axes)
+    assert q._version == version
+    with torch.inference_mode():
+        inner = torch.randn_like(q)
+        P.rotate(inner, None, positions, inv_freq, axes, out=(inner, None))
