@@ -57,7 +57,9 @@ def _has_tangent(tensors) -> bool:
 
 
 def _not_followed(*outputs):
-    """Outputs are written without autograd's knowledge: none of them may stand in its graph."""
+    """Outputs are written without autograd's knowledge: none of them may stand in its graph, or have its sign taken on reading."""
+    if any(t is not None and t.is_neg() for t in outputs):
+        raise ValueError("out must not be a negated view")
     if (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in outputs)) or _has_tangent(outputs):
         raise ValueError("autograd does not see this call: out must be detached")
 
@@ -158,6 +160,10 @@ def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, inte
     if stream is not None or torch.cuda.current_device() != device:
         with _on(q.device, stream):
             return _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, interleaved, inverse, eps, out, None)
+    held = (q, k, q_weight, k_weight, inv_freq, *grads)
+    if any(t is not None and t.is_neg() for t in held):  # their memory holds the other sign
+        q_, k_, wq_, wk_, freq_, *grads_ = (None if t is None else t.resolve_neg() for t in held)
+        return _call(name, q_, k_, tuple(grads_), wq_, wk_, positions, freq_, axes, interleaved, inverse, eps, out, None)
     y, z = _outputs(q, k, out)
     dwq = dwk = None
     if grads and q_weight is not None:

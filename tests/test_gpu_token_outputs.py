@@ -47,3 +47,29 @@ def test_autograd_notices_that_a_saved_tensor_was_written_to():
     with torch.inference_mode():
         inner = torch.randn_like(q)
         P.rotate(inner, None, positions, inv_freq, axes, out=(inner, None))
+
+
+def test_operands_that_are_stored_negated():
+    """A view whose sign is taken on reading (the imaginary part of a conjugate) is turned as what it stands for."""
+    q, k, positions, inv_freq, axes = heads()
+    wq, wk, gq, gk = torch.randn(16, device="cuda"), torch.randn(16, device="cuda"), torch.randn_like(q), torch.randn_like(k)
+
+    def stored(t):
+        n = torch._neg_view(-t)
+        assert n.is_neg() and torch.equal(n, t)
+        return n
+
+    at = (positions, inv_freq, axes)
+    for want, got in ((P.rotate(q, k, *at), P.rotate(stored(q), stored(k), positions, stored(inv_freq), axes)),
+                      (P.norm_rotate(q, k, wq, wk, *at), P.norm_rotate(stored(q), stored(k), stored(wq), stored(wk), *at)),
+                      (P.norm_rotate_backward(gq, gk, q, k, wq, wk, *at),
+                       P.norm_rotate_backward(stored(gq), stored(gk), stored(q), stored(k), stored(wq), stored(wk), *at))):
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+    part = torch.view_as_complex(torch.stack([torch.zeros_like(q), -q], -1)).conj().imag          # elements two apart
+    assert torch.equal(P.rotate(part, None, *at)[0], P.rotate(q, None, *at)[0])
+    with pytest.raises(ValueError):                  # (an output would be read back with the other sign)
+        P.rotate(q, None, *at, out=(stored(torch.zeros_like(q)), None))
+    rgb = torch.zeros(192, dtype=torch.uint8, device="cuda")
+    plan = P.patch_plan([type("Info", (), dict(out_offset=0, width=8, height=8))], 4)
+    with pytest.raises(ValueError):
+        P.patch_tokens(rgb, plan.images, plan.index, 4, (0.5,) * 3, (0.5,) * 3, dtype=torch.float32, out=stored(torch.zeros(4, 48, device="cuda")))
