@@ -260,10 +260,12 @@ int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_token
 typedef struct {
     const void* x;                 /* input                                                            */
     void* y;                       /* output; backward: the gradient of x.  x itself (or dy itself) with the
-                                      same strides, or memory that shares no element with any operand  */
+                                      same strides, or memory that shares nothing with any operand, table
+                                      or other output: else the call is refused                        */
     const void* dy;                /* backward: the gradient of the forward's output                   */
     const void* weight;            /* norm: head_dim weights; NULL = ones                              */
-    void* dweight;                 /* backward: gradient of weight, same type; NULL = not wanted       */
+    void* dweight;                 /* backward: gradient of weight, same type; NULL = not wanted.  Apart
+                                      from the other outputs and the scratch memory                    */
     int64_t x_stride[3], y_stride[3], dy_stride[3];  /* in elements: batch, token, head                */
     int32_t heads;                 /* 0: this operand is left out                                      */
     int32_t rsvd;
@@ -292,7 +294,8 @@ typedef struct {
  * lose nothing); single precision from there, one rounding to dtype.  Any strides and
  * alignments of whole elements; in place is allowed.  Rows that stand on 16-byte boundaries in heads of
  * a multiple of 16 (16 bits) or 8 (32 bits) elements are fastest, rows at odd elements slowest.
- * Errors: PCR_E_ARG (also for an output that overlaps itself), PCR_E_CUDA. */
+ * Errors: PCR_E_ARG (also for an output that overlaps itself, another output or an operand that is not
+ * its own), PCR_E_CUDA. */
 int pcr_rotate(const pcr_turn_args* args, void* stream);
 
 /* The same behind a root-mean-square norm of every head, in one pass: x * weight / sqrt(mean(x^2) + eps),
@@ -302,7 +305,8 @@ int pcr_norm_rotate(const pcr_turn_args* args, void* stream);
 /* Its backward pass from x and dy (nothing is kept from the forward pass): y = gradient of x, dweight =
  * gradient of the weights, summed over all rows in single precision and always in the same order.
  *   scratch : DEVICE, pcr_norm_rotate_scratch_bytes(args) bytes (for the same args on the same device;
- *             0 for args that the call would refuse), 4-byte aligned; not needed without a dweight.
+ *             0 for args that the call would refuse for other reasons than shared memory), 4-byte aligned,
+ *             apart from all operands and outputs; not needed without a dweight.
  * y may be x or dy. */
 size_t pcr_norm_rotate_scratch_bytes(const pcr_turn_args* args);
 int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* stream);

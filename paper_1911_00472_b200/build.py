@@ -10,7 +10,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpcr_b200.so")
 SOURCES = ["pcr_lib.cu", "pcr_tokens.cu"]
 HEADERS = ["pcr_types.h", "pcr_entropy.cuh", "pcr_long.cuh", "pcr_pixels.cuh", "pcr_refine.cuh", "pcr_sequential.cuh", "pcr_msssim.cuh",
-           "pcr_heads.cuh", "pcr_launches.h", "pcr_patches.cuh"]
+           "pcr_heads.cuh", "pcr_launches.h", "pcr_patches.cuh", "pcr_spans.h"]
 
 
 def _nvcc() -> str:

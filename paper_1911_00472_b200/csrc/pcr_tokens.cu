@@ -12,6 +12,7 @@
 #include "pcr_heads.cuh"
 #include "pcr_launches.h"
 #include "pcr_patches.cuh"
+#include "pcr_spans.h"
 
 using namespace pcr;
 
@@ -181,7 +182,47 @@ void launch_patches(const PatchArgs& A, bool pairs, bool direct, unsigned grid, 
     else patch_tokens_kernel<T, 1, false><<<grid, 32 * warps, own * warps, st>>>(A);
 }
 
+size_t scratch_bytes_of(const pcr_turn_args& a, const Cut& c) { return ((size_t)c.rows[0] + c.rows[1]) * a.head_dim * sizeof(float); }
 bool nothing(const pcr_turn_args& a) { return a.batch * a.tokens == 0 || a.q.heads + a.k.heads == 0; }
+
+// Whether an output shares memory with another output or with an operand, other than an operand's own output that lies just
+// where it (or its gradient) does: kernels read and write in no order that a caller could count on.  A weight's gradient may
+// lie on what is read: it is written when all of that is done.
+bool outputs_shared(const pcr_turn_args& a, bool norm, bool back, const void* scratch, size_t scratch_bytes) {
+    const size_t es = size_of(a.dtype), ws = size_of(a.weight_dtype);
+    const pcr_heads* of[2] = {&a.q, &a.k};
+    const int reads = back ? 2 : 1;
+    Span y[2], x[2][2], held[5], late[2];                            // outputs; operands and gradients; what else is read; weights' gradients
+    int n_held = 0, n_late = 0;
+    for (int i = 0; i < 2; ++i) {
+        const pcr_heads& h = *of[i];
+        auto heads = [&](const void* p, const int64_t (&stride)[3]) { return span_of(p, stride, a.batch, a.tokens, h.heads, a.head_dim, es); };
+        y[i] = heads(h.y, h.y_stride);
+        x[i][0] = heads(h.x, h.x_stride);
+        x[i][1] = heads(h.dy, h.dy_stride);
+        if (norm && h.weight) held[n_held++] = span_of(h.weight, a.head_dim * ws);
+        if (back && h.dweight) late[n_late++] = span_of(h.dweight, a.head_dim * ws);
+    }
+    held[n_held++] = span_of(a.positions, a.position_stride, a.n_axes, a.batch, a.tokens, 1, sizeof(int32_t));
+    held[n_held++] = span_of(a.inv_freq, a.rot_dim / 2 * (a.freq_dtype == PCR_F64 ? 8 : 4));
+    held[n_held++] = span_of(a.axes, a.rot_dim / 2 * sizeof(int32_t));
+    auto same = [](const Span& s, const Span& t) {
+        for (int i = 0; i < 3; ++i)
+            if (s.n[i] > 1 && s.step[i] != t.step[i]) return false;
+        return s.at == t.at;
+    };
+    auto any = [](const Span& s, const Span* t, int n) { return std::any_of(t, t + n, [&](const Span& u) { return share_memory(s, u); }); };
+    for (int i = 0; i < 2; ++i) {
+        for (int j = 0; j < 2; ++j)
+            for (int r = 0; r < reads; ++r)
+                if (!(i == j && same(y[i], x[j][r])) && share_memory(y[i], x[j][r])) return true;
+        if (any(y[i], held, n_held) || any(y[i], late, n_late)) return true;
+    }
+    if (share_memory(y[0], y[1]) || (n_late == 2 && share_memory(late[0], late[1]))) return true;
+    if (n_late == 0) return false;
+    const Span s = span_of(scratch, scratch_bytes);
+    return any(s, y, 2) || any(s, x[0], 2) || any(s, x[1], 2) || any(s, held, n_held) || any(s, late, n_late);
+}
 
 }  // namespace
 
@@ -191,6 +232,7 @@ int pcr_rotate(const pcr_turn_args* args, void* stream) {
     if (!args) return PCR_E_ARG;
     if (int rc = check_heads(*args, false, false)) return rc;
     if (nothing(*args)) return PCR_OK;
+    if (outputs_shared(*args, false, false, nullptr, 0)) return PCR_E_ARG;
     const Cut c = cut_of(*args, false);
     HeadArgs A;
     fill(A, *args, c);
@@ -202,6 +244,7 @@ int pcr_norm_rotate(const pcr_turn_args* args, void* stream) {
     if (!args) return PCR_E_ARG;
     if (int rc = check_heads(*args, true, false)) return rc;
     if (nothing(*args)) return PCR_OK;
+    if (outputs_shared(*args, true, false, nullptr, 0)) return PCR_E_ARG;
     const Cut c = cut_of(*args, false);
     HeadArgs A;
     fill(A, *args, c);
@@ -211,8 +254,7 @@ int pcr_norm_rotate(const pcr_turn_args* args, void* stream) {
 
 size_t pcr_norm_rotate_scratch_bytes(const pcr_turn_args* args) {
     if (!args || check_heads(*args, true, true) != PCR_OK || nothing(*args)) return 0;
-    const Cut c = cut_of(*args, true);
-    return ((size_t)c.rows[0] + c.rows[1]) * args->head_dim * sizeof(float);
+    return scratch_bytes_of(*args, cut_of(*args, true));
 }
 
 int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* stream) {
@@ -224,6 +266,7 @@ int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* str
     WeightSums S = {{nullptr, nullptr}, {args->q.dweight, args->k.dweight}, {0, 0}, args->head_dim, args->weight_dtype == PCR_F32};
     if (!nothing(*args)) {
         const Cut c = cut_of(*args, true);
+        if (outputs_shared(*args, true, true, scratch, scratch_bytes_of(*args, c))) return PCR_E_ARG;
         HeadArgs A;
         fill(A, *args, c);
         float* at = static_cast<float*>(scratch);

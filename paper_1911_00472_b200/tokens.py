@@ -218,7 +218,8 @@ def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False,
               elements of a head are turned, the others copied
     interleaved      pairs (2 i, 2 i + 1) in place of (i, i + size / 2)
     inverse   by the negative angle: the gradient of the forward call
-    out       (q, k) to write to, the operands themselves allowed
+    out       (q, k) to write to: each its own operand, or memory that shares nothing with any operand or with the
+              other output (anything else is refused)
     """
     return _call("pcr_rotate", q, k, (), None, None, positions, inv_freq, axes, interleaved, inverse, 0.0, out, stream)
 
@@ -235,7 +236,7 @@ def norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, in
                          out=None, stream=None):
     """Gradients of norm_rotate from those of its outputs and from its inputs: (q, k, q_weight, k_weight).
 
-    out   where the gradients of q and k go; (grad_q, grad_k) or (q, k) themselves allowed
+    out   where the gradients of q and k go; grad_q or q itself allowed for the first, grad_k or k for the second (see rotate)
     """
     return _call("pcr_norm_rotate_backward", q, k, (grad_q, grad_k), q_weight, k_weight, positions, inv_freq, axes, interleaved, False, eps, out, stream)
 

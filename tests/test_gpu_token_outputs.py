@@ -73,3 +73,33 @@ def test_operands_that_are_stored_negated():
     plan = P.patch_plan([type("Info", (), dict(out_offset=0, width=8, height=8))], 4)
     with pytest.raises(ValueError):
         P.patch_tokens(rgb, plan.images, plan.index, 4, (0.5,) * 3, (0.5,) * 3, dtype=torch.float32, out=stored(torch.zeros(4, 48, device="cuda")))
+
+
+def test_outputs_that_share_memory_are_refused_and_others_are_not():
+    q, k, positions, inv_freq, axes = heads()
+    wq, wk, gq, gk = torch.randn(16, device="cuda"), torch.randn(16, device="cuda"), torch.randn_like(q), torch.randn_like(k)
+    t, kept = torch.full_like(q, 7.0), (q.clone(), k.clone())
+    long = torch.zeros(6, 2, 16, device="cuda")
+    long[:5] = q
+    calls = [lambda q, k, out: P.rotate(q, k, positions, inv_freq, axes, out=out),
+             lambda q, k, out: P.norm_rotate(q, k, wq, wk, positions, inv_freq, axes, out=out),
+             lambda q, k, out: P.norm_rotate_backward(gq, gk, q, k, wq, wk, positions, inv_freq, axes, out=out)]
+    for call in calls:
+        for a, b, out in ((q, k, (k, q)), (q, k, (t, t)), (q, q, (q, t)), (q, k, (t, q)), (q, k, (wq.expand(5, 2, 16), t)),
+                          (long[:5], k, (long[1:], t)), (q, k, (t, t.view(-1).as_strided((5, 2, 16), (16, 80, 1))))):
+            with pytest.raises(P.PcrError) as e:
+                call(a, b, out)
+            assert e.value.code == -1
+    for out in ((gk, gq), (gk, t), (t, gq)):
+        with pytest.raises(P.PcrError):
+            calls[2](q, k, out)
+    assert torch.equal(q, kept[0]) and torch.equal(k, kept[1]) and bool((t == 7).all())
+    for call in calls:
+        want = call(q, k, None)
+        # queries, keys and their outputs as slices of one buffer, heads between one another
+        room = torch.zeros(5, 8, 16, device="cuda")
+        room[:, 0::4], room[:, 1::4] = q, k
+        got = call(room[:, 0::4], room[:, 1::4], (room[:, 2::4], room[:, 3::4]))
+        assert all(torch.equal(a, b) for a, b in zip(want, got)) and torch.equal(room[:, 0::4], q) and torch.equal(room[:, 1::4], k)
+        got = call(room[:, 0::4], room[:, 1::4], (room[:, 0::4], room[:, 1::4]))            # in place
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
