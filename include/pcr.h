@@ -222,7 +222,7 @@ typedef struct {
  *   rgb       : DEVICE, 4-byte aligned, rgb_bytes bytes.
  *   images    : DEVICE, n_images rows, 16-byte aligned.   index : DEVICE, n_tokens pairs of int32, 8-byte aligned.
  *   patch     : 1..32.   merge : 1..64.   mean, std : HOST, three floats each, std > 0.
- *   tokens    : DEVICE, n_tokens x (3 * patch * patch) elements of dtype.
+ *   tokens    : DEVICE, n_tokens x (3 * patch * patch) elements of dtype, apart from all that is read.
  * A token whose entry names no image, no patch of it, or an image that does not lie inside `rgb` (or a
  * rectangle not inside its image, or rows or cols that are no multiples of merge, or a resampled side
  * over 2^20) is all zeros: tables are on the device and are not read by the host.
@@ -246,6 +246,7 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
  *                that a model adds one by one); 0 for a sequence without segments.
  *   scratch    : DEVICE, pcr_token_positions_scratch_bytes(n_segments) bytes (0 up to 16384 segments),
  *                8-byte aligned.
+ * Outputs and scratch memory share nothing with one another or with the segments: else the call is refused.
  * Counts below zero are taken as 0; positions are kept modulo 2^32.   time_step : 0 .. 2^20.
  * Errors: PCR_E_ARG, PCR_E_CUDA. */
 #define PCR_POSITIONS_RESTART 1

@@ -302,6 +302,9 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
     if (n_tokens == 0) return PCR_OK;
     if ((n_images > 0 && (!rgb || !images)) || !index || !tokens) return PCR_E_ARG;
     if (!aligned(rgb, 4) || !aligned(images, 16) || !aligned(index, 8) || !aligned(tokens, size_of(dtype))) return PCR_E_ARG;
+    const Span rows = span_of(tokens, (size_t)n_tokens * 3 * patch * patch * size_of(dtype));
+    if (share_memory(rows, span_of(rgb, rgb_bytes)) || share_memory(rows, span_of(images, (size_t)n_images * sizeof(PatchImage))) ||
+        share_memory(rows, span_of(index, (size_t)n_tokens * sizeof(int2)))) return PCR_E_ARG;
     PatchArgs A;
     A.rgb = static_cast<const uint8_t*>(rgb); A.images = reinterpret_cast<const PatchImage*>(images);
     A.index = reinterpret_cast<const int2*>(index); A.out = tokens; A.rgb_bytes = rgb_bytes;
@@ -338,6 +341,9 @@ int pcr_token_positions(const int32_t* segments, int n_segments, int64_t n_token
     if ((n_segments > 0 && !segments) || (n_tokens > 0 && !positions) || (n_sequences > 0 && !next) || (n_segments > kFewSegments && !scratch)) return PCR_E_ARG;
     if (!aligned(segments, 16) || !aligned(positions, 4) || !aligned(next, 4) || !aligned(scratch, 8)) return PCR_E_ARG;
     if (n_tokens > 0 && axis_stride < n_tokens) return PCR_E_ARG;
+    const Span read = span_of(segments, (size_t)n_segments * sizeof(int4)), ends = span_of(next, (size_t)n_sequences * 4),
+               rows = span_of(positions, {axis_stride, 0, 0}, 3, 1, 1, n_tokens, 4), own = span_of(scratch, n_segments > kFewSegments ? pcr_token_positions_scratch_bytes(n_segments) : 0);
+    if (share_memory(rows, read) || share_memory(ends, read) || share_memory(rows, ends) || share_memory(own, read) || share_memory(own, ends) || share_memory(own, rows)) return PCR_E_ARG;
     PositionArgs A;
     A.segments = reinterpret_cast<const int4*>(segments);
     A.starts = static_cast<int64_t*>(scratch);

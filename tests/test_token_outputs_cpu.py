@@ -139,3 +139,24 @@ def test_one_gradient_for_two_weights_and_scratch_that_is_used_already():
     a = good()
     for at in (a.q.x, a.k.y, a.k.dy, a.q.weight, a.k.dweight, a.positions, a.inv_freq, a.axes, a.q.dweight - 4):
         assert L.pcr_norm_rotate_backward(bytes(a), at, None) == E
+
+
+def test_patch_tokens_over_what_they_are_made_of():
+    import struct
+    call = B.lib().pcr_patch_tokens
+    m, s = struct.pack("3f", 0.5, 0.5, 0.5), struct.pack("3f", 0.2, 0.2, 0.2)
+    rgb, images, index, out = 1 << 20, 2 << 20, 3 << 20, 10 * 3 * 14 * 14 * 2         # (addresses, and the bytes of the output)
+    for at in (rgb, rgb + 996, images - out + 2, images + 158, index + 78, index - 2):
+        assert call(rgb, 1000, images, 2, index, 10, 14, 2, m, s, B.PCR_BF16, at, None) == E, hex(at)
+
+
+def test_positions_over_what_they_are_made_of():
+    call = B.lib().pcr_token_positions
+    segments, after, scratch = 1 << 20, 2 << 20, 3 << 20
+    n, few, many = 100, 3, 20000
+    for at in (segments, segments + 44, segments - 8 * n - 400 + 4, after, after + 4, after - 4 * n):           # rows of 400 bytes, 400 bytes apart
+        assert call(segments, few, n, 2, 1, 1, 0, at, n, after, None, None) == E, hex(at)
+    assert call(segments, few, n, 2, 1, 1, 0, 4 << 20, n, segments + 16, None, None) == E                       # the sequences' ends over a segment
+    for at in (segments, after, 4 << 20):
+        assert call(segments, many, n, 2, 1, 1, 0, 4 << 20, n, after, at, None) == E
+    assert call(segments, many, n, 2, 1, 1, 0, scratch + 8, n, after, scratch, None) == E
