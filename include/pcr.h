@@ -221,7 +221,8 @@ typedef struct {
  * blocks row by row and patches row by row in a block (merge = 1: row by row).
  *   rgb       : DEVICE, 4-byte aligned, rgb_bytes bytes.
  *   images    : DEVICE, n_images rows, 16-byte aligned.   index : DEVICE, n_tokens pairs of int32, 8-byte aligned.
- *   patch     : 1..32.   merge : 1..64.   mean, std : HOST, three floats each, std > 0.
+ *   patch     : 1..32.   merge : 1..64.   mean, std : HOST, three floats each, std > 0,
+ *               1 / (255 std) a normal number of single precision.
  *   tokens    : DEVICE, n_tokens x (3 * patch * patch) elements of dtype, apart from all that is read.
  * A token whose entry names no image, no patch of it, or an image that does not lie inside `rgb` (or a
  * rectangle not inside its image, or rows or cols that are no multiples of merge, or a resampled side

@@ -298,7 +298,7 @@ int pcr_patch_tokens(const void* rgb, size_t rgb_bytes, const pcr_patch_image* i
     if (n_images < 0 || n_tokens < 0 || n_tokens > INT32_MAX || patch < 1 || patch > kMaxPatch || merge < 1 || merge > 64) return PCR_E_ARG;
     if (!mean || !std_ || (dtype != PCR_F16 && dtype != PCR_F32 && dtype != PCR_BF16)) return PCR_E_ARG;
     for (int c = 0; c < 3; ++c)
-        if (!(std_[c] > 0.f) || !(fabsf(mean[c]) <= 3.0e38f) || isinf(std_[c])) return PCR_E_ARG;
+        if (!(std_[c] > 0.f) || !(fabsf(mean[c]) <= 3.0e38f) || !isnormal(1.f / (255.f * std_[c]))) return PCR_E_ARG;
     if (n_tokens == 0) return PCR_OK;
     if ((n_images > 0 && (!rgb || !images)) || !index || !tokens) return PCR_E_ARG;
     if (!aligned(rgb, 4) || !aligned(images, 16) || !aligned(index, 8) || !aligned(tokens, size_of(dtype))) return PCR_E_ARG;
