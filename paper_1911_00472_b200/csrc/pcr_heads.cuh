@@ -90,13 +90,9 @@ template <typename T, int N> __device__ __forceinline__ Vec<T, N> vec_of(const f
     return v;
 }
 
-// cosine and sine of position * freq: the whole turns are taken off in 64 bits, what is left fits single precision
-__device__ __forceinline__ void turn_of(int32_t position, double freq, bool inverse, float& c, float& s) {
-    double turns = (double)position * (freq * 0.15915494309189533577);       // 1 / (2 pi)
-    turns -= rint(turns);
-    sincospif((float)(2.0 * turns), &s, &c);
-    if (inverse) s = -s;
-}
+// 1 / (2 pi) in two parts: a product with the first alone is off by 2^-53 of its turns, and times 2^31 positions by more than
+// single precision is.
+constexpr double kTurns = 0x1.45f306dc9c883p-3, kTurnsRest = -0x1.6b01ec5417056p-57;
 
 __device__ __forceinline__ double freq_at(const HeadArgs& A, int i) {
     return A.freq64 ? static_cast<const double*>(A.inv_freq)[i] : (double)static_cast<const float*>(A.inv_freq)[i];
@@ -213,15 +209,16 @@ inline int steps_of(int lanes) {
     return lanes < 8 ? -3 : lanes < 16 ? -4 : -5;
 }
 
-// A frequency as the turns of one position, a fraction of 2^64 (a whole turn, 2^64 itself, saturates to just below).
+// A frequency as the turns of one position, a fraction of 2^64, modulo whole turns: the product and what its rounding left out
+// each lose 2^-65 (half a turn, 2^63 itself, saturates to just below).
 __device__ __forceinline__ uint2 fraction_of(double freq) {
-    double t = freq * 0.15915494309189533577;                   // 1 / (2 pi)
-    t -= floor(t);
-    const unsigned long long f = __double2ull_rn(t * 18446744073709551616.0);
+    const double t = freq * kTurns, rest = fma(freq, kTurnsRest, fma(freq, kTurns, -t));
+    const unsigned long long f = (unsigned long long)__double2ll_rn((t - rint(t)) * 18446744073709551616.0) +
+                                 (unsigned long long)__double2ll_rn((rest - rint(rest)) * 18446744073709551616.0);
     return make_uint2((uint32_t)f, (uint32_t)(f >> 32));
 }
 
-// What a CTA of the vector kernels keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its
+// What a CTA keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its
 // axis, and the weights of both norms.
 template <int kParts> struct HeadTables {          // 0 parts: no weights, 1: of one operand, 2: of both
     uint2 turn[kMaxHeadDim / 2];
@@ -243,8 +240,8 @@ __device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables<kParts
 }
 
 // cosine and sine of a position's turn.  The product of the position and the 64-bit fraction is taken modulo 2^64, that is
-// modulo whole turns: exact but for the fraction's own rounding (2^-65 turns a position), however far the position.  The
-// upper 32 bits are kept (2^-32 turns: 1.5e-9 of an angle).  16-bit results take the hardware's sine and cosine, off by
+// modulo whole turns: exact but for the fraction's own rounding (2^-64 turns a position for frequencies up to 2^40), however far
+// the position.  The upper 32 bits are kept (2^-32 turns: 1.5e-9 of an angle).  16-bit results take the hardware's sine and cosine, off by
 // 2^-21.19 at most, where the result itself is rounded to 2^-8 or 2^-11 of its value: 5 instructions in the place of about 40.
 template <typename T>
 __device__ __forceinline__ void turn_by(int32_t position, uint2 turn, bool inverse, float& c, float& s) {
@@ -598,10 +595,12 @@ __global__ void __launch_bounds__(kHeadThreads, kBackCtas(V * sizeof(T))) heads_
 
 // Heads of any even or odd size, any alignment and any strides: a warp a token, lanes over pairs, then over what is not
 // turned, value by value.  Bound by its instructions and single loads: 8192 tokens, 40 heads of 128, bf16, off by one element, take
-// 101 us (rotation), 131 (norm), 396 (backward), where whole vectors take 31, 35 and 53.
+// 97 us (rotation), 127 (norm), 384 (backward), where whole vectors take 29, 32 and 51.  Turns are the vector kernels', out of a
+// table (worked out in 64-bit floating point for every pair, with what its roundings left out: 110, 137 and 438).
 template <typename T, int kMode, bool kNext>
 __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_constant__ HeadArgs A) {
     constexpr int kWarps = kHeadThreads / 32;
+    __shared__ HeadTables<0> S;
     __shared__ float sums[kMode == kNormTurnBack ? kWarps : 1][kMode == kNormTurnBack ? kMaxHeadDim : 1];
     const int which = (int)blockIdx.y >= A.part[0].slots ? 1 : 0;
     const HeadBlock& H = A.part[which];
@@ -609,9 +608,10 @@ __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_co
     const int h0 = slot * A.per, h1 = min(h0 + A.per, H.heads);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int half = A.rot / 2;
+    fill_tables<T>(A, S, 0);
     if (kMode == kNormTurnBack)
         for (int j = lane; j < A.dim; j += 32) sums[warp][j] = 0.f;          // (a lane keeps to elements of its own, but for this)
-    __syncwarp();
+    __syncthreads();
     for (uint32_t n = blockIdx.x * kWarps + warp; n < A.tokens; n += gridDim.x * kWarps) {
         const uint32_t b = n / A.seq, t = n - b * A.seq;
         int32_t p[kMaxAxes];
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_co
                     for (int i = lane; i < half; i += 32) {
                         const int ja = kNext ? 2 * i : i, jb = kNext ? 2 * i + 1 : i + half;
                         float c, s;
-                        turn_of(on_axis(p, A.axes[i]), freq_at(A, i), false, c, s);
+                        turn_by<float>(on_axis(p, S.axis[i]), S.turn[i], false, c, s);
                         const float ga = to_f(g[ja]), gb = to_f(g[jb]);
                         dot += (ga * c + gb * s) * weight(ja) * to_f(x[ja]) + (gb * c - ga * s) * weight(jb) * to_f(x[jb]);
                     }
@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_any_kernel(const __grid_co
             for (int i = lane; i < half; i += 32) {
                 const int ja = kNext ? 2 * i : i, jb = kNext ? 2 * i + 1 : i + half;
                 float c, s;
-                turn_of(on_axis(p, A.axes[i]), freq_at(A, i), A.inverse, c, s);
+                turn_by<float>(on_axis(p, S.axis[i]), S.turn[i], A.inverse, c, s);
                 float a = to_f(x[ja]), e = to_f(x[jb]);
                 if (kMode == kNormTurnBack) {
                     const float ga = to_f(g[ja]), gb = to_f(g[jb]), da = ga * c + gb * s, db = gb * c - ga * s;
