@@ -218,13 +218,14 @@ __device__ __forceinline__ uint2 fraction_of(double freq) {
     return make_uint2((uint32_t)f, (uint32_t)(f >> 32));
 }
 
-// What a CTA keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its
-// axis, and the weights of both norms.
-template <int kParts> struct HeadTables {          // 0 parts: no weights, 1: of one operand, 2: of both
+// What a CTA keeps for its tokens: every pair's turn for one position as a fraction of 2^64, its axis, and the weights of both
+// norms, which are read as vectors of up to eight.
+template <int kParts> struct alignas(32) HeadTables {          // 0 parts: no weights, 1: of one operand, 2: of both
     uint2 turn[kMaxHeadDim / 2];
     int32_t axis[kMaxHeadDim / 2];
     float w[kParts > 0 ? kParts : 1][kParts > 0 ? kMaxHeadDim : 1];
 };
+static_assert(alignof(HeadTables<2>) % alignof(Vec<float, 8>) == 0 && offsetof(HeadTables<2>, w) % alignof(Vec<float, 8>) == 0, "weights are read as whole vectors");
 
 template <typename T, int kParts>
 __device__ __forceinline__ void fill_tables(const HeadArgs& A, HeadTables<kParts>& S, int first) {
