@@ -130,9 +130,8 @@ __device__ __forceinline__ Rgb mix_single(const uint8_t* at, float f) {
 enum { kPlain, kFree, kEnd };
 template <int kHow> struct How { static constexpr int value = kHow; };
 
-// One or two columns of a source row, mixed; two at a time in every instruction.
-template <int kCols> struct Mixed { F2 c[3]; };
-template <> struct Mixed<1> { float c[3]; };
+// Two columns of a source row, mixed; both in every instruction.
+struct Mixed { F2 c[3]; };
 
 // The words that two neighbouring columns lie in: the left one's six bytes begin at `sh` bits into the first, the right
 // one's 0, 3 or 6 bytes further on.
@@ -158,12 +157,12 @@ __device__ __forceinline__ Words words_at(const uint8_t* at, bool wide, const En
     return r;
 }
 template <int kHow>
-__device__ __forceinline__ Mixed<2> mix_words(const Words& w, uint32_t own, bool wide, uint32_t shift, F2 f) {
+__device__ __forceinline__ Mixed mix_words(const Words& w, uint32_t own, bool wide, uint32_t shift, F2 f) {
     const uint32_t sh = kHow == kPlain ? own : w.sh;
     const uint32_t x0 = __funnelshift_r(w.w0, w.w1, sh), x1 = __funnelshift_r(w.w1, w.w2, sh), x2 = __funnelshift_r(w.w2, w.w3, sh);
     const uint32_t a = kHow != kPlain && wide ? x1 : x0, b = kHow != kPlain && wide ? x2 : x1, y0 = __funnelshift_r(a, b, shift), y1 = __funnelshift_r(b, x2, shift);
     const F2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f), down = pack2(-kUp, -kUp);
-    Mixed<2> r;
+    Mixed r;
 #pragma unroll
     for (int c = 0; c < 3; ++c) {
         const F2 left = pack2(byte_up(x0, c), byte_up(y0, c)), right = c == 0 ? pack2(byte_up(x0, 3), byte_up(y0, 3)) : pack2(byte_up(x1, c - 1), byte_up(y1, c - 1));
@@ -251,7 +250,7 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
             auto walk = [&](auto how, const uint8_t* from, uint32_t own_shift, bool wide, uint32_t shift, bool mirror, const End& end) {
                 constexpr int kHow = decltype(how)::value;
                 uint32_t top_at = ~0u, low_at = ~0u;
-                auto step = [&](Mixed<2>& top, Mixed<2>& low, const Words& now, Words& next, T* to, const uint4& r, const uint4& after) {
+                auto step = [&](Mixed& top, Mixed& low, const Words& now, Words& next, T* to, const uint4& r, const uint4& after) {
                     next = words_at<kHow>(from + after.y, wide, end);
                     if (r.x != low_at) top = r.x == top_at ? low : mix_words<kHow>(words_at<kHow>(from + r.x, wide, end), own_shift, wide, shift, f);
                     low = mix_words<kHow>(now, own_shift, wide, shift, f);
@@ -266,7 +265,7 @@ __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const
                         put_two(to + c * area, a, b, kHow != kPlain && mirror);
                     }
                 };
-                Mixed<2> u = {}, v = {};
+                Mixed u = {}, v = {};
                 Words even = words_at<kHow>(from + rows[0].y, wide, end), odd;
 #pragma unroll 1
                 for (int dy = 0; dy < p; dy += 2, o += 2 * p, rows += 2) {
@@ -409,15 +408,14 @@ __device__ __forceinline__ void sums_before(int64_t& tokens, int64_t& extent, bo
     __syncthreads();                                                      // the arrays may be used again
 }
 
-// Goes over this thread's share of the segments; put(i, first token, first position) is called for each.  A sequence's end
-// is written to A.next where `ends` is set.
+// Goes over this thread's share of the segments; put(i, first token, first position) is called for each.  Sequences' ends are
+// written to A.next.
 template <typename Put>
-__device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool ends, Put put) {
+__device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, Put put) {
     const int tid = threadIdx.x, n = A.n_segments, each = (int)(((int64_t)n + kScanThreads - 1) / kScanThreads);
     const int a = (int)min((int64_t)tid * each, (int64_t)n), b = (int)min((int64_t)a + each, (int64_t)n);
     const int32_t before = a > 0 && a < n ? A.segments[a - 1].w : -1;
-    if (ends)
-        for (int i = tid; i < A.n_sequences; i += kScanThreads) A.next[i] = 0;
+    for (int i = tid; i < A.n_sequences; i += kScanThreads) A.next[i] = 0;
     int64_t tokens = 0, extent = 0, total;
     bool first = false;
     for (int i = a, seq = before; i < b; ++i) {
@@ -437,7 +435,7 @@ __device__ __forceinline__ int64_t walk_segments(const PositionArgs& A, bool end
         seq = s.w;
         put(i, tokens, (int32_t)extent);
         tokens += c; extent += e;
-        if (ends && (i + 1 == n || A.segments[i + 1].w != s.w) && s.w >= 0 && s.w < A.n_sequences) A.next[s.w] = (int32_t)extent;
+        if ((i + 1 == n || A.segments[i + 1].w != s.w) && s.w >= 0 && s.w < A.n_sequences) A.next[s.w] = (int32_t)extent;
     }
     return total;
 }
@@ -535,7 +533,7 @@ __global__ void __launch_bounds__(kScanThreads) positions_kernel(const __grid_co
 // More segments: one CTA writes where each begins to device memory, then a thread a token looks its segment up there.  The one
 // CTA's walk over the segments bounds it (most of 39 us for 16385 segments); so many segments in one call are rare.
 __global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __grid_constant__ PositionArgs A) {
-    const int64_t total = walk_segments(A, true, [&](int i, int64_t token, int32_t position) { A.starts[i] = token; A.bases[i] = position; });
+    const int64_t total = walk_segments(A, [&](int i, int64_t token, int32_t position) { A.starts[i] = token; A.bases[i] = position; });
     if (threadIdx.x == 0) A.starts[A.n_segments] = total;
 }
 
