@@ -263,7 +263,8 @@ typedef struct {
     const void* x;                 /* input                                                            */
     void* y;                       /* output; backward: the gradient of x.  x itself (or dy itself) with the
                                       same strides, or memory that shares nothing with any operand, table
-                                      or other output: else the call is refused                        */
+                                      or other output: else the call is refused (as are layouts so entangled
+                                      that a bounded search cannot tell)                               */
     const void* dy;                /* backward: the gradient of the forward's output                   */
     const void* weight;            /* norm: head_dim weights; NULL = ones                              */
     void* dweight;                 /* backward: gradient of weight, same type; NULL = not wanted.  Apart

@@ -3,20 +3,32 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
 #include <utility>
 
 namespace pcr {
 
-// Rows of `bytes` bytes from `at` on, `n[i]` of them `step[i]` bytes apart on each of three axes.
+// Rows of `bytes` bytes from `at` on, `n[i]` of them `step[i]` bytes apart on each of three axes; all of them lie in from .. to
+// (to = from: there are none).
 struct Span {
     uintptr_t at;
-    int64_t bytes;
-    __int128 step[3];
-    int64_t n[3];
+    int64_t bytes, n[3];
+    __int128 step[3], from, to;
+    bool behind(const Span& s) const { return from >= s.to; }
 };
-inline Span span_of(const void* p, size_t bytes) { return {reinterpret_cast<uintptr_t>(p), (int64_t)bytes, {0, 0, 0}, {1, 1, 1}}; }
+inline Span span_of(const void* p, size_t bytes) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return {at, (int64_t)bytes, {1, 1, 1}, {0, 0, 0}, (__int128)at, (__int128)at + bytes};
+}
 inline Span span_of(const void* p, const int64_t (&stride)[3], int64_t n0, int64_t n1, int64_t n2, int64_t row, size_t es) {
-    return {reinterpret_cast<uintptr_t>(p), row * (int64_t)es, {(__int128)stride[0] * (int64_t)es, (__int128)stride[1] * (int64_t)es, (__int128)stride[2] * (int64_t)es}, {n0, n1, n2}};
+    Span s = span_of(p, row * es);
+    const int64_t n[3] = {n0, n1, n2};
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] < 1) { s.to = s.from = 0; return s; }
+        s.n[i] = n[i]; s.step[i] = (__int128)stride[i] * (int64_t)es;
+        (s.step[i] < 0 ? s.from : s.to) += s.step[i] * (n[i] - 1);
+    }
+    return s;
 }
 
 // Whether sum of c[i] z[i] lies in lo .. hi for some 0 <= z[i] < n[i], i >= k.  `reach`: the largest sum of the terms from each
@@ -35,24 +47,14 @@ inline bool sum_within(const __int128* c, const __int128* n, const __int128* rea
 
 // Whether two spans have a byte in common.  (Spans so entangled that some ten thousand steps do not tell count as if they had.)
 inline bool share_memory(const Span& a, const Span& b) {
-    if (a.bytes <= 0 || b.bytes <= 0) return false;
-    __int128 c[6], n[6], reach[7], from[2], to[2];
+    if (a.behind(b) || b.behind(a) || a.from == a.to || b.from == b.to) return false;         // (as a rule)
+    __int128 c[6], n[6], reach[7];
     int terms = 0;
-    const Span* of[2] = {&a, &b};
-    for (int s = 0; s < 2; ++s) {
-        from[s] = of[s]->at; to[s] = from[s] + of[s]->bytes;
-        for (int i = 0; i < 3; ++i) {
-            if (of[s]->n[i] < 1) return false;
-            const __int128 step = of[s]->step[i], far = step * (of[s]->n[i] - 1);
-            if (far < 0) from[s] += far; else to[s] += far;
-            if (far == 0) continue;
-            c[terms] = step < 0 ? -step : step; n[terms++] = of[s]->n[i];
-        }
-    }
-    if (to[0] <= from[1] || to[1] <= from[0]) return false;
-    // A row of a begins at from[0] + u, one of b at to[1] - b.bytes - v, u and v sums of steps: they meet where u + v lies between
-    const __int128 lo = to[1] - b.bytes - from[0] - a.bytes + 1,
-                   hi = to[1] - from[0] - 1;
+    for (const Span* s : {&a, &b})
+        for (int i = 0; i < 3; ++i)
+            if (s->n[i] > 1 && s->step[i] != 0) { c[terms] = s->step[i] < 0 ? -s->step[i] : s->step[i]; n[terms++] = s->n[i]; }
+    // A row of a begins at a.from + u, one of b at b.to - b.bytes - v, u and v sums of steps: they meet where u + v lies between
+    const __int128 lo = b.to - b.bytes - a.from - a.bytes + 1, hi = b.to - a.from - 1;
     for (int i = 0; i < terms; ++i)                                   // equal steps are one, the largest come first
         for (int j = i + 1; j < terms;) {
             if (c[j] == c[i]) { n[i] += n[j] - 1; --terms; c[j] = c[terms]; n[j] = n[terms]; continue; }

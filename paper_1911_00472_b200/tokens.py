@@ -39,12 +39,15 @@ _HERE = contextlib.nullcontext()
 # the handle of a device's current stream, without the object around it: a third of what a small call costs
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
+# (the operands are on a device: nothing is left to set up)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
 
 def _on(device: torch.device, stream):
     """The context in which a call allocates and launches: the operands' device, and `stream` where one is given."""
     if device.type != "cuda":
         raise ValueError("operands have to be on a CUDA device")
-    if stream is None and torch.cuda.current_device() == device.index:
+    if stream is None and _current_device() == device.index:
         return _HERE
     if stream is not None and stream.device != device:
         raise ValueError("the stream belongs to another device than the operands")
@@ -52,23 +55,24 @@ def _on(device: torch.device, stream):
 
 
 def _has_tangent(tensors) -> bool:
-    """Whether forward-mode differentiation follows one of them.  The level says at once that none is followed, as a rule."""
-    return getattr(forward_ad, "_current_level", 0) >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+    """Whether forward-mode differentiation follows one of them (asked where a level of it is entered: see _forward_mode)."""
+    return any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
-def _not_followed(*outputs):
-    """Outputs are written without autograd's knowledge: none of them may stand in its graph, or have its sign taken on reading."""
-    if any(t is not None and t.is_neg() for t in outputs):
+def _forward_mode() -> bool:
+    return getattr(forward_ad, "_current_level", 0) >= 0
+
+
+def _not_followed(out):
+    """Outputs are written without autograd's knowledge: none may stand in its graph, or have its sign taken on reading."""
+    if out.is_neg():
         raise ValueError("out must not be a negated view")
-    if (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in outputs)) or _has_tangent(outputs):
+    if (out.requires_grad and torch.is_grad_enabled()) or (_forward_mode() and _has_tangent((out,))):
         raise ValueError("autograd does not see this call: out must be detached")
 
 
-def _written(outputs):
-    """Tells autograd that a caller's tensors hold other values now: a graph that kept one of them says so when it needs it."""
-    for t in outputs:
-        if t is not None:
-            torch.autograd.graph.increment_version(t)
+# tells autograd that a caller's tensors hold other values now: a graph that kept one of them says so when it needs it
+_written = torch.autograd.graph.increment_version
 
 
 def _same_device(device, *tensors):
@@ -81,31 +85,35 @@ def _same_device(device, *tensors):
 
 
 def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
-    """What the calls ask of their operands; returns (batch, tokens, size, type of the weights).  One look at each property:
-    small calls take as long as the host does."""
+    """What the calls ask of their operands; returns (batch, tokens, size, heads of queries and of keys, positions' axes, pairs, type
+    of the weights, whether an operand's sign is taken on reading).  One look at each property: small calls take as long as the
+    host does."""
     shape, dtype, device = q.shape, q.dtype, q.get_device()
+    k_heads = 0
     if len(shape) == 4:
-        batch, tokens, _, size = shape
+        batch, tokens, q_heads, size = shape
     elif len(shape) == 3:
-        batch, (tokens, _, size) = 1, shape
+        batch, (tokens, q_heads, size) = 1, shape
     else:
-        batch = tokens = size = None
+        batch = tokens = q_heads = size = None
     if size is None or dtype not in _CODES:
         raise ValueError("queries must be (tokens, heads, size) or (batch, tokens, heads, size) of float16, bfloat16 or float32")
     if k is not None:
         other = k.shape
         if len(other) != len(shape) or other[-3] != tokens or other[-1] != size or other[0] != shape[0] or k.dtype != dtype:
             raise ValueError("k must have the tokens, head size and dtype of the queries")
+        k_heads = other[-2]
     other = positions.shape
     if len(other) != len(shape) - 1 or other[-1] != tokens or other[1] != shape[0] or positions.dtype != torch.int32:
         raise ValueError("positions must be int32 with shape (axes, *tokens)")
-    other = inv_freq.shape
+    n_axes, other = other[0], inv_freq.shape
     if len(other) != 1 or inv_freq.dtype not in _FREQ_CODES or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be a contiguous float32 or float64 vector")
     if axes.shape != other or axes.dtype != torch.int32 or not axes.is_contiguous():
         raise ValueError("axes must be a contiguous int32 vector as long as inv_freq")
     near = device == positions.get_device() == inv_freq.get_device() == axes.get_device() and (k is None or k.get_device() == device)
     followed = q.requires_grad or inv_freq.requires_grad or (k is not None and k.requires_grad)
+    negated = q.is_neg() or inv_freq.is_neg() or (k is not None and k.is_neg())
     weight = dtype
     if q_weight is not None or k_weight is not None:
         weight = (k_weight if q_weight is None else q_weight).dtype
@@ -115,6 +123,7 @@ def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
                     raise ValueError("weights must be contiguous vectors of the head size, of the operands' type or float32, both alike")
                 near = near and w.get_device() == device
                 followed = followed or w.requires_grad
+                negated = negated or w.is_neg()
         if k is None and k_weight is not None:
             raise ValueError("k_weight without keys")
     for g, x in zip(grads, (q, k)):
@@ -123,11 +132,12 @@ def _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads):
         if g is not None:
             near = near and g.get_device() == device
             followed = followed or g.requires_grad
+            negated = negated or g.is_neg()
     if not near:
         raise ValueError("all operands have to be on one device")
-    if (followed and torch.is_grad_enabled()) or _has_tangent((q, k, inv_freq, q_weight, k_weight, *grads)):
+    if (followed and torch.is_grad_enabled()) or (_forward_mode() and _has_tangent((q, k, inv_freq, q_weight, k_weight, *grads))):
         raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
-    return batch, tokens, size, weight
+    return batch, tokens, size, q_heads, k_heads, n_axes, other[0], weight, negated
 
 
 def _like(t):
@@ -138,6 +148,7 @@ def _like(t):
 def _outputs(q, k, out):
     if out is None:
         return _like(q), None if k is None else _like(k)
+    device = q.get_device()
     for o, x in zip(out, (q, k), strict=True):
         if (o is None) != (x is None):
             raise ValueError("out must have an output for each operand")
@@ -146,23 +157,23 @@ def _outputs(q, k, out):
                 raise ValueError("out must have the shapes and the dtype of the operands")
             if o.shape[-1] > 1 and o.stride(-1) != 1:
                 raise ValueError("the elements of a head of out must stand side by side")
-            _same_device(q.device, o)
-    _not_followed(*out)
+            if o.get_device() != device:
+                raise ValueError("all operands have to be on one device")
+            _not_followed(o)
     return out
 
 
 def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, interleaved, inverse, eps, out, stream):
     """Checks, allocates, packs a pcr_turn_args and makes the call `name`; returns its outputs (and the weights' gradients)."""
-    batch, tokens, size, weight = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads)
+    batch, tokens, size, q_heads, k_heads, n_axes, pairs, weight, negated = _check(q, k, positions, inv_freq, axes, q_weight, k_weight, grads)
     device = q.get_device()
     if device < 0:
         raise ValueError("operands have to be on a CUDA device")
-    if stream is not None or torch.cuda.current_device() != device:
+    if stream is not None or _current_device() != device:
         with _on(q.device, stream):
             return _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, interleaved, inverse, eps, out, None)
-    held = (q, k, q_weight, k_weight, inv_freq, *grads)
-    if any(t is not None and t.is_neg() for t in held):  # their memory holds the other sign
-        q_, k_, wq_, wk_, freq_, *grads_ = (None if t is None else t.resolve_neg() for t in held)
+    if negated:                                          # their memory holds the other sign
+        q_, k_, wq_, wk_, freq_, *grads_ = (None if t is None else t.resolve_neg() for t in (q, k, q_weight, k_weight, inv_freq, *grads))
         return _call(name, q_, k_, tuple(grads_), wq_, wk_, positions, freq_, axes, interleaved, inverse, eps, out, None)
     y, z = _outputs(q, k, out)
     dwq = dwk = None
@@ -171,7 +182,7 @@ def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, inte
     if grads and k_weight is not None:
         dwk = torch.empty_like(k_weight)
     parts, copies = [], []                               # (copies live until the call is made: others must not get their memory before)
-    for x, o, g, w, dw in ((q, y, grads[0] if grads else None, q_weight, dwq), (k, z, grads[1] if grads else None, k_weight, dwk)):
+    for x, o, g, w, dw, heads in ((q, y, grads[0] if grads else None, q_weight, dwq, q_heads), (k, z, grads[1] if grads else None, k_weight, dwk, k_heads)):
         if x is None:
             parts += _NO_HEADS
             continue
@@ -191,10 +202,10 @@ def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, inte
         ys = o.stride()
         if len(xs) == 3:
             xs, ys, gs = (0, *xs), (0, *ys), (0, *gs)
-        parts += (x.data_ptr(), o.data_ptr(), g_at, 0 if w is None else w.data_ptr(), 0 if dw is None else dw.data_ptr(), *xs[:3], *ys[:3], *gs[:3], x.shape[-2], 0)
+        parts += (x.data_ptr(), o.data_ptr(), g_at, 0 if w is None else w.data_ptr(), 0 if dw is None else dw.data_ptr(), *xs[:3], *ys[:3], *gs[:3], heads, 0)
     ps = positions.stride()
     args = _TURN_ARGS.pack(*parts, positions.data_ptr(), *(ps if len(ps) == 3 else (ps[0], 0, ps[1])), inv_freq.data_ptr(), axes.data_ptr(), batch, tokens,
-                           positions.shape[0], size, 2 * inv_freq.shape[0], bool(interleaved), bool(inverse), _CODES[q.dtype], _FREQ_CODES[inv_freq.dtype],
+                           n_axes, size, 2 * pairs, bool(interleaved), bool(inverse), _CODES[q.dtype], _FREQ_CODES[inv_freq.dtype],
                            _CODES[weight], eps, 0)
     L = B.lib()
     if grads:
@@ -203,7 +214,7 @@ def _call(name, q, k, grads, q_weight, k_weight, positions, inv_freq, axes, inte
     else:
         B._chk(getattr(L, name)(args, _raw_stream(device)), name)
     if out is not None:
-        _written(out)
+        _written((y,) if z is None else (y, z))
     return (y, z, dwq, dwk) if grads else (y, z)
 
 
@@ -301,7 +312,8 @@ def token_positions(segments, n_tokens, n_sequences, *, merge=1, time_step=1, re
         B._chk(L.pcr_token_positions(segments.data_ptr(), segments.shape[0], n_tokens, n_sequences, merge, time_step, flags, out.data_ptr(),
                                      out.stride(0), after.data_ptr(), scratch.data_ptr(), _raw_stream(segments.device.index)),
                "pcr_token_positions")
-    _written((given,))
+    if given is not None:
+        _written(given)
     return out, after
 
 
@@ -331,7 +343,8 @@ def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.b
     if out is not None and (out.shape != shape or out.dtype != dtype or not out.is_contiguous()):
         raise ValueError("out must be contiguous, (n_tokens, 3 * patch * patch) of dtype")
     _same_device(rgb.device, images, index, out)
-    _not_followed(out)
+    if out is not None:
+        _not_followed(out)
     given = out
     with _on(rgb.device, stream):
         if out is None:
@@ -339,7 +352,8 @@ def patch_tokens(rgb, images, index, patch, mean, std, *, merge=1, dtype=torch.b
         B._chk(B.lib().pcr_patch_tokens(rgb.data_ptr(), rgb.numel(), images.data_ptr(), images.shape[0], index.data_ptr(), shape[0], patch,
                                         merge, struct.pack("3f", *mean), struct.pack("3f", *std), _CODES[dtype], out.data_ptr(),
                                         _raw_stream(rgb.device.index)), "pcr_patch_tokens")
-    _written((given,))
+    if given is not None:
+        _written(given)
     return out
 
 

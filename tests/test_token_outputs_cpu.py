@@ -18,13 +18,11 @@ CSRC = os.path.join(os.path.dirname(paper_1911_00472_b200.__file__), "csrc")
 SHIM = r"""
 #include "pcr_spans.h"
 extern "C" int shared(const int64_t* a, const int64_t* b) {       // address, bytes, three steps, three counts
-    pcr::Span s[2];
-    const int64_t* of[2] = {a, b};
-    for (int i = 0; i < 2; ++i) {
-        s[i].at = (uintptr_t)of[i][0]; s[i].bytes = of[i][1];
-        for (int j = 0; j < 3; ++j) { s[i].step[j] = of[i][2 + j]; s[i].n[j] = of[i][5 + j]; }
-    }
-    return pcr::share_memory(s[0], s[1]);
+    auto span = [](const int64_t* s) {
+        const int64_t step[3] = {s[2], s[3], s[4]};
+        return pcr::span_of((const void*)s[0], step, s[5], s[6], s[7], s[1], 1);
+    };
+    return pcr::share_memory(span(a), span(b));
 }
 """
 
