@@ -294,9 +294,12 @@ typedef struct {
 
 /* Rotation of queries and keys, one launch: pair (a, b) becomes (a cos - b sin, a sin + b cos) with the
  * angle positions[axes[i]] * inv_freq[i], whose whole turns are taken off in 64 bits (far positions
- * lose nothing); single precision from there, one rounding to dtype.  Any strides and
- * alignments of whole elements; in place is allowed.  Rows that stand on 16-byte boundaries in heads of
- * a multiple of 16 (16 bits) or 8 (32 bits) elements are fastest, rows at odd elements slowest.
+ * lose nothing, for frequencies up to 2^40); single precision from there, one rounding to dtype.  Any
+ * strides and alignments of whole elements; in place is allowed.  Rows are read in vectors of 16, 8 or 4
+ * bytes (32 bits: 16 or 8): the longest on which all rows stand and of which head_dim and rot_dim are
+ * twice a whole number, at most 64 to a row.  Where there are none (rows at odd elements, sizes that are
+ * no multiple of 4, heads of more than 256 elements in 32 bits) values go one by one, 2 to 8 times as
+ * long.
  * Errors: PCR_E_ARG (also for an output that overlaps itself, another output or an operand that is not
  * its own), PCR_E_CUDA. */
 int pcr_rotate(const pcr_turn_args* args, void* stream);

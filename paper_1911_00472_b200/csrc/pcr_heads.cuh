@@ -1,7 +1,7 @@
 // Queries and keys turned by the positions of their tokens, with or without a root-mean-square norm of every head in
 // front, and the backward pass of both together.
 //
-//   angle_i = position[axis_i] * inv_freq_i                    (64 bits: the position may lie millions of turns away)
+//   angle_i = position[axis_i] * inv_freq_i                    (whole turns go in 64 bits: the position may lie millions of them away)
 //   turned: (a, b) -> (a cos - b sin, a sin + b cos) for the pairs (i, i + rot/2) or (2 i, 2 i + 1), i < rot/2
 //   forward, norm:  y = turn(w * x * r),  r = 1 / sqrt(mean(x^2) + eps)
 //   backward:       d = turn back(g),  u = x * r,  dx = r * (d * w - u * mean(d * w * u)),  dw = sum over rows of d * u
@@ -11,10 +11,10 @@
 // rows never leave the registers), and a thread goes over several heads of ONE token, so that cosine and sine are worked out
 // once for all of them.
 //
-// Measured on a B200 (6461 GB/s copied): norm and rotation of 32768 tokens, 32 + 8 heads of 128, bf16: 117 us, 5.7 TB/s, 89 % of
+// Measured on a B200 (6567 GB/s copied): norm and rotation of 32768 tokens, 32 + 8 heads of 128, bf16: 117 us, 5.7 TB/s, 88 % of
 // the copy rate; rotation of 8191 tokens out of a packed projection, fp16: 34 us, 4.9 TB/s (1.7 rounds of CTAs, the rest is
 // their end); rotation of 12003 tokens, 32 heads of 80, fp32: 43 us, 5.7 TB/s.  Backward of 8192 tokens, 40 heads of 128, bf16:
-// 53 us, 4.8 TB/s; of 16384 tokens, 32 heads of 72, bf16: 55.7 us, 4.1 TB/s.
+// 50 us, 5.1 TB/s, fp32: 84 us, 6.0 TB/s; of 16384 tokens, 32 heads of 72, bf16: 56.5 us, 4.0 TB/s.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -345,9 +345,10 @@ constexpr int kRowsAhead = 4;
 // thread `per` heads of its token, kAhead of them at a time.  Lanes without a token go along with the last one's data and
 // store nothing: no shuffle and no load stands in a branch.
 // HBM bounds it (32768 tokens, 40 heads of 128, bf16: DRAM 72 % busy, instructions issued in 36 % of the cycles, 7.8 of 12 stalled
-// warps wait for loads).  Four rows ahead and five CTAs an SM: two ahead take 123 us in the place of 116, six CTAs (registers
-// spilled) 127; rows handed on in registers while the next are on their way 128 to 160; a loop over tokens in a CTA, whose
-// tables then serve longer, 140.
+// warps wait for loads).  Four rows ahead and five CTAs an SM: two ahead take 123 us in the place of 116, six CTAs 127; rows handed
+// on in registers while the next are on their way 128 to 160; a loop over tokens in a CTA, whose tables then serve longer, 140.
+// With 16-byte vectors registers are spilled all the same: 228 bytes a thread at five CTAs with the norm in 16 bits (12 to 72 in
+// 32), 64 to 72 at the rotation's six (20 to 48 in 32); shorter vectors spill nothing.
 template <typename T, int V, bool kNorm, bool kNext>
 __global__ void __launch_bounds__(kHeadThreads, kNorm ? 5 : 6) heads_kernel(const __grid_constant__ HeadArgs A) {
     constexpr int kWarps = kHeadThreads / 32, kAhead = kRowsAhead, N = V / 2;

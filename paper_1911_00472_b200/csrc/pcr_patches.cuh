@@ -193,8 +193,9 @@ __device__ __forceinline__ void put_two(__nv_bfloat16* to, float a, float b, boo
 // what a token costs once (its entry, image and taps: a third of the instructions at patches of 14) is kept in 32 bits and
 // without divisions.  Looking up 32 tokens at once in shared memory (457 us) or keeping an image for several rounds of a warp
 // (560 to 620 in the place of 568) was slower: fewer warps fit.
-// Measured: 1024 images of 256 to 496 pixels a side to patches of 14, 16 bits: 405 us, 3.3 TB/s of what has to move; 96 crops of
-// images of 600 x 450 to patches of 16, 32 bits: 43 us, 4.6 TB/s; 768 patches of 4 small images: 6 us.
+// Measured: 1024 images of 256 to 496 pixels a side to patches of 14, 16 bits: 398 us, 3.4 TB/s of what has to move; of 16: 334 us, in
+// 32 bits 360 (6.0 TB/s); of 13, 15 and 17 (one column a lane): 730, 616 and 1016 us.  96 crops of images of 600 x 450 to patches
+// of 16, 32 bits: 41.5 us, 4.8 TB/s; 768 patches of 4 small images: 6 us.
 template <typename T, int kCols, bool kDirect>
 __global__ void __launch_bounds__(32 * kPatchWarps, 8) patch_tokens_kernel(const __grid_constant__ PatchArgs A) {
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -531,7 +532,8 @@ __global__ void __launch_bounds__(kScanThreads) positions_kernel(const __grid_co
 }
 
 // More segments: one CTA writes where each begins to device memory, then a thread a token looks its segment up there.  The one
-// CTA's walk over the segments bounds it (most of 39 us for 16385 segments); so many segments in one call are rare.
+// CTA's walk over the segments bounds it (most of 39 us for 16385 segments of 5 tokens, 45 of 50; 285 us for 100000); so many
+// segments in one call are rare.
 __global__ void __launch_bounds__(kScanThreads) position_scan_kernel(const __grid_constant__ PositionArgs A) {
     const int64_t total = walk_segments(A, [&](int i, int64_t token, int32_t position) { A.starts[i] = token; A.bases[i] = position; });
     if (threadIdx.x == 0) A.starts[A.n_segments] = total;

@@ -91,8 +91,9 @@ struct Cut { int v, lanes, per, slots[2], rows[2]; unsigned x, y; };
 
 Cut cut_of(const pcr_turn_args& a, bool back) {
     Cut c = {};
-    // the longest vectors that fit: 8192 tokens, 40 heads of 128, bf16, by 16 / 8 / 4 bytes and value by value: rotation 31, 31, 34 and 101 us,
-    // norm 35, 41, 57 and 131, backward 53, 56, 72 and 396
+    // the longest vectors that fit: 8192 tokens, 40 heads of 128, bf16, by 16 / 8 / 4 bytes and value by value: rotation 29, 31, 33 and 97 us,
+    // norm 32, 39, 56 and 127, backward 50, 54, 69 and 385.  A row has 32 lanes of two vectors at most, so that heads of 32 bits
+    // beyond 256 elements go value by value: 4096 tokens, 40 heads of 256: 55, 57 and 83 us, of 264: 119, 126 and 427.
     for (int v : {8, 4, 2})
         if (c.v == 0 && v * size_of(a.dtype) <= 16 && fits(a, back, v)) c.v = v;
     c.lanes = c.v ? a.head_dim / (2 * c.v) : 32;

@@ -227,7 +227,7 @@ def rotate(q, k, positions, inv_freq, axes, *, interleaved=False, inverse=False,
     positions (n_axes, *tokens) int32, any strides (expanded batches too)
     inv_freq, axes   frequency and axis of every pair of elements (rotary_axes makes them); the first 2 * len(inv_freq)
               elements of a head are turned, the others copied
-    interleaved      pairs (2 i, 2 i + 1) in place of (i, i + size / 2)
+    interleaved      pairs (2 i, 2 i + 1) in place of (i, i + len(inv_freq))
     inverse   by the negative angle: the gradient of the forward call
     out       (q, k) to write to: each its own operand, or memory that shares nothing with any operand or with the
               other output (anything else is refused)
@@ -256,8 +256,7 @@ def rotary_axes(rot, base=10000.0, sections=None, *, interleaved_axes=False, per
     """(inv_freq, axes) of `rot` turned elements, rot / 2 pairs.
 
     sections          pairs of each axis (their sum is rot / 2); None: one axis
-    interleaved_axes  pair i belongs to axis i mod len(sections) while that axis has pairs left, otherwise the sections
-                      are runs
+    interleaved_axes  the axes take turns, one that has no pairs left is passed over; otherwise the sections are runs
     per_axis          every axis has the whole range of frequencies over its own pairs (image encoders), otherwise
                       frequency i is base ** (-2 i / rot) whatever the axis
     """
