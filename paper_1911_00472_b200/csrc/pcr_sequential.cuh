@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(32 * kSeqWarps, 4) sequential_kernel(Params P,
 // The same, one lane per restart interval, for launches of many items (see sequential_in_ctas): a warp an item instead of eight, 18
 // items an SM instead of four.  Lanes stand at different kinds of symbol in every step, so a block's first symbol goes through the same
 // instructions as the others (its value is the difference), stores are predicated, and what changes from block to block comes
-// from a small table in shared memory.  Bound by the length of a lane's chain, 600 cycles a symbol: decode of 3072 CelebA-shaped images
+// from a small table in shared memory.  Bound by the length of a lane's chain, 600 cycles a symbol: decode of three records of 1024 CelebA-shaped images each
 // 980 us, with the kernel above 1118; of 1024 480 and 411.
 // ---------------------------------------------------------------------------------------
 constexpr int kSeqLaneWarps = 2;
