@@ -317,6 +317,64 @@ int pcr_norm_rotate(const pcr_turn_args* args, void* stream);
 size_t pcr_norm_rotate_scratch_bytes(const pcr_turn_args* args);
 int pcr_norm_rotate_backward(const pcr_turn_args* args, void* scratch, void* stream);
 
+/* Linear attention whose memory of earlier tokens fades at a rate of each head's own:
+ *   S_t = f S_(t-1) + k_t v_t^T,   out_t = S_t^T q_t,   f = exp(log_decay[head]),
+ * that is out_t = sum over j <= t of f^(t-j) (q_t . k_j) v_j, sequence by sequence.  (Queries take a scale with them where one is
+ * wanted.)  Consecutive query heads share a head of keys and values, q_heads / k_heads of them; every query head has a
+ * memory of its own. */
+typedef struct {
+    const void* at;                /* DEVICE: element (b, t, h, j) at b * stride[0] + t * stride[1] + h * stride[2] + j */
+    int64_t stride[3];             /* in elements */
+} pcr_rows;
+typedef struct {
+    pcr_rows q, k, v;              /* (batch, tokens, heads, size): q_heads of k_dim, k_heads of k_dim, k_heads of v_dim */
+    pcr_rows out;                  /* q_heads of v_dim: the output; backward: its gradient, which is read       */
+    pcr_rows dq, dk, dv;           /* backward: the gradients                                                    */
+    const float* log_decay;        /* DEVICE, q_heads: at most 0; minus infinity keeps nothing                   */
+    const int32_t* starts;         /* DEVICE, sequences + 1: sequence s is the tokens starts[s] .. starts[s+1]-1 (batch 1);
+                                      ascending, values outside 0..tokens are taken as the nearest.  Rows of no
+                                      sequence are left as they are (PCR_DECAY_ZERO_TAIL: set to 0).
+                                      NULL: every batch is a sequence of `tokens` tokens                         */
+    const float* state;            /* DEVICE, (sequences, q_heads, k_dim, v_dim), 4-byte aligned: the memory with which a
+                                      sequence begins; NULL: none                                                */
+    float* state_after;            /* forward: the memory behind its last token (an empty sequence's is the one it
+                                      began with); NULL: not wanted                                              */
+    const float* dstate_after;     /* backward: its gradient; NULL: 0                                            */
+    float* dstate;                 /* backward: gradient of `state`; NULL: not wanted                            */
+    int64_t batch, tokens, sequences;   /* batch * tokens < 2^31; sequences < 2^24: of `starts`, else batch      */
+    int32_t q_heads, k_heads;      /* q_heads a multiple of k_heads, at most 65535                               */
+    int32_t k_dim, v_dim;          /* 1..256 */
+    int32_t dtype;                 /* of all rows: PCR_F16, PCR_F32, PCR_BF16                                    */
+    int32_t flags;
+} pcr_decay_args;
+#define PCR_DECAY_ZERO_TAIL 1
+
+/* The whole of every sequence, forward, and its gradients (nothing is kept from the forward pass).  Sums and memories in single
+ * precision, one rounding to dtype.
+ *   scratch : DEVICE, pcr_decay_scratch_bytes(args, backward) bytes (for the same args on the same device), 16-byte aligned,
+ *             apart from all operands and outputs.
+ * Outputs share no memory with operands, tables or one another: else PCR_E_ARG.  The same call gives the same bits.
+ * A token that is not finite reaches the outputs of the tokens behind it (backward: and the gradients before it) in its sequence, no others.
+ * Errors: PCR_E_ARG, PCR_E_CUDA. */
+size_t pcr_decay_scratch_bytes(const pcr_decay_args* args, int backward);
+int pcr_decay_attention(const pcr_decay_args* args, void* scratch, void* stream);
+int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void* stream);
+
+/* The same for one new token of each of `rows` requests: the memory is brought up to date where it lies, and read.
+ *   slots : DEVICE, rows: which memory is the request's; one outside 0 .. n_slots - 1 stands for a row of no request, whose
+ *           output is 0.  Rows of one memory are taken one after the other.  NULL: row i has memory i. */
+typedef struct {
+    const void *q, *k, *v;         /* DEVICE, (rows, heads, size) as above; element (i, h, j) at i * stride[0] + h * stride[1] + j */
+    void* out;
+    int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2];
+    float* state;                  /* DEVICE, (n_slots, q_heads, k_dim, v_dim), 4-byte aligned                    */
+    const int32_t* slots;
+    const float* log_decay;        /* DEVICE, q_heads */
+    int64_t rows, n_slots;         /* rows < 2^24, n_slots < 2^31 */
+    int32_t q_heads, k_heads, k_dim, v_dim, dtype, rsvd;
+} pcr_decay_step_args;
+int pcr_decay_step(const pcr_decay_step_args* args, void* stream);
+
 /* Chroma upsampling of the decodes that follow (pcr_decode, pcr_decode_more).  The paper hands
  * its reassembled files to stock decoders (Section 5) and does not name the filter.
  *   PCR_UPSAMPLE_REPLICATE (default): pixel (x, y) takes chroma sample (x >> 1, y >> 1).

@@ -20,7 +20,8 @@ EXPORTS = ("pcr_open", "pcr_num_images", "pcr_num_groups", "pcr_get_image", "pcr
            "pcr_pixels_noalloc", "pcr_decode_more", "pcr_release_cached_memory", "pcr_decode_tensor", "pcr_msssim", "pcr_msssim_scratch_bytes", "pcr_set_upsampling",
            "pcr_selftest_bounded_wait", "pcr_get_sampling", "pcr_set_record_cache", "pcr_get_images",
            "pcr_patch_tokens", "pcr_token_positions", "pcr_token_positions_scratch_bytes", "pcr_rotate", "pcr_norm_rotate",
-           "pcr_norm_rotate_backward", "pcr_norm_rotate_scratch_bytes")
+           "pcr_norm_rotate_backward", "pcr_norm_rotate_scratch_bytes", "pcr_decay_scratch_bytes", "pcr_decay_attention",
+           "pcr_decay_attention_backward", "pcr_decay_step")
 
 
 class ImageInfo(C.Structure):
@@ -90,6 +91,11 @@ def lib():
         L.pcr_norm_rotate_scratch_bytes.restype = C.c_size_t
         L.pcr_norm_rotate_scratch_bytes.argtypes = [C.c_char_p]
         L.pcr_norm_rotate_backward.argtypes = [C.c_char_p, vp, vp]
+        L.pcr_decay_scratch_bytes.restype = C.c_size_t
+        L.pcr_decay_scratch_bytes.argtypes = [C.c_char_p, C.c_int]         # (a pcr_decay_args, packed by the caller)
+        L.pcr_decay_attention.argtypes = [C.c_char_p, vp, vp]
+        L.pcr_decay_attention_backward.argtypes = [C.c_char_p, vp, vp]
+        L.pcr_decay_step.argtypes = [C.c_char_p, vp]                       # (a pcr_decay_step_args)
         L.pcr_launch_count.restype = C.c_uint64
         L.pcr_launch_count.argtypes = []
         L.pcr_strerror.restype = C.c_char_p
@@ -160,6 +166,7 @@ def pcr_decode_more(handle: int, k: int, out_dev_ptr: int, stream: int = 0) -> N
 
 PCR_F16, PCR_F32, PCR_BF16, PCR_F64 = 0, 1, 2, 3
 PCR_POSITIONS_RESTART, PCR_POSITIONS_ZERO_TAIL = 1, 2
+PCR_DECAY_ZERO_TAIL = 1
 
 
 def pcr_decode_tensor(handle: int, k: int, crops_host_ptr: int, size: int, mean_host_ptr: int, std_host_ptr: int,

@@ -1,0 +1,419 @@
+// Linear attention whose memory fades at a rate of each head's own (see include/pcr.h).
+//
+//   S_t = f S_(t-1) + k_t v_t^T,   o_t = S_t^T q_t,   f = exp(log_decay)
+//
+// written out: o_t = sum over j <= t of f^(t-j) (q_t . k_j) v_j.  All three gradients are sums of the same form over other
+// operands, so that one kernel, a walk, does the forward and the backward pass:
+//
+//   y_t = sum over j of f^|t-j| (a_t . b_j) c_j      j <= t: out (a, b, c = q, k, v), dq (dout, v, k)
+//                                                    j >= t: dk (v, dout, q), dv (k, q, dout)
+//
+// A walk goes over a sequence in chunks.  Within a chunk the sum is a product of two matrices, (A B^T, faded and masked) C; what
+// lies before comes out of the memory R = sum f^(...) b_j c_j^T, which every chunk brings up to date.  Long sequences are cut into
+// segments that CTAs take side by side: a first launch works out what each segment adds to the memory (`states`), a
+// second adds those up along the sequence, and the walk proper begins each segment with the memory before it.
+//
+// "Before" and "along" are meant in the direction of the walk (`rev`: from the last token to the first); segments are cut from
+// the end at which it begins, so that all but a sequence's last one are whole.  R is kept aged: what R holds counts with f^0 for the
+// nearest token of the next chunk.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace pcr {
+
+constexpr int kMaxDecayDim = 256;              // of a head, keys and values
+constexpr int kWalkThreads = 256;
+constexpr int kWalkCols = 64;                  // columns of c (and of R) of a CTA of the plain kernel
+
+struct WalkRows { const void* at; int64_t st[3]; int group; };       // batch, token, head; `group` heads of the walk share one of these
+
+struct Walk {
+    WalkRows a, b, c;
+    void* y;
+    int64_t ys[3];
+    const float* first;                        // the memory before: element (i, j) of (sequence, head) at (...) bd cd + i fi + j fj
+    float* last;                               // the memory behind the last token
+    float* slots;                              // memories of segments: element (i, j) of (slot, head) at (...) bd cd + i si + j sj
+    int64_t fi, fj, li, lj, si, sj;
+    int bd, cd;                                // size of a's and b's heads, and of c's and y's
+    int rev, y32, zero_tail;                   // y32: y is in 32 bits whatever the operands are
+};
+
+struct WalkArgs {
+    Walk w[3];
+    const float* log_decay;
+    const int32_t* starts;                     // sequences + 1, or null: every batch is one of `tokens`
+    uint32_t sequences, tokens, seg;           // tokens of a segment: a multiple of the chunk
+    int heads, kinds, states, split;           // states: only what segments add; split: sequences may have several segments
+};
+
+template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
+template <typename T> __device__ __forceinline__ T from_float(float v) { return (T)v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// log2 of a head's factor; one of 0 (log_decay of minus infinity) is taken as 2^-15000, so that its power 0 is 1
+__device__ __forceinline__ float rate_of(const float* log_decay, int head) {
+    const float r = log_decay[head] * 1.4426950408889634f;
+    return r < -15000.f ? -15000.f : r;
+}
+__device__ __forceinline__ float power(float rate, int n) { return exp2f(rate * (float)n); }
+
+// What a CTA is to do: segment m of a sequence.  `begin`, `len`: the sequence in memory; `from`, `n`: the segment, counted from where
+// the walk begins.
+struct Item { int batch, seq, m, begin, len, from, n, slot; bool last; };
+
+// Where sequence i of those in the walk's order begins, counted in its direction.  Values outside 0 .. tokens are taken as the nearest.
+__device__ __forceinline__ int64_t start_of(const WalkArgs& A, int rev, uint32_t i) {
+    const int32_t v = __ldg(A.starts + (rev ? A.sequences - i : i));
+    const int64_t t = min(max((int64_t)v, (int64_t)0), (int64_t)A.tokens);
+    return rev ? (int64_t)A.tokens - t : t;
+}
+
+// Segments are numbered without gaps that could not be found again: segment m of sequence s, which begins at b, has the key
+// s + floor((b + m seg) / seg) = s + floor(b / seg) + m, and keys grow from each segment to the next.  Called by whole warps.
+__device__ __forceinline__ bool item_of(const WalkArgs& A, int rev, uint32_t key, Item& it) {
+    const int seg = (int)A.seg;
+    if (!A.starts) {
+        const uint32_t per = max(1u, (A.tokens + A.seg - 1) / A.seg);
+        it.batch = it.seq = (int)(key / per);
+        it.m = (int)(key - (uint32_t)it.seq * per);
+        it.begin = 0; it.len = (int)A.tokens;
+        it.slot = it.seq * (int)(per - 1) + it.m;
+    } else {
+        // the last sequence whose first key is not beyond `key`: 32 tries at a time
+        const int lane = threadIdx.x & 31;
+        uint32_t lo = 0, count = A.sequences;
+        while (count > 1) {
+            const uint32_t step = (count + 31) / 32, at = min((uint32_t)lane * step, count - 1);
+            const bool below = (uint32_t)(lo + at) + (uint64_t)start_of(A, rev, lo + at) / A.seg <= key;
+            const int n = max(1, __popc(__ballot_sync(~0u, below)));         // (lane 0 holds lo itself)
+            const uint32_t skip = min((uint32_t)(n - 1) * step, count - 1);
+            lo += skip; count = min(step, count - skip);
+        }
+        const int64_t b = start_of(A, rev, lo), e = start_of(A, rev, lo + 1);
+        const int64_t m = (int64_t)key - lo - b / seg;
+        it.len = (int)max(e - b, (int64_t)0);
+        if (m < 0 || (m > 0 && m * seg >= it.len)) return false;
+        it.m = (int)m;
+        it.seq = (int)(rev ? A.sequences - 1 - lo : lo);
+        it.batch = 0;
+        it.begin = (int)(rev ? (int64_t)A.tokens - b - it.len : b);
+        it.slot = (int)((b + m * seg) / seg);
+    }
+    it.from = it.m * seg;
+    it.n = min(seg, it.len - it.from);
+    it.last = it.from + it.n >= it.len;
+    return true;
+}
+
+// Rows that no sequence holds, in an output that has to be whole: zeros.
+__device__ __forceinline__ void zero_tail(const WalkArgs& A, const Walk& W, int es, uint32_t cta, uint32_t ctas, int head) {
+    if (!A.starts || !W.zero_tail) return;
+    const int64_t from = min(max((int64_t)__ldg(A.starts), (int64_t)0), (int64_t)A.tokens);
+    const int64_t to = max(from, min((int64_t)__ldg(A.starts + A.sequences), (int64_t)A.tokens));
+    const int64_t rows = from + (int64_t)A.tokens - to;
+    for (int64_t r = cta; r < rows; r += ctas) {
+        const int64_t at = (r < from ? r : r - from + to) * W.ys[1] + (int64_t)head * W.ys[2];
+        for (int c = threadIdx.x; c < W.cd; c += blockDim.x) {
+            if (es == 4) static_cast<float*>(W.y)[at + c] = 0.f;
+            else static_cast<uint16_t*>(W.y)[at + c] = 0;
+        }
+    }
+}
+
+inline size_t walk_shared(int bd, int rows) {
+    const int bdp = (bd + 3) / 4 * 4;
+    return sizeof(float) * ((size_t)2 * rows * (bdp + 4) + (size_t)rows * kWalkCols + (size_t)rows * (rows + 4) + (size_t)bdp * kWalkCols + rows + 4);
+}
+
+// The plain form of a walk, in single precision from end to end: any sizes, strides and types.  256 threads, 16 x 16; a CTA has
+// 64 columns of c, a chunk has kRows tokens (64; 32 where heads of more than 128 would not leave room for them).
+template <typename T, int kRows>
+__global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constant__ WalkArgs A) {
+    extern __shared__ float4 shared4[];
+    constexpr int kPer = kRows / 16;
+    const int slices = gridDim.z / A.kinds, kind = blockIdx.z / slices, slice = blockIdx.z - kind * slices;
+    const Walk& W = A.w[kind];
+    const int head = blockIdx.y, c0 = slice * kWalkCols;
+    if (c0 >= W.cd) return;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, warp = tid >> 5, lane = tid & 31;
+    if (!A.states && slice == 0) zero_tail(A, W, W.y32 ? 4 : (int)sizeof(T), blockIdx.x, gridDim.x, head);
+    Item it;
+    if (!item_of(A, W.rev, blockIdx.x, it)) return;
+    if (A.states && it.last) return;
+
+    const int bd = W.bd, bdp = (bd + 3) / 4 * 4, ld = bdp + 4, cols = min(kWalkCols, W.cd - c0);
+    float* As = reinterpret_cast<float*>(shared4);
+    float* Bs = As + kRows * ld;
+    float* Cs = Bs + kRows * ld;
+    float* Ps = Cs + kRows * kWalkCols;
+    float* Rs = Ps + kRows * (kRows + 4);
+    float* pw = Rs + bdp * kWalkCols;                     // powers of the factor, 0 .. kRows
+    const float rate = rate_of(A.log_decay, head);
+    for (int i = tid; i <= kRows; i += kWalkThreads) pw[i] = power(rate, i);
+    {
+        const size_t of = (size_t)bd * W.cd;
+        const float* from = nullptr;
+        int64_t fi = 0, fj = 0;
+        float age = 1.f;
+        if (!A.states) {
+            if (it.m > 0) { from = W.slots + ((size_t)(it.slot - 1) * A.heads + head) * of; fi = W.si; fj = W.sj; }
+            else if (W.first) { from = W.first + ((size_t)it.seq * A.heads + head) * of; fi = W.fi; fj = W.fj; age = W.rev ? 1.f : power(rate, 1); }
+        }
+        for (int i = warp; i < bdp; i += 8)
+            for (int j = lane; j < kWalkCols; j += 32) Rs[i * kWalkCols + j] = from && i < bd && j < cols ? age * from[i * fi + (c0 + j) * fj] : 0.f;
+    }
+    const T* a = static_cast<const T*>(W.a.at) + (int64_t)it.batch * W.a.st[0] + (int64_t)(head / W.a.group) * W.a.st[2];
+    const T* b = static_cast<const T*>(W.b.at) + (int64_t)it.batch * W.b.st[0] + (int64_t)(head / W.b.group) * W.b.st[2];
+    const T* c = static_cast<const T*>(W.c.at) + (int64_t)it.batch * W.c.st[0] + (int64_t)(head / W.c.group) * W.c.st[2] + c0;
+    const int64_t y0 = (int64_t)it.batch * W.ys[0] + (int64_t)head * W.ys[2] + c0;
+
+    for (int at = it.from; at < it.from + it.n; at += kRows) {
+        const int n = min(kRows, it.from + it.n - at);
+        const int64_t t0 = it.begin + (W.rev ? it.len - at - n : at);
+        const bool final = it.last && at + n >= it.len && !W.rev;         // forward, the memory that is given out is not aged
+        __syncthreads();                                                   // the chunk before is done with
+        for (int r = warp; r < kRows; r += 8) {
+            const bool in = r < n;
+            for (int d = lane; d < bdp; d += 32) {
+                if (!A.states) As[r * ld + d] = in && d < bd ? to_float(a[(t0 + r) * W.a.st[1] + d]) : 0.f;
+                Bs[r * ld + d] = in && d < bd ? to_float(b[(t0 + r) * W.b.st[1] + d]) : 0.f;
+            }
+            for (int d = lane; d < kWalkCols; d += 32) Cs[r * kWalkCols + d] = in && d < cols ? to_float(c[(t0 + r) * W.c.st[1] + d]) : 0.f;
+        }
+        __syncthreads();
+        if (!A.states) {
+            float s[kPer][kPer] = {};
+            for (int d = 0; d < bdp; d += 4) {
+                float4 x[kPer], z[kPer];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) x[i] = *reinterpret_cast<const float4*>(As + (ty + 16 * i) * ld + d);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) z[j] = *reinterpret_cast<const float4*>(Bs + (tx + 16 * j) * ld + d);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) s[i][j] += x[i].x * z[j].x + x[i].y * z[j].y + x[i].z * z[j].z + x[i].w * z[j].w;
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    const int r = ty + 16 * i, q = tx + 16 * j, far = W.rev ? q - r : r - q;
+                    Ps[r * (kRows + 4) + q] = far >= 0 ? s[i][j] * pw[far] : 0.f;
+                }
+            float o[kPer][4] = {};
+            for (int d = 0; d < bdp; ++d) {
+                const float4 m = *reinterpret_cast<const float4*>(Rs + d * kWalkCols + 4 * tx);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const float x = As[(ty + 16 * i) * ld + d];
+                    o[i][0] += x * m.x; o[i][1] += x * m.y; o[i][2] += x * m.z; o[i][3] += x * m.w;
+                }
+            }
+            float past[kPer][4];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = ty + 16 * i, far = W.rev ? n - 1 - r : r;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) past[i][e] = o[i][e] = o[i][e] * (r < n ? pw[far] : 0.f);
+            }
+            __syncthreads();
+            for (int q = 0; q < kRows; ++q) {
+                const float4 m = *reinterpret_cast<const float4*>(Cs + q * kWalkCols + 4 * tx);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const float x = Ps[(ty + 16 * i) * (kRows + 4) + q];
+                    o[i][0] += x * m.x; o[i][1] += x * m.y; o[i][2] += x * m.z; o[i][3] += x * m.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = ty + 16 * i;
+                if (r >= n) continue;
+                const int64_t to = y0 + (t0 + r) * W.ys[1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (4 * tx + e >= cols) continue;
+                    float v = o[i][e];
+                    if (!isfinite(v)) {                   // a masked token that is not finite leaves no trace: 0 * inf is none
+                        v = past[i][e];
+                        for (int q = W.rev ? r : 0; q <= (W.rev ? n - 1 : r); ++q) v += Ps[r * (kRows + 4) + q] * Cs[q * kWalkCols + 4 * tx + e];
+                    }
+                    if (W.y32) static_cast<float*>(W.y)[to + 4 * tx + e] = v;
+                    else static_cast<T*>(W.y)[to + 4 * tx + e] = from_float<T>(v);
+                }
+            }
+        }
+        // the memory: every thread its own elements, nobody else reads them before the next chunk
+        __syncthreads();
+        const float keep = power(rate, final ? n - 1 : n);
+        for (int i = ty; i < bdp; i += 16) {
+            float4 m = *reinterpret_cast<const float4*>(Rs + i * kWalkCols + 4 * tx);
+            m.x *= keep; m.y *= keep; m.z *= keep; m.w *= keep;
+            for (int r = 0; r < n; ++r) {
+                const float x = Bs[r * ld + i] * pw[(W.rev ? r + 1 : n - r) - (final ? 1 : 0)];
+                const float4 v = *reinterpret_cast<const float4*>(Cs + r * kWalkCols + 4 * tx);
+                m.x += x * v.x; m.y += x * v.y; m.z += x * v.z; m.w += x * v.w;
+            }
+            *reinterpret_cast<float4*>(Rs + i * kWalkCols + 4 * tx) = m;
+        }
+    }
+    __syncthreads();
+    float* out = nullptr;
+    int64_t oi = 0, oj = 0;
+    float age = 1.f;
+    const size_t of = (size_t)bd * W.cd;
+    if (A.states) { out = W.slots + ((size_t)it.slot * A.heads + head) * of; oi = W.si; oj = W.sj; }
+    else if (it.last && W.last) {
+        out = W.last + ((size_t)it.seq * A.heads + head) * of; oi = W.li; oj = W.lj;
+        if (it.len == 0) {                                // the memory as it came
+            for (int i = warp; i < bd; i += 8)
+                for (int j = lane; j < cols; j += 32)
+                    out[i * oi + (c0 + j) * oj] = W.first ? W.first[((size_t)it.seq * A.heads + head) * of + i * W.fi + (c0 + j) * W.fj] : 0.f;
+            return;
+        }
+    }
+    if (out)
+        for (int i = warp; i < bd; i += 8)
+            for (int j = lane; j < cols; j += 32) out[i * oi + (c0 + j) * oj] = age * Rs[i * kWalkCols + j];
+}
+
+// Along every sequence of more than one segment: what the segments add becomes the memory with which the next one begins.
+__global__ void __launch_bounds__(256) walk_scan_kernel(const __grid_constant__ WalkArgs A) {
+    const int blocks = gridDim.z / A.kinds, kind = blockIdx.z / blocks, block = blockIdx.z - kind * blocks;
+    const Walk& W = A.w[kind];
+    Item it;
+    if (!item_of(A, W.rev, blockIdx.x, it) || it.m != 0 || it.last) return;
+    const int head = blockIdx.y, of = W.bd * W.cd;
+    const float rate = rate_of(A.log_decay, head), keep = power(rate, (int)A.seg), age = W.rev ? 1.f : power(rate, 1);
+    const int more = (it.len - 1) / (int)A.seg;            // segments that have one behind them
+    for (int e = block * 256 + threadIdx.x; e < of; e += blocks * 256) {
+        float* p = W.slots + ((size_t)it.slot * A.heads + head) * of + e;
+        const int i = W.si >= W.sj ? e / W.cd : e % W.bd, j = W.si >= W.sj ? e % W.cd : e / W.bd;
+        float m = W.first ? age * W.first[((size_t)it.seq * A.heads + head) * of + i * W.fi + j * W.fj] : 0.f;
+#pragma unroll 8
+        for (int k = 0; k < more; ++k) {
+            m = keep * m + *p;
+            *p = m;
+            p += (size_t)A.heads * of;
+        }
+    }
+}
+
+// Gradients of keys and values that several heads share: the heads' sums, in the order of the heads.
+struct GroupSum { const float* from; void* to; int64_t ts[3]; int64_t tokens, rows; int heads, group, dim; };
+template <typename T>
+__global__ void __launch_bounds__(256) group_sum_kernel(const __grid_constant__ GroupSum G0, const __grid_constant__ GroupSum G1, const int32_t* starts, int sequences, int zero) {
+    const GroupSum& G = blockIdx.y ? G1 : G0;
+    int64_t from = 0, to = G.tokens;
+    if (starts) {                                          // rows of no sequence were not written
+        from = min(max((int64_t)starts[0], (int64_t)0), G.tokens);
+        to = max(from, min((int64_t)starts[sequences], G.tokens));
+    }
+    const int64_t n = G.rows * (G.heads / G.group) * G.dim;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
+        const int d = (int)(e % G.dim);
+        const int64_t rest = e / G.dim;
+        const int h = (int)(rest % (G.heads / G.group));
+        const int64_t row = rest / (G.heads / G.group), b = row / G.tokens, t = row - b * G.tokens;
+        const bool in = t >= from && t < to;
+        if (!in && !zero) continue;
+        float sum = 0.f;
+        if (in)
+            for (int g = 0; g < G.group; ++g) sum += G.from[(row * G.heads + h * G.group + g) * G.dim + d];
+        static_cast<T*>(G.to)[b * G.ts[0] + t * G.ts[1] + h * G.ts[2] + d] = from_float<T>(sum);
+    }
+}
+
+// ---- one token of each request ---------------------------------------------------------------------------------------------
+
+struct StepArgs {
+    const void *q, *k, *v;
+    void* out;
+    int64_t qs[2], ks[2], vs[2], os[2];        // row, head
+    float* state;
+    const int32_t* slots;                      // rows, or null: row i has memory i
+    const float* log_decay;
+    int rows, n_slots, q_heads, group, kd, vd, cols, splits;    // a memory's columns go to `splits` CTAs, `cols` to each
+};
+constexpr int kStepThreads = 256;
+constexpr int kStepAhead = 8;                  // rows of the memory on their way to a thread
+
+// A CTA has `cols` columns of a memory; a thread V of them in every (threads / lanes)-th row.  Reading and writing the memory is all
+// there is to it: 8 bytes an element at the rate of the DRAM.
+template <typename T, int V>
+__global__ void __launch_bounds__(kStepThreads) step_kernel(const __grid_constant__ StepArgs A) {
+    __shared__ float qs[kMaxDecayDim], ks[kMaxDecayDim], sums[kStepThreads * V];
+    __shared__ int next;
+    const int row0 = blockIdx.x / A.splits, head = blockIdx.y, c0 = (blockIdx.x - row0 * A.splits) * A.cols, tid = threadIdx.x;
+    const int cols = min(A.cols, A.vd - c0), lanes = A.cols / V, stripes = kStepThreads / lanes;
+    const int lane = tid % lanes, stripe = tid / lanes, c = lane * V;
+    const bool on = stripe < stripes && c < cols;
+    const float factor = exp2f(rate_of(A.log_decay, head));
+    int slot = row0, row = row0;
+    if (A.slots) {
+        slot = A.slots[row0];
+        if (slot < 0 || slot >= A.n_slots) {              // no memory: zeros
+            for (int i = tid; i < cols; i += kStepThreads) static_cast<T*>(A.out)[row0 * A.os[0] + head * A.os[1] + c0 + i] = from_float<T>(0.f);
+            return;
+        }
+        bool earlier = false;                              // rows of one memory: the first one's CTA takes them all, one after the other
+        for (int i = tid; i < row0; i += kStepThreads) earlier |= A.slots[i] == slot;
+        if (__syncthreads_or(earlier)) return;
+    }
+    float* S = A.state + ((size_t)slot * A.q_heads + head) * A.kd * A.vd + c0;
+    while (true) {
+        const T* q = static_cast<const T*>(A.q) + row * A.qs[0] + head * A.qs[1];
+        const T* k = static_cast<const T*>(A.k) + row * A.ks[0] + head / A.group * A.ks[1];
+        const T* v = static_cast<const T*>(A.v) + row * A.vs[0] + head / A.group * A.vs[1] + c0;
+        for (int i = tid; i < A.kd; i += kStepThreads) { qs[i] = to_float(q[i]); ks[i] = to_float(k[i]); }
+        if (tid == 0) next = A.rows;
+        float val[V], sum[V] = {};
+#pragma unroll
+        for (int e = 0; e < V; ++e) val[e] = on ? to_float(v[c + e]) : 0.f;
+        __syncthreads();
+        if (on)
+            for (int i0 = stripe; i0 < A.kd; i0 += kStepAhead * stripes) {
+                float m[kStepAhead][V];
+#pragma unroll
+                for (int u = 0; u < kStepAhead; ++u) {
+                    const int i = i0 + u * stripes;
+                    if (i < A.kd) {
+                        if constexpr (V == 4) *reinterpret_cast<float4*>(m[u]) = *reinterpret_cast<const float4*>(S + (size_t)i * A.vd + c);
+                        else m[u][0] = S[(size_t)i * A.vd + c];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kStepAhead; ++u) {
+                    const int i = i0 + u * stripes;
+                    if (i >= A.kd) continue;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) { m[u][e] = factor * m[u][e] + ks[i] * val[e]; sum[e] += qs[i] * m[u][e]; }
+                    if constexpr (V == 4) *reinterpret_cast<float4*>(S + (size_t)i * A.vd + c) = *reinterpret_cast<const float4*>(m[u]);
+                    else S[(size_t)i * A.vd + c] = m[u][0];
+                }
+            }
+        if (on)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sums[stripe * A.cols + c + e] = sum[e];
+        if (A.slots)
+            for (int i = row + 1 + tid; i < A.rows; i += kStepThreads)
+                if (A.slots[i] == slot) { atomicMin(&next, i); break; }
+        __syncthreads();
+        for (int i = tid; i < cols; i += kStepThreads) {
+            float total = 0.f;
+            for (int s = 0; s < stripes; ++s) total += sums[s * A.cols + i];
+            static_cast<T*>(A.out)[row * A.os[0] + head * A.os[1] + c0 + i] = from_float<T>(total);
+        }
+        if (!A.slots || next >= A.rows) return;
+        row = next;
+        __syncthreads();
+    }
+}
+
+}  // namespace pcr
