@@ -375,6 +375,41 @@ typedef struct {
 } pcr_decay_step_args;
 int pcr_decay_step(const pcr_decay_step_args* args, void* stream);
 
+/* A learned bias of the distance between two tokens, on up to four axes of positions (those of pcr_token_positions, for instance):
+ *   bias[b, h, i, j] = sum over axes a of table[a, n, h],  n = bucket_of[reach + clamp(k_positions[a, b, j] - q_positions[a, b, i])]
+ * with the distance clamped to -reach .. reach (worked out in 64 bits).  A bucket outside 0 .. buckets - 1 counts as 0.  Where the ids of
+ * row and column differ (packed sequences) the bias is minus infinity. */
+typedef struct {
+    void* table;                   /* DEVICE, (axes, buckets, heads) of table_dtype; backward: its gradient, which is written */
+    const int32_t* bucket_of;      /* DEVICE, 2 * reach + 1                                                      */
+    const int32_t* q_positions;    /* DEVICE; axis, batch, token (batch stride 0: all batches have the same)     */
+    int64_t q_stride[3];
+    const int32_t* k_positions;
+    int64_t k_stride[3];
+    const int32_t* q_ids;          /* DEVICE; batch, token; both or none                                         */
+    int64_t q_id_stride[2];
+    const int32_t* k_ids;
+    int64_t k_id_stride[2];
+    void* bias;                    /* DEVICE, of dtype; element (b, h, i, j) at b, h, i times the strides, + j; backward: its gradient, which is read */
+    int64_t bias_stride[3];
+    int64_t batch, q_tokens, k_tokens;  /* batch at most 65535, tokens 2^30                                      */
+    int32_t heads, axes, buckets, reach;  /* 1..4096, 1..4, 1..512, 0..2^20                                      */
+    int32_t dtype;                 /* of the bias */
+    int32_t table_dtype;           /* forward: dtype or PCR_F32; backward: any                                   */
+} pcr_bias_args;
+
+/* Values are added up in single precision, axis after axis, and rounded once to dtype.  The bias shares no memory with what is read.
+ * Errors: PCR_E_ARG, PCR_E_CUDA. */
+int pcr_relative_bias(const pcr_bias_args* args, void* stream);
+
+/* Gradient of the table from that of the bias, over all pairs whose ids are alike; what masked places hold does not count.
+ * Single precision, sums of sums in 64 bits, always in the same order.
+ *   scratch : DEVICE, pcr_relative_bias_scratch_bytes(args) bytes (for the same args on the same device), 16-byte aligned, apart
+ *             from all else.
+ * Errors: PCR_E_ARG, PCR_E_CUDA. */
+size_t pcr_relative_bias_scratch_bytes(const pcr_bias_args* args);
+int pcr_relative_bias_backward(const pcr_bias_args* args, void* scratch, void* stream);
+
 /* Chroma upsampling of the decodes that follow (pcr_decode, pcr_decode_more).  The paper hands
  * its reassembled files to stock decoders (Section 5) and does not name the filter.
  *   PCR_UPSAMPLE_REPLICATE (default): pixel (x, y) takes chroma sample (x >> 1, y >> 1).

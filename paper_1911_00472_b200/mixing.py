@@ -20,6 +20,7 @@ from .tokens import _CODES, _current_device, _forward_mode, _has_tangent, _not_f
 
 _DECAY_ARGS = struct.Struct("<28Q6Q3q6i")           # pcr_decay_args
 _STEP_ARGS = struct.Struct("<4Q8q3Q2q6i")           # pcr_decay_step_args
+_BIAS_ARGS = struct.Struct("<3Q3qQ3qQ2qQ2qQ3q3q6i")  # pcr_bias_args
 _NO_ROWS = (0, 0, 0, 0)
 
 
@@ -209,3 +210,116 @@ def decay_step(q, k, v, log_decay, state, *, slots=None, out=None, stream=None):
     B._chk(B.lib().pcr_decay_step(args, _raw_stream(device.index)), "pcr_decay_step")
     _written((state,) if out is None else (state, out))
     return y
+
+
+# ---- a bias of distances --------------------------------------------------------------------------------------------------------
+
+
+def relative_buckets(buckets, reach, *, one_sided=False, device="cuda:0"):
+    """Bucket (2 * reach + 1,) int32 of every distance -reach .. reach: single distances up to half of a side's buckets, then
+    distances that grow by a factor, up to `reach`, from which on all share the last one.
+
+    one_sided   keys that come later than their query share bucket 0, all buckets are for earlier ones; otherwise the first half
+                is for earlier keys and the query itself, the second for later ones
+    """
+    side = buckets if one_sided else buckets // 2
+    single = side // 2
+    if single < 1 or reach < single or (not one_sided and buckets % 2):
+        raise ValueError("buckets must be even and at least 4 (2 where they are one-sided), reach at least a quarter of them (half)")
+    got = []
+    for d in range(-reach, reach + 1):
+        a = abs(d)
+        n = a if a < single else side - 1 if reach == single else min(side - 1, single + int(math.log(a / single) / math.log(reach / single) * (side - single) + 1e-9))
+        got.append((0 if one_sided else n + side) if d > 0 else n)
+    return torch.tensor(got, dtype=torch.int32, device=device)
+
+
+def _bias_shapes(buckets, q_positions, k_positions, q_ids, k_ids):
+    """(axes, batch or None, tokens of the rows, of the columns)"""
+    if buckets.dim() != 1 or buckets.shape[0] % 2 == 0 or buckets.dtype != torch.int32 or not buckets.is_contiguous():
+        raise ValueError("buckets must be a contiguous int32 vector of 2 * reach + 1 elements")
+    if q_positions.dtype != torch.int32 or k_positions.dtype != torch.int32 or q_positions.dim() not in (2, 3) or k_positions.shape[:-1] != q_positions.shape[:-1]:
+        raise ValueError("positions must be int32, (axes, tokens) or (axes, batch, tokens), of rows and columns alike")
+    if (q_ids is None) != (k_ids is None):
+        raise ValueError("q_ids and k_ids go together")
+    for ids, positions in ((q_ids, q_positions), (k_ids, k_positions)):
+        if ids is not None and (ids.dtype != torch.int32 or ids.shape != positions.shape[1:]):
+            raise ValueError("ids must be int32 and have the shape of an axis of the positions")
+    return q_positions.shape[0], q_positions.shape[1] if q_positions.dim() == 3 else None, q_positions.shape[-1], k_positions.shape[-1]
+
+
+def _bias_pack(table, buckets, q_positions, k_positions, q_ids, k_ids, rows, batch, nq, nk, heads, axes, n_buckets):
+    def places(t):
+        s = t.stride()
+        return (t.data_ptr(), *(s if len(s) == 3 else (s[0], 0, s[1])))
+
+    def ids(t):
+        return (0, 0, 0) if t is None else (t.data_ptr(), *(t.stride() if t.dim() == 2 else (0, t.stride(0))))
+
+    return _BIAS_ARGS.pack(table.data_ptr(), buckets.data_ptr(), *places(q_positions), *places(k_positions), *ids(q_ids), *ids(k_ids),
+                           rows.data_ptr(), *(rows.stride()[:3] if rows.dim() == 4 else (0, *rows.stride()[:2])), batch, nq, nk, heads, axes, n_buckets,
+                           buckets.shape[0] // 2, _CODES[rows.dtype], _CODES[table.dtype])
+
+
+def relative_bias(table, buckets, q_positions, k_positions=None, *, q_ids=None, k_ids=None, dtype=None, out=None, stream=None):
+    """A learned bias for every head and pair of tokens, by the buckets of their distance on each axis:
+
+        bias[..., h, i, j] = sum over axes a of table[a, buckets[reach + clamp(k_positions[a, ..., j] - q_positions[a, ..., i])], h]
+
+    table        (axes, buckets, heads), contiguous
+    buckets      (2 * reach + 1,) int32: the bucket of every distance -reach .. reach (relative_buckets makes them); those beyond are
+                 taken as the ends; a bucket that the table does not have counts as 0
+    positions    (axes, tokens) or (axes, batch, tokens) int32, any strides; k_positions None: the same as q_positions
+    ids          int32, of an axis's shape: pairs whose ids differ are minus infinity (packed sequences); k_ids None: as q_ids
+    dtype        of the bias: the table's (default), or any where the table is float32
+    Returns (heads, rows, columns) or (batch, heads, rows, columns); out: where they go, a row's elements side by side
+    """
+    if k_positions is None:
+        k_positions, k_ids = q_positions, q_ids if k_ids is None else k_ids
+    axes, batch, nq, nk = _bias_shapes(buckets, q_positions, k_positions, q_ids, k_ids)
+    dtype = dtype or table.dtype
+    if table.dim() != 3 or table.shape[0] != axes or table.dtype not in _CODES or not table.is_contiguous():
+        raise ValueError("table must be contiguous (axes, buckets, heads) of float16, bfloat16 or float32")
+    if dtype not in _CODES or (table.dtype != dtype and table.dtype != torch.float32):
+        raise ValueError("dtype must be float16, bfloat16 or float32, the table's or any where that is float32")
+    heads = table.shape[2]
+    shape = (heads, nq, nk) if batch is None else (batch, heads, nq, nk)
+    device, (table, buckets, q_positions, k_positions, q_ids, k_ids) = _operands((table, buckets, q_positions, k_positions, q_ids, k_ids))
+    if out is not None:
+        _output(out, shape, dtype, device, "out")
+    if stream is not None or _current_device() != device.index:
+        with _on(device, stream):
+            return relative_bias(table, buckets, q_positions, k_positions, q_ids=q_ids, k_ids=k_ids, dtype=dtype, out=out)
+    y = table.new_empty(shape, dtype=dtype) if out is None else out
+    args = _bias_pack(table, buckets, q_positions, k_positions, q_ids, k_ids, y, 1 if batch is None else batch, nq, nk, heads, axes, table.shape[1])
+    B._chk(B.lib().pcr_relative_bias(args, _raw_stream(device.index)), "pcr_relative_bias")
+    if out is not None:
+        _written(out)
+    return y
+
+
+def relative_bias_backward(grad, n_buckets, buckets, q_positions, k_positions=None, *, q_ids=None, k_ids=None, dtype=torch.float32, stream=None):
+    """Gradient (axes, n_buckets, heads) of relative_bias's table, of `dtype`, from that of the bias (whatever masked places hold).
+
+    grad   (heads, rows, columns) or (batch, heads, rows, columns) of any strides; only where a row's elements do not stand side by
+           side is it copied first.  Positions and ids without a batch stand for all batches
+    """
+    if k_positions is None:
+        k_positions, k_ids = q_positions, q_ids if k_ids is None else k_ids
+    axes, batch, nq, nk = _bias_shapes(buckets, q_positions, k_positions, q_ids, k_ids)
+    if grad.dim() not in (3, 4) or grad.dtype not in _CODES or grad.shape[-2:] != (nq, nk) or (batch is not None and (grad.dim() == 3 or grad.shape[0] != batch)):
+        raise ValueError("grad must be (heads, rows, columns) or (batch, heads, rows, columns) of the positions, float16, bfloat16 or float32")
+    if dtype not in _CODES or n_buckets < 1:
+        raise ValueError("dtype must be float16, bfloat16 or float32, and there must be buckets")
+    heads = grad.shape[-3]
+    device, (grad, buckets, q_positions, k_positions, q_ids, k_ids) = _operands((grad, buckets, q_positions, k_positions, q_ids, k_ids))
+    if stream is not None or _current_device() != device.index:
+        with _on(device, stream):
+            return relative_bias_backward(grad, n_buckets, buckets, q_positions, k_positions, q_ids=q_ids, k_ids=k_ids, dtype=dtype)
+    grad = _side_by_side(grad)
+    dtable = grad.new_empty((axes, n_buckets, heads), dtype=dtype)
+    args = _bias_pack(dtable, buckets, q_positions, k_positions, q_ids, k_ids, grad, grad.shape[0] if grad.dim() == 4 else 1, nq, nk, heads, axes, n_buckets)
+    L = B.lib()
+    scratch = grad.new_empty(-(-L.pcr_relative_bias_scratch_bytes(args) // 4), dtype=torch.float32)
+    B._chk(L.pcr_relative_bias_backward(args, scratch.data_ptr(), _raw_stream(device.index)), "pcr_relative_bias_backward")
+    return dtable
