@@ -8,9 +8,9 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpcr_b200.so")
-SOURCES = ["pcr_lib.cu", "pcr_tokens.cu", "pcr_decay.cu", "pcr_bias.cu"]
-HEADERS = ["pcr_types.h", "pcr_entropy.cuh", "pcr_long.cuh", "pcr_pixels.cuh", "pcr_refine.cuh", "pcr_sequential.cuh", "pcr_msssim.cuh",
-           "pcr_bias.cuh", "pcr_decay.cuh", "pcr_heads.cuh", "pcr_launches.h", "pcr_patches.cuh", "pcr_spans.h"]
+SOURCES = ["pcr_lib.cu", "pcr_tokens.cu", "pcr_decay.cu", "pcr_decay_tiles.cu", "pcr_bias.cu"]
+HEADERS = ["pcr_types.h", "pcr_entropy.cuh", "pcr_long.cuh", "pcr_pixels.cuh", "pcr_refine.cuh", "pcr_walks.h", "pcr_sequential.cuh", "pcr_msssim.cuh",
+           "pcr_bias.cuh", "pcr_decay.cuh", "pcr_decay_tiles.cuh", "pcr_decay_tiles.h", "pcr_heads.cuh", "pcr_launches.h", "pcr_patches.cuh", "pcr_spans.h"]
 
 
 def _nvcc() -> str:

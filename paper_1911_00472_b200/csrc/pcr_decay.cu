@@ -8,6 +8,7 @@
 
 #include "../../include/pcr.h"
 #include "pcr_decay.cuh"
+#include "pcr_decay_tiles.h"
 #include "pcr_launches.h"
 #include "pcr_spans.h"
 
@@ -53,7 +54,8 @@ bool heads_fit(int q_heads, int k_heads, int k_dim, int v_dim, int dtype) {
 }
 
 struct Form {
-    int chunk;                                  // tokens of a chunk
+    bool tiles;                                 // on the tensor cores
+    int chunk, parts;                           // tokens of a chunk; 16-bit parts of what goes into a memory
     uint32_t seg, keys, slots;                  // tokens of a segment; segments to look for; memories of segments to keep
     bool split;                                 // whether a sequence may have several segments
     size_t slot_bytes, shared_bytes;            // of one direction's memories; of the gradients that heads share
@@ -63,12 +65,25 @@ bool nothing(const pcr_decay_args& a) { return a.sequences == 0; }
 
 Form form_of(const pcr_decay_args& a, bool back) {
     Form f = {};
-    f.chunk = std::max(a.k_dim, a.v_dim) > 128 ? 32 : 64;
-    const int64_t slices = (std::max(a.k_dim, a.v_dim) + kWalkCols - 1) / kWalkCols, wide = (int64_t)a.q_heads * slices * (back ? 3 : 1);
-    // Segments: long enough for about two CTAs an SM, at least 4 chunks
-    const int64_t all = a.batch * a.tokens * wide, want = 2 * sm_count();
-    int64_t seg = std::max<int64_t>((all / want + f.chunk) / f.chunk * f.chunk, 4 * f.chunk);
-    if (seg >= a.tokens) seg = std::max<int64_t>((a.tokens + f.chunk - 1) / f.chunk * f.chunk, f.chunk);
+    const int most = std::max(a.k_dim, a.v_dim);
+    f.tiles = tiles_fit(a, back);
+    f.chunk = f.tiles ? 128 : most > 128 ? 32 : 64;
+    // two parts of bf16 hold 16 bits of a value, which an output of 16 bits does not show; a memory that is given out would
+    f.parts = a.dtype == PCR_BF16 && (a.state_after || a.dstate) ? 3 : 2;
+    // Segments of equal length, as many of a sequence as end first by this count: rounds of CTAs times their chunks, two of which
+    // are as long as a CTA's beginning and end; several segments take another pass over b and c and two more launches.  Packed
+    // sequences are taken to be of equal length.
+    const int64_t wide = (int64_t)a.q_heads * (back ? 3 : 1) * (f.tiles ? 1 : (most + kWalkCols - 1) / kWalkCols) * a.sequences;
+    const int64_t room = (int64_t)sm_count() * (f.tiles ? 1 : 2), mean = std::max<int64_t>(1, a.batch * a.tokens / a.sequences), whole = (mean + f.chunk - 1) / f.chunk;
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t per = 1; per <= std::min<int64_t>(whole, 64); ++per) {
+        const int64_t chunks = (whole + per - 1) / per, cost = ((wide * per + room - 1) / room) * (chunks + 2) + (per > 1 ? (wide * whole + 2 * room - 1) / (2 * room) + 6 : 0);
+        if (cost < least) { least = cost; best = per; }
+    }
+    int64_t seg = (whole + best - 1) / best * f.chunk;
+    // a sequence much longer than the others is cut all the same
+    if (a.starts) seg = std::max<int64_t>(seg, ((wide * whole / room + 3) / 4) * f.chunk);
+    seg = std::min<int64_t>(seg, std::max<int64_t>((a.tokens + f.chunk - 1) / f.chunk, 1) * f.chunk);
     f.seg = (uint32_t)seg;
     f.split = a.tokens > seg;
     if (a.starts) { f.keys = (uint32_t)(a.sequences + a.tokens / seg); f.slots = f.split ? (uint32_t)(a.tokens / seg) : 0; }
@@ -166,11 +181,11 @@ int launch_any(const WalkArgs& A, const Form& f, int dtype, cudaStream_t st) {
     return launch_rows<float>(A, f, st);
 }
 
-// What segments add, the memories before them, and the walks themselves.
-int run(WalkArgs& states, WalkArgs& walks, const Form& f, int dtype, cudaStream_t st) {
+// What segments add, the memories before them, and the walks themselves.  `of`: which of q, k, v, out are a, b, c of each.
+int run(WalkArgs& states, const int (*states_of)[3], WalkArgs& walks, const int (*walks_of)[3], const Form& f, const pcr_decay_args& a, cudaStream_t st) {
     if (f.split) {
         states.states = 1;
-        if (int rc = launch_any(states, f, dtype, st)) return rc;
+        if (int rc = f.tiles ? launch_tiles(states, states_of, a, f.keys, f.parts, st) : launch_any(states, f, a.dtype, st)) return rc;
         int of = 0;
         for (int i = 0; i < states.kinds; ++i) of = std::max(of, states.w[i].bd * states.w[i].cd);
         walk_scan_kernel<<<dim3(f.keys, states.heads, states.kinds * ((of + 1023) / 1024)), 256, 0, st>>>(states);
@@ -178,7 +193,7 @@ int run(WalkArgs& states, WalkArgs& walks, const Form& f, int dtype, cudaStream_
         if (int rc = finish()) return rc;
     }
     walks.states = 0;
-    return launch_any(walks, f, dtype, st);
+    return f.tiles ? launch_tiles(walks, walks_of, a, f.keys, f.parts, st) : launch_any(walks, f, a.dtype, st);
 }
 
 WalkArgs common(const pcr_decay_args& a, const Form& f) {
@@ -215,7 +230,8 @@ int pcr_decay_attention(const pcr_decay_args* args, void* scratch, void* stream)
     w.first = a.state; w.last = a.state_after; w.slots = static_cast<float*>(scratch);
     w.fi = w.li = w.si = a.v_dim; w.fj = w.lj = w.sj = 1;
     WalkArgs S = A;
-    return run(S, A, f, a.dtype, static_cast<cudaStream_t>(stream));
+    const int of[3][3] = {{0, 1, 2}};
+    return run(S, of, A, of, f, a, static_cast<cudaStream_t>(stream));
 }
 
 int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void* stream) {
@@ -261,7 +277,8 @@ int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void
         }
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (int rc = run(S, A, f, a.dtype, st)) return rc;
+    const int states_of[3][3] = {{1, 1, 2}, {0, 0, 3}}, walks_of[3][3] = {{3, 2, 1}, {2, 3, 0}, {1, 0, 3}};
+    if (int rc = run(S, states_of, A, walks_of, f, a, st)) return rc;
     if (group > 1 && a.batch * a.tokens > 0) {
         GroupSum G[2];
         int64_t most = 0;
