@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
     const int head = blockIdx.y, c0 = slice * kWalkCols;
     if (c0 >= W.cd) return;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, warp = tid >> 5, lane = tid & 31;
-    if (!A.states && slice == 0) zero_tail(A, W, W.y32 ? 4 : (int)sizeof(T), blockIdx.x, gridDim.x, head);
+    if (!A.states && slice == 0) zero_tail(A, W, W.y32 ? 4 : (int)sizeof(T), blockIdx.x, gridDim.x, head, tid, kWalkThreads);
     Item it;
     if (!item_of(A, W.rev, blockIdx.x, it)) return;
     if (A.states && it.last) return;
@@ -177,13 +177,18 @@ __global__ void __launch_bounds__(256) walk_scan_kernel(const __grid_constant__ 
     const int more = (it.len - 1) / (int)A.seg;            // segments that have one behind them
     for (int e = block * 256 + threadIdx.x; e < of; e += blocks * 256) {
         float* p = W.slots + ((size_t)it.slot * A.heads + head) * of + e;
+        const size_t step = (size_t)A.heads * of;
         const int i = W.si >= W.sj ? e / W.cd : e % W.bd, j = W.si >= W.sj ? e % W.cd : e / W.bd;
         float m = W.first ? age * W.first[((size_t)it.seq * A.heads + head) * of + i * W.fi + j * W.fj] : 0.f;
-#pragma unroll 8
-        for (int k = 0; k < more; ++k) {
-            m = keep * m + *p;
-            *p = m;
-            p += (size_t)A.heads * of;
+        for (int k = 0; k < more; k += 8) {
+            float x[8];                                    // (all on their way before the first is needed)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = k + u < more ? p[(k + u) * step] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                m = keep * m + x[u];
+                if (k + u < more) p[(k + u) * step] = m;
+            }
         }
     }
 }

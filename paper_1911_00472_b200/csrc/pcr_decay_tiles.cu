@@ -51,7 +51,7 @@ int launch(const TileArgs& G, unsigned keys, cudaStream_t st) {
         cudaGetLastError();
         return PCR_E_CUDA;
     }
-    tile_kernel<T, DB, kStates><<<dim3(keys, G.walks.heads, G.walks.kinds), kTileThreads, TileShared<DB>::kBytes, st>>>(G);
+    tile_kernel<T, DB, kStates><<<keys * G.walks.heads * G.walks.kinds, kTileThreads, TileShared<DB>::kBytes, st>>>(G);
     ++g_launches;
     return cudaGetLastError() == cudaSuccess ? PCR_OK : PCR_E_CUDA;
 }
@@ -76,8 +76,11 @@ int launch_tiles(const WalkArgs& walks, const int (*of)[3], const pcr_decay_args
     TileArgs G;
     G.walks = walks;
     G.parts = parts;
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < 3; ++i) {
         for (int j = 0; j < 3; ++j) G.of[i][j] = of[i][j];
+        Walk& w = G.walks.w[i];
+        w.wide = reinterpret_cast<uintptr_t>(w.y) % 32 == 0 && w.ys[0] % 16 == 0 && w.ys[1] % 16 == 0 && w.ys[2] % 16 == 0;
+    }
     if (!map_of(&G.maps.q, a.q, a, a.q_heads, a.k_dim) || !map_of(&G.maps.k, a.k, a, a.k_heads, a.k_dim) || !map_of(&G.maps.v, a.v, a, a.k_heads, a.v_dim) ||
         !map_of(&G.maps.g, a.out, a, a.q_heads, a.v_dim)) return PCR_E_CUDA;
     return a.dtype == PCR_F16 ? launch_sizes<__half>(G, keys, st) : launch_sizes<__nv_bfloat16>(G, keys, st);

@@ -14,9 +14,9 @@
 // to 16 bits are P's, the image's and the output's, each half a step at most.  fp16 has few exponents: rows of P and of
 // the image are brought to about 2^14 by a power of two, which is taken off again behind the product.
 //
-// 10 warps: four turn S into P and write y (a thread a row), four make B' and keep the memory, one asks for tiles (TMA), one issues
-// the products.  What bounds it: DRAM, 4 tiles of 32 KB a chunk at 1/148 of the copy rate are 2.9 us; the products are 3072 cycles, the
-// warps' work about as much, side by side.
+// 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
+// products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
+// copies of its first tiles go on under the end of the one before.  B' = hi + lo is made beside P; lo waits in registers for A's place.
 #pragma once
 #include <cuda.h>
 
@@ -24,7 +24,7 @@
 
 namespace pcr {
 
-constexpr int kTileThreads = 320;
+constexpr int kTileThreads = 512;
 constexpr int kTile = 128;                     // tokens of a chunk
 constexpr int kHalf = 16384;                   // bytes of 128 rows of 64 elements
 
@@ -43,10 +43,16 @@ template <int DB> struct TileShared {
     static constexpr int kStages = DB == 64 ? 3 : 2;
     static constexpr int kImage = kStages * kStage;
     static constexpr int kRest = kImage + kSide;
-    static constexpr int kBytes = kRest + 2048 + 1024;         // (and what the boundary may take)
+    static constexpr int kBytes = kRest + 3072;
 };
 
-struct TileBars { uint64_t full[3], empty[3], s, i, p, k, o, d, e, r, end; };
+constexpr int kQueue = 2;                      // segments that are asked for ahead
+struct alignas(16) TileBars {
+    uint32_t won[4];                           // the launch's answer
+    uint64_t full[3], empty[3], s, i, p, kh, kl, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
+    int queue[kQueue], dead;
+    uint32_t tensor;
+};
 
 __device__ __forceinline__ uint32_t at_shared(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t* b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(at_shared(b)), "r"(n) : "memory"); }
@@ -80,11 +86,34 @@ __device__ __forceinline__ void tile_load(void* to, const CUtensorMap* map, uint
 __device__ __forceinline__ uint64_t desc_rows(uint32_t at) { return (uint64_t)((at & 0x3ffff) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
 // Rows along the summed dimension, 64 elements of M or N in a row: groups of 8 rows 1024 bytes apart, the next 64 elements kHalf.
 __device__ __forceinline__ uint64_t desc_cols(uint32_t at) { return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(kHalf >> 4) << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
+// One thread of a warp, always the same: what it issues has operands that the compiler knows to be the warp's.
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xffffffff;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
 }
 __device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t how, bool add) {       // A in tensor memory
     asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
+}
+// A whole product, step by step of 16 of the summed dimension, unrolled: issued one by one with operands worked out in a loop a step took
+// 110 cycles, so 65, the tensor cores' own time for 128 columns.
+template <int kSteps> __device__ __forceinline__ void mma_rows(uint32_t d, uint64_t a, uint64_t b, uint32_t how, uint32_t steps) {
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        const uint64_t part = ((k >> 2) * kHalf + (k & 3) * 32) / 16;      // 16 elements on along a row
+        if (k < steps) mma(d, a + part, b + part, how, k > 0);
+    }
+}
+__device__ __forceinline__ void mma_cols(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mma(d, a + 128 * k, b + 128 * k, how, add || k > 0);
+}
+__device__ __forceinline__ void mma_tensor_cols(uint32_t d, uint32_t a, uint64_t b, uint32_t how) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mma_tensor(d, a + 8 * k, b + 128 * k, how, k > 0);
 }
 __device__ __forceinline__ void mma_commit(uint64_t* b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(at_shared(b)) : "memory");
@@ -170,140 +199,232 @@ __device__ __noinline__ void careful(const WalkArgs& A, const Walk& W, const Ite
     }
 }
 
+template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+__device__ __forceinline__ void store32(void* to, const uint32_t (&w)[8]) {       // 32 bytes, aligned
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
+// What a role of the CTA works on: segment after segment, as the queue gives them, and the chunks of each.  `g` counts chunks over all
+// of them: it gives every barrier's phase.
+struct Work {
+    const TileArgs& G;
+    TileBars* bars;
+    const int* queue;
+    volatile int* dead;
+    int taken = 0, kind = 0, head = 0, key = 0, chunks = 0;
+    uint32_t g = 0;
+    Item it;
+
+    // The next segment; false: there is none.  `chunks` 0: nothing to walk over.  Called by whole warps.
+    __device__ __forceinline__ bool next(bool states) {
+        const int slot = taken % kQueue;
+        if (!warp_wait(&bars->got[slot], (taken / kQueue) & 1, dead)) return false;
+        const int x = reinterpret_cast<const volatile int*>(queue)[slot];
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(&bars->taken[slot]);
+        ++taken;
+        if (x < 0) return false;
+        const WalkArgs& A = G.walks;
+        const int rest = x / A.kinds;
+        kind = x - rest * A.kinds;
+        key = rest / A.heads;
+        head = rest - key * A.heads;
+        const bool is = item_of(A, A.w[kind].rev, key, it);
+        if (!is) it.len = -1;
+        chunks = is && !(states && it.last) ? (it.n + kTile - 1) / kTile : 0;
+        return true;
+    }
+    // A chunk's first token and its tokens.
+    __device__ __forceinline__ void chunk(int c, int64_t& t0, int& n) const {
+        const int at = it.from + c * kTile;
+        n = min(kTile, it.from + it.n - at);
+        t0 = it.begin + (G.walks.w[kind].rev ? it.len - at - n : at);
+    }
+    // Whether what a chunk adds to the memory is asked for by anything.
+    __device__ __forceinline__ bool adds(int c, bool states) const { return states || c + 1 < chunks || (it.last && G.walks.w[kind].last); }
+    __device__ __forceinline__ bool final(int c, bool states) const { return !states && it.last && c + 1 == chunks && !G.walks.w[kind].rev; }   // forward, the memory that is given out is not aged
+};
+
 template <typename T, int DB, bool kStates>
 __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ TileArgs G) {
-    extern __shared__ uint8_t raw[];
+    extern __shared__ __align__(1024) uint8_t sm[];
     using L = TileShared<DB>;
     constexpr int kStages = L::kStages;
-    constexpr bool kHalfs = sizeof(T) == 2 && Two<T>::kHow == 1u << 4;
+    constexpr bool kHalfs = Two<T>::kHow == 1u << 4;
     const WalkArgs& A = G.walks;
-    const int kind = blockIdx.z, head = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Walk& W = A.w[kind];
-    if (!kStates) zero_tail(A, W, W.y32 ? 4 : 2, blockIdx.x, gridDim.x, head);
-    Item it;
-    if (!item_of(A, W.rev, blockIdx.x, it)) return;
-    if (kStates && it.last) return;
-    const int bd = W.bd, cd = W.cd;
-    const size_t of = (size_t)bd * cd;
-    if (it.len == 0) {                                                     // the memory as it came
-        if (!kStates && W.last)
-            for (int e = tid; e < (int)of; e += kTileThreads) {
-                const int i = e / cd, j = e % cd;
-                W.last[((size_t)it.seq * A.heads + head) * of + i * W.li + j * W.lj] = W.first ? W.first[((size_t)it.seq * A.heads + head) * of + i * W.fi + j * W.fj] : 0.f;
-            }
-        return;
-    }
-    uint8_t* sm = raw + (-at_shared(raw) & 1023);
-    float* pw = reinterpret_cast<float*>(sm + L::kRest);                   // powers of the factor, 0 .. 128
-    float* cs = pw + 132;                                                  // fp16: what the image's columns were brought up by, two chunks
+    const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
+    float* powers = reinterpret_cast<float*>(sm + L::kRest);               // of the factor, 0 .. 128, of two segments
+    float* cs = powers + 2 * 132;                                          // fp16: what the image's columns were brought up by, two chunks
     TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
-    uint32_t* tensor = reinterpret_cast<uint32_t*>(bars + 1);
-    volatile int* dead = reinterpret_cast<volatile int*>(tensor + 1);
-    const float rate = rate_of(A.log_decay, head);
-    const int chunks = (it.n + kTile - 1) / kTile;
+    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 * 4 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
+    int* queue = bars->queue;
+    volatile int* dead = &bars->dead;
 
-    for (int i = tid; i <= kTile; i += kTileThreads) pw[i] = power(rate, i);
-    if (cd <= 64)                                                          // columns that no copy writes
-        for (int s = 0; s < kStages; ++s)
-            for (int i = tid; i < kHalf / 16; i += kTileThreads) reinterpret_cast<uint4*>(sm + s * L::kStage + 2 * L::kSide + kHalf)[i] = make_uint4(0, 0, 0, 0);
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
-        for (uint64_t* b : {&bars->s, &bars->i, &bars->o, &bars->d, &bars->end}) bar_init(b, 1);
-        for (uint64_t* b : {&bars->p, &bars->k, &bars->e, &bars->r}) bar_init(b, 128);
+        for (uint64_t* b : {&bars->s, &bars->i, &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
+        for (uint64_t* b : {&bars->p, &bars->kh, &bars->kl, &bars->e, &bars->r}) bar_init(b, 128);
+        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], kStates ? 10 : 14); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at_shared(tensor)) : "memory");
+    if (warp == 13) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at_shared(&bars->tensor)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     order_shared();
     order_before();
     __syncthreads();
     order_after();
-    const uint32_t tm = *tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
-    // the chunk's first token and its tokens
-    auto chunk = [&](int c, int64_t& t0, int& n) {
-        const int at = it.from + c * kTile;
-        n = min(kTile, it.from + it.n - at);
-        t0 = it.begin + (W.rev ? it.len - at - n : at);
-    };
+    const uint32_t tm = bars->tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
+    Work w{G, bars, queue, dead};
 
-    if (warp == 8) {
-        if (lane == 0) {
+    if (warp >= 12) {
+        fewer_registers<56>();
+        if (warp == 12) {                                                  // copies of tiles
             const CUtensorMap* all = &G.maps.q;
-            const CUtensorMap *ma = all + G.of[kind][0], *mb = all + G.of[kind][1], *mc = all + G.of[kind][2];
-            const int ha = head / W.a.group, hb = head / W.b.group, hc = head / W.c.group;
-            const uint32_t bytes = (kStates ? 1 : 2) * L::kSide + (cd > 64 ? 2 : 1) * kHalf;
-            int c = 0;
-            for (; c < chunks; ++c) {
-                const int s = c % kStages;
-                if (c >= kStages && !bar_wait(&bars->empty[s], (c / kStages - 1) & 1, dead)) break;
-                int64_t t0;
-                int n;
-                chunk(c, t0, n);
-                uint8_t* to = sm + s * L::kStage;
-                bar_expect(&bars->full[s], bytes);
+            while (w.next(kStates)) {
+                const Walk& W = A.w[w.kind];
+                const CUtensorMap *ma = all + G.of[w.kind][0], *mb = all + G.of[w.kind][1], *mc = all + G.of[w.kind][2];
+                const int ha = w.head / W.a.group, hb = w.head / W.b.group, hc = w.head / W.c.group, halves = W.cd > 64 ? 2 : 1;
+                const uint32_t bytes = (kStates ? 1 : 2) * L::kSide + halves * kHalf;
+                int c = 0;
+                for (; c < w.chunks; ++c, ++w.g) {
+                    const int s = w.g % kStages;
+                    if (w.g >= kStages && !warp_wait(&bars->empty[s], (w.g / kStages - 1) & 1, dead)) break;
+                    int64_t t0;
+                    int n;
+                    w.chunk(c, t0, n);
+                    uint8_t* to = sm + s * L::kStage;
+                    if (elected()) {
+                        bar_expect(&bars->full[s], bytes);
 #pragma unroll
-                for (int h = 0; h < DB / 64; ++h) {
-                    if (!kStates) tile_load(to + h * kHalf, ma, &bars->full[s], 64 * h, ha, (int)t0, it.batch);
-                    tile_load(to + L::kSide + h * kHalf, mb, &bars->full[s], 64 * h, hb, (int)t0, it.batch);
+                        for (int h = 0; h < DB / 64; ++h) {
+                            if (!kStates) tile_load(to + h * kHalf, ma, &bars->full[s], 64 * h, ha, (int)t0, w.it.batch);
+                            tile_load(to + L::kSide + h * kHalf, mb, &bars->full[s], 64 * h, hb, (int)t0, w.it.batch);
+                        }
+                        for (int h = 0; h < halves; ++h) tile_load(to + 2 * L::kSide + h * kHalf, mc, &bars->full[s], 64 * h, hc, (int)t0, w.it.batch);
+                    }
+                    __syncwarp();
                 }
-                for (int h = 0; h < (cd > 64 ? 2 : 1); ++h) tile_load(to + 2 * L::kSide + h * kHalf, mc, &bars->full[s], 64 * h, hc, (int)t0, it.batch);
+                if (c < w.chunks) break;
             }
             volatile int again = 0;                                        // copies still under way write here: none may be left
-            for (int i = max(0, c - kStages); i < c; ++i) bar_wait(&bars->full[i % kStages], (i / kStages) & 1, &again);
-        }
-    } else if (warp == 9) {
-        if (lane == 0) {
-            const uint32_t how = Two<T>::kHow, m128 = 8u << 24, cd16 = (uint32_t)(cd + 15) / 16, bd16 = (uint32_t)(bd + 15) / 16;
-            const uint32_t how_s = how | m128 | 16u << 17, how_i = how | m128 | 2 * cd16 << 17, how_o = how_i | 1u << 16, how_d = how | m128 | 1u << 15 | 1u << 16 | 2 * bd16 << 17;
-            for (int c = 0; c < chunks; ++c) {
-                const int s = c % kStages, ph = c & 1;
-                int64_t t0;
-                int n;
-                chunk(c, t0, n);
-                const uint32_t a = at_shared(sm + s * L::kStage), b = a + L::kSide, v = a + 2 * L::kSide, image = at_shared(sm + L::kImage);
-                const uint32_t steps = (uint32_t)(n + 15) / 16;            // of the chunk's tokens
-                auto part = [&](uint32_t k) { return (k >> 2) * kHalf + (k & 3) * 32; };        // 16 elements on along a row
-                if (!bar_wait(&bars->full[s], (c / kStages) & 1, dead)) break;
-                if (!kStates) {
-                    if (c > 0 && !bar_wait(&bars->o, ph ^ 1, dead)) break;                     // (P lies where S goes)
-                    for (uint32_t k = 0; k < bd16; ++k) mma(S, desc_rows(a + part(k)), desc_rows(b + part(k)), how_s, k > 0);
-                    mma_commit(&bars->s);
-                    if (!bar_wait(&bars->r, ph, dead) || (c > 0 && !bar_wait(&bars->e, ph ^ 1, dead))) break;
+            for (uint32_t i = w.g > kStages ? w.g - kStages : 0; i < w.g; ++i) bar_wait(&bars->full[i % kStages], (i / kStages) & 1, &again);
+        } else if (warp == 13) {                                           // products
+            const uint32_t how = Two<T>::kHow | 8u << 24;
+            const uint64_t a0 = desc_rows(at_shared(sm)), v0 = desc_cols(at_shared(sm) + 2 * L::kSide), ac0 = desc_cols(at_shared(sm)), image_rows = desc_rows(at_shared(sm + L::kImage)),
+                           image_cols = desc_cols(at_shared(sm + L::kImage));
+            bool ok = true;
+            while (ok && w.next(kStates)) {
+                const Walk& W = A.w[w.kind];
+                const uint32_t cd16 = (uint32_t)(W.cd + 15) / 16, bd16 = (uint32_t)(W.bd + 15) / 16;
+                const uint32_t how_s = how | 16u << 17, how_i = how | 2 * cd16 << 17, how_o = how_i | 1u << 16, how_d = how | 1u << 15 | 1u << 16 | 2 * bd16 << 17;
+                for (int c = 0; c < w.chunks; ++c, ++w.g) {
+                    const int s = w.g % kStages, ph = w.g & 1;
+                    int64_t t0;
+                    int n;
+                    w.chunk(c, t0, n);
+                    const uint64_t at = (uint64_t)(s * L::kStage / 16), side = L::kSide / 16;
+                    const bool adds = w.adds(c, kStates);
+                    ok = warp_wait(&bars->full[s], (w.g / kStages) & 1, dead);
+                    if (!kStates) {
+                        ok = ok && (w.g == 0 || warp_wait(&bars->o, ph ^ 1, dead));                // (P lies where S goes)
+                        if (!ok) break;
+                        order_after();
+                        if (elected()) {
+                            mma_rows<DB / 16>(S, a0 + at, a0 + at + side, how_s, bd16);
+                            mma_commit(&bars->s);
+                        }
+                        __syncwarp();
+                        ok = warp_wait(&bars->r, ph, dead) && (w.g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
+                        if (!ok) break;
+                        order_after();
+                        if (elected()) {
+                            mma_rows<DB / 16>(I, a0 + at, image_rows, how_i, bd16);
+                            mma_commit(&bars->i);
+                        }
+                        __syncwarp();
+                        ok = (n == kTile || warp_wait(&bars->kh, ph, dead)) && warp_wait(&bars->p, ph, dead);      // (rows behind the last token are cleared with B')
+                        if (!ok) break;
+                        order_after();
+                        if (elected()) {
+                            mma_tensor_cols(O, S, v0 + at, how_o);
+                            mma_commit(&bars->o);
+                        }
+                        __syncwarp();
+                    } else ok = ok && warp_wait(&bars->r, ph, dead);                               // (D of the chunk before has been read)
+                    ok = ok && warp_wait(&bars->kh, ph, dead);
+                    if (!ok) break;
                     order_after();
-                    for (uint32_t k = 0; k < bd16; ++k) mma(I, desc_rows(a + part(k)), desc_rows(image + part(k)), how_i, k > 0);
-                    mma_commit(&bars->i);
-                    if (n < kTile && !bar_wait(&bars->k, ph, dead)) break;                     // (rows behind the last token are cleared by then)
-                    if (!bar_wait(&bars->p, ph, dead)) break;
-                    order_after();
-                    for (uint32_t k = 0; k < steps; ++k) mma_tensor(O, S + 8 * k, desc_cols(v + 2048 * k), how_o, k > 0);
-                    mma_commit(&bars->o);
-                } else if (!bar_wait(&bars->r, ph, dead)) break;                               // (D of the chunk before has been read)
-                if (!bar_wait(&bars->k, ph, dead)) break;
-                order_after();
-                const uint32_t from[3] = {b, a, image};
-                for (int p = G.parts - 1; p >= 0; --p)                     // the small parts first
-                    for (uint32_t k = 0; k < steps; ++k) mma(D, desc_cols(v + 2048 * k), desc_cols(from[p] + 2048 * k), how_d, p < G.parts - 1 || k > 0);
-                mma_commit(&bars->d);
-                mma_commit(&bars->empty[s]);
+                    if (adds && elected()) mma_cols(D, v0 + at, ac0 + at + side, how_d, false);
+                    __syncwarp();
+                    ok = warp_wait(&bars->kl, ph, dead);
+                    if (!ok) break;
+                    if (elected()) {
+                        if (adds && G.parts > 1) mma_cols(D, v0 + at, ac0 + at, how_d, true);
+                        if (adds && G.parts > 2) mma_cols(D, v0 + at, image_cols, how_d, true);
+                        mma_commit(&bars->d);
+                        mma_commit(&bars->empty[s]);
+                    }
+                    __syncwarp();
+                }
             }
             volatile int again = 0;
-            mma_commit(&bars->end);
+            if (elected()) mma_commit(&bars->end);
+            __syncwarp();
             bar_wait(&bars->end, 0, &again);
+        } else if (warp == 14) {                                           // segments
+            int x = blockIdx.x;
+            for (int i = 0;; ++i) {
+                const int slot = i % kQueue;
+                if (i >= kQueue && !warp_wait(&bars->taken[slot], (i / kQueue - 1) & 1, dead)) break;
+                if (lane == 0) {
+                    queue[slot] = x;
+                    bar_arrive(&bars->got[slot]);
+                }
+                __syncwarp();
+                if (x < 0) break;
+                if (lane == 0) {
+                    order_shared();
+                    bar_expect(&bars->answer, 16);
+                    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(at_shared(bars->won)), "r"(at_shared(&bars->answer)) : "memory");
+                }
+                __syncwarp();
+                if (!warp_wait(&bars->answer, i & 1, dead)) break;
+                uint32_t is, to;
+                asm volatile("{\n.reg .b128 h;\n.reg .pred p;\n.reg .b64 lo, hi;\nld.shared.v2.b64 {lo, hi}, [%2];\nmov.b128 h, {lo, hi};\n"
+                             "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
+                             "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, h;\n}" : "=r"(is), "=r"(to) : "r"(at_shared(bars->won)) : "memory");
+                x = is ? (int)to : -1;
+                __syncwarp();
+            }
         }
     } else if (warp < 4) {
-        if (!kStates) {
-            const int r = tid;
-            for (int c = 0; c < chunks; ++c) {
-                const int ph = c & 1;
+        fewer_registers<112>();
+        const int r = tid;
+        int walked = 0;
+        bool ok = !kStates;
+        while (ok && w.next(kStates)) {
+            const Walk& W = A.w[w.kind];
+            const int cd = W.cd;
+            zero_tail(A, W, W.y32 ? 4 : 2, w.key, gridDim.x / (A.heads * A.kinds), w.head, r, 128);
+            if (w.chunks == 0) continue;
+            const float rate = rate_of(A.log_decay, w.head);
+            // every warp writes the table, all the same values; others may still be at the segment before, none at one before that
+            float* pw = powers + (walked++ & 1) * 132;
+            for (int i = lane; i <= kTile; i += 32) pw[i] = power(rate, i);
+            __syncwarp();
+            for (int c = 0; c < w.chunks; ++c, ++w.g) {
+                const int ph = w.g & 1;
                 int64_t t0;
                 int n;
-                chunk(c, t0, n);
-                if (!warp_wait(&bars->s, ph, dead)) break;
+                w.chunk(c, t0, n);
+                ok = warp_wait(&bars->s, ph, dead);
+                if (!ok) break;
                 order_after();
-                float off = 1.f;                                           // fp16: what brings the row of O back
+                float off = 1.f, on = 1.f;                                 // fp16: what brings a row of P up, and of O back
                 // Group g of 32 columns of S becomes 16 words of P, which lie where group g / 2 was: in this order none is lost.
                 auto faded = [&](float (&p)[32], int g) {
 #pragma unroll
@@ -312,7 +433,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         p[j] = far >= 0 && q < n ? p[j] * pw[far < 0 ? 0 : far] : 0.f;
                     }
                 };
-                float on = 1.f;
                 if (kHalfs) {
                     float most = 0.f;
 #pragma unroll 1
@@ -330,172 +450,234 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
-                    uint32_t w[16] = {};
+                    uint32_t x[16] = {};
                     if (W.rev ? g >= warp : g <= warp) {
                         float p[32];
                         tensor_load32(p, S + mine + 32 * g);
                         tensor_load_wait();
                         faded(p, g);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = kHalfs ? Two<T>::pack(on * p[2 * j], on * p[2 * j + 1]) : Two<T>::pack(p[2 * j], p[2 * j + 1]);
+                        for (int j = 0; j < 16; ++j) x[j] = kHalfs ? Two<T>::pack(on * p[2 * j], on * p[2 * j + 1]) : Two<T>::pack(p[2 * j], p[2 * j + 1]);
                     }
-                    tensor_store16(S + mine + 16 * g, w);
+                    tensor_store16(S + mine + 16 * g, x);
                 }
                 tensor_store_wait();
                 order_before();
-                if (kHalfs && !warp_wait(&bars->r, ph, dead)) break;           // (before D can be asked for, which r's next phase comes after)
+                if (kHalfs) ok = warp_wait(&bars->r, ph, dead);            // (before D can be asked for, which r's next phase comes after)
                 bar_arrive(&bars->p);
-                if (!warp_wait(&bars->o, ph, dead)) break;
+                ok = ok && warp_wait(&bars->o, ph, dead);
+                if (!ok) break;
                 order_after();
                 const float age = r < n ? pw[W.rev ? n - 1 - r : r] : 0.f;
-                const int64_t to = (int64_t)it.batch * W.ys[0] + (t0 + r) * W.ys[1] + (int64_t)head * W.ys[2];
-                bool odd = false;
-                for (int j0 = 0; j0 < cd; j0 += 16) {
-                    float o[16], m[16];
-                    tensor_load16(o, O + mine + j0);
-                    tensor_load16(m, I + mine + j0);
+                const int64_t to = (int64_t)w.it.batch * W.ys[0] + (t0 + r) * W.ys[1] + (int64_t)w.head * W.ys[2];
+                float odd = 0.f;                                           // stays 0 where all is finite
+                for (int j0 = 0; j0 < cd; j0 += 32) {
+                    float o[32], m[32];
+                    tensor_load32(o, O + mine + j0);
+                    tensor_load32(m, I + mine + j0);
                     tensor_load_wait();
-                    if (kHalfs) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) { o[j] *= off; m[j] *= cs[ph * 128 + j0 + j]; }
-                    }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        o[j] += age * m[j];
-                        odd |= !isfinite(o[j]);
+                    for (int j = 0; j < 32; ++j) {
+                        o[j] = kHalfs ? o[j] * off + age * (m[j] * cs[ph * 128 + j0 + j]) : o[j] + age * m[j];
+                        if (j0 + 32 <= cd) odd = fmaf(o[j], 0.f, odd);
+                        else if (j0 + j < cd) odd = fmaf(o[j], 0.f, odd);
                     }
                     if (r < n) {
                         if (W.y32) {
                             float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
+                            for (int e = 0; e < 8; ++e)
                                 if (j0 + 4 * e < cd) y[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                         } else {
-                            uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(W.y) + to + j0);
+                            T* y = static_cast<T*>(W.y) + to + j0;
 #pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                if (j0 + 8 * e < cd)
-                                    y[e] = make_uint4(Two<T>::pack(o[8 * e], o[8 * e + 1]), Two<T>::pack(o[8 * e + 2], o[8 * e + 3]), Two<T>::pack(o[8 * e + 4], o[8 * e + 5]), Two<T>::pack(o[8 * e + 6], o[8 * e + 7]));
+                            for (int e = 0; e < 32; e += 16) {
+                                uint32_t x[8];
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) x[j] = Two<T>::pack(o[e + 2 * j], o[e + 2 * j + 1]);
+                                if (W.wide && j0 + e + 16 <= cd) store32(y + e, x);
+                                else {
+                                    if (j0 + e < cd) reinterpret_cast<uint4*>(y + e)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+                                    if (j0 + e + 8 < cd) reinterpret_cast<uint4*>(y + e)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+                                }
+                            }
                         }
                     }
                 }
-                if (__any_sync(~0u, odd && r < n)) careful<T>(A, W, it, head, t0, n, r, rate, age, O + mine, I + mine, off, kHalfs ? cs + ph * 128 : nullptr, to);
+                if (__any_sync(~0u, !(odd == 0.f) && r < n)) careful<T>(A, W, w.it, w.head, t0, n, r, rate, age, O + mine, I + mine, off, kHalfs ? cs + ph * 128 : nullptr, to);
                 order_before();
                 bar_arrive(&bars->e);
             }
+            if (!ok)                                                       // a wait that ran out does not go unnoticed
+                for (int t = r; t < w.it.n; t += 128) {
+                    const int64_t row = w.it.begin + (W.rev ? w.it.len - w.it.from - w.it.n : w.it.from) + t, to = (int64_t)w.it.batch * W.ys[0] + row * W.ys[1] + (int64_t)w.head * W.ys[2];
+                    for (int j = 0; j < cd; ++j) {
+                        if (W.y32) static_cast<float*>(W.y)[to + j] = __int_as_float(0x7fc00000);
+                        else static_cast<uint16_t*>(W.y)[to + j] = 0x7fff;
+                    }
+                }
+        }
+    } else if (warp < 8) {
+        more_registers<184>();
+        const int r = tid - 128;                                           // an element of c
+        uint8_t* image = sm + L::kImage;
+        bool ok = true;
+        while (ok && w.next(kStates)) {
+            const Walk& W = A.w[w.kind];
+            const int bd = W.bd, cd = W.cd;
+            const size_t of = (size_t)bd * cd;
+            const Item& it = w.it;
+            if (it.len < 0 || (kStates && it.last)) continue;
+            const bool on = r < cd;
+            const float rate = rate_of(A.log_decay, w.head);
+            float R[DB];
+            {
+                const float* from = nullptr;
+                int64_t fi = 0, fj = 0;
+                float age = 1.f;
+                if (!kStates && on) {
+                    if (it.m > 0) { from = W.slots + ((size_t)(it.slot - 1) * A.heads + w.head) * of; fi = W.si; fj = W.sj; }
+                    else if (W.first) { from = W.first + ((size_t)it.seq * A.heads + w.head) * of; fi = W.fi; fj = W.fj; age = W.rev || it.len == 0 ? 1.f : power(rate, 1); }
+                }
+                if (from) from += r * fj;
+#pragma unroll
+                for (int i = 0; i < DB; ++i) {
+                    R[i] = from && i < bd ? age * *from : 0.f;
+                    from = from ? from + fi : from;
+                }
+            }
+            auto write_image = [&](int ph) {
+                float up = 1.f;
+                if (kHalfs) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
+                    const float2 f = to_middle(most);
+                    up = f.x;
+                    cs[ph * 128 + r] = f.y;
+                }
+#pragma unroll
+                for (int i = 0; i < DB; i += 8) {
+                    uint4 x;
+                    x.x = Two<T>::pack(up * R[i], up * R[i + 1]); x.y = Two<T>::pack(up * R[i + 2], up * R[i + 3]);
+                    x.z = Two<T>::pack(up * R[i + 4], up * R[i + 5]); x.w = Two<T>::pack(up * R[i + 6], up * R[i + 7]);
+                    *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16) = x;
+                }
+                order_shared();
+            };
+            if (w.chunks > 0) {
+                if (!kStates) write_image(w.g & 1);
+                order_before();
+                bar_arrive(&bars->r);
+            }
+            for (int c = 0; c < w.chunks; ++c, ++w.g) {
+                int64_t t0;
+                int n;
+                w.chunk(c, t0, n);
+                ok = warp_wait(&bars->d, w.g & 1, dead);
+                if (!ok) break;
+                if (w.adds(c, kStates)) {
+                    order_after();
+                    const float keep = power(rate, w.final(c, kStates) ? n - 1 : n);
+#pragma unroll
+                    for (int i = 0; i < DB; i += 16) {
+                        if (i >= bd) continue;                             // (nothing was put there)
+                        float x[16];
+                        tensor_load16(x, D + mine + i);
+                        tensor_load_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) R[i + j] = keep * R[i + j] + x[j];
+                    }
+                }
+                if (c + 1 < w.chunks) {
+                    if (!kStates) write_image((w.g + 1) & 1);
+                    order_before();
+                    bar_arrive(&bars->r);
+                }
+            }
+            float* out = nullptr;
+            int64_t oi = 0, oj = 0;
+            if (kStates) { out = W.slots + ((size_t)it.slot * A.heads + w.head) * of; oi = W.si; oj = W.sj; }
+            else if (it.last && W.last) { out = W.last + ((size_t)it.seq * A.heads + w.head) * of; oi = W.li; oj = W.lj; }
+            if (!ok)
+#pragma unroll
+                for (int i = 0; i < DB; ++i) R[i] = __int_as_float(0x7fc00000);
+            if (out && on) {
+                volatile float* to = out + r * oj;                         // (volatile: one address after the other, not all at once)
+#pragma unroll
+                for (int i = 0; i < DB; ++i) {
+                    if (i < bd) *to = R[i];
+                    to += oi;
+                }
+            }
         }
     } else {
-        const int r = tid - 128;                                           // an element of c; a token of B'
-        const bool on = r < cd;
-        float R[DB];
-        {
-            const float* from = nullptr;
-            int64_t fi = 0, fj = 0;
-            float age = 1.f;
-            if (!kStates && on) {
-                if (it.m > 0) { from = W.slots + ((size_t)(it.slot - 1) * A.heads + head) * of; fi = W.si; fj = W.sj; }
-                else if (W.first) { from = W.first + ((size_t)it.seq * A.heads + head) * of; fi = W.fi; fj = W.fj; age = W.rev ? 1.f : power(rate, 1); }
-            }
-#pragma unroll
-            for (int i = 0; i < DB; ++i) R[i] = from && i < bd ? age * from[i * fi + r * fj] : 0.f;
-        }
+        const int r = tid - 256;                                           // a token of the chunk
         uint8_t* image = sm + L::kImage;
-        auto write_image = [&](int ph) {
-            float up = 1.f;
-            if (kHalfs) {
-                float most = 0.f;
+        bool ok = true;
+        while (ok && w.next(kStates)) {
+            if (w.chunks == 0) continue;
+            const Walk& W = A.w[w.kind];
+            const float rate = rate_of(A.log_decay, w.head);
+            for (int c = 0; c < w.chunks; ++c, ++w.g) {
+                const int s = w.g % kStages, ph = w.g & 1;
+                int64_t t0;
+                int n;
+                w.chunk(c, t0, n);
+                ok = warp_wait(&bars->full[s], (w.g / kStages) & 1, dead) && (kStates || warp_wait(&bars->s, ph, dead));
+                // two parts: lo waits in registers until I is done with A; three would not fit there and are made behind I
+                auto behind = [&] { return kStates ? w.g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead); };
+                const bool three = !kHalfs && G.parts > 2;
+                if (three) ok = ok && behind();
+                if (!ok) break;
+                uint8_t *a = sm + s * L::kStage, *b = a + L::kSide, *v = a + 2 * L::kSide;
+                const bool in = r < n, adds = w.adds(c, kStates);
+                const float x = in ? power(rate, (W.rev ? r + 1 : n - r) - (w.final(c, kStates) ? 1 : 0)) : 0.f;
+                uint32_t lo[DB / 2];
+                if (adds) {
 #pragma unroll
-                for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
-                const float2 f = to_middle(most);
-                up = f.x;
-                cs[ph * 128 + r] = f.y;
-            }
+                    for (int i = 0; i < DB; i += 8) {
+                        const int at = (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16;
+                        uint4 q = *reinterpret_cast<const uint4*>(b + at), u;
+                        uint32_t *pq = &q.x, *pu = &u.x;
 #pragma unroll
-            for (int i = 0; i < DB; i += 8) {
-                uint4 w;
-                w.x = Two<T>::pack(up * R[i], up * R[i + 1]); w.y = Two<T>::pack(up * R[i + 2], up * R[i + 3]);
-                w.z = Two<T>::pack(up * R[i + 4], up * R[i + 5]); w.w = Two<T>::pack(up * R[i + 6], up * R[i + 7]);
-                *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16) = w;
-            }
-            order_shared();
-        };
-        if (!kStates) write_image(0);
-        bar_arrive(&bars->r);
-        int c = 0;
-        for (; c < chunks; ++c) {
-            const int s = c % kStages, ph = c & 1;
-            int64_t t0;
-            int n;
-            chunk(c, t0, n);
-            const bool final = !kStates && it.last && c == chunks - 1 && !W.rev;       // forward, the memory that is given out is not aged
-            if (!warp_wait(&bars->full[s], (c / kStages) & 1, dead) || (!kStates && !warp_wait(&bars->i, ph, dead))) break;
-            uint8_t *a = sm + s * L::kStage, *b = a + L::kSide, *v = a + 2 * L::kSide;
-            const bool in = r < n;
-            const float w = in ? pw[(W.rev ? r + 1 : n - r) - (final ? 1 : 0)] : 0.f;
-#pragma unroll 4
-            for (int i = 0; i < DB; i += 8) {
-                const int at = (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16;
-                uint4 x = *reinterpret_cast<const uint4*>(b + at), hi, lo, last;
-                uint32_t *px = &x.x, *ph_ = &hi.x, *pl = &lo.x, *pt = &last.x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float2 f = Two<T>::open(px[e]);
-                    f.x = in ? f.x * w : 0.f;
-                    f.y = in ? f.y * w : 0.f;
-                    ph_[e] = Two<T>::pack(f.x, f.y);
-                    float2 g = Two<T>::open(ph_[e]);
-                    f.x -= g.x; f.y -= g.y;
-                    pl[e] = Two<T>::pack(f.x, f.y);
-                    g = Two<T>::open(pl[e]);
-                    pt[e] = Two<T>::pack(f.x - g.x, f.y - g.y);
+                        for (int e = 0; e < 4; ++e) {
+                            float2 f = Two<T>::open(in ? pq[e] : 0u);
+                            f.x *= x; f.y *= x;
+                            pq[e] = Two<T>::pack(f.x, f.y);
+                            float2 h = Two<T>::open(pq[e]);
+                            f.x -= h.x; f.y -= h.y;
+                            lo[i / 2 + e] = Two<T>::pack(f.x, f.y);
+                            h = Two<T>::open(lo[i / 2 + e]);
+                            if (three) pu[e] = Two<T>::pack(f.x - h.x, f.y - h.y);
+                        }
+                        *reinterpret_cast<uint4*>(b + at) = q;
+                        if (three) *reinterpret_cast<uint4*>(image + at) = u;
+                    }
                 }
-                *reinterpret_cast<uint4*>(b + at) = hi;
-                if (G.parts > 1) *reinterpret_cast<uint4*>(a + at) = lo;
-                if (G.parts > 2) *reinterpret_cast<uint4*>(image + at) = last;
+                if (!in)
+                    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                order_shared();
+                bar_arrive(&bars->kh);
+                if (!three) ok = behind();
+                if (!ok) break;
+                if (adds) {
+#pragma unroll
+                    for (int i = 0; i < DB; i += 8) {
+                        const int at = (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16, e = i / 2;
+                        *reinterpret_cast<uint4*>(a + at) = make_uint4(lo[e], lo[e + 1], lo[e + 2], lo[e + 3]);
+                    }
+                    order_shared();
+                }
+                bar_arrive(&bars->kl);
             }
-            if (!in)
-                for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-            order_shared();
-            bar_arrive(&bars->k);
-            if (!warp_wait(&bars->d, ph, dead)) break;
-            order_after();
-            const float keep = pw[final ? n - 1 : n];
-#pragma unroll
-            for (int i = 0; i < DB; i += 16) {
-                if (i >= bd) continue;                                     // (nothing was put there)
-                float x[16];
-                tensor_load16(x, D + mine + i);
-                tensor_load_wait();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) R[i + j] = keep * R[i + j] + x[j];
-            }
-            if (!kStates && c + 1 < chunks) write_image((c + 1) & 1);
-            order_before();
-            bar_arrive(&bars->r);
-        }
-        float* out = nullptr;
-        int64_t oi = 0, oj = 0;
-        if (kStates) { out = W.slots + ((size_t)it.slot * A.heads + head) * of; oi = W.si; oj = W.sj; }
-        else if (it.last && W.last) { out = W.last + ((size_t)it.seq * A.heads + head) * of; oi = W.li; oj = W.lj; }
-        if (out && on) {
-#pragma unroll
-            for (int i = 0; i < DB; ++i)
-                if (i < bd) out[i * oi + r * oj] = c == chunks ? R[i] : __int_as_float(0x7fc00000);
         }
     }
     __syncwarp();
     order_before();
     __syncthreads();
     order_after();
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
-    if (!kStates && *dead && warp < 4)                                     // a wait that ran out does not go unnoticed
-        for (int t = tid; t < it.n; t += 128) {
-            const int64_t row = it.begin + (W.rev ? it.len - it.from - it.n : it.from) + t, to = (int64_t)it.batch * W.ys[0] + row * W.ys[1] + (int64_t)head * W.ys[2];
-            for (int j = 0; j < cd; ++j) {
-                if (W.y32) static_cast<float*>(W.y)[to + j] = __int_as_float(0x7fc00000);
-                else static_cast<uint16_t*>(W.y)[to + j] = 0x7fff;
-            }
-        }
+    if (warp == 13) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
 }  // namespace pcr

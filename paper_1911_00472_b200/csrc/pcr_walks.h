@@ -37,7 +37,7 @@ struct Walk {
     float* slots;                              // memories of segments: element (i, j) of (slot, head) at (...) bd cd + i si + j sj
     int64_t fi, fj, li, lj, si, sj;
     int bd, cd;                                // size of a's and b's heads, and of c's and y's
-    int rev, y32, zero_tail;                   // y32: y is in 32 bits whatever the operands are
+    int rev, y32, wide, zero_tail;             // y32: y is in 32 bits whatever the operands are; wide: 16-bit rows of y begin at 32 bytes
 };
 
 struct WalkArgs {
@@ -109,14 +109,14 @@ __device__ __forceinline__ bool item_of(const WalkArgs& A, int rev, uint32_t key
 }
 
 // Rows that no sequence holds, in an output that has to be whole: zeros.
-__device__ __forceinline__ void zero_tail(const WalkArgs& A, const Walk& W, int es, uint32_t cta, uint32_t ctas, int head) {
+__device__ __forceinline__ void zero_tail(const WalkArgs& A, const Walk& W, int es, uint32_t cta, uint32_t ctas, int head, int thread, int threads) {
     if (!A.starts || !W.zero_tail) return;
     const int64_t from = min(max((int64_t)__ldg(A.starts), (int64_t)0), (int64_t)A.tokens);
     const int64_t to = max(from, min((int64_t)__ldg(A.starts + A.sequences), (int64_t)A.tokens));
     const int64_t rows = from + (int64_t)A.tokens - to;
     for (int64_t r = cta; r < rows; r += ctas) {
         const int64_t at = (r < from ? r : r - from + to) * W.ys[1] + (int64_t)head * W.ys[2];
-        for (int c = threadIdx.x; c < W.cd; c += blockDim.x) {
+        for (int c = thread; c < W.cd; c += threads) {
             if (es == 4) static_cast<float*>(W.y)[at + c] = 0.f;
             else static_cast<uint16_t*>(W.y)[at + c] = 0;
         }
