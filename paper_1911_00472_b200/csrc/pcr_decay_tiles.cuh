@@ -46,11 +46,13 @@ template <int DB> struct TileShared {
     static constexpr int kBytes = kRest + 3072;
 };
 
-constexpr int kQueue = 2;                      // segments that are asked for ahead
+constexpr int kQueue = 3;                      // segments at work in a CTA or asked for ahead
+struct Job { int kind, head, key, chunks; Item it; };                  // kind < 0: there is none left; chunks 0: nothing to walk over
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
     uint64_t full[3], empty[3], s, i, p, kh, kl, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
-    int queue[kQueue], dead;
+    Job jobs[kQueue];
+    int dead;
     uint32_t tensor;
 };
 
@@ -67,12 +69,12 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         uint32_t done;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
         if (done) return true;
-        if (tries % 256) continue;
+        if (tries % 1024) continue;
         uint64_t now;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
         if (!begin) begin = now;
+        if (now - begin > 2000000000ull) *dead = 1;
         if (*dead) return false;
-        if (now - begin > 2000000000ull) { *dead = 1; return false; }
     }
 }
 // The same for a whole warp: all of its lanes go on, together, or none.
@@ -145,16 +147,29 @@ __device__ __forceinline__ void tensor_store16(uint32_t at, const uint32_t (&r)[
 __device__ __forceinline__ void tensor_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tensor_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Pairs of 16-bit values in a word.  cut: the pair nearest to (or, bf16, cut off from) a and b, which keep what is left.
 template <typename T> struct Two;
 template <> struct Two<__nv_bfloat16> {
     static constexpr uint32_t kHow = 1u << 4 | 1u << 7 | 1u << 10;             // 32-bit sums of bf16
     __device__ static uint32_t pack(float a, float b) { __nv_bfloat162 x = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&x); }
-    __device__ static float2 open(uint32_t w) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&w)); }
+    __device__ static float2 open(uint32_t w) { return {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
+    // the upper 16 bits, as they are: two cuts leave 2^-15 of a value at most, three nothing
+    __device__ static uint32_t cut(float& a, float& b) {
+        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+        a -= __uint_as_float(x & 0xffff0000u); b -= __uint_as_float(y & 0xffff0000u);
+        return __byte_perm(x, y, 0x7632);
+    }
 };
 template <> struct Two<__half> {
     static constexpr uint32_t kHow = 1u << 4;
     __device__ static uint32_t pack(float a, float b) { __half2 x = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&x); }
     __device__ static float2 open(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+    __device__ static uint32_t cut(float& a, float& b) {
+        const uint32_t w = pack(a, b);
+        const float2 f = open(w);
+        a -= f.x; b -= f.y;
+        return w;
+    }
 };
 // 2^14 / a power of two about as large as `most`, and what takes it off again
 __device__ __forceinline__ float2 to_middle(float most) {
@@ -165,11 +180,10 @@ __device__ __forceinline__ float2 to_middle(float most) {
 // Outputs of a chunk's rows in which some value is not finite, once more: masked tokens leave no trace (0 * inf is none), so what is not
 // finite is added up again over the tokens that a row sees.  Rare, and slow.
 template <typename T>
-__device__ __noinline__ void careful(const WalkArgs& A, const Walk& W, const Item& it, int head, int64_t t0, int n, int r, float rate, float age, uint32_t O, uint32_t I,
-                                     float off, const float* cs, int64_t to) {
-    const T* a = static_cast<const T*>(W.a.at) + (int64_t)it.batch * W.a.st[0] + (t0 + r) * W.a.st[1] + (int64_t)(head / W.a.group) * W.a.st[2];
-    const T* b = static_cast<const T*>(W.b.at) + (int64_t)it.batch * W.b.st[0] + t0 * W.b.st[1] + (int64_t)(head / W.b.group) * W.b.st[2];
-    const T* c = static_cast<const T*>(W.c.at) + (int64_t)it.batch * W.c.st[0] + t0 * W.c.st[1] + (int64_t)(head / W.c.group) * W.c.st[2];
+__device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t t0, int n, int r, float rate, float age, uint32_t O, uint32_t I, float off, const float* cs, int64_t to) {
+    const T* a = static_cast<const T*>(W.a.at) + (int64_t)batch * W.a.st[0] + (t0 + r) * W.a.st[1] + (int64_t)(head / W.a.group) * W.a.st[2];
+    const T* b = static_cast<const T*>(W.b.at) + (int64_t)batch * W.b.st[0] + t0 * W.b.st[1] + (int64_t)(head / W.b.group) * W.b.st[2];
+    const T* c = static_cast<const T*>(W.c.at) + (int64_t)batch * W.c.st[0] + t0 * W.c.st[1] + (int64_t)(head / W.c.group) * W.c.st[2];
     for (int j0 = 0; j0 < W.cd; j0 += 16) {
         float o[16], m[16];
         tensor_load16(o, O + j0);
@@ -208,43 +222,44 @@ __device__ __forceinline__ void store32(void* to, const uint32_t (&w)[8]) {     
 // What a role of the CTA works on: segment after segment, as the queue gives them, and the chunks of each.  `g` counts chunks over all
 // of them: it gives every barrier's phase.
 struct Work {
-    const TileArgs& G;
     TileBars* bars;
-    const int* queue;
-    volatile int* dead;
-    int taken = 0, kind = 0, head = 0, key = 0, chunks = 0;
     uint32_t g = 0;
-    Item it;
+    int at = -1;
+    const volatile Job* job = nullptr;
 
-    // The next segment; false: there is none.  `chunks` 0: nothing to walk over.  Called by whole warps.
-    __device__ __forceinline__ bool next(bool states) {
-        const int slot = taken % kQueue;
-        if (!warp_wait(&bars->got[slot], (taken / kQueue) & 1, dead)) return false;
-        const int x = reinterpret_cast<const volatile int*>(queue)[slot];
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) bar_arrive(&bars->taken[slot]);
-        ++taken;
-        if (x < 0) return false;
-        const WalkArgs& A = G.walks;
-        const int rest = x / A.kinds;
-        kind = x - rest * A.kinds;
-        key = rest / A.heads;
-        head = rest - key * A.heads;
-        const bool is = item_of(A, A.w[kind].rev, key, it);
-        if (!is) it.len = -1;
-        chunks = is && !(states && it.last) ? (it.n + kTile - 1) / kTile : 0;
-        return true;
+    // On to the next segment, the one before is given back; false: there is none.  Called by whole warps.
+    __device__ __forceinline__ bool next() {
+        if (at >= 0) {
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) bar_arrive(&bars->taken[at % kQueue]);
+        }
+        ++at;
+        if (!warp_wait(&bars->got[at % kQueue], (at / kQueue) & 1, &bars->dead)) return false;
+        job = bars->jobs + at % kQueue;
+        return job->kind >= 0;
     }
     // A chunk's first token and its tokens.
-    __device__ __forceinline__ void chunk(int c, int64_t& t0, int& n) const {
-        const int at = it.from + c * kTile;
-        n = min(kTile, it.from + it.n - at);
-        t0 = it.begin + (G.walks.w[kind].rev ? it.len - at - n : at);
+    __device__ __forceinline__ int tokens(int c) const { return min(kTile, job->it.n - c * kTile); }
+    __device__ __forceinline__ int begin(int c, bool rev) const {
+        const int at = job->it.from + c * kTile;
+        return job->it.begin + (rev ? job->it.len - at - tokens(c) : at);
     }
-    // Whether what a chunk adds to the memory is asked for by anything.
-    __device__ __forceinline__ bool adds(int c, bool states) const { return states || c + 1 < chunks || (it.last && G.walks.w[kind].last); }
-    __device__ __forceinline__ bool final(int c, bool states) const { return !states && it.last && c + 1 == chunks && !G.walks.w[kind].rev; }   // forward, the memory that is given out is not aged
 };
+
+// Rare or once a segment: kept out of the walk's own code, which has to stay near the warps that run it.
+__device__ __noinline__ void tile_tail(const WalkArgs& A, const Walk& W, const volatile Job* job, int segments) {
+    zero_tail(A, W, W.y32 ? 4 : 2, job->key, segments, job->head, threadIdx.x & 127, 128);
+}
+// A wait that ran out does not go unnoticed: the segment's rows are no numbers.
+__device__ __noinline__ void tile_lost(const Walk& W, const volatile Job* job) {
+    for (int t = threadIdx.x & 127; t < job->it.n; t += 128) {
+        const int64_t row = job->it.begin + (W.rev ? job->it.len - job->it.from - job->it.n : job->it.from) + t, to = (int64_t)job->it.batch * W.ys[0] + row * W.ys[1] + (int64_t)job->head * W.ys[2];
+        for (int j = 0; j < W.cd; ++j) {
+            if (W.y32) static_cast<float*>(W.y)[to + j] = __int_as_float(0x7fc00000);
+            else static_cast<uint16_t*>(W.y)[to + j] = 0x7fff;
+        }
+    }
+}
 
 template <typename T, int DB, bool kStates>
 __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ TileArgs G) {
@@ -258,7 +273,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     float* cs = powers + 2 * 132;                                          // fp16: what the image's columns were brought up by, two chunks
     TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
     static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 * 4 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
-    int* queue = bars->queue;
     volatile int* dead = &bars->dead;
 
     if (tid == 0) {
@@ -278,37 +292,35 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     __syncthreads();
     order_after();
     const uint32_t tm = bars->tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
-    Work w{G, bars, queue, dead};
+    Work w{bars};
 
     if (warp >= 12) {
         fewer_registers<56>();
         if (warp == 12) {                                                  // copies of tiles
             const CUtensorMap* all = &G.maps.q;
-            while (w.next(kStates)) {
-                const Walk& W = A.w[w.kind];
-                const CUtensorMap *ma = all + G.of[w.kind][0], *mb = all + G.of[w.kind][1], *mc = all + G.of[w.kind][2];
-                const int ha = w.head / W.a.group, hb = w.head / W.b.group, hc = w.head / W.c.group, halves = W.cd > 64 ? 2 : 1;
+            bool ok = true;
+            while (ok && w.next()) {
+                const Walk& W = A.w[w.job->kind];
+                const int *of = G.of[w.job->kind], head = w.job->head, batch = w.job->it.batch, chunks = w.job->chunks;
+                const CUtensorMap *ma = all + of[0], *mb = all + of[1], *mc = all + of[2];
+                const int ha = head / W.a.group, hb = head / W.b.group, hc = head / W.c.group, halves = W.cd > 64 ? 2 : 1;
                 const uint32_t bytes = (kStates ? 1 : 2) * L::kSide + halves * kHalf;
-                int c = 0;
-                for (; c < w.chunks; ++c, ++w.g) {
-                    const int s = w.g % kStages;
-                    if (w.g >= kStages && !warp_wait(&bars->empty[s], (w.g / kStages - 1) & 1, dead)) break;
-                    int64_t t0;
-                    int n;
-                    w.chunk(c, t0, n);
+                for (int c = 0; c < chunks; ++c, ++w.g) {
+                    const int s = w.g % kStages, t0 = w.begin(c, W.rev);
+                    ok = w.g < kStages || warp_wait(&bars->empty[s], (w.g / kStages - 1) & 1, dead);
+                    if (!ok) break;
                     uint8_t* to = sm + s * L::kStage;
                     if (elected()) {
                         bar_expect(&bars->full[s], bytes);
 #pragma unroll
                         for (int h = 0; h < DB / 64; ++h) {
-                            if (!kStates) tile_load(to + h * kHalf, ma, &bars->full[s], 64 * h, ha, (int)t0, w.it.batch);
-                            tile_load(to + L::kSide + h * kHalf, mb, &bars->full[s], 64 * h, hb, (int)t0, w.it.batch);
+                            if (!kStates) tile_load(to + h * kHalf, ma, &bars->full[s], 64 * h, ha, t0, batch);
+                            tile_load(to + L::kSide + h * kHalf, mb, &bars->full[s], 64 * h, hb, t0, batch);
                         }
-                        for (int h = 0; h < halves; ++h) tile_load(to + 2 * L::kSide + h * kHalf, mc, &bars->full[s], 64 * h, hc, (int)t0, w.it.batch);
+                        for (int h = 0; h < halves; ++h) tile_load(to + 2 * L::kSide + h * kHalf, mc, &bars->full[s], 64 * h, hc, t0, batch);
                     }
                     __syncwarp();
                 }
-                if (c < w.chunks) break;
             }
             volatile int again = 0;                                        // copies still under way write here: none may be left
             for (uint32_t i = w.g > kStages ? w.g - kStages : 0; i < w.g; ++i) bar_wait(&bars->full[i % kStages], (i / kStages) & 1, &again);
@@ -316,18 +328,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const uint32_t how = Two<T>::kHow | 8u << 24;
             const uint64_t a0 = desc_rows(at_shared(sm)), v0 = desc_cols(at_shared(sm) + 2 * L::kSide), ac0 = desc_cols(at_shared(sm)), image_rows = desc_rows(at_shared(sm + L::kImage)),
                            image_cols = desc_cols(at_shared(sm + L::kImage));
+            const int parts = G.parts;
             bool ok = true;
-            while (ok && w.next(kStates)) {
-                const Walk& W = A.w[w.kind];
+            while (ok && w.next()) {
+                const Walk& W = A.w[w.job->kind];
                 const uint32_t cd16 = (uint32_t)(W.cd + 15) / 16, bd16 = (uint32_t)(W.bd + 15) / 16;
                 const uint32_t how_s = how | 16u << 17, how_i = how | 2 * cd16 << 17, how_o = how_i | 1u << 16, how_d = how | 1u << 15 | 1u << 16 | 2 * bd16 << 17;
-                for (int c = 0; c < w.chunks; ++c, ++w.g) {
+                const int chunks = w.job->chunks, adding = chunks - (kStates || (w.job->it.last && W.last) ? 0 : 1);
+                for (int c = 0; c < chunks; ++c, ++w.g) {
                     const int s = w.g % kStages, ph = w.g & 1;
-                    int64_t t0;
-                    int n;
-                    w.chunk(c, t0, n);
                     const uint64_t at = (uint64_t)(s * L::kStage / 16), side = L::kSide / 16;
-                    const bool adds = w.adds(c, kStates);
+                    const bool adds = c < adding;
                     ok = warp_wait(&bars->full[s], (w.g / kStages) & 1, dead);
                     if (!kStates) {
                         ok = ok && (w.g == 0 || warp_wait(&bars->o, ph ^ 1, dead));                // (P lies where S goes)
@@ -346,7 +357,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                             mma_commit(&bars->i);
                         }
                         __syncwarp();
-                        ok = (n == kTile || warp_wait(&bars->kh, ph, dead)) && warp_wait(&bars->p, ph, dead);      // (rows behind the last token are cleared with B')
+                        ok = (w.tokens(c) == kTile || warp_wait(&bars->kh, ph, dead)) && warp_wait(&bars->p, ph, dead);      // (rows behind the last token are cleared with B')
                         if (!ok) break;
                         order_after();
                         if (elected()) {
@@ -363,8 +374,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     ok = warp_wait(&bars->kl, ph, dead);
                     if (!ok) break;
                     if (elected()) {
-                        if (adds && G.parts > 1) mma_cols(D, v0 + at, ac0 + at, how_d, true);
-                        if (adds && G.parts > 2) mma_cols(D, v0 + at, image_cols, how_d, true);
+                        if (adds)
+#pragma unroll 1
+                            for (int p = 1; p < parts; ++p) mma_cols(D, v0 + at, p == 1 ? ac0 + at : image_cols, how_d, true);
                         mma_commit(&bars->d);
                         mma_commit(&bars->empty[s]);
                     }
@@ -380,8 +392,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             for (int i = 0;; ++i) {
                 const int slot = i % kQueue;
                 if (i >= kQueue && !warp_wait(&bars->taken[slot], (i / kQueue - 1) & 1, dead)) break;
+                Job j = {-1, 0, 0, 0, {}};
+                if (x >= 0) {
+                    const int rest = x / A.kinds;
+                    j.kind = x - rest * A.kinds;
+                    j.key = rest / A.heads;
+                    j.head = rest - j.key * A.heads;
+                    const bool is = item_of(A, A.w[j.kind].rev, j.key, j.it);
+                    if (!is) j.it.len = -1;
+                    j.chunks = is && !(kStates && j.it.last) ? (j.it.n + kTile - 1) / kTile : 0;
+                }
                 if (lane == 0) {
-                    queue[slot] = x;
+                    bars->jobs[slot] = j;
                     bar_arrive(&bars->got[slot]);
                 }
                 __syncwarp();
@@ -402,45 +424,49 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             }
         }
     } else if (warp < 4) {
-        fewer_registers<112>();
+        more_registers<136>();
         const int r = tid;
         int walked = 0;
         bool ok = !kStates;
-        while (ok && w.next(kStates)) {
-            const Walk& W = A.w[w.kind];
-            const int cd = W.cd;
-            zero_tail(A, W, W.y32 ? 4 : 2, w.key, gridDim.x / (A.heads * A.kinds), w.head, r, 128);
-            if (w.chunks == 0) continue;
-            const float rate = rate_of(A.log_decay, w.head);
-            // every warp writes the table, all the same values; others may still be at the segment before, none at one before that
+        while (ok && w.next()) {
+            const Walk& W = A.w[w.job->kind];
+            if (A.starts && W.zero_tail) tile_tail(A, W, w.job, gridDim.x / (A.heads * A.kinds));
+            const int chunks = w.job->chunks, head = w.job->head, batch = w.job->it.batch, cd = W.cd;
+            if (chunks == 0) continue;
+            const bool rev = W.rev, y32 = W.y32, wide = W.wide;
+            const float rate = rate_of(A.log_decay, head);
+            // Powers 0 .. 128 of the factor, the other way round where the walk is, so that a row finds those of its columns in one order.
+            // Every warp writes the table, all the same values; others may still be at the segment before, none at one before that.
             float* pw = powers + (walked++ & 1) * 132;
-            for (int i = lane; i <= kTile; i += 32) pw[i] = power(rate, i);
+            for (int i = lane; i <= kTile; i += 32) pw[rev ? kTile - i : i] = power(rate, i);
             __syncwarp();
-            for (int c = 0; c < w.chunks; ++c, ++w.g) {
-                const int ph = w.g & 1;
-                int64_t t0;
-                int n;
-                w.chunk(c, t0, n);
+            for (int c = 0; c < chunks; ++c, ++w.g) {
+                const int ph = w.g & 1, n = w.tokens(c);
                 ok = warp_wait(&bars->s, ph, dead);
                 if (!ok) break;
                 order_after();
                 float off = 1.f, on = 1.f;                                 // fp16: what brings a row of P up, and of O back
-                // Group g of 32 columns of S becomes 16 words of P, which lie where group g / 2 was: in this order none is lost.
+                // Group g of 32 columns of S becomes 16 words of P, which lie where group g / 2 was: in this order none is lost.  A warp's rows
+                // see groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
+                const int first = rev ? warp : 0, end = rev ? 4 : warp + 1;
                 auto faded = [&](float (&p)[32], int g) {
+                    tensor_load32(p, S + mine + 32 * g);
+                    uint32_t seen = ~0u;
+                    if (g == warp) seen = rev ? ~0u << lane : (2u << lane) - 1;
+                    if (32 * g + 32 > n) seen &= n > 32 * g ? (1u << (n - 32 * g)) - 1 : 0u;
+                    const uint32_t f = at_shared(pw + (rev ? kTile : 0) + r - 32 * g);         // (what is not seen may lie beside the table: in shared memory all the same)
+                    float x[32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int q = 32 * g + j, far = W.rev ? q - r : r - q;
-                        p[j] = far >= 0 && q < n ? p[j] * pw[far < 0 ? 0 : far] : 0.f;
-                    }
+                    for (int j = 0; j < 32; ++j) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[j]) : "r"(f - 4 * j));       // (asm: a load that depends on a bit of `seen` waits for the one before)
+                    tensor_load_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) p[j] = seen >> j & 1 ? p[j] * x[j] : 0.f;
                 };
+                float p[32];
                 if (kHalfs) {
                     float most = 0.f;
 #pragma unroll 1
-                    for (int g = 0; g < 4; ++g) {
-                        if (W.rev ? g < warp : g > warp) continue;         // (a warp's rows see no group beyond their own)
-                        float p[32];
-                        tensor_load32(p, S + mine + 32 * g);
-                        tensor_load_wait();
+                    for (int g = first; g < end; ++g) {
                         faded(p, g);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) most = fmaxf(most, fabsf(p[j]));
@@ -451,10 +477,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
                     uint32_t x[16] = {};
-                    if (W.rev ? g >= warp : g <= warp) {
-                        float p[32];
-                        tensor_load32(p, S + mine + 32 * g);
-                        tensor_load_wait();
+                    if (g >= first && g < end) {
                         faded(p, g);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) x[j] = kHalfs ? Two<T>::pack(on * p[2 * j], on * p[2 * j + 1]) : Two<T>::pack(p[2 * j], p[2 * j + 1]);
@@ -468,82 +491,79 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 ok = ok && warp_wait(&bars->o, ph, dead);
                 if (!ok) break;
                 order_after();
-                const float age = r < n ? pw[W.rev ? n - 1 - r : r] : 0.f;
-                const int64_t to = (int64_t)w.it.batch * W.ys[0] + (t0 + r) * W.ys[1] + (int64_t)w.head * W.ys[2];
-                float odd = 0.f;                                           // stays 0 where all is finite
-                for (int j0 = 0; j0 < cd; j0 += 32) {
-                    float o[32], m[32];
-                    tensor_load32(o, O + mine + j0);
-                    tensor_load32(m, I + mine + j0);
+                const float age = r < n ? pw[rev ? kTile - (n - 1 - r) : r] : 0.f;
+                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(w.begin(c, rev) + r) * W.ys[1] + (int64_t)head * W.ys[2];
+                float odd[4] = {};                                         // sums of all, finite where all are
+#pragma unroll 1
+                for (int j0 = 0; j0 < cd; j0 += 16) {
+                    float x[16], m[16];
+                    tensor_load16(x, O + mine + j0);
+                    tensor_load16(m, I + mine + j0);
                     tensor_load_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        o[j] = kHalfs ? o[j] * off + age * (m[j] * cs[ph * 128 + j0 + j]) : o[j] + age * m[j];
-                        if (j0 + 32 <= cd) odd = fmaf(o[j], 0.f, odd);
-                        else if (j0 + j < cd) odd = fmaf(o[j], 0.f, odd);
-                    }
+                    for (int j = 0; j < 16; ++j) x[j] = kHalfs ? x[j] * off + age * (m[j] * cs[ph * 128 + j0 + j]) : x[j] + age * m[j];
+                    if (j0 + 8 >= cd)                                      // (the other half is none of y's)
+#pragma unroll
+                        for (int j = 8; j < 16; ++j) x[j] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) odd[j & 3] += x[j];
                     if (r < n) {
-                        if (W.y32) {
+                        if (y32) {
                             float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (j0 + 4 * e < cd) y[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                            for (int e = 0; e < 4; ++e)
+                                if (j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
                         } else {
                             T* y = static_cast<T*>(W.y) + to + j0;
+                            uint32_t v[8];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 16) {
-                                uint32_t x[8];
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) x[j] = Two<T>::pack(o[e + 2 * j], o[e + 2 * j + 1]);
-                                if (W.wide && j0 + e + 16 <= cd) store32(y + e, x);
-                                else {
-                                    if (j0 + e < cd) reinterpret_cast<uint4*>(y + e)[0] = make_uint4(x[0], x[1], x[2], x[3]);
-                                    if (j0 + e + 8 < cd) reinterpret_cast<uint4*>(y + e)[1] = make_uint4(x[4], x[5], x[6], x[7]);
-                                }
+                            for (int j = 0; j < 8; ++j) v[j] = Two<T>::pack(x[2 * j], x[2 * j + 1]);
+                            if (wide && j0 + 16 <= cd) store32(y, v);
+                            else {
+                                reinterpret_cast<uint4*>(y)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                                if (j0 + 8 < cd) reinterpret_cast<uint4*>(y)[1] = make_uint4(v[4], v[5], v[6], v[7]);
                             }
                         }
                     }
+                    __syncwarp();
                 }
-                if (__any_sync(~0u, !(odd == 0.f) && r < n)) careful<T>(A, W, w.it, w.head, t0, n, r, rate, age, O + mine, I + mine, off, kHalfs ? cs + ph * 128 : nullptr, to);
+                if (__any_sync(~0u, !isfinite((odd[0] + odd[1]) + (odd[2] + odd[3])) && r < n))
+                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, off, kHalfs ? cs + ph * 128 : nullptr, to);
                 order_before();
                 bar_arrive(&bars->e);
             }
-            if (!ok)                                                       // a wait that ran out does not go unnoticed
-                for (int t = r; t < w.it.n; t += 128) {
-                    const int64_t row = w.it.begin + (W.rev ? w.it.len - w.it.from - w.it.n : w.it.from) + t, to = (int64_t)w.it.batch * W.ys[0] + row * W.ys[1] + (int64_t)w.head * W.ys[2];
-                    for (int j = 0; j < cd; ++j) {
-                        if (W.y32) static_cast<float*>(W.y)[to + j] = __int_as_float(0x7fc00000);
-                        else static_cast<uint16_t*>(W.y)[to + j] = 0x7fff;
-                    }
-                }
+            if (!ok) tile_lost(W, w.job);
         }
     } else if (warp < 8) {
         more_registers<184>();
         const int r = tid - 128;                                           // an element of c
         uint8_t* image = sm + L::kImage;
         bool ok = true;
-        while (ok && w.next(kStates)) {
-            const Walk& W = A.w[w.kind];
-            const int bd = W.bd, cd = W.cd;
-            const size_t of = (size_t)bd * cd;
-            const Item& it = w.it;
-            if (it.len < 0 || (kStates && it.last)) continue;
-            const bool on = r < cd;
-            const float rate = rate_of(A.log_decay, w.head);
+        while (ok && w.next()) {
+            const volatile Job& j = *w.job;
+            const Walk& W = A.w[j.kind];
+            if (j.it.len < 0 || (kStates && j.it.last)) continue;
+            const int bd = W.bd, chunks = j.chunks, head = j.head;
+            const bool on = r < W.cd, last = j.it.last, rev = W.rev;
+            const size_t of = (size_t)bd * W.cd;
+            const float rate = rate_of(A.log_decay, head);
             float R[DB];
             {
                 const float* from = nullptr;
-                int64_t fi = 0, fj = 0;
+                int64_t fi = 0;
                 float age = 1.f;
                 if (!kStates && on) {
-                    if (it.m > 0) { from = W.slots + ((size_t)(it.slot - 1) * A.heads + w.head) * of; fi = W.si; fj = W.sj; }
-                    else if (W.first) { from = W.first + ((size_t)it.seq * A.heads + w.head) * of; fi = W.fi; fj = W.fj; age = W.rev || it.len == 0 ? 1.f : power(rate, 1); }
+                    if (j.it.m > 0) { from = W.slots + ((size_t)(j.it.slot - 1) * A.heads + head) * of + r * W.sj; fi = W.si; }
+                    else if (W.first) { from = W.first + ((size_t)j.it.seq * A.heads + head) * of + r * W.fj; fi = W.fi; age = rev || j.it.len == 0 ? 1.f : power(rate, 1); }
                 }
-                if (from) from += r * fj;
 #pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    R[i] = from && i < bd ? age * *from : 0.f;
-                    from = from ? from + fi : from;
+                for (int i = 0; i < DB; i += 8) {
+                    const bool there = from && i < bd;                     // (sizes are multiples of 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        R[i + e] = there ? age * *from : 0.f;
+                        if (there) from += fi;
+                    }
                 }
             }
             auto write_image = [&](int ph) {
@@ -565,108 +585,100 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
                 order_shared();
             };
-            if (w.chunks > 0) {
+            const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
+            if (chunks > 0) ok = true;
+            for (int c = 0; c <= chunks && chunks > 0; ++c) {
+                if (c > 0) {
+                    ok = warp_wait(&bars->d, w.g & 1, dead);
+                    if (!ok) break;
+                    ++w.g;
+                    if (c <= adding) {                                     // what chunk c - 1 adds
+                        order_after();
+                        const int n = w.tokens(c - 1);
+                        const float keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
+#pragma unroll
+                        for (int i = 0; i < DB; i += 16) {
+                            if (i >= bd) continue;                         // (nothing was put there)
+                            float x[16];
+                            tensor_load16(x, D + mine + i);
+                            tensor_load_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                        }
+                    }
+                }
+                if (c == chunks) break;
                 if (!kStates) write_image(w.g & 1);
                 order_before();
                 bar_arrive(&bars->r);
             }
-            for (int c = 0; c < w.chunks; ++c, ++w.g) {
-                int64_t t0;
-                int n;
-                w.chunk(c, t0, n);
-                ok = warp_wait(&bars->d, w.g & 1, dead);
-                if (!ok) break;
-                if (w.adds(c, kStates)) {
-                    order_after();
-                    const float keep = power(rate, w.final(c, kStates) ? n - 1 : n);
-#pragma unroll
-                    for (int i = 0; i < DB; i += 16) {
-                        if (i >= bd) continue;                             // (nothing was put there)
-                        float x[16];
-                        tensor_load16(x, D + mine + i);
-                        tensor_load_wait();
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) R[i + j] = keep * R[i + j] + x[j];
-                    }
-                }
-                if (c + 1 < w.chunks) {
-                    if (!kStates) write_image((w.g + 1) & 1);
-                    order_before();
-                    bar_arrive(&bars->r);
-                }
-            }
             float* out = nullptr;
-            int64_t oi = 0, oj = 0;
-            if (kStates) { out = W.slots + ((size_t)it.slot * A.heads + w.head) * of; oi = W.si; oj = W.sj; }
-            else if (it.last && W.last) { out = W.last + ((size_t)it.seq * A.heads + w.head) * of; oi = W.li; oj = W.lj; }
+            int64_t oi = 0;
+            if (kStates) { out = W.slots + ((size_t)j.it.slot * A.heads + head) * of + r * W.sj; oi = W.si; }
+            else if (last && W.last) { out = W.last + ((size_t)j.it.seq * A.heads + head) * of + r * W.lj; oi = W.li; }
             if (!ok)
 #pragma unroll
                 for (int i = 0; i < DB; ++i) R[i] = __int_as_float(0x7fc00000);
             if (out && on) {
-                volatile float* to = out + r * oj;                         // (volatile: one address after the other, not all at once)
+                volatile float* to = out;                                  // (volatile: one address after the other, not all at once)
 #pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    if (i < bd) *to = R[i];
-                    to += oi;
-                }
+                for (int i = 0; i < DB; i += 8)
+                    if (i < bd)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { *to = R[i + e]; to += oi; }
             }
         }
     } else {
         const int r = tid - 256;                                           // a token of the chunk
         uint8_t* image = sm + L::kImage;
+        const bool three = !kHalfs && G.parts > 2;
         bool ok = true;
-        while (ok && w.next(kStates)) {
-            if (w.chunks == 0) continue;
-            const Walk& W = A.w[w.kind];
-            const float rate = rate_of(A.log_decay, w.head);
-            for (int c = 0; c < w.chunks; ++c, ++w.g) {
-                const int s = w.g % kStages, ph = w.g & 1;
-                int64_t t0;
-                int n;
-                w.chunk(c, t0, n);
+        while (ok && w.next()) {
+            const int chunks = w.job->chunks;
+            const Walk& W = A.w[w.job->kind];
+            const float rate = rate_of(A.log_decay, w.job->head);
+            const bool rev = W.rev, last = w.job->it.last;
+            const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
+            for (int c = 0; c < chunks; ++c, ++w.g) {
+                const int s = w.g % kStages, ph = w.g & 1, n = w.tokens(c);
                 ok = warp_wait(&bars->full[s], (w.g / kStages) & 1, dead) && (kStates || warp_wait(&bars->s, ph, dead));
                 // two parts: lo waits in registers until I is done with A; three would not fit there and are made behind I
-                auto behind = [&] { return kStates ? w.g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead); };
-                const bool three = !kHalfs && G.parts > 2;
-                if (three) ok = ok && behind();
+                if (three) ok = ok && (kStates ? w.g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead));
                 if (!ok) break;
-                uint8_t *a = sm + s * L::kStage, *b = a + L::kSide, *v = a + 2 * L::kSide;
-                const bool in = r < n, adds = w.adds(c, kStates);
-                const float x = in ? power(rate, (W.rev ? r + 1 : n - r) - (w.final(c, kStates) ? 1 : 0)) : 0.f;
+                uint8_t *a = sm + s * L::kStage + r * 128, *b = a + L::kSide, *v = a + 2 * L::kSide;
+                const bool in = r < n, adds = c < adding;
+                const float x = in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && last && c + 1 == chunks && !rev ? 1 : 0)) : 0.f;
                 uint32_t lo[DB / 2];
                 if (adds) {
 #pragma unroll
                     for (int i = 0; i < DB; i += 8) {
-                        const int at = (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16;
+                        const int at = (i >> 6) * kHalf + (((i >> 3) & 7) ^ (r & 7)) * 16;
                         uint4 q = *reinterpret_cast<const uint4*>(b + at), u;
                         uint32_t *pq = &q.x, *pu = &u.x;
+                        if (!in) q = make_uint4(0, 0, 0, 0);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            float2 f = Two<T>::open(in ? pq[e] : 0u);
+                            float2 f = Two<T>::open(pq[e]);
                             f.x *= x; f.y *= x;
-                            pq[e] = Two<T>::pack(f.x, f.y);
-                            float2 h = Two<T>::open(pq[e]);
-                            f.x -= h.x; f.y -= h.y;
-                            lo[i / 2 + e] = Two<T>::pack(f.x, f.y);
-                            h = Two<T>::open(lo[i / 2 + e]);
-                            if (three) pu[e] = Two<T>::pack(f.x - h.x, f.y - h.y);
+                            pq[e] = Two<T>::cut(f.x, f.y);
+                            lo[i / 2 + e] = Two<T>::cut(f.x, f.y);
+                            if (three) pu[e] = Two<T>::cut(f.x, f.y);
                         }
                         *reinterpret_cast<uint4*>(b + at) = q;
-                        if (three) *reinterpret_cast<uint4*>(image + at) = u;
+                        if (three) *reinterpret_cast<uint4*>(image + r * 128 + at) = u;
                     }
                 }
                 if (!in)
-                    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+                    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
                 order_shared();
                 bar_arrive(&bars->kh);
-                if (!three) ok = behind();
+                if (!three) ok = kStates ? w.g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead);
                 if (!ok) break;
                 if (adds) {
 #pragma unroll
-                    for (int i = 0; i < DB; i += 8) {
-                        const int at = (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16, e = i / 2;
-                        *reinterpret_cast<uint4*>(a + at) = make_uint4(lo[e], lo[e + 1], lo[e + 2], lo[e + 3]);
-                    }
+                    for (int i = 0; i < DB; i += 8)
+                        *reinterpret_cast<uint4*>(a + (i >> 6) * kHalf + (((i >> 3) & 7) ^ (r & 7)) * 16) = make_uint4(lo[i / 2], lo[i / 2 + 1], lo[i / 2 + 2], lo[i / 2 + 3]);
                     order_shared();
                 }
                 bar_arrive(&bars->kl);
