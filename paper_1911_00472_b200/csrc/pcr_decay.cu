@@ -82,7 +82,7 @@ Form form_of(const pcr_decay_args& a, bool back) {
     }
     int64_t seg = (whole + best - 1) / best * f.chunk;
     // a sequence much longer than the others is cut all the same
-    if (a.starts) seg = std::max<int64_t>(seg, ((wide * whole / room + 3) / 4) * f.chunk);
+    if (a.starts) seg = std::max<int64_t>(seg, ((wide * whole / room + 1) / 2) * f.chunk);
     seg = std::min<int64_t>(seg, std::max<int64_t>((a.tokens + f.chunk - 1) / f.chunk, 1) * f.chunk);
     f.seg = (uint32_t)seg;
     f.split = a.tokens > seg;
@@ -188,7 +188,12 @@ int run(WalkArgs& states, const int (*states_of)[3], WalkArgs& walks, const int 
         if (int rc = f.tiles ? launch_tiles(states, states_of, a, f.keys, f.parts, st) : launch_any(states, f, a.dtype, st)) return rc;
         int of = 0;
         for (int i = 0; i < states.kinds; ++i) of = std::max(of, states.w[i].bd * states.w[i].cd);
-        walk_scan_kernel<<<dim3(f.keys, states.heads, states.kinds * ((of + 1023) / 1024)), 256, 0, st>>>(states);
+        // (memories begin at 16 bytes where they are whole vectors; several heads to a CTA where sequences alone give CTAs enough)
+        const int blocks = (of + 1023) / 1024;
+        const unsigned heads = (unsigned)std::min<int64_t>(states.heads, std::max<int64_t>(1, 8 * sm_count() / ((int64_t)states.sequences * blocks)));
+        const dim3 grid(states.sequences, heads, states.kinds * blocks);
+        if (of % 4 == 0) walk_scan_kernel<4><<<grid, 256, 0, st>>>(states);
+        else walk_scan_kernel<1><<<grid, 256, 0, st>>>(states);
         ++g_launches;
         if (int rc = finish()) return rc;
     }

@@ -166,28 +166,49 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
             for (int j = lane; j < cols; j += 32) out[i * oi + (c0 + j) * oj] = age * Rs[i * kWalkCols + j];
 }
 
-// Along every sequence of more than one segment: what the segments add becomes the memory with which the next one begins.
+// Along every sequence of more than one segment: what the segments add becomes the memory with which the next one begins.  A thread
+// goes along with V elements of a memory, eight segments' on their way at a time.
+template <int V>
 __global__ void __launch_bounds__(256) walk_scan_kernel(const __grid_constant__ WalkArgs A) {
-    const int blocks = gridDim.z / A.kinds, kind = blockIdx.z / blocks, block = blockIdx.z - kind * blocks;
+    const int blocks = gridDim.z / A.kinds, kind = blockIdx.z / blocks, block = blockIdx.z - kind * blocks, seg = (int)A.seg;
     const Walk& W = A.w[kind];
-    Item it;
-    if (!item_of(A, W.rev, blockIdx.x, it) || it.m != 0 || it.last) return;
-    const int head = blockIdx.y, of = W.bd * W.cd;
-    const float rate = rate_of(A.log_decay, head), keep = power(rate, (int)A.seg), age = W.rev ? 1.f : power(rate, 1);
-    const int more = (it.len - 1) / (int)A.seg;            // segments that have one behind them
-    for (int e = block * 256 + threadIdx.x; e < of; e += blocks * 256) {
-        float* p = W.slots + ((size_t)it.slot * A.heads + head) * of + e;
+    int64_t slot = (int64_t)blockIdx.x * ((A.tokens + A.seg - 1) / A.seg - 1), len = A.tokens;
+    if (A.starts) {                                        // (as item_of has it, for a sequence's first segment)
+        const uint32_t i = W.rev ? A.sequences - 1 - blockIdx.x : blockIdx.x;
+        const int64_t b = start_of(A, W.rev, i);
+        len = start_of(A, W.rev, i + 1) - b;
+        slot = b / seg;
+    }
+    if (len <= seg) return;
+    const int more = (int)((len - 1) / seg), of = W.bd * W.cd;         // segments that have one behind them
+    for (int head = blockIdx.y; head < A.heads; head += gridDim.y) {
+        const float rate = rate_of(A.log_decay, head), keep = power(rate, seg), age = W.rev ? 1.f : power(rate, 1);
         const size_t step = (size_t)A.heads * of;
-        const int i = W.si >= W.sj ? e / W.cd : e % W.bd, j = W.si >= W.sj ? e % W.cd : e / W.bd;
-        float m = W.first ? age * W.first[((size_t)it.seq * A.heads + head) * of + i * W.fi + j * W.fj] : 0.f;
-        for (int k = 0; k < more; k += 8) {
-            float x[8];                                    // (all on their way before the first is needed)
+        const float* first = W.first ? W.first + ((size_t)blockIdx.x * A.heads + head) * of : nullptr;
+        for (int e = (block * 256 + threadIdx.x) * V; e < of; e += blocks * 256 * V) {
+            float* p = W.slots + ((size_t)slot * A.heads + head) * of + e;
+            float m[V];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = k + u < more ? p[(k + u) * step] : 0.f;
+            for (int v = 0; v < V; ++v) {
+                const int i = W.si >= W.sj ? (e + v) / W.cd : (e + v) % W.bd, j = W.si >= W.sj ? (e + v) % W.cd : (e + v) / W.bd;
+                m[v] = first ? age * first[i * W.fi + j * W.fj] : 0.f;
+            }
+            for (int k = 0; k < more; k += 8) {
+                float x[8][V];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                m = keep * m + x[u];
-                if (k + u < more) p[(k + u) * step] = m;
+                for (int u = 0; u < 8; ++u)
+                    if (k + u < more) {
+                        if constexpr (V == 4) *reinterpret_cast<float4*>(x[u]) = *reinterpret_cast<const float4*>(p + (k + u) * step);
+                        else x[u][0] = p[(k + u) * step];
+                    }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (k + u < more) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) m[v] = keep * m[v] + x[u][v];
+                        if constexpr (V == 4) *reinterpret_cast<float4*>(p + (k + u) * step) = *reinterpret_cast<const float4*>(m);
+                        else p[(k + u) * step] = m[0];
+                    }
             }
         }
     }

@@ -16,9 +16,13 @@
 //
 // 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
-// copies of its first tiles go on under the end of the one before.  B' = hi + lo is made beside P; lo waits in registers for A's place.
+// copies of its first tiles go on under the end of the one before.  S is issued a chunk ahead; from one memory to the next it is I, B', D,
+// the sum and the image.  Code is kept short and in loops where it can be: as the roles' code runs side by side on every scheduler, what is
+// unrolled comes out of the instruction caches at 4 to 8 cycles an instruction.
 #pragma once
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "pcr_walks.h"
 
@@ -50,7 +54,7 @@ constexpr int kQueue = 3;                      // segments at work in a CTA or a
 struct Job { int kind, head, key, chunks; Item it; };                  // kind < 0: there is none left; chunks 0: nothing to walk over
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
-    uint64_t full[3], empty[3], s, i, p, kh, kl, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
+    uint64_t full[3], empty[3], s, i, p, k, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
     Job jobs[kQueue];
     int dead;
     uint32_t tensor;
@@ -76,6 +80,12 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         if (now - begin > 2000000000ull) *dead = 1;
         if (*dead) return false;
     }
+}
+// Whether that phase has ended.
+__device__ __forceinline__ bool bar_there(uint64_t* b, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
+    return done;
 }
 // The same for a whole warp: all of its lanes go on, together, or none.
 __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead) { return __all_sync(~0u, bar_wait(b, parity, dead)); }
@@ -147,40 +157,60 @@ __device__ __forceinline__ void tensor_store16(uint32_t at, const uint32_t (&r)[
 __device__ __forceinline__ void tensor_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tensor_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Pairs of 16-bit values in a word.  cut: the pair nearest to (or, bf16, cut off from) a and b, which keep what is left.
+// Pairs of 16-bit values in a word.
 template <typename T> struct Two;
 template <> struct Two<__nv_bfloat16> {
+    using Pair = __nv_bfloat162;
     static constexpr uint32_t kHow = 1u << 4 | 1u << 7 | 1u << 10;             // 32-bit sums of bf16
-    __device__ static uint32_t pack(float a, float b) { __nv_bfloat162 x = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&x); }
-    __device__ static float2 open(uint32_t w) { return {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
-    // the upper 16 bits, as they are: two cuts leave 2^-15 of a value at most, three nothing
-    __device__ static uint32_t cut(float& a, float& b) {
-        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-        a -= __uint_as_float(x & 0xffff0000u); b -= __uint_as_float(y & 0xffff0000u);
-        return __byte_perm(x, y, 0x7632);
-    }
+    __device__ static uint32_t pack(float a, float b) { Pair x = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&x); }
+    __device__ static Pair twice(float v) { return __float2bfloat162_rn(v); }
+    __device__ static float one(Pair v) { return __low2float(v); }
 };
 template <> struct Two<__half> {
+    using Pair = __half2;
     static constexpr uint32_t kHow = 1u << 4;
-    __device__ static uint32_t pack(float a, float b) { __half2 x = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&x); }
-    __device__ static float2 open(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
-    __device__ static uint32_t cut(float& a, float& b) {
-        const uint32_t w = pack(a, b);
-        const float2 f = open(w);
-        a -= f.x; b -= f.y;
-        return w;
+    __device__ static uint32_t pack(float a, float b) { Pair x = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&x); }
+    __device__ static Pair twice(float v) { return __float2half2_rn(v); }
+    __device__ static float one(Pair v) { return __low2float(v); }
+};
+// A factor in 16-bit parts, and products of pairs with it in parts, by 16-bit arithmetic: a product's rounding error is a 16-bit number, which a
+// fused multiply-add gives exactly.  hi = (x f0) rounded, lo = what that left + x f1; three parts: the error of lo's sum is found the
+// same way (Knuth's two-sum) and joins x f2.
+template <typename T> struct Factor {
+    using Pair = typename Two<T>::Pair;
+    Pair f0, f1, f2;
+    __device__ explicit Factor(float f) {
+        f0 = Two<T>::twice(f);
+        f -= Two<T>::one(f0);
+        f1 = Two<T>::twice(f);
+        f2 = Two<T>::twice(f - Two<T>::one(f1));
+    }
+    __device__ void two(uint32_t& x, uint32_t& lo) const {
+        const Pair v = *reinterpret_cast<Pair*>(&x), hi = __hmul2_rn(v, f0), left = __hfma2(v, f0, __hneg2(hi)), l = __hfma2(v, f1, left);
+        x = *reinterpret_cast<const uint32_t*>(&hi);
+        lo = *reinterpret_cast<const uint32_t*>(&l);
+    }
+    __device__ void three(uint32_t& x, uint32_t& lo, uint32_t& last) const {
+        const Pair v = *reinterpret_cast<Pair*>(&x), hi = __hmul2_rn(v, f0), left = __hfma2(v, f0, __hneg2(hi)), next = __hmul2_rn(v, f1), left2 = __hfma2(v, f1, __hneg2(next));
+        const Pair l = __hadd2_rn(left, next), b = __hsub2_rn(l, left), off = __hadd2_rn(__hsub2_rn(left, __hsub2_rn(l, b)), __hsub2_rn(next, b));
+        const Pair e = __hfma2(v, f2, __hadd2_rn(off, left2));
+        x = *reinterpret_cast<const uint32_t*>(&hi);
+        lo = *reinterpret_cast<const uint32_t*>(&l);
+        last = *reinterpret_cast<const uint32_t*>(&e);
     }
 };
-// 2^14 / a power of two about as large as `most`, and what takes it off again
-__device__ __forceinline__ float2 to_middle(float most) {
+// 2^14 / a power of two about as large as `most`; the exponent of what takes it off again
+__device__ __forceinline__ float to_middle(float most, uint8_t& back) {
     const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 250);
-    return {__uint_as_float((uint32_t)(127 + 14 + 127 - e) << 23), __uint_as_float((uint32_t)(e - 14) << 23)};
+    back = (uint8_t)(e - 14);
+    return __uint_as_float((uint32_t)(127 + 14 + 127 - e) << 23);
 }
+__device__ __forceinline__ float from_middle(uint8_t back) { return __uint_as_float((uint32_t)back << 23); }
 
 // Outputs of a chunk's rows in which some value is not finite, once more: masked tokens leave no trace (0 * inf is none), so what is not
 // finite is added up again over the tokens that a row sees.  Rare, and slow.
 template <typename T>
-__device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t t0, int n, int r, float rate, float age, uint32_t O, uint32_t I, float off, const float* cs, int64_t to) {
+__device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t t0, int n, int r, float rate, float age, uint32_t O, uint32_t I, float off, const uint8_t* cs, int64_t to) {
     const T* a = static_cast<const T*>(W.a.at) + (int64_t)batch * W.a.st[0] + (t0 + r) * W.a.st[1] + (int64_t)(head / W.a.group) * W.a.st[2];
     const T* b = static_cast<const T*>(W.b.at) + (int64_t)batch * W.b.st[0] + t0 * W.b.st[1] + (int64_t)(head / W.b.group) * W.b.st[2];
     const T* c = static_cast<const T*>(W.c.at) + (int64_t)batch * W.c.st[0] + t0 * W.c.st[1] + (int64_t)(head / W.c.group) * W.c.st[2];
@@ -192,7 +222,7 @@ __device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t
         uint32_t odd = 0;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            m[j] *= (cs ? cs[j0 + j] : 1.f) * age;
+            m[j] *= (cs ? from_middle(cs[j0 + j]) : 1.f) * age;
             if (j0 + j < W.cd && r < n && !isfinite(o[j] * off + m[j])) odd |= 1u << j;
         }
         for (int q = W.rev ? r : 0; odd && q <= (W.rev ? n - 1 : r); ++q) {
@@ -238,6 +268,8 @@ struct Work {
         job = bars->jobs + at % kQueue;
         return job->kind >= 0;
     }
+    // Whether next() would not wait.
+    __device__ __forceinline__ bool ready() const { return __all_sync(~0u, bar_there(&bars->got[(at + 1) % kQueue], ((at + 1) / kQueue) & 1)); }
     // A chunk's first token and its tokens.
     __device__ __forceinline__ int tokens(int c) const { return min(kTile, job->it.n - c * kTile); }
     __device__ __forceinline__ int begin(int c, bool rev) const {
@@ -270,16 +302,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const WalkArgs& A = G.walks;
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     float* powers = reinterpret_cast<float*>(sm + L::kRest);               // of the factor, 0 .. 128, of two segments
-    float* cs = powers + 2 * 132;                                          // fp16: what the image's columns were brought up by, two chunks
+    uint8_t* cs = reinterpret_cast<uint8_t*>(powers + 2 * 132);            // fp16: what the image's columns were brought up by, two chunks
     TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
-    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 * 4 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
+    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
     volatile int* dead = &bars->dead;
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
         for (uint64_t* b : {&bars->s, &bars->i, &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
-        for (uint64_t* b : {&bars->p, &bars->kh, &bars->kl, &bars->e, &bars->r}) bar_init(b, 128);
-        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], kStates ? 10 : 14); }
+        for (uint64_t* b : {&bars->p, &bars->e, &bars->r}) bar_init(b, 128);
+        bar_init(&bars->k, kStates ? 256 : 128);
+        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -293,6 +326,68 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     order_after();
     const uint32_t tm = bars->tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
     Work w{bars};
+
+    // B' by the threads of a warpgroup, a token each; where two have a chunk, half of its elements.
+    auto make_parts = [&](int r, int which) {
+        uint8_t* image = sm + L::kImage + r * 128;
+        bool ok = true;
+        while (ok && w.next()) {
+            const int chunks = w.job->chunks;
+            const Walk& W = A.w[w.job->kind];
+            const float rate = rate_of(A.log_decay, w.job->head);
+            const bool rev = W.rev, given = kStates || (w.job->it.last && W.last), three = !kHalfs && given && G.parts > 2;
+            const int adding = given ? chunks : chunks - 1, pieces = (W.bd + 15) / 16 * 2;
+            const int from = kStates && which ? pieces / 2 : 0, end = kStates && !which ? pieces / 2 : pieces;
+            for (int c = 0; c < chunks; ++c, ++w.g) {
+                const uint32_t g = w.g, ph = g & 1;
+                const int s = g % kStages, n = w.tokens(c);
+                // the parts' places: A's and the image's are free when I is done; where there is none, the image's when D is
+                ok = warp_wait(&bars->full[s], (g / kStages) & 1, dead) && (kStates ? g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead));
+                if (!ok) break;
+                uint8_t *a = sm + s * L::kStage + r * 128, *b = a + L::kSide, *v = a + 2 * L::kSide;
+                const bool in = r < n;
+                if (c < adding) {
+                    const Factor<T> f(in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f);
+                    // pieces of 8 elements, four (or two) at a time: a piece is a load, a dozen dependent steps and two or three stores
+                    auto all = [&](auto how) {
+                        constexpr int kTimes = decltype(how)::value ? 2 : 4;
+#pragma unroll 1
+                        for (int i = from; i < end; i += kTimes) {
+                            uint4 q[kTimes];
+                            int at[kTimes];
+#pragma unroll
+                            for (int u = 0; u < kTimes; ++u) {
+                                at[u] = ((i + u) >> 3) * kHalf + (((i + u) & 7) ^ (r & 7)) * 16;
+                                q[u] = make_uint4(0, 0, 0, 0);
+                                if (in && i + u < end) q[u] = *reinterpret_cast<const uint4*>(b + at[u]);
+                            }
+#pragma unroll
+                            for (int u = 0; u < kTimes; ++u) {
+                                uint4 lo, last;
+                                uint32_t *pq = &q[u].x, *pl = &lo.x, *pt = &last.x;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    if (decltype(how)::value) f.three(pq[e], pl[e], pt[e]);
+                                    else f.two(pq[e], pl[e]);
+                                }
+                                if (i + u >= end) continue;
+                                *reinterpret_cast<uint4*>(b + at[u]) = q[u];
+                                *reinterpret_cast<uint4*>(a + at[u]) = lo;
+                                if (decltype(how)::value) *reinterpret_cast<uint4*>(image + at[u]) = last;
+                            }
+                        }
+                    };
+                    if (three) all(std::true_type());
+                    else all(std::false_type());
+                }
+                if (!in && which == 0)
+#pragma unroll 1
+                    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                order_shared();
+                bar_arrive(&bars->k);
+            }
+        }
+    };
 
     if (warp >= 12) {
         fewer_registers<56>();
@@ -327,71 +422,98 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         } else if (warp == 13) {                                           // products
             const uint32_t how = Two<T>::kHow | 8u << 24;
             const uint64_t a0 = desc_rows(at_shared(sm)), v0 = desc_cols(at_shared(sm) + 2 * L::kSide), ac0 = desc_cols(at_shared(sm)), image_rows = desc_rows(at_shared(sm + L::kImage)),
-                           image_cols = desc_cols(at_shared(sm + L::kImage));
-            const int parts = G.parts;
-            bool ok = true;
-            while (ok && w.next()) {
-                const Walk& W = A.w[w.job->kind];
-                const uint32_t cd16 = (uint32_t)(W.cd + 15) / 16, bd16 = (uint32_t)(W.bd + 15) / 16;
-                const uint32_t how_s = how | 16u << 17, how_i = how | 2 * cd16 << 17, how_o = how_i | 1u << 16, how_d = how | 1u << 15 | 1u << 16 | 2 * bd16 << 17;
-                const int chunks = w.job->chunks, adding = chunks - (kStates || (w.job->it.last && W.last) ? 0 : 1);
-                for (int c = 0; c < chunks; ++c, ++w.g) {
-                    const int s = w.g % kStages, ph = w.g & 1;
-                    const uint64_t at = (uint64_t)(s * L::kStage / 16), side = L::kSide / 16;
-                    const bool adds = c < adding;
-                    ok = warp_wait(&bars->full[s], (w.g / kStages) & 1, dead);
-                    if (!kStates) {
-                        ok = ok && (w.g == 0 || warp_wait(&bars->o, ph ^ 1, dead));                // (P lies where S goes)
-                        if (!ok) break;
-                        order_after();
-                        if (elected()) {
-                            mma_rows<DB / 16>(S, a0 + at, a0 + at + side, how_s, bd16);
-                            mma_commit(&bars->s);
-                        }
-                        __syncwarp();
-                        ok = warp_wait(&bars->r, ph, dead) && (w.g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
-                        if (!ok) break;
-                        order_after();
-                        if (elected()) {
-                            mma_rows<DB / 16>(I, a0 + at, image_rows, how_i, bd16);
-                            mma_commit(&bars->i);
-                        }
-                        __syncwarp();
-                        ok = (w.tokens(c) == kTile || warp_wait(&bars->kh, ph, dead)) && warp_wait(&bars->p, ph, dead);      // (rows behind the last token are cleared with B')
-                        if (!ok) break;
-                        order_after();
-                        if (elected()) {
-                            mma_tensor_cols(O, S, v0 + at, how_o);
-                            mma_commit(&bars->o);
-                        }
-                        __syncwarp();
-                    } else ok = ok && warp_wait(&bars->r, ph, dead);                               // (D of the chunk before has been read)
-                    ok = ok && warp_wait(&bars->kh, ph, dead);
+                           image_cols = desc_cols(at_shared(sm + L::kImage)), side = L::kSide / 16;
+            // The chunk that comes next, of whatever segment; 0: not known yet (asked for without waiting), -1: none.
+            struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } next = {}, now = {};
+            int c = -1, chunks = 0, adding = 0;
+            auto advance = [&](bool wait) {
+                while (++c >= chunks) {
+                    --c;
+                    if (!wait && !w.ready()) return 0;
+                    if (!w.next()) return -1;
+                    const Walk& W = A.w[w.job->kind];
+                    const bool given = kStates || (w.job->it.last && W.last);
+                    c = -1; chunks = w.job->chunks; adding = given ? chunks : chunks - 1;
+                    next.bd16 = (uint32_t)(W.bd + 15) / 16;
+                    next.how_i = how | 2 * ((uint32_t)(W.cd + 15) / 16) << 17;
+                    next.how_d = how | 1u << 15 | 1u << 16 | 2 * next.bd16 << 17;
+                    next.parts = given ? G.parts : 2;
+                }
+                next.n = w.tokens(c);
+                next.adds = c < adding;
+                return 1;
+            };
+            auto issue_s = [&](uint32_t g) {
+                const uint64_t at = (uint64_t)((int)(g % kStages) * L::kStage / 16);
+                order_after();
+                if (elected()) {
+                    mma_rows<DB / 16>(S, a0 + at, a0 + at + side, how | 16u << 17, next.bd16);
+                    mma_commit(&bars->s);
+                }
+                __syncwarp();
+            };
+            bool ok = true, ahead = false;                                 // ahead: S has been issued
+            int more = advance(true);
+            while (ok && more > 0) {
+                const uint32_t g = w.g, s = g % kStages, ph = g & 1;
+                const uint64_t at = (uint64_t)((int)s * L::kStage / 16);
+                ok = warp_wait(&bars->full[s], (g / kStages) & 1, dead) && (kStates || ahead || g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
+                if (!ok) break;
+                if (!kStates && !ahead) issue_s(g);
+                now = next;
+                ahead = false;
+                more = 0;
+                if (!kStates) {
+                    ok = warp_wait(&bars->r, ph, dead) && (g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
                     if (!ok) break;
                     order_after();
-                    if (adds && elected()) mma_cols(D, v0 + at, ac0 + at + side, how_d, false);
-                    __syncwarp();
-                    ok = warp_wait(&bars->kl, ph, dead);
-                    if (!ok) break;
                     if (elected()) {
-                        if (adds)
-#pragma unroll 1
-                            for (int p = 1; p < parts; ++p) mma_cols(D, v0 + at, p == 1 ? ac0 + at : image_cols, how_d, true);
-                        mma_commit(&bars->d);
-                        mma_commit(&bars->empty[s]);
+                        mma_rows<DB / 16>(I, a0 + at, image_rows, now.how_i, now.bd16);
+                        mma_commit(&bars->i);
                     }
                     __syncwarp();
+                    ok = (now.n == kTile || warp_wait(&bars->k, ph, dead)) && warp_wait(&bars->p, ph, dead);       // (rows behind the last token are cleared with B')
+                    if (!ok) break;
+                    order_after();
+                    if (elected()) {
+                        mma_tensor_cols(O, S, v0 + at, now.how_i | 1u << 16);
+                        mma_commit(&bars->o);
+                    }
+                    __syncwarp();
+                    // S of the next chunk, where that is known and its tiles are there (P lies where it goes, and has been read when O is done).
+                    // Nothing is waited for here that might wait for this chunk's D.
+                    more = advance(false);
+                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[(g + 1) % kStages], ((g + 1) / kStages) & 1))) {
+                        ok = warp_wait(&bars->o, ph, dead);
+                        if (!ok) break;
+                        issue_s(g + 1);
+                        ahead = true;
+                    }
+                } else ok = warp_wait(&bars->r, ph, dead);                                                         // (D of the chunk before has been read)
+                ok = ok && warp_wait(&bars->k, ph, dead);
+                if (!ok) break;
+                order_after();
+                if (elected()) {
+                    if (now.adds)
+#pragma unroll 1
+                        for (int p = now.parts - 1; p >= 0; --p)           // the small parts first
+                            mma_cols(D, v0 + at, p == 0 ? ac0 + at + side : p == 1 ? ac0 + at : image_cols, now.how_d, p < now.parts - 1);
+                    mma_commit(&bars->d);
+                    mma_commit(&bars->empty[s]);
                 }
+                __syncwarp();
+                ++w.g;
+                if (more == 0) more = advance(true);
             }
             volatile int again = 0;
             if (elected()) mma_commit(&bars->end);
             __syncwarp();
             bar_wait(&bars->end, 0, &again);
         } else if (warp == 14) {                                           // segments
-            int x = blockIdx.x;
-            for (int i = 0;; ++i) {
-                const int slot = i % kQueue;
-                if (i >= kQueue && !warp_wait(&bars->taken[slot], (i / kQueue - 1) & 1, dead)) break;
+            const bool tail = !kStates && A.starts && (A.w[0].zero_tail || A.w[1].zero_tail || A.w[2].zero_tail) &&
+                              (__ldg(A.starts) > 0 || __ldg(A.starts + A.sequences) < (int64_t)A.tokens);          // rows of no sequence that become 0
+            int x = blockIdx.x, i = 0;
+            for (uint32_t asked = 0;; ++asked) {
                 Job j = {-1, 0, 0, 0, {}};
                 if (x >= 0) {
                     const int rest = x / A.kinds;
@@ -402,9 +524,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     if (!is) j.it.len = -1;
                     j.chunks = is && !(kStates && j.it.last) ? (j.it.n + kTile - 1) / kTile : 0;
                 }
-                if (lane == 0) {
-                    bars->jobs[slot] = j;
-                    bar_arrive(&bars->got[slot]);
+                // (a key of no segment, or one that there is nothing to do for, is passed over)
+                if (x < 0 || tail || j.chunks > 0 || (!kStates && j.it.len == 0 && A.w[j.kind].last)) {
+                    const int slot = i % kQueue;
+                    if (i >= kQueue && !warp_wait(&bars->taken[slot], (i / kQueue - 1) & 1, dead)) break;
+                    if (lane == 0) {
+                        bars->jobs[slot] = j;
+                        bar_arrive(&bars->got[slot]);
+                    }
+                    ++i;
                 }
                 __syncwarp();
                 if (x < 0) break;
@@ -414,7 +542,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(at_shared(bars->won)), "r"(at_shared(&bars->answer)) : "memory");
                 }
                 __syncwarp();
-                if (!warp_wait(&bars->answer, i & 1, dead)) break;
+                if (!warp_wait(&bars->answer, asked & 1, dead)) break;
                 uint32_t is, to;
                 asm volatile("{\n.reg .b128 h;\n.reg .pred p;\n.reg .b64 lo, hi;\nld.shared.v2.b64 {lo, hi}, [%2];\nmov.b128 h, {lo, hi};\n"
                              "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
@@ -424,8 +552,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             }
         }
     } else if (warp < 4) {
-        more_registers<136>();
         const int r = tid;
+        if (kStates) make_parts(r, 0);
         int walked = 0;
         bool ok = !kStates;
         while (ok && w.next()) {
@@ -445,22 +573,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 ok = warp_wait(&bars->s, ph, dead);
                 if (!ok) break;
                 order_after();
-                float off = 1.f, on = 1.f;                                 // fp16: what brings a row of P up, and of O back
+                float on = 1.f, off = 1.f;                                 // fp16: what brings a row of P up, and of O back
                 // Group g of 32 columns of S becomes 16 words of P, which lie where group g / 2 was: in this order none is lost.  A warp's rows
                 // see groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
                 const int first = rev ? warp : 0, end = rev ? 4 : warp + 1;
                 auto faded = [&](float (&p)[32], int g) {
                     tensor_load32(p, S + mine + 32 * g);
-                    uint32_t seen = ~0u;
-                    if (g == warp) seen = rev ? ~0u << lane : (2u << lane) - 1;
-                    if (32 * g + 32 > n) seen &= n > 32 * g ? (1u << (n - 32 * g)) - 1 : 0u;
                     const uint32_t f = at_shared(pw + (rev ? kTile : 0) + r - 32 * g);         // (what is not seen may lie beside the table: in shared memory all the same)
                     float x[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[j]) : "r"(f - 4 * j));       // (asm: a load that depends on a bit of `seen` waits for the one before)
                     tensor_load_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) p[j] = seen >> j & 1 ? p[j] * x[j] : 0.f;
+                    for (int j = 0; j < 32; ++j) p[j] *= x[j];
+                    if (g == warp || 32 * g + 32 > n) {
+                        uint32_t seen = ~0u;
+                        if (g == warp) seen = rev ? ~0u << lane : (2u << lane) - 1;
+                        if (32 * g + 32 > n) seen &= n > 32 * g ? (1u << (n - 32 * g)) - 1 : 0u;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) p[j] = seen >> j & 1 ? p[j] : 0.f;
+                    }
                 };
                 float p[32];
                 if (kHalfs) {
@@ -471,8 +603,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll
                         for (int j = 0; j < 32; ++j) most = fmaxf(most, fabsf(p[j]));
                     }
-                    const float2 f = to_middle(most);
-                    on = f.x; off = f.y;
+                    uint8_t back;
+                    on = to_middle(most, back);
+                    off = from_middle(back);
                 }
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
@@ -501,19 +634,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     tensor_load16(m, I + mine + j0);
                     tensor_load_wait();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = kHalfs ? x[j] * off + age * (m[j] * cs[ph * 128 + j0 + j]) : x[j] + age * m[j];
+                    for (int j = 0; j < 16; ++j) x[j] = kHalfs ? x[j] * off + age * (m[j] * from_middle(cs[ph * 128 + j0 + j])) : x[j] + age * m[j];
                     if (j0 + 8 >= cd)                                      // (the other half is none of y's)
 #pragma unroll
                         for (int j = 8; j < 16; ++j) x[j] = 0.f;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) odd[j & 3] += x[j];
                     if (r < n) {
-                        if (y32) {
-                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-                        } else {
+                        if (!y32) {
                             T* y = static_cast<T*>(W.y) + to + j0;
                             uint32_t v[8];
 #pragma unroll
@@ -523,6 +651,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                                 reinterpret_cast<uint4*>(y)[0] = make_uint4(v[0], v[1], v[2], v[3]);
                                 if (j0 + 8 < cd) reinterpret_cast<uint4*>(y)[1] = make_uint4(v[4], v[5], v[6], v[7]);
                             }
+                        } else {
+                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
                         }
                     }
                     __syncwarp();
@@ -566,49 +699,63 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     }
                 }
             }
-            auto write_image = [&](int ph) {
-                float up = 1.f;
-                if (kHalfs) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
-                    const float2 f = to_middle(most);
-                    up = f.x;
-                    cs[ph * 128 + r] = f.y;
-                }
-#pragma unroll
-                for (int i = 0; i < DB; i += 8) {
-                    uint4 x;
-                    x.x = Two<T>::pack(up * R[i], up * R[i + 1]); x.y = Two<T>::pack(up * R[i + 2], up * R[i + 3]);
-                    x.z = Two<T>::pack(up * R[i + 4], up * R[i + 5]); x.w = Two<T>::pack(up * R[i + 6], up * R[i + 7]);
-                    *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16) = x;
-                }
-                order_shared();
-            };
             const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
-            if (chunks > 0) ok = true;
             for (int c = 0; c <= chunks && chunks > 0; ++c) {
+                // the memory behind chunk c - 1, and its image for chunk c
+                const bool adds = c > 0 && c <= adding, shows = !kStates && c < chunks;
+                float keep = 1.f;
                 if (c > 0) {
                     ok = warp_wait(&bars->d, w.g & 1, dead);
                     if (!ok) break;
                     ++w.g;
-                    if (c <= adding) {                                     // what chunk c - 1 adds
+                    if (adds) {
                         order_after();
                         const int n = w.tokens(c - 1);
-                        const float keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
-#pragma unroll
-                        for (int i = 0; i < DB; i += 16) {
-                            if (i >= bd) continue;                         // (nothing was put there)
-                            float x[16];
-                            tensor_load16(x, D + mine + i);
-                            tensor_load_wait();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
-                        }
+                        keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
                     }
                 }
+                float up = 1.f;
+                if (kHalfs && adds)
+#pragma unroll
+                    for (int i = 0; i < DB; i += 16) {
+                        if (i >= bd) continue;                             // (nothing was put there)
+                        float x[16];
+                        tensor_load16(x, D + mine + i);
+                        tensor_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                    }
+                if (kHalfs && shows) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
+                    up = to_middle(most, cs[(w.g & 1) * 128 + r]);
+                }
+                float ahead[16];
+                if (!kHalfs && adds) tensor_load16(ahead, D + mine);
+#pragma unroll
+                for (int i = 0; i < DB; i += 16) {
+                    if (i >= bd) continue;
+                    if (!kHalfs && adds) {
+                        float x[16];
+                        tensor_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = ahead[e];
+                        if (i + 16 < DB && i + 16 < bd) tensor_load16(ahead, D + mine + i + 16);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                    }
+                    if (shows)
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8) {
+                            uint4 x;
+                            x.x = Two<T>::pack(up * R[i + e], up * R[i + e + 1]); x.y = Two<T>::pack(up * R[i + e + 2], up * R[i + e + 3]);
+                            x.z = Two<T>::pack(up * R[i + e + 4], up * R[i + e + 5]); x.w = Two<T>::pack(up * R[i + e + 6], up * R[i + e + 7]);
+                            *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + ((((i + e) >> 3) & 7) ^ (r & 7)) * 16) = x;
+                        }
+                }
                 if (c == chunks) break;
-                if (!kStates) write_image(w.g & 1);
+                order_shared();
                 order_before();
                 bar_arrive(&bars->r);
             }
@@ -628,63 +775,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int e = 0; e < 8; ++e) { *to = R[i + e]; to += oi; }
             }
         }
-    } else {
-        const int r = tid - 256;                                           // a token of the chunk
-        uint8_t* image = sm + L::kImage;
-        const bool three = !kHalfs && G.parts > 2;
-        bool ok = true;
-        while (ok && w.next()) {
-            const int chunks = w.job->chunks;
-            const Walk& W = A.w[w.job->kind];
-            const float rate = rate_of(A.log_decay, w.job->head);
-            const bool rev = W.rev, last = w.job->it.last;
-            const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
-            for (int c = 0; c < chunks; ++c, ++w.g) {
-                const int s = w.g % kStages, ph = w.g & 1, n = w.tokens(c);
-                ok = warp_wait(&bars->full[s], (w.g / kStages) & 1, dead) && (kStates || warp_wait(&bars->s, ph, dead));
-                // two parts: lo waits in registers until I is done with A; three would not fit there and are made behind I
-                if (three) ok = ok && (kStates ? w.g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead));
-                if (!ok) break;
-                uint8_t *a = sm + s * L::kStage + r * 128, *b = a + L::kSide, *v = a + 2 * L::kSide;
-                const bool in = r < n, adds = c < adding;
-                const float x = in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && last && c + 1 == chunks && !rev ? 1 : 0)) : 0.f;
-                uint32_t lo[DB / 2];
-                if (adds) {
-#pragma unroll
-                    for (int i = 0; i < DB; i += 8) {
-                        const int at = (i >> 6) * kHalf + (((i >> 3) & 7) ^ (r & 7)) * 16;
-                        uint4 q = *reinterpret_cast<const uint4*>(b + at), u;
-                        uint32_t *pq = &q.x, *pu = &u.x;
-                        if (!in) q = make_uint4(0, 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float2 f = Two<T>::open(pq[e]);
-                            f.x *= x; f.y *= x;
-                            pq[e] = Two<T>::cut(f.x, f.y);
-                            lo[i / 2 + e] = Two<T>::cut(f.x, f.y);
-                            if (three) pu[e] = Two<T>::cut(f.x, f.y);
-                        }
-                        *reinterpret_cast<uint4*>(b + at) = q;
-                        if (three) *reinterpret_cast<uint4*>(image + r * 128 + at) = u;
-                    }
-                }
-                if (!in)
-#pragma unroll 1
-                    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-                order_shared();
-                bar_arrive(&bars->kh);
-                if (!three) ok = kStates ? w.g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead);
-                if (!ok) break;
-                if (adds) {
-#pragma unroll
-                    for (int i = 0; i < DB; i += 8)
-                        *reinterpret_cast<uint4*>(a + (i >> 6) * kHalf + (((i >> 3) & 7) ^ (r & 7)) * 16) = make_uint4(lo[i / 2], lo[i / 2 + 1], lo[i / 2 + 2], lo[i / 2 + 3]);
-                    order_shared();
-                }
-                bar_arrive(&bars->kl);
-            }
-        }
-    }
+    } else make_parts(tid - 256, kStates ? 1 : 0);
     __syncwarp();
     order_before();
     __syncthreads();
