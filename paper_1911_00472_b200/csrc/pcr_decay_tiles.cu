@@ -47,11 +47,12 @@ bool map_of(CUtensorMap* m, const pcr_rows& r, const pcr_decay_args& a, int head
 
 template <typename T, int DB, bool kStates>
 int launch(const TileArgs& G, unsigned keys, cudaStream_t st) {
-    if (cudaFuncSetAttribute(tile_kernel<T, DB, kStates>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShared<DB>::kBytes) != cudaSuccess) {
+    constexpr int kShared = TileShared<DB, kStates>::kBytes;
+    if (cudaFuncSetAttribute(tile_kernel<T, DB, kStates>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared) != cudaSuccess) {
         cudaGetLastError();
         return PCR_E_CUDA;
     }
-    tile_kernel<T, DB, kStates><<<keys * G.walks.heads * G.walks.kinds, kTileThreads, TileShared<DB>::kBytes, st>>>(G);
+    tile_kernel<T, DB, kStates><<<keys * G.walks.heads * G.walks.kinds, kTileThreads, kShared, st>>>(G);
     ++g_launches;
     return cudaGetLastError() == cudaSuccess ? PCR_OK : PCR_E_CUDA;
 }

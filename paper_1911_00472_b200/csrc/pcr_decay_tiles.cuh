@@ -10,15 +10,19 @@
 //
 // The memory itself stays in the registers of one warpgroup, in 32 bits, a column of it (an element of c) to a thread; its 16-bit image
 // is the other operand of I.  B' is kept in two parts, x = hi + lo, three where the memory is given out in 32 bits and 16 bits of each
-// would show; they take the places of B, A and of the memory's image, which S and I are done with by then.  So the roundings
-// to 16 bits are P's, the image's and the output's, each half a step at most.  fp16 has few exponents: rows of P and of
-// the image are brought to about 2^14 by a power of two, which is taken off again behind the product.
+// would show; hi takes B's place, which S is done with by then, a third the image's.  So the roundings to 16 bits are P's, the image's
+// and the output's, each half a step at most.  fp16 has few exponents: rows of P and of the image are brought to about 2^14 by a power of two,
+// which is taken off again behind the product.
 //
 // 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
-// copies of its first tiles go on under the end of the one before.  S is issued a chunk ahead; from one memory to the next it is I, B', D,
-// the sum and the image.  Code is kept short and in loops where it can be: as the roles' code runs side by side on every scheduler, what is
-// unrolled comes out of the instruction caches at 4 to 8 cycles an instruction.
+// copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  From one chunk to
+// the next there are two chains: B' and D; and the memory's sum, its image and I.  P, O and the next S go beside them.
+// Code is kept short and in loops where it can be: the roles' code runs side by side on every scheduler, and what is unrolled comes out of
+// the instruction caches at 4 to 8 cycles an instruction.
+//
+// What bounds it, heads of 128, cycles a chunk: DRAM, 4 tiles of 32 KB at 1/148 of the copy rate, 5500; shared memory (operands of
+// products 2250, copies 770, the warps' loads and stores 1300) 4300; the products 2560.
 #pragma once
 #include <cuda.h>
 
@@ -40,21 +44,20 @@ struct TileArgs {
     int parts;                                 // of B'
 };
 
-// Shared memory of a CTA, from a boundary of 1024 bytes on.
-template <int DB> struct TileShared {
-    static constexpr int kSide = DB / 64 * kHalf;              // A, B, the image of the memory
-    static constexpr int kStage = 2 * kSide + 2 * kHalf;
-    static constexpr int kStages = DB == 64 ? 3 : 2;
-    static constexpr int kImage = kStages * kStage;
-    static constexpr int kRest = kImage + kSide;
-    static constexpr int kBytes = kRest + 3072;
+// Shared memory of a CTA, from a boundary of 1024 bytes on: a ring of tiles, the memory's image, lo.  A chunk's tiles are A, B and C, one
+// place each; sizes up to 64: A and B share a place; without an S: B and C.
+template <int DB, bool kStates> struct TileShared {
+    static constexpr int kSide = DB / 64 * kHalf;              // of A, B, the image and lo
+    static constexpr int kPlaces = DB == 64 ? 6 : 5, kPer = DB == 64 || kStates ? 2 : 3, kB = kPer == 3 ? 1 : 0;
+    static constexpr int kInA = DB == 64 && !kStates ? kHalf : 0;          // where B lies in a place that it shares
+    static constexpr int kImage = kPlaces * 2 * kHalf, kLow = kImage + kSide, kRest = kLow + kSide, kBytes = kRest + 3072;
 };
 
 constexpr int kQueue = 3;                      // segments at work in a CTA or asked for ahead
 struct Job { int kind, head, key, chunks; Item it; };                  // kind < 0: there is none left; chunks 0: nothing to walk over
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
-    uint64_t full[3], empty[3], s, i, p, k, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
+    uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
     Job jobs[kQueue];
     int dead;
     uint32_t tensor;
@@ -296,8 +299,7 @@ __device__ __noinline__ void tile_lost(const Walk& W, const volatile Job* job) {
 template <typename T, int DB, bool kStates>
 __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ TileArgs G) {
     extern __shared__ __align__(1024) uint8_t sm[];
-    using L = TileShared<DB>;
-    constexpr int kStages = L::kStages;
+    using L = TileShared<DB, kStates>;
     constexpr bool kHalfs = Two<T>::kHow == 1u << 4;
     const WalkArgs& A = G.walks;
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
@@ -308,9 +310,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     volatile int* dead = &bars->dead;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
-        for (uint64_t* b : {&bars->s, &bars->i, &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
-        for (uint64_t* b : {&bars->p, &bars->e, &bars->r}) bar_init(b, 128);
+        for (int s = 0; s < L::kPlaces; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
+        for (uint64_t* b : {&bars->s[0], &bars->s[1], &bars->i[0], &bars->i[1], &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
+        for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z}) bar_init(b, 128);
         bar_init(&bars->k, kStates ? 256 : 128);
         for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
         *dead = 0;
@@ -327,9 +329,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const uint32_t tm = bars->tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
     Work w{bars};
 
+    // Tile `which` (0: A, kB: B, kPer - 1: C) of chunk g: its place, and its barriers' phase.
+    auto place = [](uint32_t g, int which) { return (g * L::kPer + which) % L::kPlaces; };
+    auto turn = [](uint32_t g, int which) { return (g * L::kPer + which) / L::kPlaces & 1; };
+    auto has = [&](uint32_t g, int which) { return warp_wait(&bars->full[place(g, which)], turn(g, which), dead); };
+    constexpr int kC = L::kPer - 1;
+
     // B' by the threads of a warpgroup, a token each; where two have a chunk, half of its elements.
     auto make_parts = [&](int r, int which) {
-        uint8_t* image = sm + L::kImage + r * 128;
+        uint8_t *image = sm + L::kImage + r * 128, *low = sm + L::kLow + r * 128;
+        uint32_t g = 0;
         bool ok = true;
         while (ok && w.next()) {
             const int chunks = w.job->chunks;
@@ -338,14 +347,22 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const bool rev = W.rev, given = kStates || (w.job->it.last && W.last), three = !kHalfs && given && G.parts > 2;
             const int adding = given ? chunks : chunks - 1, pieces = (W.bd + 15) / 16 * 2;
             const int from = kStates && which ? pieces / 2 : 0, end = kStates && !which ? pieces / 2 : pieces;
-            for (int c = 0; c < chunks; ++c, ++w.g) {
-                const uint32_t g = w.g, ph = g & 1;
-                const int s = g % kStages, n = w.tokens(c);
-                // the parts' places: A's and the image's are free when I is done; where there is none, the image's when D is
-                ok = warp_wait(&bars->full[s], (g / kStages) & 1, dead) && (kStates ? g == 0 || warp_wait(&bars->d, ph ^ 1, dead) : warp_wait(&bars->i, ph, dead));
-                if (!ok) break;
-                uint8_t *a = sm + s * L::kStage + r * 128, *b = a + L::kSide, *v = a + 2 * L::kSide;
+            for (int c = 0; c < chunks; ++c, ++g) {
+                const int n = w.tokens(c);
                 const bool in = r < n;
+                ok = has(g, L::kB) && has(g, kC);
+                if (!ok) break;
+                uint8_t *b = sm + place(g, L::kB) * 2 * kHalf + L::kInA + r * 128, *v = sm + place(g, kC) * 2 * kHalf + r * 128;
+                if (n < kTile && which == 0) {                             // rows of C behind the last token, which P's zeros might not stop
+                    if (!in)
+#pragma unroll 1
+                        for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    order_shared();
+                    if (!kStates) bar_arrive(&bars->z);
+                }
+                // the parts' places: B's is free when S is done, lo's when the D before is, the image's when I is (or where there is none, that D)
+                ok = (g == 0 || warp_wait(&bars->d, (g - 1) & 1, dead)) && (kStates || (warp_wait(&bars->s[g & 1], g >> 1 & 1, dead) && (!three || warp_wait(&bars->i[g & 1], g >> 1 & 1, dead))));
+                if (!ok) break;
                 if (c < adding) {
                     const Factor<T> f(in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f);
                     // pieces of 8 elements, four (or two) at a time: a piece is a load, a dozen dependent steps and two or three stores
@@ -372,7 +389,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                                 }
                                 if (i + u >= end) continue;
                                 *reinterpret_cast<uint4*>(b + at[u]) = q[u];
-                                *reinterpret_cast<uint4*>(a + at[u]) = lo;
+                                *reinterpret_cast<uint4*>(low + at[u]) = lo;
                                 if (decltype(how)::value) *reinterpret_cast<uint4*>(image + at[u]) = last;
                             }
                         }
@@ -380,9 +397,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     if (three) all(std::true_type());
                     else all(std::false_type());
                 }
-                if (!in && which == 0)
-#pragma unroll 1
-                    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
                 order_shared();
                 bar_arrive(&bars->k);
             }
@@ -399,30 +413,35 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 const int *of = G.of[w.job->kind], head = w.job->head, batch = w.job->it.batch, chunks = w.job->chunks;
                 const CUtensorMap *ma = all + of[0], *mb = all + of[1], *mc = all + of[2];
                 const int ha = head / W.a.group, hb = head / W.b.group, hc = head / W.c.group, halves = W.cd > 64 ? 2 : 1;
-                const uint32_t bytes = (kStates ? 1 : 2) * L::kSide + halves * kHalf;
                 for (int c = 0; c < chunks; ++c, ++w.g) {
-                    const int s = w.g % kStages, t0 = w.begin(c, W.rev);
-                    ok = w.g < kStages || warp_wait(&bars->empty[s], (w.g / kStages - 1) & 1, dead);
-                    if (!ok) break;
-                    uint8_t* to = sm + s * L::kStage;
-                    if (elected()) {
-                        bar_expect(&bars->full[s], bytes);
-#pragma unroll
-                        for (int h = 0; h < DB / 64; ++h) {
-                            if (!kStates) tile_load(to + h * kHalf, ma, &bars->full[s], 64 * h, ha, t0, batch);
-                            tile_load(to + L::kSide + h * kHalf, mb, &bars->full[s], 64 * h, hb, t0, batch);
+                    const int t0 = w.begin(c, W.rev);
+#pragma unroll 1
+                    for (int which = 0; which < L::kPer; ++which) {
+                        const uint32_t at = w.g * L::kPer + which, s = at % L::kPlaces;
+                        ok = at < L::kPlaces || warp_wait(&bars->empty[s], (at / L::kPlaces - 1) & 1, dead);
+                        if (!ok) break;
+                        uint8_t* to = sm + s * 2 * kHalf;
+                        if (elected()) {
+                            const bool is_c = which == kC, is_b = which == L::kB && !is_c, is_a = !kStates && which == 0;
+                            const CUtensorMap* m = is_c ? mc : is_a ? ma : mb;
+                            const int h = is_c ? hc : is_a ? ha : hb, n = is_c ? halves : DB / 64;
+                            bar_expect(&bars->full[s], (uint32_t)(n + (DB == 64 && is_a ? 1 : 0)) * kHalf);
+                            for (int i = 0; i < n; ++i) tile_load(to + i * kHalf, m, &bars->full[s], 64 * i, h, t0, batch);
+                            if (DB == 64 && is_a && is_b) tile_load(to + L::kInA, mb, &bars->full[s], 0, hb, t0, batch);
                         }
-                        for (int h = 0; h < halves; ++h) tile_load(to + 2 * L::kSide + h * kHalf, mc, &bars->full[s], 64 * h, hc, t0, batch);
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    if (!ok) break;
                 }
             }
             volatile int again = 0;                                        // copies still under way write here: none may be left
-            for (uint32_t i = w.g > kStages ? w.g - kStages : 0; i < w.g; ++i) bar_wait(&bars->full[i % kStages], (i / kStages) & 1, &again);
+            const uint32_t all_of = w.g * L::kPer;
+            for (uint32_t i = all_of > L::kPlaces ? all_of - L::kPlaces : 0; i < all_of; ++i) bar_wait(&bars->full[i % L::kPlaces], (i / L::kPlaces) & 1, &again);
         } else if (warp == 13) {                                           // products
             const uint32_t how = Two<T>::kHow | 8u << 24;
-            const uint64_t a0 = desc_rows(at_shared(sm)), v0 = desc_cols(at_shared(sm) + 2 * L::kSide), ac0 = desc_cols(at_shared(sm)), image_rows = desc_rows(at_shared(sm + L::kImage)),
-                           image_cols = desc_cols(at_shared(sm + L::kImage)), side = L::kSide / 16;
+            const uint64_t rows0 = desc_rows(at_shared(sm)), cols0 = desc_cols(at_shared(sm)), image_rows = rows0 + L::kImage / 16;
+            auto rows_at = [&](uint32_t g, int which, int off) { return rows0 + (uint64_t)(place(g, which) * 2 * kHalf + off) / 16; };
+            auto cols_at = [&](uint32_t g, int which, int off) { return cols0 + (uint64_t)(place(g, which) * 2 * kHalf + off) / 16; };
             // The chunk that comes next, of whatever segment; 0: not known yet (asked for without waiting), -1: none.
             struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } next = {}, now = {};
             int c = -1, chunks = 0, adding = 0;
@@ -444,62 +463,66 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 return 1;
             };
             auto issue_s = [&](uint32_t g) {
-                const uint64_t at = (uint64_t)((int)(g % kStages) * L::kStage / 16);
                 order_after();
                 if (elected()) {
-                    mma_rows<DB / 16>(S, a0 + at, a0 + at + side, how | 16u << 17, next.bd16);
-                    mma_commit(&bars->s);
+                    mma_rows<DB / 16>(S, rows_at(g, 0, 0), rows_at(g, L::kB, L::kInA), how | 16u << 17, next.bd16);
+                    mma_commit(&bars->s[g & 1]);
                 }
                 __syncwarp();
             };
             bool ok = true, ahead = false;                                 // ahead: S has been issued
-            int more = advance(true);
+            int more = advance(true), tails = 0;
             while (ok && more > 0) {
-                const uint32_t g = w.g, s = g % kStages, ph = g & 1;
-                const uint64_t at = (uint64_t)((int)s * L::kStage / 16);
-                ok = warp_wait(&bars->full[s], (g / kStages) & 1, dead) && (kStates || ahead || g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
-                if (!ok) break;
-                if (!kStates && !ahead) issue_s(g);
+                const uint32_t g = w.g, ph = g & 1;
+                if (!kStates && !ahead) {                                  // (P lies where S goes, and has been read when O is done)
+                    ok = has(g, 0) && has(g, L::kB) && (g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
+                    if (!ok) break;
+                    issue_s(g);
+                }
                 now = next;
                 ahead = false;
                 more = 0;
+                ok = has(g, kC);
                 if (!kStates) {
-                    ok = warp_wait(&bars->r, ph, dead) && (g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
+                    // rows of C behind the last token have been cleared; P is there; O's and I's places have been read
+                    if (now.n < kTile) ok = ok && warp_wait(&bars->z, tails++ & 1, dead);
+                    ok = ok && warp_wait(&bars->p, ph, dead) && (g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
                     if (!ok) break;
                     order_after();
                     if (elected()) {
-                        mma_rows<DB / 16>(I, a0 + at, image_rows, now.how_i, now.bd16);
-                        mma_commit(&bars->i);
-                    }
-                    __syncwarp();
-                    ok = (now.n == kTile || warp_wait(&bars->k, ph, dead)) && warp_wait(&bars->p, ph, dead);       // (rows behind the last token are cleared with B')
-                    if (!ok) break;
-                    order_after();
-                    if (elected()) {
-                        mma_tensor_cols(O, S, v0 + at, now.how_i | 1u << 16);
+                        mma_tensor_cols(O, S, cols_at(g, kC, 0), now.how_i | 1u << 16);
                         mma_commit(&bars->o);
                     }
                     __syncwarp();
-                    // S of the next chunk, where that is known and its tiles are there (P lies where it goes, and has been read when O is done).
-                    // Nothing is waited for here that might wait for this chunk's D.
+                    // S of the next chunk, where that is known and its tiles are there.  Nothing is waited for here that might wait for this chunk's D.
                     more = advance(false);
-                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[(g + 1) % kStages], ((g + 1) / kStages) & 1))) {
+                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[place(g + 1, 0)], turn(g + 1, 0)) && bar_there(&bars->full[place(g + 1, L::kB)], turn(g + 1, L::kB)))) {
                         ok = warp_wait(&bars->o, ph, dead);
                         if (!ok) break;
                         issue_s(g + 1);
                         ahead = true;
                     }
-                } else ok = warp_wait(&bars->r, ph, dead);                                                         // (D of the chunk before has been read)
-                ok = ok && warp_wait(&bars->k, ph, dead);
+                }
+                ok = ok && warp_wait(&bars->r, ph, dead);                  // (the image is there, D's place has been read)
+                if (!ok) break;
+                order_after();
+                if (!kStates && elected()) {
+                    mma_rows<DB / 16>(I, rows_at(g, 0, 0), image_rows, now.how_i, now.bd16);
+                    mma_commit(&bars->i[ph]);
+                    if (L::kB) mma_commit(&bars->empty[place(g, 0)]);
+                }
+                __syncwarp();
+                ok = warp_wait(&bars->k, ph, dead);
                 if (!ok) break;
                 order_after();
                 if (elected()) {
                     if (now.adds)
 #pragma unroll 1
                         for (int p = now.parts - 1; p >= 0; --p)           // the small parts first
-                            mma_cols(D, v0 + at, p == 0 ? ac0 + at + side : p == 1 ? ac0 + at : image_cols, now.how_d, p < now.parts - 1);
+                            mma_cols(D, cols_at(g, kC, 0), p == 0 ? cols_at(g, L::kB, L::kInA) : cols0 + (p == 1 ? L::kLow : L::kImage) / 16, now.how_d, p < now.parts - 1);
                     mma_commit(&bars->d);
-                    mma_commit(&bars->empty[s]);
+                    mma_commit(&bars->empty[place(g, L::kB)]);
+                    mma_commit(&bars->empty[place(g, kC)]);
                 }
                 __syncwarp();
                 ++w.g;
@@ -568,60 +591,72 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             float* pw = powers + (walked++ & 1) * 132;
             for (int i = lane; i <= kTile; i += 32) pw[rev ? kTile - i : i] = power(rate, i);
             __syncwarp();
-            for (int c = 0; c < chunks; ++c, ++w.g) {
-                const int ph = w.g & 1, n = w.tokens(c);
-                ok = warp_wait(&bars->s, ph, dead);
-                if (!ok) break;
+            const int first = rev ? warp : 0, end = rev ? 4 : warp + 1;
+            float off = 1.f;                                               // fp16: what brings a row of O back
+            // P of chunk g, the segment's c-th.  Group j of 32 columns of S becomes 16 words of P, which lie where group j / 2 was: in this order
+            // none is lost.  A warp's rows see groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
+            auto make_p = [&](uint32_t g, int c) {
+                if (!warp_wait(&bars->s[g & 1], g >> 1 & 1, dead)) return false;
                 order_after();
-                float on = 1.f, off = 1.f;                                 // fp16: what brings a row of P up, and of O back
-                // Group g of 32 columns of S becomes 16 words of P, which lie where group g / 2 was: in this order none is lost.  A warp's rows
-                // see groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
-                const int first = rev ? warp : 0, end = rev ? 4 : warp + 1;
-                auto faded = [&](float (&p)[32], int g) {
-                    tensor_load32(p, S + mine + 32 * g);
-                    const uint32_t f = at_shared(pw + (rev ? kTile : 0) + r - 32 * g);         // (what is not seen may lie beside the table: in shared memory all the same)
-                    float x[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[j]) : "r"(f - 4 * j));       // (asm: a load that depends on a bit of `seen` waits for the one before)
-                    tensor_load_wait();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) p[j] *= x[j];
-                    if (g == warp || 32 * g + 32 > n) {
-                        uint32_t seen = ~0u;
-                        if (g == warp) seen = rev ? ~0u << lane : (2u << lane) - 1;
-                        if (32 * g + 32 > n) seen &= n > 32 * g ? (1u << (n - 32 * g)) - 1 : 0u;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) p[j] = seen >> j & 1 ? p[j] : 0.f;
-                    }
+                const int n = w.tokens(c);
+                auto seen_of = [&](int j) {
+                    uint32_t seen = ~0u;
+                    if (j == warp) seen = rev ? ~0u << lane : (2u << lane) - 1;
+                    if (32 * j + 32 > n) seen &= n > 32 * j ? (1u << (n - 32 * j)) - 1 : 0u;
+                    return seen;
                 };
-                float p[32];
-                if (kHalfs) {
+                float p[32], on = 1.f;
+                if (kHalfs) {                                              // (before they are faded: a bound that is as good)
                     float most = 0.f;
 #pragma unroll 1
-                    for (int g = first; g < end; ++g) {
-                        faded(p, g);
+                    for (int j = first; j < end; ++j) {
+                        tensor_load32(p, S + mine + 32 * j);
+                        const uint32_t seen = seen_of(j);
+                        tensor_load_wait();
+                        if (j == warp || 32 * j + 32 > n) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) most = fmaxf(most, fabsf(p[j]));
+                            for (int e = 0; e < 32; ++e) p[e] = seen >> e & 1 ? p[e] : 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(p[e]));
                     }
                     uint8_t back;
                     on = to_middle(most, back);
                     off = from_middle(back);
                 }
 #pragma unroll 1
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t x[16] = {};
-                    if (g >= first && g < end) {
-                        faded(p, g);
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t y[16] = {};
+                    if (j >= first && j < end) {
+                        tensor_load32(p, S + mine + 32 * j);
+                        const uint32_t f = at_shared(pw + (rev ? kTile : 0) + r - 32 * j);     // (what is not seen may lie beside the table: in shared memory all the same)
+                        float x[32];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) x[j] = kHalfs ? Two<T>::pack(on * p[2 * j], on * p[2 * j + 1]) : Two<T>::pack(p[2 * j], p[2 * j + 1]);
+                        for (int e = 0; e < 32; ++e) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[e]) : "r"(f - 4 * e));       // (asm: a load that depends on a bit of `seen` waits for the one before)
+                        tensor_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) p[e] *= x[e];
+                        if (j == warp || 32 * j + 32 > n) {
+                            const uint32_t seen = seen_of(j);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) p[e] = seen >> e & 1 ? p[e] : 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = kHalfs ? Two<T>::pack(on * p[2 * e], on * p[2 * e + 1]) : Two<T>::pack(p[2 * e], p[2 * e + 1]);
                     }
-                    tensor_store16(S + mine + 16 * g, x);
+                    tensor_store16(S + mine + 16 * j, y);
                 }
                 tensor_store_wait();
                 order_before();
-                if (kHalfs) ok = warp_wait(&bars->r, ph, dead);            // (before D can be asked for, which r's next phase comes after)
                 bar_arrive(&bars->p);
-                ok = ok && warp_wait(&bars->o, ph, dead);
+                return true;
+            };
+            if (!make_p(w.g, 0)) ok = false;
+            for (int c = 0; c < chunks && ok; ++c, ++w.g) {
+                const int ph = w.g & 1, n = w.tokens(c);
+                const float back = off;
+                // the next chunk's P first: its O, and S after that, need not wait for this one's y
+                ok = (c + 1 >= chunks || make_p(w.g + 1, c + 1)) && warp_wait(&bars->i[ph], w.g >> 1 & 1, dead);
                 if (!ok) break;
                 order_after();
                 const float age = r < n ? pw[rev ? kTile - (n - 1 - r) : r] : 0.f;
@@ -634,7 +669,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     tensor_load16(m, I + mine + j0);
                     tensor_load_wait();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = kHalfs ? x[j] * off + age * (m[j] * from_middle(cs[ph * 128 + j0 + j])) : x[j] + age * m[j];
+                    for (int j = 0; j < 16; ++j) x[j] = kHalfs ? x[j] * back + age * (m[j] * from_middle(cs[ph * 128 + j0 + j])) : x[j] + age * m[j];
                     if (j0 + 8 >= cd)                                      // (the other half is none of y's)
 #pragma unroll
                         for (int j = 8; j < 16; ++j) x[j] = 0.f;
@@ -661,7 +696,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     __syncwarp();
                 }
                 if (__any_sync(~0u, !isfinite((odd[0] + odd[1]) + (odd[2] + odd[3])) && r < n))
-                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, off, kHalfs ? cs + ph * 128 : nullptr, to);
+                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
                 order_before();
                 bar_arrive(&bars->e);
             }
