@@ -14,7 +14,7 @@
 // and the output's, each half a step at most.  fp16 has few exponents: rows of P and of the image are brought to about 2^14 by a power of two,
 // which is taken off again behind the product.
 //
-// 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
+// 20 warps: four turn S into P (a thread a row), four write y, four keep the memory, four make B', one asks for tiles (TMA), one issues the
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
 // copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  From one chunk to
 // the next there are two chains: B' and D; and the memory's sum, its image and I.  P, O and the next S go beside them.
@@ -32,7 +32,7 @@
 
 namespace pcr {
 
-constexpr int kTileThreads = 512;
+constexpr int kTileThreads = 640;
 constexpr int kTile = 128;                     // tokens of a chunk
 constexpr int kHalf = 16384;                   // bytes of 128 rows of 64 elements
 
@@ -74,9 +74,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
     uint64_t begin = 0;
     for (uint32_t tries = 1;; ++tries) {
         uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 100000;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
         if (done) return true;
-        if (tries % 1024) continue;
+        if (tries % 64) continue;
         uint64_t now;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
         if (!begin) begin = now;
@@ -202,6 +202,10 @@ template <typename T> struct Factor {
         last = *reinterpret_cast<const uint32_t*>(&e);
     }
 };
+// Two 32-bit numbers at once.
+__device__ __forceinline__ void mul_add2(float& a0, float& a1, float b0, float b1, float c) {          // a = a c + b
+    asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nmov.b64 c, {%4, %4};\nfma.rn.f32x2 a, a, c, b;\nmov.b64 {%0, %1}, a;\n}" : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1), "f"(c));
+}
 // 2^14 / a power of two about as large as `most`; the exponent of what takes it off again
 __device__ __forceinline__ float to_middle(float most, uint8_t& back) {
     const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 250);
@@ -305,8 +309,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     float* powers = reinterpret_cast<float*>(sm + L::kRest);               // of the factor, 0 .. 128, of two segments
     uint8_t* cs = reinterpret_cast<uint8_t*>(powers + 2 * 132);            // fp16: what the image's columns were brought up by, two chunks
-    TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
-    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
+    uint8_t* rs = cs + 256;                                                // and the rows of P
+    TileBars* bars = reinterpret_cast<TileBars*>(rs + 256);
+    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 512 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
     volatile int* dead = &bars->dead;
 
     if (tid == 0) {
@@ -314,7 +319,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         for (uint64_t* b : {&bars->s[0], &bars->s[1], &bars->i[0], &bars->i[1], &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
         for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z}) bar_init(b, 128);
         bar_init(&bars->k, kStates ? 256 : 128);
-        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
+        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], kStates ? 14 : 18); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -403,8 +408,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
     };
 
-    if (warp >= 12) {
-        fewer_registers<56>();
+    if (warp >= 12 && warp < 16) {
+        fewer_registers<48>();
         if (warp == 12) {                                                  // copies of tiles
             const CUtensorMap* all = &G.maps.q;
             bool ok = true;
@@ -580,23 +585,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         int walked = 0;
         bool ok = !kStates;
         while (ok && w.next()) {
-            const Walk& W = A.w[w.job->kind];
-            if (A.starts && W.zero_tail) tile_tail(A, W, w.job, gridDim.x / (A.heads * A.kinds));
-            const int chunks = w.job->chunks, head = w.job->head, batch = w.job->it.batch, cd = W.cd;
+            const int chunks = w.job->chunks;
             if (chunks == 0) continue;
-            const bool rev = W.rev, y32 = W.y32, wide = W.wide;
-            const float rate = rate_of(A.log_decay, head);
+            const bool rev = A.w[w.job->kind].rev;
+            const float rate = rate_of(A.log_decay, w.job->head);
             // Powers 0 .. 128 of the factor, the other way round where the walk is, so that a row finds those of its columns in one order.
             // Every warp writes the table, all the same values; others may still be at the segment before, none at one before that.
             float* pw = powers + (walked++ & 1) * 132;
             for (int i = lane; i <= kTile; i += 32) pw[rev ? kTile - i : i] = power(rate, i);
             __syncwarp();
+            // Group j of 32 columns of S becomes 16 words of P, which lie where group j / 2 was: in this order none is lost.  A warp's rows see
+            // groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
             const int first = rev ? warp : 0, end = rev ? 4 : warp + 1;
-            float off = 1.f;                                               // fp16: what brings a row of O back
-            // P of chunk g, the segment's c-th.  Group j of 32 columns of S becomes 16 words of P, which lie where group j / 2 was: in this order
-            // none is lost.  A warp's rows see groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
-            auto make_p = [&](uint32_t g, int c) {
-                if (!warp_wait(&bars->s[g & 1], g >> 1 & 1, dead)) return false;
+            for (int c = 0; c < chunks; ++c, ++w.g) {
+                ok = warp_wait(&bars->s[w.g & 1], w.g >> 1 & 1, dead);
+                if (!ok) break;
                 order_after();
                 const int n = w.tokens(c);
                 auto seen_of = [&](int j) {
@@ -620,9 +623,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll
                         for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(p[e]));
                     }
-                    uint8_t back;
-                    on = to_middle(most, back);
-                    off = from_middle(back);
+                    on = to_middle(most, rs[(w.g & 1) * 128 + r]);
                 }
 #pragma unroll 1
                 for (int j = 0; j < 4; ++j) {
@@ -649,61 +650,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 tensor_store_wait();
                 order_before();
                 bar_arrive(&bars->p);
-                return true;
-            };
-            if (!make_p(w.g, 0)) ok = false;
-            for (int c = 0; c < chunks && ok; ++c, ++w.g) {
-                const int ph = w.g & 1, n = w.tokens(c);
-                const float back = off;
-                // the next chunk's P first: its O, and S after that, need not wait for this one's y
-                ok = (c + 1 >= chunks || make_p(w.g + 1, c + 1)) && warp_wait(&bars->i[ph], w.g >> 1 & 1, dead);
-                if (!ok) break;
-                order_after();
-                const float age = r < n ? pw[rev ? kTile - (n - 1 - r) : r] : 0.f;
-                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(w.begin(c, rev) + r) * W.ys[1] + (int64_t)head * W.ys[2];
-                float odd[4] = {};                                         // sums of all, finite where all are
-#pragma unroll 1
-                for (int j0 = 0; j0 < cd; j0 += 16) {
-                    float x[16], m[16];
-                    tensor_load16(x, O + mine + j0);
-                    tensor_load16(m, I + mine + j0);
-                    tensor_load_wait();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = kHalfs ? x[j] * back + age * (m[j] * from_middle(cs[ph * 128 + j0 + j])) : x[j] + age * m[j];
-                    if (j0 + 8 >= cd)                                      // (the other half is none of y's)
-#pragma unroll
-                        for (int j = 8; j < 16; ++j) x[j] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) odd[j & 3] += x[j];
-                    if (r < n) {
-                        if (!y32) {
-                            T* y = static_cast<T*>(W.y) + to + j0;
-                            uint32_t v[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) v[j] = Two<T>::pack(x[2 * j], x[2 * j + 1]);
-                            if (wide && j0 + 16 <= cd) store32(y, v);
-                            else {
-                                reinterpret_cast<uint4*>(y)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-                                if (j0 + 8 < cd) reinterpret_cast<uint4*>(y)[1] = make_uint4(v[4], v[5], v[6], v[7]);
-                            }
-                        } else {
-                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-                        }
-                    }
-                    __syncwarp();
-                }
-                if (__any_sync(~0u, !isfinite((odd[0] + odd[1]) + (odd[2] + odd[3])) && r < n))
-                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
-                order_before();
-                bar_arrive(&bars->e);
             }
-            if (!ok) tile_lost(W, w.job);
         }
     } else if (warp < 8) {
-        more_registers<184>();
+        more_registers<176>();
         const int r = tid - 128;                                           // an element of c
         uint8_t* image = sm + L::kImage;
         bool ok = true;
@@ -758,7 +708,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         tensor_load16(x, D + mine + i);
                         tensor_load_wait();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                        for (int e = 0; e < 16; e += 2) mul_add2(R[i + e], R[i + e + 1], x[e], x[e + 1], keep);
                     }
                 if (kHalfs && shows) {
                     float most = 0.f;
@@ -778,7 +728,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int e = 0; e < 16; ++e) x[e] = ahead[e];
                         if (i + 16 < DB && i + 16 < bd) tensor_load16(ahead, D + mine + i + 16);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                        for (int e = 0; e < 16; e += 2) mul_add2(R[i + e], R[i + e + 1], x[e], x[e + 1], keep);
                     }
                     if (shows)
 #pragma unroll
@@ -810,7 +760,71 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int e = 0; e < 8; ++e) { *to = R[i + e]; to += oi; }
             }
         }
-    } else make_parts(tid - 256, kStates ? 1 : 0);
+    } else if (warp >= 16) {
+        fewer_registers<80>();
+        const int r = tid - 512;                                           // a row of y
+        bool ok = !kStates;
+        while (ok && w.next()) {
+            const Walk& W = A.w[w.job->kind];
+            if (A.starts && W.zero_tail) tile_tail(A, W, w.job, gridDim.x / (A.heads * A.kinds));
+            const int chunks = w.job->chunks, head = w.job->head, batch = w.job->it.batch, cd = W.cd;
+            const bool rev = W.rev, y32 = W.y32, wide = W.wide;
+            const float rate = rate_of(A.log_decay, head);
+            for (int c = 0; c < chunks; ++c, ++w.g) {
+                const int ph = w.g & 1, n = w.tokens(c);
+                ok = warp_wait(&bars->i[ph], w.g >> 1 & 1, dead);          // (and O: it was issued before)
+                if (!ok) break;
+                order_after();
+                const float age = r < n ? power(rate, rev ? n - 1 - r : r) : 0.f, back = kHalfs ? from_middle(rs[ph * 128 + r]) : 1.f;
+                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(w.begin(c, rev) + r) * W.ys[1] + (int64_t)head * W.ys[2];
+                float odd[4] = {};                                         // sums of all, finite where all are
+#pragma unroll 1
+                for (int j0 = 0; j0 < cd; j0 += 16) {
+                    float x[16], m[16];
+                    tensor_load16(x, O + mine + j0);
+                    tensor_load16(m, I + mine + j0);
+                    tensor_load_wait();
+                    if (kHalfs)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) { x[j] *= back; m[j] *= from_middle(cs[ph * 128 + j0 + j]); }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] += age * m[j];
+                    if (j0 + 8 >= cd)                                      // (the other half is none of y's)
+#pragma unroll
+                        for (int j = 8; j < 16; ++j) x[j] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) odd[j & 3] += x[j];
+                    if (r < n) {
+                        if (!y32) {
+                            T* y = static_cast<T*>(W.y) + to + j0;
+                            uint32_t v[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = Two<T>::pack(x[2 * j], x[2 * j + 1]);
+                            if (wide && j0 + 16 <= cd) store32(y, v);
+                            else {
+                                reinterpret_cast<uint4*>(y)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                                if (j0 + 8 < cd) reinterpret_cast<uint4*>(y)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+                            }
+                        } else {
+                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (__any_sync(~0u, !isfinite((odd[0] + odd[1]) + (odd[2] + odd[3])) && r < n))
+                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
+                order_before();
+                bar_arrive(&bars->e);
+            }
+            if (!ok) tile_lost(W, w.job);
+        }
+    } else {
+        fewer_registers<80>();
+        make_parts(tid - 256, kStates ? 1 : 0);
+    }
     __syncwarp();
     order_before();
     __syncthreads();
