@@ -16,7 +16,8 @@
 //
 // 20 warps: four turn S into P (a thread a row), four write y, four keep the memory, four make B', one asks for tiles (TMA), one issues the
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
-// copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  From one chunk to
+// copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  y goes out through
+// shared memory (TMA): stores of a row a lane take 53 cycles each, a chunk's 1700, in which no other load or store gets through.  From one chunk to
 // the next there are two chains: B' and D; and the memory's sum, its image and I.  P, O and the next S go beside them.
 // Code is kept short and in loops where it can be: the roles' code runs side by side on every scheduler, and what is unrolled comes out of
 // the instruction caches at 4 to 8 cycles an instruction.
@@ -36,7 +37,7 @@ constexpr int kTileThreads = 640;
 constexpr int kTile = 128;                     // tokens of a chunk
 constexpr int kHalf = 16384;                   // bytes of 128 rows of 64 elements
 
-struct TileMaps { CUtensorMap q, k, v, g; };   // (element, head, token, batch): boxes of 64 elements, 128 tokens
+struct TileMaps { CUtensorMap q, k, v, g, y[3]; };     // (element, head, token, batch): boxes of 64 elements, 128 tokens; of a walk's y: 32 elements, 32 tokens
 struct TileArgs {
     TileMaps maps;
     WalkArgs walks;
@@ -44,20 +45,26 @@ struct TileArgs {
     int parts;                                 // of B'
 };
 
-// Shared memory of a CTA, from a boundary of 1024 bytes on: a ring of tiles, the memory's image, lo.  A chunk's tiles are A, B and C, one
-// place each; sizes up to 64: A and B share a place; without an S: B and C.
+// Shared memory of a CTA, from a boundary of 1024 bytes on: a ring of places of 128 rows of 64 elements, the memory's image, lo, pieces of y.
+// A chunk's tiles are A (where there is an S), B and C, of one or two places each (C always of two).  The ring's length is such that no C, and
+// no tile of two, lies across its end.  Heads of more than 64: y goes out through the image's place, which is free from I to the next image.
 template <int DB, bool kStates> struct TileShared {
-    static constexpr int kSide = DB / 64 * kHalf;              // of A, B, the image and lo
-    static constexpr int kPlaces = DB == 64 ? 6 : 5, kPer = DB == 64 || kStates ? 2 : 3, kB = kPer == 3 ? 1 : 0;
-    static constexpr int kInA = DB == 64 && !kStates ? kHalf : 0;          // where B lies in a place that it shares
-    static constexpr int kImage = kPlaces * 2 * kHalf, kLow = kImage + kSide, kRest = kLow + kSide, kBytes = kRest + 3072;
+    static constexpr int kN = DB / 64, kSide = kN * kHalf;     // places of A and B; bytes of those, of the image and lo
+    static constexpr int kTiles = kStates ? 2 : 3, kA = 0, kB = kTiles - 2, kC = kTiles - 1;
+    static constexpr int kPer = (kTiles - 1) * kN + 2, kPlaces = kPer == 3 ? 9 : 10;
+    static constexpr int kImage = kPlaces * kHalf, kLow = kImage + kSide, kOwn = DB == 64 && !kStates ? kHalf : 0, kPieces = kOwn ? kLow + kSide : kImage;
+    static constexpr int kRest = kLow + kSide + kOwn, kBytes = kRest + 3072, kWarpPieces = kOwn ? 4096 : 8192;
+    // First place of a chunk's tile, counted from the chunk's first.
+    __host__ __device__ static constexpr int first(int tile) { return tile * kN; }
+    __host__ __device__ static constexpr int tile_of(int place) { return place / kN < kC ? place / kN : kC; }
 };
+constexpr int kRing = 6;                       // tiles under way or in use at most, and more
 
 constexpr int kQueue = 3;                      // segments at work in a CTA or asked for ahead
 struct Job { int kind, head, key, chunks; Item it; };                  // kind < 0: there is none left; chunks 0: nothing to walk over
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
-    uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
+    uint64_t full[kRing], done[kRing], s[2], i[2], z, p, k, o, d, e, r, y, end, got[kQueue], taken[kQueue], answer;
     Job jobs[kQueue];
     int dead;
     uint32_t tensor;
@@ -96,6 +103,12 @@ __device__ __forceinline__ void tile_load(void* to, const CUtensorMap* map, uint
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(at_shared(to)),
                  "l"(map), "r"(at_shared(bar)), "r"(x), "r"(head), "r"(token), "r"(batch) : "memory");
 }
+// 32 rows of 32 elements out of shared memory, whose 16-byte pieces are turned by half the row's number modulo 4.
+__device__ __forceinline__ void piece_store(const CUtensorMap* map, const void* from, int x, int head, int token, int batch) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];\ncp.async.bulk.commit_group;" ::"l"(map), "r"(at_shared(from)), "r"(x), "r"(head), "r"(token), "r"(batch) : "memory");
+}
+template <int kLeft> __device__ __forceinline__ void pieces_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void pieces_written() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // Descriptors of tiles in rows of 128 bytes whose 16-byte pieces are turned by the row's number modulo 8.  Rows along the tile's own
 // dimension (M or N), 64 elements of the summed one in a row: groups of 8 rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t desc_rows(uint32_t at) { return (uint64_t)((at & 0x3ffff) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
@@ -252,9 +265,6 @@ __device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t
 
 template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
-__device__ __forceinline__ void store32(void* to, const uint32_t (&w)[8]) {       // 32 bytes, aligned
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-}
 
 // What a role of the CTA works on: segment after segment, as the queue gives them, and the chunks of each.  `g` counts chunks over all
 // of them: it gives every barrier's phase.
@@ -315,10 +325,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     volatile int* dead = &bars->dead;
 
     if (tid == 0) {
-        for (int s = 0; s < L::kPlaces; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
+        for (int s = 0; s < kRing; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->done[s], 1); }
         for (uint64_t* b : {&bars->s[0], &bars->s[1], &bars->i[0], &bars->i[1], &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
         for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z}) bar_init(b, 128);
         bar_init(&bars->k, kStates ? 256 : 128);
+        bar_init(&bars->y, 4);
         for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], kStates ? 14 : 18); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -334,11 +345,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const uint32_t tm = bars->tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
     Work w{bars};
 
-    // Tile `which` (0: A, kB: B, kPer - 1: C) of chunk g: its place, and its barriers' phase.
-    auto place = [](uint32_t g, int which) { return (g * L::kPer + which) % L::kPlaces; };
-    auto turn = [](uint32_t g, int which) { return (g * L::kPer + which) / L::kPlaces & 1; };
-    auto has = [&](uint32_t g, int which) { return warp_wait(&bars->full[place(g, which)], turn(g, which), dead); };
-    constexpr int kC = L::kPer - 1;
+    // A chunk's tile: where place `half` of it begins, and whether it is there.
+    auto place = [](uint32_t g, int tile, int half) { return (int)((g * L::kPer + L::first(tile) + half) % L::kPlaces) * kHalf; };
+    auto has = [&](uint32_t g, int tile) { const uint32_t i = g * L::kTiles + tile; return warp_wait(&bars->full[i % kRing], i / kRing & 1, dead); };
+    constexpr int kC = L::kC;
 
     // B' by the threads of a warpgroup, a token each; where two have a chunk, half of its elements.
     auto make_parts = [&](int r, int which) {
@@ -357,7 +367,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 const bool in = r < n;
                 ok = has(g, L::kB) && has(g, kC);
                 if (!ok) break;
-                uint8_t *b = sm + place(g, L::kB) * 2 * kHalf + L::kInA + r * 128, *v = sm + place(g, kC) * 2 * kHalf + r * 128;
+                uint8_t *b = sm + place(g, L::kB, 0) + r * 128, *v = sm + place(g, kC, 0) + r * 128;
                 if (n < kTile && which == 0) {                             // rows of C behind the last token, which P's zeros might not stop
                     if (!in)
 #pragma unroll 1
@@ -412,6 +422,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         fewer_registers<48>();
         if (warp == 12) {                                                  // copies of tiles
             const CUtensorMap* all = &G.maps.q;
+            uint32_t freed = 0;                                            // tiles known to be done with
             bool ok = true;
             while (ok && w.next()) {
                 const Walk& W = A.w[w.job->kind];
@@ -421,18 +432,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 for (int c = 0; c < chunks; ++c, ++w.g) {
                     const int t0 = w.begin(c, W.rev);
 #pragma unroll 1
-                    for (int which = 0; which < L::kPer; ++which) {
-                        const uint32_t at = w.g * L::kPer + which, s = at % L::kPlaces;
-                        ok = at < L::kPlaces || warp_wait(&bars->empty[s], (at / L::kPlaces - 1) & 1, dead);
+                    for (int tile = 0; tile < L::kTiles; ++tile) {
+                        const uint32_t i = w.g * L::kTiles + tile, at = w.g * L::kPer + L::first(tile);
+                        const int n = tile == kC ? 2 : L::kN;
+                        // the tile that its last place held before, and all of those before that
+                        const int64_t was = (int64_t)at + n - 1 - L::kPlaces;
+                        if (was >= 0)
+                            for (const uint32_t held = (uint32_t)was / L::kPer * L::kTiles + L::tile_of((int)((uint32_t)was % L::kPer)); ok && freed <= held; ++freed)
+                                ok = warp_wait(&bars->done[freed % kRing], freed / kRing & 1, dead);
                         if (!ok) break;
-                        uint8_t* to = sm + s * 2 * kHalf;
                         if (elected()) {
-                            const bool is_c = which == kC, is_b = which == L::kB && !is_c, is_a = !kStates && which == 0;
-                            const CUtensorMap* m = is_c ? mc : is_a ? ma : mb;
-                            const int h = is_c ? hc : is_a ? ha : hb, n = is_c ? halves : DB / 64;
-                            bar_expect(&bars->full[s], (uint32_t)(n + (DB == 64 && is_a ? 1 : 0)) * kHalf);
-                            for (int i = 0; i < n; ++i) tile_load(to + i * kHalf, m, &bars->full[s], 64 * i, h, t0, batch);
-                            if (DB == 64 && is_a && is_b) tile_load(to + L::kInA, mb, &bars->full[s], 0, hb, t0, batch);
+                            const CUtensorMap* m = tile == kC ? mc : tile == L::kB ? mb : ma;
+                            const int h = tile == kC ? hc : tile == L::kB ? hb : ha, boxes = tile == kC ? halves : n;
+                            uint64_t* bar = &bars->full[i % kRing];
+                            bar_expect(bar, (uint32_t)boxes * kHalf);
+                            for (int half = 0; half < boxes; ++half) tile_load(sm + place(w.g, tile, half), m, bar, 64 * half, h, t0, batch);
                         }
                         __syncwarp();
                     }
@@ -440,13 +454,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
             }
             volatile int again = 0;                                        // copies still under way write here: none may be left
-            const uint32_t all_of = w.g * L::kPer;
-            for (uint32_t i = all_of > L::kPlaces ? all_of - L::kPlaces : 0; i < all_of; ++i) bar_wait(&bars->full[i % L::kPlaces], (i / L::kPlaces) & 1, &again);
+            const uint32_t all_of = w.g * L::kTiles;
+            for (uint32_t i = all_of > kRing ? all_of - kRing : 0; i < all_of; ++i) bar_wait(&bars->full[i % kRing], i / kRing & 1, &again);
         } else if (warp == 13) {                                           // products
             const uint32_t how = Two<T>::kHow | 8u << 24;
             const uint64_t rows0 = desc_rows(at_shared(sm)), cols0 = desc_cols(at_shared(sm)), image_rows = rows0 + L::kImage / 16;
-            auto rows_at = [&](uint32_t g, int which, int off) { return rows0 + (uint64_t)(place(g, which) * 2 * kHalf + off) / 16; };
-            auto cols_at = [&](uint32_t g, int which, int off) { return cols0 + (uint64_t)(place(g, which) * 2 * kHalf + off) / 16; };
+            auto rows_at = [&](uint32_t g, int tile) { return rows0 + (uint64_t)place(g, tile, 0) / 16; };
+            auto cols_at = [&](uint32_t g, int tile) { return cols0 + (uint64_t)place(g, tile, 0) / 16; };
+            auto give_back = [&](uint32_t g, int tile) { mma_commit(&bars->done[(g * L::kTiles + tile) % kRing]); };
             // The chunk that comes next, of whatever segment; 0: not known yet (asked for without waiting), -1: none.
             struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } next = {}, now = {};
             int c = -1, chunks = 0, adding = 0;
@@ -470,7 +485,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             auto issue_s = [&](uint32_t g) {
                 order_after();
                 if (elected()) {
-                    mma_rows<DB / 16>(S, rows_at(g, 0, 0), rows_at(g, L::kB, L::kInA), how | 16u << 17, next.bd16);
+                    mma_rows<DB / 16>(S, rows_at(g, L::kA), rows_at(g, L::kB), how | 16u << 17, next.bd16);
                     mma_commit(&bars->s[g & 1]);
                 }
                 __syncwarp();
@@ -480,7 +495,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             while (ok && more > 0) {
                 const uint32_t g = w.g, ph = g & 1;
                 if (!kStates && !ahead) {                                  // (P lies where S goes, and has been read when O is done)
-                    ok = has(g, 0) && has(g, L::kB) && (g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
+                    ok = has(g, L::kA) && has(g, L::kB) && (g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
                     if (!ok) break;
                     issue_s(g);
                 }
@@ -495,13 +510,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     if (!ok) break;
                     order_after();
                     if (elected()) {
-                        mma_tensor_cols(O, S, cols_at(g, kC, 0), now.how_i | 1u << 16);
+                        mma_tensor_cols(O, S, cols_at(g, kC), now.how_i | 1u << 16);
                         mma_commit(&bars->o);
                     }
                     __syncwarp();
                     // S of the next chunk, where that is known and its tiles are there.  Nothing is waited for here that might wait for this chunk's D.
                     more = advance(false);
-                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[place(g + 1, 0)], turn(g + 1, 0)) && bar_there(&bars->full[place(g + 1, L::kB)], turn(g + 1, L::kB)))) {
+                    const uint32_t i = (g + 1) * L::kTiles + L::kB;            // (B comes behind A)
+                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[i % kRing], i / kRing & 1)) && has(g + 1, L::kA)) {
                         ok = warp_wait(&bars->o, ph, dead);
                         if (!ok) break;
                         issue_s(g + 1);
@@ -512,9 +528,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 if (!ok) break;
                 order_after();
                 if (!kStates && elected()) {
-                    mma_rows<DB / 16>(I, rows_at(g, 0, 0), image_rows, now.how_i, now.bd16);
+                    mma_rows<DB / 16>(I, rows_at(g, L::kA), image_rows, now.how_i, now.bd16);
                     mma_commit(&bars->i[ph]);
-                    if (L::kB) mma_commit(&bars->empty[place(g, 0)]);
+                    give_back(g, L::kA);
                 }
                 __syncwarp();
                 ok = warp_wait(&bars->k, ph, dead);
@@ -524,10 +540,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     if (now.adds)
 #pragma unroll 1
                         for (int p = now.parts - 1; p >= 0; --p)           // the small parts first
-                            mma_cols(D, cols_at(g, kC, 0), p == 0 ? cols_at(g, L::kB, L::kInA) : cols0 + (p == 1 ? L::kLow : L::kImage) / 16, now.how_d, p < now.parts - 1);
+                            mma_cols(D, cols_at(g, kC), p == 0 ? cols_at(g, L::kB) : cols0 + (p == 1 ? L::kLow : L::kImage) / 16, now.how_d, p < now.parts - 1);
                     mma_commit(&bars->d);
-                    mma_commit(&bars->empty[place(g, L::kB)]);
-                    mma_commit(&bars->empty[place(g, kC)]);
+                    give_back(g, L::kB);
+                    give_back(g, kC);
                 }
                 __syncwarp();
                 ++w.g;
@@ -699,6 +715,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
                     }
                 }
+                if (shows && !L::kOwn && w.g > 0) {                        // (y of the chunk before went out through the image's place)
+                    ok = warp_wait(&bars->y, (w.g - 1) & 1, dead);
+                    if (!ok) break;
+                }
                 float up = 1.f;
                 if (kHalfs && adds)
 #pragma unroll
@@ -768,7 +788,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const Walk& W = A.w[w.job->kind];
             if (A.starts && W.zero_tail) tile_tail(A, W, w.job, gridDim.x / (A.heads * A.kinds));
             const int chunks = w.job->chunks, head = w.job->head, batch = w.job->it.batch, cd = W.cd;
-            const bool rev = W.rev, y32 = W.y32, wide = W.wide;
+            const bool rev = W.rev, y32 = W.y32;
+            const int kind = w.job->kind;
+            // (a third part of B' takes the image's place; rows of 32 bits go as they come)
+            const bool free = !y32 && (L::kOwn || kHalfs || G.parts < 3 || !(w.job->it.last && W.last));
             const float rate = rate_of(A.log_decay, head);
             for (int c = 0; c < chunks; ++c, ++w.g) {
                 const int ph = w.g & 1, n = w.tokens(c);
@@ -776,51 +799,81 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 if (!ok) break;
                 order_after();
                 const float age = r < n ? power(rate, rev ? n - 1 - r : r) : 0.f, back = kHalfs ? from_middle(rs[ph * 128 + r]) : 1.f;
-                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(w.begin(c, rev) + r) * W.ys[1] + (int64_t)head * W.ys[2];
-                float odd[4] = {};                                         // sums of all, finite where all are
+                const int t0 = w.begin(c, rev), warp0 = (warp & 3) * 32;
+                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(t0 + r) * W.ys[1] + (int64_t)head * W.ys[2];
+                const bool pieces = free && warp0 + 32 <= n;               // (a piece has 32 rows: where some are none of the segment's, rows go one by one)
+                float odd[2] = {};                                         // sums of all, finite where all are
 #pragma unroll 1
-                for (int j0 = 0; j0 < cd; j0 += 16) {
-                    float x[16], m[16];
-                    tensor_load16(x, O + mine + j0);
-                    tensor_load16(m, I + mine + j0);
-                    tensor_load_wait();
-                    if (kHalfs)
+                for (int j0 = 0; j0 < cd; j0 += 32) {
+                    uint8_t *piece = sm + L::kPieces + (warp & 3) * L::kWarpPieces + j0 * 64 % L::kWarpPieces, *mine_of = piece + lane * 64;
+                    if (L::kOwn && pieces) {                               // (the piece before the last has been read)
+                        if (lane == 0) pieces_read<1>();
+                        __syncwarp();
+                    }
+#pragma unroll 1
+                    for (int j1 = j0; j1 < min(j0 + 32, cd); j1 += 16) {
+                        float x[16], m[16];
+                        tensor_load16(x, O + mine + j1);
+                        tensor_load16(m, I + mine + j1);
+                        uint4 up = kHalfs ? *reinterpret_cast<const uint4*>(cs + ph * 128 + j1) : make_uint4(0, 0, 0, 0);
+                        tensor_load_wait();
+                        if (kHalfs)
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) { x[j] *= back; m[j] *= from_middle(cs[ph * 128 + j0 + j]); }
+                            for (int j = 0; j < 16; ++j) { x[j] *= back; m[j] *= from_middle((&up.x)[j / 4] >> 8 * (j % 4) & 255); }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] += age * m[j];
-                    if (j0 + 8 >= cd)                                      // (the other half is none of y's)
+                        for (int j = 0; j < 16; ++j) x[j] += age * m[j];
+                        if (j1 + 8 >= cd)                                  // (the other half is none of y's)
 #pragma unroll
-                        for (int j = 8; j < 16; ++j) x[j] = 0.f;
+                            for (int j = 8; j < 16; ++j) x[j] = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) odd[j & 3] += x[j];
-                    if (r < n) {
-                        if (!y32) {
-                            T* y = static_cast<T*>(W.y) + to + j0;
-                            uint32_t v[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) v[j] = Two<T>::pack(x[2 * j], x[2 * j + 1]);
-                            if (wide && j0 + 16 <= cd) store32(y, v);
-                            else {
-                                reinterpret_cast<uint4*>(y)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-                                if (j0 + 8 < cd) reinterpret_cast<uint4*>(y)[1] = make_uint4(v[4], v[5], v[6], v[7]);
-                            }
-                        } else {
-                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
+                        for (int j = 0; j < 16; ++j) odd[j & 1] += x[j];
+                        if (y32) {
+                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j1);
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                if (j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                                if (r < n && j1 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                        } else {
+                            uint4 v[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                v[e] = make_uint4(Two<T>::pack(x[8 * e], x[8 * e + 1]), Two<T>::pack(x[8 * e + 2], x[8 * e + 3]), Two<T>::pack(x[8 * e + 4], x[8 * e + 5]), Two<T>::pack(x[8 * e + 6], x[8 * e + 7]));
+                            uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(W.y) + to + j1);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                if (pieces) *reinterpret_cast<uint4*>(mine_of + (((j1 - j0) / 8 + e) ^ (lane >> 1 & 3)) * 16) = v[e];
+                                else if (r < n && j1 + 8 * e < cd) y[e] = v[e];
+                            }
                         }
+                    }
+                    if (pieces) {
+                        order_shared();
+                        __syncwarp();
+                        if (lane == 0) piece_store(&G.maps.y[kind], piece, j0, head, t0 + warp0, batch);
+                    }
+                }
+                __syncwarp();
+                if (__any_sync(~0u, !isfinite(odd[0] + odd[1]) && r < n)) {
+                    if (lane == 0) pieces_written();                       // (what follows is written over it)
+                    __syncwarp();
+                    careful<T>(W, batch, head, t0, n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
+                }
+                order_before();
+                bar_arrive(&bars->e);
+                if (!L::kOwn) {                                            // the image's place has been read
+                    if (lane == 0) {
+                        pieces_read<0>();
+                        bar_arrive(&bars->y);
                     }
                     __syncwarp();
                 }
-                if (__any_sync(~0u, !isfinite((odd[0] + odd[1]) + (odd[2] + odd[3])) && r < n))
-                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
-                order_before();
-                bar_arrive(&bars->e);
             }
-            if (!ok) tile_lost(W, w.job);
+            if (!ok) {
+                if (lane == 0) pieces_written();
+                __syncwarp();
+                tile_lost(W, w.job);
+            }
         }
+        if (lane == 0) pieces_written();
     } else {
         fewer_registers<80>();
         make_parts(tid - 256, kStates ? 1 : 0);
