@@ -18,7 +18,7 @@
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
 // copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  y goes out through
 // shared memory (TMA): stores of a row a lane take 53 cycles each, a chunk's 1700, in which no other load or store gets through.  From one chunk to
-// the next there are two chains: B' and D; and the memory's sum, its image and I.  P, O and the next S go beside them.
+// the next there are two chains: B' and D; and the memory's sum, its image and I.
 // Code is kept short and in loops where it can be: the roles' code runs side by side on every scheduler, and what is unrolled comes out of
 // the instruction caches at 4 to 8 cycles an instruction.
 //
@@ -90,12 +90,6 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         if (now - begin > 2000000000ull) *dead = 1;
         if (*dead) return false;
     }
-}
-// Whether that phase has ended.
-__device__ __forceinline__ bool bar_there(uint64_t* b, uint32_t parity) {
-    uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
-    return done;
 }
 // The same for a whole warp: all of its lanes go on, together, or none.
 __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead) { return __all_sync(~0u, bar_wait(b, parity, dead)); }
@@ -285,8 +279,6 @@ struct Work {
         job = bars->jobs + at % kQueue;
         return job->kind >= 0;
     }
-    // Whether next() would not wait.
-    __device__ __forceinline__ bool ready() const { return __all_sync(~0u, bar_there(&bars->got[(at + 1) % kQueue], ((at + 1) / kQueue) & 1)); }
     // A chunk's first token and its tokens.
     __device__ __forceinline__ int tokens(int c) const { return min(kTile, job->it.n - c * kTile); }
     __device__ __forceinline__ int begin(int c, bool rev) const {
@@ -365,7 +357,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             for (int c = 0; c < chunks; ++c, ++g) {
                 const int n = w.tokens(c);
                 const bool in = r < n;
-                ok = has(g, L::kB) && has(g, kC);
+                ok = has(g, L::kB) && (n == kTile || has(g, kC));
                 if (!ok) break;
                 uint8_t *b = sm + place(g, L::kB, 0) + r * 128, *v = sm + place(g, kC, 0) + r * 128;
                 if (n < kTile && which == 0) {                             // rows of C behind the last token, which P's zeros might not stop
@@ -380,35 +372,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 if (!ok) break;
                 if (c < adding) {
                     const Factor<T> f(in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f);
-                    // pieces of 8 elements, four (or two) at a time: a piece is a load, a dozen dependent steps and two or three stores
+                    // pieces of 8 elements, a few at a time: a piece is a load, a dozen dependent steps and two or three stores
                     auto all = [&](auto how) {
-                        constexpr int kTimes = decltype(how)::value ? 2 : 4;
-#pragma unroll 1
-                        for (int i = from; i < end; i += kTimes) {
-                            uint4 q[kTimes];
-                            int at[kTimes];
+#pragma unroll decltype(how)::value ? 2 : 4
+                        for (int i = from; i < end; ++i) {
+                            const int at = (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16;
+                            uint4 q = *reinterpret_cast<const uint4*>(b + at), lo, last;
+                            uint32_t *pq = &q.x, *pl = &lo.x, *pt = &last.x;
 #pragma unroll
-                            for (int u = 0; u < kTimes; ++u) {
-                                at[u] = ((i + u) >> 3) * kHalf + (((i + u) & 7) ^ (r & 7)) * 16;
-                                q[u] = make_uint4(0, 0, 0, 0);
-                                if (in && i + u < end) q[u] = *reinterpret_cast<const uint4*>(b + at[u]);
+                            for (int e = 0; e < 4; ++e) {
+                                if (decltype(how)::value) f.three(pq[e], pl[e], pt[e]);
+                                else f.two(pq[e], pl[e]);
                             }
-#pragma unroll
-                            for (int u = 0; u < kTimes; ++u) {
-                                uint4 lo, last;
-                                uint32_t *pq = &q[u].x, *pl = &lo.x, *pt = &last.x;
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    if (decltype(how)::value) f.three(pq[e], pl[e], pt[e]);
-                                    else f.two(pq[e], pl[e]);
-                                }
-                                if (i + u >= end) continue;
-                                *reinterpret_cast<uint4*>(b + at[u]) = q[u];
-                                *reinterpret_cast<uint4*>(low + at[u]) = lo;
-                                if (decltype(how)::value) *reinterpret_cast<uint4*>(image + at[u]) = last;
-                            }
+                            *reinterpret_cast<uint4*>(b + at) = q;
+                            *reinterpret_cast<uint4*>(low + at) = lo;
+                            if (decltype(how)::value) *reinterpret_cast<uint4*>(image + at) = last;
                         }
                     };
+                    if (!in)                                               // (no product with 0: what stands there might be anything)
+#pragma unroll 1
+                        for (int i = from; i < end; ++i) *reinterpret_cast<uint4*>(b + (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16) = make_uint4(0, 0, 0, 0);
                     if (three) all(std::true_type());
                     else all(std::false_type());
                 }
@@ -462,51 +445,55 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             auto rows_at = [&](uint32_t g, int tile) { return rows0 + (uint64_t)place(g, tile, 0) / 16; };
             auto cols_at = [&](uint32_t g, int tile) { return cols0 + (uint64_t)place(g, tile, 0) / 16; };
             auto give_back = [&](uint32_t g, int tile) { mma_commit(&bars->done[(g * L::kTiles + tile) % kRing]); };
-            // The chunk that comes next, of whatever segment; 0: not known yet (asked for without waiting), -1: none.
-            struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } next = {}, now = {};
+            // The chunk that comes next, of whatever segment.
+            struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } now = {};
             int c = -1, chunks = 0, adding = 0;
-            auto advance = [&](bool wait) {
+            auto advance = [&] {
                 while (++c >= chunks) {
-                    --c;
-                    if (!wait && !w.ready()) return 0;
-                    if (!w.next()) return -1;
+                    if (!w.next()) return false;
                     const Walk& W = A.w[w.job->kind];
                     const bool given = kStates || (w.job->it.last && W.last);
                     c = -1; chunks = w.job->chunks; adding = given ? chunks : chunks - 1;
-                    next.bd16 = (uint32_t)(W.bd + 15) / 16;
-                    next.how_i = how | 2 * ((uint32_t)(W.cd + 15) / 16) << 17;
-                    next.how_d = how | 1u << 15 | 1u << 16 | 2 * next.bd16 << 17;
-                    next.parts = given ? G.parts : 2;
+                    now.bd16 = (uint32_t)(W.bd + 15) / 16;
+                    now.how_i = how | 2 * ((uint32_t)(W.cd + 15) / 16) << 17;
+                    now.how_d = how | 1u << 15 | 1u << 16 | 2 * now.bd16 << 17;
+                    now.parts = given ? G.parts : 2;
                 }
-                next.n = w.tokens(c);
-                next.adds = c < adding;
-                return 1;
+                now.n = w.tokens(c);
+                now.adds = c < adding;
+                return true;
             };
             auto issue_s = [&](uint32_t g) {
                 order_after();
                 if (elected()) {
-                    mma_rows<DB / 16>(S, rows_at(g, L::kA), rows_at(g, L::kB), how | 16u << 17, next.bd16);
+                    mma_rows<DB / 16>(S, rows_at(g, L::kA), rows_at(g, L::kB), how | 16u << 17, now.bd16);
                     mma_commit(&bars->s[g & 1]);
                 }
                 __syncwarp();
             };
-            bool ok = true, ahead = false;                                 // ahead: S has been issued
-            int more = advance(true), tails = 0;
-            while (ok && more > 0) {
+            bool ok = true;
+            int tails = 0;
+            while (ok && advance()) {
                 const uint32_t g = w.g, ph = g & 1;
-                if (!kStates && !ahead) {                                  // (P lies where S goes, and has been read when O is done)
+                if (!kStates) {                                            // (P lies where S goes, and has been read when O is done)
                     ok = has(g, L::kA) && has(g, L::kB) && (g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
                     if (!ok) break;
                     issue_s(g);
                 }
-                now = next;
-                ahead = false;
-                more = 0;
-                ok = has(g, kC);
+                                // the image is there, D's place has been read, O's and I's too
+                ok = warp_wait(&bars->r, ph, dead) && (kStates || g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
+                if (!ok) break;
+                order_after();
                 if (!kStates) {
-                    // rows of C behind the last token have been cleared; P is there; O's and I's places have been read
-                    if (now.n < kTile) ok = ok && warp_wait(&bars->z, tails++ & 1, dead);
-                    ok = ok && warp_wait(&bars->p, ph, dead) && (g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
+                    // I first: with it A's place goes back to the ring, where this segment's C of the next chunk waits for it
+                    if (elected()) {
+                        mma_rows<DB / 16>(I, rows_at(g, L::kA), image_rows, now.how_i, now.bd16);
+                        mma_commit(&bars->i[ph]);
+                        give_back(g, L::kA);
+                    }
+                    __syncwarp();
+                    // P is there, and rows of C behind the last token have been cleared
+                    ok = has(g, kC) && warp_wait(&bars->p, ph, dead) && (now.n == kTile || warp_wait(&bars->z, tails++ & 1, dead));
                     if (!ok) break;
                     order_after();
                     if (elected()) {
@@ -514,26 +501,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         mma_commit(&bars->o);
                     }
                     __syncwarp();
-                    // S of the next chunk, where that is known and its tiles are there.  Nothing is waited for here that might wait for this chunk's D.
-                    more = advance(false);
-                    const uint32_t i = (g + 1) * L::kTiles + L::kB;            // (B comes behind A)
-                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[i % kRing], i / kRing & 1)) && has(g + 1, L::kA)) {
-                        ok = warp_wait(&bars->o, ph, dead);
-                        if (!ok) break;
-                        issue_s(g + 1);
-                        ahead = true;
-                    }
-                }
-                ok = ok && warp_wait(&bars->r, ph, dead);                  // (the image is there, D's place has been read)
-                if (!ok) break;
-                order_after();
-                if (!kStates && elected()) {
-                    mma_rows<DB / 16>(I, rows_at(g, L::kA), image_rows, now.how_i, now.bd16);
-                    mma_commit(&bars->i[ph]);
-                    give_back(g, L::kA);
-                }
-                __syncwarp();
-                ok = warp_wait(&bars->k, ph, dead);
+                } else ok = has(g, kC);
+                ok = ok && warp_wait(&bars->k, ph, dead);
                 if (!ok) break;
                 order_after();
                 if (elected()) {
@@ -547,7 +516,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
                 __syncwarp();
                 ++w.g;
-                if (more == 0) more = advance(true);
             }
             volatile int again = 0;
             if (elected()) mma_commit(&bars->end);
@@ -703,7 +671,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
             for (int c = 0; c <= chunks && chunks > 0; ++c) {
                 // the memory behind chunk c - 1, and its image for chunk c
-                const bool adds = c > 0 && c <= adding, shows = !kStates && c < chunks;
+                const bool adds = c > 0 && c <= adding;
                 float keep = 1.f;
                 if (c > 0) {
                     ok = warp_wait(&bars->d, w.g & 1, dead);
@@ -715,33 +683,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
                     }
                 }
-                if (shows && !L::kOwn && w.g > 0) {                        // (y of the chunk before went out through the image's place)
-                    ok = warp_wait(&bars->y, (w.g - 1) & 1, dead);
-                    if (!ok) break;
-                }
-                float up = 1.f;
-                if (kHalfs && adds)
+                if (adds) {
+                    float ahead[16];
+                    tensor_load16(ahead, D + mine);
 #pragma unroll
                     for (int i = 0; i < DB; i += 16) {
                         if (i >= bd) continue;                             // (nothing was put there)
-                        float x[16];
-                        tensor_load16(x, D + mine + i);
-                        tensor_load_wait();
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) mul_add2(R[i + e], R[i + e + 1], x[e], x[e + 1], keep);
-                    }
-                if (kHalfs && shows) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
-                    up = to_middle(most, cs[(w.g & 1) * 128 + r]);
-                }
-                float ahead[16];
-                if (!kHalfs && adds) tensor_load16(ahead, D + mine);
-#pragma unroll
-                for (int i = 0; i < DB; i += 16) {
-                    if (i >= bd) continue;
-                    if (!kHalfs && adds) {
                         float x[16];
                         tensor_load_wait();
 #pragma unroll
@@ -750,16 +697,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll
                         for (int e = 0; e < 16; e += 2) mul_add2(R[i + e], R[i + e + 1], x[e], x[e + 1], keep);
                     }
-                    if (shows)
-#pragma unroll
-                        for (int e = 0; e < 16; e += 8) {
-                            uint4 x;
-                            x.x = Two<T>::pack(up * R[i + e], up * R[i + e + 1]); x.y = Two<T>::pack(up * R[i + e + 2], up * R[i + e + 3]);
-                            x.z = Two<T>::pack(up * R[i + e + 4], up * R[i + e + 5]); x.w = Two<T>::pack(up * R[i + e + 6], up * R[i + e + 7]);
-                            *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + ((((i + e) >> 3) & 7) ^ (r & 7)) * 16) = x;
-                        }
                 }
                 if (c == chunks) break;
+                if (!kStates) {
+                    if (!L::kOwn && w.g > 0) ok = warp_wait(&bars->y, (w.g - 1) & 1, dead);       // (y of the chunk before went out through the image's place)
+                    if (!ok) break;
+                    float up = 1.f;
+                    if (kHalfs) {
+                        float most = 0.f;
+#pragma unroll
+                        for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
+                        up = to_middle(most, cs[(w.g & 1) * 128 + r]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < DB; i += 8) {
+                        if (i >= (bd + 15 & ~15)) continue;                // (whole steps of I's sum, zeros behind the memory's own)
+                        uint4 x;
+                        if (kHalfs)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) (&x.x)[e] = Two<T>::pack(up * R[i + 2 * e], up * R[i + 2 * e + 1]);
+                        else
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) (&x.x)[e] = Two<T>::pack(R[i + 2 * e], R[i + 2 * e + 1]);
+                        *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16) = x;
+                    }
+                }
                 order_shared();
                 order_before();
                 bar_arrive(&bars->r);
@@ -781,7 +743,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             }
         }
     } else if (warp >= 16) {
-        fewer_registers<80>();
         const int r = tid - 512;                                           // a row of y
         bool ok = !kStates;
         while (ok && w.next()) {
@@ -795,64 +756,62 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const float rate = rate_of(A.log_decay, head);
             for (int c = 0; c < chunks; ++c, ++w.g) {
                 const int ph = w.g & 1, n = w.tokens(c);
-                ok = warp_wait(&bars->i[ph], w.g >> 1 & 1, dead);          // (and O: it was issued before)
+                ok = warp_wait(&bars->o, ph, dead);                        // (and I: it was issued before)
                 if (!ok) break;
                 order_after();
                 const float age = r < n ? power(rate, rev ? n - 1 - r : r) : 0.f, back = kHalfs ? from_middle(rs[ph * 128 + r]) : 1.f;
                 const int t0 = w.begin(c, rev), warp0 = (warp & 3) * 32;
                 const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(t0 + r) * W.ys[1] + (int64_t)head * W.ys[2];
                 const bool pieces = free && warp0 + 32 <= n;               // (a piece has 32 rows: where some are none of the segment's, rows go one by one)
-                float odd[2] = {};                                         // sums of all, finite where all are
+                typename Two<T>::Pair odd[2] = {Two<T>::twice(0.f), Two<T>::twice(0.f)};     // 0 times all, 0 where all are finite
 #pragma unroll 1
                 for (int j0 = 0; j0 < cd; j0 += 32) {
-                    uint8_t *piece = sm + L::kPieces + (warp & 3) * L::kWarpPieces + j0 * 64 % L::kWarpPieces, *mine_of = piece + lane * 64;
-                    if (L::kOwn && pieces) {                               // (the piece before the last has been read)
-                        if (lane == 0) pieces_read<1>();
-                        __syncwarp();
-                    }
-#pragma unroll 1
-                    for (int j1 = j0; j1 < min(j0 + 32, cd); j1 += 16) {
-                        float x[16], m[16];
-                        tensor_load16(x, O + mine + j1);
-                        tensor_load16(m, I + mine + j1);
-                        uint4 up = kHalfs ? *reinterpret_cast<const uint4*>(cs + ph * 128 + j1) : make_uint4(0, 0, 0, 0);
-                        tensor_load_wait();
-                        if (kHalfs)
+                    float x[32], m[32];
+                    tensor_load32(x, O + mine + j0);
+                    tensor_load32(m, I + mine + j0);
+                    if (L::kOwn && pieces && lane == 0) pieces_read<1>();  // (the piece before the last has been read)
+                    tensor_load_wait();
+                    if (kHalfs)
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) { x[j] *= back; m[j] *= from_middle((&up.x)[j / 4] >> 8 * (j % 4) & 255); }
+                        for (int j = 0; j < 32; j += 16) {
+                            const uint4 up = *reinterpret_cast<const uint4*>(cs + ph * 128 + j0 + j);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) x[j] += age * m[j];
-                        if (j1 + 8 >= cd)                                  // (the other half is none of y's)
-#pragma unroll
-                            for (int j = 8; j < 16; ++j) x[j] = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) odd[j & 1] += x[j];
-                        if (y32) {
-                            float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j1);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (r < n && j1 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-                        } else {
-                            uint4 v[2];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                v[e] = make_uint4(Two<T>::pack(x[8 * e], x[8 * e + 1]), Two<T>::pack(x[8 * e + 2], x[8 * e + 3]), Two<T>::pack(x[8 * e + 4], x[8 * e + 5]), Two<T>::pack(x[8 * e + 6], x[8 * e + 7]));
-                            uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(W.y) + to + j1);
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                if (pieces) *reinterpret_cast<uint4*>(mine_of + (((j1 - j0) / 8 + e) ^ (lane >> 1 & 3)) * 16) = v[e];
-                                else if (r < n && j1 + 8 * e < cd) y[e] = v[e];
-                            }
+                            for (int e = 0; e < 16; ++e) { x[j + e] *= back; m[j + e] *= from_middle((&up.x)[e / 4] >> 8 * (e % 4) & 255); }
                         }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] += age * m[j];
+                    if (y32) {
+                        float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (r < n && j0 + 4 * e < cd) y[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
                     }
+                    uint32_t v[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] = Two<T>::pack(x[2 * j], x[2 * j + 1]);
+                    if (j0 + 32 > cd)                                      // (what lies behind the head is none of y's)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] = j0 + 2 * j < cd ? v[j] : 0u;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) odd[j & 1] = __hfma2(*reinterpret_cast<const typename Two<T>::Pair*>(&v[j]), Two<T>::twice(0.f), odd[j & 1]);
                     if (pieces) {
+                        uint8_t *piece = sm + L::kPieces + (warp & 3) * L::kWarpPieces + j0 * 64 % L::kWarpPieces, *mine_of = piece + lane * 64;
+                        if (L::kOwn) __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(mine_of + (e ^ (lane >> 1 & 3)) * 16) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                         order_shared();
                         __syncwarp();
                         if (lane == 0) piece_store(&G.maps.y[kind], piece, j0, head, t0 + warp0, batch);
+                    } else if (!y32) {
+                        uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(W.y) + to + j0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (r < n && j0 + 8 * e < cd) y[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                     }
                 }
                 __syncwarp();
-                if (__any_sync(~0u, !isfinite(odd[0] + odd[1]) && r < n)) {
+                odd[0] = __hadd2(odd[0], odd[1]);
+                if (__any_sync(~0u, !(__low2float(odd[0]) == 0.f && __high2float(odd[0]) == 0.f) && r < n)) {
                     if (lane == 0) pieces_written();                       // (what follows is written over it)
                     __syncwarp();
                     careful<T>(W, batch, head, t0, n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
@@ -875,7 +834,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
         if (lane == 0) pieces_written();
     } else {
-        fewer_registers<80>();
+        fewer_registers<64>();
         make_parts(tid - 256, kStates ? 1 : 0);
     }
     __syncwarp();
