@@ -35,15 +35,14 @@ bool fits(const pcr_rows& r, int64_t batch, int64_t tokens, int heads) {
     return true;
 }
 
-// `piece`: what y goes out in, 32 rows of 32 elements; else what operands come in by.
-bool map_of(CUtensorMap* m, const pcr_rows& r, const pcr_decay_args& a, int heads, int dim, bool piece) {
+bool map_of(CUtensorMap* m, const pcr_rows& r, const pcr_decay_args& a, int heads, int dim) {
     const cuuint64_t size[4] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)a.tokens, (cuuint64_t)a.batch};
     const int64_t st[3] = {r.stride[2], r.stride[1], r.stride[0]};
     cuuint64_t step[3];
     for (int i = 0; i < 3; ++i) step[i] = size[i + 1] > 1 ? (cuuint64_t)st[i] * 2 : 256;       // (a single one has no step)
-    const cuuint32_t box[4] = {piece ? 32u : 64u, 1, piece ? 32u : (cuuint32_t)kTile, 1}, each[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)kTile, 1}, each[4] = {1, 1, 1, 1};
     return encoder()(m, a.dtype == PCR_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(r.at), size, step, box, each,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, piece ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int DB, bool kStates>
@@ -80,14 +79,11 @@ int launch_tiles(const WalkArgs& walks, const int (*of)[3], const pcr_decay_args
     G.parts = parts;
     for (int i = 0; i < 3; ++i) {
         for (int j = 0; j < 3; ++j) G.of[i][j] = of[i][j];
+        Walk& w = G.walks.w[i];
+        w.wide = reinterpret_cast<uintptr_t>(w.y) % 32 == 0 && w.ys[0] % 16 == 0 && w.ys[1] % 16 == 0 && w.ys[2] % 16 == 0;
     }
-    if (!map_of(&G.maps.q, a.q, a, a.q_heads, a.k_dim, false) || !map_of(&G.maps.k, a.k, a, a.k_heads, a.k_dim, false) || !map_of(&G.maps.v, a.v, a, a.k_heads, a.v_dim, false) ||
-        !map_of(&G.maps.g, a.out, a, a.q_heads, a.v_dim, false)) return PCR_E_CUDA;
-    for (int i = 0; i < walks.kinds; ++i) {
-        const Walk& w = walks.w[i];
-        const pcr_rows y = {w.y, {w.ys[0], w.ys[1], w.ys[2]}};
-        if (!walks.states && !w.y32 && !map_of(&G.maps.y[i], y, a, a.q_heads, w.cd, true)) return PCR_E_CUDA;
-    }
+    if (!map_of(&G.maps.q, a.q, a, a.q_heads, a.k_dim) || !map_of(&G.maps.k, a.k, a, a.k_heads, a.k_dim) || !map_of(&G.maps.v, a.v, a, a.k_heads, a.v_dim) ||
+        !map_of(&G.maps.g, a.out, a, a.q_heads, a.v_dim)) return PCR_E_CUDA;
     return a.dtype == PCR_F16 ? launch_sizes<__half>(G, keys, st) : launch_sizes<__nv_bfloat16>(G, keys, st);
 }
 

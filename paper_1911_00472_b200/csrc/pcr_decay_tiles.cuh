@@ -14,11 +14,10 @@
 // and the output's, each half a step at most.  fp16 has few exponents: rows of P and of the image are brought to about 2^14 by a power of two,
 // which is taken off again behind the product.
 //
-// 20 warps: four turn S into P (a thread a row), four write y, four keep the memory, four make B', one asks for tiles (TMA), one issues the
+// 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
-// copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  y goes out through
-// shared memory (TMA): stores of a row a lane take 53 cycles each, a chunk's 1700, in which no other load or store gets through.  From one chunk to
-// the next there are two chains: B' and D; and the memory's sum, its image and I.
+// copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  From one chunk to
+// the next there are two chains: B' and D; and the memory's sum, its image and I.  P, O and the next S go beside them.
 // Code is kept short and in loops where it can be: the roles' code runs side by side on every scheduler, and what is unrolled comes out of
 // the instruction caches at 4 to 8 cycles an instruction.
 //
@@ -33,11 +32,11 @@
 
 namespace pcr {
 
-constexpr int kTileThreads = 640;
+constexpr int kTileThreads = 512;
 constexpr int kTile = 128;                     // tokens of a chunk
 constexpr int kHalf = 16384;                   // bytes of 128 rows of 64 elements
 
-struct TileMaps { CUtensorMap q, k, v, g, y[3]; };     // (element, head, token, batch): boxes of 64 elements, 128 tokens; of a walk's y: 32 elements, 32 tokens
+struct TileMaps { CUtensorMap q, k, v, g; };   // (element, head, token, batch): boxes of 64 elements, 128 tokens
 struct TileArgs {
     TileMaps maps;
     WalkArgs walks;
@@ -45,26 +44,20 @@ struct TileArgs {
     int parts;                                 // of B'
 };
 
-// Shared memory of a CTA, from a boundary of 1024 bytes on: a ring of places of 128 rows of 64 elements, the memory's image, lo, pieces of y.
-// A chunk's tiles are A (where there is an S), B and C, of one or two places each (C always of two).  The ring's length is such that no C, and
-// no tile of two, lies across its end.  Heads of more than 64: y goes out through the image's place, which is free from I to the next image.
+// Shared memory of a CTA, from a boundary of 1024 bytes on: a ring of tiles, the memory's image, lo.  A chunk's tiles are A, B and C, one
+// place each; sizes up to 64: A and B share a place; without an S: B and C.
 template <int DB, bool kStates> struct TileShared {
-    static constexpr int kN = DB / 64, kSide = kN * kHalf;     // places of A and B; bytes of those, of the image and lo
-    static constexpr int kTiles = kStates ? 2 : 3, kA = 0, kB = kTiles - 2, kC = kTiles - 1;
-    static constexpr int kPer = (kTiles - 1) * kN + 2, kPlaces = kPer == 3 ? 9 : 10;
-    static constexpr int kImage = kPlaces * kHalf, kLow = kImage + kSide, kOwn = DB == 64 && !kStates ? kHalf : 0, kPieces = kOwn ? kLow + kSide : kImage;
-    static constexpr int kRest = kLow + kSide + kOwn, kBytes = kRest + 3072, kWarpPieces = kOwn ? 4096 : 8192;
-    // First place of a chunk's tile, counted from the chunk's first.
-    __host__ __device__ static constexpr int first(int tile) { return tile * kN; }
-    __host__ __device__ static constexpr int tile_of(int place) { return place / kN < kC ? place / kN : kC; }
+    static constexpr int kSide = DB / 64 * kHalf;              // of A, B, the image and lo
+    static constexpr int kPlaces = DB == 64 ? 6 : 5, kPer = DB == 64 || kStates ? 2 : 3, kB = kPer == 3 ? 1 : 0;
+    static constexpr int kInA = DB == 64 && !kStates ? kHalf : 0;          // where B lies in a place that it shares
+    static constexpr int kImage = kPlaces * 2 * kHalf, kLow = kImage + kSide, kRest = kLow + kSide, kBytes = kRest + 3072;
 };
-constexpr int kRing = 6;                       // tiles under way or in use at most, and more
 
 constexpr int kQueue = 3;                      // segments at work in a CTA or asked for ahead
-struct Job { int kind, head, key, chunks; Item it; };                  // kind < 0: there is none left; chunks 0: nothing to walk over
+struct Job { int kind, head, key, chunks, tail; float rate; Item it; };      // kind < 0: there is none left; chunks 0: nothing to walk over; tail: rows of no sequence
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
-    uint64_t full[kRing], done[kRing], s[2], i[2], z, p, k, o, d, e, r, y, end, got[kQueue], taken[kQueue], answer;
+    uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
     Job jobs[kQueue];
     int dead;
     uint32_t tensor;
@@ -81,9 +74,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
     uint64_t begin = 0;
     for (uint32_t tries = 1;; ++tries) {
         uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 100000;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
         if (done) return true;
-        if (tries % 64) continue;
+        if (tries % 1024) continue;
         uint64_t now;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
         if (!begin) begin = now;
@@ -91,18 +84,18 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         if (*dead) return false;
     }
 }
+// Whether that phase has ended.
+__device__ __forceinline__ bool bar_there(uint64_t* b, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at_shared(b)), "r"(parity) : "memory");
+    return done;
+}
 // The same for a whole warp: all of its lanes go on, together, or none.
 __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead) { return __all_sync(~0u, bar_wait(b, parity, dead)); }
 __device__ __forceinline__ void tile_load(void* to, const CUtensorMap* map, uint64_t* bar, int x, int head, int token, int batch) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(at_shared(to)),
                  "l"(map), "r"(at_shared(bar)), "r"(x), "r"(head), "r"(token), "r"(batch) : "memory");
 }
-// 32 rows of 32 elements out of shared memory, whose 16-byte pieces are turned by half the row's number modulo 4.
-__device__ __forceinline__ void piece_store(const CUtensorMap* map, const void* from, int x, int head, int token, int batch) {
-    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];\ncp.async.bulk.commit_group;" ::"l"(map), "r"(at_shared(from)), "r"(x), "r"(head), "r"(token), "r"(batch) : "memory");
-}
-template <int kLeft> __device__ __forceinline__ void pieces_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
-__device__ __forceinline__ void pieces_written() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // Descriptors of tiles in rows of 128 bytes whose 16-byte pieces are turned by the row's number modulo 8.  Rows along the tile's own
 // dimension (M or N), 64 elements of the summed one in a row: groups of 8 rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t desc_rows(uint32_t at) { return (uint64_t)((at & 0x3ffff) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
@@ -209,10 +202,6 @@ template <typename T> struct Factor {
         last = *reinterpret_cast<const uint32_t*>(&e);
     }
 };
-// Two 32-bit numbers at once.
-__device__ __forceinline__ void mul_add2(float& a0, float& a1, float b0, float b1, float c) {          // a = a c + b
-    asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nmov.b64 c, {%4, %4};\nfma.rn.f32x2 a, a, c, b;\nmov.b64 {%0, %1}, a;\n}" : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1), "f"(c));
-}
 // 2^14 / a power of two about as large as `most`; the exponent of what takes it off again
 __device__ __forceinline__ float to_middle(float most, uint8_t& back) {
     const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 250);
@@ -259,6 +248,9 @@ __device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t
 
 template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+__device__ __forceinline__ void store32(void* to, const uint32_t (&w)[8]) {       // 32 bytes, aligned
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
 
 // What a role of the CTA works on: segment after segment, as the queue gives them, and the chunks of each.  `g` counts chunks over all
 // of them: it gives every barrier's phase.
@@ -279,6 +271,8 @@ struct Work {
         job = bars->jobs + at % kQueue;
         return job->kind >= 0;
     }
+    // Whether next() would not wait.
+    __device__ __forceinline__ bool ready() const { return __all_sync(~0u, bar_there(&bars->got[(at + 1) % kQueue], ((at + 1) / kQueue) & 1)); }
     // A chunk's first token and its tokens.
     __device__ __forceinline__ int tokens(int c) const { return min(kTile, job->it.n - c * kTile); }
     __device__ __forceinline__ int begin(int c, bool rev) const {
@@ -311,18 +305,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     float* powers = reinterpret_cast<float*>(sm + L::kRest);               // of the factor, 0 .. 128, of two segments
     uint8_t* cs = reinterpret_cast<uint8_t*>(powers + 2 * 132);            // fp16: what the image's columns were brought up by, two chunks
-    uint8_t* rs = cs + 256;                                                // and the rows of P
-    TileBars* bars = reinterpret_cast<TileBars*>(rs + 256);
-    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 512 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
+    TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
+    static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
     volatile int* dead = &bars->dead;
 
     if (tid == 0) {
-        for (int s = 0; s < kRing; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->done[s], 1); }
+        for (int s = 0; s < L::kPlaces; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
         for (uint64_t* b : {&bars->s[0], &bars->s[1], &bars->i[0], &bars->i[1], &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
         for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z}) bar_init(b, 128);
         bar_init(&bars->k, kStates ? 256 : 128);
-        bar_init(&bars->y, 4);
-        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], kStates ? 14 : 18); }
+        for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -337,10 +329,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const uint32_t tm = bars->tensor, S = tm, O = tm + 128, I = tm + 256, D = tm + 384, mine = (uint32_t)(warp & 3) << 21;       // (a warp's 32 lanes)
     Work w{bars};
 
-    // A chunk's tile: where place `half` of it begins, and whether it is there.
-    auto place = [](uint32_t g, int tile, int half) { return (int)((g * L::kPer + L::first(tile) + half) % L::kPlaces) * kHalf; };
-    auto has = [&](uint32_t g, int tile) { const uint32_t i = g * L::kTiles + tile; return warp_wait(&bars->full[i % kRing], i / kRing & 1, dead); };
-    constexpr int kC = L::kC;
+    // Tile `which` (0: A, kB: B, kPer - 1: C) of chunk g: its place, and its barriers' phase.
+    auto place = [](uint32_t g, int which) { return (g * L::kPer + which) % L::kPlaces; };
+    auto turn = [](uint32_t g, int which) { return (g * L::kPer + which) / L::kPlaces & 1; };
+    auto has = [&](uint32_t g, int which) { return warp_wait(&bars->full[place(g, which)], turn(g, which), dead); };
+    constexpr int kC = L::kPer - 1;
 
     // B' by the threads of a warpgroup, a token each; where two have a chunk, half of its elements.
     auto make_parts = [&](int r, int which) {
@@ -350,7 +343,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         while (ok && w.next()) {
             const int chunks = w.job->chunks;
             const Walk& W = A.w[w.job->kind];
-            const float rate = rate_of(A.log_decay, w.job->head);
+            const float rate = w.job->rate;
             const bool rev = W.rev, given = kStates || (w.job->it.last && W.last), three = !kHalfs && given && G.parts > 2;
             const int adding = given ? chunks : chunks - 1, pieces = (W.bd + 15) / 16 * 2;
             const int from = kStates && which ? pieces / 2 : 0, end = kStates && !which ? pieces / 2 : pieces;
@@ -359,7 +352,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 const bool in = r < n;
                 ok = has(g, L::kB) && (n == kTile || has(g, kC));
                 if (!ok) break;
-                uint8_t *b = sm + place(g, L::kB, 0) + r * 128, *v = sm + place(g, kC, 0) + r * 128;
+                uint8_t *b = sm + place(g, L::kB) * 2 * kHalf + L::kInA + r * 128, *v = sm + place(g, kC) * 2 * kHalf + r * 128;
                 if (n < kTile && which == 0) {                             // rows of C behind the last token, which P's zeros might not stop
                     if (!in)
 #pragma unroll 1
@@ -401,11 +394,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
     };
 
-    if (warp >= 12 && warp < 16) {
-        fewer_registers<48>();
+    if (warp >= 12) {
+        fewer_registers<56>();
         if (warp == 12) {                                                  // copies of tiles
             const CUtensorMap* all = &G.maps.q;
-            uint32_t freed = 0;                                            // tiles known to be done with
             bool ok = true;
             while (ok && w.next()) {
                 const Walk& W = A.w[w.job->kind];
@@ -415,21 +407,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 for (int c = 0; c < chunks; ++c, ++w.g) {
                     const int t0 = w.begin(c, W.rev);
 #pragma unroll 1
-                    for (int tile = 0; tile < L::kTiles; ++tile) {
-                        const uint32_t i = w.g * L::kTiles + tile, at = w.g * L::kPer + L::first(tile);
-                        const int n = tile == kC ? 2 : L::kN;
-                        // the tile that its last place held before, and all of those before that
-                        const int64_t was = (int64_t)at + n - 1 - L::kPlaces;
-                        if (was >= 0)
-                            for (const uint32_t held = (uint32_t)was / L::kPer * L::kTiles + L::tile_of((int)((uint32_t)was % L::kPer)); ok && freed <= held; ++freed)
-                                ok = warp_wait(&bars->done[freed % kRing], freed / kRing & 1, dead);
+                    for (int which = 0; which < L::kPer; ++which) {
+                        const uint32_t at = w.g * L::kPer + which, s = at % L::kPlaces;
+                        ok = at < L::kPlaces || warp_wait(&bars->empty[s], (at / L::kPlaces - 1) & 1, dead);
                         if (!ok) break;
+                        uint8_t* to = sm + s * 2 * kHalf;
                         if (elected()) {
-                            const CUtensorMap* m = tile == kC ? mc : tile == L::kB ? mb : ma;
-                            const int h = tile == kC ? hc : tile == L::kB ? hb : ha, boxes = tile == kC ? halves : n;
-                            uint64_t* bar = &bars->full[i % kRing];
-                            bar_expect(bar, (uint32_t)boxes * kHalf);
-                            for (int half = 0; half < boxes; ++half) tile_load(sm + place(w.g, tile, half), m, bar, 64 * half, h, t0, batch);
+                            const bool is_c = which == kC, is_b = which == L::kB && !is_c, is_a = !kStates && which == 0;
+                            const CUtensorMap* m = is_c ? mc : is_a ? ma : mb;
+                            const int h = is_c ? hc : is_a ? ha : hb, n = is_c ? halves : DB / 64;
+                            bar_expect(&bars->full[s], (uint32_t)(n + (DB == 64 && is_a ? 1 : 0)) * kHalf);
+                            for (int i = 0; i < n; ++i) tile_load(to + i * kHalf, m, &bars->full[s], 64 * i, h, t0, batch);
+                            if (DB == 64 && is_a && is_b) tile_load(to + L::kInA, mb, &bars->full[s], 0, hb, t0, batch);
                         }
                         __syncwarp();
                     }
@@ -437,85 +426,98 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
             }
             volatile int again = 0;                                        // copies still under way write here: none may be left
-            const uint32_t all_of = w.g * L::kTiles;
-            for (uint32_t i = all_of > kRing ? all_of - kRing : 0; i < all_of; ++i) bar_wait(&bars->full[i % kRing], i / kRing & 1, &again);
+            const uint32_t all_of = w.g * L::kPer;
+            for (uint32_t i = all_of > L::kPlaces ? all_of - L::kPlaces : 0; i < all_of; ++i) bar_wait(&bars->full[i % L::kPlaces], (i / L::kPlaces) & 1, &again);
         } else if (warp == 13) {                                           // products
             const uint32_t how = Two<T>::kHow | 8u << 24;
             const uint64_t rows0 = desc_rows(at_shared(sm)), cols0 = desc_cols(at_shared(sm)), image_rows = rows0 + L::kImage / 16;
-            auto rows_at = [&](uint32_t g, int tile) { return rows0 + (uint64_t)place(g, tile, 0) / 16; };
-            auto cols_at = [&](uint32_t g, int tile) { return cols0 + (uint64_t)place(g, tile, 0) / 16; };
-            auto give_back = [&](uint32_t g, int tile) { mma_commit(&bars->done[(g * L::kTiles + tile) % kRing]); };
-            // The chunk that comes next, of whatever segment.
-            struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } now = {};
+            auto rows_at = [&](uint32_t g, int which, int off) { return rows0 + (uint64_t)(place(g, which) * 2 * kHalf + off) / 16; };
+            auto cols_at = [&](uint32_t g, int which, int off) { return cols0 + (uint64_t)(place(g, which) * 2 * kHalf + off) / 16; };
+            // The chunk that comes next, of whatever segment; 0: not known yet (asked for without waiting), -1: none.
+            struct { uint32_t how_i, how_d, bd16; int n, parts; bool adds; } next = {}, now = {};
             int c = -1, chunks = 0, adding = 0;
-            auto advance = [&] {
+            auto advance = [&](bool wait) {
                 while (++c >= chunks) {
-                    if (!w.next()) return false;
+                    --c;
+                    if (!wait && !w.ready()) return 0;
+                    if (!w.next()) return -1;
                     const Walk& W = A.w[w.job->kind];
                     const bool given = kStates || (w.job->it.last && W.last);
                     c = -1; chunks = w.job->chunks; adding = given ? chunks : chunks - 1;
-                    now.bd16 = (uint32_t)(W.bd + 15) / 16;
-                    now.how_i = how | 2 * ((uint32_t)(W.cd + 15) / 16) << 17;
-                    now.how_d = how | 1u << 15 | 1u << 16 | 2 * now.bd16 << 17;
-                    now.parts = given ? G.parts : 2;
+                    next.bd16 = (uint32_t)(W.bd + 15) / 16;
+                    next.how_i = how | 2 * ((uint32_t)(W.cd + 15) / 16) << 17;
+                    next.how_d = how | 1u << 15 | 1u << 16 | 2 * next.bd16 << 17;
+                    next.parts = given ? G.parts : 2;
                 }
-                now.n = w.tokens(c);
-                now.adds = c < adding;
-                return true;
+                next.n = w.tokens(c);
+                next.adds = c < adding;
+                return 1;
             };
             auto issue_s = [&](uint32_t g) {
                 order_after();
                 if (elected()) {
-                    mma_rows<DB / 16>(S, rows_at(g, L::kA), rows_at(g, L::kB), how | 16u << 17, now.bd16);
+                    mma_rows<DB / 16>(S, rows_at(g, 0, 0), rows_at(g, L::kB, L::kInA), how | 16u << 17, next.bd16);
                     mma_commit(&bars->s[g & 1]);
                 }
                 __syncwarp();
             };
-            bool ok = true;
-            int tails = 0;
-            while (ok && advance()) {
+            bool ok = true, ahead = false;                                 // ahead: S has been issued
+            int more = advance(true), tails = 0;
+            while (ok && more > 0) {
                 const uint32_t g = w.g, ph = g & 1;
-                if (!kStates) {                                            // (P lies where S goes, and has been read when O is done)
-                    ok = has(g, L::kA) && has(g, L::kB) && (g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
+                if (!kStates && !ahead) {                                  // (P lies where S goes, and has been read when O is done)
+                    ok = has(g, 0) && has(g, L::kB) && (g == 0 || warp_wait(&bars->o, ph ^ 1, dead));
                     if (!ok) break;
                     issue_s(g);
                 }
-                                // the image is there, D's place has been read, O's and I's too
-                ok = warp_wait(&bars->r, ph, dead) && (kStates || g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
-                if (!ok) break;
-                order_after();
+                now = next;
+                ahead = false;
+                more = 0;
+                ok = has(g, kC);
                 if (!kStates) {
-                    // I first: with it A's place goes back to the ring, where this segment's C of the next chunk waits for it
-                    if (elected()) {
-                        mma_rows<DB / 16>(I, rows_at(g, L::kA), image_rows, now.how_i, now.bd16);
-                        mma_commit(&bars->i[ph]);
-                        give_back(g, L::kA);
-                    }
-                    __syncwarp();
-                    // P is there, and rows of C behind the last token have been cleared
-                    ok = has(g, kC) && warp_wait(&bars->p, ph, dead) && (now.n == kTile || warp_wait(&bars->z, tails++ & 1, dead));
+                    // rows of C behind the last token have been cleared; P is there; O's and I's places have been read
+                    if (now.n < kTile) ok = ok && warp_wait(&bars->z, tails++ & 1, dead);
+                    ok = ok && warp_wait(&bars->p, ph, dead) && (g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
                     if (!ok) break;
                     order_after();
                     if (elected()) {
-                        mma_tensor_cols(O, S, cols_at(g, kC), now.how_i | 1u << 16);
+                        mma_tensor_cols(O, S, cols_at(g, kC, 0), now.how_i | 1u << 16);
                         mma_commit(&bars->o);
                     }
                     __syncwarp();
-                } else ok = has(g, kC);
-                ok = ok && warp_wait(&bars->k, ph, dead);
+                    // S of the next chunk, where that is known and its tiles are there.  Nothing is waited for here that might wait for this chunk's D.
+                    more = advance(false);
+                    if (more > 0 && __all_sync(~0u, bar_there(&bars->full[place(g + 1, 0)], turn(g + 1, 0)) && bar_there(&bars->full[place(g + 1, L::kB)], turn(g + 1, L::kB)))) {
+                        ok = warp_wait(&bars->o, ph, dead);
+                        if (!ok) break;
+                        issue_s(g + 1);
+                        ahead = true;
+                    }
+                }
+                ok = ok && warp_wait(&bars->r, ph, dead);                  // (the image is there, D's place has been read)
+                if (!ok) break;
+                order_after();
+                if (!kStates && elected()) {
+                    mma_rows<DB / 16>(I, rows_at(g, 0, 0), image_rows, now.how_i, now.bd16);
+                    mma_commit(&bars->i[ph]);
+                    if (L::kB) mma_commit(&bars->empty[place(g, 0)]);
+                }
+                __syncwarp();
+                ok = warp_wait(&bars->k, ph, dead);
                 if (!ok) break;
                 order_after();
                 if (elected()) {
                     if (now.adds)
 #pragma unroll 1
                         for (int p = now.parts - 1; p >= 0; --p)           // the small parts first
-                            mma_cols(D, cols_at(g, kC), p == 0 ? cols_at(g, L::kB) : cols0 + (p == 1 ? L::kLow : L::kImage) / 16, now.how_d, p < now.parts - 1);
+                            mma_cols(D, cols_at(g, kC, 0), p == 0 ? cols_at(g, L::kB, L::kInA) : cols0 + (p == 1 ? L::kLow : L::kImage) / 16, now.how_d, p < now.parts - 1);
                     mma_commit(&bars->d);
-                    give_back(g, L::kB);
-                    give_back(g, kC);
+                    mma_commit(&bars->empty[place(g, L::kB)]);
+                    mma_commit(&bars->empty[place(g, kC)]);
                 }
                 __syncwarp();
                 ++w.g;
+                if (more == 0) more = advance(true);
             }
             volatile int again = 0;
             if (elected()) mma_commit(&bars->end);
@@ -526,12 +528,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                               (__ldg(A.starts) > 0 || __ldg(A.starts + A.sequences) < (int64_t)A.tokens);          // rows of no sequence that become 0
             int x = blockIdx.x, i = 0;
             for (uint32_t asked = 0;; ++asked) {
-                Job j = {-1, 0, 0, 0, {}};
+                Job j = {-1, 0, 0, 0, tail, 0.f, {}};
                 if (x >= 0) {
                     const int rest = x / A.kinds;
                     j.kind = x - rest * A.kinds;
                     j.key = rest / A.heads;
                     j.head = rest - j.key * A.heads;
+                    j.rate = rate_of(A.log_decay, j.head);
                     const bool is = item_of(A, A.w[j.kind].rev, j.key, j.it);
                     if (!is) j.it.len = -1;
                     j.chunks = is && !(kStates && j.it.last) ? (j.it.n + kTile - 1) / kTile : 0;
@@ -569,21 +572,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         int walked = 0;
         bool ok = !kStates;
         while (ok && w.next()) {
-            const int chunks = w.job->chunks;
+            const Walk& W = A.w[w.job->kind];
+            if (w.job->tail) tile_tail(A, W, w.job, gridDim.x / (A.heads * A.kinds));
+            const int chunks = w.job->chunks, head = w.job->head, batch = w.job->it.batch, cd = W.cd;
             if (chunks == 0) continue;
-            const bool rev = A.w[w.job->kind].rev;
-            const float rate = rate_of(A.log_decay, w.job->head);
+            const bool rev = W.rev, y32 = W.y32, wide = W.wide;
+            const float rate = w.job->rate;
             // Powers 0 .. 128 of the factor, the other way round where the walk is, so that a row finds those of its columns in one order.
             // Every warp writes the table, all the same values; others may still be at the segment before, none at one before that.
             float* pw = powers + (walked++ & 1) * 132;
             for (int i = lane; i <= kTile; i += 32) pw[rev ? kTile - i : i] = power(rate, i);
             __syncwarp();
-            // Group j of 32 columns of S becomes 16 words of P, which lie where group j / 2 was: in this order none is lost.  A warp's rows see
-            // groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
             const int first = rev ? warp : 0, end = rev ? 4 : warp + 1;
-            for (int c = 0; c < chunks; ++c, ++w.g) {
-                ok = warp_wait(&bars->s[w.g & 1], w.g >> 1 & 1, dead);
-                if (!ok) break;
+            float off = 1.f;                                               // fp16: what brings a row of O back
+            // P of chunk g, the segment's c-th.  Group j of 32 columns of S becomes 16 words of P, which lie where group j / 2 was: in this order
+            // none is lost.  A warp's rows see groups up to (or from) their own; what a row does not see is replaced, not multiplied by 0.
+            auto make_p = [&](uint32_t g, int c) {
+                if (!warp_wait(&bars->s[g & 1], g >> 1 & 1, dead)) return false;
                 order_after();
                 const int n = w.tokens(c);
                 auto seen_of = [&](int j) {
@@ -607,7 +612,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll
                         for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(p[e]));
                     }
-                    on = to_middle(most, rs[(w.g & 1) * 128 + r]);
+                    uint8_t back;
+                    on = to_middle(most, back);
+                    off = from_middle(back);
                 }
 #pragma unroll 1
                 for (int j = 0; j < 4; ++j) {
@@ -634,142 +641,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 tensor_store_wait();
                 order_before();
                 bar_arrive(&bars->p);
-            }
-        }
-    } else if (warp < 8) {
-        more_registers<176>();
-        const int r = tid - 128;                                           // an element of c
-        uint8_t* image = sm + L::kImage;
-        bool ok = true;
-        while (ok && w.next()) {
-            const volatile Job& j = *w.job;
-            const Walk& W = A.w[j.kind];
-            if (j.it.len < 0 || (kStates && j.it.last)) continue;
-            const int bd = W.bd, chunks = j.chunks, head = j.head;
-            const bool on = r < W.cd, last = j.it.last, rev = W.rev;
-            const size_t of = (size_t)bd * W.cd;
-            const float rate = rate_of(A.log_decay, head);
-            float R[DB];
-            {
-                const float* from = nullptr;
-                int64_t fi = 0;
-                float age = 1.f;
-                if (!kStates && on) {
-                    if (j.it.m > 0) { from = W.slots + ((size_t)(j.it.slot - 1) * A.heads + head) * of + r * W.sj; fi = W.si; }
-                    else if (W.first) { from = W.first + ((size_t)j.it.seq * A.heads + head) * of + r * W.fj; fi = W.fi; age = rev || j.it.len == 0 ? 1.f : power(rate, 1); }
-                }
-#pragma unroll
-                for (int i = 0; i < DB; i += 8) {
-                    const bool there = from && i < bd;                     // (sizes are multiples of 8)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        R[i + e] = there ? age * *from : 0.f;
-                        if (there) from += fi;
-                    }
-                }
-            }
-            const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
-            for (int c = 0; c <= chunks && chunks > 0; ++c) {
-                // the memory behind chunk c - 1, and its image for chunk c
-                const bool adds = c > 0 && c <= adding;
-                float keep = 1.f;
-                if (c > 0) {
-                    ok = warp_wait(&bars->d, w.g & 1, dead);
-                    if (!ok) break;
-                    ++w.g;
-                    if (adds) {
-                        order_after();
-                        const int n = w.tokens(c - 1);
-                        keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
-                    }
-                }
-                if (adds) {
-                    float ahead[16];
-                    tensor_load16(ahead, D + mine);
-#pragma unroll
-                    for (int i = 0; i < DB; i += 16) {
-                        if (i >= bd) continue;                             // (nothing was put there)
-                        float x[16];
-                        tensor_load_wait();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = ahead[e];
-                        if (i + 16 < DB && i + 16 < bd) tensor_load16(ahead, D + mine + i + 16);
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) mul_add2(R[i + e], R[i + e + 1], x[e], x[e + 1], keep);
-                    }
-                }
-                if (c == chunks) break;
-                if (!kStates) {
-                    if (!L::kOwn && w.g > 0) ok = warp_wait(&bars->y, (w.g - 1) & 1, dead);       // (y of the chunk before went out through the image's place)
-                    if (!ok) break;
-                    float up = 1.f;
-                    if (kHalfs) {
-                        float most = 0.f;
-#pragma unroll
-                        for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
-                        up = to_middle(most, cs[(w.g & 1) * 128 + r]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < DB; i += 8) {
-                        if (i >= (bd + 15 & ~15)) continue;                // (whole steps of I's sum, zeros behind the memory's own)
-                        uint4 x;
-                        if (kHalfs)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) (&x.x)[e] = Two<T>::pack(up * R[i + 2 * e], up * R[i + 2 * e + 1]);
-                        else
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) (&x.x)[e] = Two<T>::pack(R[i + 2 * e], R[i + 2 * e + 1]);
-                        *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + (((i >> 3) & 7) ^ (r & 7)) * 16) = x;
-                    }
-                }
-                order_shared();
-                order_before();
-                bar_arrive(&bars->r);
-            }
-            float* out = nullptr;
-            int64_t oi = 0;
-            if (kStates) { out = W.slots + ((size_t)j.it.slot * A.heads + head) * of + r * W.sj; oi = W.si; }
-            else if (last && W.last) { out = W.last + ((size_t)j.it.seq * A.heads + head) * of + r * W.lj; oi = W.li; }
-            if (!ok)
-#pragma unroll
-                for (int i = 0; i < DB; ++i) R[i] = __int_as_float(0x7fc00000);
-            if (out && on) {
-                volatile float* to = out;                                  // (volatile: one address after the other, not all at once)
-#pragma unroll
-                for (int i = 0; i < DB; i += 8)
-                    if (i < bd)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) { *to = R[i + e]; to += oi; }
-            }
-        }
-    } else if (warp >= 16) {
-        const int r = tid - 512;                                           // a row of y
-        bool ok = !kStates;
-        while (ok && w.next()) {
-            const Walk& W = A.w[w.job->kind];
-            if (A.starts && W.zero_tail) tile_tail(A, W, w.job, gridDim.x / (A.heads * A.kinds));
-            const int chunks = w.job->chunks, head = w.job->head, batch = w.job->it.batch, cd = W.cd;
-            const bool rev = W.rev, y32 = W.y32;
-            const int kind = w.job->kind;
-            // (a third part of B' takes the image's place; rows of 32 bits go as they come)
-            const bool free = !y32 && (L::kOwn || kHalfs || G.parts < 3 || !(w.job->it.last && W.last));
-            const float rate = rate_of(A.log_decay, head);
-            for (int c = 0; c < chunks; ++c, ++w.g) {
+                return true;
+            };
+            if (!make_p(w.g, 0)) ok = false;
+            for (int c = 0; c < chunks && ok; ++c, ++w.g) {
                 const int ph = w.g & 1, n = w.tokens(c);
-                ok = warp_wait(&bars->o, ph, dead);                        // (and I: it was issued before)
+                const float back = off;
+                // the next chunk's P first: its O, and S after that, need not wait for this one's y
+                ok = (c + 1 >= chunks || make_p(w.g + 1, c + 1)) && warp_wait(&bars->i[ph], w.g >> 1 & 1, dead);
                 if (!ok) break;
                 order_after();
-                const float age = r < n ? power(rate, rev ? n - 1 - r : r) : 0.f, back = kHalfs ? from_middle(rs[ph * 128 + r]) : 1.f;
-                const int t0 = w.begin(c, rev), warp0 = (warp & 3) * 32;
-                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(t0 + r) * W.ys[1] + (int64_t)head * W.ys[2];
-                const bool pieces = free && warp0 + 32 <= n;               // (a piece has 32 rows: where some are none of the segment's, rows go one by one)
+                const float age = r < n ? pw[rev ? kTile - (n - 1 - r) : r] : 0.f;
+                const int64_t to = (int64_t)batch * W.ys[0] + (int64_t)(w.begin(c, rev) + r) * W.ys[1] + (int64_t)head * W.ys[2];
                 typename Two<T>::Pair odd[2] = {Two<T>::twice(0.f), Two<T>::twice(0.f)};     // 0 times all, 0 where all are finite
 #pragma unroll 1
                 for (int j0 = 0; j0 < cd; j0 += 32) {
                     float x[32], m[32];
                     tensor_load32(x, O + mine + j0);
                     tensor_load32(m, I + mine + j0);
-                    if (L::kOwn && pieces && lane == 0) pieces_read<1>();  // (the piece before the last has been read)
                     tensor_load_wait();
                     if (kHalfs)
 #pragma unroll
@@ -794,49 +683,139 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int j = 0; j < 16; ++j) v[j] = j0 + 2 * j < cd ? v[j] : 0u;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) odd[j & 1] = __hfma2(*reinterpret_cast<const typename Two<T>::Pair*>(&v[j]), Two<T>::twice(0.f), odd[j & 1]);
-                    if (pieces) {
-                        uint8_t *piece = sm + L::kPieces + (warp & 3) * L::kWarpPieces + j0 * 64 % L::kWarpPieces, *mine_of = piece + lane * 64;
-                        if (L::kOwn) __syncwarp();
+                    if (!y32 && r < n) {
+                        T* y = static_cast<T*>(W.y) + to + j0;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(mine_of + (e ^ (lane >> 1 & 3)) * 16) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-                        order_shared();
-                        __syncwarp();
-                        if (lane == 0) piece_store(&G.maps.y[kind], piece, j0, head, t0 + warp0, batch);
-                    } else if (!y32) {
-                        uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(W.y) + to + j0);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (r < n && j0 + 8 * e < cd) y[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                        for (int e = 0; e < 2; ++e) {
+                            uint32_t (&u)[8] = *reinterpret_cast<uint32_t (*)[8]>(v + 8 * e);
+                            if (wide && j0 + 16 * e + 16 <= cd) store32(y + 16 * e, u);
+                            else {
+                                if (j0 + 16 * e < cd) reinterpret_cast<uint4*>(y)[2 * e] = make_uint4(u[0], u[1], u[2], u[3]);
+                                if (j0 + 16 * e + 8 < cd) reinterpret_cast<uint4*>(y)[2 * e + 1] = make_uint4(u[4], u[5], u[6], u[7]);
+                            }
+                        }
                     }
-                }
-                __syncwarp();
-                odd[0] = __hadd2(odd[0], odd[1]);
-                if (__any_sync(~0u, !(__low2float(odd[0]) == 0.f && __high2float(odd[0]) == 0.f) && r < n)) {
-                    if (lane == 0) pieces_written();                       // (what follows is written over it)
                     __syncwarp();
-                    careful<T>(W, batch, head, t0, n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
                 }
+                odd[0] = __hadd2(odd[0], odd[1]);
+                if (__any_sync(~0u, !(__low2float(odd[0]) == 0.f && __high2float(odd[0]) == 0.f) && r < n))
+                    careful<T>(W, batch, head, w.begin(c, rev), n, r, rate, age, O + mine, I + mine, back, kHalfs ? cs + ph * 128 : nullptr, to);
                 order_before();
                 bar_arrive(&bars->e);
-                if (!L::kOwn) {                                            // the image's place has been read
-                    if (lane == 0) {
-                        pieces_read<0>();
-                        bar_arrive(&bars->y);
+            }
+            if (!ok) tile_lost(W, w.job);
+        }
+    } else if (warp < 8) {
+        more_registers<184>();
+        const int r = tid - 128;                                           // an element of c
+        uint8_t* image = sm + L::kImage;
+        bool ok = true;
+        while (ok && w.next()) {
+            const volatile Job& j = *w.job;
+            const Walk& W = A.w[j.kind];
+            if (j.it.len < 0 || (kStates && j.it.last)) continue;
+            const int bd = W.bd, chunks = j.chunks, head = j.head;
+            const bool on = r < W.cd, last = j.it.last, rev = W.rev;
+            const size_t of = (size_t)bd * W.cd;
+            const float rate = w.job->rate;
+            float R[DB];
+            {
+                const float* from = nullptr;
+                int64_t fi = 0;
+                float age = 1.f;
+                if (!kStates && on) {
+                    if (j.it.m > 0) { from = W.slots + ((size_t)(j.it.slot - 1) * A.heads + head) * of + r * W.sj; fi = W.si; }
+                    else if (W.first) { from = W.first + ((size_t)j.it.seq * A.heads + head) * of + r * W.fj; fi = W.fi; age = rev || j.it.len == 0 ? 1.f : power(rate, 1); }
+                }
+#pragma unroll
+                for (int i = 0; i < DB; ++i) R[i] = 0.f;
+                if (!kStates && (j.it.m > 0 || W.first))
+#pragma unroll
+                for (int i = 0; i < DB; i += 8) {
+                    const bool there = from && i < bd;                     // (sizes are multiples of 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (there) { R[i + e] = age * *from; from += fi; }
                     }
-                    __syncwarp();
                 }
             }
-            if (!ok) {
-                if (lane == 0) pieces_written();
-                __syncwarp();
-                tile_lost(W, w.job);
+            const int adding = chunks - (kStates || (last && W.last) ? 0 : 1);
+            for (int c = 0; c <= chunks && chunks > 0; ++c) {
+                // the memory behind chunk c - 1, and its image for chunk c
+                const bool adds = c > 0 && c <= adding, shows = !kStates && c < chunks;
+                float keep = 1.f;
+                if (c > 0) {
+                    ok = warp_wait(&bars->d, w.g & 1, dead);
+                    if (!ok) break;
+                    ++w.g;
+                    if (adds) {
+                        order_after();
+                        const int n = w.tokens(c - 1);
+                        keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
+                    }
+                }
+                float up = 1.f;
+                if (kHalfs && adds)
+#pragma unroll
+                    for (int i = 0; i < DB; i += 16) {
+                        if (i >= bd) continue;                             // (nothing was put there)
+                        float x[16];
+                        tensor_load16(x, D + mine + i);
+                        tensor_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                    }
+                if (kHalfs && shows) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
+                    up = to_middle(most, cs[(w.g & 1) * 128 + r]);
+                }
+                float ahead[16];
+                if (!kHalfs && adds) tensor_load16(ahead, D + mine);
+#pragma unroll
+                for (int i = 0; i < DB; i += 16) {
+                    if (i >= bd) continue;
+                    if (!kHalfs && adds) {
+                        float x[16];
+                        tensor_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = ahead[e];
+                        if (i + 16 < DB && i + 16 < bd) tensor_load16(ahead, D + mine + i + 16);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                    }
+                    if (shows)
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8) {
+                            uint4 x;
+                            x.x = Two<T>::pack(up * R[i + e], up * R[i + e + 1]); x.y = Two<T>::pack(up * R[i + e + 2], up * R[i + e + 3]);
+                            x.z = Two<T>::pack(up * R[i + e + 4], up * R[i + e + 5]); x.w = Two<T>::pack(up * R[i + e + 6], up * R[i + e + 7]);
+                            *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + ((((i + e) >> 3) & 7) ^ (r & 7)) * 16) = x;
+                        }
+                }
+                if (c == chunks) break;
+                order_shared();
+                order_before();
+                bar_arrive(&bars->r);
+            }
+            float* out = nullptr;
+            int64_t oi = 0;
+            if (kStates) { out = W.slots + ((size_t)j.it.slot * A.heads + head) * of + r * W.sj; oi = W.si; }
+            else if (last && W.last) { out = W.last + ((size_t)j.it.seq * A.heads + head) * of + r * W.lj; oi = W.li; }
+            if (!ok)
+#pragma unroll
+                for (int i = 0; i < DB; ++i) R[i] = __int_as_float(0x7fc00000);
+            if (out && on) {
+                volatile float* to = out;                                  // (volatile: one address after the other, not all at once)
+#pragma unroll
+                for (int i = 0; i < DB; i += 8)
+                    if (i < bd)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { *to = R[i + e]; to += oi; }
             }
         }
-        if (lane == 0) pieces_written();
-    } else {
-        fewer_registers<64>();
-        make_parts(tid - 256, kStates ? 1 : 0);
-    }
+    } else make_parts(tid - 256, kStates ? 1 : 0);
     __syncwarp();
     order_before();
     __syncthreads();

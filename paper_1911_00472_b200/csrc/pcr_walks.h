@@ -37,7 +37,7 @@ struct Walk {
     float* slots;                              // memories of segments: element (i, j) of (slot, head) at (...) bd cd + i si + j sj
     int64_t fi, fj, li, lj, si, sj;
     int bd, cd;                                // size of a's and b's heads, and of c's and y's
-    int rev, y32, zero_tail;                   // y32: y is in 32 bits whatever the operands are
+    int rev, y32, wide, zero_tail;             // y32: y is in 32 bits whatever the operands are; wide: 16-bit rows of y begin at 32 bytes
 };
 
 struct WalkArgs {
