@@ -99,14 +99,34 @@ void launch_axes(const BiasArgs& A, dim3 grid, size_t shared, cudaStream_t st) {
 template <typename T>
 int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
+    // All combinations of buckets first, where 44 KB hold them for four heads at least and there are more pairs for every CTA than lines.
+    int64_t lines = 1;
+    for (int a = 0; a < A.axes; ++a) lines *= A.buckets + 1;
+    const int64_t most = 44 * 1024 / (4 * (int64_t)sizeof(T) * (lines + 1)) * 4;
+    if (most >= 4 && (A.axes == 1 || (int64_t)A.batch * A.nq * A.nk >= lines * 2 * sm_count())) {
+        const int64_t columns = A.nk + (!wide && sizeof(T) == 2 ? 1 : 0);         // (a row's first pair of columns may begin before it)
+        A.tiles = (int)((columns + 32 * V - 1) / (32 * V));
+        A.lines = (int)lines;
+        const int64_t ctas = ((int64_t)A.batch * A.nq * A.tiles + 7) / 8, room = 4 * sm_count();
+        int group = (int)std::min<int64_t>((A.heads + 3) / 4 * 4, most);
+        while (group > 4 && ctas * ((A.heads + group - 1) / group) < 2 * sm_count()) group = (group / 2 + 3) / 4 * 4;
+        A.group = group;
+        const int groups = (A.heads + group - 1) / group;
+        const dim3 grid((unsigned)std::min<int64_t>(ctas, std::max<int64_t>(1, room / groups)), groups);
+        const size_t shared = (size_t)group * (lines + 1) * sizeof(T);
+        if (wide) bias_joint_kernel<T, true><<<grid, kBiasThreads, shared, st>>>(A);
+        else bias_joint_kernel<T, false><<<grid, kBiasThreads, shared, st>>>(A);
+        ++g_launches;
+        return finish();
+    }
     A.tiles = (A.nk + 32 * V - 1) / (32 * V);
     const int64_t ctas = ((int64_t)A.nq * A.tiles + 7) / 8;
-    const int lines = A.axes * (A.buckets + 1);
+    const int held = A.axes * (A.buckets + 1);
     // Heads of a CTA: as many as 40 KB of table hold, fewer where that leaves SMs without work
-    int group = std::max(4, std::min((A.heads + 3) / 4 * 4, 40 * 1024 / (16 * lines) * 4));
+    int group = std::max(4, std::min((A.heads + 3) / 4 * 4, 40 * 1024 / (16 * held) * 4));
     while (group > 4 && ctas * A.batch * ((A.heads + group - 1) / group) < 2 * sm_count()) group = (group / 2 + 3) / 4 * 4;
     A.group = group;
-    const size_t shared = (size_t)group * lines * 4;
+    const size_t shared = (size_t)group * held * 4;
     const dim3 grid((unsigned)ctas, (A.heads + group - 1) / group, A.batch);
     if (wide) launch_axes<T, V, true>(A, grid, shared, st);
     else launch_axes<T, V, false>(A, grid, shared, st);
@@ -114,10 +134,30 @@ int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
     return finish();
 }
 
-struct BackForm { int tiles, per, slabs, slice, slices; };
+// The gradient's form: as products of matrices where at least four heads (or batches' heads) share a look-up and the map fits into shared
+// memory; else by lanes' own sums.
+struct BackForm { bool products; int tiles, per, slabs, slice, slices, nt, kt, combos, batches, rows, col_blocks, row_slabs, each; };
 
 BackForm back_form(const pcr_bias_args& a) {
-    BackForm f;
+    BackForm f = {};
+    // all batches have the same positions: their heads are further columns of the product
+    const bool shared = a.batch > 1 && a.q_stride[1] == 0 && a.k_stride[1] == 0 && (!a.q_ids || (a.q_id_stride[0] == 0 && a.k_id_stride[0] == 0));
+    f.batches = shared ? (int)a.batch : 1;
+    f.combos = f.batches * a.heads;
+    f.rows = (int)((shared ? 1 : a.batch) * a.q_tokens);
+    f.products = f.combos >= 4 && 2 * a.reach + 1 <= kBackMap && (shared ? 1 : a.batch) * a.q_tokens <= INT32_MAX;
+    if (f.products) {
+        f.kt = a.buckets <= 16 ? 1 : a.buckets <= 32 ? 2 : 4;
+        f.slices = (a.buckets + 16 * f.kt - 1) / (16 * f.kt);
+        f.nt = f.combos > 8 ? (a.dtype == PCR_F32 ? 2 : 4) : 1;
+        f.col_blocks = (int)((a.k_tokens + kBackCols - 1) / kBackCols);
+        const int64_t beside = (int64_t)a.axes * f.slices * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)) * f.col_blocks;
+        const int64_t want = std::max<int64_t>(1, 4 * sm_count() / std::max<int64_t>(1, beside));
+        f.each = (int)std::max<int64_t>(8, (f.rows + want - 1) / want);
+        f.row_slabs = std::max(1, (f.rows + f.each - 1) / f.each);
+        f.slabs = f.row_slabs * std::max(1, f.col_blocks) * f.batches;
+        return f;
+    }
     const int v = 16 / (int)size_of(a.dtype);
     f.tiles = (int)((a.k_tokens + 32 * v - 1) / (32 * v));
     f.slice = std::min(a.axes * a.buckets, 96);           // 4 warps, 128 bytes a bucket: 48 KB
@@ -126,6 +166,28 @@ BackForm back_form(const pcr_bias_args& a) {
     f.per = (int)std::max<int64_t>(4, (units + want - 1) / want);
     f.slabs = (int)std::max<int64_t>(1, (units + f.per - 1) / f.per);
     return f;
+}
+
+template <typename T, int kTiles, int kNt>
+int launch_products(const BackArgs& G, dim3 grid, bool wide, cudaStream_t st) {
+    const size_t map = (2 * (size_t)G.a.reach + 1) * 2, sums = (size_t)16 * kTiles * 8 * kNt * 4, shared = sums + std::max<size_t>((G.a.k_ids ? 2 : 1) * kBackCols * 4 + map, sums);
+    static_assert(2 * 16 * kTiles * 8 * kNt * 4 <= 48 * 1024 && 16 * kTiles * 8 * kNt * 4 + 8 * kBackCols + 2 * kBackMap <= 48 * 1024, "no more than any launch may have");
+    if (wide) bias_back_mma_kernel<T, kTiles, kNt, true><<<grid, 256, shared, st>>>(G);
+    else bias_back_mma_kernel<T, kTiles, kNt, false><<<grid, 256, shared, st>>>(G);
+    ++g_launches;
+    return finish();
+}
+template <typename T, int kNt>
+int launch_tiles_of(const BackArgs& G, dim3 grid, int kt, bool wide, cudaStream_t st) {
+    if (kt == 1) return launch_products<T, 1, kNt>(G, grid, wide, st);
+    if (kt == 2) return launch_products<T, 2, kNt>(G, grid, wide, st);
+    return launch_products<T, 4, kNt>(G, grid, wide, st);
+}
+template <typename T>
+int launch_back(const BackArgs& G, const BackForm& f, bool wide, cudaStream_t st) {
+    const dim3 grid((unsigned)(f.row_slabs * f.col_blocks * G.a.axes * f.slices), (f.combos + 8 * f.nt - 1) / (8 * f.nt));
+    if (f.nt == 1) return launch_tiles_of<T, 1>(G, grid, f.kt, wide, st);
+    return launch_tiles_of<T, sizeof(T) == 4 ? 2 : 4>(G, grid, f.kt, wide, st);
 }
 
 }  // namespace
@@ -160,7 +222,11 @@ int pcr_relative_bias_backward(const pcr_bias_args* args, void* scratch, void* s
     const BackForm f = back_form(a);
     A.tiles = f.tiles; A.per = f.per; A.slabs = pairs(a) ? f.slabs : 0; A.slice = f.slice;
     A.partial = static_cast<float*>(scratch);
-    if (pairs(a)) {
+    if (pairs(a) && f.products) {
+        BackArgs G = {A, f.combos, f.batches, f.rows, f.col_blocks, f.row_slabs, f.each, f.slices};
+        const bool wide = whole(a);
+        if (int rc = a.dtype == PCR_F16 ? launch_back<__half>(G, f, wide, st) : a.dtype == PCR_BF16 ? launch_back<__nv_bfloat16>(G, f, wide, st) : launch_back<float>(G, f, wide, st)) return rc;
+    } else if (pairs(a)) {
         const dim3 grid(f.slabs, a.heads, f.slices);
         const size_t shared = (size_t)4 * f.slice * 128;
         const bool wide = whole(a);
@@ -170,10 +236,10 @@ int pcr_relative_bias_backward(const pcr_bias_args* args, void* scratch, void* s
         else launch(bias_back_kernel<float, 4, true>, bias_back_kernel<float, 4, false>);
         ++g_launches;
     }
-    const unsigned grid = (unsigned)(((int64_t)a.axes * a.buckets * a.heads + 7) / 8);
-    if (a.table_dtype == PCR_F16) bias_sum_kernel<__half><<<grid, 256, 0, st>>>(A);
-    else if (a.table_dtype == PCR_BF16) bias_sum_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(A);
-    else bias_sum_kernel<float><<<grid, 256, 0, st>>>(A);
+    const unsigned grid = (unsigned)(((int64_t)a.axes * a.buckets * a.heads + 31) / 32);
+    if (a.table_dtype == PCR_F16) bias_sum_kernel<__half><<<grid, 1024, 0, st>>>(A);
+    else if (a.table_dtype == PCR_BF16) bias_sum_kernel<__nv_bfloat16><<<grid, 1024, 0, st>>>(A);
+    else bias_sum_kernel<float><<<grid, 1024, 0, st>>>(A);
     ++g_launches;
     return finish();
 }
