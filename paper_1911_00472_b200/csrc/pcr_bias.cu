@@ -102,7 +102,9 @@ int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
     // All combinations of buckets first, where 44 KB hold them for four heads at least and there are more pairs for every CTA than lines.
     int64_t lines = 1;
     for (int a = 0; a < A.axes; ++a) lines *= A.buckets + 1;
-    const int64_t most = 44 * 1024 / (4 * (int64_t)sizeof(T) * (lines + 1)) * 4;
+    const int64_t map = 2 * (2 * (int64_t)A.reach + 1) + 16;
+    A.mapped = map <= 8 * 1024;
+    const int64_t most = (46 * 1024 - (A.mapped ? map : 0)) / (4 * (int64_t)sizeof(T) * (lines + 1) + 16 * A.axes * (A.buckets + 1)) * 4;
     if (most >= 4 && (A.axes == 1 || (int64_t)A.batch * A.nq * A.nk >= lines * 2 * sm_count())) {
         const int64_t columns = A.nk + (!wide && sizeof(T) == 2 ? 1 : 0);         // (a row's first pair of columns may begin before it)
         A.tiles = (int)((columns + 32 * V - 1) / (32 * V));
@@ -113,7 +115,7 @@ int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
         A.group = group;
         const int groups = (A.heads + group - 1) / group;
         const dim3 grid((unsigned)std::min<int64_t>(ctas, std::max<int64_t>(1, room / groups)), groups);
-        const size_t shared = (size_t)group * (lines + 1) * sizeof(T);
+        const size_t shared = (size_t)group * (lines + 1) * sizeof(T) + 16 + (size_t)group * A.axes * (A.buckets + 1) * sizeof(float) + (A.mapped ? map : 0);
         if (wide) bias_joint_kernel<T, true><<<grid, kBiasThreads, shared, st>>>(A);
         else bias_joint_kernel<T, false><<<grid, kBiasThreads, shared, st>>>(A);
         ++g_launches;
@@ -136,7 +138,7 @@ int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
 
 // The gradient's form: as products of matrices where at least four heads (or batches' heads) share a look-up and the map fits into shared
 // memory; else by lanes' own sums.
-struct BackForm { bool products; int tiles, per, slabs, slice, slices, nt, kt, combos, batches, rows, col_blocks, row_slabs, each; };
+struct BackForm { bool products; int tiles, per, slabs, slice, slices, nt, kt, combos, batches, rows, width, col_blocks, row_slabs, each; };
 
 BackForm back_form(const pcr_bias_args& a) {
     BackForm f = {};
@@ -150,9 +152,13 @@ BackForm back_form(const pcr_bias_args& a) {
         f.kt = a.buckets <= 16 ? 1 : a.buckets <= 32 ? 2 : 4;
         f.slices = (a.buckets + 16 * f.kt - 1) / (16 * f.kt);
         f.nt = f.combos > 8 ? (a.dtype == PCR_F32 ? 2 : 4) : 1;
-        f.col_blocks = (int)((a.k_tokens + kBackCols - 1) / kBackCols);
-        const int64_t beside = (int64_t)a.axes * f.slices * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)) * f.col_blocks;
-        const int64_t want = std::max<int64_t>(1, 4 * sm_count() / std::max<int64_t>(1, beside));
+        // about 3 CTAs an SM, of long rows where there are enough of them: a CTA's beginning and end are a warp's work on some hundred columns
+        const int64_t beside = (int64_t)a.axes * f.slices * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)), room = 3 * sm_count();
+        f.width = kBackCols;
+        auto blocks = [&] { return (a.k_tokens + f.width - 1) / f.width; };
+        while (f.width > 128 && beside * blocks() * ((f.rows + 31) / 32) < room) f.width /= 2;
+        f.col_blocks = (int)blocks();
+        const int64_t want = std::max<int64_t>(1, room / std::max<int64_t>(1, beside * f.col_blocks));
         f.each = (int)std::max<int64_t>(8, (f.rows + want - 1) / want);
         f.row_slabs = std::max(1, (f.rows + f.each - 1) / f.each);
         f.slabs = f.row_slabs * std::max(1, f.col_blocks) * f.batches;
@@ -223,7 +229,7 @@ int pcr_relative_bias_backward(const pcr_bias_args* args, void* scratch, void* s
     A.tiles = f.tiles; A.per = f.per; A.slabs = pairs(a) ? f.slabs : 0; A.slice = f.slice;
     A.partial = static_cast<float*>(scratch);
     if (pairs(a) && f.products) {
-        BackArgs G = {A, f.combos, f.batches, f.rows, f.col_blocks, f.row_slabs, f.each, f.slices};
+        BackArgs G = {A, f.combos, f.batches, f.rows, f.col_blocks, f.row_slabs, f.each, f.slices, f.width};
         const bool wide = whole(a);
         if (int rc = a.dtype == PCR_F16 ? launch_back<__half>(G, f, wide, st) : a.dtype == PCR_BF16 ? launch_back<__nv_bfloat16>(G, f, wide, st) : launch_back<float>(G, f, wide, st)) return rc;
     } else if (pairs(a)) {

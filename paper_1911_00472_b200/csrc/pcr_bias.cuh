@@ -27,7 +27,7 @@ struct BiasArgs {
     float* partial;                            // backward: sums of CTAs, (slab, axis, bucket, head)
     int batch, nq, nk, heads, axes, buckets, reach, table32;
     int group;                                 // forward: heads of a CTA, a multiple of 4
-    int lines;                                 // combinations of buckets (and of none) of all axes
+    int lines, mapped;                         // combinations of buckets (and of none) of all axes; whether the map is in shared memory
     int tiles;                                 // spans of a row that warps take
     int per, slabs, slice;                     // backward: (row, span)s of a CTA; CTAs of a head; (axis, bucket)s of a CTA
 };
@@ -139,42 +139,62 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
     using Vec = typename Quad<T>::V;
     constexpr int kCols = 16 / sizeof(T);                  // of a lane
     constexpr bool kPairs = !kWide && sizeof(T) == 2;
-    constexpr int kLook = kPairs ? 12 : kCols;
+    constexpr int kLook = kPairs ? 9 : kCols;
     extern __shared__ __align__(16) uint8_t shared[];
     Vec* joint = reinterpret_cast<Vec*>(shared);
     const int tid = threadIdx.x, lane = tid & 31, h0 = blockIdx.y * A.group, group = min(A.group, A.heads - h0), fours = (group + 3) / 4, lines = A.lines + 1, n1 = A.buckets + 1;
+    // the table by itself, zeros behind its last bucket and head, then every combination
+    float4* own = reinterpret_cast<float4*>(joint + (fours * lines + 1) / 2 * 2);
+    for (int i = tid; i < fours * A.axes * n1 * 4; i += kBiasThreads) {
+        const int e = i & 3, n = (i >> 2) % n1, rest = (i >> 2) / n1, a = rest % A.axes, h = h0 + 4 * (rest / A.axes) + e;
+        float v = 0.f;
+        if (n < A.buckets && h < A.heads) {
+            const size_t at = ((size_t)a * A.buckets + n) * A.heads + h;
+            v = A.table32 ? static_cast<const float*>(A.table)[at] : (float)static_cast<const T*>(A.table)[at];
+        }
+        reinterpret_cast<float*>(own)[i] = v;
+    }
+    __syncthreads();
     for (int i = tid; i < fours * lines; i += kBiasThreads) {
         const int four = i / lines, line = i - four * lines;
-        float s[4] = {};
-        int rest = line;
-        for (int a = A.axes - 1; a >= 0; --a) {            // (the last axis's bucket counts single lines)
-            const int n = rest % n1;
-            rest /= n1;
-            for (int e = 0; e < 4; ++e) {
-                const int h = h0 + 4 * four + e;
-                if (n >= A.buckets || h >= A.heads) continue;
-                const size_t at = ((size_t)a * A.buckets + n) * A.heads + h;
-                s[e] += A.table32 ? static_cast<const float*>(A.table)[at] : (float)static_cast<const T*>(A.table)[at];
+        int at[kBiasAxes], rest = line;
+        for (int a = A.axes - 1; a >= 0; --a) { at[a] = rest % n1; rest /= n1; }          // (the last axis's bucket counts single lines)
+        float4 s = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (line < A.lines) {
+            s = own[four * A.axes * n1 + at[0]];
+            for (int a = 1; a < A.axes; ++a) {                                            // axis after axis
+                const float4 x = own[(four * A.axes + a) * n1 + at[a]];
+                s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
             }
         }
         union { T t[4]; Vec v; } x;
-        for (int e = 0; e < 4; ++e) x.t[e] = bias_from<T>(line == A.lines ? -INFINITY : s[e]);
+        x.t[0] = bias_from<T>(s.x); x.t[1] = bias_from<T>(s.y); x.t[2] = bias_from<T>(s.z); x.t[3] = bias_from<T>(s.w);
         joint[i] = x.v;
     }
+    uint16_t* map = reinterpret_cast<uint16_t*>(own + fours * A.axes * n1);
+    if (A.mapped)
+        for (int i = tid; i <= 2 * A.reach; i += kBiasThreads) {
+            const int n = __ldg(A.bucket_of + i);
+            map[i] = (uint16_t)(n >= 0 && n < A.buckets ? n : A.buckets);
+        }
     __syncthreads();
     const int64_t per = (int64_t)A.nq * A.tiles, all = per * A.batch;
     for (int64_t unit = (int64_t)blockIdx.x * (kBiasThreads / 32) + (tid >> 5); unit < all; unit += (int64_t)gridDim.x * (kBiasThreads / 32)) {
         const int batch = (int)(unit / per), in = (int)(unit - batch * per), row = in / A.tiles, j0 = (in - row * A.tiles) * 32 * kCols;
-        // a lane's columns: side by side; or every 32nd; or the three around every 64th even one
-        auto column = [&](int v) { return kWide ? j0 + lane * kCols + v : kPairs ? j0 + 64 * (v / 3) + 2 * lane + v % 3 - 1 : j0 + 32 * v + lane; };
+        // a lane's columns: side by side; or every 32nd; or two of every 64, and (the last) the one before the span
+        auto column = [&](int v) { return kWide ? j0 + lane * kCols + v : kPairs ? (v == 8 ? j0 - 1 : j0 + 64 * (v / 2) + 2 * lane + v % 2) : j0 + 32 * v + lane; };
         int line[kLook] = {};
         for (int a = 0; a < A.axes; ++a) {
             const int q = A.q_pos[a * A.qs[0] + batch * A.qs[1] + (int64_t)row * A.qs[2]];
             const int32_t* k = A.k_pos + a * A.ks[0] + batch * A.ks[1];
 #pragma unroll
             for (int v = 0; v < kLook; ++v) {
-                const int j = min(max(column(v), 0), A.nk - 1), n = bucket_of(A, k[j * A.ks[2]], q);
-                line[v] = line[v] * n1 + (n < 0 ? A.buckets : n);
+                const int at = map_at(A.reach, k[min(max(column(v), 0), A.nk - 1) * A.ks[2]], q);
+                if (A.mapped) line[v] = line[v] * n1 + map[at];
+                else {
+                    const int n = __ldg(A.bucket_of + at);
+                    line[v] = line[v] * n1 + (n >= 0 && n < A.buckets ? n : A.buckets);
+                }
             }
         }
         if (A.q_ids) {
@@ -185,6 +205,15 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
                 if (A.k_ids[batch * A.kis[0] + (int64_t)j * A.kis[1]] != q) line[v] = A.lines;
             }
         }
+        int before[kPairs ? 4 : 1];                        // of the columns before the lane's own two
+        if constexpr (kPairs)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                before[v] = __shfl_up_sync(~0u, line[2 * v + 1], 1);
+                const int last = v == 0 ? line[8] : __shfl_sync(~0u, line[v == 0 ? 0 : 2 * v - 1], 31);
+                if (lane == 0) before[v] = last;
+            }
+        const bool inside = j0 > 0 && j0 + 32 * kCols < A.nk;                             // (nothing of the span lies beyond the row)
         T* out = static_cast<T*>(A.rows) + batch * A.rs[0] + (int64_t)h0 * A.rs[1] + (int64_t)row * A.rs[2];
         for (int f = 0; f < fours; ++f) {
             const Vec* from = joint + f * lines;
@@ -205,25 +234,41 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
                         for (int v = 0; v < kCols; ++v) if (column(v) < A.nk) to[column(v)] = got[e][v];
                 }
             } else {
-                uint2 x[kLook];
+                uint2 x[8], y[kPairs ? 4 : 1];
 #pragma unroll
-                for (int v = 0; v < kLook; ++v) x[v] = from[line[v]];
+                for (int v = 0; v < 8; ++v) x[v] = from[line[v]];
+                if constexpr (kPairs)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) y[v] = from[before[v]];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (4 * f + e >= group) break;
                     uint16_t* to = reinterpret_cast<uint16_t*>(out + (4 * f + e) * A.rs[1]);
-                    auto two = [&](int v, int w) { return __byte_perm(e < 2 ? x[v].x : x[v].y, e < 2 ? x[w].x : x[w].y, e & 1 ? 0x7632 : 0x5410); };
+                    auto two = [&](const uint2& a, const uint2& b) { return __byte_perm(e < 2 ? a.x : a.y, e < 2 ? b.x : b.y, e & 1 ? 0x7632 : 0x5410); };
                     if constexpr (kWide) {
-                        if (column(0) < A.nk) *reinterpret_cast<uint4*>(to + column(0)) = make_uint4(two(0, 1), two(2, 3), two(4, 5), two(6, 7));
+                        if (column(0) < A.nk) *reinterpret_cast<uint4*>(to + column(0)) = make_uint4(two(x[0], x[1]), two(x[2], x[3]), two(x[4], x[5]), two(x[6], x[7]));
                     } else {
-                        const int odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1 & 1);       // (of the whole warp)
+                        const int odd = (int)(reinterpret_cast<uintptr_t>(to) >> 1 & 1);  // (of the whole warp)
+                        uint32_t w[4];
+                        if (odd) {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const uint32_t y = odd ? two(3 * v, 3 * v + 1) : two(3 * v + 1, 3 * v + 2);
-                            const int j = column(3 * v + 1) - odd;
-                            if (j >= 0 && j + 1 < A.nk) *reinterpret_cast<uint32_t*>(to + j) = y;
-                            else if (j >= 0 && j < A.nk) to[j] = (uint16_t)y;
-                            else if (j == -1) to[0] = (uint16_t)(y >> 16);
+                            for (int v = 0; v < 4; ++v) w[v] = two(y[v], x[2 * v]);
+                        } else {
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) w[v] = two(x[2 * v], x[2 * v + 1]);
+                        }
+                        to += j0 + 2 * lane - odd;
+                        if (inside) {
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) *reinterpret_cast<uint32_t*>(to + 64 * v) = w[v];
+                        } else {
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) {
+                                const int j = j0 + 64 * v + 2 * lane - odd;
+                                if (j >= 0 && j + 1 < A.nk) *reinterpret_cast<uint32_t*>(to + 64 * v) = w[v];
+                                else if (j >= 0 && j < A.nk) to[64 * v] = (uint16_t)w[v];
+                                else if (j == -1) to[64 * v + 1] = (uint16_t)(w[v] >> 16);
+                            }
                         }
                     }
                 }
@@ -295,9 +340,9 @@ __global__ void __launch_bounds__(128) bias_back_kernel(const __grid_constant__ 
 
 // The same as products of matrices: (bucket, pair) times (pair, head), where the first is 1 at a pair's bucket and 0 elsewhere, so that all
 // products are exact and the sums are the tensor cores' 32 bits.  A CTA has 16 kTiles buckets of an axis, kNt groups of 8 heads (or
-// batches' heads, where all batches have the same positions), a block of columns and a share of the rows; a warp goes along a row, 32 pairs
-// at a time.  Which of the 16 pairs of a step stands where is free as long as both operands agree: lane l has heads l / 4 and, of the step's 32
-// columns, 8 (l % 4) .. + 7, one vector of 16 bits, two steps.  32-bit values are cut into three parts of 8 bits of mantissa each.
+// batches' heads, where all batches have the same positions), a block of columns and a share of the rows; a warp goes along a row, 64 pairs
+// at a time, whole lines of 128 bytes of every head.  Which of the 16 pairs of a product stands where is free as long as both operands agree:
+// lane l has head l / 4 and, of the 64 columns, 16 (l % 4) .. + 15, four products.  32-bit values are cut into three parts of 8 bits of mantissa each.
 // What bounds it: instructions.  A bucket is looked up once for all heads of a CTA; the comparison with a bucket's number makes a
 // register of the first operand in one instruction (16-bit numbers hold 0 .. 255).
 constexpr int kBackCols = 1024, kBackMap = 16384;       // columns of a CTA; places of the map in shared memory at most
@@ -328,6 +373,7 @@ struct BackArgs {
     int combos, batches, rows;                 // heads, or all batches' where they share positions; those batches; rows of all batches that do not
     int col_blocks, row_slabs, each;           // blocks of columns; shares of the rows, `each` rows
     int slices;                                // of an axis's buckets
+    int width;                                 // of a block
 };
 
 template <typename T, int kTiles, int kNt, bool kWide>
@@ -340,7 +386,7 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = lane >> 2, quarter = lane & 3;
     // axes and slices of buckets side by side: what one CTA has read, the others find in the second-level cache
     const int sides = A.axes * G.slices, side = blockIdx.x % sides, share = blockIdx.x / sides, axis = side / G.slices, base = (side - axis * G.slices) * 16 * kTiles;
-    const int block = share % G.col_blocks, slab = share / G.col_blocks, j0 = block * kBackCols, cols = min(kBackCols, A.nk - j0);
+    const int block = share % G.col_blocks, slab = share / G.col_blocks, j0 = block * G.width, cols = min(G.width, A.nk - j0);
     const int first = blockIdx.y * 8 * kNt;
     float* extra = reinterpret_cast<float*>(shared);                       // sums of what is not finite
     int32_t* pos = reinterpret_cast<int32_t*>(extra + 16 * kTiles * 8 * kNt);
@@ -378,8 +424,8 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
                 at[t] = static_cast<const T*>(A.rows) + (int64_t)(batch + b) * A.rs[0] + (int64_t)(combo - b * A.heads) * A.rs[1] + (int64_t)row * A.rs[2] + j0;
             }
             // a lane's eight values of each group, those of the next step on their way
-            uint4 raw[kNt][kParts == 1 ? 1 : 2];
-            auto load = [&](int c) {
+            uint4 raw[2][kNt][kParts == 1 ? 1 : 2];
+            auto load = [&](uint4 (&raw)[kNt][kParts == 1 ? 1 : 2], int c) {
 #pragma unroll
                 for (int t = 0; t < kNt; ++t) {
                     if constexpr (kParts == 1) {
@@ -388,51 +434,65 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
                         else {
                             uint32_t e[8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) e[i] = has[t] && c + i < cols ? __ldcs(reinterpret_cast<const unsigned short*>(at[t] + c + i)) : 0;
+                            for (int i = 0; i < 8; ++i) e[i] = has[t] && c + 4 * i < cols ? __ldcs(reinterpret_cast<const unsigned short*>(at[t] + c + 4 * i)) : 0;
                             raw[t][0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
                         }
                     } else {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             raw[t][i] = make_uint4(0, 0, 0, 0);
-                            const uint32_t* p = reinterpret_cast<const uint32_t*>(at[t] + c + 4 * i);
+                            const uint32_t* p = reinterpret_cast<const uint32_t*>(at[t] + c + (kWide ? 4 : 16) * i);
                             if (kWide) { if (has[t] && c + 4 * i < cols) raw[t][i] = __ldcs(reinterpret_cast<const uint4*>(p)); }
                             else if (has[t]) {
-                                if (c + 4 * i < cols) raw[t][i].x = __ldcs(p);
-                                if (c + 4 * i + 1 < cols) raw[t][i].y = __ldcs(p + 1);
-                                if (c + 4 * i + 2 < cols) raw[t][i].z = __ldcs(p + 2);
-                                if (c + 4 * i + 3 < cols) raw[t][i].w = __ldcs(p + 3);
+                                if (c + 16 * i < cols) raw[t][i].x = __ldcs(p);
+                                if (c + 16 * i + 4 < cols) raw[t][i].y = __ldcs(p + 4);
+                                if (c + 16 * i + 8 < cols) raw[t][i].z = __ldcs(p + 8);
+                                if (c + 16 * i + 12 < cols) raw[t][i].w = __ldcs(p + 12);
                             }
                         }
                     }
                 }
             };
-            load(8 * quarter);
+            // (rows that begin anywhere are read value by value: every fourth column is a lane's, so that four lanes read side by side)
+            const int lane0 = kWide ? 16 * quarter : quarter, next = kWide ? 8 : 32;
+            load(raw[0], lane0);
+            load(raw[1], lane0 + next);
 #pragma unroll 1
-            for (int c0 = 0; c0 < cols; c0 += 32) {
-                const int c = c0 + 8 * quarter;
+            for (int c0 = 0; c0 < cols; c0 += 64)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int c = c0 + lane0 + next * half;
                 uint32_t v[kNt][kParts][4];
-                uint32_t counts = c + 8 <= cols ? 255u : c < cols ? (1u << (cols - c)) - 1 : 0u;
+                uint32_t counts = 255u;                                    // which of the lane's eight columns count
+                if (kWide) counts = c + 8 <= cols ? 255u : c < cols ? (1u << (cols - c)) - 1 : 0u;
+                else if (c + 28 >= cols) counts = c < cols ? (2u << ((cols - 1 - c) >> 2)) - 1 : 0u;
                 float whole[kParts == 3 ? kNt : 1][8];
 #pragma unroll
                 for (int t = 0; t < kNt; ++t) {
-                    if constexpr (kParts == 1) { v[t][0][0] = raw[t][0].x; v[t][0][1] = raw[t][0].y; v[t][0][2] = raw[t][0].z; v[t][0][3] = raw[t][0].w; }
+                    if constexpr (kParts == 1) { v[t][0][0] = raw[half][t][0].x; v[t][0][1] = raw[half][t][0].y; v[t][0][2] = raw[half][t][0].z; v[t][0][3] = raw[half][t][0].w; }
                     else
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            whole[t][4 * i] = __uint_as_float(raw[t][i].x); whole[t][4 * i + 1] = __uint_as_float(raw[t][i].y);
-                            whole[t][4 * i + 2] = __uint_as_float(raw[t][i].z); whole[t][4 * i + 3] = __uint_as_float(raw[t][i].w);
+                            whole[t][4 * i] = __uint_as_float(raw[half][t][i].x); whole[t][4 * i + 1] = __uint_as_float(raw[half][t][i].y);
+                            whole[t][4 * i + 2] = __uint_as_float(raw[half][t][i].z); whole[t][4 * i + 3] = __uint_as_float(raw[half][t][i].w);
                         }
                 }
-                if (c0 + 32 < cols) load(c + 32);
+                if (c0 + 64 < cols) load(raw[half], c + 64);
                 // buckets of the lane's eight columns; pairs that do not count have none
                 uint32_t n2[4];
                 {
-                    const int4 p0 = *reinterpret_cast<const int4*>(pos + c), p1 = *reinterpret_cast<const int4*>(pos + c + 4);
-                    const int k[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+                    int k[8], id[8];
+                    auto eight = [&](int (&x)[8], const int32_t* from) {
+                        if (kWide) {
+                            const int4 a = *reinterpret_cast<const int4*>(from + c), b = *reinterpret_cast<const int4*>(from + c + 4);
+                            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                        } else
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] = from[c + 4 * i];
+                    };
+                    eight(k, pos);
                     if (A.q_ids) {
-                        const int4 s0 = *reinterpret_cast<const int4*>(ids + c), s1 = *reinterpret_cast<const int4*>(ids + c + 4);
-                        const int id[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+                        eight(id, ids);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) counts &= id[i] == q_id ? ~0u : ~(1u << i);
                     }
