@@ -105,11 +105,11 @@ int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
     const int64_t map = 2 * (2 * (int64_t)A.reach + 1) + 16;
     A.mapped = map <= 8 * 1024;
     const int64_t most = (46 * 1024 - (A.mapped ? map : 0)) / (4 * (int64_t)sizeof(T) * (lines + 1) + 16 * A.axes * (A.buckets + 1)) * 4;
-    if (most >= 4 && (A.axes == 1 || (int64_t)A.batch * A.nq * A.nk >= lines * 2 * sm_count())) {
+    if (most >= 4 && (int64_t)A.batch * A.nq < INT32_MAX / 2 && (A.axes == 1 || (int64_t)A.batch * A.nq * A.nk >= lines * 2 * sm_count())) {
         const int64_t columns = A.nk + (!wide && sizeof(T) == 2 ? 1 : 0);         // (a row's first pair of columns may begin before it)
         A.tiles = (int)((columns + 32 * V - 1) / (32 * V));
         A.lines = (int)lines;
-        const int64_t ctas = ((int64_t)A.batch * A.nq * A.tiles + 7) / 8, room = 4 * sm_count();
+        const int64_t ctas = ((int64_t)A.batch * A.nq * A.tiles + 7) / 8, room = 3 * sm_count();
         int group = (int)std::min<int64_t>((A.heads + 3) / 4 * 4, most);
         while (group > 4 && ctas * ((A.heads + group - 1) / group) < 2 * sm_count()) group = (group / 2 + 3) / 4 * 4;
         A.group = group;
@@ -138,7 +138,7 @@ int launch_bias(BiasArgs& A, bool wide, cudaStream_t st) {
 
 // The gradient's form: as products of matrices where at least four heads (or batches' heads) share a look-up and the map fits into shared
 // memory; else by lanes' own sums.
-struct BackForm { bool products; int tiles, per, slabs, slice, slices, nt, kt, combos, batches, rows, width, col_blocks, row_slabs, each; };
+struct BackForm { bool products; int ax, tiles, per, slabs, slice, slices, nt, kt, combos, batches, rows, width, col_blocks, row_slabs, each; };
 
 BackForm back_form(const pcr_bias_args& a) {
     BackForm f = {};
@@ -149,11 +149,13 @@ BackForm back_form(const pcr_bias_args& a) {
     f.rows = (int)((shared ? 1 : a.batch) * a.q_tokens);
     f.products = f.combos >= 4 && 2 * a.reach + 1 <= kBackMap && (shared ? 1 : a.batch) * a.q_tokens <= INT32_MAX;
     if (f.products) {
+        // axes of a CTA: what is read serves them all, as long as their sums stay in registers
         f.kt = a.buckets <= 16 ? 1 : a.buckets <= 32 ? 2 : 4;
+        f.ax = f.kt == 4 ? 1 : a.axes == 3 ? 3 : std::min(a.axes, 2);
         f.slices = (a.buckets + 16 * f.kt - 1) / (16 * f.kt);
-        f.nt = f.combos > 8 ? (a.dtype == PCR_F32 ? 2 : 4) : 1;
+        f.nt = f.combos <= 8 ? 1 : f.combos > 16 && f.ax == 1 && a.dtype != PCR_F32 ? 4 : 2;
         // about 3 CTAs an SM, of long rows where there are enough of them: a CTA's beginning and end are a warp's work on some hundred columns
-        const int64_t beside = (int64_t)a.axes * f.slices * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)), room = 3 * sm_count();
+        const int64_t beside = (int64_t)((a.axes + f.ax - 1) / f.ax) * f.slices * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)), room = 3 * sm_count();
         f.width = kBackCols;
         auto blocks = [&] { return (a.k_tokens + f.width - 1) / f.width; };
         while (f.width > 128 && beside * blocks() * ((f.rows + 31) / 32) < room) f.width /= 2;
@@ -174,26 +176,35 @@ BackForm back_form(const pcr_bias_args& a) {
     return f;
 }
 
-template <typename T, int kTiles, int kNt>
+template <typename T, int kAx, int kTiles, int kNt>
 int launch_products(const BackArgs& G, dim3 grid, bool wide, cudaStream_t st) {
-    const size_t map = (2 * (size_t)G.a.reach + 1) * 2, sums = (size_t)16 * kTiles * 8 * kNt * 4, shared = sums + std::max<size_t>((G.a.k_ids ? 2 : 1) * kBackCols * 4 + map, sums);
-    static_assert(2 * 16 * kTiles * 8 * kNt * 4 <= 48 * 1024 && 16 * kTiles * 8 * kNt * 4 + 8 * kBackCols + 2 * kBackMap <= 48 * 1024, "no more than any launch may have");
-    if (wide) bias_back_mma_kernel<T, kTiles, kNt, true><<<grid, 256, shared, st>>>(G);
-    else bias_back_mma_kernel<T, kTiles, kNt, false><<<grid, 256, shared, st>>>(G);
+    constexpr size_t kSums = (size_t)kAx * 16 * kTiles * 8 * kNt * 4;
+    const size_t shared = kSums + std::max<size_t>((kAx + (G.a.k_ids ? 1 : 0)) * kBackCols * 4 + (2 * (size_t)G.a.reach + 1) * 2, kSums);
+    static_assert(2 * kSums <= 48 * 1024 && kSums + (kAx + 1) * kBackCols * 4 + 2 * kBackMap <= 48 * 1024, "no more than any launch may have");
+    if (wide) bias_back_mma_kernel<T, kAx, kTiles, kNt, true><<<grid, 256, shared, st>>>(G);
+    else bias_back_mma_kernel<T, kAx, kTiles, kNt, false><<<grid, 256, shared, st>>>(G);
     ++g_launches;
     return finish();
 }
 template <typename T, int kNt>
-int launch_tiles_of(const BackArgs& G, dim3 grid, int kt, bool wide, cudaStream_t st) {
-    if (kt == 1) return launch_products<T, 1, kNt>(G, grid, wide, st);
-    if (kt == 2) return launch_products<T, 2, kNt>(G, grid, wide, st);
-    return launch_products<T, 4, kNt>(G, grid, wide, st);
+int launch_tiles_of(const BackArgs& G, const BackForm& f, dim3 grid, bool wide, cudaStream_t st) {
+    if (f.ax == 3) return f.kt == 1 ? launch_products<T, 3, 1, kNt>(G, grid, wide, st) : launch_products<T, 3, 2, kNt>(G, grid, wide, st);
+    if (f.ax == 2) return f.kt == 1 ? launch_products<T, 2, 1, kNt>(G, grid, wide, st) : launch_products<T, 2, 2, kNt>(G, grid, wide, st);
+    if (f.kt == 1) return launch_products<T, 1, 1, kNt>(G, grid, wide, st);
+    if (f.kt == 2) return launch_products<T, 1, 2, kNt>(G, grid, wide, st);
+    return launch_products<T, 1, 4, kNt>(G, grid, wide, st);
 }
 template <typename T>
 int launch_back(const BackArgs& G, const BackForm& f, bool wide, cudaStream_t st) {
-    const dim3 grid((unsigned)(f.row_slabs * f.col_blocks * G.a.axes * f.slices), (f.combos + 8 * f.nt - 1) / (8 * f.nt));
-    if (f.nt == 1) return launch_tiles_of<T, 1>(G, grid, f.kt, wide, st);
-    return launch_tiles_of<T, sizeof(T) == 4 ? 2 : 4>(G, grid, f.kt, wide, st);
+    const dim3 grid((unsigned)(f.row_slabs * f.col_blocks * ((G.a.axes + f.ax - 1) / f.ax) * f.slices), (f.combos + 8 * f.nt - 1) / (8 * f.nt));
+    if (f.nt == 1) return launch_tiles_of<T, 1>(G, f, grid, wide, st);
+    if constexpr (sizeof(T) == 2)
+        if (f.nt == 4) {
+            if (f.kt == 1) return launch_products<T, 1, 1, 4>(G, grid, wide, st);
+            if (f.kt == 2) return launch_products<T, 1, 2, 4>(G, grid, wide, st);
+            return launch_products<T, 1, 4, 4>(G, grid, wide, st);
+        }
+    return launch_tiles_of<T, 2>(G, f, grid, wide, st);
 }
 
 }  // namespace

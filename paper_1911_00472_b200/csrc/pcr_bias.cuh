@@ -155,21 +155,22 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
         reinterpret_cast<float*>(own)[i] = v;
     }
     __syncthreads();
-    for (int i = tid; i < fours * lines; i += kBiasThreads) {
-        const int four = i / lines, line = i - four * lines;
+    for (int line = tid; line < lines; line += kBiasThreads) {
         int at[kBiasAxes], rest = line;
         for (int a = A.axes - 1; a >= 0; --a) { at[a] = rest % n1; rest /= n1; }          // (the last axis's bucket counts single lines)
-        float4 s = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        if (line < A.lines) {
-            s = own[four * A.axes * n1 + at[0]];
-            for (int a = 1; a < A.axes; ++a) {                                            // axis after axis
-                const float4 x = own[(four * A.axes + a) * n1 + at[a]];
-                s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        for (int four = 0; four < fours; ++four) {
+            float4 s = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (line < A.lines) {
+                s = own[four * A.axes * n1 + at[0]];
+                for (int a = 1; a < A.axes; ++a) {                                        // axis after axis
+                    const float4 x = own[(four * A.axes + a) * n1 + at[a]];
+                    s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+                }
             }
+            union { T t[4]; Vec v; } x;
+            x.t[0] = bias_from<T>(s.x); x.t[1] = bias_from<T>(s.y); x.t[2] = bias_from<T>(s.z); x.t[3] = bias_from<T>(s.w);
+            joint[four * lines + line] = x.v;
         }
-        union { T t[4]; Vec v; } x;
-        x.t[0] = bias_from<T>(s.x); x.t[1] = bias_from<T>(s.y); x.t[2] = bias_from<T>(s.z); x.t[3] = bias_from<T>(s.w);
-        joint[i] = x.v;
     }
     uint16_t* map = reinterpret_cast<uint16_t*>(own + fours * A.axes * n1);
     if (A.mapped)
@@ -178,18 +179,22 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
             map[i] = (uint16_t)(n >= 0 && n < A.buckets ? n : A.buckets);
         }
     __syncthreads();
-    const int64_t per = (int64_t)A.nq * A.tiles, all = per * A.batch;
-    for (int64_t unit = (int64_t)blockIdx.x * (kBiasThreads / 32) + (tid >> 5); unit < all; unit += (int64_t)gridDim.x * (kBiasThreads / 32)) {
-        const int batch = (int)(unit / per), in = (int)(unit - batch * per), row = in / A.tiles, j0 = (in - row * A.tiles) * 32 * kCols;
+    // (row, span) after (row, span): the next is a fixed number of either on
+    const uint32_t all = (uint32_t)A.batch * A.nq, step = gridDim.x * (kBiasThreads / 32), step_rows = step / A.tiles, step_spans = step - step_rows * A.tiles;
+    uint32_t line_no = (blockIdx.x * (kBiasThreads / 32) + (tid >> 5)) / A.tiles, span = blockIdx.x * (kBiasThreads / 32) + (tid >> 5) - line_no * A.tiles;
+    for (; line_no < all; line_no += step_rows, span += step_spans) {
+        if (span >= (uint32_t)A.tiles) { span -= A.tiles; ++line_no; if (line_no >= all) break; }
+        const int batch = (int)(line_no / A.nq), row = (int)(line_no - batch * A.nq), j0 = (int)span * 32 * kCols;
         // a lane's columns: side by side; or every 32nd; or two of every 64, and (the last) the one before the span
         auto column = [&](int v) { return kWide ? j0 + lane * kCols + v : kPairs ? (v == 8 ? j0 - 1 : j0 + 64 * (v / 2) + 2 * lane + v % 2) : j0 + 32 * v + lane; };
         int line[kLook] = {};
         for (int a = 0; a < A.axes; ++a) {
             const int q = A.q_pos[a * A.qs[0] + batch * A.qs[1] + (int64_t)row * A.qs[2]];
             const int32_t* k = A.k_pos + a * A.ks[0] + batch * A.ks[1];
+            const bool dense = A.ks[2] == 1;
 #pragma unroll
             for (int v = 0; v < kLook; ++v) {
-                const int at = map_at(A.reach, k[min(max(column(v), 0), A.nk - 1) * A.ks[2]], q);
+                const int j = min(max(column(v), 0), A.nk - 1), at = map_at(A.reach, dense ? k[j] : k[j * A.ks[2]], q);
                 if (A.mapped) line[v] = line[v] * n1 + map[at];
                 else {
                     const int n = __ldg(A.bucket_of + at);
@@ -213,7 +218,7 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
                 const int last = v == 0 ? line[8] : __shfl_sync(~0u, line[v == 0 ? 0 : 2 * v - 1], 31);
                 if (lane == 0) before[v] = last;
             }
-        const bool inside = j0 > 0 && j0 + 32 * kCols < A.nk;                             // (nothing of the span lies beyond the row)
+        const bool inside = j0 + 32 * kCols <= A.nk;                                      // (nothing of the span lies behind the row)
         T* out = static_cast<T*>(A.rows) + batch * A.rs[0] + (int64_t)h0 * A.rs[1] + (int64_t)row * A.rs[2];
         for (int f = 0; f < fours; ++f) {
             const Vec* from = joint + f * lines;
@@ -258,7 +263,7 @@ __global__ void __launch_bounds__(kBiasThreads) bias_joint_kernel(const __grid_c
                             for (int v = 0; v < 4; ++v) w[v] = two(x[2 * v], x[2 * v + 1]);
                         }
                         to += j0 + 2 * lane - odd;
-                        if (inside) {
+                        if (inside && (j0 > 0 || !odd)) {
 #pragma unroll
                             for (int v = 0; v < 4; ++v) *reinterpret_cast<uint32_t*>(to + 64 * v) = w[v];
                         } else {
@@ -345,7 +350,7 @@ __global__ void __launch_bounds__(128) bias_back_kernel(const __grid_constant__ 
 // lane l has head l / 4 and, of the 64 columns, 16 (l % 4) .. + 15, four products.  32-bit values are cut into three parts of 8 bits of mantissa each.
 // What bounds it: instructions.  A bucket is looked up once for all heads of a CTA; the comparison with a bucket's number makes a
 // register of the first operand in one instruction (16-bit numbers hold 0 .. 255).
-constexpr int kBackCols = 1024, kBackMap = 16384;       // columns of a CTA; places of the map in shared memory at most
+constexpr int kBackCols = 1024, kBackMap = 8192;       // columns of a CTA; places of the map in shared memory at most
 
 template <typename T> struct OneHot;
 template <> struct OneHot<__nv_bfloat16> {
@@ -376,7 +381,7 @@ struct BackArgs {
     int width;                                 // of a block
 };
 
-template <typename T, int kTiles, int kNt, bool kWide>
+template <typename T, int kAx, int kTiles, int kNt, bool kWide>
 __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constant__ BackArgs G) {
     using H = typename BackAs<T>::Half;
     using Pair = typename OneHot<H>::Pair;
@@ -384,21 +389,21 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
     extern __shared__ __align__(16) uint8_t shared[];
     const BiasArgs& A = G.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = lane >> 2, quarter = lane & 3;
-    // axes and slices of buckets side by side: what one CTA has read, the others find in the second-level cache
-    const int sides = A.axes * G.slices, side = blockIdx.x % sides, share = blockIdx.x / sides, axis = side / G.slices, base = (side - axis * G.slices) * 16 * kTiles;
+    // groups of axes and slices of buckets side by side: what one CTA has read, the others find in the second-level cache
+    const int sides = (A.axes + kAx - 1) / kAx * G.slices, side = blockIdx.x % sides, share = blockIdx.x / sides, axis0 = side / G.slices * kAx, base = side % G.slices * 16 * kTiles;
     const int block = share % G.col_blocks, slab = share / G.col_blocks, j0 = block * G.width, cols = min(G.width, A.nk - j0);
     const int first = blockIdx.y * 8 * kNt;
     float* extra = reinterpret_cast<float*>(shared);                       // sums of what is not finite
-    int32_t* pos = reinterpret_cast<int32_t*>(extra + 16 * kTiles * 8 * kNt);
-    int32_t* ids = pos + kBackCols;
+    int32_t* pos = reinterpret_cast<int32_t*>(extra + kAx * 16 * kTiles * 8 * kNt);
+    int32_t* ids = pos + kAx * kBackCols;
     H* map = reinterpret_cast<H*>(ids + (A.k_ids ? kBackCols : 0));
     float* sums = reinterpret_cast<float*>(pos);                           // (when all else has been read)
-    for (int i = tid; i < 16 * kTiles * 8 * kNt; i += 256) extra[i] = 0.f;
+    for (int i = tid; i < kAx * 16 * kTiles * 8 * kNt; i += 256) extra[i] = 0.f;
     for (int i = tid; i <= 2 * A.reach; i += 256) {
         const int n = __ldg(A.bucket_of + i) - base;
         map[i] = (H)(float)(n >= 0 && n < 16 * kTiles && n + base < A.buckets ? n : 255);
     }
-    float acc[kNt][kTiles][4] = {};
+    float acc[kAx][kNt][kTiles][4] = {};
     int held = -1;                                                         // the batch whose columns' positions are in shared memory
     const int from = slab * G.each, to = min(from + G.each, G.rows);
     for (int line = from; line < to;) {
@@ -406,7 +411,8 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
         if (batch != held) {
             __syncthreads();
             for (int i = tid; i < kBackCols; i += 256) {
-                pos[i] = i < cols ? A.k_pos[axis * A.ks[0] + batch * A.ks[1] + (int64_t)(j0 + i) * A.ks[2]] : 0;
+#pragma unroll
+                for (int x = 0; x < kAx; ++x) pos[x * kBackCols + i] = i < cols && axis0 + x < A.axes ? A.k_pos[(axis0 + x) * A.ks[0] + batch * A.ks[1] + (int64_t)(j0 + i) * A.ks[2]] : 0;
                 if (A.k_ids) ids[i] = i < cols ? A.k_ids[batch * A.kis[0] + (int64_t)(j0 + i) * A.kis[1]] : 0;
             }
             held = batch;
@@ -414,7 +420,10 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
         }
         for (int l = line + warp; l < until; l += 8) {
             const int row = l - batch * A.nq;
-            const int q = A.q_pos[axis * A.qs[0] + batch * A.qs[1] + (int64_t)row * A.qs[2]], q_id = A.q_ids ? A.q_ids[batch * A.qis[0] + (int64_t)row * A.qis[1]] : 0;
+            int q[kAx];
+#pragma unroll
+            for (int x = 0; x < kAx; ++x) q[x] = axis0 + x < A.axes ? A.q_pos[(axis0 + x) * A.qs[0] + batch * A.qs[1] + (int64_t)row * A.qs[2]] : 0;
+            const int q_id = A.q_ids ? A.q_ids[batch * A.qis[0] + (int64_t)row * A.qis[1]] : 0;
             const T* at[kNt];
             bool has[kNt];
 #pragma unroll
@@ -478,28 +487,30 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
                         }
                 }
                 if (c0 + 64 < cols) load(raw[half], c + 64);
-                // buckets of the lane's eight columns; pairs that do not count have none
-                uint32_t n2[4];
-                {
-                    int k[8], id[8];
-                    auto eight = [&](int (&x)[8], const int32_t* from) {
-                        if (kWide) {
-                            const int4 a = *reinterpret_cast<const int4*>(from + c), b = *reinterpret_cast<const int4*>(from + c + 4);
-                            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-                        } else
+                auto eight = [&](int (&x)[8], const int32_t* from) {
+                    if (kWide) {
+                        const int4 a = *reinterpret_cast<const int4*>(from + c), b = *reinterpret_cast<const int4*>(from + c + 4);
+                        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                    } else
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = from[c + 4 * i];
-                    };
-                    eight(k, pos);
-                    if (A.q_ids) {
-                        eight(id, ids);
+                        for (int i = 0; i < 8; ++i) x[i] = from[c + 4 * i];
+                };
+                if (A.q_ids) {
+                    int id[8];
+                    eight(id, ids);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) counts &= id[i] == q_id ? ~0u : ~(1u << i);
-                    }
+                    for (int i = 0; i < 8; ++i) counts &= id[i] == q_id ? ~0u : ~(1u << i);
+                }
+                // buckets of the lane's eight columns
+                uint32_t n2[kAx][4];
+#pragma unroll
+                for (int x = 0; x < kAx; ++x) {
+                    int k[8];
+                    eight(k, pos + x * kBackCols);
                     const uint16_t* bits = reinterpret_cast<const uint16_t*>(map);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        n2[i] = bits[map_at(A.reach, k[2 * i], q)] | (uint32_t)bits[map_at(A.reach, k[2 * i + 1], q)] << 16;
+                        n2[x][i] = bits[map_at(A.reach, k[2 * i], q[x])] | (uint32_t)bits[map_at(A.reach, k[2 * i + 1], q[x])] << 16;
                 }
                 if (__any_sync(~0u, counts != 255u)) {                     // what does not count is 0, whatever stands there
 #pragma unroll
@@ -539,9 +550,12 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
                             if constexpr (kParts == 1) { const Pair p = *reinterpret_cast<const Pair*>(&v[t][0][i / 2]); x = i & 1 ? __high2float(p) : __low2float(p); }
                             else x = whole[t][i];
                             if (isfinite(x)) continue;
-                            const Pair np = *reinterpret_cast<const Pair*>(&n2[i / 2]);
-                            const int n = (int)(i & 1 ? __high2float(np) : __low2float(np));
-                            if (n < 16 * kTiles) atomicAdd(&extra[n * 8 * kNt + 8 * t + group], x);
+#pragma unroll
+                            for (int y = 0; y < kAx; ++y) {
+                                const Pair np = *reinterpret_cast<const Pair*>(&n2[y][i / 2]);
+                                const int n = (int)(i & 1 ? __high2float(np) : __low2float(np));
+                                if (n < 16 * kTiles) atomicAdd(&extra[(y * 16 * kTiles + n) * 8 * kNt + 8 * t + group], x);
+                            }
                             if constexpr (kParts == 1) v[t][0][i / 2] &= i & 1 ? 0xffffu : 0xffff0000u;
                             else whole[t][i] = 0.f;
                         }
@@ -565,18 +579,20 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
                 for (int m = 0; m < kTiles; ++m) {
                     const Pair lo = both<H>((float)(16 * m + group)), hi = both<H>((float)(16 * m + group + 8));
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        uint32_t a[4];
+                    for (int x = 0; x < kAx; ++x)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const Pair one = __heq2(*reinterpret_cast<const Pair*>(&n2[2 * s + e / 2]), e & 1 ? hi : lo);
-                            a[e] = *reinterpret_cast<const uint32_t*>(&one);
+                        for (int s = 0; s < 2; ++s) {
+                            uint32_t a[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const Pair one = __heq2(*reinterpret_cast<const Pair*>(&n2[x][2 * s + e / 2]), e & 1 ? hi : lo);
+                                a[e] = *reinterpret_cast<const uint32_t*>(&one);
+                            }
+#pragma unroll
+                            for (int t = 0; t < kNt; ++t)
+#pragma unroll
+                                for (int p = kParts - 1; p >= 0; --p) OneHot<H>::mma(acc[x][t][m], a, v[t][p][2 * s], v[t][p][2 * s + 1]);
                         }
-#pragma unroll
-                        for (int t = 0; t < kNt; ++t)
-#pragma unroll
-                            for (int p = kParts - 1; p >= 0; --p) OneHot<H>::mma(acc[t][m], a, v[t][p][2 * s], v[t][p][2 * s + 1]);
-                    }
                 }
             }
         }
@@ -587,21 +603,23 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
     for (int w = 0; w < 8; ++w) {
         if (warp == w)
 #pragma unroll
-            for (int t = 0; t < kNt; ++t)
+            for (int x = 0; x < kAx; ++x)
 #pragma unroll
-                for (int m = 0; m < kTiles; ++m)
+                for (int t = 0; t < kNt; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float& s = sums[(16 * m + group + 8 * (e / 2)) * 8 * kNt + 8 * t + 2 * quarter + (e & 1)];
-                        s = w == 0 ? acc[t][m][e] : s + acc[t][m][e];
-                    }
+                    for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float& s = sums[((x * kTiles + m) * 16 + group + 8 * (e / 2)) * 8 * kNt + 8 * t + 2 * quarter + (e & 1)];
+                            s = w == 0 ? acc[x][t][m][e] : s + acc[x][t][m][e];
+                        }
         __syncthreads();
     }
-    for (int i = tid; i < 16 * kTiles * 8 * kNt; i += 256) {
-        const int n = i / (8 * kNt), combo = first + i % (8 * kNt);
-        if (base + n >= A.buckets || combo >= G.combos) continue;
+    for (int i = tid; i < kAx * 16 * kTiles * 8 * kNt; i += 256) {
+        const int at = i / (8 * kNt), n = base + at % (16 * kTiles), axis = axis0 + at / (16 * kTiles), combo = first + i % (8 * kNt);
+        if (n >= A.buckets || axis >= A.axes || combo >= G.combos) continue;
         const int b = combo / A.heads;
-        A.partial[(((size_t)share * G.batches + b) * A.axes * A.buckets + (size_t)axis * A.buckets + base + n) * A.heads + combo - b * A.heads] = sums[i] + extra[i];
+        A.partial[(((size_t)share * G.batches + b) * A.axes * A.buckets + (size_t)axis * A.buckets + n) * A.heads + combo - b * A.heads] = sums[i] + extra[i];
     }
 }
 
