@@ -70,19 +70,21 @@ Form form_of(const pcr_decay_args& a, bool back) {
     f.chunk = f.tiles ? 128 : most > 128 ? 32 : 64;
     // two parts of bf16 hold 16 bits of a value, which an output of 16 bits does not show; a memory that is given out would
     f.parts = a.dtype == PCR_BF16 && (a.state_after || a.dstate) ? 3 : 2;
-    // Segments of equal length, as many of a sequence as end first by this count: rounds of CTAs times their chunks, two of which
-    // are as long as a CTA's beginning and end; several segments take another pass over b and c and two more launches.  Packed
-    // sequences are taken to be of equal length.
+    // Segments of equal length, as many of a sequence as end first by this count, in halves of a chunk's time: rounds of CTAs times their
+    // chunks and a CTA's beginning and end (a chunk; two where chunks are short, on the tensor cores), and for several segments half as much again
+    // and two more launches (a chunk of the plain kernel takes 14 us, one on the tensor cores 3.5).  Packed sequences are taken to be of
+    // equal length.
     const int64_t wide = (int64_t)a.q_heads * (back ? 3 : 1) * (f.tiles ? 1 : (most + kWalkCols - 1) / kWalkCols) * a.sequences;
     const int64_t room = (int64_t)sm_count() * (f.tiles ? 1 : 2), mean = std::max<int64_t>(1, a.batch * a.tokens / a.sequences), whole = (mean + f.chunk - 1) / f.chunk;
     int64_t best = 1, least = INT64_MAX;
     for (int64_t per = 1; per <= std::min<int64_t>(whole, 64); ++per) {
-        const int64_t chunks = (whole + per - 1) / per, cost = ((wide * per + room - 1) / room) * (chunks + 2) + (per > 1 ? (wide * whole + 2 * room - 1) / (2 * room) + 6 : 0);
+        const int64_t chunks = (whole + per - 1) / per, ends = f.tiles ? 2 : 1, rounds = (wide * per + room - 1) / room, less = (wide * (per - 1) + room - 1) / room;
+        const int64_t cost = 2 * rounds * (chunks + ends) + (per > 1 ? less * (chunks + ends) + (f.tiles ? 8 : 2) : 0);
         if (cost < least) { least = cost; best = per; }
     }
     int64_t seg = (whole + best - 1) / best * f.chunk;
-    // a sequence much longer than the others is cut all the same
-    if (a.starts) seg = std::max<int64_t>(seg, ((wide * whole / room + 1) / 2) * f.chunk);
+    // a sequence much longer than the others is cut all the same, but for four chunks not at all
+    if (a.starts) seg = std::max<int64_t>({seg, ((wide * whole / room + 1) / 2) * f.chunk, (int64_t)4 * f.chunk});
     seg = std::min<int64_t>(seg, std::max<int64_t>((a.tokens + f.chunk - 1) / f.chunk, 1) * f.chunk);
     f.seg = (uint32_t)seg;
     f.split = a.tokens > seg;

@@ -60,13 +60,27 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         const int64_t t0 = it.begin + (W.rev ? it.len - at - n : at);
         const bool final = it.last && at + n >= it.len && !W.rev;         // forward, the memory that is given out is not aged
         __syncthreads();                                                   // the chunk before is done with
-        for (int r = warp; r < kRows; r += 8) {
-            const bool in = r < n;
-            for (int d = lane; d < bdp; d += 32) {
-                if (!A.states) As[r * ld + d] = in && d < bd ? to_float(a[(t0 + r) * W.a.st[1] + d]) : 0.f;
-                Bs[r * ld + d] = in && d < bd ? to_float(b[(t0 + r) * W.b.st[1] + d]) : 0.f;
+        // 32 columns of every eighth row a warp, all three operands' on their way before the first is needed
+        for (int d0 = 0; d0 < max(bdp, kWalkCols); d0 += 32) {
+            constexpr int kEach = kRows / 8;
+            const int d = d0 + lane;
+            const bool ab = d < bd, cc = d < cols;
+            T x[3][kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = warp + 8 * i;
+                const bool in = r < n;
+                const T none = from_float<T>(0.f);
+                x[0][i] = !A.states && in && ab ? a[(t0 + r) * W.a.st[1] + d] : none;
+                x[1][i] = in && ab ? b[(t0 + r) * W.b.st[1] + d] : none;
+                x[2][i] = in && cc ? c[(t0 + r) * W.c.st[1] + d] : none;
             }
-            for (int d = lane; d < kWalkCols; d += 32) Cs[r * kWalkCols + d] = in && d < cols ? to_float(c[(t0 + r) * W.c.st[1] + d]) : 0.f;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = warp + 8 * i;
+                if (d < bdp) { As[r * ld + d] = to_float(x[0][i]); Bs[r * ld + d] = to_float(x[1][i]); }
+                if (d < kWalkCols) Cs[r * kWalkCols + d] = to_float(x[2][i]);
+            }
         }
         __syncthreads();
         if (!A.states) {
@@ -89,15 +103,25 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
                     const int r = ty + 16 * i, q = tx + 16 * j, far = W.rev ? q - r : r - q;
                     Ps[r * (kRows + 4) + q] = far >= 0 ? s[i][j] * pw[far] : 0.f;
                 }
+            // four rows by four columns a thread, four steps of the sum at a time: eight loads of 16 bytes for 64 products
             float o[kPer][4] = {};
-            for (int d = 0; d < bdp; ++d) {
-                const float4 m = *reinterpret_cast<const float4*>(Rs + d * kWalkCols + 4 * tx);
+            auto add = [&](const float* rows, int ld_rows, const float* with, int steps) {
+#pragma unroll 2
+                for (int d = 0; d < steps; d += 4) {
+                    float4 m[4];
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const float x = As[(ty + 16 * i) * ld + d];
-                    o[i][0] += x * m.x; o[i][1] += x * m.y; o[i][2] += x * m.z; o[i][3] += x * m.w;
+                    for (int e = 0; e < 4; ++e) m[e] = *reinterpret_cast<const float4*>(with + (d + e) * kWalkCols + 4 * tx);
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        const float4 x = *reinterpret_cast<const float4*>(rows + (ty + 16 * i) * ld_rows + d);
+                        o[i][0] += x.x * m[0].x + x.y * m[1].x + x.z * m[2].x + x.w * m[3].x;
+                        o[i][1] += x.x * m[0].y + x.y * m[1].y + x.z * m[2].y + x.w * m[3].y;
+                        o[i][2] += x.x * m[0].z + x.y * m[1].z + x.z * m[2].z + x.w * m[3].z;
+                        o[i][3] += x.x * m[0].w + x.y * m[1].w + x.z * m[2].w + x.w * m[3].w;
+                    }
                 }
-            }
+            };
+            add(As, ld, Rs, bdp);
             float past[kPer][4];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -106,14 +130,7 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
                 for (int e = 0; e < 4; ++e) past[i][e] = o[i][e] = o[i][e] * (r < n ? pw[far] : 0.f);
             }
             __syncthreads();
-            for (int q = 0; q < kRows; ++q) {
-                const float4 m = *reinterpret_cast<const float4*>(Cs + q * kWalkCols + 4 * tx);
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const float x = Ps[(ty + 16 * i) * (kRows + 4) + q];
-                    o[i][0] += x * m.x; o[i][1] += x * m.y; o[i][2] += x * m.z; o[i][3] += x * m.w;
-                }
-            }
+            add(Ps, kRows + 4, Cs, kRows);
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int r = ty + 16 * i;
@@ -132,18 +149,33 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
                 }
             }
         }
-        // the memory: every thread its own elements, nobody else reads them before the next chunk
+        // the memory: rows of B times their factors, then four rows by four columns of it a thread
+        __syncthreads();
+        for (int i = tid; i < kRows * (bdp / 4); i += kWalkThreads) {
+            const int r = i / (bdp / 4);
+            float4* x = reinterpret_cast<float4*>(Bs + r * ld) + (i - r * (bdp / 4));
+            const float f = r < n ? pw[(W.rev ? r + 1 : n - r) - (final ? 1 : 0)] : 0.f;
+            *x = make_float4(x->x * f, x->y * f, x->z * f, x->w * f);
+        }
         __syncthreads();
         const float keep = power(rate, final ? n - 1 : n);
-        for (int i = ty; i < bdp; i += 16) {
-            float4 m = *reinterpret_cast<const float4*>(Rs + i * kWalkCols + 4 * tx);
-            m.x *= keep; m.y *= keep; m.z *= keep; m.w *= keep;
-            for (int r = 0; r < n; ++r) {
-                const float x = Bs[r * ld + i] * pw[(W.rev ? r + 1 : n - r) - (final ? 1 : 0)];
-                const float4 v = *reinterpret_cast<const float4*>(Cs + r * kWalkCols + 4 * tx);
-                m.x += x * v.x; m.y += x * v.y; m.z += x * v.z; m.w += x * v.w;
+        for (int i = 4 * ty; i < bdp; i += 64) {
+            float m[4][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float4 x = *reinterpret_cast<const float4*>(Rs + (i + e) * kWalkCols + 4 * tx);
+                m[e][0] = x.x * keep; m[e][1] = x.y * keep; m[e][2] = x.z * keep; m[e][3] = x.w * keep;
             }
-            *reinterpret_cast<float4*>(Rs + i * kWalkCols + 4 * tx) = m;
+#pragma unroll 4
+            for (int r = 0; r < n; ++r) {
+                const float4 x = *reinterpret_cast<const float4*>(Bs + r * ld + i), v = *reinterpret_cast<const float4*>(Cs + r * kWalkCols + 4 * tx);
+                m[0][0] += x.x * v.x; m[0][1] += x.x * v.y; m[0][2] += x.x * v.z; m[0][3] += x.x * v.w;
+                m[1][0] += x.y * v.x; m[1][1] += x.y * v.y; m[1][2] += x.y * v.z; m[1][3] += x.y * v.w;
+                m[2][0] += x.z * v.x; m[2][1] += x.z * v.y; m[2][2] += x.z * v.z; m[2][3] += x.z * v.w;
+                m[3][0] += x.w * v.x; m[3][1] += x.w * v.y; m[3][2] += x.w * v.z; m[3][3] += x.w * v.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<float4*>(Rs + (i + e) * kWalkCols + 4 * tx) = make_float4(m[e][0], m[e][1], m[e][2], m[e][3]);
         }
     }
     __syncthreads();
