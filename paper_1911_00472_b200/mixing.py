@@ -36,10 +36,10 @@ def _operands(tensors):
             raise ValueError("all operands have to be on one device")
         followed = followed or t.requires_grad
         negated = negated or t.is_neg()
-    if device.type != "cuda":
-        raise ValueError("operands have to be on a CUDA device")
     if (followed and torch.is_grad_enabled()) or (_forward_mode() and _has_tangent(tensors)):
         raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
+    if device.type != "cuda":
+        raise ValueError("operands have to be on a CUDA device")
     if negated:
         tensors = [None if t is None else t.resolve_neg() for t in tensors]
     return device, tensors
