@@ -196,7 +196,7 @@ int launch_tiles_of(const BackArgs& G, const BackForm& f, dim3 grid, bool wide, 
 }
 template <typename T>
 int launch_back(const BackArgs& G, const BackForm& f, bool wide, cudaStream_t st) {
-    const dim3 grid((unsigned)(f.row_slabs * f.col_blocks * ((G.a.axes + f.ax - 1) / f.ax) * f.slices), (f.combos + 8 * f.nt - 1) / (8 * f.nt));
+    const dim3 grid((unsigned)(f.row_slabs * f.col_blocks * ((G.a.axes + f.ax - 1) / f.ax) * f.slices) * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)));
     if (f.nt == 1) return launch_tiles_of<T, 1>(G, f, grid, wide, st);
     if constexpr (sizeof(T) == 2)
         if (f.nt == 4) {

@@ -390,9 +390,9 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
     const BiasArgs& A = G.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = lane >> 2, quarter = lane & 3;
     // groups of axes and slices of buckets side by side: what one CTA has read, the others find in the second-level cache
-    const int sides = (A.axes + kAx - 1) / kAx * G.slices, side = blockIdx.x % sides, share = blockIdx.x / sides, axis0 = side / G.slices * kAx, base = side % G.slices * 16 * kTiles;
+    const int sides = (A.axes + kAx - 1) / kAx * G.slices, side = blockIdx.x % sides, all = G.col_blocks * G.row_slabs, share = blockIdx.x / sides % all, axis0 = side / G.slices * kAx, base = side % G.slices * 16 * kTiles;
     const int block = share % G.col_blocks, slab = share / G.col_blocks, j0 = block * G.width, cols = min(G.width, A.nk - j0);
-    const int first = blockIdx.y * 8 * kNt;
+    const int first = (int)(blockIdx.x / sides / all) * 8 * kNt;
     float* extra = reinterpret_cast<float*>(shared);                       // sums of what is not finite
     int32_t* pos = reinterpret_cast<int32_t*>(extra + kAx * 16 * kTiles * 8 * kNt);
     int32_t* ids = pos + kAx * kBackCols;
@@ -400,8 +400,8 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
     float* sums = reinterpret_cast<float*>(pos);                           // (when all else has been read)
     for (int i = tid; i < kAx * 16 * kTiles * 8 * kNt; i += 256) extra[i] = 0.f;
     for (int i = tid; i <= 2 * A.reach; i += 256) {
-        const int n = __ldg(A.bucket_of + i) - base;
-        map[i] = (H)(float)(n >= 0 && n < 16 * kTiles && n + base < A.buckets ? n : 255);
+        const int n = __ldg(A.bucket_of + i);
+        map[i] = (H)(float)(n >= base && n < base + 16 * kTiles && n < A.buckets ? n - base : 255);
     }
     float acc[kAx][kNt][kTiles][4] = {};
     int held = -1;                                                         // the batch whose columns' positions are in shared memory

@@ -61,12 +61,13 @@ struct Form {
     size_t slot_bytes, shared_bytes;            // of one direction's memories; of the gradients that heads share
 };
 
-bool nothing(const pcr_decay_args& a) { return a.sequences == 0; }
+// (rows of no sequence may have to become 0 all the same)
+bool nothing(const pcr_decay_args& a) { return a.sequences == 0 && !(a.starts && a.tokens > 0 && (a.flags & PCR_DECAY_ZERO_TAIL)); }
 
 Form form_of(const pcr_decay_args& a, bool back) {
     Form f = {};
     const int most = std::max(a.k_dim, a.v_dim);
-    f.tiles = tiles_fit(a, back);
+    f.tiles = a.sequences > 0 && tiles_fit(a, back);
     f.chunk = f.tiles ? 128 : most > 128 ? 32 : 64;
     // two parts of bf16 hold 16 bits of a value, which an output of 16 bits does not show; a memory that is given out would
     f.parts = a.dtype == PCR_BF16 && (a.state_after || a.dstate) ? 3 : 2;
@@ -75,7 +76,7 @@ Form form_of(const pcr_decay_args& a, bool back) {
     // and two more launches (a chunk of the plain kernel takes 14 us, one on the tensor cores 3.5).  Packed sequences are taken to be of
     // equal length.
     const int64_t wide = (int64_t)a.q_heads * (back ? 3 : 1) * (f.tiles ? 1 : (most + kWalkCols - 1) / kWalkCols) * a.sequences;
-    const int64_t room = (int64_t)sm_count() * (f.tiles ? 1 : 2), mean = std::max<int64_t>(1, a.batch * a.tokens / a.sequences), whole = (mean + f.chunk - 1) / f.chunk;
+    const int64_t room = (int64_t)sm_count() * (f.tiles ? 1 : 2), mean = std::max<int64_t>(1, a.batch * a.tokens / std::max<int64_t>(1, a.sequences)), whole = (mean + f.chunk - 1) / f.chunk;
     int64_t best = 1, least = INT64_MAX;
     for (int64_t per = 1; per <= std::min<int64_t>(whole, 64); ++per) {
         const int64_t chunks = (whole + per - 1) / per, ends = f.tiles ? 2 : 1, rounds = (wide * per + room - 1) / room, less = (wide * (per - 1) + room - 1) / room;
@@ -88,7 +89,7 @@ Form form_of(const pcr_decay_args& a, bool back) {
     seg = std::min<int64_t>(seg, std::max<int64_t>((a.tokens + f.chunk - 1) / f.chunk, 1) * f.chunk);
     f.seg = (uint32_t)seg;
     f.split = a.tokens > seg;
-    if (a.starts) { f.keys = (uint32_t)(a.sequences + a.tokens / seg); f.slots = f.split ? (uint32_t)(a.tokens / seg) : 0; }
+    if (a.starts) { f.keys = (uint32_t)std::max<int64_t>(1, a.sequences + a.tokens / seg); f.slots = f.split ? (uint32_t)(a.tokens / seg) : 0; }
     else {
         const int64_t per = std::max<int64_t>((a.tokens + seg - 1) / seg, 1);
         f.keys = (uint32_t)(a.batch * per); f.slots = (uint32_t)(a.batch * (per - 1));
@@ -206,7 +207,7 @@ int run(WalkArgs& states, const int (*states_of)[3], WalkArgs& walks, const int 
 WalkArgs common(const pcr_decay_args& a, const Form& f) {
     WalkArgs A = {};
     A.log_decay = a.log_decay; A.starts = a.starts; A.sequences = (uint32_t)a.sequences; A.tokens = (uint32_t)a.tokens;
-    A.seg = f.seg; A.heads = a.q_heads; A.split = f.split;
+    A.seg = f.seg; A.heads = a.q_heads;
     return A;
 }
 

@@ -68,6 +68,8 @@ int launch_sizes(const TileArgs& G, unsigned keys, cudaStream_t st) {
 
 bool tiles_fit(const pcr_decay_args& a, bool back) {
     if (a.dtype == PCR_F32 || a.k_dim > 128 || a.v_dim > 128 || a.k_dim % 8 || a.v_dim % 8 || a.batch * a.tokens == 0 || !encoder()) return false;
+    // (one CTA for every segment, head and gradient, numbered in 31 bits)
+    if ((a.sequences + a.batch * (a.tokens / kTile + 1)) * a.q_heads * (back ? 3 : 1) > INT32_MAX) return false;
     const bool in = fits(a.q, a.batch, a.tokens, a.q_heads) && fits(a.k, a.batch, a.tokens, a.k_heads) && fits(a.v, a.batch, a.tokens, a.k_heads) && fits(a.out, a.batch, a.tokens, a.q_heads);
     if (!in || !back) return in;
     return fits(a.dq, a.batch, a.tokens, a.q_heads) && fits(a.dk, a.batch, a.tokens, a.k_heads) && fits(a.dv, a.batch, a.tokens, a.k_heads);

@@ -222,13 +222,13 @@ __device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t
         tensor_load16(o, O + j0);
         tensor_load16(m, I + j0);
         tensor_load_wait();
-        uint32_t odd = 0;
+        uint32_t odd = 0, open = 0;                                        // open: not settled by the memory, which is no number from a token like that on
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             m[j] *= (cs ? from_middle(cs[j0 + j]) : 1.f) * age;
-            if (j0 + j < W.cd && r < n && !isfinite(o[j] * off + m[j])) odd |= 1u << j;
+            if (j0 + j < W.cd && r < n && !isfinite(o[j] * off + m[j])) { odd |= 1u << j; open |= (uint32_t)!isnan(m[j]) << j; }
         }
-        for (int q = W.rev ? r : 0; odd && q <= (W.rev ? n - 1 : r); ++q) {
+        for (int q = W.rev ? r : 0; open && q <= (W.rev ? n - 1 : r); ++q) {
             float s = 0.f;
             for (int d = 0; d < W.bd; ++d) s += to_float(a[d]) * to_float(b[q * W.b.st[1] + d]);
             s *= power(rate, W.rev ? q - r : r - q);

@@ -45,7 +45,7 @@ struct WalkArgs {
     const float* log_decay;
     const int32_t* starts;                     // sequences + 1, or null: every batch is one of `tokens`
     uint32_t sequences, tokens, seg;           // tokens of a segment: a multiple of the chunk
-    int heads, kinds, states, split;           // states: only what segments add; split: sequences may have several segments
+    int heads, kinds, states;                  // states: only what segments add
 };
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
@@ -82,6 +82,7 @@ __device__ __forceinline__ bool item_of(const WalkArgs& A, int rev, uint32_t key
         it.begin = 0; it.len = (int)A.tokens;
         it.slot = it.seq * (int)(per - 1) + it.m;
     } else {
+        if (A.sequences == 0) return false;
         // the last sequence whose first key is not beyond `key`: 32 tries at a time
         const int lane = threadIdx.x & 31;
         uint32_t lo = 0, count = A.sequences;

@@ -24,8 +24,9 @@ _BIAS_ARGS = struct.Struct("<3Q3qQ3qQ2qQ2qQ3q3q6i")  # pcr_bias_args
 _NO_ROWS = (0, 0, 0, 0)
 
 
-def _operands(tensors):
-    """One device, none that autograd follows (it does not see these calls), signs resolved: the tensors to read from."""
+def _operands(tensors, stream):
+    """One device, none that autograd follows (it does not see these calls), signs resolved (once the call is on its own device and stream):
+    the tensors to read from."""
     device, followed, negated = None, False, False
     for t in tensors:
         if t is None:
@@ -40,7 +41,7 @@ def _operands(tensors):
         raise ValueError("autograd does not see this call: detach the operands and call the backward pass yourself")
     if device.type != "cuda":
         raise ValueError("operands have to be on a CUDA device")
-    if negated:
+    if negated and stream is None and _current_device() == device.index:
         tensors = [None if t is None else t.resolve_neg() for t in tensors]
     return device, tensors
 
@@ -127,7 +128,7 @@ def decay_attention(q, k, v, log_decay, *, starts=None, state=None, final=False,
     batch, tokens, n, hq, hk, kd, vd = _decay_shapes(q, k, v, log_decay, starts, (3, 4))
     memories = (n, hq, kd, vd)
     _memory(state, memories, "state")
-    device, (q, k, v, log_decay, starts, state) = _operands((q, k, v, log_decay, starts, state))
+    device, (q, k, v, log_decay, starts, state) = _operands((q, k, v, log_decay, starts, state), stream)
     if out is not None:
         _output(out, (*q.shape[:-1], vd), q.dtype, device, "out")
     given = torch.is_tensor(final)
@@ -160,7 +161,7 @@ def decay_attention_backward(grad, q, k, v, log_decay, *, starts=None, state=Non
     _memory(grad_final, memories, "grad_final")
     if grad.shape != (*q.shape[:-1], vd) or grad.dtype != q.dtype:
         raise ValueError("grad must have the shape and the dtype of the outputs")
-    device, (grad, q, k, v, log_decay, starts, state, grad_final) = _operands((grad, q, k, v, log_decay, starts, state, grad_final))
+    device, (grad, q, k, v, log_decay, starts, state, grad_final) = _operands((grad, q, k, v, log_decay, starts, state, grad_final), stream)
     if out is not None:
         for o, x, what in zip(out, (q, k, v), ("out[0]", "out[1]", "out[2]"), strict=True):
             _output(o, x.shape, x.dtype, device, what)
@@ -194,7 +195,7 @@ def decay_step(q, k, v, log_decay, state, *, slots=None, out=None, stream=None):
             raise ValueError("state must have a memory for every request")
     elif slots.shape != (rows,) or slots.dtype != torch.int32 or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int32 vector, an element for each request")
-    device, (q, k, v, log_decay, slots) = _operands((q, k, v, log_decay, slots))
+    device, (q, k, v, log_decay, slots) = _operands((q, k, v, log_decay, slots), stream)
     if state.device != device:
         raise ValueError("all operands have to be on one device")
     _not_followed(state)
@@ -284,7 +285,7 @@ def relative_bias(table, buckets, q_positions, k_positions=None, *, q_ids=None, 
         raise ValueError("dtype must be float16, bfloat16 or float32, the table's or any where that is float32")
     heads = table.shape[2]
     shape = (heads, nq, nk) if batch is None else (batch, heads, nq, nk)
-    device, (table, buckets, q_positions, k_positions, q_ids, k_ids) = _operands((table, buckets, q_positions, k_positions, q_ids, k_ids))
+    device, (table, buckets, q_positions, k_positions, q_ids, k_ids) = _operands((table, buckets, q_positions, k_positions, q_ids, k_ids), stream)
     if out is not None:
         _output(out, shape, dtype, device, "out")
     if stream is not None or _current_device() != device.index:
@@ -312,7 +313,7 @@ def relative_bias_backward(grad, n_buckets, buckets, q_positions, k_positions=No
     if dtype not in _CODES or n_buckets < 1:
         raise ValueError("dtype must be float16, bfloat16 or float32, and there must be buckets")
     heads = grad.shape[-3]
-    device, (grad, buckets, q_positions, k_positions, q_ids, k_ids) = _operands((grad, buckets, q_positions, k_positions, q_ids, k_ids))
+    device, (grad, buckets, q_positions, k_positions, q_ids, k_ids) = _operands((grad, buckets, q_positions, k_positions, q_ids, k_ids), stream)
     if stream is not None or _current_device() != device.index:
         with _on(device, stream):
             return relative_bias_backward(grad, n_buckets, buckets, q_positions, k_positions, q_ids=q_ids, k_ids=k_ids, dtype=dtype)
