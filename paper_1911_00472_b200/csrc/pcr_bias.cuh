@@ -403,7 +403,19 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
         const int n = __ldg(A.bucket_of + i);
         map[i] = (H)(float)(n >= base && n < base + 16 * kTiles && n < A.buckets ? n - base : 255);
     }
-    float acc[kAx][kNt][kTiles][4] = {};
+    float acc[kAx][kNt][kTiles][4] = {}, total[kAx][kNt][kTiles][4] = {};
+    // The tensor cores cut off what their sums have no bits for: single ones would lose half a step with every product, always to the same side.  So they add
+    // up a few products only (which values of 16 bits leave exact, or nearly so, for a row), and those sums are rounded.
+    auto settle = [&] {
+#pragma unroll
+        for (int x = 0; x < kAx; ++x)
+#pragma unroll
+            for (int t = 0; t < kNt; ++t)
+#pragma unroll
+                for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { total[x][t][m][e] += acc[x][t][m][e]; acc[x][t][m][e] = 0.f; }
+    };
     int held = -1;                                                         // the batch whose columns' positions are in shared memory
     const int from = slab * G.each, to = min(from + G.each, G.rows);
     for (int line = from; line < to;) {
@@ -594,7 +606,9 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
                                 for (int p = kParts - 1; p >= 0; --p) OneHot<H>::mma(acc[x][t][m], a, v[t][p][2 * s], v[t][p][2 * s + 1]);
                         }
                 }
+                if (kParts == 3 && half) settle();
             }
+            if (kParts == 1) settle();
         }
         line = until;
     }
@@ -611,7 +625,7 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             float& s = sums[((x * kTiles + m) * 16 + group + 8 * (e / 2)) * 8 * kNt + 8 * t + 2 * quarter + (e & 1)];
-                            s = w == 0 ? acc[x][t][m][e] : s + acc[x][t][m][e];
+                            s = w == 0 ? total[x][t][m][e] : s + total[x][t][m][e];
                         }
         __syncthreads();
     }

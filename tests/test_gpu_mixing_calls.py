@@ -209,3 +209,23 @@ def test_a_memory_that_is_no_number(dtype):
     assert ((y[0, :3, 1, 5].double() - clean[0, :3, 1, 5].double()).abs() <= 2 * torch.finfo(dtype).eps * E).all()
     where[0, :3, 1, 5] = True
     assert torch.equal(y[~where], clean[~where])
+
+
+@pytest.mark.parametrize("n,dtype", [(4096, torch.float32), (16384, torch.bfloat16), (16384, torch.float16)], ids=str)
+def test_long_sums_of_one_sign(n, dtype):
+    """Gradients that are all positive, so that nothing hides what a sum loses.  u = 2^-24; every error is relative to the sum itself.
+    A sum in the tensor cores goes over 64 columns (32 bits: 12 products, 3 parts of 4) or a row's 1024 (16 bits: 64 products), each of
+    which may cut off 2 u.  Those sums are added up by warps, rounded: at most (n rows, n / 1024 blocks of columns, 400 CTAs of 8 warps at
+    the least, and one row more) rows times 16 or 1; then 8 warps, then 64 bits, one rounding."""
+    g = torch.Generator(device=DEV).manual_seed(6)
+    grad = torch.rand(4, n, n, device=DEV, generator=g, dtype=torch.float32).to(dtype)
+    pos = torch.arange(n, device=DEV, dtype=torch.int32)[None]
+    buckets = P.relative_buckets(32, 128, device=DEV)
+    got = P.relative_bias_backward(grad, 32, buckets, pos)[0].double()
+    want = torch.zeros(32, 4, dtype=torch.float64, device=DEV)
+    for r in range(0, n, 512):
+        at = buckets.long()[(pos[0][None, :] - pos[0][r:r + 512][:, None]).long().clamp(-128, 128) + 128]
+        want.index_add_(0, at.flatten(), grad[:, r:r + 512].double().flatten(1).T)
+    rows = n * (n // 1024) // (400 * 8) + 1
+    cut, added = (24, 16 * rows) if dtype == torch.float32 else (128, rows)
+    assert ((got - want).abs() <= (cut + added + 8 + 1) * 2.0 ** -24 * want).all()
