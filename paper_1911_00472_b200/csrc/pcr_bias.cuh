@@ -355,16 +355,18 @@ constexpr int kBackCols = 1024, kBackMap = 8192;       // columns of a CTA; plac
 template <typename T> struct OneHot;
 template <> struct OneHot<__nv_bfloat16> {
     using Pair = __nv_bfloat162;
-    __device__ static void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    __device__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
     }
 };
 template <> struct OneHot<__half> {
     using Pair = __half2;
-    __device__ static void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    __device__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
     }
 };
 template <typename H> __device__ __forceinline__ typename OneHot<H>::Pair both(float v);
@@ -381,8 +383,10 @@ struct BackArgs {
     int width;                                 // of a block
 };
 
+// (Two CTAs an SM where their sums leave room: 2048 x 2048, 32 heads, two axes of 32 buckets in bf16 163 us, at one 183; what is added to once a
+// row may wait in local memory.  With more sums than that their own loads and stores cost more than the second CTA gives.)
 template <typename T, int kAx, int kTiles, int kNt, bool kWide>
-__global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constant__ BackArgs G) {
+__global__ void __launch_bounds__(256, kAx * kTiles * kNt <= (sizeof(T) == 2 ? 8 : 4) ? 2 : 1) bias_back_mma_kernel(const __grid_constant__ BackArgs G) {
     using H = typename BackAs<T>::Half;
     using Pair = typename OneHot<H>::Pair;
     constexpr int kParts = BackAs<T>::kParts;
@@ -414,7 +418,7 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
 #pragma unroll
                 for (int m = 0; m < kTiles; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { total[x][t][m][e] += acc[x][t][m][e]; acc[x][t][m][e] = 0.f; }
+                    for (int e = 0; e < 4; ++e) { total[x][t][m][e] += acc[x][t][m][e]; if (kParts == 1) acc[x][t][m][e] = 0.f; }
     };
     int held = -1;                                                         // the batch whose columns' positions are in shared memory
     const int from = slab * G.each, to = min(from + G.each, G.rows);
@@ -603,7 +607,11 @@ __global__ void __launch_bounds__(256) bias_back_mma_kernel(const __grid_constan
 #pragma unroll
                             for (int t = 0; t < kNt; ++t)
 #pragma unroll
-                                for (int p = kParts - 1; p >= 0; --p) OneHot<H>::mma(acc[x][t][m], a, v[t][p][2 * s], v[t][p][2 * s + 1]);
+                                for (int p = kParts - 1; p >= 0; --p) {
+                                    const float none[4] = {};
+                                    if (kParts == 3 && half == 0 && s == 0 && p == 2) OneHot<H>::mma(acc[x][t][m], a, v[t][p][2 * s], v[t][p][2 * s + 1], none);
+                                    else OneHot<H>::mma(acc[x][t][m], a, v[t][p][2 * s], v[t][p][2 * s + 1], acc[x][t][m]);
+                                }
                         }
                 }
                 if (kParts == 3 && half) settle();
