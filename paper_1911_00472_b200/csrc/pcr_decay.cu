@@ -188,7 +188,7 @@ int launch_any(const WalkArgs& A, const Form& f, int dtype, cudaStream_t st) {
 int run(WalkArgs& states, const int (*states_of)[3], WalkArgs& walks, const int (*walks_of)[3], const Form& f, const pcr_decay_args& a, cudaStream_t st) {
     if (f.split) {
         states.states = 1;
-        if (int rc = f.tiles ? launch_tiles(states, states_of, a, f.keys, f.parts, st) : launch_any(states, f, a.dtype, st)) return rc;
+        if (int rc = f.tiles ? launch_tiles(states, states_of, a, f.keys, f.parts, sm_count(), st) : launch_any(states, f, a.dtype, st)) return rc;
         int of = 0;
         for (int i = 0; i < states.kinds; ++i) of = std::max(of, states.w[i].bd * states.w[i].cd);
         // (memories begin at 16 bytes where they are whole vectors; several heads to a CTA where sequences alone give CTAs enough)
@@ -201,7 +201,7 @@ int run(WalkArgs& states, const int (*states_of)[3], WalkArgs& walks, const int 
         if (int rc = finish()) return rc;
     }
     walks.states = 0;
-    return f.tiles ? launch_tiles(walks, walks_of, a, f.keys, f.parts, st) : launch_any(walks, f, a.dtype, st);
+    return f.tiles ? launch_tiles(walks, walks_of, a, f.keys, f.parts, sm_count(), st) : launch_any(walks, f, a.dtype, st);
 }
 
 WalkArgs common(const pcr_decay_args& a, const Form& f) {

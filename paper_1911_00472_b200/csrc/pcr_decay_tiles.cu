@@ -46,22 +46,23 @@ bool map_of(CUtensorMap* m, const pcr_rows& r, const pcr_decay_args& a, int head
 }
 
 template <typename T, int DB, bool kStates>
-int launch(const TileArgs& G, unsigned keys, cudaStream_t st) {
+int launch(TileArgs& G, unsigned keys, int sms, cudaStream_t st) {
     constexpr int kShared = TileShared<DB, kStates>::kBytes;
     if (cudaFuncSetAttribute(tile_kernel<T, DB, kStates>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared) != cudaSuccess) {
         cudaGetLastError();
         return PCR_E_CUDA;
     }
-    tile_kernel<T, DB, kStates><<<keys * G.walks.heads * G.walks.kinds, kTileThreads, kShared, st>>>(G);
+    G.items = keys * G.walks.heads * G.walks.kinds;
+    tile_kernel<T, DB, kStates><<<kStates ? std::min(G.items, (unsigned)sms) : G.items, kTileThreads, kShared, st>>>(G);
     ++g_launches;
     return cudaGetLastError() == cudaSuccess ? PCR_OK : PCR_E_CUDA;
 }
 template <typename T>
-int launch_sizes(const TileArgs& G, unsigned keys, cudaStream_t st) {
+int launch_sizes(TileArgs& G, unsigned keys, int sms, cudaStream_t st) {
     int bd = 0;
     for (int i = 0; i < G.walks.kinds; ++i) bd = std::max(bd, G.walks.w[i].bd);
-    if (G.walks.states) return bd <= 64 ? launch<T, 64, true>(G, keys, st) : launch<T, 128, true>(G, keys, st);
-    return bd <= 64 ? launch<T, 64, false>(G, keys, st) : launch<T, 128, false>(G, keys, st);
+    if (G.walks.states) return bd <= 64 ? launch<T, 64, true>(G, keys, sms, st) : launch<T, 128, true>(G, keys, sms, st);
+    return bd <= 64 ? launch<T, 64, false>(G, keys, sms, st) : launch<T, 128, false>(G, keys, sms, st);
 }
 
 }  // namespace
@@ -75,7 +76,7 @@ bool tiles_fit(const pcr_decay_args& a, bool back) {
     return fits(a.dq, a.batch, a.tokens, a.q_heads) && fits(a.dk, a.batch, a.tokens, a.k_heads) && fits(a.dv, a.batch, a.tokens, a.k_heads);
 }
 
-int launch_tiles(const WalkArgs& walks, const int (*of)[3], const pcr_decay_args& a, unsigned keys, int parts, cudaStream_t st) {
+int launch_tiles(const WalkArgs& walks, const int (*of)[3], const pcr_decay_args& a, unsigned keys, int parts, int sms, cudaStream_t st) {
     TileArgs G;
     G.walks = walks;
     G.parts = parts;
@@ -86,7 +87,7 @@ int launch_tiles(const WalkArgs& walks, const int (*of)[3], const pcr_decay_args
     }
     if (!map_of(&G.maps.q, a.q, a, a.q_heads, a.k_dim) || !map_of(&G.maps.k, a.k, a, a.k_heads, a.k_dim) || !map_of(&G.maps.v, a.v, a, a.k_heads, a.v_dim) ||
         !map_of(&G.maps.g, a.out, a, a.q_heads, a.v_dim)) return PCR_E_CUDA;
-    return a.dtype == PCR_F16 ? launch_sizes<__half>(G, keys, st) : launch_sizes<__nv_bfloat16>(G, keys, st);
+    return a.dtype == PCR_F16 ? launch_sizes<__half>(G, keys, sms, st) : launch_sizes<__nv_bfloat16>(G, keys, sms, st);
 }
 
 }  // namespace pcr

@@ -15,8 +15,8 @@
 // which is taken off again behind the product.
 //
 // 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
-// products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue), so that
-// copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  From one chunk to
+// products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue; what
+// segments add is dealt out), so that copies of its first tiles go on under the end of the one before.  Tiles lie in a ring, each is given back by itself.  From one chunk to
 // the next there are two chains: B' and D; and the memory's sum, its image and I.  P, O and the next S go beside them.
 // Code is kept short and in loops where it can be: the roles' code runs side by side on every scheduler, and what is unrolled comes out of
 // the instruction caches at 4 to 8 cycles an instruction.
@@ -42,6 +42,7 @@ struct TileArgs {
     WalkArgs walks;
     int of[3][3];                              // which map is a, b, c of a walk
     int parts;                                 // of B'
+    uint32_t items;                            // segments (of every head and walk) to look at
 };
 
 // Shared memory of a CTA, from a boundary of 1024 bytes on: a ring of tiles, the memory's image, lo.  A chunk's tiles are A, B and C, one
@@ -308,6 +309,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
     static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
     volatile int* dead = &bars->dead;
+    // Packed sequences, whose lengths the host does not know: often none of them is longer than a segment (looked up by as many threads as there are, up to
+    // some number that takes about a microsecond).
+    if (kStates && A.starts && A.sequences <= 16 * kTileThreads) {
+        bool longer = false;
+        for (uint32_t i = tid; i < A.sequences; i += kTileThreads) longer |= start_of(A, 0, i + 1) - start_of(A, 0, i) > A.seg;
+        if (!__syncthreads_or(longer)) return;
+    }
 
     if (tid == 0) {
         for (int s = 0; s < L::kPlaces; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
@@ -551,6 +559,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
                 __syncwarp();
                 if (x < 0) break;
+                if (kStates) {                                             // all of a length, and many none: dealt out
+                    x = (uint32_t)x + gridDim.x < G.items ? (int)(x + gridDim.x) : -1;
+                    continue;
+                }
                 if (lane == 0) {
                     order_shared();
                     bar_expect(&bars->answer, 16);
