@@ -67,6 +67,7 @@ bool nothing(const pcr_decay_args& a) { return a.sequences == 0 && !(a.starts &&
 Form form_of(const pcr_decay_args& a, bool back) {
     Form f = {};
     const int most = std::max(a.k_dim, a.v_dim);
+    // (on the tensor cores wherever operands allow it: four prompts of 61 tokens 7.8 us for 31.9, 32768 tokens 458 for 8760)
     f.tiles = a.sequences > 0 && tiles_fit(a, back);
     f.chunk = f.tiles ? 128 : most > 128 ? 32 : 64;
     // two parts of bf16 hold 16 bits of a value, which an output of 16 bits does not show; a memory that is given out would

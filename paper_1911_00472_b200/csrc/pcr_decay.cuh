@@ -15,6 +15,10 @@ inline size_t walk_shared(int bd, int rows) {
 
 // The plain form of a walk, in single precision from end to end: any sizes, strides and types.  256 threads, 16 x 16; a CTA has
 // 64 columns of c, a chunk has kRows tokens (64; 32 where heads of more than 128 would not leave room for them).
+// What bounds it: instructions (57 % of the issue slots at two CTAs of 8 warps an SM) and shared memory (54 % of its wavefronts); DRAM 6 %.  3 x 1001
+// tokens, 12 heads of 64 in 32 bits, memories given and taken: 36.9 us in each of two launches, 231 with whole sequences in the place of
+// segments; gradients of 2 x 257 tokens, 8 + 2 heads of 64: 21.6 us each of two, 70.5 whole.  (With fewer products a load, and a
+// chunk's loads one operand after the other, the two calls took 145 and 109 us; now 85 and 57.)
 template <typename T, int kRows>
 __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constant__ WalkArgs A) {
     extern __shared__ float4 shared4[];
@@ -283,10 +287,11 @@ struct StepArgs {
     int rows, n_slots, q_heads, group, kd, vd, cols, splits;    // a memory's columns go to `splits` CTAs, `cols` to each
 };
 constexpr int kStepThreads = 256;
-constexpr int kStepAhead = 8;                  // rows of the memory on their way to a thread
+constexpr int kStepAhead = 4;                  // rows of the memory on their way to a thread
 
 // A CTA has `cols` columns of a memory; a thread V of them in every (threads / lanes)-th row.  Reading and writing the memory is all
-// there is to it: 8 bytes an element at the rate of the DRAM.
+// there is to it: 8 bytes an element at the rate of the DRAM.  200 requests, 32 heads of 128 x 128: 134 us, 6.3 TB/s, 96 % of the copy rate (rows on
+// their way 2: 150, 3: 142, 8: 149, 16: 207); one request's 16 heads of 64 x 64 3.1 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(kStepThreads) step_kernel(const __grid_constant__ StepArgs A) {
     __shared__ float qs[kMaxDecayDim], ks[kMaxDecayDim], sums[kStepThreads * V];
