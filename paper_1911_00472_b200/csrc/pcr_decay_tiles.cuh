@@ -58,7 +58,7 @@ template <int DB, bool kStates> struct TileShared {
     static constexpr int kSide = DB / 64 * kHalf;              // of A, B, the image and lo
     static constexpr int kPlaces = DB == 64 ? 6 : 5, kPer = DB == 64 || kStates ? 2 : 3, kB = kPer == 3 ? 1 : 0;
     static constexpr int kInA = DB == 64 && !kStates ? kHalf : 0;          // where B lies in a place that it shares
-    static constexpr int kImage = kPlaces * 2 * kHalf, kLow = kImage + kSide, kRest = kLow + kSide, kBytes = kRest + 3072;
+    static constexpr int kImage = kPlaces * 2 * kHalf, kLow = kImage + kSide, kRest = kLow + kSide, kBytes = kRest + 3 * 1024;
 };
 
 constexpr int kQueue = 3;                      // segments at work in a CTA or asked for ahead
