@@ -11,8 +11,8 @@
 // The memory itself stays in the registers of one warpgroup, in 32 bits, a column of it (an element of c) to a thread; its 16-bit image
 // is the other operand of I.  B' is kept in two parts, x = hi + lo, three where the memory is given out in 32 bits and 16 bits of each
 // would show; hi takes B's place, which S is done with by then, a third the image's.  So the roundings to 16 bits are P's, the image's
-// and the output's, each half a step at most.  fp16 has few exponents: rows of P and of the image are brought to about 2^14 by a power of two,
-// which is taken off again behind the product.
+// and the output's, each half a step at most.  fp16 has few exponents: rows of P, of the image and all of a chunk's B' are brought to about 2^14 by a
+// power of two, which is taken off again behind the product.
 //
 // 16 warps: four turn S into P and write y (a thread a row), four keep the memory, four make B', one asks for tiles (TMA), one issues the
 // products, one asks for work: a CTA that is done with a segment takes the next one that no CTA has begun (the launch's own queue; what
@@ -29,7 +29,8 @@
 //
 // Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 171 us what segments add, 271 the walk (1.07 GB: 164 at the copy rate);
 // whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 238 us (floor 72; plain 5680).
-// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 398 us (floor 98; plain 2170); four prompts of 61 tokens 7.8 us (plain 31.9).
+// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 399 to 413 us (floor 98; plain 2170; B' in its own exponents 391, which loses
+// what is smaller than 2^-24); four prompts of 61 tokens 7.8 us (plain 31.9).
 #pragma once
 #include <cuda.h>
 
@@ -65,8 +66,10 @@ constexpr int kQueue = 3;                      // segments at work in a CTA or a
 struct Job { int kind, head, key, chunks, tail; float rate; Item it; };      // kind < 0: there is none left; chunks 0: nothing to walk over; tail: rows of no sequence
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
-    uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, end, got[kQueue], taken[kQueue], answer;
+    uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, t, end, got[kQueue], taken[kQueue], answer;
     Job jobs[kQueue];
+    uint32_t tops[2][8];                       // fp16: bits of the largest key times factor that a warp has, two chunks
+    float down[2];                             // what takes D back to size
     int dead;
     uint32_t tensor;
 };
@@ -184,17 +187,38 @@ template <> struct Two<__half> {
     __device__ static Pair twice(float v) { return __float2half2_rn(v); }
     __device__ static float one(Pair v) { return __low2float(v); }
 };
+// 2^14 / a power of two about as large as `most`; the exponent of what takes it off again
+__device__ __forceinline__ float to_middle(float most, uint8_t& back) {
+    const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 250);
+    back = (uint8_t)(e - 14);
+    return __uint_as_float((uint32_t)(127 + 14 + 127 - e) << 23);
+}
+__device__ __forceinline__ float from_middle(uint8_t back) { return __uint_as_float((uint32_t)back << 23); }
+
 // A factor in 16-bit parts, and products of pairs with it in parts, by 16-bit arithmetic: a product's rounding error is a 16-bit number, which a
 // fused multiply-add gives exactly.  hi = (x f0) rounded, lo = what that left + x f1; three parts: the error of lo's sum is found the
-// same way (Knuth's two-sum) and joins x f2.
+// same way (Knuth's two-sum) and joins x f2.  fp16 has bits for that where products are large: those of a chunk are brought to 2^14 at most by
+// a power of two, which is taken off D again, so that hi + lo resolves 2^-39 of the chunk's largest product whatever its size.  That power
+// goes into the factor, of which a row of small keys would ask for too large a one: such a row is lifted first (exactly) by 2^12 or 2^24.
 template <typename T> struct Factor {
     using Pair = typename Two<T>::Pair;
-    Pair f0, f1, f2;
+    Pair f0, f1, f2, lift[2];
+    bool lifts = false;                        // (of a whole warp)
+    // for a row whose largest element is `most`, in a chunk that is brought up by `up`
+    __device__ Factor(float f, float most, float up) : Factor(most > 0.f ? f * up * (most < 1.f ? 0x1p-12f : 1.f) * (most < 0x1p-12f ? 0x1p-12f : 1.f) : 0.f) {
+        lift[0] = Two<T>::twice(most < 1.f ? 4096.f : 1.f);
+        lift[1] = Two<T>::twice(most < 0x1p-12f ? 4096.f : 1.f);
+        lifts = __any_sync(~0u, most < 1.f);
+    }
     __device__ explicit Factor(float f) {
         f0 = Two<T>::twice(f);
         f -= Two<T>::one(f0);
         f1 = Two<T>::twice(f);
         f2 = Two<T>::twice(f - Two<T>::one(f1));
+    }
+    __device__ uint32_t lifted(uint32_t x) const {
+        const Pair v = __hmul2_rn(__hmul2_rn(*reinterpret_cast<Pair*>(&x), lift[0]), lift[1]);
+        return *reinterpret_cast<const uint32_t*>(&v);
     }
     __device__ void two(uint32_t& x, uint32_t& lo) const {
         const Pair v = *reinterpret_cast<Pair*>(&x), hi = __hmul2_rn(v, f0), left = __hfma2(v, f0, __hneg2(hi)), l = __hfma2(v, f1, left);
@@ -210,13 +234,34 @@ template <typename T> struct Factor {
         last = *reinterpret_cast<const uint32_t*>(&e);
     }
 };
-// 2^14 / a power of two about as large as `most`; the exponent of what takes it off again
-__device__ __forceinline__ float to_middle(float most, uint8_t& back) {
-    const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 250);
-    back = (uint8_t)(e - 14);
-    return __uint_as_float((uint32_t)(127 + 14 + 127 - e) << 23);
+
+// The largest element of pieces `from` .. `end` of a row, those that are not finite left out.  (fp16)
+template <typename T>
+__device__ __noinline__ float finite_most(const uint8_t* b, int r, int from, int end) {
+    float most = 0.f;
+    for (int i = from; i < end; ++i) {
+        const T* x = reinterpret_cast<const T*>(b + (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16);
+        for (int e = 0; e < 8; ++e) {
+            const float v = fabsf(to_float(x[e]));
+            if (isfinite(v)) most = fmaxf(most, v);
+        }
+    }
+    return most;
 }
-__device__ __forceinline__ float from_middle(uint8_t back) { return __uint_as_float((uint32_t)back << 23); }
+template <typename T>
+__device__ __forceinline__ float row_most(const uint8_t* b, int r, int from, int end) {
+    typename Two<T>::Pair most[2] = {Two<T>::twice(0.f), Two<T>::twice(0.f)};
+#pragma unroll 4
+    for (int i = from; i < end; ++i) {
+        const uint4 q = *reinterpret_cast<const uint4*>(b + (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16);
+        const uint32_t* x = &q.x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most[e & 1] = __hmax2(most[e & 1], __habs2(*reinterpret_cast<const typename Two<T>::Pair*>(x + e)));
+    }
+    most[0] = __hmax2(most[0], most[1]);
+    const float m = fmaxf(__low2float(most[0]), __high2float(most[0]));
+    return m < INFINITY ? m : finite_most<T>(b, r, from, end);
+}
 
 // Outputs of a chunk's rows in which some value is not finite, once more: masked tokens leave no trace (0 * inf is none), so what is not
 // finite is added up again over the tokens that a row sees.  Rare, and slow.
@@ -329,6 +374,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         for (uint64_t* b : {&bars->s[0], &bars->s[1], &bars->i[0], &bars->i[1], &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
         for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z}) bar_init(b, 128);
         bar_init(&bars->k, kStates ? 256 : 128);
+        bar_init(&bars->t, kStates ? 8 : 4);
         for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -353,7 +399,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     // B' by the threads of a warpgroup, a token each; where two have a chunk, half of its elements.
     auto make_parts = [&](int r, int which) {
         uint8_t *image = sm + L::kImage + r * 128, *low = sm + L::kLow + r * 128;
-        uint32_t g = 0;
+        uint32_t g = 0, tops = 0;                                          // (tops: chunks whose largest product was looked for)
         bool ok = true;
         while (ok && w.next()) {
             const int chunks = w.job->chunks;
@@ -375,11 +421,32 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     order_shared();
                     if (!kStates) bar_arrive(&bars->z);
                 }
+                const float fade = c < adding && in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f;
+                float most = 0.f, up = 1.f;
+                uint8_t down = 127;
+                if (kHalfs && c < adding) {                                // the largest product of the chunk: of the row, of the warp
+                    if (in) most = row_most<T>(b, r, from, end);
+                    const uint32_t top = __reduce_max_sync(~0u, __float_as_uint(most * fade));
+                    if ((threadIdx.x & 31) == 0) {
+                        bars->tops[tops & 1][which * 4 + (r >> 5)] = top;
+                        bar_arrive(&bars->t);
+                    }
+                }
                 // the parts' places: B's is free when S is done, lo's when the D before is, the image's when I is (or where there is none, that D)
                 ok = (g == 0 || warp_wait(&bars->d, (g - 1) & 1, dead)) && (kStates || (warp_wait(&bars->s[g & 1], g >> 1 & 1, dead) && (!three || warp_wait(&bars->i[g & 1], g >> 1 & 1, dead))));
                 if (!ok) break;
+                if (kHalfs && c < adding) {
+                    ok = warp_wait(&bars->t, tops & 1, dead);
+                    if (!ok) break;
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int i = 0; i < (kStates ? 8 : 4); ++i) top = max(top, ((volatile uint32_t*)bars->tops[tops & 1])[i]);
+                    if (top) up = to_middle(__uint_as_float(top), down);
+                    if (which == 0 && r == 0) bars->down[g & 1] = from_middle(down);       // (the one two chunks ago has been used: D has, since)
+                    ++tops;
+                }
                 if (c < adding) {
-                    const Factor<T> f(in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f);
+                    const Factor<T> f = kHalfs ? Factor<T>(fade, most, up) : Factor<T>(fade);
                     // pieces of 8 elements, a few at a time: a piece is a load, a dozen dependent steps and two or three stores
                     auto all = [&](auto how) {
 #pragma unroll decltype(how)::value ? 2 : 4
@@ -387,6 +454,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                             const int at = (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16;
                             uint4 q = *reinterpret_cast<const uint4*>(b + at), lo, last;
                             uint32_t *pq = &q.x, *pl = &lo.x, *pt = &last.x;
+                            if (kHalfs && f.lifts)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) pq[e] = f.lifted(pq[e]);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 if (decltype(how)::value) f.three(pq[e], pl[e], pt[e]);
@@ -774,6 +844,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     }
                 }
                 float up = 1.f;
+                const float down = kHalfs && adds ? ((volatile float*)bars->down)[(w.g - 1) & 1] : 1.f;
                 if (kHalfs && adds)
 #pragma unroll
                     for (int i = 0; i < DB; i += 16) {
@@ -782,7 +853,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         tensor_load16(x, D + mine + i);
                         tensor_load_wait();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + x[e];
+                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + down * x[e];
                     }
                 if (kHalfs && shows) {
                     float most = 0.f;
