@@ -29,8 +29,8 @@
 //
 // Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 171 us what segments add, 271 the walk (1.07 GB: 164 at the copy rate);
 // whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 238 us (floor 72; plain 5680).
-// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 399 to 413 us (floor 98; plain 2170; B' in its own exponents 391, which loses
-// what is smaller than 2^-24); four prompts of 61 tokens 7.8 us (plain 31.9).
+// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 410 to 433 us (floor 98; plain 2170; 391 with B' in its own exponents and
+// rows of P by what they are before they fade, which loses small keys and what stands beside large faded ones); four prompts of 61 tokens 7.8 us (plain 31.9).
 #pragma once
 #include <cuda.h>
 
@@ -347,6 +347,25 @@ __device__ __noinline__ void tile_lost(const Walk& W, const volatile Job* job) {
             else static_cast<uint16_t*>(W.y)[to + j] = 0x7fff;
         }
     }
+}
+
+// The largest of a row's products, faded.  (fp16)
+__device__ __noinline__ float faded_most(uint32_t S, uint32_t powers, int first, int end, int r, int n, bool rev) {
+    float most = 0.f;
+#pragma unroll 1
+    for (int j = first; j < end; ++j) {
+        float p[32], x[32];
+        tensor_load32(p, S + 32 * j);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[e]) : "r"(powers - 4 * (32 * j + e)));       // (what is not seen may lie beside the table)
+        tensor_load_wait();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const int q = 32 * j + e;
+            most = fmaxf(most, q < n && (rev ? q >= r : q <= r) ? fabsf(p[e] * x[e]) : 0.f);
+        }
+    }
+    return most;
 }
 
 template <typename T, int DB, bool kStates>
@@ -687,8 +706,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     return seen;
                 };
                 float p[32], on = 1.f;
-                if (kHalfs) {                                              // (before they are faded: a bound that is as good)
+                if (kHalfs) {
+                    // The row's largest product, faded; where 15 tokens fade to no less than 2^-18, a bound of it within that: the largest of 16 tokens times
+                    // the factor of the nearest, which leaves the largest at 2^-4 and the last bit at 2^-20 of it.
                     float most = 0.f;
+                    if (rate < -18.f / 15) most = faded_most(S + mine, at_shared(pw + (rev ? kTile : 0) + r), first, end, r, n, rev);
+                    else
 #pragma unroll 1
                     for (int j = first; j < end; ++j) {
                         tensor_load32(p, S + mine + 32 * j);
@@ -699,7 +722,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                             for (int e = 0; e < 32; ++e) p[e] = seen >> e & 1 ? p[e] : 0.f;
                         }
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(p[e]));
+                        for (int i = 0; i < 32; i += 16) {
+                            float largest = 0.f;
+#pragma unroll
+                            for (int e = i; e < i + 16; ++e) largest = fmaxf(largest, fabsf(p[e]));
+                            most = fmaxf(most, largest * pw[rev ? kTile - max(32 * j + i - r, 0) : max(r - 32 * j - i - 15, 0)]);
+                        }
                     }
                     uint8_t back;
                     on = to_middle(most, back);

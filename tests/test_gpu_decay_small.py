@@ -13,7 +13,7 @@ import pytest
 import torch
 
 import paper_1911_00472_b200 as P
-from test_gpu_decay import DEV, U, walk
+from test_gpu_decay import DEV, U, walk, weights
 
 pytestmark = pytest.mark.gpu
 HALVES = [torch.float16, torch.bfloat16]
@@ -91,3 +91,30 @@ def test_gradients_of_a_few_last_bits(n, size, units, dtype):
             y, E, _, _ = walk(s, t, u, rate, zero, rev, not rev)
             if y.abs().max() < torch.finfo(dtype).max / 2:
                 output_near(got[:, h], y, E, t, u, s, dtype, size, (what, h))
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("large,small", [(2.0 ** 13, 2.0 ** -17), (2.0 ** 11, 2.0 ** -20), (1.0, 1.0)])
+@pytest.mark.parametrize("n,size", [(300, 64), (200, 128), (128, 40)], ids=str)
+def test_a_fast_head_behind_large_keys(n, size, large, small, dtype):
+    """Products of a row that are far above all others before they fade, and far below behind: what is left is right by itself.  A row's largest
+    faded product lies at 2^-4 or more in fp16, so that half of the last bit, 2^-25, is 2^-21 of it, for each token's |c|."""
+    q, k, v = draw(n, 3, size, 1.0, dtype, n), draw(n, 3, size, small, dtype, n + 1), draw(n, 3, size, 2.0 ** 10, dtype, n + 2)
+    for at in (0, 1, 64, n - 1):
+        k[at] = draw(1, 3, size, large, dtype, at)[0]
+    log_decay = torch.tensor([-3.0, -1.0, -0.8], device=DEV)
+    out, _ = P.decay_attention(q, k, v, log_decay, starts=torch.tensor([0, n], dtype=torch.int32, device=DEV))
+    dq, dk, dv, _ = P.decay_attention_backward(v, q, k, v, log_decay)
+    zero = torch.zeros(size, size, device=DEV, dtype=torch.float64)
+    for h in range(3):
+        a, b, c = (x[:, h].double() for x in (q, k, v))
+        for what, got, (s, t, u), rev in (("out", out, (a, b, c), False), ("dv", dv, (b, a, c), True)):
+            y, E, _, _ = walk(s, t, u, float(log_decay[h]), zero, rev, not rev)
+            fine = y.abs().amax(-1) < torch.finfo(dtype).max / 2
+            assert fine.any()
+            eps = torch.finfo(dtype).eps
+            w = weights(float(log_decay[h]), n)[0]
+            most = ((s @ t.T).abs() * (w.T if rev else w)).amax(-1, keepdim=True)
+            tol = ((size + 170) * U + eps) * E + 2.0 ** -21 * most * u.abs().sum(0) + eps / 2 * y.abs() + torch.finfo(dtype).smallest_normal * eps / 2
+            worst = ((got[:, h].double() - y).abs() / tol)[fine].max()
+            assert worst <= 1, (what, h, float(worst))
