@@ -27,10 +27,11 @@
 // memory's sum, its image and I, each waiting for the one before.  Rows of y are written by the lane that has them, 53 cycles a store; warps
 // of their own for y (257 us for the gradients below, 407 for the images) and y through shared memory (245, 413) were not faster.
 //
-// Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 171 us what segments add, 271 the walk (1.07 GB: 164 at the copy rate);
-// whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 238 us (floor 72; plain 5680).
-// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 410 to 433 us (floor 98; plain 2170; 391 with B' in its own exponents and
-// rows of P by what they are before they fade, which loses small keys and what stands beside large faded ones); four prompts of 61 tokens 7.8 us (plain 31.9).
+// Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 176 us what segments add, 276 the walk (1.07 GB: 164 at the copy rate);
+// whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 241 us (floor 72; plain 5680).
+// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 431 to 438 us (floor 98; plain 2170; 391 with B' in its own exponents and
+// rows of P by what they are before they fade, which loses small keys and what stands beside large faded ones).  Looking for what is not finite in
+// what a chunk adds costs 2 to 4 % of these (169, 268, 236, 429 without it).; four prompts of 61 tokens 7.8 us (plain 31.9).
 #pragma once
 #include <cuda.h>
 
@@ -70,6 +71,7 @@ struct alignas(16) TileBars {
     Job jobs[kQueue];
     uint32_t tops[2][8];                       // fp16: bits of the largest key times factor that a warp has, two chunks
     float down[2];                             // what takes D back to size
+    uint32_t odd[2];                           // 1 + the last of every other chunk in which a key is not finite
     int dead;
     uint32_t tensor;
 };
@@ -235,7 +237,7 @@ template <typename T> struct Factor {
     }
 };
 
-// The largest element of pieces `from` .. `end` of a row, those that are not finite left out.  (fp16)
+// The largest element of pieces `from` .. `end` of a row, those that are not finite left out; row_most: infinity where there are some.  (fp16)
 template <typename T>
 __device__ __noinline__ float finite_most(const uint8_t* b, int r, int from, int end) {
     float most = 0.f;
@@ -256,11 +258,11 @@ __device__ __forceinline__ float row_most(const uint8_t* b, int r, int from, int
         const uint4 q = *reinterpret_cast<const uint4*>(b + (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16);
         const uint32_t* x = &q.x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most[e & 1] = __hmax2(most[e & 1], __habs2(*reinterpret_cast<const typename Two<T>::Pair*>(x + e)));
+        for (int e = 0; e < 4; ++e) most[e & 1] = __hmax2_nan(most[e & 1], __habs2(*reinterpret_cast<const typename Two<T>::Pair*>(x + e)));
     }
-    most[0] = __hmax2(most[0], most[1]);
-    const float m = fmaxf(__low2float(most[0]), __high2float(most[0]));
-    return m < INFINITY ? m : finite_most<T>(b, r, from, end);
+    most[0] = __hmax2_nan(most[0], most[1]);
+    const float m = __low2float(most[0]), other = __high2float(most[0]);
+    return m < INFINITY && other < INFINITY ? fmaxf(m, other) : INFINITY;
 }
 
 // Outputs of a chunk's rows in which some value is not finite, once more: masked tokens leave no trace (0 * inf is none), so what is not
@@ -296,6 +298,41 @@ __device__ __noinline__ void careful(const Walk& W, int batch, int head, int64_t
                 else static_cast<T*>(W.y)[to + j0 + j] = from_float<T>(m[j]);
             }
         __syncwarp();
+    }
+}
+
+// What a chunk adds to a column of the memory (r of c), once more where it is not finite: an infinity in parts is none (inf - inf, 0 * inf), so the
+// sum is that of the factors themselves.  It goes to where D has it.  Rare, and slow, but for what is no number at once.
+template <typename T>
+__device__ __noinline__ void careful_sum(const Walk& W, int batch, int head, int64_t t0, int n, int r, float rate, int near, float up, uint32_t D) {
+    const T* b = static_cast<const T*>(W.b.at) + (int64_t)batch * W.b.st[0] + t0 * W.b.st[1] + (int64_t)(head / W.b.group) * W.b.st[2];
+    const T* c = static_cast<const T*>(W.c.at) + (int64_t)batch * W.c.st[0] + t0 * W.c.st[1] + (int64_t)(head / W.c.group) * W.c.st[2];
+    const bool on = r < W.cd;
+    for (int i = 0; i < W.bd; i += 16) {
+        float x[16], zero = 0.f;
+        tensor_load16(x, D + i);
+        tensor_load_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) zero = fmaf(x[e], 0.f, zero);
+        if (!__any_sync(~0u, !(zero == 0.f))) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = 0.f;
+        for (int t = 0; t < n; ++t) {
+            const float v = on ? to_float(c[t * W.c.st[1] + r]) : 0.f, f = power(rate, (W.rev ? t + 1 : n - t) - near);
+            bool open = false;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (on && i + e < W.bd) {
+                    x[e] += to_float(b[t * W.b.st[1] + i + e]) * f * v;
+                    open |= !isnan(x[e]);
+                }
+            if (!__any_sync(~0u, open)) break;
+        }
+        uint32_t y[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[e] * up);
+        tensor_store16(D + i, y);
+        tensor_store_wait();
     }
 }
 
@@ -396,6 +433,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         bar_init(&bars->t, kStates ? 8 : 4);
         for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
         *dead = 0;
+        bars->odd[0] = bars->odd[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 13) {
@@ -442,9 +480,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
                 const float fade = c < adding && in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f;
                 float most = 0.f, up = 1.f;
+                bool odd = false;                                          // (fp16) an element is not finite
                 uint8_t down = 127;
                 if (kHalfs && c < adding) {                                // the largest product of the chunk: of the row, of the warp
-                    if (in) most = row_most<T>(b, r, from, end);
+                    if (in) {
+                        most = row_most<T>(b, r, from, end);
+                        if (!(most < INFINITY)) { odd = true; most = finite_most<T>(b, r, from, end); }
+                    }
                     const uint32_t top = __reduce_max_sync(~0u, __float_as_uint(most * fade));
                     if ((threadIdx.x & 31) == 0) {
                         bars->tops[tops & 1][which * 4 + (r >> 5)] = top;
@@ -466,6 +508,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 }
                 if (c < adding) {
                     const Factor<T> f = kHalfs ? Factor<T>(fade, most, up) : Factor<T>(fade);
+                    typename Two<T>::Pair zero = Two<T>::twice(0.f);       // 0 times all of lo, which is no number where the element is not finite
                     // pieces of 8 elements, a few at a time: a piece is a load, a dozen dependent steps and two or three stores
                     auto all = [&](auto how) {
 #pragma unroll decltype(how)::value ? 2 : 4
@@ -480,6 +523,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                             for (int e = 0; e < 4; ++e) {
                                 if (decltype(how)::value) f.three(pq[e], pl[e], pt[e]);
                                 else f.two(pq[e], pl[e]);
+                                if (!kHalfs) zero = __hfma2(*reinterpret_cast<const typename Two<T>::Pair*>(pl + e), Two<T>::twice(0.f), zero);
                             }
                             *reinterpret_cast<uint4*>(b + at) = q;
                             *reinterpret_cast<uint4*>(low + at) = lo;
@@ -491,6 +535,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int i = from; i < end; ++i) *reinterpret_cast<uint4*>(b + (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16) = make_uint4(0, 0, 0, 0);
                     if (three) all(std::true_type());
                     else all(std::false_type());
+                    if (kHalfs ? odd : in && !(__low2float(zero) == 0.f && __high2float(zero) == 0.f)) bars->odd[g & 1] = g + 1;
                 }
                 order_shared();
                 bar_arrive(&bars->k);
@@ -860,7 +905,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             for (int c = 0; c <= chunks && chunks > 0; ++c) {
                 // the memory behind chunk c - 1, and its image for chunk c
                 const bool adds = c > 0 && c <= adding, shows = !kStates && c < chunks;
-                float keep = 1.f;
+                float keep = 1.f, ahead[16];
                 if (c > 0) {
                     ok = warp_wait(&bars->d, w.g & 1, dead);
                     if (!ok) break;
@@ -868,7 +913,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     if (adds) {
                         order_after();
                         const int n = w.tokens(c - 1);
-                        keep = power(rate, !kStates && last && c == chunks && !rev ? n - 1 : n);      // forward, the memory that is given out is not aged
+                        const int near = !kStates && last && c == chunks && !rev ? 1 : 0;
+                        keep = power(rate, n - near);                      // forward, the memory that is given out is not aged
+                        // a key that is not finite makes all columns so, a value its own column from end to end
+                        tensor_load16(ahead, D + mine);
+                        tensor_load_wait();
+                        if (((volatile uint32_t*)bars->odd)[(w.g - 1) & 1] == w.g || __any_sync(~0u, !isfinite(ahead[0]))) {
+                            careful_sum<T>(W, j.it.batch, head, w.begin(c - 1, rev), n, r, rate, near, kHalfs ? 1.f / ((volatile float*)bars->down)[(w.g - 1) & 1] : 1.f, D + mine);
+                            tensor_load16(ahead, D + mine);
+                            tensor_load_wait();
+                        }
                     }
                 }
                 float up = 1.f;
@@ -878,10 +932,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     for (int i = 0; i < DB; i += 16) {
                         if (i >= bd) continue;                             // (nothing was put there)
                         float x[16];
-                        tensor_load16(x, D + mine + i);
-                        tensor_load_wait();
+                        if (i) {
+                            tensor_load16(x, D + mine + i);
+                            tensor_load_wait();
+                        }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + down * x[e];
+                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + down * (i ? x[e] : ahead[e]);
                     }
                 if (kHalfs && shows) {
                     float most = 0.f;
@@ -889,14 +945,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     for (int i = 0; i < DB; ++i) most = fmaxf(most, fabsf(R[i]));
                     up = to_middle(most, cs[(w.g & 1) * 128 + r]);
                 }
-                float ahead[16];
-                if (!kHalfs && adds) tensor_load16(ahead, D + mine);
 #pragma unroll
                 for (int i = 0; i < DB; i += 16) {
                     if (i >= bd) continue;
                     if (!kHalfs && adds) {
                         float x[16];
-                        tensor_load_wait();
+                        if (i) tensor_load_wait();
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[e] = ahead[e];
                         if (i + 16 < DB && i + 16 < bd) tensor_load16(ahead, D + mine + i + 16);
