@@ -355,6 +355,7 @@ typedef struct {
  *             apart from all operands and outputs.
  * Outputs share no memory with operands, tables or one another: else PCR_E_ARG.  The same call gives the same bits.
  * A token that is not finite reaches the outputs of the tokens behind it (backward: and the gradients before it) in its sequence, no others.
+ * Waits within a kernel end after two seconds; segments in which one did (none is known to) become NaN, memories and all behind them too.
  * Errors: PCR_E_ARG, PCR_E_CUDA. */
 size_t pcr_decay_scratch_bytes(const pcr_decay_args* args, int backward);
 int pcr_decay_attention(const pcr_decay_args* args, void* scratch, void* stream);
@@ -521,6 +522,12 @@ int pcr_pixels_noalloc(const int16_t* dev_coeffs, uint32_t width, uint32_t heigh
  * normally and the context stays usable), 0 if it claims to have seen the flag.
  * Errors: PCR_E_ARG, PCR_E_NOMEM, PCR_E_CUDA. */
 int pcr_selftest_bounded_wait(int* gave_up);
+
+/* Test hook for the waits of pcr_decay_attention (back: pcr_decay_attention_backward) on the tensor cores: the same call, in which the
+ * copies of operands of every CTA stop behind `after` of its chunks of 128 tokens and waits end after a millisecond.  What could not be
+ * worked out is NaN, outputs and memories alike; the kernels return normally and the context stays usable.
+ * Errors: PCR_E_ARG (also where the call would not take that path), PCR_E_CUDA. */
+int pcr_selftest_decay_waits(const pcr_decay_args* args, int back, void* scratch, uint32_t after, void* stream);
 
 /* Counts kernel launches issued by this library since it was loaded (all records). */
 uint64_t pcr_launch_count(void);

@@ -22,7 +22,7 @@ EXPORTS = ("pcr_open", "pcr_num_images", "pcr_num_groups", "pcr_get_image", "pcr
            "pcr_patch_tokens", "pcr_token_positions", "pcr_token_positions_scratch_bytes", "pcr_rotate", "pcr_norm_rotate",
            "pcr_norm_rotate_backward", "pcr_norm_rotate_scratch_bytes", "pcr_decay_scratch_bytes", "pcr_decay_attention",
            "pcr_decay_attention_backward", "pcr_decay_step", "pcr_relative_bias", "pcr_relative_bias_backward",
-           "pcr_relative_bias_scratch_bytes")
+           "pcr_relative_bias_scratch_bytes", "pcr_selftest_decay_waits")
 
 
 class ImageInfo(C.Structure):
@@ -96,6 +96,7 @@ def lib():
         L.pcr_decay_scratch_bytes.argtypes = [C.c_char_p, C.c_int]         # (a pcr_decay_args, packed by the caller)
         L.pcr_decay_attention.argtypes = [C.c_char_p, vp, vp]
         L.pcr_decay_attention_backward.argtypes = [C.c_char_p, vp, vp]
+        L.pcr_selftest_decay_waits.argtypes = [C.c_char_p, C.c_int, vp, C.c_uint32, vp]
         L.pcr_decay_step.argtypes = [C.c_char_p, vp]                       # (a pcr_decay_step_args)
         L.pcr_relative_bias.argtypes = [C.c_char_p, vp]                    # (a pcr_bias_args)
         L.pcr_relative_bias_scratch_bytes.restype = C.c_size_t

@@ -53,6 +53,8 @@ bool heads_fit(int q_heads, int k_heads, int k_dim, int v_dim, int dtype) {
            v_dim <= kMaxDecayDim && (dtype == PCR_F16 || dtype == PCR_F32 || dtype == PCR_BF16);
 }
 
+constexpr uint32_t kNever = UINT32_MAX, kTestPatience = 1000000;           // (nanoseconds, where waits are to run out)
+
 struct Form {
     bool tiles;                                 // on the tensor cores
     int chunk, parts;                           // tokens of a chunk; 16-bit parts of what goes into a memory
@@ -205,32 +207,23 @@ int run(WalkArgs& states, const int (*states_of)[3], WalkArgs& walks, const int 
     return f.tiles ? launch_tiles(walks, walks_of, a, f.keys, f.parts, sm_count(), st) : launch_any(walks, f, a.dtype, st);
 }
 
-WalkArgs common(const pcr_decay_args& a, const Form& f) {
+// `stop`: chunks after which the copies of tiles of a CTA stop, so that its waits run out; kNever
+WalkArgs common(const pcr_decay_args& a, const Form& f, uint32_t stop) {
     WalkArgs A = {};
     A.log_decay = a.log_decay; A.starts = a.starts; A.sequences = (uint32_t)a.sequences; A.tokens = (uint32_t)a.tokens;
-    A.seg = f.seg; A.heads = a.q_heads;
+    A.seg = f.seg; A.heads = a.q_heads; A.limit = stop == kNever ? kPatience : kTestPatience; A.stop = stop;
     return A;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t pcr_decay_scratch_bytes(const pcr_decay_args* args, int backward) {
-    if (!args || check(*args, backward != 0) != PCR_OK || nothing(*args)) return 0;
-    return scratch_of(form_of(*args, backward != 0), backward != 0);
-}
-
-int pcr_decay_attention(const pcr_decay_args* args, void* scratch, void* stream) {
-    if (!args) return PCR_E_ARG;
-    const pcr_decay_args& a = *args;
+int forward(const pcr_decay_args& a, void* scratch, void* stream, uint32_t stop) {
     if (int rc = check(a, false)) return rc;
     if (nothing(a)) return PCR_OK;
     const Form f = form_of(a, false);
     const size_t need = scratch_of(f, false);
     if ((need && !scratch) || !aligned(scratch, 16) || shares(a, false, scratch, need)) return PCR_E_ARG;
     const int group = a.q_heads / a.k_heads;
-    WalkArgs A = common(a, f);
+    if (stop != kNever && !f.tiles) return PCR_E_ARG;
+    WalkArgs A = common(a, f, stop);
     Walk& w = A.w[0];
     A.kinds = 1;
     w.a = walk_rows(a.q, 1); w.b = walk_rows(a.k, group); w.c = walk_rows(a.v, group);
@@ -243,9 +236,7 @@ int pcr_decay_attention(const pcr_decay_args* args, void* scratch, void* stream)
     return run(S, of, A, of, f, a, static_cast<cudaStream_t>(stream));
 }
 
-int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void* stream) {
-    if (!args) return PCR_E_ARG;
-    const pcr_decay_args& a = *args;
+int backward(const pcr_decay_args& a, void* scratch, void* stream, uint32_t stop) {
     if (int rc = check(a, true)) return rc;
     if (nothing(a)) return PCR_OK;
     const Form f = form_of(a, true);
@@ -258,7 +249,8 @@ int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void
     float* const dv32 = dk32 + (size_t)a.batch * a.tokens * a.q_heads * a.k_dim;
     const WalkRows q = walk_rows(a.q, 1), k = walk_rows(a.k, group), v = walk_rows(a.v, group), g = walk_rows(a.out, 1);
 
-    WalkArgs S = common(a, f), A = S;
+    if (stop != kNever && !f.tiles) return PCR_E_ARG;
+    WalkArgs S = common(a, f, stop), A = S;
     S.kinds = 2;                                // the memories from either end, as (k_dim, v_dim)
     S.w[0].b = k; S.w[0].c = v; S.w[0].first = a.state; S.w[0].slots = slots;
     S.w[1].b = q; S.w[1].c = g; S.w[1].first = a.dstate_after; S.w[1].slots = slots_back; S.w[1].rev = 1;
@@ -304,6 +296,24 @@ int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void
         ++g_launches;
     }
     return finish();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t pcr_decay_scratch_bytes(const pcr_decay_args* args, int backward) {
+    if (!args || check(*args, backward != 0) != PCR_OK || nothing(*args)) return 0;
+    return scratch_of(form_of(*args, backward != 0), backward != 0);
+}
+
+int pcr_decay_attention(const pcr_decay_args* args, void* scratch, void* stream) { return args ? forward(*args, scratch, stream, kNever) : PCR_E_ARG; }
+
+int pcr_decay_attention_backward(const pcr_decay_args* args, void* scratch, void* stream) { return args ? backward(*args, scratch, stream, kNever) : PCR_E_ARG; }
+
+int pcr_selftest_decay_waits(const pcr_decay_args* args, int back, void* scratch, uint32_t after, void* stream) {
+    if (!args || after == kNever) return PCR_E_ARG;
+    return back ? backward(*args, scratch, stream, after) : forward(*args, scratch, stream, after);
 }
 
 int pcr_decay_step(const pcr_decay_step_args* args, void* stream) {

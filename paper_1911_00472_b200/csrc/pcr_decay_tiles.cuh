@@ -65,14 +65,17 @@ template <int DB, bool kStates> struct TileShared {
 
 constexpr int kQueue = 3;                      // segments at work in a CTA or asked for ahead
 struct Job { int kind, head, key, chunks, tail; float rate; Item it; };      // kind < 0: there is none left; chunks 0: nothing to walk over; tail: rows of no sequence
+struct Patience { int dead; uint32_t limit; };     // whether some wait of the CTA ran out; nanoseconds
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
     uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, t, end, got[kQueue], taken[kQueue], answer;
-    Job jobs[kQueue];
+    Job jobs[kQueue], held;                    // held: one that was taken and could not be put among them
     uint32_t tops[2][8];                       // fp16: bits of the largest key times factor that a warp has, two chunks
     float down[2];                             // what takes D back to size
     uint32_t odd[2];                           // 1 + the last of every other chunk in which a key is not finite
-    int dead;
+    Patience patience;
+    int undone, posted;                        // after a wait that ran out: the first segment that may not be whole; segments put among `jobs`
+    uint32_t rest;                             // and (dealt out) the first that nobody has looked at
     uint32_t tensor;
 };
 
@@ -82,8 +85,8 @@ __device__ __forceinline__ void bar_arrive(uint64_t* b) { asm volatile("mbarrier
 __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(at_shared(b)), "r"(bytes) : "memory");
 }
-// Waits for the phase of that parity to end, for two seconds at most: false if it gave up, or if another thread did before.
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
+// Waits for the phase of that parity to end, for some time at most: false if it gave up, or if another thread did before.
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile Patience* dead) {
     uint64_t begin = 0;
     for (uint32_t tries = 1;; ++tries) {
         uint32_t done;
@@ -93,8 +96,8 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
         uint64_t now;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
         if (!begin) begin = now;
-        if (now - begin > 2000000000ull) *dead = 1;
-        if (*dead) return false;
+        if (now - begin > dead->limit) dead->dead = 1;
+        if (dead->dead) return false;
     }
 }
 // Whether that phase has ended.
@@ -104,7 +107,7 @@ __device__ __forceinline__ bool bar_there(uint64_t* b, uint32_t parity) {
     return done;
 }
 // The same for a whole warp: all of its lanes go on, together, or none.
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead) { return __all_sync(~0u, bar_wait(b, parity, dead)); }
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile Patience* dead) { return __all_sync(~0u, bar_wait(b, parity, dead)); }
 __device__ __forceinline__ void tile_load(void* to, const CUtensorMap* map, uint64_t* bar, int x, int head, int token, int batch) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(at_shared(to)),
                  "l"(map), "r"(at_shared(bar)), "r"(x), "r"(head), "r"(token), "r"(batch) : "memory");
@@ -357,7 +360,7 @@ struct Work {
             if ((threadIdx.x & 31) == 0) bar_arrive(&bars->taken[at % kQueue]);
         }
         ++at;
-        if (!warp_wait(&bars->got[at % kQueue], (at / kQueue) & 1, &bars->dead)) return false;
+        if (!warp_wait(&bars->got[at % kQueue], (at / kQueue) & 1, &bars->patience)) return false;
         job = bars->jobs + at % kQueue;
         return job->kind >= 0;
     }
@@ -375,14 +378,49 @@ struct Work {
 __device__ __noinline__ void tile_tail(const WalkArgs& A, const Walk& W, const volatile Job* job, int segments) {
     zero_tail(A, W, W.y32 ? 4 : 2, job->key, segments, job->head, threadIdx.x & 127, 128);
 }
-// A wait that ran out does not go unnoticed: the segment's rows are no numbers.
-__device__ __noinline__ void tile_lost(const Walk& W, const volatile Job* job) {
-    for (int t = threadIdx.x & 127; t < job->it.n; t += 128) {
-        const int64_t row = job->it.begin + (W.rev ? job->it.len - job->it.from - job->it.n : job->it.from) + t, to = (int64_t)job->it.batch * W.ys[0] + row * W.ys[1] + (int64_t)job->head * W.ys[2];
-        for (int j = 0; j < W.cd; ++j) {
-            if (W.y32) static_cast<float*>(W.y)[to + j] = __int_as_float(0x7fc00000);
-            else static_cast<uint16_t*>(W.y)[to + j] = 0x7fff;
-        }
+// A wait that ran out does not go unnoticed: what the CTA has taken on and not brought to an end becomes no numbers, rows and memories alike.  A
+// segment that nobody has taken goes to another CTA.
+constexpr int kLosers = 256;                   // threads (those whose registers are as many as at the launch)
+template <bool kStates>
+__device__ __forceinline__ void lose(const WalkArgs& A, const volatile Job* job, int segments, int thread) {
+    if (job->kind < 0) return;
+    const Walk& W = A.w[job->kind];
+    const size_t of = (size_t)W.bd * W.cd;
+    if (job->tail) zero_tail(A, W, W.y32 ? 4 : 2, job->key, segments, job->head, thread, kLosers);
+    if (job->it.len < 0) return;
+    float* memory = nullptr;
+    if (kStates) { if (!job->it.last) memory = W.slots + ((size_t)job->it.slot * A.heads + job->head) * of; }
+    else if (job->it.last && W.last) memory = W.last + ((size_t)job->it.seq * A.heads + job->head) * of;
+    if (memory)
+        for (size_t i = thread; i < of; i += kLosers) memory[i] = __int_as_float(0x7fc00000);
+    if (kStates) return;
+    const int64_t first = job->it.begin + (W.rev ? job->it.len - job->it.from - job->it.n : job->it.from);
+    for (int64_t i = thread; i < (int64_t)job->it.n * W.cd; i += kLosers) {
+        const int64_t to = (int64_t)job->it.batch * W.ys[0] + (first + i / W.cd) * W.ys[1] + (int64_t)job->head * W.ys[2] + i % W.cd;
+        if (W.y32) static_cast<float*>(W.y)[to] = __int_as_float(0x7fc00000);
+        else static_cast<uint16_t*>(W.y)[to] = 0x7fff;
+    }
+}
+// The segment of number x, by a whole warp.
+template <bool kStates> __device__ __forceinline__ Job job_of(const WalkArgs& A, uint32_t x, bool tail) {
+    Job j = {-1, 0, 0, 0, tail, 0.f, {}};
+    const int rest = (int)x / A.kinds;
+    j.kind = (int)x - rest * A.kinds;
+    j.key = rest / A.heads;
+    j.head = rest - j.key * A.heads;
+    j.rate = rate_of(A.log_decay, j.head);
+    const bool is = item_of(A, A.w[j.kind].rev, j.key, j.it);
+    if (!is) j.it.len = -1;
+    j.chunks = is && !(kStates && j.it.last) ? (j.it.n + kTile - 1) / kTile : 0;
+    return j;
+}
+template <bool kStates> __device__ __noinline__ void lose_all(const TileArgs& G, const TileBars* bars, int thread) {
+    const int segments = kStates ? 0 : gridDim.x / (G.walks.heads * G.walks.kinds);
+    for (int i = bars->undone; i < bars->posted; ++i) lose<kStates>(G.walks, bars->jobs + i % kQueue, segments, thread);
+    lose<kStates>(G.walks, &bars->held, segments, thread);
+    for (uint32_t x = bars->rest; x < G.items; x += gridDim.x) {
+        const Job j = job_of<kStates>(G.walks, x, false);
+        lose<kStates>(G.walks, &j, segments, thread);
     }
 }
 
@@ -416,7 +454,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     uint8_t* cs = reinterpret_cast<uint8_t*>(powers + 2 * 132);            // fp16: what the image's columns were brought up by, two chunks
     TileBars* bars = reinterpret_cast<TileBars*>(cs + 256);
     static_assert(2 * 132 * 4 % 16 == 0 && 2 * 132 * 4 + 256 + sizeof(TileBars) <= L::kBytes - L::kRest, "all of it fits, where it has to lie");
-    volatile int* dead = &bars->dead;
+    volatile Patience* dead = &bars->patience;
     // Packed sequences, whose lengths the host does not know: often none of them is longer than a segment (looked up by as many threads as there are, up to
     // some number that takes about a microsecond).
     if (kStates && A.starts && A.sequences <= 16 * kTileThreads) {
@@ -432,7 +470,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         bar_init(&bars->k, kStates ? 256 : 128);
         bar_init(&bars->t, kStates ? 8 : 4);
         for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
-        *dead = 0;
+        bars->patience = {0, A.limit};
+        bars->held.kind = -1;
+        bars->undone = INT32_MAX;
+        bars->posted = 0;
+        bars->rest = ~0u;
         bars->odd[0] = bars->odd[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -547,6 +589,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         fewer_registers<56>();
         if (warp == 12) {                                                  // copies of tiles
             const CUtensorMap* all = &G.maps.q;
+            uint32_t issued = 0;                                           // tiles
             bool ok = true;
             while (ok && w.next()) {
                 const Walk& W = A.w[w.job->kind];
@@ -554,6 +597,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 const CUtensorMap *ma = all + of[0], *mb = all + of[1], *mc = all + of[2];
                 const int ha = head / W.a.group, hb = head / W.b.group, hc = head / W.c.group, halves = W.cd > 64 ? 2 : 1;
                 for (int c = 0; c < chunks; ++c, ++w.g) {
+                    ok = w.g != A.stop;
+                    if (!ok) break;
                     const int t0 = w.begin(c, W.rev);
 #pragma unroll 1
                     for (int which = 0; which < L::kPer; ++which) {
@@ -569,14 +614,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                             for (int i = 0; i < n; ++i) tile_load(to + i * kHalf, m, &bars->full[s], 64 * i, h, t0, batch);
                             if (DB == 64 && is_a && is_b) tile_load(to + L::kInA, mb, &bars->full[s], 0, hb, t0, batch);
                         }
+                        issued = at + 1;
                         __syncwarp();
                     }
                     if (!ok) break;
                 }
             }
-            volatile int again = 0;                                        // copies still under way write here: none may be left
-            const uint32_t all_of = w.g * L::kPer;
-            for (uint32_t i = all_of > L::kPlaces ? all_of - L::kPlaces : 0; i < all_of; ++i) bar_wait(&bars->full[i % L::kPlaces], (i / L::kPlaces) & 1, &again);
+            volatile Patience again = {0, kPatience};                     // copies still under way write here: none may be left
+            for (uint32_t i = issued > L::kPlaces ? issued - L::kPlaces : 0; i < issued; ++i) bar_wait(&bars->full[i % L::kPlaces], (i / L::kPlaces) & 1, &again);
         } else if (warp == 13) {                                           // products
             const uint32_t how = Two<T>::kHow | 8u << 24;
             const uint64_t rows0 = desc_rows(at_shared(sm)), cols0 = desc_cols(at_shared(sm)), image_rows = rows0 + L::kImage / 16;
@@ -668,7 +713,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 ++w.g;
                 if (more == 0) more = advance(true);
             }
-            volatile int again = 0;
+            volatile Patience again = {0, kPatience};
             if (elected()) mma_commit(&bars->end);
             __syncwarp();
             bar_wait(&bars->end, 0, &again);
@@ -676,22 +721,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const bool tail = !kStates && A.starts && (A.w[0].zero_tail || A.w[1].zero_tail || A.w[2].zero_tail) &&
                               (__ldg(A.starts) > 0 || __ldg(A.starts + A.sequences) < (int64_t)A.tokens);          // rows of no sequence that become 0
             int x = blockIdx.x, i = 0;
+            bool late = false;
             for (uint32_t asked = 0;; ++asked) {
                 Job j = {-1, 0, 0, 0, tail, 0.f, {}};
-                if (x >= 0) {
-                    const int rest = x / A.kinds;
-                    j.kind = x - rest * A.kinds;
-                    j.key = rest / A.heads;
-                    j.head = rest - j.key * A.heads;
-                    j.rate = rate_of(A.log_decay, j.head);
-                    const bool is = item_of(A, A.w[j.kind].rev, j.key, j.it);
-                    if (!is) j.it.len = -1;
-                    j.chunks = is && !(kStates && j.it.last) ? (j.it.n + kTile - 1) / kTile : 0;
-                }
+                if (x >= 0) j = job_of<kStates>(A, x, tail);
                 // (a key of no segment, or one that there is nothing to do for, is passed over)
                 if (x < 0 || tail || j.chunks > 0 || (!kStates && j.it.len == 0 && A.w[j.kind].last)) {
                     const int slot = i % kQueue;
-                    if (i >= kQueue && !warp_wait(&bars->taken[slot], (i / kQueue - 1) & 1, dead)) break;
+                    if (late || (i >= kQueue && !warp_wait(&bars->taken[slot], (i / kQueue - 1) & 1, dead))) {
+                        if (lane == 0) {
+                            bars->held = j;
+                            if (kStates && x >= 0) bars->rest = (uint32_t)x + gridDim.x;
+                        }
+                        break;
+                    }
                     if (lane == 0) {
                         bars->jobs[slot] = j;
                         bar_arrive(&bars->got[slot]);
@@ -710,7 +753,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(at_shared(bars->won)), "r"(at_shared(&bars->answer)) : "memory");
                 }
                 __syncwarp();
-                if (!warp_wait(&bars->answer, asked & 1, dead)) break;
+                // (an answer that is late is waited for all the same: it may be a segment, and is written to this CTA's memory)
+                late = !warp_wait(&bars->answer, asked & 1, dead);
+                if (late) {
+                    volatile Patience again = {0, kPatience};
+                    if (!warp_wait(&bars->answer, asked & 1, &again)) break;
+                }
                 uint32_t is, to;
                 asm volatile("{\n.reg .b128 h;\n.reg .pred p;\n.reg .b64 lo, hi;\nld.shared.v2.b64 {lo, hi}, [%2];\nmov.b128 h, {lo, hi};\n"
                              "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
@@ -718,6 +766,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 x = is ? (int)to : -1;
                 __syncwarp();
             }
+            if (lane == 0) bars->posted = i;
         }
     } else if (warp < 4) {
         const int r = tid;
@@ -865,7 +914,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 order_before();
                 bar_arrive(&bars->e);
             }
-            if (!ok) tile_lost(W, w.job);
         }
     } else if (warp < 8) {
         more_registers<184>();
@@ -989,9 +1037,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
     } else make_parts(tid - 256, kStates ? 1 : 0);
     __syncwarp();
+    if (lane == 0 && warp < 8 && (!kStates || warp >= 4)) atomicMin(&bars->undone, w.at);        // (y or memory are whole up to here)
     order_before();
     __syncthreads();
     order_after();
+    if (dead->dead && (warp < 4 || (warp >= 8 && warp < 12))) lose_all<kStates>(G, bars, warp < 4 ? tid : tid - 128);
     if (warp == 13) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 

@@ -25,6 +25,7 @@
 namespace pcr {
 
 constexpr int kMaxDecayDim = 256;              // of a head, keys and values
+constexpr uint32_t kPatience = 2000000000u;    // nanoseconds that a wait goes on at most
 
 struct WalkRows { const void* at; int64_t st[3]; int group; };       // batch, token, head; `group` heads of the walk share one of these
 
@@ -46,6 +47,7 @@ struct WalkArgs {
     const int32_t* starts;                     // sequences + 1, or null: every batch is one of `tokens`
     uint32_t sequences, tokens, seg;           // tokens of a segment: a multiple of the chunk
     int heads, kinds, states;                  // states: only what segments add
+    uint32_t limit, stop;                      // nanoseconds of a wait; chunks after which a CTA's copies of tiles stop (for tests of waits that run out)
 };
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
