@@ -27,11 +27,12 @@
 // memory's sum, its image and I, each waiting for the one before.  Rows of y are written by the lane that has them, 53 cycles a store; warps
 // of their own for y (257 us for the gradients below, 407 for the images) and y through shared memory (245, 413) were not faster.
 //
-// Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 176 us what segments add, 276 the walk (1.07 GB: 164 at the copy rate);
+// Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 176 us what segments add, 281 the walk (1.07 GB: 164 at the copy rate);
 // whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 241 us (floor 72; plain 5680).
-// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 431 to 438 us (floor 98; plain 2170; 391 with B' in its own exponents and
-// rows of P by what they are before they fade, which loses small keys and what stands beside large faded ones).  Looking for what is not finite in
-// what a chunk adds costs 2 to 4 % of these (169, 268, 236, 429 without it).; four prompts of 61 tokens 7.8 us (plain 31.9).
+// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 419 to 440 us (floor 98; plain 2170; 391 with B' in its own exponents and
+// rows of P by what they are before they fade, which loses small keys and what stands beside large faded ones; looking for what is not finite in
+// what a chunk adds costs 2 to 4 % of these (169, 268, 236, 429 without it);
+// four prompts of 61 tokens 8.0 us (plain 31.9).
 #pragma once
 #include <cuda.h>
 
@@ -209,11 +210,11 @@ template <typename T> struct Factor {
     using Pair = typename Two<T>::Pair;
     Pair f0, f1, f2, lift[2];
     bool lifts = false;                        // (of a whole warp)
-    // for a row whose largest element is `most`, in a chunk that is brought up by `up`
-    __device__ Factor(float f, float most, float up) : Factor(most > 0.f ? f * up * (most < 1.f ? 0x1p-12f : 1.f) * (most < 0x1p-12f ? 0x1p-12f : 1.f) : 0.f) {
-        lift[0] = Two<T>::twice(most < 1.f ? 4096.f : 1.f);
-        lift[1] = Two<T>::twice(most < 0x1p-12f ? 4096.f : 1.f);
-        lifts = __any_sync(~0u, most < 1.f);
+    // for a row whose largest element is `most`, in a chunk that is brought up by `up`: f up most is 2^15 at most
+    __device__ Factor(float f, float most, float up) : Factor(most > 0.f ? f * up * (f * up >= 0x1p15f ? 0x1p-12f : 1.f) * (f * up >= 0x1p27f ? 0x1p-12f : 1.f) : 0.f) {
+        lift[0] = Two<T>::twice(f * up >= 0x1p15f ? 4096.f : 1.f);
+        lift[1] = Two<T>::twice(f * up >= 0x1p27f ? 4096.f : 1.f);
+        lifts = __any_sync(~0u, most > 0.f && f * up >= 0x1p15f);
     }
     __device__ explicit Factor(float f) {
         f0 = Two<T>::twice(f);
@@ -255,16 +256,17 @@ __device__ __noinline__ float finite_most(const uint8_t* b, int r, int from, int
 }
 template <typename T>
 __device__ __forceinline__ float row_most(const uint8_t* b, int r, int from, int end) {
-    typename Two<T>::Pair most[2] = {Two<T>::twice(0.f), Two<T>::twice(0.f)};
+    uint32_t most[2] = {};                     // (signs do not count)
 #pragma unroll 4
     for (int i = from; i < end; ++i) {
         const uint4 q = *reinterpret_cast<const uint4*>(b + (i >> 3) * kHalf + ((i & 7) ^ (r & 7)) * 16);
         const uint32_t* x = &q.x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most[e & 1] = __hmax2_nan(most[e & 1], __habs2(*reinterpret_cast<const typename Two<T>::Pair*>(x + e)));
+        for (int e = 0; e < 4; ++e) asm("max.NaN.xorsign.abs.f16x2 %0, %0, %1;" : "+r"(most[e & 1]) : "r"(x[e]));
     }
-    most[0] = __hmax2_nan(most[0], most[1]);
-    const float m = __low2float(most[0]), other = __high2float(most[0]);
+    asm("max.NaN.xorsign.abs.f16x2 %0, %0, %1;" : "+r"(most[0]) : "r"(most[1]));
+    most[0] &= 0x7fff7fff;
+    const float m = __low2float(*reinterpret_cast<__half2*>(most)), other = __high2float(*reinterpret_cast<__half2*>(most));
     return m < INFINITY && other < INFINITY ? fmaxf(m, other) : INFINITY;
 }
 
@@ -534,22 +536,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         bars->tops[tops & 1][which * 4 + (r >> 5)] = top;
                         bar_arrive(&bars->t);
                     }
+                    ok = warp_wait(&bars->t, tops & 1, dead);
+                    if (!ok) break;
+                    uint32_t all = 0;
+#pragma unroll
+                    for (int i = 0; i < (kStates ? 8 : 4); ++i) all = max(all, ((volatile uint32_t*)bars->tops[tops & 1])[i]);
+                    if (all) up = to_middle(__uint_as_float(all), down);
+                    ++tops;
                 }
+                const Factor<T> f = kHalfs ? Factor<T>(fade, most, up) : Factor<T>(fade);
                 // the parts' places: B's is free when S is done, lo's when the D before is, the image's when I is (or where there is none, that D)
                 ok = (g == 0 || warp_wait(&bars->d, (g - 1) & 1, dead)) && (kStates || (warp_wait(&bars->s[g & 1], g >> 1 & 1, dead) && (!three || warp_wait(&bars->i[g & 1], g >> 1 & 1, dead))));
                 if (!ok) break;
-                if (kHalfs && c < adding) {
-                    ok = warp_wait(&bars->t, tops & 1, dead);
-                    if (!ok) break;
-                    uint32_t top = 0;
-#pragma unroll
-                    for (int i = 0; i < (kStates ? 8 : 4); ++i) top = max(top, ((volatile uint32_t*)bars->tops[tops & 1])[i]);
-                    if (top) up = to_middle(__uint_as_float(top), down);
-                    if (which == 0 && r == 0) bars->down[g & 1] = from_middle(down);       // (the one two chunks ago has been used: D has, since)
-                    ++tops;
-                }
                 if (c < adding) {
-                    const Factor<T> f = kHalfs ? Factor<T>(fade, most, up) : Factor<T>(fade);
+                    if (kHalfs && which == 0 && r == 0) bars->down[g & 1] = from_middle(down);         // (the one two chunks ago has been used: D has, since)
                     typename Two<T>::Pair zero = Two<T>::twice(0.f);       // 0 times all of lo, which is no number where the element is not finite
                     // pieces of 8 elements, a few at a time: a piece is a load, a dozen dependent steps and two or three stores
                     auto all = [&](auto how) {
@@ -802,8 +802,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 float p[32], on = 1.f;
                 if (kHalfs) {
                     // The row's largest product, faded; where 15 tokens fade to no less than 2^-18, a bound of it within that: the largest of 16 tokens times
-                    // the factor of the nearest, which leaves the largest at 2^-4 and the last bit at 2^-20 of it.
+                    // the factor of the nearest, which leaves the largest at 2^-4 and the last bit at 2^-20 of it; where all of a chunk's do, the largest.
                     float most = 0.f;
+                    const bool even = rate > -18.f / 127;
                     if (rate < -18.f / 15) most = faded_most(S + mine, at_shared(pw + (rev ? kTile : 0) + r), first, end, r, n, rev);
                     else
 #pragma unroll 1
@@ -815,13 +816,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll
                             for (int e = 0; e < 32; ++e) p[e] = seen >> e & 1 ? p[e] : 0.f;
                         }
+                        float low = 0.f, high = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 16) {
-                            float largest = 0.f;
-#pragma unroll
-                            for (int e = i; e < i + 16; ++e) largest = fmaxf(largest, fabsf(p[e]));
-                            most = fmaxf(most, largest * pw[rev ? kTile - max(32 * j + i - r, 0) : max(r - 32 * j - i - 15, 0)]);
+                        for (int e = 0; e < 16; ++e) { low = fmaxf(low, fabsf(p[e])); high = fmaxf(high, fabsf(p[e + 16])); }
+                        if (!even) {
+                            low *= pw[rev ? kTile - max(32 * j - r, 0) : max(r - 32 * j - 15, 0)];
+                            high *= pw[rev ? kTile - max(32 * j + 16 - r, 0) : max(r - 32 * j - 31, 0)];
                         }
+                        most = fmaxf(most, fmaxf(low, high));
                     }
                     uint8_t back;
                     on = to_middle(most, back);
