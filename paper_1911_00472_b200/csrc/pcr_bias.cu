@@ -158,11 +158,11 @@ BackForm back_form(const pcr_bias_args& a) {
         const int64_t beside = (int64_t)((a.axes + f.ax - 1) / f.ax) * f.slices * ((f.combos + 8 * f.nt - 1) / (8 * f.nt)), room = 3 * sm_count();
         f.width = kBackCols;
         auto blocks = [&] { return (a.k_tokens + f.width - 1) / f.width; };
-        while (f.width > 128 && beside * blocks() * ((f.rows + 31) / 32) < room) f.width /= 2;
+        while (f.width > 128 && beside * blocks() * (((int64_t)f.rows + 31) / 32) < room) f.width /= 2;
         f.col_blocks = (int)blocks();
         const int64_t want = std::max<int64_t>(1, room / std::max<int64_t>(1, beside * f.col_blocks));
         f.each = (int)std::max<int64_t>(8, (f.rows + want - 1) / want);
-        f.row_slabs = std::max(1, (f.rows + f.each - 1) / f.each);
+        f.row_slabs = (int)std::max<int64_t>(1, ((int64_t)f.rows + f.each - 1) / f.each);
         f.slabs = f.row_slabs * std::max(1, f.col_blocks) * f.batches;
         return f;
     }

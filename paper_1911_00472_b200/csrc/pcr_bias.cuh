@@ -425,9 +425,11 @@ __global__ void __launch_bounds__(256, kAx * kTiles * kNt <= (sizeof(T) == 2 ? 8
                     for (int e = 0; e < 4; ++e) { total[x][t][m][e] += acc[x][t][m][e]; if (kParts == 1) acc[x][t][m][e] = 0.f; }
     };
     int held = -1;                                                         // the batch whose columns' positions are in shared memory
-    const int from = slab * G.each, to = min(from + G.each, G.rows);
-    for (int line = from; line < to;) {
-        const int batch = line / A.nq, until = min(to, (batch + 1) * A.nq);       // rows of one batch
+    // (rows are fewer than 2^31, but what lies behind a share or a warp's last row may be more)
+    const uint32_t from = (uint32_t)slab * G.each, to = min(from + G.each, (uint32_t)G.rows);
+    for (uint32_t line = from; line < to;) {
+        const int batch = (int)(line / A.nq);
+        const uint32_t until = min(to, (uint32_t)(batch + 1) * A.nq);              // rows of one batch
         if (batch != held) {
             __syncthreads();
             for (int i = tid; i < kBackCols; i += 256) {
@@ -438,8 +440,8 @@ __global__ void __launch_bounds__(256, kAx * kTiles * kNt <= (sizeof(T) == 2 ? 8
             held = batch;
             __syncthreads();
         }
-        for (int l = line + warp; l < until; l += 8) {
-            const int row = l - batch * A.nq;
+        for (uint32_t l = line + warp; l < until; l += 8) {
+            const int row = (int)(l - (uint32_t)batch * A.nq);
             int q[kAx];
 #pragma unroll
             for (int x = 0; x < kAx; ++x) q[x] = axis0 + x < A.axes ? A.q_pos[(axis0 + x) * A.qs[0] + batch * A.qs[1] + (int64_t)row * A.qs[2]] : 0;

@@ -221,3 +221,14 @@ def test_positions_of_packed_images_and_captured():
     z = P.relative_bias(table, bucket_of, pos, q_ids=ids, stream=side)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(z, y)
+
+
+def test_gradient_of_nearly_as_many_rows_as_31_bits_hold():
+    """Shares of the rows whose ends lie beyond 31 bits: no row is left out.  Operands whose strides are 0 stand for 2 147 483 646 rows of a column; all
+    sums are whole numbers below 2^24 up to the slabs' in 64 bits."""
+    rows = 715827882
+    grad = torch.ones(1, 1, 1, 1, device=DEV, dtype=torch.bfloat16).expand(3, 4, rows, 1)
+    q = torch.zeros(1, 1, 1, dtype=torch.int32, device=DEV).expand(1, 3, rows)
+    k = torch.zeros(1, 3, 1, dtype=torch.int32, device=DEV)
+    got = P.relative_bias_backward(grad, 2, torch.tensor([0, 1, 0], dtype=torch.int32, device=DEV), q, k)
+    assert not got[0, 0].any() and (got[0, 1] == 3.0 * rows).all()
