@@ -393,7 +393,7 @@ typedef struct {
     int64_t k_id_stride[2];
     void* bias;                    /* DEVICE, of dtype; element (b, h, i, j) at b, h, i times the strides, + j; backward: its gradient, which is read */
     int64_t bias_stride[3];
-    int64_t batch, q_tokens, k_tokens;  /* batch at most 65535, tokens 2^30                                      */
+    int64_t batch, q_tokens, k_tokens;  /* batch at most 65535, tokens 2^30, their product 2^48                  */
     int32_t heads, axes, buckets, reach;  /* 1..4096, 1..4, 1..512, 0..2^20                                      */
     int32_t dtype;                 /* of the bias */
     int32_t table_dtype;           /* forward: dtype or PCR_F32; backward: any                                   */

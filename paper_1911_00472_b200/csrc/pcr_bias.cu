@@ -33,6 +33,7 @@ int check(const pcr_bias_args& a, bool back) {
     if (!is_dtype(a.dtype) || !is_dtype(a.table_dtype) || (!back && a.table_dtype != a.dtype && a.table_dtype != PCR_F32)) return PCR_E_ARG;
     if (a.heads < 1 || a.heads > 4096 || a.axes < 1 || a.axes > kBiasAxes || a.buckets < 1 || a.buckets > kBiasBuckets || a.reach < 0 || a.reach > kBiasReach) return PCR_E_ARG;
     for (int64_t n : {a.batch, a.q_tokens, a.k_tokens}) if (n < 0 || n > 1 << 30) return PCR_E_ARG;
+    if ((__int128)a.batch * a.q_tokens * a.k_tokens > (__int128)1 << 48) return PCR_E_ARG;
     if (a.batch > 65535 || (a.q_ids == nullptr) != (a.k_ids == nullptr)) return PCR_E_ARG;
     if (!a.table || !aligned(a.table, size_of(a.table_dtype))) return PCR_E_ARG;
     if (pairs(a) == 0) return PCR_OK;
@@ -147,8 +148,7 @@ BackForm back_form(const pcr_bias_args& a) {
     f.batches = shared ? (int)a.batch : 1;
     f.combos = f.batches * a.heads;
     f.rows = (int)((shared ? 1 : a.batch) * a.q_tokens);
-    f.products = f.combos >= 4 && 2 * a.reach + 1 <= kBackMap && (shared ? 1 : a.batch) * a.q_tokens <= INT32_MAX;
-    if (f.products) {
+    if (f.combos >= 4 && 2 * a.reach + 1 <= kBackMap && (shared ? 1 : a.batch) * a.q_tokens <= INT32_MAX) {
         // axes of a CTA: what is read serves them all, as long as their sums stay in registers
         f.kt = a.buckets <= 16 ? 1 : a.buckets <= 32 ? 2 : 4;
         f.ax = f.kt == 4 ? 1 : a.axes == 3 ? 3 : std::min(a.axes, 2);
@@ -163,15 +163,18 @@ BackForm back_form(const pcr_bias_args& a) {
         const int64_t want = std::max<int64_t>(1, room / std::max<int64_t>(1, beside * f.col_blocks));
         f.each = (int)std::max<int64_t>(8, (f.rows + want - 1) / want);
         f.row_slabs = (int)std::max<int64_t>(1, ((int64_t)f.rows + f.each - 1) / f.each);
-        f.slabs = f.row_slabs * std::max(1, f.col_blocks) * f.batches;
-        return f;
+        // (slabs and CTAs are numbered in 31 bits: gradients that many batches share by strides of 0 may have more)
+        const int64_t slabs = (int64_t)f.row_slabs * std::max(1, f.col_blocks) * f.batches;
+        f.products = slabs <= INT32_MAX / 2 && (__int128)f.row_slabs * f.col_blocks * beside <= INT32_MAX;
+        f.slabs = (int)slabs;
+        if (f.products) return f;
     }
     const int v = 16 / (int)size_of(a.dtype);
     f.tiles = (int)((a.k_tokens + 32 * v - 1) / (32 * v));
     f.slice = std::min(a.axes * a.buckets, 96);           // 4 warps, 128 bytes a bucket: 48 KB
     f.slices = (a.axes * a.buckets + f.slice - 1) / f.slice;
     const int64_t units = a.batch * a.q_tokens * f.tiles, want = std::max<int64_t>(1, sm_count() * 8 / a.heads);
-    f.per = (int)std::max<int64_t>(4, (units + want - 1) / want);
+    f.per = (int)std::min<int64_t>(INT32_MAX, std::max<int64_t>(4, (units + want - 1) / want));
     f.slabs = (int)std::max<int64_t>(1, (units + f.per - 1) / f.per);
     return f;
 }

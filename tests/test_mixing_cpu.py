@@ -206,6 +206,28 @@ def test_bias_outputs_and_scratch():
     assert L.pcr_relative_bias(None, None) == E and L.pcr_relative_bias_backward(None, None, None) == E
 
 
+@pytest.mark.parametrize("batch,q_tokens,k_tokens,heads", [(32768, 1, 1 << 27, 4), (65535, 1, 1 << 30, 4), (65535, 1, 1 << 30, 4096), (32768, 1, 1 << 25, 64), (40000, 3, 1 << 26, 4)])
+def test_bias_gradients_of_many_batches_that_share_all(batch, q_tokens, k_tokens, heads):
+    """Strides of 0 stand for any number of batches: the scratch memory holds a sum for every one of the slabs, however many there are."""
+    a = bias_args()
+    a.batch, a.q_tokens, a.k_tokens, a.heads = batch, q_tokens, k_tokens, heads
+    a.table = 1 << 60
+    for s in (a.q_stride, a.k_stride):
+        s[0], s[1], s[2] = 0, 0, 0
+    a.bias_stride[0] = a.bias_stride[1] = a.bias_stride[2] = 0
+    one = a.axes * a.buckets * heads * 4
+    got = B.lib().pcr_relative_bias_scratch_bytes(bytes(a))
+    assert got % one == 0 and 1 <= got // one < 1 << 31
+
+
+def test_bias_of_more_pairs_than_are_counted():
+    a = bias_args()
+    a.batch, a.q_tokens, a.k_tokens = 16, 1 << 30, 1 << 30        # 2^64 of them: 0 in 64 bits
+    raw = bytes(a)
+    L = B.lib()
+    assert L.pcr_relative_bias(raw, None) == E and L.pcr_relative_bias_scratch_bytes(raw) == 0 and L.pcr_relative_bias_backward(raw, FAR + 8 * (1 << 32), None) == E
+
+
 # ---- the Python calls ------------------------------------------------------------------------------------------------------------
 
 
