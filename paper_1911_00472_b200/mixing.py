@@ -271,12 +271,15 @@ def relative_bias(table, buckets, q_positions, k_positions=None, *, q_ids=None, 
     buckets      (2 * reach + 1,) int32: the bucket of every distance -reach .. reach (relative_buckets makes them); those beyond are
                  taken as the ends; a bucket that the table does not have counts as 0
     positions    (axes, tokens) or (axes, batch, tokens) int32, any strides; k_positions None: the same as q_positions
-    ids          int32, of an axis's shape: pairs whose ids differ are minus infinity (packed sequences); k_ids None: as q_ids
+    ids          int32, of an axis's shape: pairs whose ids differ are minus infinity (packed sequences); k_ids None: as q_ids, for as
+                 many tokens
     dtype        of the bias: the table's (default), or any where the table is float32
     Returns (heads, rows, columns) or (batch, heads, rows, columns); out: where they go, a row's elements side by side
     """
     if k_positions is None:
-        k_positions, k_ids = q_positions, q_ids if k_ids is None else k_ids
+        k_positions = q_positions
+    if k_ids is None and k_positions.shape == q_positions.shape:
+        k_ids = q_ids
     axes, batch, nq, nk = _bias_shapes(buckets, q_positions, k_positions, q_ids, k_ids)
     dtype = dtype or table.dtype
     if table.dim() != 3 or table.shape[0] != axes or table.dtype not in _CODES or not table.is_contiguous():
@@ -306,7 +309,9 @@ def relative_bias_backward(grad, n_buckets, buckets, q_positions, k_positions=No
            side is it copied first.  Positions and ids without a batch stand for all batches
     """
     if k_positions is None:
-        k_positions, k_ids = q_positions, q_ids if k_ids is None else k_ids
+        k_positions = q_positions
+    if k_ids is None and k_positions.shape == q_positions.shape:
+        k_ids = q_ids
     axes, batch, nq, nk = _bias_shapes(buckets, q_positions, k_positions, q_ids, k_ids)
     if grad.dim() not in (3, 4) or grad.dtype not in _CODES or grad.shape[-2:] != (nq, nk) or (batch is not None and (grad.dim() == 3 or grad.shape[0] != batch)):
         raise ValueError("grad must be (heads, rows, columns) or (batch, heads, rows, columns) of the positions, float16, bfloat16 or float32")

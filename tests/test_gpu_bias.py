@@ -232,3 +232,11 @@ def test_gradient_of_nearly_as_many_rows_as_31_bits_hold():
     k = torch.zeros(1, 3, 1, dtype=torch.int32, device=DEV)
     got = P.relative_bias_backward(grad, 2, torch.tensor([0, 1, 0], dtype=torch.int32, device=DEV), q, k)
     assert not got[0, 0].any() and (got[0, 1] == 3.0 * rows).all()
+
+
+def test_columns_of_positions_of_their_own_take_the_ids_of_the_rows():
+    table, bucket_of, q, k, ids, _, _ = make((2, 60, 60, 4, 2, 32, 20), torch.float32, packed=True)
+    bias = P.relative_bias(table, bucket_of, q, k, q_ids=ids)
+    assert torch.equal(bias, P.relative_bias(table, bucket_of, q, k, q_ids=ids, k_ids=ids)) and bias.isinf().any()
+    grad = torch.randn_like(bias)
+    assert torch.equal(P.relative_bias_backward(grad, 32, bucket_of, q, k, q_ids=ids), P.relative_bias_backward(grad, 32, bucket_of, q, k, q_ids=ids, k_ids=ids))

@@ -287,6 +287,16 @@ def test_bias_call_refusals(change, match):
         P.relative_bias(**bias(**change))
 
 
+def test_ids_of_the_columns_are_those_of_the_rows():
+    """Where there are as many tokens, also of positions of their own (the next thing that is looked at is the device)."""
+    a = bias(k_positions=torch.ones(2, 5, dtype=torch.int32), q_ids=torch.zeros(5, dtype=torch.int32))
+    with pytest.raises(ValueError, match="CUDA device"):
+        P.relative_bias(**a)
+    del a["table"]
+    with pytest.raises(ValueError, match="CUDA device"):
+        P.relative_bias_backward(torch.zeros(4, 5, 5), 16, **a)
+
+
 def test_bias_gradient_call_refusals():
     a = bias()
     del a["table"]
