@@ -27,12 +27,11 @@
 // memory's sum, its image and I, each waiting for the one before.  Rows of y are written by the lane that has them, 53 cycles a store; warps
 // of their own for y (257 us for the gradients below, 407 for the images) and y through shared memory (245, 413) were not faster.
 //
-// Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 176 us what segments add, 281 the walk (1.07 GB: 164 at the copy rate);
-// whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 241 us (floor 72; plain 5680).
-// 96 packed images of 729 tokens, 16 heads of 72 in fp16, 419 to 440 us (floor 98; plain 2170; 391 with B' in its own exponents and
-// rows of P by what they are before they fade, which loses small keys and what stands beside large faded ones; looking for what is not finite in
-// what a chunk adds costs 2 to 4 % of these (169, 268, 236, 429 without it);
-// four prompts of 61 tokens 8.0 us (plain 31.9).
+// Measured: 32768 tokens, 32 heads of 128, bf16, memories given and taken: 174 us what segments add, 277 the walk (1.07 GB: 164 at the copy rate);
+// whole sequences in the place of segments 1456, the plain kernel 8740.  Gradients of 4 x 4096 tokens, 16 heads of 128, 240 us (floor 72; plain 5680),
+// in fp16 302.  96 packed images of 729 tokens, 16 heads of 72 in fp16, 419 us (floor 98; plain 2170).  Four prompts of 61 tokens 8.0 us (plain 31.9).
+// Of these, exactness costs 2 % in bf16 (looking for what is not finite in what a chunk adds) and, in fp16, 26 us of the images (the largest product of
+// a chunk's B' and of a row of P as it is faded); products by twos (f32x2) took 20 of them back.
 #pragma once
 #include <cuda.h>
 
@@ -176,6 +175,14 @@ __device__ __forceinline__ void tensor_store16(uint32_t at, const uint32_t (&r)[
 }
 __device__ __forceinline__ void tensor_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tensor_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two products, or sums of products, by one instruction.
+__device__ __forceinline__ void mul2(float& a, float& b, float f, float g) {                      // a times f, b times g
+    asm("{\n.reg .b64 x, y;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %3};\nmul.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}" : "+f"(a), "+f"(b) : "f"(f), "f"(g));
+}
+__device__ __forceinline__ void fma2(float& a, float& b, float f, float c, float d) {              // a, b times f, plus c, d
+    asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %2};\nmov.b64 z, {%3, %4};\nfma.rn.f32x2 x, x, y, z;\nmov.b64 {%0, %1}, x;\n}" : "+f"(a), "+f"(b) : "f"(f), "f"(c), "f"(d));
+}
 
 // Pairs of 16-bit values in a word.
 template <typename T> struct Two;
@@ -840,14 +847,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int e = 0; e < 32; ++e) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[e]) : "r"(f - 4 * e));       // (asm: a load that depends on a bit of `seen` waits for the one before)
                         tensor_load_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) p[e] *= x[e];
+                        for (int e = 0; e < 32; e += 2) mul2(p[e], p[e + 1], x[e], x[e + 1]);
+                        if (kHalfs)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) mul2(p[e], p[e + 1], on, on);
                         if (j == warp || 32 * j + 32 > n) {
                             const uint32_t seen = seen_of(j);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) p[e] = seen >> e & 1 ? p[e] : 0.f;
                         }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = kHalfs ? Two<T>::pack(on * p[2 * e], on * p[2 * e + 1]) : Two<T>::pack(p[2 * e], p[2 * e + 1]);
+                        for (int e = 0; e < 16; ++e) y[e] = Two<T>::pack(p[2 * e], p[2 * e + 1]);
                     }
                     tensor_store16(S + mine + 16 * j, y);
                 }
@@ -878,10 +888,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                         for (int j = 0; j < 32; j += 16) {
                             const uint4 up = *reinterpret_cast<const uint4*>(cs + ph * 128 + j0 + j);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) { x[j + e] *= back; m[j + e] *= from_middle((&up.x)[e / 4] >> 8 * (e % 4) & 255); }
+                            for (int e = 0; e < 16; e += 2) {
+                                mul2(x[j + e], x[j + e + 1], back, back);
+                                mul2(m[j + e], m[j + e + 1], from_middle((&up.x)[e / 4] >> 8 * (e % 4) & 255), from_middle((&up.x)[e / 4] >> 8 * (e % 4 + 1) & 255));
+                            }
                         }
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] += age * m[j];
+                    for (int j = 0; j < 32; j += 2) {
+                        fma2(m[j], m[j + 1], age, x[j], x[j + 1]);
+                        x[j] = m[j]; x[j + 1] = m[j + 1];
+                    }
                     if (y32) {
                         float4* y = reinterpret_cast<float4*>(static_cast<float*>(W.y) + to + j0);
 #pragma unroll
@@ -987,7 +1003,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                             tensor_load_wait();
                         }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) R[i + e] = keep * R[i + e] + down * (i ? x[e] : ahead[e]);
+                        for (int e = 0; e < 16; e += 2) {
+                            float (&d)[16] = i ? x : ahead;
+                            mul2(d[e], d[e + 1], down, down);
+                            fma2(R[i + e], R[i + e + 1], keep, d[e], d[e + 1]);
+                        }
                     }
                 if (kHalfs && shows) {
                     float most = 0.f;
@@ -1011,8 +1031,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll
                         for (int e = 0; e < 16; e += 8) {
                             uint4 x;
-                            x.x = Two<T>::pack(up * R[i + e], up * R[i + e + 1]); x.y = Two<T>::pack(up * R[i + e + 2], up * R[i + e + 3]);
-                            x.z = Two<T>::pack(up * R[i + e + 4], up * R[i + e + 5]); x.w = Two<T>::pack(up * R[i + e + 6], up * R[i + e + 7]);
+                            float m[8];
+#pragma unroll
+                            for (int u = 0; u < 8; u += 2) {
+                                m[u] = R[i + e + u]; m[u + 1] = R[i + e + u + 1];
+                                if (kHalfs) mul2(m[u], m[u + 1], up, up);
+                            }
+                            x.x = Two<T>::pack(m[0], m[1]); x.y = Two<T>::pack(m[2], m[3]); x.z = Two<T>::pack(m[4], m[5]); x.w = Two<T>::pack(m[6], m[7]);
                             *reinterpret_cast<uint4*>(image + (i >> 6) * kHalf + r * 128 + ((((i + e) >> 3) & 7) ^ (r & 7)) * 16) = x;
                         }
                 }
