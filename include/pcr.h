@@ -350,11 +350,19 @@ typedef struct {
 #define PCR_DECAY_ZERO_TAIL 1
 
 /* The whole of every sequence, forward, and its gradients (nothing is kept from the forward pass).  Sums and memories in single
- * precision, one rounding to dtype.
+ * precision, outputs rounded once to dtype.
+ * 16-bit rows go through the tensor cores where heads have up to 128 elements, in multiples of 8, and rows begin at 16 bytes with strides that
+ * are positive multiples of 8 elements.  Their operands are of dtype, so that on the way there
+ *   - a token's products with those before it (q . k; backward: dout . v, v . dout, k . q), faded, and the memory before every 128
+ *     tokens are rounded to dtype (fp16: products not below 2^-21 of the token's largest),
+ *   - what goes into a memory is kept to 2^-16 of itself in bf16, to 2^-24 in calls that give a memory out, to 2^-21 in fp16 (there not
+ *     below 2^-31 of the largest among 128 tokens).
+ * The same values in another layout may differ by these roundings.  Factors below the range of single precision count as 0.
  *   scratch : DEVICE, pcr_decay_scratch_bytes(args, backward) bytes (for the same args on the same device), 16-byte aligned,
  *             apart from all operands and outputs.
  * Outputs share no memory with operands, tables or one another: else PCR_E_ARG.  The same call gives the same bits.
- * A token that is not finite reaches the outputs of the tokens behind it (backward: and the gradients before it) in its sequence, no others.
+ * A token that is not finite reaches the outputs of the tokens behind it (backward: and the gradients before it) in its sequence, no others; an
+ * infinite element of a key or value is an infinity in the memory, as long as its factor is not 0.
  * Waits within a kernel end after two seconds; segments in which one did (none is known to) become NaN, memories and all behind them too.
  * Errors: PCR_E_ARG, PCR_E_CUDA. */
 size_t pcr_decay_scratch_bytes(const pcr_decay_args* args, int backward);

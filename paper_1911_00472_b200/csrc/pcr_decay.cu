@@ -69,7 +69,7 @@ bool nothing(const pcr_decay_args& a) { return a.sequences == 0 && !(a.starts &&
 Form form_of(const pcr_decay_args& a, bool back) {
     Form f = {};
     const int most = std::max(a.k_dim, a.v_dim);
-    // (on the tensor cores wherever operands allow it: four prompts of 61 tokens 7.8 us for 31.9, 32768 tokens 458 for 8760)
+    // (on the tensor cores wherever operands allow it: four prompts of 61 tokens 8.0 us for 31.9, 32768 tokens 465 for 8760)
     f.tiles = a.sequences > 0 && tiles_fit(a, back);
     f.chunk = f.tiles ? 128 : most > 128 ? 32 : 64;
     // two parts of bf16 hold 16 bits of a value, which an output of 16 bits does not show; a memory that is given out would
@@ -77,7 +77,8 @@ Form form_of(const pcr_decay_args& a, bool back) {
     // Segments of equal length, as many of a sequence as end first by this count, in halves of a chunk's time: rounds of CTAs times their
     // chunks and a CTA's beginning and end (a chunk; two where chunks are short, on the tensor cores), and for several segments half as much again
     // and two more launches (a chunk of the plain kernel takes 14 us, one on the tensor cores 3.5).  Packed sequences are taken to be of
-    // equal length.
+    // equal length.  (Two CTAs an SM of the plain kernel: heads of 104 to 128 and of 200 and more ask for 113 KB of shared memory and more each, so
+    // that one fits, and their rounds are too few here; not measured.)
     const int64_t wide = (int64_t)a.q_heads * (back ? 3 : 1) * (f.tiles ? 1 : (most + kWalkCols - 1) / kWalkCols) * a.sequences;
     const int64_t room = (int64_t)sm_count() * (f.tiles ? 1 : 2), mean = std::max<int64_t>(1, a.batch * a.tokens / std::max<int64_t>(1, a.sequences)), whole = (mean + f.chunk - 1) / f.chunk;
     int64_t best = 1, least = INT64_MAX;

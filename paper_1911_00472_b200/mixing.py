@@ -3,7 +3,8 @@ head's own, and a learned bias of the distance between two tokens.
 
 torch is used for memory and streams only; all arithmetic happens behind the C ABI (include/pcr.h: pcr_decay_attention,
 pcr_decay_attention_backward, pcr_decay_step, pcr_relative_bias, pcr_relative_bias_backward).  Nothing is kept between calls and
-nothing waits, so every call may be captured into a graph.  Gradients are calls of their own: operands that autograd follows are
+nothing waits, so every call may be captured into a graph; relative_buckets apart, which makes a map on the host and copies it, once for a
+model.  Gradients are calls of their own: operands that autograd follows are
 refused, not silently cut off.
 
 Work goes to `stream` (default: torch's current stream of the operands' device); what a call allocates belongs to it.
@@ -124,6 +125,9 @@ def decay_attention(q, k, v, log_decay, *, starts=None, state=None, final=False,
     state      (sequences, heads, key size, value size) float32: memories to begin with
     final      whether the memories behind the last tokens are wanted, or where they go
     out        where the outputs go: rows of no sequence stay as they are there; without it they are 0
+
+    Memories are in single precision.  16-bit operands go through the tensor cores where their layout allows it, and some products
+    on the way are rounded to their type then (include/pcr.h says which): the same values in another layout may differ by that.
     """
     batch, tokens, n, hq, hk, kd, vd = _decay_shapes(q, k, v, log_decay, starts, (3, 4))
     memories = (n, hq, kd, vd)
@@ -218,7 +222,7 @@ def decay_step(q, k, v, log_decay, state, *, slots=None, out=None, stream=None):
 
 def relative_buckets(buckets, reach, *, one_sided=False, device="cuda:0"):
     """Bucket (2 * reach + 1,) int32 of every distance -reach .. reach: single distances up to half of a side's buckets, then
-    distances that grow by a factor, up to `reach`, from which on all share the last one.
+    distances that grow by a factor, up to `reach`, from which on all share the last one.  Made on the host: not for a capture.
 
     one_sided   keys that come later than their query share bucket 0, all buckets are for earlier ones; otherwise the first half
                 is for earlier keys and the query itself, the second for later ones
