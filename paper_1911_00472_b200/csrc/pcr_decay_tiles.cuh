@@ -202,7 +202,7 @@ template <> struct Two<__half> {
 };
 // 2^14 / a power of two about as large as `most`; the exponent of what takes it off again
 __device__ __forceinline__ float to_middle(float most, uint8_t& back) {
-    const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 250);
+    const int e = min(max((int)(__float_as_uint(most) >> 23 & 255), 15), 254);
     back = (uint8_t)(e - 14);
     return __uint_as_float((uint32_t)(127 + 14 + 127 - e) << 23);
 }

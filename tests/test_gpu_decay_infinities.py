@@ -94,3 +94,18 @@ def test_infinite_memories_to_begin_with(dtype):
     assert (out[:, 0, 7] == float("inf")).all() and (out[:, 1, 11] == -float("inf")).all()
     out[:, 0, 7] = out[:, 1, 11] = 0
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [64, 128])
+def test_memories_near_the_end_of_single_precision(size, dtype):
+    """Memories of 2^125 are numbers: a query of zeros reads 0 from them, a small one what is there (2^-24 2^125 is above fp16's range, in bf16 a number)."""
+    n = 200
+    q = torch.zeros(1, n, 2, size, device=DEV, dtype=dtype)
+    q[:, 150:, :, 3] = 2.0 ** -24
+    k = torch.zeros_like(q)
+    v = torch.ones_like(q)
+    first = torch.full((1, 2, size, size), 2.0 ** 125, device=DEV)
+    out, after = P.decay_attention(q, k, v, torch.zeros(2, device=DEV), state=first, final=True)
+    assert not out[:, :150].any() and torch.equal(after, first)
+    assert (out[:, 150:] == (float("inf") if dtype == torch.float16 else 2.0 ** 101)).all()
