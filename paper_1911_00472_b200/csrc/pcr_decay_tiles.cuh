@@ -68,7 +68,7 @@ struct Job { int kind, head, key, chunks, tail; float rate; Item it; };      // 
 struct Patience { int dead; uint32_t limit; };     // whether some wait of the CTA ran out; nanoseconds
 struct alignas(16) TileBars {
     uint32_t won[4];                           // the launch's answer
-    uint64_t full[6], empty[6], s[2], i[2], z, p, k, o, d, e, r, t, end, got[kQueue], taken[kQueue], answer;
+    uint64_t full[6], empty[6], s[2], i[2], z[2], p, k, o, d, e, r, t, end, got[kQueue], taken[kQueue], answer;
     Job jobs[kQueue], held;                    // held: one that was taken and could not be put among them
     uint32_t tops[2][8];                       // fp16: bits of the largest key times factor that a warp has, two chunks
     float down[2];                             // what takes D back to size
@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     if (tid == 0) {
         for (int s = 0; s < L::kPlaces; ++s) { bar_init(&bars->full[s], 1); bar_init(&bars->empty[s], 1); }
         for (uint64_t* b : {&bars->s[0], &bars->s[1], &bars->i[0], &bars->i[1], &bars->o, &bars->d, &bars->end, &bars->answer}) bar_init(b, 1);
-        for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z}) bar_init(b, 128);
+        for (uint64_t* b : {&bars->p, &bars->e, &bars->r, &bars->z[0], &bars->z[1]}) bar_init(b, 128);
         bar_init(&bars->k, kStates ? 256 : 128);
         bar_init(&bars->t, kStates ? 8 : 4);
         for (int s = 0; s < kQueue; ++s) { bar_init(&bars->got[s], 1); bar_init(&bars->taken[s], 14); }
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     // B' by the threads of a warpgroup, a token each; where two have a chunk, half of its elements.
     auto make_parts = [&](int r, int which) {
         uint8_t *image = sm + L::kImage + r * 128, *low = sm + L::kLow + r * 128;
-        uint32_t g = 0, tops = 0;                                          // (tops: chunks whose largest product was looked for)
+        uint32_t g = 0, tops = 0, tails = 0;                               // (tops: chunks whose largest product was looked for; tails: of fewer tokens)
         bool ok = true;
         while (ok && w.next()) {
             const int chunks = w.job->chunks;
@@ -527,7 +527,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
 #pragma unroll 1
                         for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(v + (i >> 3) * kHalf + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
                     order_shared();
-                    if (!kStates) bar_arrive(&bars->z);
+                    // (of two chunks in turn: the next one's rows may be cleared before the warp that issues products has looked for this one's)
+                    if (!kStates) bar_arrive(&bars->z[tails++ & 1]);
                 }
                 const float fade = c < adding && in ? power(rate, (rev ? r + 1 : n - r) - (!kStates && given && c + 1 == chunks && !rev ? 1 : 0)) : 0.f;
                 float most = 0.f, up = 1.f;
@@ -663,7 +664,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 __syncwarp();
             };
             bool ok = true, ahead = false;                                 // ahead: S has been issued
-            int more = advance(true), tails = 0;
+            int more = advance(true);
+            uint32_t tails = 0;
             while (ok && more > 0) {
                 const uint32_t g = w.g, ph = g & 1;
                 if (!kStates && !ahead) {                                  // (P lies where S goes, and has been read when O is done)
@@ -677,7 +679,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 ok = has(g, kC);
                 if (!kStates) {
                     // rows of C behind the last token have been cleared; P is there; O's and I's places have been read
-                    if (now.n < kTile) ok = ok && warp_wait(&bars->z, tails++ & 1, dead);
+                    if (now.n < kTile) { ok = ok && warp_wait(&bars->z[tails & 1], tails >> 1 & 1, dead); ++tails; }
                     ok = ok && warp_wait(&bars->p, ph, dead) && (g == 0 || warp_wait(&bars->e, ph ^ 1, dead));
                     if (!ok) break;
                     order_after();

@@ -99,3 +99,18 @@ def test_only_where_there_are_such_waits():
     q, k, v, _, _, log_decay, _, _ = make([64], 2, 2, 64, 64, torch.float32, packed=False)
     assert lost(0, (q, k, v, torch.empty_like(q), None, None, None), (log_decay, None), (None,) * 4, (1, 64, 1, 2, 2, 64, 64), torch.float32, 0) == B.PCR_E_ARG
     assert B.lib().pcr_selftest_decay_waits(None, 0, None, C.c_uint32(0), None) == B.PCR_E_ARG
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("size", [16, 40, 128])
+def test_short_sequences_one_behind_the_other(size, dtype):
+    """Segments of a chunk with rows to clear each, many to a CTA, as fast as they come: no wait runs out (after two seconds there would be NaN)."""
+    lengths = [127, 5, 61, 1, 127, 127, 2, 100, 13, 126, 90, 1, 127, 33, 120, 7] * 2
+    q, k, v, g, starts, log_decay, _, _ = make(lengths, 16, 16, size, size, dtype, seed=29)
+    want = (P.decay_attention(q, k, v, log_decay, starts=starts)[0], *P.decay_attention_backward(g, q, k, v, log_decay, starts=starts)[:3])
+    for x, y in zip(want, (P.decay_attention(q.float(), k.float(), v.float(), log_decay, starts=starts)[0],
+                           *P.decay_attention_backward(g.float(), q.float(), k.float(), v.float(), log_decay, starts=starts)[:3])):
+        assert float((x.float() - y).norm() / y.norm()) < torch.finfo(dtype).eps
+    for _ in range(150):
+        got = (P.decay_attention(q, k, v, log_decay, starts=starts)[0], *P.decay_attention_backward(g, q, k, v, log_decay, starts=starts)[:3])
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
